@@ -1,0 +1,404 @@
+// Host side of the operators on a routed batch (hwr_ops.h): validation, work
+// space and launches.
+#include <hip/hip_runtime.h>
+
+#include <cstring>
+#include <string>
+#include <vector>
+
+#include "c_boundary.hpp"
+#include "hwr_ops.h"
+#include "ops_internal.hpp"
+
+using namespace hwr;
+
+struct hwr_ops {
+    int dev = 0, cus = 0;
+    hipStream_t stream = nullptr;
+    void *zeros = nullptr;
+    // Work space: the last block is in use.  Blocks grow by powers of two and stay
+    // until hwr_ops_free: captured graphs hold their addresses.
+    std::vector<void *> blocks;
+    uint64_t size = 0;
+    std::string err;
+};
+
+namespace {
+
+thread_local std::string g_ops_error;
+
+constexpr int kMaxWidth = 65536;
+constexpr int kMaxRank = 128;
+constexpr uint64_t kZeroBytes = 256;
+
+hwr_status fail(hwr_ops *c, hwr_status s, const std::string &msg) {
+    (c ? c->err : g_ops_error) = msg;
+    return s;
+}
+hwr_status invalid(hwr_ops *c, const char *msg) { return fail(c, HWR_ERR_INVALID_ARG, msg); }
+
+hwr_status hip_fail(hwr_ops *c, hipError_t e, const char *what) {
+    std::string m = std::string(what) + ": " + hipGetErrorName(e) + " (" + hipGetErrorString(e) + ")";
+    return fail(c, e == hipErrorOutOfMemory ? HWR_ERR_OOM : HWR_ERR_HIP, m);
+}
+
+#define OPS_HIP(ctx, call)                                           \
+    do {                                                             \
+        hipError_t e_ = (call);                                      \
+        if (e_ != hipSuccess) return hip_fail((ctx), e_, #call);     \
+    } while (0)
+
+void release(hwr_ops *c) {
+    for (void *p : c->blocks) (void)hipFree(p);
+    if (c->zeros) (void)hipFree(c->zeros);
+    delete c;
+}
+
+hwr_status use_device(hwr_ops *c) {
+    int dev = -1;
+    OPS_HIP(c, hipGetDevice(&dev));
+    if (dev != c->dev) OPS_HIP(c, hipSetDevice(c->dev));
+    return HWR_OK;
+}
+
+// At least `bytes` of work space at *out.
+hwr_status workspace(hwr_ops *c, uint64_t bytes, char **out) {
+    if (bytes > c->size) {
+        hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+        if (c->stream) OPS_HIP(c, hipStreamIsCapturing(c->stream, &cap));
+        if (cap != hipStreamCaptureStatusNone)
+            return fail(c, HWR_ERR_STATE, "this call needs more work space than the context has, and its stream is being "
+                        "captured: hwr_ops_reserve " + std::to_string(bytes) + " bytes before");
+        uint64_t size = c->size ? c->size : uint64_t(1) << 20;
+        while (size < bytes) size *= 2;
+        c->blocks.reserve(c->blocks.size() + 1);
+        void *p = nullptr;
+        hipError_t e = hipMalloc(&p, size);
+        if (e == hipErrorOutOfMemory && size > bytes) {
+            (void)hipGetLastError();
+            size = bytes;
+            e = hipMalloc(&p, size);
+        }
+        if (e != hipSuccess) {
+            (void)hipGetLastError();
+            return hip_fail(c, e, "work space");
+        }
+        c->blocks.push_back(p);
+        c->size = size;
+    }
+    *out = c->blocks.empty() ? nullptr : static_cast<char *>(c->blocks.back());
+    return HWR_OK;
+}
+
+hwr_status init_impl(int32_t device, void *stream, hwr_ops **out) {
+    if (!out) return invalid(nullptr, "out is NULL");
+    *out = nullptr;
+    int ndev = 0;
+    hipError_t e = hipGetDeviceCount(&ndev);
+    if (e != hipSuccess || ndev < 1) return fail(nullptr, HWR_ERR_HIP, "no HIP device available");
+    if (device < 0 || device >= ndev) return invalid(nullptr, "device ordinal out of range");
+    hipDeviceProp_t prop;
+    if (hipGetDeviceProperties(&prop, device) != hipSuccess)
+        return fail(nullptr, HWR_ERR_HIP, "hipGetDeviceProperties failed");
+    if (std::strncmp(prop.gcnArchName, "gfx950", 6) != 0)
+        return fail(nullptr, HWR_ERR_UNSUPPORTED, std::string("library is built for gfx950, device is ") + prop.gcnArchName);
+    OPS_HIP(nullptr, hipSetDevice(device));
+    hwr_ops *c = new hwr_ops();
+    c->dev = device;
+    c->cus = prop.multiProcessorCount;
+    c->stream = static_cast<hipStream_t>(stream);
+    e = hipMalloc(&c->zeros, kZeroBytes);
+    if (e == hipSuccess) e = hipMemset(c->zeros, 0, kZeroBytes);
+    if (e == hipSuccess) e = hipDeviceSynchronize();
+    if (e != hipSuccess) {
+        release(c);
+        return hip_fail(nullptr, e, "context memory");
+    }
+    *out = c;
+    return HWR_OK;
+}
+
+// ---------------------------------------------------------------- checks
+struct Shape {
+    int32_t dtype, k, m;
+};
+
+// Null when sound, else what is wrong.
+const char *check_groups(const hwr_groups *g) {
+    if (!g) return "groups is NULL";
+    if (g->n < 0) return "n < 0";
+    if (g->n_groups < 1 || g->n_groups > kMaxPairs) return "n_groups outside 1..1024";
+    if (!g->offsets) return "offsets is NULL";
+    return nullptr;
+}
+const char *check_shape(int32_t dtype, int32_t k, int32_t m) {
+    if (dtype != HWR_F32 && dtype != HWR_BF16) return "unknown dtype";
+    if (k < 1 || k > kMaxWidth || m < 1 || m > kMaxWidth) return "k or m outside 1..65536";
+    return nullptr;
+}
+const char *check_rank(int32_t rank) { return rank < 1 || rank > kMaxRank ? "rank outside 1..128" : nullptr; }
+bool bad_ld(int64_t ld, int32_t width) { return ld != 0 && ld < width; }
+int64_t dense(int64_t ld, int32_t width) { return ld ? ld : width; }
+bool misaligned(int32_t dtype, std::initializer_list<const void *> ptrs) {
+    for (const void *p : ptrs)
+        if (reinterpret_cast<uintptr_t>(p) & (dtype == HWR_BF16 ? 1 : 3)) return true;
+    return false;
+}
+
+GroupsArg groups_arg(const hwr_groups *g) { return {g->n, g->n_groups, g->offsets, g->order}; }
+
+int rank_blocks(int rank) { return (rank + kRankBlock - 1) / kRankBlock; }
+uint64_t low_bytes(int n, int rank) { return static_cast<uint64_t>(n) * rank_blocks(rank) * kLowBytes; }
+
+// low[place] = scale[g] x[row] w_g
+hwr_status shrink(hwr_ops *c, const hwr_groups *g, int32_t dtype, bool ks, const void *x, int64_t ldx, int k, const void *w,
+                  int rank, const float *scale, void *low) {
+    RowsArgs r{};
+    r.g = groups_arg(g);
+    r.k = k;
+    r.m = rank;
+    r.x = x;
+    r.ldx = ldx;
+    r.w = w;
+    r.w_stride = static_cast<int64_t>(k) * rank;
+    r.y = low;
+    r.scale = scale;
+    r.zeros = c->zeros;
+    OPS_HIP(c, launch_rows(dtype == HWR_BF16, RowsKind::kShrink, ks, r, c->cus, c->stream));
+    return HWR_OK;
+}
+
+// y[row] = x[row] w + low[place] lw_g
+hwr_status expand(hwr_ops *c, const hwr_groups *g, int32_t dtype, bool ks, const void *x, int64_t ldx, int k, const void *w,
+                  int m, const void *low, const void *lw, int rank, void *y, int64_t ldy) {
+    RowsArgs r{};
+    r.g = groups_arg(g);
+    r.k = k;
+    r.m = m;
+    r.x = x;
+    r.ldx = ldx;
+    r.w = w;
+    r.y = y;
+    r.ldy = ldy;
+    r.low = low;
+    r.lw = lw;
+    r.rank = rank;
+    r.zeros = c->zeros;
+    OPS_HIP(c, launch_rows(dtype == HWR_BF16, RowsKind::kAdapter, ks, r, c->cus, c->stream));
+    return HWR_OK;
+}
+
+// ---------------------------------------------------------------- operators
+hwr_status group_rows(hwr_ops *c, int32_t n, const int32_t *choice, const int32_t *table, int32_t n_table, int32_t n_groups,
+                      int32_t *offsets, int32_t *order) {
+    if (!c) return invalid(nullptr, "ops is NULL");
+    if (n < 0) return invalid(c, "n < 0");
+    if (n_groups < 1 || n_groups > kMaxPairs) return invalid(c, "n_groups outside 1..1024");
+    if (!offsets || (n > 0 && (!choice || !order))) return invalid(c, "choice, offsets and order are required");
+    if (table ? n_table < 1 : n_table != 0) return invalid(c, "n_table must be > 0 with a table and 0 without");
+    if (misaligned(HWR_F32, {choice, table, offsets, order})) return invalid(c, "a pointer is not aligned to its elements");
+    if (hwr_status st = use_device(c)) return st;
+    GroupRowsArgs a{n, n_table, n_groups, choice, table, offsets, order, nullptr, group_rows_blocks(n)};
+    char *ws = nullptr;
+    if (hwr_status st = workspace(c, static_cast<uint64_t>(n_groups + 1) * a.blocks * sizeof(int32_t), &ws)) return st;
+    a.hist = reinterpret_cast<int32_t *>(ws);
+    OPS_HIP(c, launch_group_rows(a, c->stream));
+    return HWR_OK;
+}
+
+hwr_status grouped_matmul(hwr_ops *c, const hwr_groups *g, const hwr_matmul_args *a) {
+    if (!c) return invalid(nullptr, "ops is NULL");
+    if (const char *m = check_groups(g)) return invalid(c, m);
+    if (!a) return invalid(c, "arguments are NULL");
+    if (const char *m = check_shape(a->dtype, a->k, a->m)) return invalid(c, m);
+    if (bad_ld(a->ldx, a->k) || bad_ld(a->ldy, a->m)) return invalid(c, "a row stride is smaller than the row");
+    if (g->n == 0) return HWR_OK;
+    if (!a->x || !a->w || !a->y) return invalid(c, "x, w and y are required");
+    if (misaligned(a->dtype, {a->x, a->w, a->y})) return invalid(c, "a pointer is not aligned to its elements");
+    if (hwr_status st = use_device(c)) return st;
+    RowsArgs r{};
+    r.g = groups_arg(g);
+    r.k = a->k;
+    r.m = a->m;
+    r.x = a->x;
+    r.ldx = dense(a->ldx, a->k);
+    r.w = a->w;
+    r.w_stride = static_cast<int64_t>(a->k) * a->m;
+    r.y = a->y;
+    r.ldy = dense(a->ldy, a->m);
+    r.zeros = c->zeros;
+    OPS_HIP(c, launch_rows(a->dtype == HWR_BF16, RowsKind::kGrouped, true, r, c->cus, c->stream));
+    return HWR_OK;
+}
+
+hwr_status grouped_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_matmul_grad_args *a) {
+    if (!c) return invalid(nullptr, "ops is NULL");
+    if (const char *m = check_groups(g)) return invalid(c, m);
+    if (!a) return invalid(c, "arguments are NULL");
+    if (const char *m = check_shape(a->dtype, a->k, a->m)) return invalid(c, m);
+    if (bad_ld(a->lddy, a->m) || bad_ld(a->ldx, a->k) || bad_ld(a->lddx, a->k))
+        return invalid(c, "a row stride is smaller than the row");
+    if (g->n > 0 && (!a->dy || (a->dx && !a->w) || (a->dw && !a->x)))
+        return invalid(c, "dy is required, w for dx, and x for dw");
+    if (misaligned(a->dtype, {a->dy, a->x, a->w, a->dx, a->dw})) return invalid(c, "a pointer is not aligned to its elements");
+    if (hwr_status st = use_device(c)) return st;
+    const bool bf16 = a->dtype == HWR_BF16;
+    if (a->dx && g->n > 0) {
+        RowsArgs r{};
+        r.g = groups_arg(g);
+        r.k = a->m;
+        r.m = a->k;
+        r.x = a->dy;
+        r.ldx = dense(a->lddy, a->m);
+        r.w = a->w;
+        r.w_stride = static_cast<int64_t>(a->k) * a->m;
+        r.y = a->dx;
+        r.ldy = dense(a->lddx, a->k);
+        r.zeros = c->zeros;
+        OPS_HIP(c, launch_rows(bf16, RowsKind::kGrouped, false, r, c->cus, c->stream));
+    }
+    if (a->dw) {
+        ColsArgs w{};
+        w.g = groups_arg(g);
+        w.np = a->k;
+        w.nq = a->m;
+        w.p = a->x;
+        w.q = a->dy;
+        w.ldp = dense(a->ldx, a->k);
+        w.ldq = dense(a->lddy, a->m);
+        w.out = a->dw;
+        w.zeros = c->zeros;
+        OPS_HIP(c, launch_cols(bf16, ColsKind::kDense, w, c->cus, c->stream));
+    }
+    return HWR_OK;
+}
+
+hwr_status adapter_matmul(hwr_ops *c, const hwr_groups *g, const hwr_adapter_args *a) {
+    if (!c) return invalid(nullptr, "ops is NULL");
+    if (const char *m = check_groups(g)) return invalid(c, m);
+    if (!a) return invalid(c, "arguments are NULL");
+    if (const char *m = check_shape(a->dtype, a->k, a->m)) return invalid(c, m);
+    if (const char *m = check_rank(a->rank)) return invalid(c, m);
+    if (bad_ld(a->ldx, a->k) || bad_ld(a->ldy, a->m)) return invalid(c, "a row stride is smaller than the row");
+    if (g->n == 0) return HWR_OK;
+    if (!a->x || !a->w || !a->a || !a->b || !a->y) return invalid(c, "x, w, a, b and y are required");
+    if (misaligned(a->dtype, {a->x, a->w, a->a, a->b, a->y}) || misaligned(HWR_F32, {a->scale}))
+        return invalid(c, "a pointer is not aligned to its elements");
+    if (hwr_status st = use_device(c)) return st;
+    char *low = nullptr;
+    if (hwr_status st = workspace(c, low_bytes(g->n, a->rank), &low)) return st;
+    const int64_t ldx = dense(a->ldx, a->k);
+    if (hwr_status st = shrink(c, g, a->dtype, true, a->x, ldx, a->k, a->a, a->rank, a->scale, low)) return st;
+    return expand(c, g, a->dtype, true, a->x, ldx, a->k, a->w, a->m, low, a->b, a->rank, a->y, dense(a->ldy, a->m));
+}
+
+hwr_status adapter_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_adapter_grad_args *a) {
+    if (!c) return invalid(nullptr, "ops is NULL");
+    if (const char *m = check_groups(g)) return invalid(c, m);
+    if (!a) return invalid(c, "arguments are NULL");
+    if (const char *m = check_shape(a->dtype, a->k, a->m)) return invalid(c, m);
+    if (const char *m = check_rank(a->rank)) return invalid(c, m);
+    if (bad_ld(a->lddy, a->m) || bad_ld(a->ldx, a->k) || bad_ld(a->lddx, a->k))
+        return invalid(c, "a row stride is smaller than the row");
+    if (g->n > 0 && (!a->dy || ((a->dx || a->da) && !a->b) || (a->dx && (!a->w || !a->a)) || (a->da && !a->x) ||
+                     (a->db && (!a->x || !a->a))))
+        return invalid(c, "dy is required; w, a and b for dx; x and b for da; x and a for db");
+    if (misaligned(a->dtype, {a->dy, a->x, a->w, a->a, a->b, a->dx, a->da, a->db}) || misaligned(HWR_F32, {a->scale}))
+        return invalid(c, "a pointer is not aligned to its elements");
+    if (hwr_status st = use_device(c)) return st;
+    const bool bf16 = a->dtype == HWR_BF16;
+    const int64_t lddy = dense(a->lddy, a->m), ldx = dense(a->ldx, a->k);
+    const uint64_t each = low_bytes(g->n, a->rank);
+    char *ws = nullptr;
+    if (hwr_status st = workspace(c, 2 * each, &ws)) return st;
+    char *up = ws, *low = ws + each;
+    if (g->n > 0 && (a->dx || a->da))
+        if (hwr_status st = shrink(c, g, a->dtype, false, a->dy, lddy, a->m, a->b, a->rank, a->scale, up)) return st;
+    if (g->n > 0 && a->db)
+        if (hwr_status st = shrink(c, g, a->dtype, true, a->x, ldx, a->k, a->a, a->rank, a->scale, low)) return st;
+    if (g->n > 0 && a->dx)
+        if (hwr_status st = expand(c, g, a->dtype, false, a->dy, lddy, a->m, a->w, a->k, up, a->a, a->rank, a->dx,
+                                   dense(a->lddx, a->k)))
+            return st;
+    ColsArgs w{};
+    w.g = groups_arg(g);
+    w.blocks = rank_blocks(a->rank);
+    w.zeros = c->zeros;
+    if (a->da) {
+        w.np = a->k;
+        w.nq = a->rank;
+        w.p = a->x;
+        w.ldp = ldx;
+        w.q = up;
+        w.out = a->da;
+        OPS_HIP(c, launch_cols(bf16, ColsKind::kLowQ, w, c->cus, c->stream));
+    }
+    if (a->db) {
+        w.np = a->rank;
+        w.nq = a->m;
+        w.p = low;
+        w.q = a->dy;
+        w.ldq = lddy;
+        w.out = a->db;
+        OPS_HIP(c, launch_cols(bf16, ColsKind::kLowP, w, c->cus, c->stream));
+    }
+    return HWR_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+hwr_status hwr_ops_init(int32_t device, void *stream, hwr_ops **out) {
+    return c_boundary([&] { return init_impl(device, stream, out); }, [](const char *m) { fail(nullptr, HWR_ERR_OOM, m); });
+}
+
+void hwr_ops_free(hwr_ops *ops) {
+    if (!ops) return;
+    c_boundary(
+        [&] {
+            (void)hipSetDevice(ops->dev);
+            (void)hipStreamSynchronize(ops->stream);
+            release(ops);
+            return HWR_OK;
+        },
+        [](const char *) {});
+}
+
+const char *hwr_ops_last_error(const hwr_ops *ops) { return ops ? ops->err.c_str() : g_ops_error.c_str(); }
+
+hwr_status hwr_ops_reserve(hwr_ops *ops, uint64_t bytes) {
+    return c_boundary(
+        [&]() -> hwr_status {
+            if (!ops) return invalid(nullptr, "ops is NULL");
+            if (bytes > uint64_t(1) << 40) return invalid(ops, "bytes above 1 TiB");
+            if (hwr_status st = use_device(ops)) return st;
+            char *p;
+            return workspace(ops, bytes, &p);
+        },
+        [&](const char *m) { fail(ops, HWR_ERR_OOM, m); });
+}
+
+hwr_status hwr_group_rows(hwr_ops *ops, int32_t n, const int32_t *choice, const int32_t *table, int32_t n_table,
+                          int32_t n_groups, int32_t *offsets, int32_t *order) {
+    return c_boundary([&] { return group_rows(ops, n, choice, table, n_table, n_groups, offsets, order); },
+                      [&](const char *m) { fail(ops, HWR_ERR_OOM, m); });
+}
+
+hwr_status hwr_grouped_matmul(hwr_ops *ops, const hwr_groups *g, const hwr_matmul_args *a) {
+    return c_boundary([&] { return grouped_matmul(ops, g, a); }, [&](const char *m) { fail(ops, HWR_ERR_OOM, m); });
+}
+
+hwr_status hwr_grouped_matmul_grad(hwr_ops *ops, const hwr_groups *g, const hwr_matmul_grad_args *a) {
+    return c_boundary([&] { return grouped_matmul_grad(ops, g, a); }, [&](const char *m) { fail(ops, HWR_ERR_OOM, m); });
+}
+
+hwr_status hwr_adapter_matmul(hwr_ops *ops, const hwr_groups *g, const hwr_adapter_args *a) {
+    return c_boundary([&] { return adapter_matmul(ops, g, a); }, [&](const char *m) { fail(ops, HWR_ERR_OOM, m); });
+}
+
+hwr_status hwr_adapter_matmul_grad(hwr_ops *ops, const hwr_groups *g, const hwr_adapter_grad_args *a) {
+    return c_boundary([&] { return adapter_matmul_grad(ops, g, a); }, [&](const char *m) { fail(ops, HWR_ERR_OOM, m); });
+}
+
+}  // extern "C"

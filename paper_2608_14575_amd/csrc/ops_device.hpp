@@ -1,0 +1,216 @@
+// Device code shared by the operators on a routed batch: element types and
+// their matrix instruction, staged tiles and their LDS layout, and the walk
+// over ragged groups.
+//
+// All products run on 16x16 MFMA with the weights (or the right-hand factor) as
+// the A operand and the rows as the B operand, so that a lane ends up with four
+// neighbouring output columns of one row: D[i] of lane l is column 4 (l / 16) + i,
+// row l % 16.  An operand fragment is 16 bytes a lane: lane l holds, for its
+// column or row l % 16, the contraction elements of its quarter l / 16.
+#pragma once
+
+#include "ops_internal.hpp"
+
+namespace hwr {
+
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+// 16 bytes at any element alignment
+typedef uint32_t u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+
+template <class E>
+struct Elem;
+
+template <>
+struct Elem<__bf16> {
+    using Frag = bf16x8;
+    using Vec = u32x4_a2;
+    using Out4 = bf16x4;
+    static constexpr int kBk = 64;    // contraction elements of a stage
+    static constexpr int kEpc = 8;    // elements of a 16-byte chunk
+    static __device__ f32x4 mma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+
+template <>
+struct Elem<float> {
+    using Frag = f32x4;
+    using Vec = u32x4_a4;
+    using Out4 = f32x4;
+    static constexpr int kBk = 32;
+    static constexpr int kEpc = 4;
+    static __device__ f32x4 mma(Frag a, Frag b, f32x4 c) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+        return c;
+    }
+};
+
+constexpr int kStageBytes = 128;      // contraction bytes of a stage, in either tile layout
+
+// ---------------------------------------------------------------- staged tiles
+// A tile is stored in 16-byte chunks.  KC: line i is row (or column) i, 8
+// chunks of contraction elements.  KS: line e is contraction element e, with
+// the chunks of neighbouring columns.  Chunks are permuted within a line so
+// that the fragment reads below spread over all banks: chunk c of line i is
+// stored at c ^ swz(i).
+template <class E, bool KS, int N>
+struct Tile {
+    static constexpr int kLines = KS ? Elem<E>::kBk : N;
+    static constexpr int kCpl = KS ? N * (int)sizeof(E) / 16 : 8;   // chunks of a line
+    static constexpr int kChunks = N * 8;
+    static constexpr int kBytes = kChunks * 16;
+    static __device__ int swz(int line) {
+        if constexpr (!KS) return (line >> 1) & 7;
+        else if constexpr (sizeof(E) == 4) return (((line >> 2) & 3) << 2) & (kCpl - 1);
+        else if constexpr (kCpl >= 16) return ((line & 3) | ((line >> 3) & 1) << 2) << 1;
+        else if constexpr (kCpl == 8) return (((line >> 1) & 1) | ((line >> 3) & 1) << 1) << 1;
+        else if constexpr (kCpl == 4) return ((line >> 3) & 1) << 1;
+        else return 0;
+    }
+    // Fragment of the 16 rows (columns) from c0 on, contraction half `sub` of the stage.
+    static __device__ typename Elem<E>::Frag frag(const char *t, int c0, int sub, int lane) {
+        const int m = lane & 15, q = lane >> 4;
+        if constexpr (!KS) {
+            const int line = c0 + m;
+            return *reinterpret_cast<const typename Elem<E>::Frag *>(t + line * 128 + (((sub * 4 + q) ^ swz(line)) << 4));
+        } else if constexpr (sizeof(E) == 4) {
+            f32x4 v;
+            const int c = c0 + m;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int line = sub * 16 + q * 4 + i;
+                v[i] = *reinterpret_cast<const float *>(t + line * (kCpl * 16) + (((c >> 2) ^ swz(line)) << 4) + (c & 3) * 4);
+            }
+            return v;
+        } else {
+            // the transposing read: 16 lanes fetch 4 lines x 16 columns, lane m gets column m
+            typedef __attribute__((address_space(3))) i16x4 lds_v;
+            const int c = c0 + (m & 3) * 4;
+            union { i16x4 h[2]; bf16x8 f; } u;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int line = sub * 32 + q * 8 + i * 4 + (m >> 2);
+                u.h[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (lds_v *)(t + line * (kCpl * 16) + (((c >> 3) ^ swz(line)) << 4) + (c & 4) * 2));
+            }
+            return u.f;
+        }
+    }
+};
+
+// Elements [e, e + kEpc) of a line that has `len` elements, zeros past it; any
+// element alignment.
+template <class E>
+__device__ inline u32x4 load_chunk(const E *line, int e, int len) {
+    constexpr int kEpc = Elem<E>::kEpc;
+    if (line == nullptr || e >= len) return u32x4{0, 0, 0, 0};
+    if (e + kEpc <= len) {
+        const typename Elem<E>::Vec v = *reinterpret_cast<const typename Elem<E>::Vec *>(line + e);
+        return u32x4{v[0], v[1], v[2], v[3]};
+    }
+    union { u32x4 v; E s[kEpc]; } u;
+    u.v = u32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < kEpc; ++i)
+        if (e + i < len) u.s[i] = line[e + i];
+    return u.v;
+}
+
+// ---------------------------------------------------------------- groups
+// offsets as places: clamped to [0, n], so that whatever the array holds stays in bounds
+__device__ inline int place_of(const GroupsArg &g, int i) {
+    const int v = g.offsets[i];
+    return v < 0 ? 0 : v > g.n ? g.n : v;
+}
+
+// Row at place p, or -1.
+__device__ inline int row_at(const GroupsArg &g, int p) {
+    const int r = g.order ? g.order[p] : p;
+    return static_cast<unsigned>(r) < static_cast<unsigned>(g.n) ? r : -1;
+}
+
+// Rows of a tile: places [p0, p1) of group g (g == G: the rows in no group).
+struct RowTile {
+    int g, p0, p1;
+};
+
+// Every group is cut into tiles of bm places.  The tiles of lane i's groups in
+// a block of 64 groups; group G are the rows in no group.
+__device__ inline int lane_tiles(const GroupsArg &g, int i, int bm, bool tail, int &p0, int &p1) {
+    p0 = p1 = 0;
+    if (i < g.G) {
+        p0 = place_of(g, i);
+        p1 = place_of(g, i + 1);
+    } else if (i == g.G && tail) {
+        p0 = place_of(g, i);
+        p1 = g.n;
+    }
+    return p1 > p0 ? (p1 - p0 + bm - 1) / bm : 0;
+}
+
+__device__ inline int wave_scan(int v, int lane) {   // inclusive
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(v, d);
+        if (lane >= d) v += o;
+    }
+    return v;
+}
+
+// Tiles of all groups; one wave.
+__device__ inline int count_tiles(const GroupsArg &g, int bm, bool tail, int lane) {
+    int sum = 0, p0, p1;
+    for (int b = 0; b <= g.G; b += 64) sum += lane_tiles(g, b + lane, bm, tail, p0, p1);
+#pragma unroll
+    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+    return __builtin_amdgcn_readfirstlane(sum);
+}
+
+// Tile t of all groups (t < count_tiles); one wave.
+__device__ inline RowTile find_tile(const GroupsArg &g, int t, int bm, bool tail, int lane) {
+    for (int b = 0; b <= g.G; b += 64) {
+        int p0, p1;
+        const int mine = lane_tiles(g, b + lane, bm, tail, p0, p1);
+        const int upto = wave_scan(mine, lane);
+        const uint64_t hit = __ballot(upto > t);
+        if (hit) {
+            const int l = __builtin_ctzll(hit);
+            const int first = __builtin_amdgcn_readlane(upto - mine, l);
+            const int a = __builtin_amdgcn_readlane(p0, l) + (t - first) * bm, e = __builtin_amdgcn_readlane(p1, l);
+            return {b + l, a, a + bm < e ? a + bm : e};
+        }
+        t -= __builtin_amdgcn_readlane(upto, 63);
+    }
+    return {g.G, 0, 0};
+}
+
+// First group that ends past place p (G if none); one wave.
+__device__ inline int group_of(const GroupsArg &g, int p, int lane) {
+    for (int b = 0; b < g.G; b += 64) {
+        const uint64_t hit = __ballot(b + lane < g.G && place_of(g, b + lane + 1) > p);
+        if (hit) return b + __builtin_ctzll(hit);
+    }
+    return g.G;
+}
+
+// Workgroup id -> work item, so that the items of one of the 8 L2s (ids are
+// dealt out in turn) are neighbours.  Returns -1 past the last item.
+__device__ inline int xcd_item(int id, int items) {
+    const int share = (items + 7) >> 3;
+    const int at = id >> 3, i = (id & 7) * share + at;
+    return at < share && i < items ? i : -1;
+}
+
+template <int VM>
+__device__ inline void wait_vm() {    // at most VM vector-memory loads in flight
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (VM & 15) | (VM >> 4) << 14);
+}
+__device__ inline void wait_lds() { __builtin_amdgcn_s_waitcnt(0xC07F); }   // every LDS access done
+__device__ inline void barrier() {    // execution and LDS order; does not wait for loads in flight
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+}  // namespace hwr

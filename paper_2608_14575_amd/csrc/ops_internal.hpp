@@ -1,0 +1,67 @@
+// Arguments and launchers of the operators on a routed batch (hwr_ops.h).
+#pragma once
+
+#include "hwr_internal.hpp"
+
+namespace hwr {
+
+// Low-rank intermediates (s x A, u) are kept by place, in blocks of kRankBlock
+// columns of 128 bytes: fp32 values, or bf16 pairs hi[kRankBlock], lo[kRankBlock]
+// with hi + lo the value to 16 significant bits.
+constexpr int kRankBlock = 32;
+constexpr int kLowBytes = 128;
+
+struct GroupsArg {
+    int n, G;
+    const int32_t *offsets, *order;   // order may be null
+};
+
+// Products by row: out[r][c] = sum_e x[r][e] w_g(e, c), and for the adapter
+// plus sum_e low[place][e] lw_g(e, c).
+struct RowsArgs {
+    GroupsArg g;
+    int k, m;                     // contraction width (e), output width (c)
+    const void *x;
+    int64_t ldx;                  // elements
+    const void *w;                // KS: [k][m], else [m][k] (transposed use)
+    int64_t w_stride;             // elements between groups
+    void *y;
+    int64_t ldy;
+    const void *zeros;            // 256 zero bytes
+    // adapter
+    const void *low;              // [n][blocks] low-rank intermediates
+    const void *lw;               // [G][rank][m] (KS) or [G][m][rank]
+    int rank;
+    // shrink: y is the low-rank intermediate, scaled
+    const float *scale;           // [G] or null
+};
+
+// Weight gradients: out[g][p][q] = sum over places of g of P[place][p] Q[place][q].
+struct ColsArgs {
+    GroupsArg g;
+    int np, nq;                   // widths of P and Q as they stand in out
+    const void *p, *q;            // rows through order, or low-rank intermediates by place
+    int64_t ldp, ldq;             // elements
+    void *out;                    // [G][np][nq]
+    int blocks;                   // rank blocks (low-rank side)
+    const void *zeros;
+};
+
+struct GroupRowsArgs {
+    int n, n_table, G;
+    const int32_t *choice, *table;
+    int32_t *offsets, *order;
+    int32_t *hist;                // [G + 1][blocks] work space
+    int blocks;
+};
+
+enum class RowsKind { kGrouped, kAdapter, kShrink };
+
+hipError_t launch_group_rows(const GroupRowsArgs &a, hipStream_t s);
+int group_rows_blocks(int n);
+// ks: weights [k][m]; else [m][k]
+hipError_t launch_rows(bool bf16, RowsKind kind, bool ks, const RowsArgs &a, int cus, hipStream_t s);
+enum class ColsKind { kDense, kLowP, kLowQ };
+hipError_t launch_cols(bool bf16, ColsKind kind, const ColsArgs &a, int cus, hipStream_t s);
+
+}  // namespace hwr

@@ -33,7 +33,9 @@ EXPORTS = ["hwr_init", "hwr_update_hw_state", "hwr_route_batch", "hwr_route_batc
            "hwr_last_error",
            "hwr_profile_enable", "hwr_profile_read", "hwr_sim_run", "hwr_sim_last_error",
            "hwr_probe_mfma_bf16", "hwr_probe_hbm_read", "hwr_probe_hbm_write", "hwr_probe_launch_floor",
-           "hwr_probe_feature_log"]
+           "hwr_probe_feature_log",
+           "hwr_ops_init", "hwr_ops_free", "hwr_ops_last_error", "hwr_ops_reserve", "hwr_group_rows",
+           "hwr_grouped_matmul", "hwr_grouped_matmul_grad", "hwr_adapter_matmul", "hwr_adapter_matmul_grad"]
 
 _STATUS = {0: "HWR_OK", -1: "HWR_ERR_INVALID_ARG", -2: "HWR_ERR_OOM", -3: "HWR_ERR_HIP",
            -4: "HWR_ERR_STATE", -5: "HWR_ERR_UNSUPPORTED"}
@@ -118,6 +120,32 @@ class hwr_sim_result(C.Structure):
                 + [(k, C.c_double) for k in SIM_METRICS[5:]])
 
 
+# ---- include/hwr_ops.h
+class hwr_groups(C.Structure):
+    _fields_ = [("n", C.c_int32), ("n_groups", C.c_int32), ("offsets", _vp), ("order", _vp)]
+
+
+class hwr_matmul_args(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("k", C.c_int32), ("m", C.c_int32), ("x", _vp), ("ldx", C.c_int64), ("w", _vp),
+                ("y", _vp), ("ldy", C.c_int64)]
+
+
+class hwr_matmul_grad_args(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("k", C.c_int32), ("m", C.c_int32), ("dy", _vp), ("lddy", C.c_int64),
+                ("x", _vp), ("ldx", C.c_int64), ("w", _vp), ("dx", _vp), ("lddx", C.c_int64), ("dw", _vp)]
+
+
+class hwr_adapter_args(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("k", C.c_int32), ("m", C.c_int32), ("rank", C.c_int32), ("x", _vp),
+                ("ldx", C.c_int64), ("w", _vp), ("a", _vp), ("b", _vp), ("scale", _vp), ("y", _vp), ("ldy", C.c_int64)]
+
+
+class hwr_adapter_grad_args(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("k", C.c_int32), ("m", C.c_int32), ("rank", C.c_int32), ("dy", _vp),
+                ("lddy", C.c_int64), ("x", _vp), ("ldx", C.c_int64), ("w", _vp), ("a", _vp), ("b", _vp), ("scale", _vp),
+                ("dx", _vp), ("lddx", C.c_int64), ("da", _vp), ("db", _vp)]
+
+
 hwr_sim_router_fn = C.CFUNCTYPE(C.c_int32, C.c_void_p, C.POINTER(hwr_hw_state), C.c_int32, C.c_int32,
                                 C.c_int32, _i32p, _f32p, _f32p)
 STATE_DTYPE = np.dtype([("running_q", "<i4"), ("waiting_q", "<i4"), ("kv_util", "<f4"),
@@ -178,6 +206,20 @@ def load(path: Optional[str] = None) -> C.CDLL:
     L.hwr_probe_hbm_write.argtypes = [C.c_int32, _vp, C.c_uint64, C.c_int32, C.c_int32, C.POINTER(C.c_double)]
     L.hwr_probe_feature_log.restype = C.c_int
     L.hwr_probe_feature_log.argtypes = [C.c_int32, _vp, C.c_int64, _vp]
+    L.hwr_ops_init.restype = C.c_int
+    L.hwr_ops_init.argtypes = [C.c_int32, _vp, C.POINTER(_vp)]
+    L.hwr_ops_free.restype = None
+    L.hwr_ops_free.argtypes = [_vp]
+    L.hwr_ops_last_error.restype = C.c_char_p
+    L.hwr_ops_last_error.argtypes = [_vp]
+    L.hwr_ops_reserve.restype = C.c_int
+    L.hwr_ops_reserve.argtypes = [_vp, C.c_uint64]
+    L.hwr_group_rows.restype = C.c_int
+    L.hwr_group_rows.argtypes = [_vp, C.c_int32, _vp, _vp, C.c_int32, C.c_int32, _vp, _vp]
+    for fn, args in (("hwr_grouped_matmul", hwr_matmul_args), ("hwr_grouped_matmul_grad", hwr_matmul_grad_args),
+                     ("hwr_adapter_matmul", hwr_adapter_args), ("hwr_adapter_matmul_grad", hwr_adapter_grad_args)):
+        getattr(L, fn).restype = C.c_int
+        getattr(L, fn).argtypes = [_vp, C.POINTER(hwr_groups), C.POINTER(args)]
     if path is None:
         _lib = L
     return L
@@ -268,6 +310,51 @@ def hwr_profile_read(ctx, reset: bool = True) -> dict:
     t = hwr_kernel_times()
     _check(load().hwr_profile_read(ctx, C.byref(t), 1 if reset else 0), ctx)
     return {KERNEL_NAMES[k]: (t.ms[k], int(t.launches[k])) for k in range(HWR_K_COUNT)}
+
+
+# ---------------------------------------------------------------- operators on a routed batch
+def _check_ops(status: int, ops) -> None:
+    if status != HWR_OK:
+        raise HwrError(status, hwr_ops_last_error(ops))
+
+
+def hwr_ops_init(device: int, stream: int):
+    ops = _vp()
+    _check_ops(load().hwr_ops_init(device, stream, C.byref(ops)), None)
+    return ops
+
+
+def hwr_ops_free(ops) -> None:
+    load().hwr_ops_free(ops)
+
+
+def hwr_ops_last_error(ops) -> str:
+    m = load().hwr_ops_last_error(ops)
+    return m.decode() if m else ""
+
+
+def hwr_ops_reserve(ops, nbytes: int) -> None:
+    _check_ops(load().hwr_ops_reserve(ops, nbytes), ops)
+
+
+def hwr_group_rows(ops, n: int, choice: int, table: int, n_table: int, n_groups: int, offsets: int, order: int) -> None:
+    _check_ops(load().hwr_group_rows(ops, n, choice, table, n_table, n_groups, offsets, order), ops)
+
+
+def hwr_grouped_matmul(ops, groups: hwr_groups, args: hwr_matmul_args) -> None:
+    _check_ops(load().hwr_grouped_matmul(ops, C.byref(groups), C.byref(args)), ops)
+
+
+def hwr_grouped_matmul_grad(ops, groups: hwr_groups, args: hwr_matmul_grad_args) -> None:
+    _check_ops(load().hwr_grouped_matmul_grad(ops, C.byref(groups), C.byref(args)), ops)
+
+
+def hwr_adapter_matmul(ops, groups: hwr_groups, args: hwr_adapter_args) -> None:
+    _check_ops(load().hwr_adapter_matmul(ops, C.byref(groups), C.byref(args)), ops)
+
+
+def hwr_adapter_matmul_grad(ops, groups: hwr_groups, args: hwr_adapter_grad_args) -> None:
+    _check_ops(load().hwr_adapter_matmul_grad(ops, C.byref(groups), C.byref(args)), ops)
 
 
 # ---------------------------------------------------------------- convenience

@@ -1,0 +1,541 @@
+"""The operators on a routed batch (include/hwr_ops.h) against plain 64-bit
+implementations: row grouping, grouped products and adapters with their
+gradients, in bf16 and fp32, at ragged, odd, empty, strided and single-row
+sizes; what masked places and other groups hold; refusals; other streams and
+graphs.
+
+Tolerances, element by element.  A product of width K accumulated in fp32 is
+off by at most (K + 16) 2^-24 S, S the sum of the terms' magnitudes (taken in 64
+bits); its rounding to bf16 by 2^-8 of the value, to fp32 by 2^-24.  A low-rank
+intermediate has that error too, carried through the second product, and in
+bf16 calls one of 2^-16 of its value for being the sum of two bf16 numbers."""
+import numpy as np
+import pytest
+
+from paper_2608_14575_amd import hwr, routed
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+TYPES = {"bf16": (torch.bfloat16, 2.0 ** -8, 2.0 ** -16), "f32": (torch.float32, 2.0 ** -24, 0.0)}
+EPS = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def ops():
+    assert torch.cuda.is_available(), "GPU tests need a device"
+    o = routed.RoutedOps(stream=torch.cuda.current_stream().cuda_stream)
+    yield o
+    o.close()
+
+
+def sizes_of(kind, n, G, rng):
+    """Group of every row, -1 for none."""
+    if kind == "even":
+        g = np.arange(n) % G
+    elif kind == "one":           # all rows in one group, the others empty
+        g = np.full(n, G // 2)
+    elif kind == "none":
+        g = np.full(n, -1)
+    else:                         # skewed, some in no group
+        p = 1.0 / (1 + np.arange(G)) ** 1.2
+        g = rng.choice(G, n, p=p / p.sum())
+        g[rng.random(n) < 0.15] = -1
+    return rng.permutation(g).astype(np.int64)
+
+
+def grouped(gid, G, ordered=False):
+    """(gid, offsets, order) on the device; with `ordered` the rows are already in group order."""
+    key = np.where(gid < 0, G, gid)
+    if ordered:
+        key = np.sort(key, kind="stable")
+        gid = np.where(key == G, -1, key)
+    order = np.argsort(key, kind="stable")
+    offsets = np.searchsorted(key[order], np.arange(G + 1))
+    dev = lambda a: torch.from_numpy(a.astype(np.int32)).cuda()  # noqa: E731
+    return gid, dev(offsets), None if ordered else dev(order)
+
+
+def rand(gen, *shape, dtype, std=1.0):
+    return (torch.randn(shape, generator=gen, device="cuda") * std).to(dtype)
+
+
+def strided(t, pad):
+    """The same rows in a wider buffer."""
+    if not pad:
+        return t
+    buf = torch.full((t.shape[0], t.shape[1] + pad), float("nan"), dtype=t.dtype, device="cuda")
+    buf[:, :t.shape[1]] = t
+    return buf[:, :t.shape[1]]
+
+
+def close(got, ref, tol):
+    assert not torch.isnan(got).any()
+    bad = (got.double() - ref).abs() > tol
+    assert not bad.any(), f"{int(bad.sum())} of {bad.numel()} off, worst {((got.double() - ref).abs() / tol.clamp(min=1e-300)).max():.3g} of the tolerance"
+
+
+def product(x, w, gid):
+    """sum_e x[r][e] w[g(r)][e][c] in 64 bits, and the same of magnitudes."""
+    y = torch.zeros(x.shape[0], w.shape[2], dtype=torch.float64, device="cuda")
+    s = torch.zeros_like(y)
+    for g in range(w.shape[0]):
+        r = torch.from_numpy(np.nonzero(gid == g)[0]).cuda()
+        if r.numel():
+            xd, wd = x[r].double(), w[g].double()
+            y[r], s[r] = xd @ wd, xd.abs() @ wd.abs()
+    return y, s
+
+
+def outer(p, q, gid, G):
+    """sum over rows of a group of p[r]^T q[r], and the same of magnitudes, and rows of the group."""
+    o = torch.zeros(G, p.shape[1], q.shape[1], dtype=torch.float64, device="cuda")
+    s = torch.zeros_like(o)
+    for g in range(G):
+        r = torch.from_numpy(np.nonzero(gid == g)[0]).cuda()
+        if r.numel():
+            a, b = p[r].double().t(), q[r].double()
+            o[g], s[g] = a @ b, a.abs() @ b.abs()
+    n = torch.tensor([max(1, int((gid == g).sum())) for g in range(G)], device="cuda")[:, None, None]
+    return o, s, n
+
+
+# ---------------------------------------------------------------- rows by group
+@pytest.mark.parametrize("n", [0, 1, 63, 64, 65, 1000, 4095, 4096, 4097, 8191, 100003])
+@pytest.mark.parametrize("G,P", [(1, 0), (2, 0), (16, 32), (1000, 0), (1024, 1024), (31, 97)])
+def test_group(ops, n, G, P):
+    rng = np.random.default_rng(n * 7 + G)
+    hi = P or G
+    choice = rng.integers(-2, hi + 2, n).astype(np.int32)
+    if n > 3:
+        choice[:3] = [np.iinfo(np.int32).max, np.iinfo(np.int32).min, -1]
+    table = rng.integers(-1, G + 1, P).astype(np.int32) if P else None
+    key = np.where((choice >= 0) & (choice < hi), choice, -1)
+    if P:
+        key = np.where(key >= 0, table[np.maximum(key, 0)], -1)
+    key = np.where((key >= 0) & (key < G), key, G)
+    order = torch.full((n,), -7, dtype=torch.int32, device="cuda")
+    offsets = torch.full((G + 1,), -7, dtype=torch.int32, device="cuda")
+    ops.group(torch.from_numpy(choice).cuda(), G, offsets=offsets, order=order,
+              table=None if table is None else torch.from_numpy(table).cuda())
+    want = np.argsort(key, kind="stable")
+    assert np.array_equal(order.cpu().numpy(), want)
+    assert np.array_equal(offsets.cpu().numpy(), np.searchsorted(key[want], np.arange(G + 1)))
+
+
+# ---------------------------------------------------------------- grouped products
+SHAPES = [
+    # n, G, k, m, groups, already ordered, stride padding
+    (1, 1, 1, 1, "even", False, 0),
+    (1, 5, 64, 48, "one", False, 0),
+    (3, 4, 7, 5, "even", True, 1),
+    (17, 3, 33, 130, "skew", False, 3),
+    (40, 16, 256, 200, "skew", False, 0),
+    (64, 70, 72, 64, "skew", False, 8),
+    (65, 2, 65, 66, "even", False, 0),
+    (130, 1, 200, 260, "even", True, 0),
+    (300, 3, 128, 128, "none", False, 0),
+    (513, 4, 520, 264, "skew", False, 8),
+    (777, 6, 384, 385, "one", False, 0),
+    (1500, 5, 136, 1032, "skew", True, 16),
+    (2049, 1000, 24, 40, "skew", False, 0),
+    (4100, 2, 1024, 512, "skew", False, 0),
+    (3000, 3, 96, 96, "even", False, 5),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,G,k,m,kind,ordered,pad", SHAPES)
+def test_matmul_and_gradients(ops, n, G, k, m, kind, ordered, pad, dtype):
+    t, u, _ = TYPES[dtype]
+    gen = torch.Generator("cuda").manual_seed(n + k)
+    gid, off, order = grouped(sizes_of(kind, n, G, np.random.default_rng(n)), G, ordered)
+    x, dy = strided(rand(gen, n, k, dtype=t), pad), strided(rand(gen, n, m, dtype=t), pad)
+    w = rand(gen, G, k, m, dtype=t)
+    y = strided(torch.full((n, m), 7.0, dtype=t, device="cuda"), pad)
+    ops.matmul(x, w, off, order, y=y)
+    ref, s = product(x, w, gid)
+    close(y, ref, u * ref.abs() + (k + 16) * EPS * s)
+    dx = strided(torch.full((n, k), 7.0, dtype=t, device="cuda"), pad)
+    dw = torch.full((G, k, m), 7.0, dtype=t, device="cuda")
+    ops.matmul_grad(dy, x, w, off, order, dx=dx, dw=dw)
+    ref, s = product(dy, w.transpose(1, 2).contiguous(), gid)
+    close(dx, ref, u * ref.abs() + (m + 16) * EPS * s)
+    ref, s, cnt = outer(x, dy, gid, G)
+    close(dw, ref, u * ref.abs() + (cnt + 16) * EPS * s)
+    # either gradient alone, and the same bits again
+    dx2, dw2 = torch.zeros_like(dx), torch.zeros_like(dw)
+    ops.matmul_grad(dy, x, w, off, order, dx=dx2)
+    ops.matmul_grad(dy, x, w, off, order, dw=dw2)
+    assert torch.equal(dx2, dx) and torch.equal(dw2, dw)
+
+
+# ---------------------------------------------------------------- adapters
+ADAPTERS = [
+    # n, G, k, m, rank, groups, ordered, pad, scaled
+    (1, 1, 1, 1, 1, "even", False, 0, True),
+    (1, 32, 256, 512, 16, "one", False, 0, True),
+    (1, 3, 40, 72, 8, "none", False, 0, True),
+    (2, 2, 100, 36, 4, "even", True, 0, False),
+    (16, 40, 64, 200, 5, "skew", False, 1, True),
+    (48, 32, 512, 320, 16, "skew", False, 0, True),
+    (64, 64, 136, 264, 33, "even", False, 8, True),
+    (65, 7, 70, 131, 12, "skew", False, 0, True),
+    (200, 5, 384, 256, 64, "skew", False, 0, False),
+    (513, 4, 264, 520, 32, "skew", False, 8, True),
+    (1025, 3, 128, 390, 128, "even", True, 0, True),
+    (3000, 6, 768, 768, 8, "skew", False, 0, True),
+    (2600, 900, 32, 64, 16, "skew", False, 0, True),
+]
+
+
+
+def scaled(scale, gid):
+    """[n][1] scale of each row's group (0 in none)."""
+    g = torch.from_numpy(np.maximum(gid, 0)).cuda()
+    s = torch.ones(len(gid), dtype=torch.float64, device="cuda") if scale is None else scale.double()[g]
+    return torch.where(torch.from_numpy(gid >= 0).cuda(), s, 0.0)[:, None]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,G,k,m,R,kind,ordered,pad,with_scale", ADAPTERS)
+def test_adapter_and_gradients(ops, n, G, k, m, R, kind, ordered, pad, with_scale, dtype):
+    t, u, lo = TYPES[dtype]
+    gen = torch.Generator("cuda").manual_seed(n + k + R)
+    gid, off, order = grouped(sizes_of(kind, n, G, np.random.default_rng(n)), G, ordered)
+    x, dy = strided(rand(gen, n, k, dtype=t), pad), strided(rand(gen, n, m, dtype=t), pad)
+    w, a, b = rand(gen, k, m, dtype=t), rand(gen, G, k, R, dtype=t), rand(gen, G, R, m, dtype=t)
+    scale = (0.5 + torch.rand(G, generator=gen, device="cuda")) if with_scale else None
+    sc = scaled(scale, gid)
+    y = strided(torch.full((n, m), 7.0, dtype=t, device="cuda"), pad)
+    ops.adapter(x, w, a, b, scale, off, order, y=y)
+
+    xa, sxa = product(x, a, gid)
+    low, slow = xa * sc, sxa * sc
+    shared = np.zeros(n, np.int64)
+    main, smain = product(x, w[None], shared)
+    add, _ = product(low, b, gid)
+    tb, _ = product(low.abs(), b.abs(), gid)       # |low| |b|
+    sadd, _ = product(slow, b.abs(), gid)
+    close(y, main + add, u * (main + add).abs() + (k + R + 32) * EPS * (smain + sadd) + 2 * lo * tb)
+
+    dx = strided(torch.full((n, k), 7.0, dtype=t, device="cuda"), pad)
+    da, db = torch.full_like(a, 7.0), torch.full_like(b, 7.0)
+    ops.adapter_grad(dy, x, w, a, b, scale, off, order, dx=dx, da=da, db=db)
+    bt, at = b.transpose(1, 2).contiguous(), a.transpose(1, 2).contiguous()
+    up, sup = product(dy, bt, gid)
+    up, sup = up * sc, sup * sc
+    main, smain = product(dy, w.t().contiguous()[None], shared)
+    add, _ = product(up, at, gid)
+    ua, _ = product(up.abs(), at.abs(), gid)
+    sadd, _ = product(sup, at.abs(), gid)
+    close(dx, main + add, u * (main + add).abs() + (m + R + 32) * EPS * (smain + sadd) + 2 * lo * ua)
+    ref, _, cnt = outer(x, up, gid, G)
+    xu, _, _ = outer(x.abs(), up.abs(), gid, G)
+    xs, _, _ = outer(x.abs(), sup, gid, G)
+    close(da, ref, u * ref.abs() + (m + cnt + 32) * EPS * xs + 2 * lo * xu)
+    ref, _, _ = outer(low, dy, gid, G)
+    ld, _, _ = outer(low.abs(), dy.abs(), gid, G)
+    ls, _, _ = outer(slow, dy.abs(), gid, G)
+    close(db, ref, u * ref.abs() + (k + cnt + 32) * EPS * ls + 2 * lo * ld)
+    # each gradient alone, and the same bits again
+    for name, v in (("dx", dx), ("da", da), ("db", db)):
+        alone = torch.zeros_like(v)
+        ops.adapter_grad(dy, x, w, a, b, scale, off, order, **{name: alone})
+        assert torch.equal(alone, v), name
+
+
+# ---------------------------------------------------------------- gradients against differences
+@pytest.mark.parametrize("what", ["x", "w"])
+def test_matmul_gradient_is_the_difference(ops, what):
+    """y is linear in x and in w: a central difference of sum(y c) along a
+    direction equals the gradient's product with it up to the products' rounding."""
+    gen = torch.Generator("cuda").manual_seed(5)
+    n, G, k, m = 70, 4, 50, 36
+    gid, off, order = grouped(sizes_of("skew", n, G, np.random.default_rng(3)), G)
+    f = torch.float32
+    v = {"x": rand(gen, n, k, dtype=f), "w": rand(gen, G, k, m, dtype=f)}
+    c, d = rand(gen, n, m, dtype=f), torch.randn(v[what].shape, generator=gen, device="cuda")
+    grad = {"dx": torch.empty(n, k, device="cuda"), "dw": torch.empty(G, k, m, device="cuda")}
+    ops.matmul_grad(c, v["x"], v["w"], off, order, **grad)
+    y = torch.empty(n, m, device="cuda")
+
+    def loss(h):
+        p = {**v, what: v[what] + h * d}
+        ops.matmul(p["x"], p["w"], off, order, y=y)
+        return float((y.double() * c.double()).sum())
+
+    diff = (loss(1.0) - loss(-1.0)) / 2
+    terms = (y.abs().double() * c.abs().double()).sum() + (grad["d" + what].abs().double() * d.abs().double()).sum()
+    assert abs(diff - float((grad["d" + what].double() * d.double()).sum())) <= (k + m + n) * 8 * EPS * float(terms)
+
+
+@pytest.mark.parametrize("what", ["x", "a", "b"])
+def test_adapter_gradient_is_the_difference(ops, what):
+    gen = torch.Generator("cuda").manual_seed(6)
+    n, G, k, m, R = 60, 3, 48, 40, 6
+    gid, off, order = grouped(sizes_of("skew", n, G, np.random.default_rng(4)), G)
+    f = torch.float32
+    v = {"x": rand(gen, n, k, dtype=f), "a": rand(gen, G, k, R, dtype=f), "b": rand(gen, G, R, m, dtype=f)}
+    w, scale = rand(gen, k, m, dtype=f), 0.5 + torch.rand(G, generator=gen, device="cuda")
+    c, d = rand(gen, n, m, dtype=f), torch.randn(v[what].shape, generator=gen, device="cuda")
+    grad = {"d" + q: torch.empty_like(v[q]) for q in v}
+    ops.adapter_grad(c, v["x"], w, v["a"], v["b"], scale, off, order, **grad)
+    y = torch.empty(n, m, device="cuda")
+
+    def loss(h):
+        p = {**v, what: v[what] + h * d}
+        ops.adapter(p["x"], w, p["a"], p["b"], scale, off, order, y=y)
+        return float((y.double() * c.double()).sum())
+
+    diff = (loss(1.0) - loss(-1.0)) / 2
+    terms = (y.abs().double() * c.abs().double()).sum() + (grad["d" + what].abs().double() * d.abs().double()).sum()
+    assert abs(diff - float((grad["d" + what].double() * d.double()).sum())) <= (k + m + n) * 8 * EPS * float(terms)
+
+
+# ---------------------------------------------------------------- infinities and NaN
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [40, 700])
+def test_values_stay_in_their_rows_and_groups(ops, dtype, n):
+    """A NaN or infinity in a row, or in a group's weights, changes no other row
+    and no other group's gradients; rows in no group and strides' padding never
+    count; what an earlier call left in the work space does not either."""
+    t = TYPES[dtype][0]
+    gen = torch.Generator("cuda").manual_seed(9)
+    G, k, m, R = 4, 100, 72, 12
+    gid = np.arange(n) % (G + 1) - 1              # -1: in no group
+    gid, off, order = grouped(gid, G)
+    x, dy = strided(rand(gen, n, k, dtype=t), 4), strided(rand(gen, n, m, dtype=t), 4)
+    ws, w = rand(gen, k, m, dtype=t), rand(gen, G, k, m, dtype=t)
+    a, b = rand(gen, G, k, R, dtype=t), rand(gen, G, R, m, dtype=t)
+    scale = torch.ones(G, device="cuda")
+
+    def run(x, dy, w, a, b):
+        o = {"y": torch.empty(n, m, dtype=t, device="cuda"), "z": torch.empty(n, m, dtype=t, device="cuda"),
+             "dx": torch.empty(n, k, dtype=t, device="cuda"), "dz": torch.empty(n, k, dtype=t, device="cuda"),
+             "dw": torch.empty_like(w), "da": torch.empty_like(a), "db": torch.empty_like(b)}
+        ops.matmul(x, w, off, order, y=o["y"])
+        ops.matmul_grad(dy, x, w, off, order, dx=o["dx"], dw=o["dw"])
+        ops.adapter(x, ws, a, b, scale, off, order, y=o["z"])
+        ops.adapter_grad(dy, x, ws, a, b, scale, off, order, dx=o["dz"], da=o["da"], db=o["db"])
+        return o
+
+    clean = run(x, dy, w, a, b)
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        # the last row of group 1, and a row in no group
+        for row in (int(np.nonzero(gid == 1)[0][-1]), int(np.nonzero(gid == -1)[0][0])):
+            xb, yb = x.clone(), dy.clone()
+            xb[row, 3], yb[row, 5] = bad, bad
+            got = run(xb, yb, w, a, b)
+            rest = torch.arange(n, device="cuda") != row
+            for q in ("y", "z", "dx", "dz"):
+                assert torch.equal(got[q][rest], clean[q][rest]), (q, bad, row)
+            others = [g for g in range(G) if g != gid[row]]
+            for q in ("dw", "da", "db"):
+                assert torch.equal(got[q][others], clean[q][others]), (q, bad, row)
+            if gid[row] < 0:
+                assert not got["y"][row].any() and not got["dx"][row].any()
+            else:
+                assert not torch.isfinite(got["y"][row]).any() and not torch.isfinite(got["dw"][1][3]).any()
+        # group 2's weights
+        wb, ab, bb = w.clone(), a.clone(), b.clone()
+        wb[2, 0, 0], ab[2, 1, 1], bb[2, 2, 2] = bad, bad, bad
+        got = run(x, dy, wb, ab, bb)
+        rest = torch.from_numpy(gid != 2).cuda()
+        for q in ("y", "z", "dx", "dz"):
+            assert torch.equal(got[q][rest], clean[q][rest]), (q, bad)
+        for q in ("dw", "da", "db"):
+            assert torch.equal(got[q][[0, 1, 3]], clean[q][[0, 1, 3]]), (q, bad)
+    again = run(x, dy, w, a, b)
+    assert all(torch.equal(again[q], clean[q]) for q in clean)
+
+
+@pytest.mark.parametrize("n", [8, 300])
+def test_infinite_weights_give_infinities(ops, n):
+    """An infinite adapter weight makes its outputs infinite, of the sign the
+    formula gives, and not NaN, though bf16 intermediates are sums of two parts."""
+    gen = torch.Generator("cuda").manual_seed(2)
+    t, k, m, R = torch.bfloat16, 64, 40, 8
+    x, w, a = rand(gen, n, k, dtype=t), rand(gen, k, m, dtype=t), rand(gen, 1, k, R, dtype=t)
+    b = rand(gen, 1, R, m, dtype=t)
+    b[0, 3, 5] = float("inf")
+    dy = rand(gen, n, m, dtype=t)
+    off = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    y = torch.empty(n, m, dtype=t, device="cuda")
+    ops.adapter(x, w, a, b, None, off, y=y)
+    low = (x.double() @ a[0].double())[:, 3]
+    assert torch.equal(y[:, 5].double(), torch.where(low > 0, float("inf"), -float("inf")))
+    assert torch.isfinite(y[:, :5]).all() and torch.isfinite(y[:, 6:]).all()
+    xi = x.clone()
+    xi[1, 7] = float("inf")
+    da = torch.empty_like(a)
+    b[0, 3, 5] = 1.0
+    ops.adapter_grad(dy, xi, w, a, b, None, off, da=da)
+    up = (dy.double() @ b[0].double().t())[1]
+    assert torch.equal(da[0, 7].double(), torch.where(up > 0, float("inf"), -float("inf")))
+
+
+# ---------------------------------------------------------------- places
+def test_empty_batch(ops):
+    off = torch.zeros(4, dtype=torch.int32, device="cuda")
+    e = lambda *s: torch.empty(s, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    x, y, w, a, b = e(0, 8), e(0, 16), e(3, 8, 16), e(3, 8, 4), e(3, 4, 16)
+    ops.matmul(x, w, off, y=y)
+    ops.adapter(x, w[0], a, b, None, off, y=y)
+    dw, da, db = (torch.full_like(v, 3) for v in (w, a, b))
+    ops.matmul_grad(y, x, w, off, dx=e(0, 8), dw=dw)
+    ops.adapter_grad(y, x, w[0], a, b, None, off, dx=e(0, 8), da=da, db=db)
+    assert not dw.any() and not da.any() and not db.any()
+
+
+def test_rows_past_32_bit_offsets(ops):
+    """Row strides that put rows past 2^32 bytes (and 2^31 elements)."""
+    n, k, m, ld, G, R = 130000, 40, 24, 17000, 3, 4
+    t = torch.bfloat16
+    gen = torch.Generator("cuda").manual_seed(1)
+    buf = torch.empty(n * ld, dtype=t, device="cuda")
+    x, y = buf.view(n, ld)[:, :k], buf.view(n, ld)[:, 128:128 + m]
+    x.copy_(rand(gen, n, k, dtype=t))
+    y.fill_(0)
+    w, a, b = rand(gen, G, k, m, dtype=t), rand(gen, G, k, R, dtype=t), rand(gen, G, R, m, dtype=t)
+    gid, off, order = grouped(sizes_of("skew", n, G, np.random.default_rng(0)), G)
+    ops.matmul(x, w, off, order, y=y)
+    xc = x.contiguous()
+    ref, s = product(xc, w, gid)
+    close(y, ref, 2.0 ** -8 * ref.abs() + (k + 16) * EPS * s)
+    dw, dw2 = torch.empty_like(w), torch.empty_like(w)
+    ops.matmul_grad(y, x, w, off, order, dw=dw)
+    ops.matmul_grad(y.contiguous(), xc, w, off, order, dw=dw2)
+    assert torch.equal(dw, dw2)
+    z = torch.empty(n, m, dtype=t, device="cuda")
+    ops.adapter(xc, w[0], a, b, None, off, order, y=z)
+    ops.adapter(x, w[0], a, b, None, off, order, y=y)
+    assert torch.equal(y, z)
+
+
+def test_other_stream(ops):
+    """A context on a stream of its own, ordered against the default one by events."""
+    s = torch.cuda.Stream()
+    o = routed.RoutedOps(stream=s.cuda_stream)
+    gen = torch.Generator("cuda").manual_seed(3)
+    n, G, k, m = 600, 3, 256, 320
+    gid, off, order = grouped(sizes_of("skew", n, G, np.random.default_rng(1)), G)
+    w = rand(gen, G, k, m, dtype=torch.bfloat16)
+    y, want = (torch.empty(n, m, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for i in range(5):
+        x = rand(gen, n, k, dtype=torch.bfloat16)
+        s.wait_stream(torch.cuda.current_stream())
+        o.matmul(x, w, off, order, y=y)
+        torch.cuda.current_stream().wait_stream(s)
+        ops.matmul(x, w, off, order, y=want)
+        assert torch.equal(y, want)
+    o.close()
+
+
+def test_graph(ops):
+    """Captured calls replay on new contents; a capture that would have to allocate is refused."""
+    gen = torch.Generator("cuda").manual_seed(4)
+    t = torch.bfloat16
+    n, G, k, m, R = 300, 5, 128, 192, 8
+    s = torch.cuda.Stream()
+    o = routed.RoutedOps(stream=s.cuda_stream)
+    choice = torch.zeros(n, dtype=torch.int32, device="cuda")
+    off, order = torch.empty(G + 1, dtype=torch.int32, device="cuda"), torch.empty(n, dtype=torch.int32, device="cuda")
+    x, dy = rand(gen, n, k, dtype=t), rand(gen, n, m, dtype=t)
+    w, a, b = rand(gen, k, m, dtype=t), rand(gen, G, k, R, dtype=t), rand(gen, G, R, m, dtype=t)
+    out = {"y": torch.empty(n, m, dtype=t, device="cuda"), "dx": torch.empty_like(x), "da": torch.empty_like(a),
+           "db": torch.empty_like(b)}
+
+    def step(q, out):
+        q.group(choice, G, offsets=off, order=order)
+        q.adapter(x, w, a, b, None, off, order, y=out["y"])
+        q.adapter_grad(dy, x, w, a, b, None, off, order, dx=out["dx"], da=out["da"], db=out["db"])
+
+    big = torch.empty(200000, k, dtype=t, device="cuda")
+    big_y = torch.empty(200000, m, dtype=t, device="cuda")
+    s.wait_stream(torch.cuda.current_stream())
+    step(o, out)                                   # work space
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        with pytest.raises(hwr.HwrError) as e:
+            o.adapter(big, w, a, b, None, off, None, y=big_y)
+        step(o, out)
+    assert e.value.status == hwr.HWR_ERR_STATE
+    for i in range(4):
+        choice.copy_(torch.randint(-1, G, (n,), generator=gen, device="cuda"))
+        x.copy_(rand(gen, n, k, dtype=t))
+        want = {q: torch.empty_like(v) for q, v in out.items()}
+        step(ops, want)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for q in out:
+            assert torch.equal(out[q], want[q]), (i, q)
+        if i == 1:                                 # the context's work space grows; the graph keeps its own
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                o.reserve(1 << 28)
+            torch.cuda.synchronize()
+    del g
+    o.close()
+
+
+# ---------------------------------------------------------------- refusals
+def test_refusals(ops):
+    e = lambda *s, dtype=torch.bfloat16: torch.zeros(s, dtype=dtype, device="cuda")  # noqa: E731
+    i = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")  # noqa: E731
+    x, y, w, off, order = e(4, 8), e(4, 16), e(2, 8, 16), i(3), i(4)
+    a, b, sc = e(2, 8, 4), e(2, 4, 16), torch.ones(2, device="cuda")
+    bad = [
+        lambda: ops.matmul(x.float(), w, off, order, y=y),
+        lambda: ops.matmul(x.half(), w.half(), off, order, y=y.half()),
+        lambda: ops.matmul(x.cpu(), w, off, order, y=y),
+        lambda: ops.matmul(e(4, 16)[:, ::2], w, off, order, y=y),
+        lambda: ops.matmul(x[:1].expand(4, 8), w, off, order, y=y),
+        lambda: ops.matmul(x, w.transpose(1, 2), off, order, y=y),
+        lambda: ops.matmul(x, e(2, 9, 16), off, order, y=y),
+        lambda: ops.matmul(x, w, i(4), order, y=y),
+        lambda: ops.matmul(x, w, off, i(5), y=y),
+        lambda: ops.matmul(x, w, off, order.long(), y=y),
+        lambda: ops.matmul(x, w, off, order, y=e(4, 15)),
+        lambda: ops.matmul(x, e(1025, 8, 16), i(1026), order, y=y),
+        lambda: ops.matmul(e(4, 0), e(2, 0, 16), off, order, y=y),
+        lambda: ops.matmul_grad(y, x, w, off, order, dx=e(4, 9)),
+        lambda: ops.matmul_grad(y, x, w, off, order, dw=e(2, 16, 8)),
+        lambda: ops.adapter(x, e(8, 16), a, e(2, 5, 16), sc, off, order, y=y),
+        lambda: ops.adapter(x, e(8, 16), a, b, sc.bfloat16(), off, order, y=y),
+        lambda: ops.adapter(x, e(8, 16), e(2, 8, 129), e(2, 129, 16), sc, off, order, y=y),
+        lambda: ops.adapter_grad(y, x, e(8, 16), a, b, sc, off, order, da=e(2, 4, 8)),
+        lambda: ops.group(order, 0, offsets=i(1), order=i(4)),
+        lambda: ops.group(order, 1025, offsets=i(1026), order=i(4)),
+        lambda: ops.group(order, 2, offsets=i(2), order=i(4)),
+        lambda: ops.group(order.float(), 2, offsets=i(3), order=i(4)),
+    ]
+    for n, f in enumerate(bad):
+        with pytest.raises(hwr.HwrError) as err:
+            f()
+        assert err.value.status == hwr.HWR_ERR_INVALID_ARG, n
+    # through the C ABI: sizes, strides, missing and misaligned pointers; nothing is launched
+    import ctypes as C
+    lib = hwr.load()
+    g = hwr.hwr_groups(4, 2, off.data_ptr(), order.data_ptr())
+    good = dict(dtype=hwr.HWR_BF16, k=8, m=16, x=x.data_ptr(), ldx=0, w=w.data_ptr(), y=y.data_ptr(), ldy=0)
+    for change in (dict(dtype=2), dict(k=0), dict(m=65537), dict(x=None), dict(w=None), dict(y=None), dict(ldx=7),
+                   dict(ldy=-1), dict(x=x.data_ptr() + 1)):
+        m = hwr.hwr_matmul_args(**{**good, **change})
+        assert lib.hwr_grouped_matmul(ops.ctx, C.byref(g), C.byref(m)) == hwr.HWR_ERR_INVALID_ARG, change
+        assert hwr.hwr_ops_last_error(ops.ctx)
+    for groups in ((-1, 2, off.data_ptr()), (4, 0, off.data_ptr()), (4, 2, None)):
+        gb = hwr.hwr_groups(*groups, order.data_ptr())
+        m = hwr.hwr_matmul_args(**good)
+        assert lib.hwr_grouped_matmul(ops.ctx, C.byref(gb), C.byref(m)) == hwr.HWR_ERR_INVALID_ARG, groups
+    assert lib.hwr_grouped_matmul(ops.ctx, None, C.byref(m)) == hwr.HWR_ERR_INVALID_ARG
+    assert lib.hwr_grouped_matmul(ops.ctx, C.byref(g), None) == hwr.HWR_ERR_INVALID_ARG
+    with pytest.raises(hwr.HwrError):
+        routed.RoutedOps(device=4096)
+
+
+def test_example_learns():
+    losses = routed.example(steps=4, n=2000)
+    assert losses[-1] < losses[0] and all(np.isfinite(losses))

@@ -1,0 +1,50 @@
+"""hwr_ops.h without a device: the argument structures' layout against the C
+compiler's, NULL contexts, and the binding's checks of torch tensors."""
+import ctypes as C
+import os
+import subprocess
+
+import pytest
+
+from paper_2608_14575_amd import hwr, routed
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+STRUCTS = ["hwr_groups", "hwr_matmul_args", "hwr_matmul_grad_args", "hwr_adapter_args", "hwr_adapter_grad_args"]
+
+
+def test_layout_matches_header(tmp_path):
+    src = ['#include <stdio.h>', '#include <stddef.h>', '#include "hwr_ops.h"', "int main(void) {"]
+    for s in STRUCTS:
+        src.append(f'printf("{s} sizeof %zu\\n", sizeof({s}));')
+        src += [f'printf("{s} {f} %zu\\n", offsetof({s}, {f}));' for f, _ in getattr(hwr, s)._fields_]
+    src.append("return 0; }")
+    c, exe = tmp_path / "layout.c", tmp_path / "layout"
+    c.write_text("\n".join(src))
+    subprocess.check_call(["gcc", "-std=c11", "-Wall", "-Werror", f"-I{os.path.join(ROOT, 'include')}", str(c), "-o", str(exe)])
+    for line in subprocess.check_output([str(exe)], text=True).splitlines():
+        s, f, v = line.split()
+        cls = getattr(hwr, s)
+        assert int(v) == (C.sizeof(cls) if f == "sizeof" else getattr(cls, f).offset), line
+
+
+def test_null_arguments():
+    lib = hwr.load()
+    g = hwr.hwr_groups()
+    assert lib.hwr_ops_init(0, None, None) == hwr.HWR_ERR_INVALID_ARG
+    assert "out is NULL" in hwr.hwr_ops_last_error(None)
+    assert lib.hwr_ops_reserve(None, 1) == hwr.HWR_ERR_INVALID_ARG
+    assert lib.hwr_group_rows(None, 0, None, None, 0, 1, None, None) == hwr.HWR_ERR_INVALID_ARG
+    for fn, args in (("hwr_grouped_matmul", "hwr_matmul_args"), ("hwr_grouped_matmul_grad", "hwr_matmul_grad_args"),
+                     ("hwr_adapter_matmul", "hwr_adapter_args"), ("hwr_adapter_matmul_grad", "hwr_adapter_grad_args")):
+        assert getattr(lib, fn)(None, C.byref(g), C.byref(getattr(hwr, args)())) == hwr.HWR_ERR_INVALID_ARG
+        assert "ops is NULL" in hwr.hwr_ops_last_error(None)
+    hwr.hwr_ops_free(None)
+
+
+def test_no_device_is_a_clean_error():
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("a device is present")
+    with pytest.raises(hwr.HwrError) as e:
+        routed.RoutedOps()
+    assert e.value.status == hwr.HWR_ERR_HIP

@@ -58,9 +58,9 @@ __global__ void __launch_bounds__(WP *WQ * 64) k_cols(ColsArgs a) {
         for (int sub = 0; sub < 2; ++sub) {
             typename El::Frag fq[QF], fp[PF];
 #pragma unroll
-            for (int j = 0; j < QF; ++j) fq[j] = QT::frag(sq, (wq * QF + j) * 16, sub, lane);
+            for (int j = 0; j < QF; ++j) fq[j] = QT::frag(sq, 0, (wq * QF + j) * 16, sub, lane);
 #pragma unroll
-            for (int i = 0; i < PF; ++i) fp[i] = PT::frag(sp, (wp * PF + i) * 16, sub, lane);
+            for (int i = 0; i < PF; ++i) fp[i] = PT::frag(sp, 0, (wp * PF + i) * 16, sub, lane);
 #pragma unroll
             for (int i = 0; i < PF; ++i)
 #pragma unroll

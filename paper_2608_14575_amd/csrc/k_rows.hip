@@ -42,140 +42,79 @@ __device__ inline u32x4 finite_only(u32x4 v) {
     return v;
 }
 
-template <class E, RowsKind KIND, bool KS, int BM, int BN, int WR, int WC>
-__global__ void __launch_bounds__(WR *WC * 64) k_rows(RowsArgs a) {
+// The adapters of the tile's groups: one stage for every 32 of the rank, whose
+// contraction is hi and lo against the same weights in bf16.  Only the rows of
+// the group take the result (a zero would turn another group's infinity into NaN).
+template <class E, bool KS, int BM, int BN, int WR, int WC>
+__device__ inline void add_adapters(const RowsArgs &a, const RowTile &rt, int c0, char *sx, char *sw,
+                                    f32x4 (&acc)[BM / WR / 16][BN / WC / 16], int tid) {
     using El = Elem<E>;
-    constexpr int NT = WR * WC * 64, RF = BM / WR / 16, CF = BN / WC / 16, kBk = El::kBk;
+    constexpr int NT = WR * WC * 64, RF = BM / WR / 16, CF = BN / WC / 16;
     using XT = Tile<E, false, BM>;
     using WT = Tile<E, KS, BN>;
-    __shared__ __attribute__((aligned(16))) char sx[XT::kBytes], sw[WT::kBytes];
-    __shared__ int rows[BM];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wr = wave / WC, wc = wave % WC;
-
-    const bool tail = KIND == RowsKind::kGrouped;
-    const int tiles = KIND == RowsKind::kAdapter ? (a.g.n + BM - 1) / BM : count_tiles(a.g, BM, tail, lane);
-    const int ct = (a.m + BN - 1) / BN;
-    const int item = xcd_item(blockIdx.x, tiles * ct);
-    if (item < 0) return;
-    const int panel = item / (8 * ct) * 8, in = item - panel * ct, rp = min(8, tiles - panel);
-    const int t = panel + in % rp, c0 = in / rp * BN;
-    RowTile rt;
-    if (KIND == RowsKind::kAdapter) rt = {0, t * BM, min(t * BM + BM, a.g.n)};
-    else rt = find_tile(a.g, t, BM, tail, lane);
-
-    for (int i = tid; i < BM; i += NT) rows[i] = rt.p0 + i < rt.p1 ? row_at(a.g, rt.p0 + i) : -1;
-    __syncthreads();
-
-    const E *x = static_cast<const E *>(a.x);
-    const E *w = static_cast<const E *>(a.w) + (KIND == RowsKind::kAdapter ? 0 : rt.g) * a.w_stride;
-    const int k = KIND == RowsKind::kGrouped && rt.g == a.g.G ? 0 : a.k;
-
-    auto weights = [&](const E *base, int k0, int klen) {   // KS: lines are elements; else columns
-        return [=, &a](int line, int c) {
-            if constexpr (KS) {
-                return load_chunk<E>(k0 + line < klen ? base + static_cast<int64_t>(k0 + line) * a.m : nullptr,
-                                     c0 + c * El::kEpc, a.m);
-            } else {
-                return load_chunk<E>(c0 + line < a.m ? base + static_cast<int64_t>(c0 + line) * klen : nullptr,
-                                     k0 + c * El::kEpc, klen);
-            }
-        };
-    };
-    auto inputs = [&](int k0) {
-        return [=, &a](int line, int c) {
-            const int r = rows[line];
-            return load_chunk<E>(r >= 0 ? x + r * a.ldx : nullptr, k0 + c * El::kEpc, k);
-        };
-    };
-
-    f32x4 acc[RF][CF] = {};
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WC, wc = wave % WC;
     Staged<E, false, BM, NT> gx;
     Staged<E, KS, BN, NT> gw;
-    if (k > 0) {
-        gx.load(inputs(0), tid);
-        gw.load(weights(w, 0, k), tid);
-    }
-    for (int k0 = 0; k0 < k; k0 += kBk) {
-        gx.store(sx, tid);
-        gw.store(sw, tid);
-        __syncthreads();
-        if (k0 + kBk < k) {
-            gx.load(inputs(k0 + kBk), tid);
-            gw.load(weights(w, k0 + kBk, k), tid);
-        }
+    const E *lw = static_cast<const E *>(a.lw);
+    const char *low = static_cast<const char *>(a.low);
+    const int blocks = (a.rank + kRankBlock - 1) / kRankBlock;
+    for (int g = group_of(a.g, rt.p0, lane); g < a.g.G; ++g) {
+        const int lo = max(place_of(a.g, g), rt.p0), hi = min(place_of(a.g, g + 1), rt.p1);
+        if (place_of(a.g, g) >= rt.p1) break;
+        if (lo >= hi) continue;
+        const E *gl = lw + static_cast<int64_t>(g) * a.rank * a.m;
+        for (int b = 0; b < blocks; ++b) {
+            const int r0 = b * kRankBlock;
+            gx.load([&](int line, int c) {
+                const int p = rt.p0 + line;
+                if (p < lo || p >= hi) return u32x4{0, 0, 0, 0};
+                return *reinterpret_cast<const u32x4 *>(low + (static_cast<int64_t>(p) * blocks + b) * kLowBytes + c * 16);
+            }, tid);
+            gw.load([&](int line, int c) {
+                u32x4 v;
+                const int e = KS ? line : c * El::kEpc;        // contraction element of the stage
+                const int r = r0 + (e & (kRankBlock - 1));
+                if constexpr (KS)
+                    v = load_chunk<E>(r < a.rank ? gl + static_cast<int64_t>(r) * a.m : nullptr, c0 + c * El::kEpc, a.m);
+                else
+                    v = load_chunk<E>(c0 + line < a.m ? gl + static_cast<int64_t>(c0 + line) * a.rank : nullptr, r, a.rank);
+                return e < kRankBlock ? v : finite_only(v);    // past kRankBlock: the low parts (bf16)
+            }, tid);
+            gx.store(sx, tid);
+            gw.store(sw, tid);
+            __syncthreads();
 #pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-            typename El::Frag fw[CF], fx[RF];
+            for (int sub = 0; sub < 2; ++sub) {
+                typename El::Frag fw[CF];
 #pragma unroll
-            for (int j = 0; j < CF; ++j) fw[j] = WT::frag(sw, (wc * CF + j) * 16, sub, lane);
+                for (int j = 0; j < CF; ++j) fw[j] = WT::frag(sw, 0, (wc * CF + j) * 16, sub, lane);
 #pragma unroll
-            for (int i = 0; i < RF; ++i) fx[i] = XT::frag(sx, (wr * RF + i) * 16, sub, lane);
+                for (int i = 0; i < RF; ++i) {
+                    const int f0 = rt.p0 + (wr * RF + i) * 16;
+                    if (f0 + 16 <= lo || f0 >= hi) continue;
+                    const typename El::Frag fx = XT::frag(sx, 0, (wr * RF + i) * 16, sub, lane);
+                    const int p = f0 + (lane & 15);
+                    const bool in_group = p >= lo && p < hi;
 #pragma unroll
-            for (int i = 0; i < RF; ++i)
+                    for (int j = 0; j < CF; ++j) {
+                        const f32x4 v = El::mma(fw[j], fx, acc[i][j]);
 #pragma unroll
-                for (int j = 0; j < CF; ++j) acc[i][j] = El::mma(fw[j], fx[i], acc[i][j]);
-        }
-        __syncthreads();
-    }
-
-    // The adapters of the tile's groups: one stage for every 32 of the rank, whose
-    // contraction is hi and lo against the same weights in bf16.  Only the rows of
-    // the group take the result (a zero would turn another group's infinity into NaN).
-    if constexpr (KIND == RowsKind::kAdapter) {
-        const E *lw = static_cast<const E *>(a.lw);
-        const char *low = static_cast<const char *>(a.low);
-        const int blocks = (a.rank + kRankBlock - 1) / kRankBlock;
-        for (int g = group_of(a.g, rt.p0, lane); g < a.g.G; ++g) {
-            const int lo = max(place_of(a.g, g), rt.p0), hi = min(place_of(a.g, g + 1), rt.p1);
-            if (place_of(a.g, g) >= rt.p1) break;
-            if (lo >= hi) continue;
-            const E *gl = lw + static_cast<int64_t>(g) * a.rank * a.m;
-            for (int b = 0; b < blocks; ++b) {
-                const int r0 = b * kRankBlock;
-                gx.load([&](int line, int c) {
-                    const int p = rt.p0 + line;
-                    if (p < lo || p >= hi) return u32x4{0, 0, 0, 0};
-                    return *reinterpret_cast<const u32x4 *>(low + (static_cast<int64_t>(p) * blocks + b) * kLowBytes + c * 16);
-                }, tid);
-                gw.load([&](int line, int c) {
-                    u32x4 v;
-                    const int e = KS ? line : c * El::kEpc;        // contraction element of the stage
-                    const int r = r0 + (e & (kRankBlock - 1));
-                    if constexpr (KS)
-                        v = load_chunk<E>(r < a.rank ? gl + static_cast<int64_t>(r) * a.m : nullptr, c0 + c * El::kEpc, a.m);
-                    else
-                        v = load_chunk<E>(c0 + line < a.m ? gl + static_cast<int64_t>(c0 + line) * a.rank : nullptr, r, a.rank);
-                    return e < kRankBlock ? v : finite_only(v);    // past kRankBlock: the low parts (bf16)
-                }, tid);
-                gx.store(sx, tid);
-                gw.store(sw, tid);
-                __syncthreads();
-#pragma unroll
-                for (int sub = 0; sub < 2; ++sub) {
-                    typename El::Frag fw[CF];
-#pragma unroll
-                    for (int j = 0; j < CF; ++j) fw[j] = WT::frag(sw, (wc * CF + j) * 16, sub, lane);
-#pragma unroll
-                    for (int i = 0; i < RF; ++i) {
-                        const int f0 = rt.p0 + (wr * RF + i) * 16;
-                        if (f0 + 16 <= lo || f0 >= hi) continue;
-                        const typename El::Frag fx = XT::frag(sx, (wr * RF + i) * 16, sub, lane);
-                        const int p = f0 + (lane & 15);
-                        const bool in_group = p >= lo && p < hi;
-#pragma unroll
-                        for (int j = 0; j < CF; ++j) {
-                            const f32x4 v = El::mma(fw[j], fx, acc[i][j]);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[i][j][e] = in_group ? v[e] : acc[i][j][e];
-                        }
+                        for (int e = 0; e < 4; ++e) acc[i][j][e] = in_group ? v[e] : acc[i][j][e];
                     }
                 }
-                __syncthreads();
             }
+            __syncthreads();
         }
     }
+}
 
+// A lane holds, for row l % 16 of fragment i, four columns of fragment j.
+template <class E, RowsKind KIND, int BM, int BN, int WR, int WC>
+__device__ inline void store_rows(const RowsArgs &a, const RowTile &rt, int c0, const int *rows,
+                                  const f32x4 (&acc)[BM / WR / 16][BN / WC / 16], int tid) {
+    constexpr int RF = BM / WR / 16, CF = BN / WC / 16;
+    using El = Elem<E>;
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WC, wc = wave % WC;
     const int q = lane >> 4;
     if constexpr (KIND == RowsKind::kShrink) {
         const float s = a.scale ? a.scale[rt.g] : 1.0f;
@@ -232,7 +171,205 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows(RowsArgs a) {
     }
 }
 
+// The workgroup's tile of places and first column.  Tiles go in panels of 8 row
+// tiles, column by column, so that the workgroups that run together on one L2
+// share rows and weights.  False past the last tile.
+template <RowsKind KIND, int BM, int BN>
+__device__ inline bool my_tile(const RowsArgs &a, int lane, RowTile &rt, int &c0) {
+    const bool tail = KIND == RowsKind::kGrouped;
+    const int tiles = KIND == RowsKind::kAdapter ? (a.g.n + BM - 1) / BM : count_tiles(a.g, BM, tail, lane);
+    const int ct = (a.m + BN - 1) / BN;
+    const int item = xcd_item(blockIdx.x, tiles * ct);
+    if (item < 0) return false;
+    const int panel = item / (8 * ct) * 8, in = item - panel * ct, rp = min(8, tiles - panel);
+    const int t = panel + in % rp;
+    c0 = in / rp * BN;
+    if (KIND == RowsKind::kAdapter) rt = {0, t * BM, min(t * BM + BM, a.g.n)};
+    else rt = find_tile(a.g, t, BM, tail, lane);
+    return true;
+}
+
+// Any widths, strides and alignment: operands pass through registers.
 template <class E, RowsKind KIND, bool KS, int BM, int BN, int WR, int WC>
+__global__ void __launch_bounds__(WR *WC * 64) k_rows(RowsArgs a) {
+    using El = Elem<E>;
+    constexpr int NT = WR * WC * 64, RF = BM / WR / 16, CF = BN / WC / 16, kBk = El::kBk;
+    using XT = Tile<E, false, BM>;
+    using WT = Tile<E, KS, BN>;
+    __shared__ __attribute__((aligned(16))) char sx[XT::kBytes], sw[WT::kBytes];
+    __shared__ int rows[BM];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wr = wave / WC, wc = wave % WC;
+    RowTile rt;
+    int c0;
+    if (!my_tile<KIND, BM, BN>(a, lane, rt, c0)) return;
+
+    for (int i = tid; i < BM; i += NT) rows[i] = rt.p0 + i < rt.p1 ? row_at(a.g, rt.p0 + i) : -1;
+    __syncthreads();
+
+    const E *x = static_cast<const E *>(a.x);
+    const E *w = static_cast<const E *>(a.w) + (KIND == RowsKind::kAdapter ? 0 : rt.g) * a.w_stride;
+    const int k = KIND == RowsKind::kGrouped && rt.g == a.g.G ? 0 : a.k;
+
+    auto weights = [&](const E *base, int k0, int klen) {   // KS: lines are elements; else columns
+        return [=, &a](int line, int c) {
+            if constexpr (KS) {
+                return load_chunk<E>(k0 + line < klen ? base + static_cast<int64_t>(k0 + line) * a.m : nullptr,
+                                     c0 + c * El::kEpc, a.m);
+            } else {
+                return load_chunk<E>(c0 + line < a.m ? base + static_cast<int64_t>(c0 + line) * klen : nullptr,
+                                     k0 + c * El::kEpc, klen);
+            }
+        };
+    };
+    auto inputs = [&](int k0) {
+        return [=, &a](int line, int c) {
+            const int r = rows[line];
+            return load_chunk<E>(r >= 0 ? x + r * a.ldx : nullptr, k0 + c * El::kEpc, k);
+        };
+    };
+
+    f32x4 acc[RF][CF] = {};
+    Staged<E, false, BM, NT> gx;
+    Staged<E, KS, BN, NT> gw;
+    if (k > 0) {
+        gx.load(inputs(0), tid);
+        gw.load(weights(w, 0, k), tid);
+    }
+    for (int k0 = 0; k0 < k; k0 += kBk) {
+        gx.store(sx, tid);
+        gw.store(sw, tid);
+        __syncthreads();
+        if (k0 + kBk < k) {
+            gx.load(inputs(k0 + kBk), tid);
+            gw.load(weights(w, k0 + kBk, k), tid);
+        }
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub) {
+            typename El::Frag fw[CF], fx[RF];
+#pragma unroll
+            for (int j = 0; j < CF; ++j) fw[j] = WT::frag(sw, 0, (wc * CF + j) * 16, sub, lane);
+#pragma unroll
+            for (int i = 0; i < RF; ++i) fx[i] = XT::frag(sx, 0, (wr * RF + i) * 16, sub, lane);
+#pragma unroll
+            for (int i = 0; i < RF; ++i)
+#pragma unroll
+                for (int j = 0; j < CF; ++j) acc[i][j] = El::mma(fw[j], fx[i], acc[i][j]);
+        }
+        __syncthreads();
+    }
+
+    if constexpr (KIND == RowsKind::kAdapter) add_adapters<E, KS, BM, BN, WR, WC>(a, rt, c0, sx, sw, acc, tid);
+    store_rows<E, KIND, BM, BN, WR, WC>(a, rt, c0, rows, acc, tid);
+}
+
+// Whole chunks of 16 bytes everywhere: operands go from memory straight into LDS,
+// the next stage's while this one is multiplied.  Rows in no place and columns past
+// the last are loaded from a valid one and not stored; contraction elements past
+// the last are zeros on both sides.
+template <class E, RowsKind KIND, bool KS, int BM, int BN, int WR, int WC>
+__global__ void __launch_bounds__(WR *WC * 64) k_rows_direct(RowsArgs a) {
+    using El = Elem<E>;
+    constexpr int NT = WR * WC * 64, RF = BM / WR / 16, CF = BN / WC / 16, kBk = El::kBk, kEpc = El::kEpc;
+    using XT = Tile<E, false, BM>;
+    using WT = Tile<E, KS, BN>;
+    constexpr int UX = XT::kChunks / NT, UW = WT::kChunks / NT;
+    static_assert(XT::kChunks % NT == 0 && WT::kChunks % NT == 0);
+    constexpr int kBuf = XT::kBytes + WT::kBytes;
+    // an array each, so that the compiler sees that reads of one do not depend on the
+    // loads in flight into the other
+    __shared__ __attribute__((aligned(16))) char buf0[kBuf], buf1[kBuf];
+    __shared__ int rows[BM];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wr = wave / WC, wc = wave % WC;
+    RowTile rt;
+    int c0;
+    if (!my_tile<KIND, BM, BN>(a, lane, rt, c0)) return;
+    for (int i = tid; i < BM; i += NT) rows[i] = rt.p0 + i < rt.p1 ? row_at(a.g, rt.p0 + i) : -1;
+    __syncthreads();
+
+    const int k = KIND == RowsKind::kGrouped && rt.g == a.g.G ? 0 : a.k;
+    const char *xp[UX], *wp[UW];
+    int xe[UX], we[UW];                    // first contraction element of the thread's chunks
+#pragma unroll
+    for (int i = 0; i < UX; ++i) {
+        const int u = i * NT + tid, line = u / XT::kCpl, r = rows[line];
+        xe[i] = ((u % XT::kCpl) ^ XT::swz(line)) * kEpc;
+        xp[i] = reinterpret_cast<const char *>(static_cast<const E *>(a.x) + (r < 0 ? 0 : r) * a.ldx + xe[i]);
+    }
+    const E *w = static_cast<const E *>(a.w) + (KIND == RowsKind::kAdapter || k == 0 ? 0 : rt.g) * a.w_stride;
+#pragma unroll
+    for (int i = 0; i < UW; ++i) {
+        const int u = i * NT + tid, line = u / WT::kCpl, c = (u % WT::kCpl) ^ WT::swz(line);
+        we[i] = KS ? line : c * kEpc;
+        const int64_t at = KS ? static_cast<int64_t>(line) * a.m + min(c0 + c * kEpc, a.m - kEpc)
+                              : static_cast<int64_t>(min(c0 + line, a.m - 1)) * a.k + c * kEpc;
+        wp[i] = reinterpret_cast<const char *>(w + at);
+    }
+    const int64_t wstep = KS ? static_cast<int64_t>(kBk) * a.m * sizeof(E) : kStageBytes;
+    const char *zeros = static_cast<const char *>(a.zeros);
+    auto issue = [&](char *b, int k0) {
+        const bool whole = k0 + kBk <= k;
+#pragma unroll
+        for (int i = 0; i < UX; ++i) {
+            const char *src = whole || k0 + xe[i] < k ? xp[i] : zeros;
+            load_lds(src, b + (i * NT + wave * 64) * 16);
+            xp[i] += kStageBytes;
+        }
+#pragma unroll
+        for (int i = 0; i < UW; ++i) {
+            const char *src = whole || k0 + we[i] < k ? wp[i] : zeros;
+            load_lds(src, b + XT::kBytes + (i * NT + wave * 64) * 16);
+            wp[i] += wstep;
+        }
+    };
+    f32x4 acc[RF][CF] = {};
+    auto multiply = [&](const char *b) {
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub) {
+            typename El::Frag fw[CF], fx[RF];
+#pragma unroll
+            for (int j = 0; j < CF; ++j) fw[j] = WT::frag(b, XT::kBytes, (wc * CF + j) * 16, sub, lane);
+#pragma unroll
+            for (int i = 0; i < RF; ++i) fx[i] = XT::frag(b, 0, (wr * RF + i) * 16, sub, lane);
+#pragma unroll
+            for (int i = 0; i < RF; ++i)
+#pragma unroll
+                for (int j = 0; j < CF; ++j) acc[i][j] = El::mma(fw[j], fx[i], acc[i][j]);
+        }
+    };
+    auto finished = [&] {                  // this stage's buffer may be overwritten
+        wait_lds();
+        barrier();
+    };
+    if (k > 0) {
+        issue(buf0, 0);
+        int k0 = 0;
+        for (; k0 + 2 * kBk < k; k0 += 2 * kBk) {
+            issue(buf1, k0 + kBk);
+            wait_vm<UX + UW>();
+            barrier();
+            multiply(buf0);
+            finished();
+            issue(buf0, k0 + 2 * kBk);
+            wait_vm<UX + UW>();
+            barrier();
+            multiply(buf1);
+            finished();
+        }
+        if (k0 + kBk < k) issue(buf1, k0 + kBk);
+        wait_vm<0>();
+        barrier();
+        multiply(buf0);
+        if (k0 + kBk < k) multiply(buf1);
+        finished();
+    }
+
+    if constexpr (KIND == RowsKind::kAdapter) add_adapters<E, KS, BM, BN, WR, WC>(a, rt, c0, buf0, buf0 + XT::kBytes, acc, tid);
+    store_rows<E, KIND, BM, BN, WR, WC>(a, rt, c0, rows, acc, tid);
+}
+
+template <class E, RowsKind KIND, bool KS, int BM, int BN, int WR, int WC, bool DIRECT = false>
 hipError_t go(const RowsArgs &a, hipStream_t s) {
     const int64_t n = a.g.n;
     // a group adds at most one partial tile, and a tile holds at least one row
@@ -240,7 +377,17 @@ hipError_t go(const RowsArgs &a, hipStream_t s) {
     const int64_t items = tiles * ((a.m + BN - 1) / BN);
     const int64_t blocks = (items + 7) / 8 * 8;
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
-    return launch_kernel(k_rows<E, KIND, KS, BM, BN, WR, WC>, dim3(static_cast<uint32_t>(blocks)), dim3(WR * WC * 64), 0, s, a);
+    const dim3 grid(static_cast<uint32_t>(blocks)), block(WR * WC * 64);
+    if constexpr (DIRECT) return launch_kernel(k_rows_direct<E, KIND, KS, BM, BN, WR, WC>, grid, block, 0, s, a);
+    else return launch_kernel(k_rows<E, KIND, KS, BM, BN, WR, WC>, grid, block, 0, s, a);
+}
+
+// Rows and weights in whole, aligned chunks of 16 bytes.
+template <class E, bool KS>
+bool whole_chunks(const RowsArgs &a) {
+    constexpr int kEpc = Elem<E>::kEpc;
+    const auto ptrs = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w);
+    return (ptrs & 15) == 0 && a.ldx % kEpc == 0 && a.k % kEpc == 0 && (!KS || a.m % kEpc == 0);
 }
 
 template <class E, RowsKind KIND, bool KS>
@@ -251,6 +398,10 @@ hipError_t pick(const RowsArgs &a, hipStream_t s) {
     } else {
         const bool small = KIND == RowsKind::kAdapter ? a.g.n <= 64 : a.g.n <= 64 * a.g.G;
         if (small) return go<E, KIND, KS, 16, 64, 1, 4>(a, s);
+        if (whole_chunks<E, KS>(a)) {
+            if constexpr (sizeof(E) == 2) return go<E, KIND, KS, 256, 256, 2, 4, true>(a, s);
+            else return go<E, KIND, KS, 128, 128, 2, 2, true>(a, s);
+        }
         return go<E, KIND, KS, 128, 128, 2, 2>(a, s);
     }
 }

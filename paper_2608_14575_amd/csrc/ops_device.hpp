@@ -68,32 +68,34 @@ struct Tile {
         else if constexpr (kCpl == 4) return ((line >> 3) & 1) << 1;
         else return 0;
     }
-    // Fragment of the 16 rows (columns) from c0 on, contraction half `sub` of the stage.
-    static __device__ typename Elem<E>::Frag frag(const char *t, int c0, int sub, int lane) {
+    // Fragment of the 16 rows (columns) from c0 on, contraction half `sub` of the
+    // stage; the tile lies at byte `at` of the LDS array.  (One offset, added once:
+    // the compiler follows an array through few additions only, and reads that it
+    // cannot place wait for every load in flight into LDS.)
+    static __device__ typename Elem<E>::Frag frag(const char *lds, int at, int c0, int sub, int lane) {
         const int m = lane & 15, q = lane >> 4;
         if constexpr (!KS) {
-            const int line = c0 + m;
-            return *reinterpret_cast<const typename Elem<E>::Frag *>(t + line * 128 + (((sub * 4 + q) ^ swz(line)) << 4));
+            const int line = c0 + m, o = at + line * 128 + (((sub * 4 + q) ^ swz(line)) << 4);
+            return *reinterpret_cast<const typename Elem<E>::Frag *>(lds + o);
         } else if constexpr (sizeof(E) == 4) {
             f32x4 v;
             const int c = c0 + m;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int line = sub * 16 + q * 4 + i;
-                v[i] = *reinterpret_cast<const float *>(t + line * (kCpl * 16) + (((c >> 2) ^ swz(line)) << 4) + (c & 3) * 4);
+                const int o = at + line * (kCpl * 16) + (((c >> 2) ^ swz(line)) << 4) + (c & 3) * 4;
+                v[i] = *reinterpret_cast<const float *>(lds + o);
             }
             return v;
         } else {
-            // the transposing read: 16 lanes fetch 4 lines x 16 columns, lane m gets column m
+            // the transposing read: 16 lanes fetch 4 lines x 16 columns, lane m gets
+            // column m (line + 4 has the same chunk order)
             typedef __attribute__((address_space(3))) i16x4 lds_v;
-            const int c = c0 + (m & 3) * 4;
+            const int c = c0 + (m & 3) * 4, line = sub * 32 + q * 8 + (m >> 2);
+            const int o = at + line * (kCpl * 16) + (((c >> 3) ^ swz(line)) << 4) + (c & 4) * 2;
             union { i16x4 h[2]; bf16x8 f; } u;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int line = sub * 32 + q * 8 + i * 4 + (m >> 2);
-                u.h[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (lds_v *)(t + line * (kCpl * 16) + (((c >> 3) ^ swz(line)) << 4) + (c & 4) * 2));
-            }
+            u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v *)(lds + o));
+            u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v *)(lds + o + 4 * kCpl * 16));
             return u.f;
         }
     }
@@ -202,6 +204,13 @@ __device__ inline int xcd_item(int id, int items) {
     return at < share && i < items ? i : -1;
 }
 
+// 16 bytes of every lane from memory into LDS, lane after lane from the wave's
+// uniform address on.
+__device__ inline void load_lds(const char *src, char *dst) {
+    typedef const __attribute__((address_space(1))) void *global_p;
+    typedef __attribute__((address_space(3))) void *lds_p;
+    __builtin_amdgcn_global_load_lds((global_p)src, (lds_p)dst, 16, 0, 0);
+}
 template <int VM>
 __device__ inline void wait_vm() {    // at most VM vector-memory loads in flight
     __builtin_amdgcn_s_waitcnt(0x0F70 | (VM & 15) | (VM >> 4) << 14);

@@ -188,6 +188,23 @@ hwr_status expand(hwr_ops *c, const hwr_groups *g, int32_t dtype, bool ks, const
     return HWR_OK;
 }
 
+constexpr int kLowParts = 4;      // parts of the shrink's contraction, few rows
+
+// Few rows: the weights are streamed (launch_few), with its partial sums in the work space.
+hwr_status few(hwr_ops *c, FewArgs f, bool bf16, bool adapter) {
+    f.m_pad = (f.m + 3) / 4 * 4;
+    f.parts = few_parts(f.g.n, f.g.G, f.k, f.m, bf16, adapter, c->cus);
+    f.low_parts = kLowParts;
+    const uint64_t sums = adapter || f.parts > 1 ? static_cast<uint64_t>(f.parts) * f.g.n * f.m_pad : 0;
+    const uint64_t lows = adapter ? static_cast<uint64_t>(f.low_parts) * f.g.n * f.rank : 0;
+    char *ws = nullptr;
+    if (hwr_status st = workspace(c, (sums + lows) * sizeof(float), &ws)) return st;
+    f.partial = reinterpret_cast<float *>(ws);
+    f.low = f.partial + sums;
+    OPS_HIP(c, launch_few(bf16, adapter, f, c->stream));
+    return HWR_OK;
+}
+
 // ---------------------------------------------------------------- operators
 hwr_status group_rows(hwr_ops *c, int32_t n, const int32_t *choice, const int32_t *table, int32_t n_table, int32_t n_groups,
                       int32_t *offsets, int32_t *order) {
@@ -216,6 +233,19 @@ hwr_status grouped_matmul(hwr_ops *c, const hwr_groups *g, const hwr_matmul_args
     if (!a->x || !a->w || !a->y) return invalid(c, "x, w and y are required");
     if (misaligned(a->dtype, {a->x, a->w, a->y})) return invalid(c, "a pointer is not aligned to its elements");
     if (hwr_status st = use_device(c)) return st;
+    if (few_rows(g->n, g->n_groups, false)) {
+        FewArgs f{};
+        f.g = groups_arg(g);
+        f.k = a->k;
+        f.m = a->m;
+        f.x = a->x;
+        f.ldx = dense(a->ldx, a->k);
+        f.w = a->w;
+        f.w_stride = static_cast<int64_t>(a->k) * a->m;
+        f.y = a->y;
+        f.ldy = dense(a->ldy, a->m);
+        return few(c, f, a->dtype == HWR_BF16, false);
+    }
     RowsArgs r{};
     r.g = groups_arg(g);
     r.k = a->k;
@@ -285,9 +315,25 @@ hwr_status adapter_matmul(hwr_ops *c, const hwr_groups *g, const hwr_adapter_arg
     if (misaligned(a->dtype, {a->x, a->w, a->a, a->b, a->y}) || misaligned(HWR_F32, {a->scale}))
         return invalid(c, "a pointer is not aligned to its elements");
     if (hwr_status st = use_device(c)) return st;
+    const int64_t ldx = dense(a->ldx, a->k);
+    if (few_rows(g->n, g->n_groups, true)) {
+        FewArgs f{};
+        f.g = groups_arg(g);
+        f.k = a->k;
+        f.m = a->m;
+        f.rank = a->rank;
+        f.x = a->x;
+        f.ldx = ldx;
+        f.w = a->w;
+        f.y = a->y;
+        f.ldy = dense(a->ldy, a->m);
+        f.a = a->a;
+        f.b = a->b;
+        f.scale = a->scale;
+        return few(c, f, a->dtype == HWR_BF16, true);
+    }
     char *low = nullptr;
     if (hwr_status st = workspace(c, low_bytes(g->n, a->rank), &low)) return st;
-    const int64_t ldx = dense(a->ldx, a->k);
     if (hwr_status st = shrink(c, g, a->dtype, true, a->x, ldx, a->k, a->a, a->rank, a->scale, low)) return st;
     return expand(c, g, a->dtype, true, a->x, ldx, a->k, a->w, a->m, low, a->b, a->rank, a->y, dense(a->ldy, a->m));
 }

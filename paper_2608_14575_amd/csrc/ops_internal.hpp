@@ -47,6 +47,24 @@ struct ColsArgs {
     const void *zeros;
 };
 
+// Few rows: y = x w_g, or with an adapter x w + scale[g] (x a_g) b_g, by streaming the weights.
+constexpr int kFewRows = 64, kFewTile = 16;
+struct FewArgs {
+    GroupsArg g;
+    int k, m, m_pad, rank;        // m_pad: m up to a multiple of 4
+    const void *x;
+    int64_t ldx;                  // elements
+    const void *w;                // [k][m], groups w_stride elements apart
+    int64_t w_stride;
+    void *y;
+    int64_t ldy;
+    const void *a, *b;            // adapters
+    const float *scale;
+    int parts, low_parts;         // parts of the contraction
+    float *partial;               // [parts][n][m_pad], with parts > 1 or an adapter
+    float *low;                   // [low_parts][n][rank]
+};
+
 struct GroupRowsArgs {
     int n, n_table, G;
     const int32_t *choice, *table;
@@ -61,6 +79,10 @@ hipError_t launch_group_rows(const GroupRowsArgs &a, hipStream_t s);
 int group_rows_blocks(int n);
 // ks: weights [k][m]; else [m][k]
 hipError_t launch_rows(bool bf16, RowsKind kind, bool ks, const RowsArgs &a, int cus, hipStream_t s);
+bool few_rows(int n, int G, bool adapter);              // whether launch_few is meant for the batch
+int few_tiles(int n, int G, bool adapter);
+int few_parts(int n, int G, int k, int m, bool bf16, bool adapter, int cus);
+hipError_t launch_few(bool bf16, bool adapter, const FewArgs &a, hipStream_t s);
 enum class ColsKind { kDense, kLowP, kLowQ };
 hipError_t launch_cols(bool bf16, ColsKind kind, const ColsArgs &a, int cus, hipStream_t s);
 

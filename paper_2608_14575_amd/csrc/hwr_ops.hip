@@ -153,18 +153,8 @@ uint64_t low_bytes(int n, int rank) { return static_cast<uint64_t>(n) * rank_blo
 // low[place] = scale[g] x[row] w_g
 hwr_status shrink(hwr_ops *c, const hwr_groups *g, int32_t dtype, bool ks, const void *x, int64_t ldx, int k, const void *w,
                   int rank, const float *scale, void *low) {
-    RowsArgs r{};
-    r.g = groups_arg(g);
-    r.k = k;
-    r.m = rank;
-    r.x = x;
-    r.ldx = ldx;
-    r.w = w;
-    r.w_stride = static_cast<int64_t>(k) * rank;
-    r.y = low;
-    r.scale = scale;
-    r.zeros = c->zeros;
-    OPS_HIP(c, launch_rows(dtype == HWR_BF16, RowsKind::kShrink, ks, r, c->cus, c->stream));
+    const ShrinkArgs r{groups_arg(g), k, rank, x, ldx, w, scale, low};
+    OPS_HIP(c, launch_shrink(dtype == HWR_BF16, ks, r, c->cus, c->stream));
     return HWR_OK;
 }
 

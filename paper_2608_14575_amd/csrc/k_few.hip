@@ -19,18 +19,6 @@ namespace {
 
 constexpr int kWaves = 8;
 
-// Operand fragment j of V 16-byte vectors: element j of each.
-__device__ inline bf16x8 column(const u32x4 (&in)[8], int j) {
-    union { u32x4 v; bf16x8 f; } o;
-    const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;   // high or low halves
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o.v[i] = __builtin_amdgcn_perm(in[2 * i + 1][j >> 1], in[2 * i][j >> 1], sel);
-    return o.f;
-}
-__device__ inline f32x4 column(const u32x4 (&in)[4], int j) {
-    return f32x4{__uint_as_float(in[0][j]), __uint_as_float(in[1][j]), __uint_as_float(in[2][j]), __uint_as_float(in[3][j])};
-}
-
 // low[s][place][r]: partial sums of x[row] a_g over the s-th part of the contraction
 template <class E>
 __device__ void few_shrink(const FewArgs &a, int item, float *lds) {
@@ -84,7 +72,10 @@ __global__ void __launch_bounds__(kWaves * 64, 4) k_few(FewArgs a) {   // two wo
         item -= a.g.n * a.low_parts;
     }
     const int ct = (a.m + BN - 1) / BN;
-    const int s = item % a.parts, tc = item / a.parts, t = tc / ct, c0 = tc % ct * BN;
+    const int s = item % a.parts, tc = item / a.parts, t = tc / ct;
+    // the last tile of columns ends with the row: it shares columns with the one before
+    // (both give them the same bits), and no chunk is cut
+    const int c0 = a.m < BN ? 0 : min(tc % ct * BN, a.m - BN);
     RowTile rt;
     if (ADAPTER) {
         rt = {0, t * BM, min(t * BM + BM, a.g.n)};
@@ -162,7 +153,7 @@ __global__ void __launch_bounds__(kWaves * 64, 4) k_few(FewArgs a) {   // two wo
             for (int j = 0; j < V; j += 4) {
                 const int c = c0 + (4 * q + e) * V + j;
                 if (c < a.m_pad)
-                    *reinterpret_cast<f32x4 *>(out + c) = f32x4{acc[j][e], acc[j + 1][e], acc[j + 2][e], acc[j + 3][e]};
+                    *reinterpret_cast<f32x4_a4 *>(out + c) = f32x4{acc[j][e], acc[j + 1][e], acc[j + 2][e], acc[j + 3][e]};
             }
     } else if (row >= 0) {
         E *y = static_cast<E *>(a.y) + row * a.ldy;
@@ -253,14 +244,15 @@ int few_tiles(int n, int G, bool adapter) {
     return adapter ? (n + kFewTile - 1) / kFewTile : n / kFewTile + (n < G + 1 ? n : G + 1);
 }
 
-// Workgroups that share a tile's contraction: enough to occupy half of the compute
-// units, while every wave has a step of its own (4096 x 4096 bf16: one row 21.4 /
+// Workgroups that share a tile's contraction: enough to occupy the compute units (half of
+// them beside the shrink's workgroups), while every wave has a step of its own (4096 x 4096 bf16: one row 21.4 /
 // 13.6 / 10.7 / 10.6 us in 1 / 2 / 4 / 8 parts, 48 rows 14.8 / 18.5 / 22.1 in 2 / 4 / 8).
 int few_parts(int n, int G, int k, int m, bool bf16, bool adapter, int cus) {
     const int v = bf16 ? 8 : 4, steps = (k + 4 * v - 1) / (4 * v);
     const int64_t tiles = static_cast<int64_t>(few_tiles(n, G, adapter)) * ((m + 16 * v - 1) / (16 * v));
     int parts = 1;
-    while (tiles * parts < cus / 2 && parts * 2 * kWaves <= steps) parts *= 2;
+    const int enough = adapter ? cus / 2 : cus;
+    while (tiles * parts < enough && parts * 2 * kWaves <= steps) parts *= 2;
     return parts;
 }
 

@@ -1,6 +1,5 @@
 // Products by row: every row of a routed batch with the weights of its group
-// (kGrouped), with shared weights plus its group's low-rank adapter (kAdapter),
-// or into the low-rank intermediate (kShrink).
+// (kGrouped), or with shared weights plus its group's low-rank adapter (kAdapter).
 #include "ops_device.hpp"
 
 namespace hwr {
@@ -109,63 +108,31 @@ __device__ inline void add_adapters(const RowsArgs &a, const RowTile &rt, int c0
 }
 
 // A lane holds, for row l % 16 of fragment i, four columns of fragment j.
-template <class E, RowsKind KIND, int BM, int BN, int WR, int WC>
-__device__ inline void store_rows(const RowsArgs &a, const RowTile &rt, int c0, const int *rows,
+template <class E, int BM, int BN, int WR, int WC>
+__device__ inline void store_rows(const RowsArgs &a, int c0, const int *rows,
                                   const f32x4 (&acc)[BM / WR / 16][BN / WC / 16], int tid) {
     constexpr int RF = BM / WR / 16, CF = BN / WC / 16;
     using El = Elem<E>;
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WC, wc = wave % WC;
     const int q = lane >> 4;
-    if constexpr (KIND == RowsKind::kShrink) {
-        const float s = a.scale ? a.scale[rt.g] : 1.0f;
-        const int blocks = (a.m + kRankBlock - 1) / kRankBlock;
+    E *y = static_cast<E *>(a.y);
+    const bool vec = (a.m & 3) == 0 && (a.ldy & 3) == 0 && (reinterpret_cast<uintptr_t>(y) & (4 * sizeof(E) - 1)) == 0;
 #pragma unroll
-        for (int i = 0; i < RF; ++i) {
-            const int p = rt.p0 + (wr * RF + i) * 16 + (lane & 15);
-            if (p >= rt.p1) continue;
+    for (int i = 0; i < RF; ++i) {
+        const int r = rows[(wr * RF + i) * 16 + (lane & 15)];
+        if (r < 0) continue;
+        E *line = y + r * a.ldy;
 #pragma unroll
-            for (int j = 0; j < CF; ++j) {
-                const int c = c0 + (wc * CF + j) * 16 + q * 4;
-                if (c >= blocks * kRankBlock) continue;
-                char *at = static_cast<char *>(a.y) + (static_cast<int64_t>(p) * blocks + c / kRankBlock) * kLowBytes;
-                f32x4 v;
+        for (int j = 0; j < CF; ++j) {
+            const int c = c0 + (wc * CF + j) * 16 + q * 4;
+            typename El::Out4 o;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = c + e < a.m ? acc[i][j][e] * s : 0.0f;   // not 0 * inf past the rank
-                if constexpr (sizeof(E) == 4) {
-                    *reinterpret_cast<f32x4 *>(at + c % kRankBlock * 4) = v;
-                } else {
-                    bf16x4 hi, lo;
+            for (int e = 0; e < 4; ++e) o[e] = static_cast<E>(acc[i][j][e]);
+            if (vec && c < a.m) *reinterpret_cast<typename El::Out4 *>(line + c) = o;
+            else {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        hi[e] = static_cast<__bf16>(v[e]);
-                        const float h = static_cast<float>(hi[e]);
-                        lo[e] = static_cast<__bf16>(__builtin_isfinite(h) ? v[e] - h : 0.0f);
-                    }
-                    *reinterpret_cast<bf16x4 *>(at + c % kRankBlock * 2) = hi;
-                    *reinterpret_cast<bf16x4 *>(at + 64 + c % kRankBlock * 2) = lo;
-                }
-            }
-        }
-    } else {
-        E *y = static_cast<E *>(a.y);
-        const bool vec = (a.m & 3) == 0 && (a.ldy & 3) == 0 && (reinterpret_cast<uintptr_t>(y) & (4 * sizeof(E) - 1)) == 0;
-#pragma unroll
-        for (int i = 0; i < RF; ++i) {
-            const int r = rows[(wr * RF + i) * 16 + (lane & 15)];
-            if (r < 0) continue;
-            E *line = y + r * a.ldy;
-#pragma unroll
-            for (int j = 0; j < CF; ++j) {
-                const int c = c0 + (wc * CF + j) * 16 + q * 4;
-                typename El::Out4 o;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = static_cast<E>(acc[i][j][e]);
-                if (vec && c < a.m) *reinterpret_cast<typename El::Out4 *>(line + c) = o;
-                else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (c + e < a.m) line[c + e] = o[e];
-                }
+                for (int e = 0; e < 4; ++e)
+                    if (c + e < a.m) line[c + e] = o[e];
             }
         }
     }
@@ -183,7 +150,9 @@ __device__ inline bool my_tile(const RowsArgs &a, int lane, RowTile &rt, int &c0
     if (item < 0) return false;
     const int panel = item / (8 * ct) * 8, in = item - panel * ct, rp = min(8, tiles - panel);
     const int t = panel + in % rp;
-    c0 = in / rp * BN;
+    // the last tile of columns ends with the row: it shares columns with the one before
+    // (both give them the same bits), and no chunk is cut
+    c0 = a.m < BN ? 0 : min(in / rp * BN, a.m - BN);
     if (KIND == RowsKind::kAdapter) rt = {0, t * BM, min(t * BM + BM, a.g.n)};
     else rt = find_tile(a.g, t, BM, tail, lane);
     return true;
@@ -260,7 +229,7 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows(RowsArgs a) {
     }
 
     if constexpr (KIND == RowsKind::kAdapter) add_adapters<E, KS, BM, BN, WR, WC>(a, rt, c0, sx, sw, acc, tid);
-    store_rows<E, KIND, BM, BN, WR, WC>(a, rt, c0, rows, acc, tid);
+    store_rows<E, BM, BN, WR, WC>(a, c0, rows, acc, tid);
 }
 
 // Whole chunks of 16 bytes everywhere: operands go from memory straight into LDS,
@@ -366,7 +335,7 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows_direct(RowsArgs a) {
     }
 
     if constexpr (KIND == RowsKind::kAdapter) add_adapters<E, KS, BM, BN, WR, WC>(a, rt, c0, buf0, buf0 + XT::kBytes, acc, tid);
-    store_rows<E, KIND, BM, BN, WR, WC>(a, rt, c0, rows, acc, tid);
+    store_rows<E, BM, BN, WR, WC>(a, c0, rows, acc, tid);
 }
 
 template <class E, RowsKind KIND, bool KS, int BM, int BN, int WR, int WC, bool DIRECT = false>
@@ -391,35 +360,32 @@ bool whole_chunks(const RowsArgs &a) {
 }
 
 template <class E, RowsKind KIND, bool KS>
-hipError_t pick(const RowsArgs &a, hipStream_t s) {
-    if constexpr (KIND == RowsKind::kShrink) {
-        if (a.m <= 32) return go<E, KIND, KS, 32, 32, 2, 1>(a, s);
-        return go<E, KIND, KS, 32, 64, 2, 2>(a, s);
-    } else {
-        const bool small = KIND == RowsKind::kAdapter ? a.g.n <= 64 : a.g.n <= 64 * a.g.G;
-        if (small) return go<E, KIND, KS, 16, 64, 1, 4>(a, s);
-        if (whole_chunks<E, KS>(a)) {
-            if constexpr (sizeof(E) == 2) return go<E, KIND, KS, 256, 256, 2, 4, true>(a, s);
-            else return go<E, KIND, KS, 128, 128, 2, 2, true>(a, s);
-        }
-        return go<E, KIND, KS, 128, 128, 2, 2>(a, s);
+hipError_t pick(const RowsArgs &a, int cus, hipStream_t s) {
+    // the largest tile that still gives every compute unit a workgroup
+    auto tiles = [&](int64_t bm, int64_t bn) {
+        return (a.g.n / bm + (KIND == RowsKind::kAdapter ? 1 : a.g.G)) * ((a.m + bn - 1) / bn);
+    };
+    if (whole_chunks<E, KS>(a)) {
+        if constexpr (sizeof(E) == 2)
+            if (tiles(256, 256) >= cus) return go<E, KIND, KS, 256, 256, 2, 4, true>(a, s);
+        if (tiles(128, 128) >= cus) return go<E, KIND, KS, 128, 128, 2, 2, true>(a, s);
+        return go<E, KIND, KS, 64, 64, 2, 2, true>(a, s);
     }
+    if (tiles(128, 128) >= cus) return go<E, KIND, KS, 128, 128, 2, 2>(a, s);
+    return go<E, KIND, KS, 64, 64, 2, 2>(a, s);
 }
 
 template <class E>
-hipError_t pick_kind(RowsKind kind, bool ks, const RowsArgs &a, hipStream_t s) {
-    switch (kind) {
-    case RowsKind::kGrouped: return ks ? pick<E, RowsKind::kGrouped, true>(a, s) : pick<E, RowsKind::kGrouped, false>(a, s);
-    case RowsKind::kAdapter: return ks ? pick<E, RowsKind::kAdapter, true>(a, s) : pick<E, RowsKind::kAdapter, false>(a, s);
-    default: return ks ? pick<E, RowsKind::kShrink, true>(a, s) : pick<E, RowsKind::kShrink, false>(a, s);
-    }
+hipError_t pick_kind(RowsKind kind, bool ks, const RowsArgs &a, int cus, hipStream_t s) {
+    if (kind == RowsKind::kGrouped)
+        return ks ? pick<E, RowsKind::kGrouped, true>(a, cus, s) : pick<E, RowsKind::kGrouped, false>(a, cus, s);
+    return ks ? pick<E, RowsKind::kAdapter, true>(a, cus, s) : pick<E, RowsKind::kAdapter, false>(a, cus, s);
 }
 
 }  // namespace
 
 hipError_t launch_rows(bool bf16, RowsKind kind, bool ks, const RowsArgs &a, int cus, hipStream_t s) {
-    (void)cus;
-    return bf16 ? pick_kind<__bf16>(kind, ks, a, s) : pick_kind<float>(kind, ks, a, s);
+    return bf16 ? pick_kind<__bf16>(kind, ks, a, cus, s) : pick_kind<float>(kind, ks, a, cus, s);
 }
 
 }  // namespace hwr

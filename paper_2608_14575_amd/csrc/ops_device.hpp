@@ -18,6 +18,7 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 // 16 bytes at any element alignment
 typedef uint32_t u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
 
 template <class E>
 struct Elem;
@@ -117,6 +118,36 @@ __device__ inline u32x4 load_chunk(const E *line, int e, int len) {
     for (int i = 0; i < kEpc; ++i)
         if (e + i < len) u.s[i] = line[e + i];
     return u.v;
+}
+
+// Operand fragment j of V 16-byte vectors: element j of each.
+__device__ inline bf16x8 column(const u32x4 (&in)[8], int j) {
+    union { u32x4 v; bf16x8 f; } o;
+    const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;   // high or low halves
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o.v[i] = __builtin_amdgcn_perm(in[2 * i + 1][j >> 1], in[2 * i][j >> 1], sel);
+    return o.f;
+}
+__device__ inline f32x4 column(const u32x4 (&in)[4], int j) {
+    return f32x4{__uint_as_float(in[0][j]), __uint_as_float(in[1][j]), __uint_as_float(in[2][j]), __uint_as_float(in[3][j])};
+}
+
+// Four values of a low-rank intermediate, at column c of its 128-byte block.
+template <class E>
+__device__ inline void store_low(char *block, int c, f32x4 v) {
+    if constexpr (sizeof(E) == 4) {
+        *reinterpret_cast<f32x4 *>(block + c * 4) = v;
+    } else {
+        bf16x4 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            hi[e] = static_cast<__bf16>(v[e]);
+            const float h = static_cast<float>(hi[e]);
+            lo[e] = static_cast<__bf16>(__builtin_isfinite(h) ? v[e] - h : 0.0f);
+        }
+        *reinterpret_cast<bf16x4 *>(block + c * 2) = hi;
+        *reinterpret_cast<bf16x4 *>(block + kLowBytes / 2 + c * 2) = lo;
+    }
 }
 
 // ---------------------------------------------------------------- groups

@@ -32,8 +32,17 @@ struct RowsArgs {
     const void *low;              // [n][blocks] low-rank intermediates
     const void *lw;               // [G][rank][m] (KS) or [G][m][rank]
     int rank;
-    // shrink: y is the low-rank intermediate, scaled
+};
+
+// low[place] = scale[g] x[row] w_g
+struct ShrinkArgs {
+    GroupsArg g;
+    int k, rank;
+    const void *x;
+    int64_t ldx;                  // elements
+    const void *w;                // [G][k][rank] (KS) or [G][rank][k]
     const float *scale;           // [G] or null
+    void *low;
 };
 
 // Weight gradients: out[g][p][q] = sum over places of g of P[place][p] Q[place][q].
@@ -73,12 +82,13 @@ struct GroupRowsArgs {
     int blocks;
 };
 
-enum class RowsKind { kGrouped, kAdapter, kShrink };
+enum class RowsKind { kGrouped, kAdapter };
 
 hipError_t launch_group_rows(const GroupRowsArgs &a, hipStream_t s);
 int group_rows_blocks(int n);
 // ks: weights [k][m]; else [m][k]
 hipError_t launch_rows(bool bf16, RowsKind kind, bool ks, const RowsArgs &a, int cus, hipStream_t s);
+hipError_t launch_shrink(bool bf16, bool ks, const ShrinkArgs &a, int cus, hipStream_t s);
 bool few_rows(int n, int G, bool adapter);              // whether launch_few is meant for the batch
 int few_tiles(int n, int G, bool adapter);
 int few_parts(int n, int G, int k, int m, bool bf16, bool adapter, int cus);

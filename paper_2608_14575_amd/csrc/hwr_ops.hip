@@ -2,6 +2,7 @@
 // space and launches.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstring>
 #include <string>
 #include <vector>
@@ -178,6 +179,22 @@ hwr_status expand(hwr_ops *c, const hwr_groups *g, int32_t dtype, bool ks, const
     return HWR_OK;
 }
 
+// out[g] = P^T Q, with the partial sums past the first `used` bytes of the work space
+// (the call has reserved them: weight_grad_bytes).
+uint64_t weight_grad_bytes(hwr_ops *c, bool bf16, ColsKind kind, const ColsArgs &w) {
+    const int parts = cols_parts(bf16, kind, w, c->cus);
+    return parts > 1 ? static_cast<uint64_t>(parts) * w.g.G * w.np * w.nq * sizeof(float) : 0;
+}
+hwr_status weight_grad(hwr_ops *c, bool bf16, ColsKind kind, ColsArgs w, uint64_t used) {
+    char *ws = nullptr;
+    if (hwr_status st = workspace(c, used + weight_grad_bytes(c, bf16, kind, w), &ws)) return st;
+    w.parts = cols_parts(bf16, kind, w, c->cus);
+    w.partial = reinterpret_cast<float *>(ws + used);
+    w.zeros = c->zeros;
+    OPS_HIP(c, launch_cols(bf16, kind, w, c->cus, c->stream));
+    return HWR_OK;
+}
+
 constexpr int kLowParts = 4;      // parts of the shrink's contraction, few rows
 
 // Few rows: the weights are streamed (launch_few), with its partial sums in the work space.
@@ -287,8 +304,7 @@ hwr_status grouped_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_matmul
         w.ldp = dense(a->ldx, a->k);
         w.ldq = dense(a->lddy, a->m);
         w.out = a->dw;
-        w.zeros = c->zeros;
-        OPS_HIP(c, launch_cols(bf16, ColsKind::kDense, w, c->cus, c->stream));
+        if (hwr_status st = weight_grad(c, bf16, ColsKind::kDense, w, 0)) return st;
     }
     return HWR_OK;
 }
@@ -345,8 +361,23 @@ hwr_status adapter_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_adapte
     const bool bf16 = a->dtype == HWR_BF16;
     const int64_t lddy = dense(a->lddy, a->m), ldx = dense(a->ldx, a->k);
     const uint64_t each = low_bytes(g->n, a->rank);
+    ColsArgs wa{}, wb{};
+    wa.g = wb.g = groups_arg(g);
+    wa.blocks = wb.blocks = rank_blocks(a->rank);
+    wa.np = a->k;
+    wa.nq = a->rank;
+    wa.p = a->x;
+    wa.ldp = ldx;
+    wa.out = a->da;
+    wb.np = a->rank;
+    wb.nq = a->m;
+    wb.q = a->dy;
+    wb.ldq = lddy;
+    wb.out = a->db;
+    const uint64_t parts = std::max(a->da ? weight_grad_bytes(c, bf16, ColsKind::kLowQ, wa) : 0,
+                                    a->db ? weight_grad_bytes(c, bf16, ColsKind::kLowP, wb) : 0);
     char *ws = nullptr;
-    if (hwr_status st = workspace(c, 2 * each, &ws)) return st;
+    if (hwr_status st = workspace(c, 2 * each + parts, &ws)) return st;
     char *up = ws, *low = ws + each;
     if (g->n > 0 && (a->dx || a->da))
         if (hwr_status st = shrink(c, g, a->dtype, false, a->dy, lddy, a->m, a->b, a->rank, a->scale, up)) return st;
@@ -356,27 +387,13 @@ hwr_status adapter_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_adapte
         if (hwr_status st = expand(c, g, a->dtype, false, a->dy, lddy, a->m, a->w, a->k, up, a->a, a->rank, a->dx,
                                    dense(a->lddx, a->k)))
             return st;
-    ColsArgs w{};
-    w.g = groups_arg(g);
-    w.blocks = rank_blocks(a->rank);
-    w.zeros = c->zeros;
     if (a->da) {
-        w.np = a->k;
-        w.nq = a->rank;
-        w.p = a->x;
-        w.ldp = ldx;
-        w.q = up;
-        w.out = a->da;
-        OPS_HIP(c, launch_cols(bf16, ColsKind::kLowQ, w, c->cus, c->stream));
+        wa.q = up;
+        if (hwr_status st = weight_grad(c, bf16, ColsKind::kLowQ, wa, 2 * each)) return st;
     }
     if (a->db) {
-        w.np = a->rank;
-        w.nq = a->m;
-        w.p = low;
-        w.q = a->dy;
-        w.ldq = lddy;
-        w.out = a->db;
-        OPS_HIP(c, launch_cols(bf16, ColsKind::kLowP, w, c->cus, c->stream));
+        wb.p = low;
+        if (hwr_status st = weight_grad(c, bf16, ColsKind::kLowP, wb, 2 * each)) return st;
     }
     return HWR_OK;
 }

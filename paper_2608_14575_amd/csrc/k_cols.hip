@@ -1,80 +1,60 @@
 // Weight gradients of a routed batch: out[g] = P^T Q over the places of group
 // g, with P and Q rows of the batch (through the row order) or low-rank
 // intermediates (by place).
+//
+// Both factors are staged by place, 64 (bf16) or 32 (fp32) places to a stage, and
+// read by columns.  Where the output has few tiles, workgroups share a tile's
+// places and write fp32 partial sums that k_cols_sum adds, in order.
 #include "ops_device.hpp"
 
 namespace hwr {
 namespace {
 
-template <class E, ColsKind KIND, int BP, int BQ, int WP, int WQ>
-__global__ void __launch_bounds__(WP *WQ * 64) k_cols(ColsArgs a) {
-    using El = Elem<E>;
-    constexpr int NT = WP * WQ * 64, PF = BP / WP / 16, QF = BQ / WQ / 16, kBk = El::kBk;
-    using PT = Tile<E, true, BP>;
-    using QT = Tile<E, true, BQ>;
-    // a rank block as a tile: 32 columns, in bf16 hi then lo
-    constexpr int kLowCols = kLowBytes / sizeof(E);
-    static_assert(KIND != ColsKind::kLowP || (BP == kLowCols && WP == 1));
-    static_assert(KIND != ColsKind::kLowQ || (BQ == kLowCols && WQ == 1));
-    __shared__ __attribute__((aligned(16))) char sp[PT::kBytes], sq[QT::kBytes];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wp = wave / WQ, wq = wave % WQ;
-    const int g = blockIdx.y;
+// The workgroup's tile of the output and places.
+struct ColsTile {
+    int g, ip, iq, part, p0, p1;
+};
+
+// Tiles of a group go in panels of 8 row tiles, as the products by row; parts side by side.
+template <ColsKind KIND, int BP, int BQ, int kBk>
+__device__ inline bool my_tile(const ColsArgs &a, ColsTile &t) {
     const int tp = KIND == ColsKind::kLowP ? a.blocks : (a.np + BP - 1) / BP;
-    const int ip = blockIdx.x % tp, iq = blockIdx.x / tp;
-    const int pc = ip * BP, qc = iq * BQ;
-    const int p0 = place_of(a.g, g), p1 = place_of(a.g, g + 1);
-
-    f32x4 acc[PF][QF] = {};
-    constexpr int UP = PT::kChunks / NT, UQ = QT::kChunks / NT;
-    static_assert(PT::kChunks % NT == 0 && QT::kChunks % NT == 0);
-    auto chunk = [&](const void *src, int64_t ld, int width, int c0, bool low, int block, int place, int c) {
-        if (place >= p1) return u32x4{0, 0, 0, 0};
-        if (low)
-            return *reinterpret_cast<const u32x4 *>(static_cast<const char *>(src) +
-                                                    (static_cast<int64_t>(place) * a.blocks + block) * kLowBytes + c * 16);
-        const int r = row_at(a.g, place);
-        return load_chunk<E>(r >= 0 ? static_cast<const E *>(src) + r * ld : nullptr, c0 + c * El::kEpc, width);
-    };
-    for (int p = p0; p < p1; p += kBk) {
-        u32x4 vp[UP], vq[UQ];
-#pragma unroll
-        for (int i = 0; i < UP; ++i) {
-            const int u = i * NT + tid, line = u / PT::kCpl, c = (u % PT::kCpl) ^ PT::swz(line);
-            vp[i] = chunk(a.p, a.ldp, a.np, pc, KIND == ColsKind::kLowP, ip, p + line, c);
-        }
-#pragma unroll
-        for (int i = 0; i < UQ; ++i) {
-            const int u = i * NT + tid, line = u / QT::kCpl, c = (u % QT::kCpl) ^ QT::swz(line);
-            vq[i] = chunk(a.q, a.ldq, a.nq, qc, KIND == ColsKind::kLowQ, iq, p + line, c);
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < UP; ++i) *reinterpret_cast<u32x4 *>(sp + (i * NT + tid) * 16) = vp[i];
-#pragma unroll
-        for (int i = 0; i < UQ; ++i) *reinterpret_cast<u32x4 *>(sq + (i * NT + tid) * 16) = vq[i];
-        __syncthreads();
-#pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-            typename El::Frag fq[QF], fp[PF];
-#pragma unroll
-            for (int j = 0; j < QF; ++j) fq[j] = QT::frag(sq, 0, (wq * QF + j) * 16, sub, lane);
-#pragma unroll
-            for (int i = 0; i < PF; ++i) fp[i] = PT::frag(sp, 0, (wp * PF + i) * 16, sub, lane);
-#pragma unroll
-            for (int i = 0; i < PF; ++i)
-#pragma unroll
-                for (int j = 0; j < QF; ++j) acc[i][j] = El::mma(fq[j], fp[i], acc[i][j]);
-        }
+    const int tq = KIND == ColsKind::kLowQ ? a.blocks : (a.nq + BQ - 1) / BQ;
+    const int per = tp * tq * a.parts;
+    const int item = xcd_item(blockIdx.x, a.g.G * per);
+    if (item < 0) return false;
+    t.g = item / per;
+    const int in_group = item % per, tile = in_group / a.parts;
+    t.part = in_group % a.parts;
+    const int panel = tile / (8 * tq) * 8, in = tile - panel * tq, rp = min(8, tp - panel);
+    t.ip = panel + in % rp;
+    t.iq = in / rp;
+    t.p0 = place_of(a.g, t.g);
+    t.p1 = place_of(a.g, t.g + 1);
+    if (a.parts > 1) {                     // whole stages each
+        const int stages = max(0, t.p1 - t.p0 + kBk - 1) / kBk;
+        const int s0 = static_cast<int>(static_cast<int64_t>(stages) * t.part / a.parts),
+                  s1 = static_cast<int>(static_cast<int64_t>(stages) * (t.part + 1) / a.parts);
+        t.p1 = min(t.p1, t.p0 + s1 * kBk);
+        t.p0 += s0 * kBk;
     }
+    return true;
+}
 
-    // lane: P column l % 16 of fragment i, four Q columns of fragment j
-    E *out = static_cast<E *>(a.out) + static_cast<int64_t>(g) * a.np * a.nq;
+// Lane: P column l % 16 of fragment i, four Q columns of fragment j.
+template <class E, ColsKind KIND, int BP, int BQ, int WP, int WQ>
+__device__ inline void store_tile(const ColsArgs &a, const ColsTile &t, const f32x4 (&acc)[BP / WP / 16][BQ / WQ / 16],
+                                  int lane, int wp, int wq) {
+    using El = Elem<E>;
+    constexpr int PF = BP / WP / 16, QF = BQ / WQ / 16;
     constexpr bool kPair = sizeof(E) == 2;    // low-rank sides hold hi and lo columns
     constexpr int PN = KIND == ColsKind::kLowP ? 2 : PF, QN = KIND == ColsKind::kLowQ ? 2 : QF;
-    const int p_first = KIND == ColsKind::kLowP ? ip * kRankBlock : pc + wp * PF * 16;
-    const int q_first = KIND == ColsKind::kLowQ ? iq * kRankBlock : qc + wq * QF * 16;
-    const bool vec = (a.nq & 3) == 0 && (reinterpret_cast<uintptr_t>(a.out) & (4 * sizeof(E) - 1)) == 0;
+    const int p_first = KIND == ColsKind::kLowP ? t.ip * kRankBlock : t.ip * BP + wp * PF * 16;
+    const int q_first = KIND == ColsKind::kLowQ ? t.iq * kRankBlock : t.iq * BQ + wq * QF * 16;
+    const int64_t each = static_cast<int64_t>(a.np) * a.nq;
+    E *out = static_cast<E *>(a.out) + t.g * each;
+    float *part = a.partial + (static_cast<int64_t>(t.part) * a.g.G + t.g) * each;
+    const bool vec = (a.nq & 3) == 0 && (a.parts > 1 || (reinterpret_cast<uintptr_t>(a.out) & (4 * sizeof(E) - 1)) == 0);
 #pragma unroll
     for (int i = 0; i < PN; ++i) {
         const int pr = p_first + i * 16 + (lane & 15);
@@ -89,42 +69,279 @@ __global__ void __launch_bounds__(WP *WQ * 64) k_cols(ColsArgs a) {
                 for (int e = 0; e < 4; ++e) v[e] = __builtin_isfinite(v[e]) ? v[e] + lo[e] : v[e];
             }
             const int c = q_first + j * 16 + (lane >> 4) * 4;
-            E *line = out + static_cast<int64_t>(pr) * a.nq;
+            const int64_t at = static_cast<int64_t>(pr) * a.nq + c;
+            if (a.parts > 1) {
+                if (vec && c < a.nq) *reinterpret_cast<f32x4 *>(part + at) = v;
+                else
+                    for (int e = 0; e < 4; ++e)
+                        if (c + e < a.nq) part[at + e] = v[e];
+                continue;
+            }
             typename El::Out4 o;
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] = static_cast<E>(v[e]);
-            if (vec && c < a.nq) *reinterpret_cast<typename El::Out4 *>(line + c) = o;
+            if (vec && c < a.nq) *reinterpret_cast<typename El::Out4 *>(out + at) = o;
             else {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (c + e < a.nq) line[c + e] = o[e];
+                    if (c + e < a.nq) out[at + e] = o[e];
             }
         }
     }
 }
 
+template <class E, ColsKind KIND, int BP, int BQ>
+struct ColsTiles {
+    using PT = Tile<E, true, BP>;
+    using QT = Tile<E, true, BQ>;
+    // a rank block as a tile: 32 columns, in bf16 hi then lo
+    static constexpr int kLowCols = kLowBytes / sizeof(E);
+    static constexpr bool kLowP = KIND == ColsKind::kLowP, kLowQ = KIND == ColsKind::kLowQ;
+    static_assert(!kLowP || BP == kLowCols);
+    static_assert(!kLowQ || BQ == kLowCols);
+};
+
+template <class E, class PT, class QT, int PF, int QF>
+__device__ inline void multiply_tile(const char *lds, int at_q, int p0, int q0, int lane, f32x4 (&acc)[PF][QF]) {
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub) {
+        typename Elem<E>::Frag fq[QF], fp[PF];
+#pragma unroll
+        for (int j = 0; j < QF; ++j) fq[j] = QT::frag(lds, at_q, q0 + j * 16, sub, lane);
+#pragma unroll
+        for (int i = 0; i < PF; ++i) fp[i] = PT::frag(lds, 0, p0 + i * 16, sub, lane);
+#pragma unroll
+        for (int i = 0; i < PF; ++i)
+#pragma unroll
+            for (int j = 0; j < QF; ++j) acc[i][j] = Elem<E>::mma(fq[j], fp[i], acc[i][j]);
+    }
+}
+
+// Any widths, strides and alignment: operands pass through registers.
 template <class E, ColsKind KIND, int BP, int BQ, int WP, int WQ>
+__global__ void __launch_bounds__(WP *WQ * 64) k_cols(ColsArgs a) {
+    using El = Elem<E>;
+    using TT = ColsTiles<E, KIND, BP, BQ>;
+    using PT = typename TT::PT;
+    using QT = typename TT::QT;
+    static_assert((!TT::kLowP || WP == 1) && (!TT::kLowQ || WQ == 1));
+    constexpr int NT = WP * WQ * 64, PF = BP / WP / 16, QF = BQ / WQ / 16, kBk = El::kBk;
+    __shared__ __attribute__((aligned(16))) char buf[PT::kBytes + QT::kBytes];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wp = wave / WQ, wq = wave % WQ;
+    ColsTile t;
+    if (!my_tile<KIND, BP, BQ, kBk>(a, t)) return;
+
+    f32x4 acc[PF][QF] = {};
+    constexpr int UP = PT::kChunks / NT, UQ = QT::kChunks / NT;
+    static_assert(PT::kChunks % NT == 0 && QT::kChunks % NT == 0);
+    auto chunk = [&](const void *src, int64_t ld, int width, int c0, bool low, int block, int place, int c) {
+        if (place >= t.p1) return u32x4{0, 0, 0, 0};
+        if (low)
+            return *reinterpret_cast<const u32x4 *>(static_cast<const char *>(src) +
+                                                    (static_cast<int64_t>(place) * a.blocks + block) * kLowBytes + c * 16);
+        const int r = row_at(a.g, place);
+        return load_chunk<E>(r >= 0 ? static_cast<const E *>(src) + r * ld : nullptr, c0 + c * El::kEpc, width);
+    };
+    u32x4 vp[UP], vq[UQ];
+    auto load = [&](int p) {
+#pragma unroll
+        for (int i = 0; i < UP; ++i) {
+            const int u = i * NT + tid, line = u / PT::kCpl, c = (u % PT::kCpl) ^ PT::swz(line);
+            vp[i] = chunk(a.p, a.ldp, a.np, t.ip * BP, TT::kLowP, t.ip, p + line, c);
+        }
+#pragma unroll
+        for (int i = 0; i < UQ; ++i) {
+            const int u = i * NT + tid, line = u / QT::kCpl, c = (u % QT::kCpl) ^ QT::swz(line);
+            vq[i] = chunk(a.q, a.ldq, a.nq, t.iq * BQ, TT::kLowQ, t.iq, p + line, c);
+        }
+    };
+    if (t.p0 < t.p1) load(t.p0);
+    for (int p = t.p0; p < t.p1; p += kBk) {
+#pragma unroll
+        for (int i = 0; i < UP; ++i) *reinterpret_cast<u32x4 *>(buf + (i * NT + tid) * 16) = vp[i];
+#pragma unroll
+        for (int i = 0; i < UQ; ++i) *reinterpret_cast<u32x4 *>(buf + PT::kBytes + (i * NT + tid) * 16) = vq[i];
+        __syncthreads();
+        if (p + kBk < t.p1) load(p + kBk);
+        multiply_tile<E, PT, QT, PF, QF>(buf, PT::kBytes, wp * PF * 16, wq * QF * 16, lane, acc);
+        __syncthreads();
+    }
+    store_tile<E, KIND, BP, BQ, WP, WQ>(a, t, acc, lane, wp, wq);
+}
+
+// Whole chunks of 16 bytes everywhere: operands go from memory straight into LDS,
+// the next stage's while this one is multiplied; the rows of the stage after that
+// are looked up meanwhile.  Places past the last are zeros on both sides; columns
+// past the last are loaded from a valid place and not stored.
+template <class E, ColsKind KIND, int BP, int BQ, int WP, int WQ>
+__global__ void __launch_bounds__(WP *WQ * 64) k_cols_direct(ColsArgs a) {
+    using El = Elem<E>;
+    using TT = ColsTiles<E, KIND, BP, BQ>;
+    using PT = typename TT::PT;
+    using QT = typename TT::QT;
+    static_assert((!TT::kLowP || WP == 1) && (!TT::kLowQ || WQ == 1));
+    constexpr int NT = WP * WQ * 64, PF = BP / WP / 16, QF = BQ / WQ / 16, kBk = El::kBk, kEpc = El::kEpc;
+    constexpr int UP = PT::kChunks / NT, UQ = QT::kChunks / NT;
+    static_assert(PT::kChunks % NT == 0 && QT::kChunks % NT == 0);
+    // an array each, so that the compiler sees that reads of one do not depend on the
+    // loads in flight into the other
+    __shared__ __attribute__((aligned(16))) char buf0[PT::kBytes + QT::kBytes], buf1[PT::kBytes + QT::kBytes];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wp = wave / WQ, wq = wave % WQ;
+    ColsTile t;
+    if (!my_tile<KIND, BP, BQ, kBk>(a, t)) return;
+
+    // the thread's chunks: line (place of the stage) and byte within the row
+    int pl[UP], ql[UQ], pb[UP], qb[UQ], pr[UP], qr[UQ];
+#pragma unroll
+    for (int i = 0; i < UP; ++i) {
+        const int u = i * NT + tid, c = (u % PT::kCpl) ^ PT::swz(u / PT::kCpl);
+        pl[i] = u / PT::kCpl;
+        pb[i] = TT::kLowP ? t.ip * kLowBytes + c * 16 : min(t.ip * BP + c * kEpc, a.np - kEpc) * (int)sizeof(E);
+    }
+#pragma unroll
+    for (int i = 0; i < UQ; ++i) {
+        const int u = i * NT + tid, c = (u % QT::kCpl) ^ QT::swz(u / QT::kCpl);
+        ql[i] = u / QT::kCpl;
+        qb[i] = TT::kLowQ ? t.iq * kLowBytes + c * 16 : min(t.iq * BQ + c * kEpc, a.nq - kEpc) * (int)sizeof(E);
+    }
+    auto look_up = [&](int p) {            // rows (or places) of the stage from p on; -1: zeros
+#pragma unroll
+        for (int i = 0; i < UP; ++i) pr[i] = p + pl[i] >= t.p1 ? -1 : TT::kLowP ? p + pl[i] : row_at(a.g, p + pl[i]);
+#pragma unroll
+        for (int i = 0; i < UQ; ++i) qr[i] = p + ql[i] >= t.p1 ? -1 : TT::kLowQ ? p + ql[i] : row_at(a.g, p + ql[i]);
+    };
+    const int64_t pld = TT::kLowP ? a.blocks * kLowBytes : a.ldp * (int64_t)sizeof(E);
+    const int64_t qld = TT::kLowQ ? a.blocks * kLowBytes : a.ldq * (int64_t)sizeof(E);
+    const char *zeros = static_cast<const char *>(a.zeros), *ps = static_cast<const char *>(a.p),
+               *qs = static_cast<const char *>(a.q);
+    auto issue = [&](char *b) {
+#pragma unroll
+        for (int i = 0; i < UP; ++i)
+            load_lds(pr[i] < 0 ? zeros : ps + pr[i] * pld + pb[i], b + (i * NT + wave * 64) * 16);
+#pragma unroll
+        for (int i = 0; i < UQ; ++i)
+            load_lds(qr[i] < 0 ? zeros : qs + qr[i] * qld + qb[i], b + PT::kBytes + (i * NT + wave * 64) * 16);
+    };
+    f32x4 acc[PF][QF] = {};
+    auto multiply = [&](const char *b) {
+        multiply_tile<E, PT, QT, PF, QF>(b, PT::kBytes, wp * PF * 16, wq * QF * 16, lane, acc);
+    };
+    auto finished = [&] {                  // this stage's buffer may be overwritten
+        wait_lds();
+        barrier();
+    };
+    int p = t.p0;
+    if (p < t.p1) {
+        look_up(p);
+        issue(buf0);
+        look_up(p + kBk);
+        for (; p + 2 * kBk < t.p1; p += 2 * kBk) {
+            issue(buf1);
+            look_up(p + 2 * kBk);
+            wait_vm<2 * (UP + UQ)>();      // (the look-up is in flight too)
+            barrier();
+            multiply(buf0);
+            finished();
+            issue(buf0);
+            look_up(p + 3 * kBk);
+            wait_vm<2 * (UP + UQ)>();
+            barrier();
+            multiply(buf1);
+            finished();
+        }
+        if (p + kBk < t.p1) issue(buf1);
+        wait_vm<0>();
+        barrier();
+        multiply(buf0);
+        if (p + kBk < t.p1) multiply(buf1);
+    }
+    store_tile<E, KIND, BP, BQ, WP, WQ>(a, t, acc, lane, wp, wq);
+}
+
+// out = sum of the parts
+template <class E>
+__global__ void __launch_bounds__(256) k_cols_sum(ColsArgs a, int64_t count) {
+    const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
+    if (i >= count) return;
+    if (i + 4 <= count) {
+        f32x4 v = {};
+#pragma unroll 4
+        for (int s = 0; s < a.parts; ++s) v += *reinterpret_cast<const f32x4_a4 *>(a.partial + s * count + i);
+        for (int e = 0; e < 4; ++e) static_cast<E *>(a.out)[i + e] = static_cast<E>(v[e]);
+    } else {
+        for (int64_t j = i; j < count; ++j) {
+            float v = 0.0f;
+            for (int s = 0; s < a.parts; ++s) v += a.partial[s * count + j];
+            static_cast<E *>(a.out)[j] = static_cast<E>(v);
+        }
+    }
+}
+
+// Rows in whole, aligned chunks of 16 bytes.
+template <class E, ColsKind KIND>
+bool whole_chunks(const ColsArgs &a) {
+    constexpr int kEpc = Elem<E>::kEpc;
+    auto whole = [](const void *p, int64_t ld, int width) {
+        return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % kEpc == 0 && width % kEpc == 0;
+    };
+    return (KIND == ColsKind::kLowP || whole(a.p, a.ldp, a.np)) && (KIND == ColsKind::kLowQ || whole(a.q, a.ldq, a.nq));
+}
+
+template <class E, ColsKind KIND, int BP, int BQ, int WP, int WQ, bool DIRECT>
 hipError_t go(const ColsArgs &a, hipStream_t s) {
     const int64_t tp = KIND == ColsKind::kLowP ? a.blocks : (a.np + BP - 1) / BP;
     const int64_t tq = KIND == ColsKind::kLowQ ? a.blocks : (a.nq + BQ - 1) / BQ;
-    return launch_kernel(k_cols<E, KIND, BP, BQ, WP, WQ>, dim3(static_cast<uint32_t>(tp * tq), a.g.G), dim3(WP * WQ * 64), 0, s, a);
+    const int64_t blocks = (tp * tq * a.parts * a.g.G + 7) / 8 * 8;
+    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    const dim3 grid(static_cast<uint32_t>(blocks)), block(WP * WQ * 64);
+    hipError_t e;
+    if constexpr (DIRECT) e = launch_kernel(k_cols_direct<E, KIND, BP, BQ, WP, WQ>, grid, block, 0, s, a);
+    else e = launch_kernel(k_cols<E, KIND, BP, BQ, WP, WQ>, grid, block, 0, s, a);
+    if (e != hipSuccess || a.parts == 1) return e;
+    const int64_t count = static_cast<int64_t>(a.g.G) * a.np * a.nq;
+    return launch_kernel(k_cols_sum<E>, dim3(static_cast<uint32_t>((count + 1023) / 1024)), dim3(256), 0, s, a, count);
 }
 
 template <class E>
-hipError_t pick(ColsKind kind, const ColsArgs &a, hipStream_t s) {
+hipError_t pick(ColsKind kind, const ColsArgs &a, int cus, hipStream_t s) {
     constexpr int L = kLowBytes / sizeof(E);
-    switch (kind) {
-    case ColsKind::kDense: return go<E, ColsKind::kDense, 128, 128, 2, 2>(a, s);
-    case ColsKind::kLowP: return go<E, ColsKind::kLowP, L, 128, 1, 4>(a, s);
-    default: return go<E, ColsKind::kLowQ, 128, L, 4, 1>(a, s);
+    if (kind == ColsKind::kLowP)
+        return whole_chunks<E, ColsKind::kLowP>(a) ? go<E, ColsKind::kLowP, L, 128, 1, 4, true>(a, s)
+                                                   : go<E, ColsKind::kLowP, L, 128, 1, 4, false>(a, s);
+    if (kind == ColsKind::kLowQ)
+        return whole_chunks<E, ColsKind::kLowQ>(a) ? go<E, ColsKind::kLowQ, 128, L, 4, 1, true>(a, s)
+                                                   : go<E, ColsKind::kLowQ, 128, L, 4, 1, false>(a, s);
+    const int64_t big = static_cast<int64_t>(a.g.G) * ((a.np + 255) / 256) * ((a.nq + 255) / 256);
+    const int64_t mid = static_cast<int64_t>(a.g.G) * ((a.np + 127) / 128) * ((a.nq + 127) / 128);
+    if (whole_chunks<E, ColsKind::kDense>(a)) {
+        if constexpr (sizeof(E) == 2)
+            if (big >= cus) return go<E, ColsKind::kDense, 256, 256, 2, 4, true>(a, s);
+        if (mid >= cus) return go<E, ColsKind::kDense, 128, 128, 2, 2, true>(a, s);
+        return go<E, ColsKind::kDense, 64, 64, 2, 2, true>(a, s);
     }
+    if (mid >= cus) return go<E, ColsKind::kDense, 128, 128, 2, 2, false>(a, s);
+    return go<E, ColsKind::kDense, 64, 64, 2, 2, false>(a, s);
 }
 
 }  // namespace
 
+// Workgroups that share a tile's places: enough to fill the device, each with at
+// least four stages of an average group.
+int cols_parts(bool bf16, ColsKind kind, const ColsArgs &a, int cus) {
+    const int stage = bf16 ? 64 : 32, tile = kind == ColsKind::kDense ? 64 : 128;
+    const int64_t tp = kind == ColsKind::kLowP ? a.blocks : (a.np + tile - 1) / tile;
+    const int64_t tq = kind == ColsKind::kLowQ ? a.blocks : (a.nq + tile - 1) / tile;
+    const int64_t items = tp * tq * a.g.G, stages = a.g.n / (static_cast<int64_t>(a.g.G) * stage);
+    const int enough = kind == ColsKind::kDense ? cus : 3 * cus;
+    int parts = 1;
+    while (items * parts < enough && parts * 4 < stages) parts *= 2;
+    return parts;
+}
+
 hipError_t launch_cols(bool bf16, ColsKind kind, const ColsArgs &a, int cus, hipStream_t s) {
-    (void)cus;
-    return bf16 ? pick<__bf16>(kind, a, s) : pick<float>(kind, a, s);
+    return bf16 ? pick<__bf16>(kind, a, cus, s) : pick<float>(kind, a, cus, s);
 }
 
 }  // namespace hwr

@@ -53,6 +53,8 @@ struct ColsArgs {
     int64_t ldp, ldq;             // elements
     void *out;                    // [G][np][nq]
     int blocks;                   // rank blocks (low-rank side)
+    int parts;                    // workgroups that share a tile's places
+    float *partial;               // [parts][G][np][nq], with parts > 1
     const void *zeros;
 };
 
@@ -94,6 +96,7 @@ int few_tiles(int n, int G, bool adapter);
 int few_parts(int n, int G, int k, int m, bool bf16, bool adapter, int cus);
 hipError_t launch_few(bool bf16, bool adapter, const FewArgs &a, hipStream_t s);
 enum class ColsKind { kDense, kLowP, kLowQ };
+int cols_parts(bool bf16, ColsKind kind, const ColsArgs &a, int cus);
 hipError_t launch_cols(bool bf16, ColsKind kind, const ColsArgs &a, int cus, hipStream_t s);
 
 }  // namespace hwr

@@ -15,16 +15,16 @@ struct ColsTile {
     int g, ip, iq, part, p0, p1;
 };
 
-// Tiles of a group go in panels of 8 row tiles, as the products by row; parts side by side.
+// Every L2 takes a share of every group (groups differ in places, and so in work),
+// in panels of 8 tiles as the products by row; parts side by side.
 template <ColsKind KIND, int BP, int BQ, int kBk>
 __device__ inline bool my_tile(const ColsArgs &a, ColsTile &t) {
     const int tp = KIND == ColsKind::kLowP ? a.blocks : (a.np + BP - 1) / BP;
     const int tq = KIND == ColsKind::kLowQ ? a.blocks : (a.nq + BQ - 1) / BQ;
-    const int per = tp * tq * a.parts;
-    const int item = xcd_item(blockIdx.x, a.g.G * per);
-    if (item < 0) return false;
-    t.g = item / per;
-    const int in_group = item % per, tile = in_group / a.parts;
+    const int per = tp * tq * a.parts, share = (per + 7) >> 3, at = blockIdx.x >> 3;
+    t.g = at / share;
+    const int in_group = ((blockIdx.x + t.g) & 7) * share + at % share, tile = in_group / a.parts;
+    if (in_group >= per) return false;
     t.part = in_group % a.parts;
     const int panel = tile / (8 * tq) * 8, in = tile - panel * tq, rp = min(8, tp - panel);
     t.ip = panel + in % rp;
@@ -170,9 +170,8 @@ __global__ void __launch_bounds__(WP *WQ * 64) k_cols(ColsArgs a) {
     store_tile<E, KIND, BP, BQ, WP, WQ>(a, t, acc, lane, wp, wq);
 }
 
-// Whole chunks of 16 bytes everywhere: operands go from memory straight into LDS,
-// the next stage's while this one is multiplied; the rows of the stage after that
-// are looked up meanwhile.  Places past the last are zeros on both sides; columns
+// Whole chunks of 16 bytes everywhere: operands go from memory straight into LDS
+// (run_stages); a stage's rows are looked up when the stage before it is loaded.  Places past the last are zeros on both sides; columns
 // past the last are loaded from a valid place and not stored.
 template <class E, ColsKind KIND, int BP, int BQ, int WP, int WQ>
 __global__ void __launch_bounds__(WP *WQ * 64) k_cols_direct(ColsArgs a) {
@@ -192,70 +191,56 @@ __global__ void __launch_bounds__(WP *WQ * 64) k_cols_direct(ColsArgs a) {
     ColsTile t;
     if (!my_tile<KIND, BP, BQ, kBk>(a, t)) return;
 
-    // the thread's chunks: line (place of the stage) and byte within the row
-    int pl[UP], ql[UQ], pb[UP], qb[UQ], pr[UP], qr[UQ];
+    // the thread's chunks: byte within the row.  Lines 16 apart have the same order of chunks.
+    constexpr int kLinesP = NT / PT::kCpl, kLinesQ = NT / QT::kCpl;
+    constexpr int BPN = kLinesP % 16 ? UP : 1, BQN = kLinesQ % 16 ? UQ : 1;
+    int pb[BPN], qb[BQN];
 #pragma unroll
-    for (int i = 0; i < UP; ++i) {
+    for (int i = 0; i < BPN; ++i) {
         const int u = i * NT + tid, c = (u % PT::kCpl) ^ PT::swz(u / PT::kCpl);
-        pl[i] = u / PT::kCpl;
         pb[i] = TT::kLowP ? t.ip * kLowBytes + c * 16 : min(t.ip * BP + c * kEpc, a.np - kEpc) * (int)sizeof(E);
     }
 #pragma unroll
-    for (int i = 0; i < UQ; ++i) {
+    for (int i = 0; i < BQN; ++i) {
         const int u = i * NT + tid, c = (u % QT::kCpl) ^ QT::swz(u / QT::kCpl);
-        ql[i] = u / QT::kCpl;
         qb[i] = TT::kLowQ ? t.iq * kLowBytes + c * 16 : min(t.iq * BQ + c * kEpc, a.nq - kEpc) * (int)sizeof(E);
     }
-    auto look_up = [&](int p) {            // rows (or places) of the stage from p on; -1: zeros
+    // rows (or places) of a stage's lines; -1: zeros.  Tiles of one width share them.
+    constexpr bool kShared = KIND == ColsKind::kDense && BP == BQ;
+    int pr[UP], qr[kShared ? 1 : UQ];
+    auto look_up = [&](int stage) {
+        const int p = t.p0 + stage * kBk;
 #pragma unroll
-        for (int i = 0; i < UP; ++i) pr[i] = p + pl[i] >= t.p1 ? -1 : TT::kLowP ? p + pl[i] : row_at(a.g, p + pl[i]);
+        for (int i = 0; i < UP; ++i) {
+            const int at = p + i * kLinesP + tid / PT::kCpl;
+            pr[i] = at >= t.p1 ? -1 : TT::kLowP ? at : row_at(a.g, at);
+        }
+        if constexpr (!kShared)
 #pragma unroll
-        for (int i = 0; i < UQ; ++i) qr[i] = p + ql[i] >= t.p1 ? -1 : TT::kLowQ ? p + ql[i] : row_at(a.g, p + ql[i]);
+            for (int i = 0; i < UQ; ++i) {
+                const int at = p + i * kLinesQ + tid / QT::kCpl;
+                qr[i] = at >= t.p1 ? -1 : TT::kLowQ ? at : row_at(a.g, at);
+            }
     };
     const int64_t pld = TT::kLowP ? a.blocks * kLowBytes : a.ldp * (int64_t)sizeof(E);
     const int64_t qld = TT::kLowQ ? a.blocks * kLowBytes : a.ldq * (int64_t)sizeof(E);
     const char *zeros = static_cast<const char *>(a.zeros), *ps = static_cast<const char *>(a.p),
                *qs = static_cast<const char *>(a.q);
-    auto issue = [&](char *b) {
+    auto issue = [&](char *b, int stage) {
 #pragma unroll
         for (int i = 0; i < UP; ++i)
-            load_lds(pr[i] < 0 ? zeros : ps + pr[i] * pld + pb[i], b + (i * NT + wave * 64) * 16);
+            load_lds(pr[i] < 0 ? zeros : ps + pr[i] * pld + pb[i % BPN], b + (i * NT + wave * 64) * 16);
 #pragma unroll
-        for (int i = 0; i < UQ; ++i)
-            load_lds(qr[i] < 0 ? zeros : qs + qr[i] * qld + qb[i], b + PT::kBytes + (i * NT + wave * 64) * 16);
+        for (int i = 0; i < UQ; ++i) {
+            const int r = kShared ? pr[i] : qr[kShared ? 0 : i];
+            load_lds(r < 0 ? zeros : qs + r * qld + qb[i % BQN], b + PT::kBytes + (i * NT + wave * 64) * 16);
+        }
+        look_up(stage + 1);
     };
     f32x4 acc[PF][QF] = {};
-    auto multiply = [&](const char *b) {
-        multiply_tile<E, PT, QT, PF, QF>(b, PT::kBytes, wp * PF * 16, wq * QF * 16, lane, acc);
-    };
-    auto finished = [&] {                  // this stage's buffer may be overwritten
-        wait_lds();
-        barrier();
-    };
-    int p = t.p0;
-    if (p < t.p1) {
-        look_up(p);
-        issue(buf0);
-        look_up(p + kBk);
-        for (; p + 2 * kBk < t.p1; p += 2 * kBk) {
-            issue(buf1);
-            look_up(p + 2 * kBk);
-            wait_vm<2 * (UP + UQ)>();      // (the look-up is in flight too)
-            barrier();
-            multiply(buf0);
-            finished();
-            issue(buf0);
-            look_up(p + 3 * kBk);
-            wait_vm<2 * (UP + UQ)>();
-            barrier();
-            multiply(buf1);
-            finished();
-        }
-        if (p + kBk < t.p1) issue(buf1);
-        wait_vm<0>();
-        barrier();
-        multiply(buf0);
-        if (p + kBk < t.p1) multiply(buf1);
+    if (t.p0 < t.p1) {
+        look_up(0);
+        run_stages<E, PT, QT, PF, QF>((t.p1 - t.p0 + kBk - 1) / kBk, issue, buf0, buf1, wp * PF * 16, wq * QF * 16, lane, acc);
     }
     store_tile<E, KIND, BP, BQ, WP, WQ>(a, t, acc, lane, wp, wq);
 }
@@ -293,7 +278,7 @@ template <class E, ColsKind KIND, int BP, int BQ, int WP, int WQ, bool DIRECT>
 hipError_t go(const ColsArgs &a, hipStream_t s) {
     const int64_t tp = KIND == ColsKind::kLowP ? a.blocks : (a.np + BP - 1) / BP;
     const int64_t tq = KIND == ColsKind::kLowQ ? a.blocks : (a.nq + BQ - 1) / BQ;
-    const int64_t blocks = (tp * tq * a.parts * a.g.G + 7) / 8 * 8;
+    const int64_t blocks = (tp * tq * a.parts + 7) / 8 * 8 * a.g.G;
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
     const dim3 grid(static_cast<uint32_t>(blocks)), block(WP * WQ * 64);
     hipError_t e;

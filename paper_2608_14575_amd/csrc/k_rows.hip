@@ -69,6 +69,7 @@ __device__ inline void add_adapters(const RowsArgs &a, const RowTile &rt, int c0
                 if (p < lo || p >= hi) return u32x4{0, 0, 0, 0};
                 return *reinterpret_cast<const u32x4 *>(low + (static_cast<int64_t>(p) * blocks + b) * kLowBytes + c * 16);
             }, tid);
+            gx.store(sx, tid);
             gw.load([&](int line, int c) {
                 u32x4 v;
                 const int e = KS ? line : c * El::kEpc;        // contraction element of the stage
@@ -79,7 +80,6 @@ __device__ inline void add_adapters(const RowsArgs &a, const RowTile &rt, int c0
                     v = load_chunk<E>(c0 + line < a.m ? gl + static_cast<int64_t>(c0 + line) * a.rank : nullptr, r, a.rank);
                 return e < kRankBlock ? v : finite_only(v);    // past kRankBlock: the low parts (bf16)
             }, tid);
-            gx.store(sx, tid);
             gw.store(sw, tid);
             __syncthreads();
 #pragma unroll
@@ -232,10 +232,9 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows(RowsArgs a) {
     store_rows<E, BM, BN, WR, WC>(a, c0, rows, acc, tid);
 }
 
-// Whole chunks of 16 bytes everywhere: operands go from memory straight into LDS,
-// the next stage's while this one is multiplied.  Rows in no place and columns past
-// the last are loaded from a valid one and not stored; contraction elements past
-// the last are zeros on both sides.
+// Whole chunks of 16 bytes everywhere and at least BN columns: operands go from
+// memory straight into LDS (run_stages).  A place without a row computes one that it
+// does not store; contraction elements past the last are zeros on both sides.
 template <class E, RowsKind KIND, bool KS, int BM, int BN, int WR, int WC>
 __global__ void __launch_bounds__(WR *WC * 64) k_rows_direct(RowsArgs a) {
     using El = Elem<E>;
@@ -244,6 +243,11 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows_direct(RowsArgs a) {
     using WT = Tile<E, KS, BN>;
     constexpr int UX = XT::kChunks / NT, UW = WT::kChunks / NT;
     static_assert(XT::kChunks % NT == 0 && WT::kChunks % NT == 0);
+    // a thread's chunks lie a multiple of 16 lines apart: one order of chunks (not in
+    // fp32 tiles of 128 columns)
+    constexpr int kLinesX = NT / XT::kCpl, kLinesW = NT / WT::kCpl;
+    static_assert(kLinesX % 16 == 0);
+    constexpr bool kOneOrder = kLinesW % 16 == 0;
     constexpr int kBuf = XT::kBytes + WT::kBytes;
     // an array each, so that the compiler sees that reads of one do not depend on the
     // loads in flight into the other
@@ -258,81 +262,49 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows_direct(RowsArgs a) {
     __syncthreads();
 
     const int k = KIND == RowsKind::kGrouped && rt.g == a.g.G ? 0 : a.k;
-    const char *xp[UX], *wp[UW];
-    int xe[UX], we[UW];                    // first contraction element of the thread's chunks
+    const int xline = tid / XT::kCpl, xe = ((tid % XT::kCpl) ^ XT::swz(xline)) * kEpc;   // first element of the thread's chunks
+    const char *xp[UX];
 #pragma unroll
     for (int i = 0; i < UX; ++i) {
-        const int u = i * NT + tid, line = u / XT::kCpl, r = rows[line];
-        xe[i] = ((u % XT::kCpl) ^ XT::swz(line)) * kEpc;
-        xp[i] = reinterpret_cast<const char *>(static_cast<const E *>(a.x) + (r < 0 ? 0 : r) * a.ldx + xe[i]);
+        const int r = rows[i * kLinesX + xline];
+        xp[i] = reinterpret_cast<const char *>(static_cast<const E *>(a.x) + (r < 0 ? 0 : r) * a.ldx + xe);
     }
     const E *w = static_cast<const E *>(a.w) + (KIND == RowsKind::kAdapter || k == 0 ? 0 : rt.g) * a.w_stride;
-#pragma unroll
-    for (int i = 0; i < UW; ++i) {
-        const int u = i * NT + tid, line = u / WT::kCpl, c = (u % WT::kCpl) ^ WT::swz(line);
-        we[i] = KS ? line : c * kEpc;
-        const int64_t at = KS ? static_cast<int64_t>(line) * a.m + min(c0 + c * kEpc, a.m - kEpc)
-                              : static_cast<int64_t>(min(c0 + line, a.m - 1)) * a.k + c * kEpc;
-        wp[i] = reinterpret_cast<const char *>(w + at);
-    }
+    const int wline = tid / WT::kCpl, ldw = KS ? a.m : a.k;
+    auto chunk = [&](int i) { return ((tid % WT::kCpl) ^ WT::swz(i * kLinesW + wline)) * kEpc; };
+    const int we = KS ? wline : chunk(0);
+    const char *wp = reinterpret_cast<const char *>(KS ? w + static_cast<int64_t>(wline) * ldw + c0
+                                                       : w + static_cast<int64_t>(c0 + wline) * ldw) +
+                     (kOneOrder ? chunk(0) * sizeof(E) : 0);
+    auto weight = [&](int i) {
+        const char *at = wp + static_cast<int64_t>(i) * kLinesW * ldw * sizeof(E);
+        return kOneOrder ? at : at + chunk(i) * sizeof(E);
+    };
     const int64_t wstep = KS ? static_cast<int64_t>(kBk) * a.m * sizeof(E) : kStageBytes;
-    const char *zeros = static_cast<const char *>(a.zeros);
-    auto issue = [&](char *b, int k0) {
-        const bool whole = k0 + kBk <= k;
+    auto issue = [&](char *b, int stage) {
+        const int k0 = stage * kBk;
+        if (k0 + kBk <= k) {
 #pragma unroll
-        for (int i = 0; i < UX; ++i) {
-            const char *src = whole || k0 + xe[i] < k ? xp[i] : zeros;
-            load_lds(src, b + (i * NT + wave * 64) * 16);
-            xp[i] += kStageBytes;
+            for (int i = 0; i < UX; ++i) load_lds(xp[i], b + (i * NT + wave * 64) * 16);
+#pragma unroll
+            for (int i = 0; i < UW; ++i) load_lds(weight(i), b + XT::kBytes + (i * NT + wave * 64) * 16);
+        } else {
+            const char *zeros = static_cast<const char *>(a.zeros);
+#pragma unroll
+            for (int i = 0; i < UX; ++i) load_lds(k0 + xe < k ? xp[i] : zeros, b + (i * NT + wave * 64) * 16);
+#pragma unroll
+            for (int i = 0; i < UW; ++i) {
+                const int e = KS ? i * kLinesW + we : kOneOrder ? we : chunk(i);
+                load_lds(k0 + e < k ? weight(i) : zeros, b + XT::kBytes + (i * NT + wave * 64) * 16);
+            }
         }
 #pragma unroll
-        for (int i = 0; i < UW; ++i) {
-            const char *src = whole || k0 + we[i] < k ? wp[i] : zeros;
-            load_lds(src, b + XT::kBytes + (i * NT + wave * 64) * 16);
-            wp[i] += wstep;
-        }
+        for (int i = 0; i < UX; ++i) xp[i] += kStageBytes;
+        wp += wstep;
     };
     f32x4 acc[RF][CF] = {};
-    auto multiply = [&](const char *b) {
-#pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-            typename El::Frag fw[CF], fx[RF];
-#pragma unroll
-            for (int j = 0; j < CF; ++j) fw[j] = WT::frag(b, XT::kBytes, (wc * CF + j) * 16, sub, lane);
-#pragma unroll
-            for (int i = 0; i < RF; ++i) fx[i] = XT::frag(b, 0, (wr * RF + i) * 16, sub, lane);
-#pragma unroll
-            for (int i = 0; i < RF; ++i)
-#pragma unroll
-                for (int j = 0; j < CF; ++j) acc[i][j] = El::mma(fw[j], fx[i], acc[i][j]);
-        }
-    };
-    auto finished = [&] {                  // this stage's buffer may be overwritten
-        wait_lds();
-        barrier();
-    };
-    if (k > 0) {
-        issue(buf0, 0);
-        int k0 = 0;
-        for (; k0 + 2 * kBk < k; k0 += 2 * kBk) {
-            issue(buf1, k0 + kBk);
-            wait_vm<UX + UW>();
-            barrier();
-            multiply(buf0);
-            finished();
-            issue(buf0, k0 + 2 * kBk);
-            wait_vm<UX + UW>();
-            barrier();
-            multiply(buf1);
-            finished();
-        }
-        if (k0 + kBk < k) issue(buf1, k0 + kBk);
-        wait_vm<0>();
-        barrier();
-        multiply(buf0);
-        if (k0 + kBk < k) multiply(buf1);
-        finished();
-    }
+    if (k > 0) run_stages<E, XT, WT, RF, CF>((k + kBk - 1) / kBk, issue, buf0, buf1, wr * RF * 16, wc * CF * 16, lane, acc);
+    __syncthreads();
 
     if constexpr (KIND == RowsKind::kAdapter) add_adapters<E, KS, BM, BN, WR, WC>(a, rt, c0, buf0, buf0 + XT::kBytes, acc, tid);
     store_rows<E, BM, BN, WR, WC>(a, c0, rows, acc, tid);
@@ -365,10 +337,10 @@ hipError_t pick(const RowsArgs &a, int cus, hipStream_t s) {
     auto tiles = [&](int64_t bm, int64_t bn) {
         return (a.g.n / bm + (KIND == RowsKind::kAdapter ? 1 : a.g.G)) * ((a.m + bn - 1) / bn);
     };
-    if (whole_chunks<E, KS>(a)) {
+    if (whole_chunks<E, KS>(a) && a.m >= 64) {
         if constexpr (sizeof(E) == 2)
-            if (tiles(256, 256) >= cus) return go<E, KIND, KS, 256, 256, 2, 4, true>(a, s);
-        if (tiles(128, 128) >= cus) return go<E, KIND, KS, 128, 128, 2, 2, true>(a, s);
+            if (a.m >= 256 && tiles(256, 256) >= cus) return go<E, KIND, KS, 256, 256, 2, 4, true>(a, s);
+        if (a.m >= 128 && tiles(128, 128) >= cus) return go<E, KIND, KS, 128, 128, 2, 2, true>(a, s);
         return go<E, KIND, KS, 64, 64, 2, 2, true>(a, s);
     }
     if (tiles(128, 128) >= cus) return go<E, KIND, KS, 128, 128, 2, 2>(a, s);

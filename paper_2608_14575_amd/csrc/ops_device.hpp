@@ -253,4 +253,80 @@ __device__ inline void barrier() {    // execution and LDS order; does not wait 
     asm volatile("" ::: "memory");
 }
 
+// ---------------------------------------------------------------- staged products
+// acc[i][j] += X W over `stages` stages (at least one): RF row fragments from line x0 of the
+// X tile, CF column fragments from line w0 of the W tile; each buffer holds an X
+// tile, then a W tile.  issue(buffer, stage) starts the loads of a stage into LDS, in
+// order of stages.
+//
+// Two buffers and one barrier a stage.  A stage is two halves of RF groups, a group
+// the CF products of one X fragment.  Fragments are read from LDS kAhead groups
+// before they are multiplied, across halves and stages, in the order written here: left
+// to itself the compiler reads and waits, and reads and products add up (2.1 us
+// for a stage of 256 x 256 x 64 whose products take 1.0).  At the barrier, kAhead
+// groups before the end of the stage, every wave has read all of its buffer: the
+// loads of the stage after the next go into it, and those of the next, issued a
+// stage before, have arrived.
+template <class E, class XT, class WT, int RF, int CF, class Issue>
+__device__ inline void run_stages(int stages, Issue issue, char *buf0, char *buf1, int x0, int w0, int lane,
+                                  f32x4 (&acc)[RF][CF]) {
+    using El = Elem<E>;
+    constexpr int kAhead = RF / 2, kBarrier = 2 * RF - kAhead;
+    typename El::Frag x[RF], w[2][CF];
+    auto read_x = [&](const char *b, int group) {        // groups 0 .. 2 RF - 1 of a stage
+        x[group % RF] = XT::frag(b, 0, x0 + group % RF * 16, group / RF, lane);
+    };
+    auto read_w = [&](const char *b, int half, int j) { w[half][j] = WT::frag(b, XT::kBytes, w0 + j * 16, half, lane); };
+    auto arrived = [&] {
+        wait_lds();
+        wait_vm<0>();
+        barrier();
+    };
+    auto first = [&](const char *b) {
+#pragma unroll
+        for (int j = 0; j < CF; ++j) read_w(b, 0, j);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) read_x(b, i);
+    };
+    auto stage = [&](char *cur, char *next, int s) {
+#pragma unroll
+        for (int group = 0; group < 2 * RF; ++group) {
+            if (group == kBarrier) {
+                arrived();
+                if (s + 2 < stages) issue(cur, s + 2);
+            }
+            const int to = group + kAhead;
+            if (to < 2 * RF) read_x(cur, to);
+            else read_x(next, to - 2 * RF);
+#pragma unroll
+            for (int j = 0; j < CF; ++j) {
+                if (group == j * RF / CF) read_w(cur, 1, j);
+                if (group == kBarrier + j * kAhead / (2 * CF)) read_w(next, 0, j);
+            }
+#pragma unroll
+            for (int j = 0; j < CF; ++j) acc[group % RF][j] = El::mma(w[group / RF][j], x[group % RF], acc[group % RF][j]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // An odd stage goes first: the sums then pass through one loop, with no other way
+    // to its end (merging them would cost the registers twice).
+    int s = stages & 1;
+    if (s) {
+        issue(buf1, 0);
+        arrived();
+        if (stages > 1) issue(buf0, 1);
+        first(buf1);
+        stage(buf1, buf0, 0);
+    } else {
+        issue(buf0, 0);
+        arrived();
+        issue(buf1, 1);
+        first(buf0);
+    }
+    for (; s < stages; s += 2) {
+        stage(buf0, buf1, s);
+        stage(buf1, buf0, s + 1);
+    }
+}
+
 }  // namespace hwr

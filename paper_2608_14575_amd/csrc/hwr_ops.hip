@@ -222,10 +222,14 @@ hwr_status group_rows(hwr_ops *c, int32_t n, const int32_t *choice, const int32_
     if (table ? n_table < 1 : n_table != 0) return invalid(c, "n_table must be > 0 with a table and 0 without");
     if (misaligned(HWR_F32, {choice, table, offsets, order})) return invalid(c, "a pointer is not aligned to its elements");
     if (hwr_status st = use_device(c)) return st;
-    GroupRowsArgs a{n, n_table, n_groups, choice, table, offsets, order, nullptr, group_rows_blocks(n)};
-    char *ws = nullptr;
-    if (hwr_status st = workspace(c, static_cast<uint64_t>(n_groups + 1) * a.blocks * sizeof(int32_t), &ws)) return st;
-    a.hist = reinterpret_cast<int32_t *>(ws);
+    GroupRowsArgs a{n, n_table, n_groups, choice, table, offsets, order, group_rows_blocks(n), nullptr, nullptr};
+    if (a.blocks > 1) {
+        const uint64_t counts = static_cast<uint64_t>(n_groups + 1) * a.blocks;
+        char *ws = nullptr;
+        if (hwr_status st = workspace(c, (counts + n_groups + 1) * sizeof(int32_t), &ws)) return st;
+        a.hist = reinterpret_cast<int32_t *>(ws);
+        a.totals = a.hist + counts;
+    }
     OPS_HIP(c, launch_group_rows(a, c->stream));
     return HWR_OK;
 }

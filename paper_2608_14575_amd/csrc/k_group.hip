@@ -1,11 +1,20 @@
 // Rows by group: a stable counting sort of the routed rows.
+//
+// A wave takes 512 rows in order, 64 at a time, and counts them by key in LDS.
+// A row's place is where its key begins, plus the rows of the key before the
+// wave, plus those before the row in the wave: lanes of one key find each other by
+// a ballot for each bit of the key.  Up to 8,192 rows fit one workgroup and one
+// launch; more take three: counts by block, a scan over the blocks of every key, and the
+// places.  Latency bounds the small form, three launches and the scattered row
+// numbers the large one (8 MB for a million rows).
 #include "ops_device.hpp"
 
 namespace hwr {
 namespace {
 
-constexpr int kGroupThreads = 256;
-constexpr int kGroupRows = 4096;      // rows of a workgroup
+constexpr int kChunks = 8, kWaveRows = 64 * kChunks;
+constexpr int kBlockWaves = 4, kBlockRows = kBlockWaves * kWaveRows;     // several blocks
+constexpr int kOneWaves = 16, kOneRows = kOneWaves * kWaveRows;          // one workgroup
 
 __device__ inline int group_key(const GroupRowsArgs &a, int row) {
     int c = a.choice[row];
@@ -13,77 +22,115 @@ __device__ inline int group_key(const GroupRowsArgs &a, int row) {
     return static_cast<unsigned>(c) < static_cast<unsigned>(a.G) ? c : a.G;
 }
 
-// hist[key][block]: rows of each key in the block's range
-__global__ void __launch_bounds__(kGroupThreads) k_group_count(GroupRowsArgs a) {
-    __shared__ int h[kMaxPairs + 1];
-    for (int i = threadIdx.x; i <= a.G; i += kGroupThreads) h[i] = 0;
-    __syncthreads();
-    const int r0 = blockIdx.x * kGroupRows, r1 = min(r0 + kGroupRows, a.n);
-    for (int r = r0 + threadIdx.x; r < r1; r += kGroupThreads) atomicAdd(&h[group_key(a, r)], 1);
-    __syncthreads();
-    for (int i = threadIdx.x; i <= a.G; i += kGroupThreads) a.hist[static_cast<int64_t>(i) * a.blocks + blockIdx.x] = h[i];
-}
-
-// hist in place: place of each block's first row of each key; offsets
-__global__ void __launch_bounds__(1024) k_group_scan(GroupRowsArgs a) {
-    __shared__ int part[16], total;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int count = (a.G + 1) * a.blocks;
+// Exclusive prefix over i < count of value(i), handed to use(i, before).
+template <int WAVES, class Value, class Use>
+__device__ inline void scan_keys(int count, Value value, Use use) {
+    __shared__ int part[WAVES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int base = 0;
-    for (int i0 = 0; i0 < count; i0 += 1024) {
-        const int i = i0 + threadIdx.x;
-        const int v = i < count ? a.hist[i] : 0;
-        const int upto = wave_scan(v, lane);
+    for (int i0 = 0; i0 < count; i0 += WAVES * 64) {
+        const int i = i0 + tid, v = i < count ? value(i) : 0, upto = wave_scan(v, lane);
         if (lane == 63) part[wave] = upto;
         __syncthreads();
         int before = base;
-        for (int w = 0; w < wave; ++w) before += part[w];
-        if (i < count) {
-            a.hist[i] = before + upto - v;
-            if (i % a.blocks == 0 && i / a.blocks <= a.G) a.offsets[i / a.blocks] = before + upto - v;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            if (w < wave) before += part[w];
+            base += part[w];
         }
-        if (threadIdx.x == 1023) total = before + upto;
+        if (i < count) use(i, before + upto - v);
         __syncthreads();
-        base = total;
     }
 }
 
-__global__ void __launch_bounds__(64) k_group_place(GroupRowsArgs a) {
-    __shared__ int next[kMaxPairs + 1];
-    const int lane = threadIdx.x;
-    for (int i = lane; i <= a.G; i += 64) next[i] = a.hist[static_cast<int64_t>(i) * a.blocks + blockIdx.x];
+enum class Step { kAll, kCount, kPlace };
+
+template <Step STEP, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64) k_group(GroupRowsArgs a) {
+    // counts by wave, then the place of the wave's next row of each key
+    __shared__ int count[WAVES][kMaxPairs + 1];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, keys = a.G + 1;
+    const int64_t r0 = (static_cast<int64_t>(blockIdx.x) * WAVES + wave) * kWaveRows + lane;
+    int key[kChunks];
+#pragma unroll
+    for (int j = 0; j < kChunks; ++j) key[j] = r0 + j * 64 < a.n ? group_key(a, static_cast<int>(r0 + j * 64)) : -1;
+    for (int i = lane; i < keys; i += 64) count[wave][i] = 0;
     __syncthreads();
-    const int r0 = blockIdx.x * kGroupRows, r1 = min(r0 + kGroupRows, a.n);
-    for (int b = r0; b < r1; b += 64) {
-        const int r = b + lane;
-        const int key = r < r1 ? group_key(a, r) : -1;
-        // lanes of the same key: rank among them, and the last one advances the counter
-        uint64_t same = __ballot(key >= 0);
-        for (int bit = 0; (a.G >> bit) != 0; ++bit) {
-            const uint64_t set = __ballot((key >> bit) & 1);
-            same &= ((key >> bit) & 1) ? set : ~set;
-        }
-        const int rank = __popcll(same & ((1ull << lane) - 1));
-        const int at = key >= 0 ? next[key] : 0;
-        __syncthreads();
-        if (key >= 0) {
-            a.order[at + rank] = r;
-            if (rank == __popcll(same) - 1) next[key] = at + rank + 1;
-        }
-        __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kChunks; ++j)
+        if (key[j] >= 0) atomicAdd(&count[wave][key[j]], 1);
+    __syncthreads();
+    auto in_block = [&](int i) {
+        int v = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) v += count[w][i];
+        return v;
+    };
+    if constexpr (STEP == Step::kCount) {
+        for (int i = tid; i < keys; i += WAVES * 64) a.hist[static_cast<int64_t>(i) * a.blocks + blockIdx.x] = in_block(i);
+        return;
     }
+    scan_keys<WAVES>(
+        keys, [&](int i) { return STEP == Step::kAll ? in_block(i) : a.totals[i]; },
+        [&](int i, int before) {
+            if (blockIdx.x == 0 && i <= a.G) a.offsets[i] = before;
+            if (STEP == Step::kPlace) before += a.hist[static_cast<int64_t>(i) * a.blocks + blockIdx.x];
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                const int c = count[w][i];
+                count[w][i] = before;
+                before += c;
+            }
+        });
+    int *next = count[wave];
+#pragma unroll
+    for (int j = 0; j < kChunks; ++j) {
+        const int k = key[j];
+        uint64_t same = __ballot(k >= 0);
+        for (int bit = 0; (a.G >> bit) != 0; ++bit) {
+            const uint64_t set = __ballot((k >> bit) & 1);
+            same &= ((k >> bit) & 1) ? set : ~set;
+        }
+        const int rank = __popcll(same & ((1ull << lane) - 1)), at = k < 0 ? 0 : next[k];
+        if (k >= 0) a.order[at + rank] = static_cast<int>(r0 + j * 64);
+        wave_lds();                                      // every lane has its place: the first moves it on
+        if (k >= 0 && rank == 0) next[k] = at + __popcll(same);
+        wave_lds();
+    }
+}
+
+// hist of a key: rows in the blocks before each; totals: its rows.  A wave to a key.
+__global__ void __launch_bounds__(256) k_group_scan(GroupRowsArgs a) {
+    const int lane = threadIdx.x & 63, key = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (key > a.G) return;
+    int *h = a.hist + static_cast<int64_t>(key) * a.blocks;
+    int base = 0;
+    for (int b0 = 0; b0 < a.blocks; b0 += 64 * 8) {
+        int v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = b0 + j * 64 + lane < a.blocks ? h[b0 + j * 64 + lane] : 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int upto = wave_scan(v[j], lane);
+            if (b0 + j * 64 + lane < a.blocks) h[b0 + j * 64 + lane] = base + upto - v[j];
+            base += __builtin_amdgcn_readlane(upto, 63);
+        }
+    }
+    if (lane == 0) a.totals[key] = base;
 }
 
 }  // namespace
 
-int group_rows_blocks(int n) { return n > 0 ? (n + kGroupRows - 1) / kGroupRows : 1; }
+int group_rows_blocks(int n) { return n > kOneRows ? static_cast<int>((static_cast<int64_t>(n) + kBlockRows - 1) / kBlockRows) : 1; }
 
 hipError_t launch_group_rows(const GroupRowsArgs &a, hipStream_t s) {
-    hipError_t e = launch_kernel(k_group_count, dim3(a.blocks), dim3(kGroupThreads), 0, s, a);
+    if (a.n <= kBlockRows) return launch_kernel(k_group<Step::kAll, kBlockWaves>, dim3(1), dim3(kBlockWaves * 64), 0, s, a);
+    if (a.blocks == 1) return launch_kernel(k_group<Step::kAll, kOneWaves>, dim3(1), dim3(kOneWaves * 64), 0, s, a);
+    hipError_t e = launch_kernel(k_group<Step::kCount, kBlockWaves>, dim3(a.blocks), dim3(kBlockWaves * 64), 0, s, a);
     if (e != hipSuccess) return e;
-    e = launch_kernel(k_group_scan, dim3(1), dim3(1024), 0, s, a);
+    e = launch_kernel(k_group_scan, dim3((a.G + 4) / 4), dim3(256), 0, s, a);
     if (e != hipSuccess) return e;
-    return launch_kernel(k_group_place, dim3(a.blocks), dim3(64), 0, s, a);
+    return launch_kernel(k_group<Step::kPlace, kBlockWaves>, dim3(a.blocks), dim3(kBlockWaves * 64), 0, s, a);
 }
 
 }  // namespace hwr

@@ -1,7 +1,11 @@
 // Low-rank intermediates: low[place] = scale[g] x[row] w_g, with w_g [k][rank]
-// (KS) or [rank][k].  The rows are read once, straight into matrix operands; the
-// narrow weights come from the L2s.  A workgroup takes the places of one group in
-// tiles; its waves take every kWaves-th step of the contraction and add up through LDS.
+// or [rank][k].
+//
+// The rows are read once, straight into matrix operands; the narrow weights come
+// from the L2s.  A workgroup takes a tile of places of one group; its waves take every
+// kWaves-th step of the contraction and add up through LDS.  A wave waits for
+// no other until then, and keeps the loads of several steps in flight: that, and not
+// the L2s, bounded a form with one step ahead (12,288 rows of 4096 bf16: 75 us).
 #include "ops_device.hpp"
 
 namespace hwr {
@@ -9,17 +13,29 @@ namespace {
 
 constexpr int kWaves = 8;
 
-// KS: fragment j holds the columns m V + j (as in the products of few rows), V
-// fragments whatever the rank; else the columns 16 j + m, as many as the rank takes.
-template <class E, bool KS, int RB>
-__global__ void __launch_bounds__(kWaves * 64) k_shrink(ShrinkArgs a) {
+// (stored and read as different types)
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), may_alias));
+
+// How the weights come into operand form.  kDirect: [rank][k], 16 bytes of a lane are
+// its operand.  kTurned: [k][rank] with whole chunks in a row; a step's rows are one
+// piece of memory, which goes through a part of LDS that is the wave's own and is
+// read by columns.  kAny: [k][rank] of any rank and alignment, transposed in
+// registers (fragment j then holds the columns m V + j).
+enum class From { kDirect, kTurned, kAny };
+
+// NF column fragments (kAny: V, one pass over the columns for each 16 V), RB row fragments.
+template <class E, From FROM, int NF, int RB>
+__global__ void __launch_bounds__(kWaves * 64, 4) k_shrink(ShrinkArgs a) {
     using El = Elem<E>;
-    constexpr int V = El::kEpc, BM = 16 * RB, kStep = 4 * V, kCols = 16 * V;
-    constexpr int kAcc = RB * V;
-    __shared__ f32x4 part[kWaves / 2 * kAcc * 64];
+    constexpr int V = El::kEpc, BM = 16 * RB, kStep = 4 * V, kCols = 16 * NF;
+    constexpr int kAcc = RB * NF, kDeep = NF <= 2 ? 4 : FROM == From::kAny ? 1 : 2;
+    // a step's weights for each wave, or half of the waves' sums
+    constexpr int kOwn = FROM == From::kTurned ? kStep * kCols * sizeof(E) : 0, kSums = kAcc * 64 * 16;
+    constexpr int kLds = kWaves * kOwn > kWaves / 2 * kSums ? kWaves * kOwn : kWaves / 2 * kSums;
+    __shared__ __attribute__((aligned(16))) char lds[kLds];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int m = lane & 15, q = lane >> 4;
-    const int ct = (a.rank + kCols - 1) / kCols;
+    const int ct = FROM == From::kAny ? (a.rank + kCols - 1) / kCols : 1;
     const int t = blockIdx.x / ct, c0 = blockIdx.x % ct * kCols;
     if (t >= count_tiles(a.g, BM, false, lane)) return;
     const RowTile rt = find_tile(a.g, t, BM, false, lane);
@@ -35,67 +51,103 @@ __global__ void __launch_bounds__(kWaves * 64) k_shrink(ShrinkArgs a) {
         in_tile[i] = p < rt.p1;
         x[i] = static_cast<const E *>(a.x) + (r < 0 ? 0 : r) * a.ldx + q * V;
     }
-    f32x4 acc[RB][V] = {};
-    u32x4 nw[V], nx[RB];
+    f32x4 acc[RB][NF] = {};
+    u32x4 nw[kDeep][NF], nx[kDeep][RB];
     const int steps = (a.k + kStep - 1) / kStep;
-    auto load = [&](int step) {
+    auto load = [&](u32x4 (&lw)[NF], u32x4 (&lx)[RB], int step) {
         const bool whole = (step + 1) * kStep <= a.k;
 #pragma unroll
         for (int i = 0; i < RB; ++i) {
-            if (whole) nx[i] = *reinterpret_cast<const typename El::Vec *>(x[i] + step * kStep);
-            else nx[i] = load_chunk<E>(x[i], step * kStep, a.k - q * V);
+            if (whole) lx[i] = *reinterpret_cast<const typename El::Vec *>(x[i] + step * kStep);
+            else lx[i] = load_chunk<E>(x[i], step * kStep, a.k - q * V);
         }
         const int e = step * kStep + q * V;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            if constexpr (KS) {
-                nw[i] = load_chunk<E>(e + i < a.k ? w + static_cast<int64_t>(e + i) * a.rank + c0 : nullptr, m * V, cols);
+        for (int i = 0; i < NF; ++i) {
+            if constexpr (FROM == From::kDirect) {
+                const E *line = w + static_cast<int64_t>(min(i * 16 + m, a.rank - 1)) * a.k;   // past the rank: not used
+                if (whole) lw[i] = *reinterpret_cast<const typename El::Vec *>(line + e);
+                else lw[i] = load_chunk<E>(line, e, a.k);
+            } else if constexpr (FROM == From::kTurned) {
+                const int64_t at = static_cast<int64_t>(step) * kStep * a.rank + (i * 64 + lane) * V;
+                lw[i] = u32x4{0, 0, 0, 0};
+                if ((i * 64 + lane) * V < kStep * a.rank && at < static_cast<int64_t>(a.k) * a.rank)
+                    lw[i] = *reinterpret_cast<const u32x4 *>(w + at);
             } else {
-                if (i * 16 >= cols) break;
-                nw[i] = load_chunk<E>(i * 16 + m < cols ? w + static_cast<int64_t>(c0 + i * 16 + m) * a.k : nullptr, e, a.k);
+                lw[i] = load_chunk<E>(e + i < a.k ? w + static_cast<int64_t>(e + i) * a.rank + c0 : nullptr, m * V, cols);
             }
         }
     };
-    int step = wave;
-    if (step < steps) load(step);
-    for (; step < steps; step += kWaves) {
-        typename El::Frag fw[V];
-        union Chunk { u32x4 v; typename El::Frag f; } fx[RB], u;
+    auto consume = [&](const u32x4 (&lw)[NF], const u32x4 (&lx)[RB]) {
+        union Chunk { u32x4 v; typename El::Frag f; E e[V]; } u;
+        typename El::Frag fw[NF];
+        char *own = lds + wave * kOwn;
+        if constexpr (FROM == From::kTurned) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            if constexpr (KS) {
-                fw[j] = column(nw, j);
-            } else {
-                u.v = nw[j];
-                fw[j] = u.f;
-            }
+            for (int i = 0; i < NF; ++i)
+                if ((i * 64 + lane) * V < kStep * a.rank) *reinterpret_cast<u32x4_any *>(own + (i * 64 + lane) * 16) = lw[i];
+            wave_lds();
         }
 #pragma unroll
-        for (int i = 0; i < RB; ++i) fx[i].v = nx[i];
-        if (step + kWaves < steps) load(step + kWaves);
+        for (int j = 0; j < NF; ++j) {
+            if constexpr (FROM == From::kDirect) {
+                u.v = lw[j];
+            } else if constexpr (FROM == From::kTurned) {
+                // (columns past the rank take what follows in LDS, and are not used)
+                const int line = a.rank * (int)sizeof(E);
+                if constexpr (sizeof(E) == 2) {
+                    typedef __attribute__((address_space(3))) i16x4 lds_v;
+                    union { i16x4 h[2]; u32x4 v; } r;
+                    const int o = (q * 8 + (m >> 2)) * line + (j * 16 + (m & 3) * 4) * 2;
+                    r.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v *)(own + min(o, kOwn - 8)));
+                    r.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v *)(own + min(o + 4 * line, kOwn - 8)));
+                    u.v = r.v;
+                } else {
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            if (!KS && j * 16 >= cols) break;
+                    for (int i = 0; i < V; ++i)
+                        u.e[i] = *reinterpret_cast<const E *>(own + min((q * V + i) * line + (j * 16 + m) * 4, kOwn - 4));
+                }
+            } else {
+                u.f = column(lw, j);
+            }
+            fw[j] = u.f;
+        }
+        if constexpr (FROM == From::kTurned) wave_lds();       // before the next step overwrites it
 #pragma unroll
-            for (int i = 0; i < RB; ++i) acc[i][j] = El::mma(fw[j], fx[i].f, acc[i][j]);
+        for (int i = 0; i < RB; ++i) {
+            u.v = lx[i];
+#pragma unroll
+            for (int j = 0; j < NF; ++j) acc[i][j] = El::mma(fw[j], u.f, acc[i][j]);
+        }
+    };
+    // kDeep steps in flight, in turn (a step past the last is zeros on both sides)
+#pragma unroll
+    for (int d = 0; d < kDeep; ++d) load(nw[d], nx[d], wave + d * kWaves);
+    for (int step = wave; step < steps; step += kDeep * kWaves) {
+#pragma unroll
+        for (int d = 0; d < kDeep; ++d) {
+            consume(nw[d], nx[d]);
+            load(nw[d], nx[d], step + (kDeep + d) * kWaves);
         }
     }
 
+    f32x4 *part = reinterpret_cast<f32x4 *>(lds);
+    __syncthreads();
 #pragma unroll
     for (int half = kWaves / 2; half; half /= 2) {
         if (wave >= half && wave < 2 * half)
 #pragma unroll
-            for (int i = 0; i < kAcc; ++i) part[((wave - half) * kAcc + i) * 64 + lane] = acc[i / V][i % V];
+            for (int i = 0; i < kAcc; ++i) part[((wave - half) * kAcc + i) * 64 + lane] = acc[i / NF][i % NF];
         __syncthreads();
         if (wave < half)
 #pragma unroll
-            for (int i = 0; i < kAcc; ++i) acc[i / V][i % V] += part[(wave * kAcc + i) * 64 + lane];
+            for (int i = 0; i < kAcc; ++i) acc[i / NF][i % NF] += part[(wave * kAcc + i) * 64 + lane];
         __syncthreads();
     }
     if (wave != 0) return;
 
-    // lane: place m of block i; KS: columns (4 q + e) V + j, else 16 j + 4 q + e.
-    // Zeros past the rank (not 0 x infinity).
+    // lane: place m of block i; columns 16 j + 4 q + e, kAny: (4 q + e) V + j.  Zeros past the
+    // rank (not 0 x infinity).
     const float s = a.scale ? a.scale[rt.g] : 1.0f;
     const int blocks = (a.rank + kRankBlock - 1) / kRankBlock;
 #pragma unroll
@@ -108,33 +160,50 @@ __global__ void __launch_bounds__(kWaves * 64) k_shrink(ShrinkArgs a) {
             for (int e = 0; e < 4; ++e) v[e] = c + e < cols ? v[e] * s : 0.0f;
             store_low<E>(at + (c0 + c) / kRankBlock * kLowBytes, (c0 + c) % kRankBlock, v);
         };
+        if constexpr (FROM == From::kAny) {
 #pragma unroll
-        for (int j = 0; j < V; j += KS ? 4 : 1)
-            if constexpr (KS) {
+            for (int j = 0; j < NF; j += 4)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     put((4 * q + e) * V + j, f32x4{acc[i][j][e], acc[i][j + 1][e], acc[i][j + 2][e], acc[i][j + 3][e]});
-            } else {
-                put(j * 16 + 4 * q, acc[i][j]);
-            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < NF; ++j) put(j * 16 + 4 * q, acc[i][j]);
+            if constexpr (NF == 1) put(16 + 4 * q, f32x4{});       // the block's other half
+        }
     }
 }
 
-template <class E, bool KS>
+template <class E, From FROM, int NF>
 hipError_t go(const ShrinkArgs &a, int cus, hipStream_t s) {
-    constexpr int kCols = 16 * Elem<E>::kEpc;
-    const int ct = (a.rank + kCols - 1) / kCols;
+    const int ct = FROM == From::kAny ? (a.rank + 16 * NF - 1) / (16 * NF) : 1;
     auto tiles = [&](int bm) { return static_cast<uint32_t>(a.g.n / bm + (a.g.n < a.g.G ? a.g.n : a.g.G)); };
-    // two blocks of rows share the weights' loads where that leaves the device full
-    if (a.g.n >= 32 * 2 * cus) return launch_kernel(k_shrink<E, KS, 2>, dim3(tiles(32) * ct), dim3(kWaves * 64), 0, s, a);
-    return launch_kernel(k_shrink<E, KS, 1>, dim3(tiles(16) * ct), dim3(kWaves * 64), 0, s, a);
+    // two blocks of rows share the weights' loads where the device stays full
+    if constexpr (FROM != From::kAny && NF <= 4)
+        if (a.g.n >= 32 * cus) return launch_kernel(k_shrink<E, FROM, NF, 2>, dim3(tiles(32)), dim3(kWaves * 64), 0, s, a);
+    return launch_kernel(k_shrink<E, FROM, NF, 1>, dim3(tiles(16) * ct), dim3(kWaves * 64), 0, s, a);
+}
+
+template <class E, From FROM>
+hipError_t ranks(const ShrinkArgs &a, int cus, hipStream_t s) {
+    if (a.rank <= 16) return go<E, FROM, 1>(a, cus, s);
+    if (a.rank <= 32) return go<E, FROM, 2>(a, cus, s);
+    if (a.rank <= 64) return go<E, FROM, 4>(a, cus, s);
+    return go<E, FROM, 8>(a, cus, s);
+}
+
+template <class E>
+hipError_t pick(bool ks, const ShrinkArgs &a, int cus, hipStream_t s) {
+    constexpr int V = Elem<E>::kEpc;
+    if (!ks) return ranks<E, From::kDirect>(a, cus, s);
+    if (a.rank % V == 0 && (reinterpret_cast<uintptr_t>(a.w) & 15) == 0) return ranks<E, From::kTurned>(a, cus, s);
+    return go<E, From::kAny, V>(a, cus, s);
 }
 
 }  // namespace
 
 hipError_t launch_shrink(bool bf16, bool ks, const ShrinkArgs &a, int cus, hipStream_t s) {
-    if (bf16) return ks ? go<__bf16, true>(a, cus, s) : go<__bf16, false>(a, cus, s);
-    return ks ? go<float, true>(a, cus, s) : go<float, false>(a, cus, s);
+    return bf16 ? pick<__bf16>(ks, a, cus, s) : pick<float>(ks, a, cus, s);
 }
 
 }  // namespace hwr

@@ -242,6 +242,13 @@ __device__ inline void load_lds(const char *src, char *dst) {
     typedef __attribute__((address_space(3))) void *lds_p;
     __builtin_amdgcn_global_load_lds((global_p)src, (lds_p)dst, 16, 0, 0);
 }
+// LDS written by other lanes of the wave before this point may be read after it, and
+// the other way round (the lanes run together: the compiler has to keep the order).
+__device__ inline void wave_lds() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 template <int VM>
 __device__ inline void wait_vm() {    // at most VM vector-memory loads in flight
     __builtin_amdgcn_s_waitcnt(0x0F70 | (VM & 15) | (VM >> 4) << 14);

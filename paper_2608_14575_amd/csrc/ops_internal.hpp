@@ -80,8 +80,8 @@ struct GroupRowsArgs {
     int n, n_table, G;
     const int32_t *choice, *table;
     int32_t *offsets, *order;
-    int32_t *hist;                // [G + 1][blocks] work space
-    int blocks;
+    int blocks;                   // 1: one launch, without work space
+    int32_t *hist, *totals;       // [G + 1][blocks], [G + 1] work space
 };
 
 enum class RowsKind { kGrouped, kAdapter };

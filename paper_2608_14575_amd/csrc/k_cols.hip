@@ -15,18 +15,36 @@ struct ColsTile {
     int g, ip, iq, part, p0, p1;
 };
 
-// Every L2 takes a share of every group (groups differ in places, and so in work),
-// in panels of 8 tiles as the products by row; parts side by side.
+// The group whose turn it is, the largest first (up to 64 groups; more go as they
+// stand): the long workgroups then start early, and short ones fill the end.
+__device__ inline int largest_group(const GroupsArg &g, int turn) {
+    if (g.G > 64) return turn;
+    const int lane = threadIdx.x & 63;
+    const int size = lane < g.G ? place_of(g, lane + 1) - place_of(g, lane) : 0;
+    int before = 0;
+    for (int i = 0; i < g.G; ++i) {
+        const int other = __builtin_amdgcn_readlane(size, i);
+        before += other > size || (other == size && i < lane);
+    }
+    return __builtin_ctzll(__ballot(lane < g.G && before == turn));
+}
+
+// The tiles of a group (with their parts side by side) are cut into shares of about
+// 16, which go to the L2s in turn: 4 x 4 tiles that run together read 8 panels of rows.
+__host__ __device__ inline int cols_shares(int64_t per) { return per < 32 ? 1 : per < 128 ? static_cast<int>(per / 16) : 8; }
+
 template <ColsKind KIND, int BP, int BQ, int kBk>
 __device__ inline bool my_tile(const ColsArgs &a, ColsTile &t) {
     const int tp = KIND == ColsKind::kLowP ? a.blocks : (a.np + BP - 1) / BP;
     const int tq = KIND == ColsKind::kLowQ ? a.blocks : (a.nq + BQ - 1) / BQ;
-    const int per = tp * tq * a.parts, share = (per + 7) >> 3, at = blockIdx.x >> 3;
-    t.g = at / share;
-    const int in_group = ((blockIdx.x + t.g) & 7) * share + at % share, tile = in_group / a.parts;
-    if (in_group >= per) return false;
+    const int per = tp * tq * a.parts, shares = cols_shares(per), share = (per + shares - 1) / shares;
+    const int at = blockIdx.x >> 3, turn = at / share * 8 + (blockIdx.x & 7);
+    const int in_group = turn % shares * share + at % share;
+    if (turn >= a.g.G * shares || in_group >= per) return false;
+    t.g = largest_group(a.g, turn / shares);
+    const int tile = in_group / a.parts;
     t.part = in_group % a.parts;
-    const int panel = tile / (8 * tq) * 8, in = tile - panel * tq, rp = min(8, tp - panel);
+    const int panel = tile / (4 * tq) * 4, in = tile - panel * tq, rp = min(4, tp - panel);
     t.ip = panel + in % rp;
     t.iq = in / rp;
     t.p0 = place_of(a.g, t.g);
@@ -185,7 +203,10 @@ __global__ void __launch_bounds__(WP *WQ * 64) k_cols_direct(ColsArgs a) {
     static_assert(PT::kChunks % NT == 0 && QT::kChunks % NT == 0);
     // an array each, so that the compiler sees that reads of one do not depend on the
     // loads in flight into the other
-    __shared__ __attribute__((aligned(16))) char buf0[PT::kBytes + QT::kBytes], buf1[PT::kBytes + QT::kBytes];
+    constexpr int kBuf = PT::kBytes + QT::kBytes;
+    __shared__ __attribute__((aligned(16))) char buf0[kBuf], buf1[kBuf];
+    constexpr bool kDeep = BP == 64 && BQ == 64;     // run_stages_deep
+    __shared__ __attribute__((aligned(16))) char buf2[kDeep ? kBuf : 16], buf3[kDeep ? kBuf : 16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wp = wave / WQ, wq = wave % WQ;
     ColsTile t;
@@ -207,40 +228,46 @@ __global__ void __launch_bounds__(WP *WQ * 64) k_cols_direct(ColsArgs a) {
     }
     // rows (or places) of a stage's lines; -1: zeros.  Tiles of one width share them.
     constexpr bool kShared = KIND == ColsKind::kDense && BP == BQ;
-    int pr[UP], qr[kShared ? 1 : UQ];
-    auto look_up = [&](int stage) {
+    // Looked up one stage before they are loaded, or four (run_stages_deep), in turn.
+    constexpr int kSlots = kDeep ? 4 : 1, kLead = kDeep ? 4 : 1;
+    int pr[kSlots][UP], qr[kSlots][kShared ? 1 : UQ];
+    auto look_up = [&](int stage, int slot) {
         const int p = t.p0 + stage * kBk;
 #pragma unroll
         for (int i = 0; i < UP; ++i) {
             const int at = p + i * kLinesP + tid / PT::kCpl;
-            pr[i] = at >= t.p1 ? -1 : TT::kLowP ? at : row_at(a.g, at);
+            pr[slot][i] = at >= t.p1 ? -1 : TT::kLowP ? at : row_at(a.g, at);
         }
         if constexpr (!kShared)
 #pragma unroll
             for (int i = 0; i < UQ; ++i) {
                 const int at = p + i * kLinesQ + tid / QT::kCpl;
-                qr[i] = at >= t.p1 ? -1 : TT::kLowQ ? at : row_at(a.g, at);
+                qr[slot][i] = at >= t.p1 ? -1 : TT::kLowQ ? at : row_at(a.g, at);
             }
     };
     const int64_t pld = TT::kLowP ? a.blocks * kLowBytes : a.ldp * (int64_t)sizeof(E);
     const int64_t qld = TT::kLowQ ? a.blocks * kLowBytes : a.ldq * (int64_t)sizeof(E);
     const char *zeros = static_cast<const char *>(a.zeros), *ps = static_cast<const char *>(a.p),
                *qs = static_cast<const char *>(a.q);
-    auto issue = [&](char *b, int stage) {
+    auto issue = [&](char *b, int stage, auto... in_turn) {
+        constexpr int slot = kDeep ? (decltype(in_turn)::value + ... + 0) : 0;
 #pragma unroll
         for (int i = 0; i < UP; ++i)
-            load_lds(pr[i] < 0 ? zeros : ps + pr[i] * pld + pb[i % BPN], b + (i * NT + wave * 64) * 16);
+            load_lds(pr[slot][i] < 0 ? zeros : ps + pr[slot][i] * pld + pb[i % BPN], b + (i * NT + wave * 64) * 16);
 #pragma unroll
         for (int i = 0; i < UQ; ++i) {
-            const int r = kShared ? pr[i] : qr[kShared ? 0 : i];
+            const int r = kShared ? pr[slot][i] : qr[slot][kShared ? 0 : i];
             load_lds(r < 0 ? zeros : qs + r * qld + qb[i % BQN], b + PT::kBytes + (i * NT + wave * 64) * 16);
         }
-        look_up(stage + 1);
+        look_up(stage + kLead, (slot + kLead) % kSlots);
     };
     f32x4 acc[PF][QF] = {};
     if (t.p0 < t.p1) {
-        look_up(0);
-        run_stages<E, PT, QT, PF, QF>((t.p1 - t.p0 + kBk - 1) / kBk, issue, buf0, buf1, wp * PF * 16, wq * QF * 16, lane, acc);
+        const int stages = (t.p1 - t.p0 + kBk - 1) / kBk, p_at = wp * PF * 16, q_at = wq * QF * 16;
+#pragma unroll
+        for (int i = 0; i < kLead; ++i) look_up(i, i);
+        if constexpr (kDeep) run_stages_deep<E, PT, QT, PF, QF, UP + UQ>(stages, issue, buf0, buf1, buf2, buf3, p_at, q_at, lane, acc);
+        else run_stages<E, PT, QT, PF, QF>(stages, issue, buf0, buf1, p_at, q_at, lane, acc);
     }
     store_tile<E, KIND, BP, BQ, WP, WQ>(a, t, acc, lane, wp, wq);
 }
@@ -278,7 +305,8 @@ template <class E, ColsKind KIND, int BP, int BQ, int WP, int WQ, bool DIRECT>
 hipError_t go(const ColsArgs &a, hipStream_t s) {
     const int64_t tp = KIND == ColsKind::kLowP ? a.blocks : (a.np + BP - 1) / BP;
     const int64_t tq = KIND == ColsKind::kLowQ ? a.blocks : (a.nq + BQ - 1) / BQ;
-    const int64_t blocks = (tp * tq * a.parts + 7) / 8 * 8 * a.g.G;
+    const int64_t per = tp * tq * a.parts, shares = cols_shares(per), share = (per + shares - 1) / shares;
+    const int64_t blocks = (a.g.G * shares + 7) / 8 * 8 * share;
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
     const dim3 grid(static_cast<uint32_t>(blocks)), block(WP * WQ * 64);
     hipError_t e;

@@ -252,6 +252,8 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows_direct(RowsArgs a) {
     // an array each, so that the compiler sees that reads of one do not depend on the
     // loads in flight into the other
     __shared__ __attribute__((aligned(16))) char buf0[kBuf], buf1[kBuf];
+    constexpr bool kDeep = BM == 64;       // run_stages_deep
+    __shared__ __attribute__((aligned(16))) char buf2[kDeep ? kBuf : 16], buf3[kDeep ? kBuf : 16];
     __shared__ int rows[BM];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wr = wave / WC, wc = wave % WC;
@@ -281,7 +283,7 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows_direct(RowsArgs a) {
         return kOneOrder ? at : at + chunk(i) * sizeof(E);
     };
     const int64_t wstep = KS ? static_cast<int64_t>(kBk) * a.m * sizeof(E) : kStageBytes;
-    auto issue = [&](char *b, int stage) {
+    auto issue = [&](char *b, int stage, auto...) {
         const int k0 = stage * kBk;
         if (k0 + kBk <= k) {
 #pragma unroll
@@ -303,7 +305,12 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows_direct(RowsArgs a) {
         wp += wstep;
     };
     f32x4 acc[RF][CF] = {};
-    if (k > 0) run_stages<E, XT, WT, RF, CF>((k + kBk - 1) / kBk, issue, buf0, buf1, wr * RF * 16, wc * CF * 16, lane, acc);
+    const int stages = (k + kBk - 1) / kBk, x0 = wr * RF * 16, w0 = wc * CF * 16;
+    if constexpr (kDeep) {
+        if (k > 0) run_stages_deep<E, XT, WT, RF, CF, UX + UW>(stages, issue, buf0, buf1, buf2, buf3, x0, w0, lane, acc);
+    } else {
+        if (k > 0) run_stages<E, XT, WT, RF, CF>(stages, issue, buf0, buf1, x0, w0, lane, acc);
+    }
     __syncthreads();
 
     if constexpr (KIND == RowsKind::kAdapter) add_adapters<E, KS, BM, BN, WR, WC>(a, rt, c0, buf0, buf0 + XT::kBytes, acc, tid);

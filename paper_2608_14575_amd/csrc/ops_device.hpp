@@ -9,6 +9,8 @@
 // column or row l % 16, the contraction elements of its quarter l / 16.
 #pragma once
 
+#include <type_traits>
+
 #include "ops_internal.hpp"
 
 namespace hwr {
@@ -333,6 +335,65 @@ __device__ inline void run_stages(int stages, Issue issue, char *buf0, char *buf
     for (; s < stages; s += 2) {
         stage(buf0, buf1, s);
         stage(buf1, buf0, s + 1);
+    }
+}
+
+// The same with four buffers, for tiles whose products take less than the way from
+// memory: three stages are in flight.  issue is also told the stage modulo 4, as a
+// constant.  (Few sums: the loop may be left anywhere.)
+template <class E, class XT, class WT, int RF, int CF, int LOADS, class Issue>
+__device__ inline void run_stages_deep(int stages, Issue issue, char *buf0, char *buf1, char *buf2, char *buf3, int x0, int w0,
+                                       int lane, f32x4 (&acc)[RF][CF]) {
+    using El = Elem<E>;
+    typename El::Frag x[2][RF], w[2][CF];
+    auto read = [&](const char *b, int half) {
+#pragma unroll
+        for (int j = 0; j < CF; ++j) w[half][j] = WT::frag(b, XT::kBytes, w0 + j * 16, half, lane);
+#pragma unroll
+        for (int i = 0; i < RF; ++i) x[half][i] = XT::frag(b, 0, x0 + i * 16, half, lane);
+    };
+    auto multiply = [&](int half) {
+#pragma unroll
+        for (int i = 0; i < RF; ++i)
+#pragma unroll
+            for (int j = 0; j < CF; ++j) acc[i][j] = El::mma(w[half][j], x[half][i], acc[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto stage = [&](char *cur, char *next, auto slot, int s) {
+        read(cur, 1);
+        multiply(0);
+        wait_lds();
+        if (s + 3 < stages) wait_vm<2 * LOADS>();
+        else wait_vm<0>();
+        barrier();
+        if (s + 4 < stages) issue(cur, s + 4, slot);
+        read(next, 0);
+        multiply(1);
+    };
+    constexpr std::integral_constant<int, 0> c0{};
+    constexpr std::integral_constant<int, 1> c1{};
+    constexpr std::integral_constant<int, 2> c2{};
+    constexpr std::integral_constant<int, 3> c3{};
+    issue(buf0, 0, c0);
+    if (stages > 1) issue(buf1, 1, c1);
+    if (stages > 2) issue(buf2, 2, c2);
+    if (stages > 3) {
+        issue(buf3, 3, c3);
+        wait_vm<3 * LOADS>();
+    } else {
+        wait_vm<0>();
+    }
+    barrier();
+    read(buf0, 0);
+    for (int s = 0;;) {
+        stage(buf0, buf1, c0, s);
+        if (++s >= stages) break;
+        stage(buf1, buf2, c1, s);
+        if (++s >= stages) break;
+        stage(buf2, buf3, c2, s);
+        if (++s >= stages) break;
+        stage(buf3, buf0, c3, s);
+        if (++s >= stages) break;
     }
 }
 

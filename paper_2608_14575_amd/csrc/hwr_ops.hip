@@ -159,9 +159,10 @@ hwr_status shrink(hwr_ops *c, const hwr_groups *g, int32_t dtype, bool ks, const
     return HWR_OK;
 }
 
-// y[row] = x[row] w + low[place] lw_g
-hwr_status expand(hwr_ops *c, const hwr_groups *g, int32_t dtype, bool ks, const void *x, int64_t ldx, int k, const void *w,
-                  int m, const void *low, const void *lw, int rank, void *y, int64_t ldy) {
+// A product by row, with its partial sums past the first `used` bytes of the work
+// space (the call has reserved them: rows_bytes).
+RowsArgs rows_args(hwr_ops *c, const hwr_groups *g, const void *x, int64_t ldx, int k, const void *w, int64_t w_stride, int m,
+                   void *y, int64_t ldy) {
     RowsArgs r{};
     r.g = groups_arg(g);
     r.k = k;
@@ -169,13 +170,33 @@ hwr_status expand(hwr_ops *c, const hwr_groups *g, int32_t dtype, bool ks, const
     r.x = x;
     r.ldx = ldx;
     r.w = w;
+    r.w_stride = w_stride;
     r.y = y;
     r.ldy = ldy;
-    r.low = low;
-    r.lw = lw;
-    r.rank = rank;
     r.zeros = c->zeros;
-    OPS_HIP(c, launch_rows(dtype == HWR_BF16, RowsKind::kAdapter, ks, r, c->cus, c->stream));
+    r.m_pad = (m + 3) / 4 * 4;
+    return r;
+}
+uint64_t rows_bytes(hwr_ops *c, bool bf16, RowsKind kind, bool ks, const RowsArgs &r) {
+    const int parts = rows_plan(bf16, kind, ks, r, c->cus).parts;
+    return parts > 1 ? static_cast<uint64_t>(parts) * r.g.n * r.m_pad * sizeof(float) : 0;
+}
+hwr_status rows(hwr_ops *c, bool bf16, RowsKind kind, bool ks, RowsArgs r, uint64_t used) {
+    char *ws = nullptr;
+    if (hwr_status st = workspace(c, used + rows_bytes(c, bf16, kind, ks, r), &ws)) return st;
+    r.parts = rows_plan(bf16, kind, ks, r, c->cus).parts;
+    r.partial = reinterpret_cast<float *>(ws + used);
+    OPS_HIP(c, launch_rows(bf16, kind, ks, r, c->cus, c->stream));
+    if (r.parts == 1) return HWR_OK;
+    FewArgs f{};
+    f.g = r.g;
+    f.m = r.m;
+    f.m_pad = r.m_pad;
+    f.y = r.y;
+    f.ldy = r.ldy;
+    f.parts = r.parts;
+    f.partial = r.partial;
+    OPS_HIP(c, launch_join(bf16, f, c->stream));
     return HWR_OK;
 }
 
@@ -257,19 +278,9 @@ hwr_status grouped_matmul(hwr_ops *c, const hwr_groups *g, const hwr_matmul_args
         f.ldy = dense(a->ldy, a->m);
         return few(c, f, a->dtype == HWR_BF16, false);
     }
-    RowsArgs r{};
-    r.g = groups_arg(g);
-    r.k = a->k;
-    r.m = a->m;
-    r.x = a->x;
-    r.ldx = dense(a->ldx, a->k);
-    r.w = a->w;
-    r.w_stride = static_cast<int64_t>(a->k) * a->m;
-    r.y = a->y;
-    r.ldy = dense(a->ldy, a->m);
-    r.zeros = c->zeros;
-    OPS_HIP(c, launch_rows(a->dtype == HWR_BF16, RowsKind::kGrouped, true, r, c->cus, c->stream));
-    return HWR_OK;
+    const RowsArgs r = rows_args(c, g, a->x, dense(a->ldx, a->k), a->k, a->w, static_cast<int64_t>(a->k) * a->m, a->m, a->y,
+                                 dense(a->ldy, a->m));
+    return rows(c, a->dtype == HWR_BF16, RowsKind::kGrouped, true, r, 0);
 }
 
 hwr_status grouped_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_matmul_grad_args *a) {
@@ -285,18 +296,9 @@ hwr_status grouped_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_matmul
     if (hwr_status st = use_device(c)) return st;
     const bool bf16 = a->dtype == HWR_BF16;
     if (a->dx && g->n > 0) {
-        RowsArgs r{};
-        r.g = groups_arg(g);
-        r.k = a->m;
-        r.m = a->k;
-        r.x = a->dy;
-        r.ldx = dense(a->lddy, a->m);
-        r.w = a->w;
-        r.w_stride = static_cast<int64_t>(a->k) * a->m;
-        r.y = a->dx;
-        r.ldy = dense(a->lddx, a->k);
-        r.zeros = c->zeros;
-        OPS_HIP(c, launch_rows(bf16, RowsKind::kGrouped, false, r, c->cus, c->stream));
+        const RowsArgs r = rows_args(c, g, a->dy, dense(a->lddy, a->m), a->m, a->w, static_cast<int64_t>(a->k) * a->m, a->k,
+                                     a->dx, dense(a->lddx, a->k));
+        if (hwr_status st = rows(c, bf16, RowsKind::kGrouped, false, r, 0)) return st;
     }
     if (a->dw) {
         ColsArgs w{};
@@ -342,10 +344,16 @@ hwr_status adapter_matmul(hwr_ops *c, const hwr_groups *g, const hwr_adapter_arg
         f.scale = a->scale;
         return few(c, f, a->dtype == HWR_BF16, true);
     }
+    const bool bf16 = a->dtype == HWR_BF16;
+    RowsArgs r = rows_args(c, g, a->x, ldx, a->k, a->w, 0, a->m, a->y, dense(a->ldy, a->m));
+    r.lw = a->b;
+    r.rank = a->rank;
+    const uint64_t each = low_bytes(g->n, a->rank);
     char *low = nullptr;
-    if (hwr_status st = workspace(c, low_bytes(g->n, a->rank), &low)) return st;
+    if (hwr_status st = workspace(c, each + rows_bytes(c, bf16, RowsKind::kAdapter, true, r), &low)) return st;
     if (hwr_status st = shrink(c, g, a->dtype, true, a->x, ldx, a->k, a->a, a->rank, a->scale, low)) return st;
-    return expand(c, g, a->dtype, true, a->x, ldx, a->k, a->w, a->m, low, a->b, a->rank, a->y, dense(a->ldy, a->m));
+    r.low = low;
+    return rows(c, bf16, RowsKind::kAdapter, true, r, each);
 }
 
 hwr_status adapter_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_adapter_grad_args *a) {
@@ -378,8 +386,12 @@ hwr_status adapter_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_adapte
     wb.q = a->dy;
     wb.ldq = lddy;
     wb.out = a->db;
-    const uint64_t parts = std::max(a->da ? weight_grad_bytes(c, bf16, ColsKind::kLowQ, wa) : 0,
-                                    a->db ? weight_grad_bytes(c, bf16, ColsKind::kLowP, wb) : 0);
+    RowsArgs r = rows_args(c, g, a->dy, lddy, a->m, a->w, 0, a->k, a->dx, dense(a->lddx, a->k));
+    r.lw = a->a;
+    r.rank = a->rank;
+    const uint64_t parts = std::max({a->da ? weight_grad_bytes(c, bf16, ColsKind::kLowQ, wa) : 0,
+                                     a->db ? weight_grad_bytes(c, bf16, ColsKind::kLowP, wb) : 0,
+                                     a->dx ? rows_bytes(c, bf16, RowsKind::kAdapter, false, r) : 0});
     char *ws = nullptr;
     if (hwr_status st = workspace(c, 2 * each + parts, &ws)) return st;
     char *up = ws, *low = ws + each;
@@ -387,10 +399,10 @@ hwr_status adapter_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_adapte
         if (hwr_status st = shrink(c, g, a->dtype, false, a->dy, lddy, a->m, a->b, a->rank, a->scale, up)) return st;
     if (g->n > 0 && a->db)
         if (hwr_status st = shrink(c, g, a->dtype, true, a->x, ldx, a->k, a->a, a->rank, a->scale, low)) return st;
-    if (g->n > 0 && a->dx)
-        if (hwr_status st = expand(c, g, a->dtype, false, a->dy, lddy, a->m, a->w, a->k, up, a->a, a->rank, a->dx,
-                                   dense(a->lddx, a->k)))
-            return st;
+    if (g->n > 0 && a->dx) {
+        r.low = up;
+        if (hwr_status st = rows(c, bf16, RowsKind::kAdapter, false, r, 2 * each)) return st;
+    }
     if (a->da) {
         wa.q = up;
         if (hwr_status st = weight_grad(c, bf16, ColsKind::kLowQ, wa, 2 * each)) return st;

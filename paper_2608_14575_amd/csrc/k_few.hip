@@ -223,6 +223,13 @@ __global__ void __launch_bounds__(kJoinThreads) k_join(FewArgs a) {
 }
 
 template <class E, bool ADAPTER>
+hipError_t join(const FewArgs &a, hipStream_t s) {
+    const int64_t blocks = static_cast<int64_t>((a.m_pad / 4 + kJoinThreads - 1) / kJoinThreads) * a.g.n;
+    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    return launch_kernel(k_join<E, ADAPTER>, dim3(static_cast<uint32_t>(blocks)), dim3(kJoinThreads), 0, s, a);
+}
+
+template <class E, bool ADAPTER>
 hipError_t go(const FewArgs &a, hipStream_t s) {
     const int ct = (a.m + 16 * Elem<E>::kEpc - 1) / (16 * Elem<E>::kEpc);
     const int64_t items = static_cast<int64_t>(few_tiles(a.g.n, a.g.G, ADAPTER)) * ct * a.parts +
@@ -231,9 +238,7 @@ hipError_t go(const FewArgs &a, hipStream_t s) {
     const dim3 grid(static_cast<uint32_t>(items)), block(kWaves * 64);
     const hipError_t e = launch_kernel(k_few<E, ADAPTER>, grid, block, 0, s, a);
     if (e != hipSuccess || (!ADAPTER && a.parts == 1)) return e;
-    const int64_t join = static_cast<int64_t>((a.m_pad / 4 + kJoinThreads - 1) / kJoinThreads) * a.g.n;
-    if (join > INT32_MAX) return hipErrorInvalidValue;
-    return launch_kernel(k_join<E, ADAPTER>, dim3(static_cast<uint32_t>(join)), dim3(kJoinThreads), 0, s, a);
+    return join<E, ADAPTER>(a, s);
 }
 
 }  // namespace
@@ -259,6 +264,10 @@ int few_parts(int n, int G, int k, int m, bool bf16, bool adapter, int cus) {
 hipError_t launch_few(bool bf16, bool adapter, const FewArgs &a, hipStream_t s) {
     if (bf16) return adapter ? go<__bf16, true>(a, s) : go<__bf16, false>(a, s);
     return adapter ? go<float, true>(a, s) : go<float, false>(a, s);
+}
+
+hipError_t launch_join(bool bf16, const FewArgs &a, hipStream_t s) {
+    return bf16 ? join<__bf16, false>(a, s) : join<float, false>(a, s);
 }
 
 }  // namespace hwr

@@ -109,12 +109,26 @@ __device__ inline void add_adapters(const RowsArgs &a, const RowTile &rt, int c0
 
 // A lane holds, for row l % 16 of fragment i, four columns of fragment j.
 template <class E, int BM, int BN, int WR, int WC>
-__device__ inline void store_rows(const RowsArgs &a, int c0, const int *rows,
+__device__ inline void store_rows(const RowsArgs &a, const RowTile &rt, int c0, int part, const int *rows,
                                   const f32x4 (&acc)[BM / WR / 16][BN / WC / 16], int tid) {
     constexpr int RF = BM / WR / 16, CF = BN / WC / 16;
     using El = Elem<E>;
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WC, wc = wave % WC;
     const int q = lane >> 4;
+    if (a.parts > 1) {
+        float *out = a.partial + static_cast<int64_t>(part) * a.g.n * a.m_pad;
+#pragma unroll
+        for (int i = 0; i < RF; ++i) {
+            const int p = rt.p0 + (wr * RF + i) * 16 + (lane & 15);
+            if (p >= rt.p1) continue;
+#pragma unroll
+            for (int j = 0; j < CF; ++j) {
+                const int c = c0 + (wc * CF + j) * 16 + q * 4;
+                if (c < a.m_pad) *reinterpret_cast<f32x4_a4 *>(out + static_cast<int64_t>(p) * a.m_pad + c) = acc[i][j];
+            }
+        }
+        return;
+    }
     E *y = static_cast<E *>(a.y);
     const bool vec = (a.m & 3) == 0 && (a.ldy & 3) == 0 && (reinterpret_cast<uintptr_t>(y) & (4 * sizeof(E) - 1)) == 0;
 #pragma unroll
@@ -138,16 +152,18 @@ __device__ inline void store_rows(const RowsArgs &a, int c0, const int *rows,
     }
 }
 
-// The workgroup's tile of places and first column.  Tiles go in panels of 8 row
+// The workgroup's tile of places, first column and part.  Tiles go in panels of 8 row
 // tiles, column by column, so that the workgroups that run together on one L2
 // share rows and weights.  False past the last tile.
 template <RowsKind KIND, int BM, int BN>
-__device__ inline bool my_tile(const RowsArgs &a, int lane, RowTile &rt, int &c0) {
+__device__ inline bool my_tile(const RowsArgs &a, int lane, RowTile &rt, int &c0, int &part) {
     const bool tail = KIND == RowsKind::kGrouped;
     const int tiles = KIND == RowsKind::kAdapter ? (a.g.n + BM - 1) / BM : count_tiles(a.g, BM, tail, lane);
     const int ct = (a.m + BN - 1) / BN;
-    const int item = xcd_item(blockIdx.x, tiles * ct);
+    int item = xcd_item(blockIdx.x, tiles * ct * a.parts);
     if (item < 0) return false;
+    part = item / (tiles * ct);
+    item -= part * (tiles * ct);
     const int panel = item / (8 * ct) * 8, in = item - panel * ct, rp = min(8, tiles - panel);
     const int t = panel + in % rp;
     // the last tile of columns ends with the row: it shares columns with the one before
@@ -156,6 +172,12 @@ __device__ inline bool my_tile(const RowsArgs &a, int lane, RowTile &rt, int &c0
     if (KIND == RowsKind::kAdapter) rt = {0, t * BM, min(t * BM + BM, a.g.n)};
     else rt = find_tile(a.g, t, BM, tail, lane);
     return true;
+}
+
+// Stages of a part of the contraction.
+__device__ inline void my_stages(int stages, int part, int parts, int &first, int &last) {
+    first = static_cast<int>(static_cast<int64_t>(stages) * part / parts);
+    last = static_cast<int>(static_cast<int64_t>(stages) * (part + 1) / parts);
 }
 
 // Any widths, strides and alignment: operands pass through registers.
@@ -170,8 +192,8 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows(RowsArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wr = wave / WC, wc = wave % WC;
     RowTile rt;
-    int c0;
-    if (!my_tile<KIND, BM, BN>(a, lane, rt, c0)) return;
+    int c0, part;
+    if (!my_tile<KIND, BM, BN>(a, lane, rt, c0, part)) return;
 
     for (int i = tid; i < BM; i += NT) rows[i] = rt.p0 + i < rt.p1 ? row_at(a.g, rt.p0 + i) : -1;
     __syncthreads();
@@ -179,6 +201,8 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows(RowsArgs a) {
     const E *x = static_cast<const E *>(a.x);
     const E *w = static_cast<const E *>(a.w) + (KIND == RowsKind::kAdapter ? 0 : rt.g) * a.w_stride;
     const int k = KIND == RowsKind::kGrouped && rt.g == a.g.G ? 0 : a.k;
+    int first, last;
+    my_stages((k + kBk - 1) / kBk, part, a.parts, first, last);
 
     auto weights = [&](const E *base, int k0, int klen) {   // KS: lines are elements; else columns
         return [=, &a](int line, int c) {
@@ -201,17 +225,17 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows(RowsArgs a) {
     f32x4 acc[RF][CF] = {};
     Staged<E, false, BM, NT> gx;
     Staged<E, KS, BN, NT> gw;
-    if (k > 0) {
-        gx.load(inputs(0), tid);
-        gw.load(weights(w, 0, k), tid);
+    if (first < last) {
+        gx.load(inputs(first * kBk), tid);
+        gw.load(weights(w, first * kBk, k), tid);
     }
-    for (int k0 = 0; k0 < k; k0 += kBk) {
+    for (int stage = first; stage < last; ++stage) {
         gx.store(sx, tid);
         gw.store(sw, tid);
         __syncthreads();
-        if (k0 + kBk < k) {
-            gx.load(inputs(k0 + kBk), tid);
-            gw.load(weights(w, k0 + kBk, k), tid);
+        if (stage + 1 < last) {
+            gx.load(inputs((stage + 1) * kBk), tid);
+            gw.load(weights(w, (stage + 1) * kBk, k), tid);
         }
 #pragma unroll
         for (int sub = 0; sub < 2; ++sub) {
@@ -228,8 +252,9 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows(RowsArgs a) {
         __syncthreads();
     }
 
-    if constexpr (KIND == RowsKind::kAdapter) add_adapters<E, KS, BM, BN, WR, WC>(a, rt, c0, sx, sw, acc, tid);
-    store_rows<E, BM, BN, WR, WC>(a, c0, rows, acc, tid);
+    if constexpr (KIND == RowsKind::kAdapter)
+        if (part == 0) add_adapters<E, KS, BM, BN, WR, WC>(a, rt, c0, sx, sw, acc, tid);
+    store_rows<E, BM, BN, WR, WC>(a, rt, c0, part, rows, acc, tid);
 }
 
 // Whole chunks of 16 bytes everywhere and at least BN columns: operands go from
@@ -252,24 +277,26 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows_direct(RowsArgs a) {
     // an array each, so that the compiler sees that reads of one do not depend on the
     // loads in flight into the other
     __shared__ __attribute__((aligned(16))) char buf0[kBuf], buf1[kBuf];
-    constexpr bool kDeep = BM == 64;       // run_stages_deep
+    constexpr bool kDeep = BN == 64;       // run_stages_deep
     __shared__ __attribute__((aligned(16))) char buf2[kDeep ? kBuf : 16], buf3[kDeep ? kBuf : 16];
     __shared__ int rows[BM];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wr = wave / WC, wc = wave % WC;
     RowTile rt;
-    int c0;
-    if (!my_tile<KIND, BM, BN>(a, lane, rt, c0)) return;
+    int c0, part;
+    if (!my_tile<KIND, BM, BN>(a, lane, rt, c0, part)) return;
     for (int i = tid; i < BM; i += NT) rows[i] = rt.p0 + i < rt.p1 ? row_at(a.g, rt.p0 + i) : -1;
     __syncthreads();
 
     const int k = KIND == RowsKind::kGrouped && rt.g == a.g.G ? 0 : a.k;
+    int first, last;
+    my_stages((k + kBk - 1) / kBk, part, a.parts, first, last);
     const int xline = tid / XT::kCpl, xe = ((tid % XT::kCpl) ^ XT::swz(xline)) * kEpc;   // first element of the thread's chunks
     const char *xp[UX];
 #pragma unroll
     for (int i = 0; i < UX; ++i) {
         const int r = rows[i * kLinesX + xline];
-        xp[i] = reinterpret_cast<const char *>(static_cast<const E *>(a.x) + (r < 0 ? 0 : r) * a.ldx + xe);
+        xp[i] = reinterpret_cast<const char *>(static_cast<const E *>(a.x) + (r < 0 ? 0 : r) * a.ldx + xe + first * kBk);
     }
     const E *w = static_cast<const E *>(a.w) + (KIND == RowsKind::kAdapter || k == 0 ? 0 : rt.g) * a.w_stride;
     const int wline = tid / WT::kCpl, ldw = KS ? a.m : a.k;
@@ -283,8 +310,9 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows_direct(RowsArgs a) {
         return kOneOrder ? at : at + chunk(i) * sizeof(E);
     };
     const int64_t wstep = KS ? static_cast<int64_t>(kBk) * a.m * sizeof(E) : kStageBytes;
+    wp += first * wstep;
     auto issue = [&](char *b, int stage, auto...) {
-        const int k0 = stage * kBk;
+        const int k0 = (first + stage) * kBk;
         if (k0 + kBk <= k) {
 #pragma unroll
             for (int i = 0; i < UX; ++i) load_lds(xp[i], b + (i * NT + wave * 64) * 16);
@@ -305,24 +333,25 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows_direct(RowsArgs a) {
         wp += wstep;
     };
     f32x4 acc[RF][CF] = {};
-    const int stages = (k + kBk - 1) / kBk, x0 = wr * RF * 16, w0 = wc * CF * 16;
+    const int stages = last - first, x0 = wr * RF * 16, w0 = wc * CF * 16;
     if constexpr (kDeep) {
-        if (k > 0) run_stages_deep<E, XT, WT, RF, CF, UX + UW>(stages, issue, buf0, buf1, buf2, buf3, x0, w0, lane, acc);
+        if (stages > 0) run_stages_deep<E, XT, WT, RF, CF, UX + UW>(stages, issue, buf0, buf1, buf2, buf3, x0, w0, lane, acc);
     } else {
-        if (k > 0) run_stages<E, XT, WT, RF, CF>(stages, issue, buf0, buf1, x0, w0, lane, acc);
+        if (stages > 0) run_stages<E, XT, WT, RF, CF>(stages, issue, buf0, buf1, x0, w0, lane, acc);
     }
     __syncthreads();
 
-    if constexpr (KIND == RowsKind::kAdapter) add_adapters<E, KS, BM, BN, WR, WC>(a, rt, c0, buf0, buf0 + XT::kBytes, acc, tid);
-    store_rows<E, BM, BN, WR, WC>(a, c0, rows, acc, tid);
+    if constexpr (KIND == RowsKind::kAdapter)
+        if (part == 0) add_adapters<E, KS, BM, BN, WR, WC>(a, rt, c0, buf0, buf0 + XT::kBytes, acc, tid);
+    store_rows<E, BM, BN, WR, WC>(a, rt, c0, part, rows, acc, tid);
 }
 
-template <class E, RowsKind KIND, bool KS, int BM, int BN, int WR, int WC, bool DIRECT = false>
+template <class E, RowsKind KIND, bool KS, int BM, int BN, int WR, int WC, bool DIRECT>
 hipError_t go(const RowsArgs &a, hipStream_t s) {
     const int64_t n = a.g.n;
     // a group adds at most one partial tile, and a tile holds at least one row
     const int64_t tiles = KIND == RowsKind::kAdapter ? (n + BM - 1) / BM : n / BM + (n < a.g.G + 1 ? n : a.g.G + 1);
-    const int64_t items = tiles * ((a.m + BN - 1) / BN);
+    const int64_t items = tiles * ((a.m + BN - 1) / BN) * a.parts;
     const int64_t blocks = (items + 7) / 8 * 8;
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
     const dim3 grid(static_cast<uint32_t>(blocks)), block(WR * WC * 64);
@@ -330,41 +359,55 @@ hipError_t go(const RowsArgs &a, hipStream_t s) {
     else return launch_kernel(k_rows<E, KIND, KS, BM, BN, WR, WC>, grid, block, 0, s, a);
 }
 
-// Rows and weights in whole, aligned chunks of 16 bytes.
-template <class E, bool KS>
-bool whole_chunks(const RowsArgs &a) {
-    constexpr int kEpc = Elem<E>::kEpc;
-    const auto ptrs = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w);
-    return (ptrs & 15) == 0 && a.ldx % kEpc == 0 && a.k % kEpc == 0 && (!KS || a.m % kEpc == 0);
-}
-
 template <class E, RowsKind KIND, bool KS>
-hipError_t pick(const RowsArgs &a, int cus, hipStream_t s) {
-    // the largest tile that still gives every compute unit a workgroup
-    auto tiles = [&](int64_t bm, int64_t bn) {
-        return (a.g.n / bm + (KIND == RowsKind::kAdapter ? 1 : a.g.G)) * ((a.m + bn - 1) / bn);
-    };
-    if (whole_chunks<E, KS>(a) && a.m >= 64) {
-        if constexpr (sizeof(E) == 2)
-            if (a.m >= 256 && tiles(256, 256) >= cus) return go<E, KIND, KS, 256, 256, 2, 4, true>(a, s);
-        if (a.m >= 128 && tiles(128, 128) >= cus) return go<E, KIND, KS, 128, 128, 2, 2, true>(a, s);
+hipError_t pick(const RowsPlan &p, const RowsArgs &a, hipStream_t s) {
+    if (p.direct) {
+        if constexpr (sizeof(E) == 2) {
+            if (p.bm == 256) return go<E, KIND, KS, 256, 256, 2, 4, true>(a, s);
+        } else {
+            if (p.bm == 32) return go<E, KIND, KS, 32, 64, 1, 4, true>(a, s);
+        }
+        if (p.bm == 128) return go<E, KIND, KS, 128, 128, 2, 2, true>(a, s);
         return go<E, KIND, KS, 64, 64, 2, 2, true>(a, s);
     }
-    if (tiles(128, 128) >= cus) return go<E, KIND, KS, 128, 128, 2, 2>(a, s);
-    return go<E, KIND, KS, 64, 64, 2, 2>(a, s);
+    if (p.bm == 128) return go<E, KIND, KS, 128, 128, 2, 2, false>(a, s);
+    return go<E, KIND, KS, 64, 64, 2, 2, false>(a, s);
 }
 
 template <class E>
-hipError_t pick_kind(RowsKind kind, bool ks, const RowsArgs &a, int cus, hipStream_t s) {
+hipError_t pick_kind(RowsKind kind, bool ks, const RowsPlan &p, const RowsArgs &a, hipStream_t s) {
     if (kind == RowsKind::kGrouped)
-        return ks ? pick<E, RowsKind::kGrouped, true>(a, cus, s) : pick<E, RowsKind::kGrouped, false>(a, cus, s);
-    return ks ? pick<E, RowsKind::kAdapter, true>(a, cus, s) : pick<E, RowsKind::kAdapter, false>(a, cus, s);
+        return ks ? pick<E, RowsKind::kGrouped, true>(p, a, s) : pick<E, RowsKind::kGrouped, false>(p, a, s);
+    return ks ? pick<E, RowsKind::kAdapter, true>(p, a, s) : pick<E, RowsKind::kAdapter, false>(p, a, s);
+}
+
+// Rows and weights in whole, aligned chunks of 16 bytes.
+bool whole_chunks(bool bf16, bool ks, const RowsArgs &a) {
+    const int epc = bf16 ? 8 : 4;
+    const auto ptrs = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w);
+    return (ptrs & 15) == 0 && a.ldx % epc == 0 && a.k % epc == 0 && (!ks || a.m % epc == 0);
 }
 
 }  // namespace
 
+// The largest tile that still gives every compute unit a workgroup; where even small
+// tiles do not, parts of the contraction of at least four stages.
+RowsPlan rows_plan(bool bf16, RowsKind kind, bool ks, const RowsArgs &a, int cus) {
+    auto tiles = [&](int64_t bm, int64_t bn) {
+        return (a.g.n / bm + (kind == RowsKind::kAdapter ? 1 : a.g.G)) * ((a.m + bn - 1) / bn);
+    };
+    RowsPlan p{whole_chunks(bf16, ks, a) && a.m >= 64, 64, 64, 1};
+    if (p.direct && bf16 && a.m >= 256 && tiles(256, 256) >= cus) p.bm = p.bn = 256;
+    else if ((!p.direct || a.m >= 128) && tiles(128, 128) >= cus) p.bm = p.bn = 128;
+    else if (p.direct && !bf16 && tiles(64, 64) < 2 * cus) p.bm = 32;
+    const int stages = (a.k + (bf16 ? 63 : 31)) / (bf16 ? 64 : 32);
+    while (tiles(p.bm, p.bn) * p.parts < cus && stages >= 8 * p.parts) p.parts *= 2;
+    return p;
+}
+
 hipError_t launch_rows(bool bf16, RowsKind kind, bool ks, const RowsArgs &a, int cus, hipStream_t s) {
-    return bf16 ? pick_kind<__bf16>(kind, ks, a, cus, s) : pick_kind<float>(kind, ks, a, cus, s);
+    const RowsPlan p = rows_plan(bf16, kind, ks, a, cus);
+    return bf16 ? pick_kind<__bf16>(kind, ks, p, a, s) : pick_kind<float>(kind, ks, p, a, s);
 }
 
 }  // namespace hwr

@@ -28,6 +28,9 @@ struct RowsArgs {
     void *y;
     int64_t ldy;
     const void *zeros;            // 256 zero bytes
+    int parts;                    // workgroups that share a tile's contraction (rows_plan)
+    int m_pad;                    // m up to a multiple of 4
+    float *partial;               // [parts][n][m_pad], with parts > 1
     // adapter
     const void *low;              // [n][blocks] low-rank intermediates
     const void *lw;               // [G][rank][m] (KS) or [G][m][rank]
@@ -88,13 +91,21 @@ enum class RowsKind { kGrouped, kAdapter };
 
 hipError_t launch_group_rows(const GroupRowsArgs &a, hipStream_t s);
 int group_rows_blocks(int n);
+// Tile of places and columns, and parts, for a product by row.
+struct RowsPlan {
+    bool direct;                  // whole chunks: straight into LDS
+    int bm, bn, parts;
+};
 // ks: weights [k][m]; else [m][k]
+RowsPlan rows_plan(bool bf16, RowsKind kind, bool ks, const RowsArgs &a, int cus);
 hipError_t launch_rows(bool bf16, RowsKind kind, bool ks, const RowsArgs &a, int cus, hipStream_t s);
 hipError_t launch_shrink(bool bf16, bool ks, const ShrinkArgs &a, int cus, hipStream_t s);
 bool few_rows(int n, int G, bool adapter);              // whether launch_few is meant for the batch
 int few_tiles(int n, int G, bool adapter);
 int few_parts(int n, int G, int k, int m, bool bf16, bool adapter, int cus);
 hipError_t launch_few(bool bf16, bool adapter, const FewArgs &a, hipStream_t s);
+// y[row] = sum of the partial sums of its place
+hipError_t launch_join(bool bf16, const FewArgs &a, hipStream_t s);
 enum class ColsKind { kDense, kLowP, kLowQ };
 int cols_parts(bool bf16, ColsKind kind, const ColsArgs &a, int cus);
 hipError_t launch_cols(bool bf16, ColsKind kind, const ColsArgs &a, int cus, hipStream_t s);

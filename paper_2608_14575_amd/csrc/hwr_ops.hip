@@ -203,13 +203,13 @@ hwr_status rows(hwr_ops *c, bool bf16, RowsKind kind, bool ks, RowsArgs r, uint6
 // out[g] = P^T Q, with the partial sums past the first `used` bytes of the work space
 // (the call has reserved them: weight_grad_bytes).
 uint64_t weight_grad_bytes(hwr_ops *c, bool bf16, ColsKind kind, const ColsArgs &w) {
-    const int parts = cols_parts(bf16, kind, w, c->cus);
+    const int parts = cols_plan(bf16, kind, w, c->cus).parts;
     return parts > 1 ? static_cast<uint64_t>(parts) * w.g.G * w.np * w.nq * sizeof(float) : 0;
 }
 hwr_status weight_grad(hwr_ops *c, bool bf16, ColsKind kind, ColsArgs w, uint64_t used) {
     char *ws = nullptr;
     if (hwr_status st = workspace(c, used + weight_grad_bytes(c, bf16, kind, w), &ws)) return st;
-    w.parts = cols_parts(bf16, kind, w, c->cus);
+    w.parts = cols_plan(bf16, kind, w, c->cus).parts;
     w.partial = reinterpret_cast<float *>(ws + used);
     w.zeros = c->zeros;
     OPS_HIP(c, launch_cols(bf16, kind, w, c->cus, c->stream));

@@ -5,6 +5,8 @@
 // Both factors are staged by place, 64 (bf16) or 32 (fp32) places to a stage, and
 // read by columns.  Where the output has few tiles, workgroups share a tile's
 // places and write fp32 partial sums that k_cols_sum adds, in order.
+#include <algorithm>
+
 #include "ops_device.hpp"
 
 namespace hwr {
@@ -226,38 +228,51 @@ __global__ void __launch_bounds__(WP *WQ * 64) k_cols_direct(ColsArgs a) {
         const int u = i * NT + tid, c = (u % QT::kCpl) ^ QT::swz(u / QT::kCpl);
         qb[i] = TT::kLowQ ? t.iq * kLowBytes + c * 16 : min(t.iq * BQ + c * kEpc, a.nq - kEpc) * (int)sizeof(E);
     }
-    // rows (or places) of a stage's lines; -1: zeros.  Tiles of one width share them.
-    constexpr bool kShared = KIND == ColsKind::kDense && BP == BQ;
+    // Rows of a stage's lines, as they stand in the order (checked when they are used:
+    // a check here would wait for the loads in flight).  Tiles of one width share them.
     // Looked up one stage before they are loaded, or four (run_stages_deep), in turn.
+    constexpr bool kShared = KIND == ColsKind::kDense && BP == BQ;
     constexpr int kSlots = kDeep ? 4 : 1, kLead = kDeep ? 4 : 1;
     int pr[kSlots][UP], qr[kSlots][kShared ? 1 : UQ];
     auto look_up = [&](int stage, int slot) {
         const int p = t.p0 + stage * kBk;
+        auto row = [&](int at) {
+            at = min(at, t.p1 - 1);
+            return a.g.order ? a.g.order[at] : at;
+        };
+        if constexpr (!TT::kLowP)
 #pragma unroll
-        for (int i = 0; i < UP; ++i) {
-            const int at = p + i * kLinesP + tid / PT::kCpl;
-            pr[slot][i] = at >= t.p1 ? -1 : TT::kLowP ? at : row_at(a.g, at);
-        }
-        if constexpr (!kShared)
+            for (int i = 0; i < UP; ++i) pr[slot][i] = row(p + i * kLinesP + tid / PT::kCpl);
+        if constexpr (!kShared && !TT::kLowQ)
 #pragma unroll
-            for (int i = 0; i < UQ; ++i) {
-                const int at = p + i * kLinesQ + tid / QT::kCpl;
-                qr[slot][i] = at >= t.p1 ? -1 : TT::kLowQ ? at : row_at(a.g, at);
-            }
+            for (int i = 0; i < UQ; ++i) qr[slot][i] = row(p + i * kLinesQ + tid / QT::kCpl);
     };
     const int64_t pld = TT::kLowP ? a.blocks * kLowBytes : a.ldp * (int64_t)sizeof(E);
     const int64_t qld = TT::kLowQ ? a.blocks * kLowBytes : a.ldq * (int64_t)sizeof(E);
-    const char *zeros = static_cast<const char *>(a.zeros), *ps = static_cast<const char *>(a.p),
-               *qs = static_cast<const char *>(a.q);
+    const char *ps = static_cast<const char *>(a.p), *qs = static_cast<const char *>(a.q);
+    auto in_range = [&](int row) { return min(static_cast<unsigned>(row), static_cast<unsigned>(a.g.n - 1)); };
     auto issue = [&](char *b, int stage, auto... in_turn) {
         constexpr int slot = kDeep ? (decltype(in_turn)::value + ... + 0) : 0;
+        const int p = t.p0 + stage * kBk;
+        auto p_row = [&](int i) -> int64_t { return TT::kLowP ? p + i * kLinesP + tid / PT::kCpl : in_range(pr[slot][i]); };
+        auto q_row = [&](int i) -> int64_t {
+            return TT::kLowQ ? p + i * kLinesQ + tid / QT::kCpl : in_range(kShared ? pr[slot][i] : qr[slot][kShared ? 0 : i]);
+        };
+        auto to_p = [&](int i, const char *src) { load_lds(src, b + (i * NT + wave * 64) * 16); };
+        auto to_q = [&](int i, const char *src) { load_lds(src, b + PT::kBytes + (i * NT + wave * 64) * 16); };
+        if (p + kBk <= t.p1) {
 #pragma unroll
-        for (int i = 0; i < UP; ++i)
-            load_lds(pr[slot][i] < 0 ? zeros : ps + pr[slot][i] * pld + pb[i % BPN], b + (i * NT + wave * 64) * 16);
+            for (int i = 0; i < UP; ++i) to_p(i, ps + p_row(i) * pld + pb[i % BPN]);
 #pragma unroll
-        for (int i = 0; i < UQ; ++i) {
-            const int r = kShared ? pr[slot][i] : qr[slot][kShared ? 0 : i];
-            load_lds(r < 0 ? zeros : qs + r * qld + qb[i % BQN], b + PT::kBytes + (i * NT + wave * 64) * 16);
+            for (int i = 0; i < UQ; ++i) to_q(i, qs + q_row(i) * qld + qb[i % BQN]);
+        } else {                           // lines past the last place are zeros
+            const char *zeros = static_cast<const char *>(a.zeros);
+#pragma unroll
+            for (int i = 0; i < UP; ++i)
+                to_p(i, p + i * kLinesP + tid / PT::kCpl < t.p1 ? ps + p_row(i) * pld + pb[i % BPN] : zeros);
+#pragma unroll
+            for (int i = 0; i < UQ; ++i)
+                to_q(i, p + i * kLinesQ + tid / QT::kCpl < t.p1 ? qs + q_row(i) * qld + qb[i % BQN] : zeros);
         }
         look_up(stage + kLead, (slot + kLead) % kSlots);
     };
@@ -318,43 +333,64 @@ hipError_t go(const ColsArgs &a, hipStream_t s) {
 }
 
 template <class E>
-hipError_t pick(ColsKind kind, const ColsArgs &a, int cus, hipStream_t s) {
+hipError_t pick(ColsKind kind, const ColsPlan &p, const ColsArgs &a, hipStream_t s) {
     constexpr int L = kLowBytes / sizeof(E);
     if (kind == ColsKind::kLowP)
-        return whole_chunks<E, ColsKind::kLowP>(a) ? go<E, ColsKind::kLowP, L, 128, 1, 4, true>(a, s)
-                                                   : go<E, ColsKind::kLowP, L, 128, 1, 4, false>(a, s);
+        return p.direct ? go<E, ColsKind::kLowP, L, 128, 1, 4, true>(a, s) : go<E, ColsKind::kLowP, L, 128, 1, 4, false>(a, s);
     if (kind == ColsKind::kLowQ)
-        return whole_chunks<E, ColsKind::kLowQ>(a) ? go<E, ColsKind::kLowQ, 128, L, 4, 1, true>(a, s)
-                                                   : go<E, ColsKind::kLowQ, 128, L, 4, 1, false>(a, s);
-    const int64_t big = static_cast<int64_t>(a.g.G) * ((a.np + 255) / 256) * ((a.nq + 255) / 256);
-    const int64_t mid = static_cast<int64_t>(a.g.G) * ((a.np + 127) / 128) * ((a.nq + 127) / 128);
-    if (whole_chunks<E, ColsKind::kDense>(a)) {
+        return p.direct ? go<E, ColsKind::kLowQ, 128, L, 4, 1, true>(a, s) : go<E, ColsKind::kLowQ, 128, L, 4, 1, false>(a, s);
+    if (p.direct) {
         if constexpr (sizeof(E) == 2)
-            if (big >= cus) return go<E, ColsKind::kDense, 256, 256, 2, 4, true>(a, s);
-        if (mid >= cus) return go<E, ColsKind::kDense, 128, 128, 2, 2, true>(a, s);
+            if (p.tile == 256) return go<E, ColsKind::kDense, 256, 256, 2, 4, true>(a, s);
+        if (p.tile == 128) return go<E, ColsKind::kDense, 128, 128, 2, 2, true>(a, s);
         return go<E, ColsKind::kDense, 64, 64, 2, 2, true>(a, s);
     }
-    if (mid >= cus) return go<E, ColsKind::kDense, 128, 128, 2, 2, false>(a, s);
+    if (p.tile == 128) return go<E, ColsKind::kDense, 128, 128, 2, 2, false>(a, s);
     return go<E, ColsKind::kDense, 64, 64, 2, 2, false>(a, s);
 }
 
 }  // namespace
 
-// Workgroups that share a tile's places: enough to fill the device, each with at
-// least four stages of an average group.
-int cols_parts(bool bf16, ColsKind kind, const ColsArgs &a, int cus) {
-    const int stage = bf16 ? 64 : 32, tile = kind == ColsKind::kDense ? 64 : 128;
-    const int64_t tp = kind == ColsKind::kLowP ? a.blocks : (a.np + tile - 1) / tile;
-    const int64_t tq = kind == ColsKind::kLowQ ? a.blocks : (a.nq + tile - 1) / tile;
-    const int64_t items = tp * tq * a.g.G, stages = a.g.n / (static_cast<int64_t>(a.g.G) * stage);
-    const int enough = kind == ColsKind::kDense ? cus : 3 * cus;
-    int parts = 1;
-    while (items * parts < enough && parts * 4 < stages) parts *= 2;
-    return parts;
+// The largest tile with which workgroups fill the device, sharing tiles' places if need be:
+// each part has at least 8 stages of an average group (4 with the smallest tile; its
+// partial sums are written and read once, 1.6 ps an element).
+ColsPlan cols_plan(bool bf16, ColsKind kind, const ColsArgs &a, int cus) {
+    ColsPlan p{false, 64, 1};
+    if (bf16)
+        p.direct = kind == ColsKind::kLowP   ? whole_chunks<__bf16, ColsKind::kLowP>(a)
+                   : kind == ColsKind::kLowQ ? whole_chunks<__bf16, ColsKind::kLowQ>(a)
+                                             : whole_chunks<__bf16, ColsKind::kDense>(a);
+    else
+        p.direct = kind == ColsKind::kLowP   ? whole_chunks<float, ColsKind::kLowP>(a)
+                   : kind == ColsKind::kLowQ ? whole_chunks<float, ColsKind::kLowQ>(a)
+                                             : whole_chunks<float, ColsKind::kDense>(a);
+    const int64_t stages = a.g.n / (static_cast<int64_t>(a.g.G) * (bf16 ? 64 : 32));
+    // parts that bring `items` workgroups to `enough`
+    auto parts = [](int64_t items, int64_t enough) {
+        int64_t n = 1;
+        while (items * n < enough) n *= 2;
+        return n;
+    };
+    auto tiles = [&](int64_t t) { return a.g.G * ((a.np + t - 1) / t) * ((a.nq + t - 1) / t); };
+    if (kind == ColsKind::kDense) {
+        for (int t = p.direct && bf16 ? 256 : 128; t >= 64; t /= 2) {
+            const int64_t n = parts(tiles(t), cus);
+            if (t > 64 && (a.np < t || a.nq < t || n > std::max<int64_t>(1, stages / 8))) continue;
+            p.tile = t;
+            p.parts = static_cast<int>(std::min<int64_t>(n, std::max<int64_t>(1, stages / 4)));
+            break;
+        }
+        return p;
+    }
+    const int64_t wide = kind == ColsKind::kLowP ? a.nq : a.np;
+    const int64_t n = parts(a.blocks * ((wide + 127) / 128) * a.g.G, 3 * cus);
+    p.parts = static_cast<int>(std::min<int64_t>(n, std::max<int64_t>(1, stages / 4)));
+    return p;
 }
 
 hipError_t launch_cols(bool bf16, ColsKind kind, const ColsArgs &a, int cus, hipStream_t s) {
-    return bf16 ? pick<__bf16>(kind, a, cus, s) : pick<float>(kind, a, cus, s);
+    const ColsPlan p = cols_plan(bf16, kind, a, cus);
+    return bf16 ? pick<__bf16>(kind, p, a, s) : pick<float>(kind, p, a, s);
 }
 
 }  // namespace hwr

@@ -107,7 +107,12 @@ hipError_t launch_few(bool bf16, bool adapter, const FewArgs &a, hipStream_t s);
 // y[row] = sum of the partial sums of its place
 hipError_t launch_join(bool bf16, const FewArgs &a, hipStream_t s);
 enum class ColsKind { kDense, kLowP, kLowQ };
-int cols_parts(bool bf16, ColsKind kind, const ColsArgs &a, int cus);
+// Tile, and parts of the places, for a weight gradient.
+struct ColsPlan {
+    bool direct;                  // whole chunks: straight into LDS
+    int tile, parts;
+};
+ColsPlan cols_plan(bool bf16, ColsKind kind, const ColsArgs &a, int cus);
 hipError_t launch_cols(bool bf16, ColsKind kind, const ColsArgs &a, int cus, hipStream_t s);
 
 }  // namespace hwr

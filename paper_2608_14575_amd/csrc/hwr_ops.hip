@@ -2,7 +2,6 @@
 // space and launches.
 #include <hip/hip_runtime.h>
 
-#include <algorithm>
 #include <cstring>
 #include <string>
 #include <vector>
@@ -159,10 +158,68 @@ hwr_status shrink(hwr_ops *c, const hwr_groups *g, int32_t dtype, bool ks, const
     return HWR_OK;
 }
 
-// A product by row, with its partial sums past the first `used` bytes of the work
-// space (the call has reserved them: rows_bytes).
-RowsArgs rows_args(hwr_ops *c, const hwr_groups *g, const void *x, int64_t ldx, int k, const void *w, int64_t w_stride, int m,
-                   void *y, int64_t ldy) {
+// ---------------------------------------------------------------- odd widths
+// Matrices of a call whose rows are not whole, aligned chunks, and their padded
+// copies in the work space.
+class Pads {
+  public:
+    explicit Pads(bool bf16) : bf16_(bf16) { args_.count = 0; }
+    // The matrix at *src ([rows][width], rows *ld elements apart), if it needs a copy.  One
+    // that this call does not use counts all the same: what an output is made of, and so its
+    // bits, does not depend on which others are asked for.
+    void add(const void **src, int64_t *ld, int64_t rows, int width, bool used = true) {
+        const int64_t chunk = padded_width(bf16_, 1);
+        if ((reinterpret_cast<uintptr_t>(*src) & 15) == 0 && *ld % chunk == 0 && width % chunk == 0) return;
+        const PadArgs::Matrix m{*src, nullptr, rows, *ld, width};
+        all_ += size(m);
+        if (!used) return;
+        slots_[args_.count] = {src, ld};
+        args_.m[args_.count++] = m;
+    }
+    // Where copies are worth their time for products of so many operations: makes them
+    // past the first *used bytes of the work space (and counts them in), leaves their
+    // addresses and row strides where the matrices' were, and sets *padded.  A copy is a
+    // pass over the matrix (3.5 TB/s, 3 us to launch); without it operands pass through
+    // registers, which takes about twice the time of the products at their ordinary rate.
+    hwr_status copy(hwr_ops *c, double flops, uint64_t *used, bool *padded) {
+        *padded = all_ > 0 && all_ / 1.75e12 + 3e-6 < flops / (bf16_ ? 6e14 : 8e13);
+        if (!*padded || args_.count == 0) return HWR_OK;
+        char *at = nullptr;
+        if (hwr_status st = workspace(c, *used + bytes(), &at)) return st;
+        at += *used;
+        *used += bytes();
+        for (int i = 0; i < args_.count; ++i) {
+            args_.m[i].dst = at;
+            *slots_[i].src = at;
+            *slots_[i].ld = padded_width(bf16_, args_.m[i].width);
+            at += size(args_.m[i]);
+        }
+        OPS_HIP(c, launch_pad(bf16_, args_, c->stream));
+        return HWR_OK;
+    }
+
+  private:
+    struct Slot {
+        const void **src;
+        int64_t *ld;
+    };
+    uint64_t bytes() const {
+        uint64_t b = 0;
+        for (int i = 0; i < args_.count; ++i) b += size(args_.m[i]);
+        return b;
+    }
+    uint64_t size(const PadArgs::Matrix &m) const {
+        return (static_cast<uint64_t>(m.rows) * padded_width(bf16_, m.width) * (bf16_ ? 2 : 4) + 255) / 256 * 256;
+    }
+    bool bf16_;
+    uint64_t all_ = 0;
+    PadArgs args_;
+    Slot slots_[kMaxPads];
+};
+
+// A product by row: w has `lines` rows of `ldw` elements a group, or one group for all rows (shared).
+RowsArgs rows_args(hwr_ops *c, const hwr_groups *g, bool ks, bool padded, const void *x, int64_t ldx, int k, const void *w,
+                   int64_t ldw, int lines, bool shared, int m, void *y, int64_t ldy) {
     RowsArgs r{};
     r.g = groups_arg(g);
     r.k = k;
@@ -170,7 +227,10 @@ RowsArgs rows_args(hwr_ops *c, const hwr_groups *g, const void *x, int64_t ldx, 
     r.x = x;
     r.ldx = ldx;
     r.w = w;
-    r.w_stride = w_stride;
+    r.w_stride = shared ? 0 : lines * ldw;
+    r.ldw = static_cast<int>(ldw);
+    r.mw = ks ? r.ldw : m;
+    r.padded = padded;
     r.y = y;
     r.ldy = ldy;
     r.zeros = c->zeros;
@@ -181,6 +241,8 @@ uint64_t rows_bytes(hwr_ops *c, bool bf16, RowsKind kind, bool ks, const RowsArg
     const int parts = rows_plan(bf16, kind, ks, r, c->cus).parts;
     return parts > 1 ? static_cast<uint64_t>(parts) * r.g.n * r.m_pad * sizeof(float) : 0;
 }
+// With its partial sums past the first `used` bytes of the work space.  (A block that has
+// to be larger leaves the one before as it is, so what lies there stays.)
 hwr_status rows(hwr_ops *c, bool bf16, RowsKind kind, bool ks, RowsArgs r, uint64_t used) {
     char *ws = nullptr;
     if (hwr_status st = workspace(c, used + rows_bytes(c, bf16, kind, ks, r), &ws)) return st;
@@ -200,8 +262,7 @@ hwr_status rows(hwr_ops *c, bool bf16, RowsKind kind, bool ks, RowsArgs r, uint6
     return HWR_OK;
 }
 
-// out[g] = P^T Q, with the partial sums past the first `used` bytes of the work space
-// (the call has reserved them: weight_grad_bytes).
+// out[g] = P^T Q, with the partial sums past the first `used` bytes of the work space.
 uint64_t weight_grad_bytes(hwr_ops *c, bool bf16, ColsKind kind, const ColsArgs &w) {
     const int parts = cols_plan(bf16, kind, w, c->cus).parts;
     return parts > 1 ? static_cast<uint64_t>(parts) * w.g.G * w.np * w.nq * sizeof(float) : 0;
@@ -278,9 +339,17 @@ hwr_status grouped_matmul(hwr_ops *c, const hwr_groups *g, const hwr_matmul_args
         f.ldy = dense(a->ldy, a->m);
         return few(c, f, a->dtype == HWR_BF16, false);
     }
-    const RowsArgs r = rows_args(c, g, a->x, dense(a->ldx, a->k), a->k, a->w, static_cast<int64_t>(a->k) * a->m, a->m, a->y,
-                                 dense(a->ldy, a->m));
-    return rows(c, a->dtype == HWR_BF16, RowsKind::kGrouped, true, r, 0);
+    const bool bf16 = a->dtype == HWR_BF16;
+    const void *x = a->x, *w = a->w;
+    int64_t ldx = dense(a->ldx, a->k), ldw = a->m;
+    uint64_t used = 0;
+    bool padded = false;
+    Pads pads(bf16);
+    pads.add(&x, &ldx, g->n, a->k);
+    pads.add(&w, &ldw, static_cast<int64_t>(g->n_groups) * a->k, a->m);
+    if (hwr_status st = pads.copy(c, 2.0 * g->n * a->k * a->m, &used, &padded)) return st;
+    return rows(c, bf16, RowsKind::kGrouped, true,
+                rows_args(c, g, true, padded, x, ldx, a->k, w, ldw, a->k, false, a->m, a->y, dense(a->ldy, a->m)), used);
 }
 
 hwr_status grouped_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_matmul_grad_args *a) {
@@ -295,22 +364,32 @@ hwr_status grouped_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_matmul
     if (misaligned(a->dtype, {a->dy, a->x, a->w, a->dx, a->dw})) return invalid(c, "a pointer is not aligned to its elements");
     if (hwr_status st = use_device(c)) return st;
     const bool bf16 = a->dtype == HWR_BF16;
+    const void *dy = a->dy, *x = a->x, *w = a->w;
+    int64_t lddy = dense(a->lddy, a->m), ldx = dense(a->ldx, a->k), ldw = a->m;
+    uint64_t used = 0;
+    bool padded = false;
+    Pads pads(bf16);
+    pads.add(&dy, &lddy, g->n, a->m);
+    pads.add(&w, &ldw, static_cast<int64_t>(g->n_groups) * a->k, a->m, a->dx != nullptr);
+    pads.add(&x, &ldx, g->n, a->k, a->dw != nullptr);
+    if (hwr_status st = pads.copy(c, 4.0 * g->n * a->k * a->m, &used, &padded)) return st;
     if (a->dx && g->n > 0) {
-        const RowsArgs r = rows_args(c, g, a->dy, dense(a->lddy, a->m), a->m, a->w, static_cast<int64_t>(a->k) * a->m, a->k,
-                                     a->dx, dense(a->lddx, a->k));
-        if (hwr_status st = rows(c, bf16, RowsKind::kGrouped, false, r, 0)) return st;
+        const RowsArgs r =
+            rows_args(c, g, false, padded, dy, lddy, a->m, w, ldw, a->k, false, a->k, a->dx, dense(a->lddx, a->k));
+        if (hwr_status st = rows(c, bf16, RowsKind::kGrouped, false, r, used)) return st;
     }
     if (a->dw) {
-        ColsArgs w{};
-        w.g = groups_arg(g);
-        w.np = a->k;
-        w.nq = a->m;
-        w.p = a->x;
-        w.q = a->dy;
-        w.ldp = dense(a->ldx, a->k);
-        w.ldq = dense(a->lddy, a->m);
-        w.out = a->dw;
-        if (hwr_status st = weight_grad(c, bf16, ColsKind::kDense, w, 0)) return st;
+        ColsArgs d{};
+        d.g = groups_arg(g);
+        d.np = a->k;
+        d.nq = a->m;
+        d.padded = padded;
+        d.p = x;
+        d.q = dy;
+        d.ldp = ldx;
+        d.ldq = lddy;
+        d.out = a->dw;
+        if (hwr_status st = weight_grad(c, bf16, ColsKind::kDense, d, used)) return st;
     }
     return HWR_OK;
 }
@@ -345,15 +424,22 @@ hwr_status adapter_matmul(hwr_ops *c, const hwr_groups *g, const hwr_adapter_arg
         return few(c, f, a->dtype == HWR_BF16, true);
     }
     const bool bf16 = a->dtype == HWR_BF16;
-    RowsArgs r = rows_args(c, g, a->x, ldx, a->k, a->w, 0, a->m, a->y, dense(a->ldy, a->m));
+    uint64_t used = low_bytes(g->n, a->rank);
+    char *low = nullptr;
+    if (hwr_status st = workspace(c, used, &low)) return st;
+    if (hwr_status st = shrink(c, g, a->dtype, true, a->x, ldx, a->k, a->a, a->rank, a->scale, low)) return st;
+    const void *x = a->x, *w = a->w;
+    int64_t ldxp = ldx, ldw = a->m;
+    bool padded = false;
+    Pads pads(bf16);
+    pads.add(&x, &ldxp, g->n, a->k);
+    pads.add(&w, &ldw, a->k, a->m);
+    if (hwr_status st = pads.copy(c, 2.0 * g->n * a->k * a->m, &used, &padded)) return st;
+    RowsArgs r = rows_args(c, g, true, padded, x, ldxp, a->k, w, ldw, a->k, true, a->m, a->y, dense(a->ldy, a->m));
+    r.low = low;
     r.lw = a->b;
     r.rank = a->rank;
-    const uint64_t each = low_bytes(g->n, a->rank);
-    char *low = nullptr;
-    if (hwr_status st = workspace(c, each + rows_bytes(c, bf16, RowsKind::kAdapter, true, r), &low)) return st;
-    if (hwr_status st = shrink(c, g, a->dtype, true, a->x, ldx, a->k, a->a, a->rank, a->scale, low)) return st;
-    r.low = low;
-    return rows(c, bf16, RowsKind::kAdapter, true, r, each);
+    return rows(c, bf16, RowsKind::kAdapter, true, r, used);
 }
 
 hwr_status adapter_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_adapter_grad_args *a) {
@@ -373,43 +459,50 @@ hwr_status adapter_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_adapte
     const bool bf16 = a->dtype == HWR_BF16;
     const int64_t lddy = dense(a->lddy, a->m), ldx = dense(a->ldx, a->k);
     const uint64_t each = low_bytes(g->n, a->rank);
-    ColsArgs wa{}, wb{};
-    wa.g = wb.g = groups_arg(g);
-    wa.blocks = wb.blocks = rank_blocks(a->rank);
-    wa.np = a->k;
-    wa.nq = a->rank;
-    wa.p = a->x;
-    wa.ldp = ldx;
-    wa.out = a->da;
-    wb.np = a->rank;
-    wb.nq = a->m;
-    wb.q = a->dy;
-    wb.ldq = lddy;
-    wb.out = a->db;
-    RowsArgs r = rows_args(c, g, a->dy, lddy, a->m, a->w, 0, a->k, a->dx, dense(a->lddx, a->k));
-    r.lw = a->a;
-    r.rank = a->rank;
-    const uint64_t parts = std::max({a->da ? weight_grad_bytes(c, bf16, ColsKind::kLowQ, wa) : 0,
-                                     a->db ? weight_grad_bytes(c, bf16, ColsKind::kLowP, wb) : 0,
-                                     a->dx ? rows_bytes(c, bf16, RowsKind::kAdapter, false, r) : 0});
-    char *ws = nullptr;
-    if (hwr_status st = workspace(c, 2 * each + parts, &ws)) return st;
-    char *up = ws, *low = ws + each;
+    uint64_t used = 2 * each;
+    char *up = nullptr;
+    if (hwr_status st = workspace(c, used, &up)) return st;
+    char *low = up + each;
     if (g->n > 0 && (a->dx || a->da))
         if (hwr_status st = shrink(c, g, a->dtype, false, a->dy, lddy, a->m, a->b, a->rank, a->scale, up)) return st;
     if (g->n > 0 && a->db)
         if (hwr_status st = shrink(c, g, a->dtype, true, a->x, ldx, a->k, a->a, a->rank, a->scale, low)) return st;
+    const void *dy = a->dy, *x = a->x, *w = a->w;
+    int64_t lddyp = lddy, ldxp = ldx, ldw = a->m;
+    bool padded = false;
+    Pads pads(bf16);
+    pads.add(&dy, &lddyp, g->n, a->m, a->dx || a->db);
+    pads.add(&w, &ldw, a->k, a->m, a->dx != nullptr);
+    pads.add(&x, &ldxp, g->n, a->k, a->da != nullptr);
+    if (hwr_status st = pads.copy(c, 2.0 * g->n * a->k * a->m, &used, &padded)) return st;
     if (g->n > 0 && a->dx) {
+        RowsArgs r = rows_args(c, g, false, padded, dy, lddyp, a->m, w, ldw, a->k, true, a->k, a->dx, dense(a->lddx, a->k));
         r.low = up;
-        if (hwr_status st = rows(c, bf16, RowsKind::kAdapter, false, r, 2 * each)) return st;
+        r.lw = a->a;
+        r.rank = a->rank;
+        if (hwr_status st = rows(c, bf16, RowsKind::kAdapter, false, r, used)) return st;
     }
+    ColsArgs d{};
+    d.g = groups_arg(g);
+    d.padded = padded;
+    d.blocks = rank_blocks(a->rank);
     if (a->da) {
-        wa.q = up;
-        if (hwr_status st = weight_grad(c, bf16, ColsKind::kLowQ, wa, 2 * each)) return st;
+        d.np = a->k;
+        d.nq = a->rank;
+        d.p = x;
+        d.ldp = ldxp;
+        d.q = up;
+        d.out = a->da;
+        if (hwr_status st = weight_grad(c, bf16, ColsKind::kLowQ, d, used)) return st;
     }
     if (a->db) {
-        wb.p = low;
-        if (hwr_status st = weight_grad(c, bf16, ColsKind::kLowP, wb, 2 * each)) return st;
+        d.np = a->rank;
+        d.nq = a->m;
+        d.p = low;
+        d.q = dy;
+        d.ldq = lddyp;
+        d.out = a->db;
+        if (hwr_status st = weight_grad(c, bf16, ColsKind::kLowP, d, used)) return st;
     }
     return HWR_OK;
 }

@@ -221,12 +221,12 @@ __global__ void __launch_bounds__(WP *WQ * 64) k_cols_direct(ColsArgs a) {
 #pragma unroll
     for (int i = 0; i < BPN; ++i) {
         const int u = i * NT + tid, c = (u % PT::kCpl) ^ PT::swz(u / PT::kCpl);
-        pb[i] = TT::kLowP ? t.ip * kLowBytes + c * 16 : min(t.ip * BP + c * kEpc, a.np - kEpc) * (int)sizeof(E);
+        pb[i] = TT::kLowP ? t.ip * kLowBytes + c * 16 : min(t.ip * BP + c * kEpc, (a.np - 1) / kEpc * kEpc) * (int)sizeof(E);
     }
 #pragma unroll
     for (int i = 0; i < BQN; ++i) {
         const int u = i * NT + tid, c = (u % QT::kCpl) ^ QT::swz(u / QT::kCpl);
-        qb[i] = TT::kLowQ ? t.iq * kLowBytes + c * 16 : min(t.iq * BQ + c * kEpc, a.nq - kEpc) * (int)sizeof(E);
+        qb[i] = TT::kLowQ ? t.iq * kLowBytes + c * 16 : min(t.iq * BQ + c * kEpc, (a.nq - 1) / kEpc * kEpc) * (int)sizeof(E);
     }
     // Rows of a stage's lines, as they stand in the order (checked when they are used:
     // a check here would wait for the loads in flight).  Tiles of one width share them.
@@ -310,8 +310,8 @@ __global__ void __launch_bounds__(256) k_cols_sum(ColsArgs a, int64_t count) {
 template <class E, ColsKind KIND>
 bool whole_chunks(const ColsArgs &a) {
     constexpr int kEpc = Elem<E>::kEpc;
-    auto whole = [](const void *p, int64_t ld, int width) {
-        return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % kEpc == 0 && width % kEpc == 0;
+    auto whole = [&](const void *p, int64_t ld, int width) {
+        return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % kEpc == 0 && (a.padded || width % kEpc == 0);
     };
     return (KIND == ColsKind::kLowP || whole(a.p, a.ldp, a.np)) && (KIND == ColsKind::kLowQ || whole(a.q, a.ldq, a.nq));
 }

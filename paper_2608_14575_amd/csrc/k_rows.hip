@@ -168,7 +168,7 @@ __device__ inline bool my_tile(const RowsArgs &a, int lane, RowTile &rt, int &c0
     const int t = panel + in % rp;
     // the last tile of columns ends with the row: it shares columns with the one before
     // (both give them the same bits), and no chunk is cut
-    c0 = a.m < BN ? 0 : min(in / rp * BN, a.m - BN);
+    c0 = a.mw < BN ? 0 : min(in / rp * BN, a.mw - BN);
     if (KIND == RowsKind::kAdapter) rt = {0, t * BM, min(t * BM + BM, a.g.n)};
     else rt = find_tile(a.g, t, BM, tail, lane);
     return true;
@@ -207,10 +207,10 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows(RowsArgs a) {
     auto weights = [&](const E *base, int k0, int klen) {   // KS: lines are elements; else columns
         return [=, &a](int line, int c) {
             if constexpr (KS) {
-                return load_chunk<E>(k0 + line < klen ? base + static_cast<int64_t>(k0 + line) * a.m : nullptr,
+                return load_chunk<E>(k0 + line < klen ? base + static_cast<int64_t>(k0 + line) * a.ldw : nullptr,
                                      c0 + c * El::kEpc, a.m);
             } else {
-                return load_chunk<E>(c0 + line < a.m ? base + static_cast<int64_t>(c0 + line) * klen : nullptr,
+                return load_chunk<E>(c0 + line < a.m ? base + static_cast<int64_t>(c0 + line) * a.ldw : nullptr,
                                      k0 + c * El::kEpc, klen);
             }
         };
@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows(RowsArgs a) {
     store_rows<E, BM, BN, WR, WC>(a, rt, c0, part, rows, acc, tid);
 }
 
-// Whole chunks of 16 bytes everywhere and at least BN columns: operands go from
+// Whole chunks of 16 bytes everywhere (rows padded to them with zeros) and at least BN columns: operands go from
 // memory straight into LDS (run_stages).  A place without a row computes one that it
 // does not store; contraction elements past the last are zeros on both sides.
 template <class E, RowsKind KIND, bool KS, int BM, int BN, int WR, int WC>
@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows_direct(RowsArgs a) {
         xp[i] = reinterpret_cast<const char *>(static_cast<const E *>(a.x) + (r < 0 ? 0 : r) * a.ldx + xe + first * kBk);
     }
     const E *w = static_cast<const E *>(a.w) + (KIND == RowsKind::kAdapter || k == 0 ? 0 : rt.g) * a.w_stride;
-    const int wline = tid / WT::kCpl, ldw = KS ? a.m : a.k;
+    const int wline = tid / WT::kCpl, ldw = a.ldw;
     auto chunk = [&](int i) { return ((tid % WT::kCpl) ^ WT::swz(i * kLinesW + wline)) * kEpc; };
     const int we = KS ? wline : chunk(0);
     const char *wp = reinterpret_cast<const char *>(KS ? w + static_cast<int64_t>(wline) * ldw + c0
@@ -309,7 +309,7 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows_direct(RowsArgs a) {
         const char *at = wp + static_cast<int64_t>(i) * kLinesW * ldw * sizeof(E);
         return kOneOrder ? at : at + chunk(i) * sizeof(E);
     };
-    const int64_t wstep = KS ? static_cast<int64_t>(kBk) * a.m * sizeof(E) : kStageBytes;
+    const int64_t wstep = KS ? static_cast<int64_t>(kBk) * ldw * sizeof(E) : kStageBytes;
     wp += first * wstep;
     auto issue = [&](char *b, int stage, auto...) {
         const int k0 = (first + stage) * kBk;
@@ -385,7 +385,8 @@ hipError_t pick_kind(RowsKind kind, bool ks, const RowsPlan &p, const RowsArgs &
 bool whole_chunks(bool bf16, bool ks, const RowsArgs &a) {
     const int epc = bf16 ? 8 : 4;
     const auto ptrs = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w);
-    return (ptrs & 15) == 0 && a.ldx % epc == 0 && a.k % epc == 0 && (!ks || a.m % epc == 0);
+    return (ptrs & 15) == 0 && a.ldx % epc == 0 && a.ldw % epc == 0 && a.w_stride % epc == 0 && (a.padded || a.k % epc == 0) &&
+           (!ks || a.mw % epc == 0);
 }
 
 }  // namespace
@@ -396,9 +397,9 @@ RowsPlan rows_plan(bool bf16, RowsKind kind, bool ks, const RowsArgs &a, int cus
     auto tiles = [&](int64_t bm, int64_t bn) {
         return (a.g.n / bm + (kind == RowsKind::kAdapter ? 1 : a.g.G)) * ((a.m + bn - 1) / bn);
     };
-    RowsPlan p{whole_chunks(bf16, ks, a) && a.m >= 64, 64, 64, 1};
-    if (p.direct && bf16 && a.m >= 256 && tiles(256, 256) >= cus) p.bm = p.bn = 256;
-    else if ((!p.direct || a.m >= 128) && tiles(128, 128) >= cus) p.bm = p.bn = 128;
+    RowsPlan p{whole_chunks(bf16, ks, a) && a.mw >= 64, 64, 64, 1};
+    if (p.direct && bf16 && a.mw >= 256 && tiles(256, 256) >= cus) p.bm = p.bn = 256;
+    else if ((!p.direct || a.mw >= 128) && tiles(128, 128) >= cus) p.bm = p.bn = 128;
     else if (p.direct && !bf16 && tiles(64, 64) < 2 * cus) p.bm = 32;
     const int stages = (a.k + (bf16 ? 63 : 31)) / (bf16 ? 64 : 32);
     while (tiles(p.bm, p.bn) * p.parts < cus && stages >= 8 * p.parts) p.parts *= 2;

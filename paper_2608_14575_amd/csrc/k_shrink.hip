@@ -17,30 +17,27 @@ constexpr int kWaves = 8;
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), may_alias));
 
 // How the weights come into operand form.  kDirect: [rank][k], 16 bytes of a lane are
-// its operand.  kTurned: [k][rank] with whole chunks in a row; a step's rows are one
-// piece of memory, which goes through a part of LDS that is the wave's own and is
-// read by columns.  kAny: [k][rank] of any rank and alignment, transposed in
-// registers (fragment j then holds the columns m V + j).
-enum class From { kDirect, kTurned, kAny };
+// its operand.  Else [k][rank]: a step's rows are one piece of memory, which goes
+// through a part of LDS that is the wave's own and is read by columns: kTurned with
+// the transposing read (bf16, ranks that are multiples of 4), kPicked by single elements.
+enum class From { kDirect, kTurned, kPicked };
 
-// NF column fragments (kAny: V, one pass over the columns for each 16 V), RB row fragments.
+// NF column fragments, RB row fragments.
 template <class E, From FROM, int NF, int RB>
-__global__ void __launch_bounds__(kWaves * 64, 4) k_shrink(ShrinkArgs a) {
+__global__ void __launch_bounds__(kWaves * 64, NF == 8 || (FROM == From::kPicked && NF * RB == 8) ? 2 : 4) k_shrink(ShrinkArgs a) {
     using El = Elem<E>;
     constexpr int V = El::kEpc, BM = 16 * RB, kStep = 4 * V, kCols = 16 * NF;
-    constexpr int kAcc = RB * NF, kDeep = NF <= 2 ? 4 : FROM == From::kAny ? 1 : 2;
+    constexpr int kAcc = RB * NF, kDeep = NF <= 2 ? 4 : 2;
     // a step's weights for each wave, or half of the waves' sums
-    constexpr int kOwn = FROM == From::kTurned ? kStep * kCols * sizeof(E) : 0, kSums = kAcc * 64 * 16;
+    constexpr int kOwn = FROM != From::kDirect ? kStep * kCols * sizeof(E) : 0, kSums = kAcc * 64 * 16;
     constexpr int kLds = kWaves * kOwn > kWaves / 2 * kSums ? kWaves * kOwn : kWaves / 2 * kSums;
     __shared__ __attribute__((aligned(16))) char lds[kLds];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int m = lane & 15, q = lane >> 4;
-    const int ct = FROM == From::kAny ? (a.rank + kCols - 1) / kCols : 1;
-    const int t = blockIdx.x / ct, c0 = blockIdx.x % ct * kCols;
+    const int t = blockIdx.x;
     if (t >= count_tiles(a.g, BM, false, lane)) return;
     const RowTile rt = find_tile(a.g, t, BM, false, lane);
     const E *w = static_cast<const E *>(a.w) + static_cast<int64_t>(rt.g) * a.k * a.rank;
-    const int cols = min(a.rank - c0, kCols);
 
     // (a place without a row takes row 0; its intermediate is never used)
     const E *x[RB];
@@ -68,13 +65,13 @@ __global__ void __launch_bounds__(kWaves * 64, 4) k_shrink(ShrinkArgs a) {
                 const E *line = w + static_cast<int64_t>(min(i * 16 + m, a.rank - 1)) * a.k;   // past the rank: not used
                 if (whole) lw[i] = *reinterpret_cast<const typename El::Vec *>(line + e);
                 else lw[i] = load_chunk<E>(line, e, a.k);
-            } else if constexpr (FROM == From::kTurned) {
-                const int64_t at = static_cast<int64_t>(step) * kStep * a.rank + (i * 64 + lane) * V;
-                lw[i] = u32x4{0, 0, 0, 0};
-                if ((i * 64 + lane) * V < kStep * a.rank && at < static_cast<int64_t>(a.k) * a.rank)
-                    lw[i] = *reinterpret_cast<const u32x4 *>(w + at);
             } else {
-                lw[i] = load_chunk<E>(e + i < a.k ? w + static_cast<int64_t>(e + i) * a.rank + c0 : nullptr, m * V, cols);
+                const int at = step * kStep * a.rank + (i * 64 + lane) * V, all = a.k * a.rank;
+                lw[i] = u32x4{0, 0, 0, 0};
+                if ((i * 64 + lane) * V < kStep * a.rank) {
+                    if (at + V <= all) lw[i] = *reinterpret_cast<const typename El::Vec *>(w + at);
+                    else lw[i] = load_chunk<E>(w, at, all);
+                }
             }
         }
     };
@@ -82,7 +79,7 @@ __global__ void __launch_bounds__(kWaves * 64, 4) k_shrink(ShrinkArgs a) {
         union Chunk { u32x4 v; typename El::Frag f; E e[V]; } u;
         typename El::Frag fw[NF];
         char *own = lds + wave * kOwn;
-        if constexpr (FROM == From::kTurned) {
+        if constexpr (FROM != From::kDirect) {
 #pragma unroll
             for (int i = 0; i < NF; ++i)
                 if ((i * 64 + lane) * V < kStep * a.rank) *reinterpret_cast<u32x4_any *>(own + (i * 64 + lane) * 16) = lw[i];
@@ -92,10 +89,10 @@ __global__ void __launch_bounds__(kWaves * 64, 4) k_shrink(ShrinkArgs a) {
         for (int j = 0; j < NF; ++j) {
             if constexpr (FROM == From::kDirect) {
                 u.v = lw[j];
-            } else if constexpr (FROM == From::kTurned) {
+            } else {
                 // (columns past the rank take what follows in LDS, and are not used)
                 const int line = a.rank * (int)sizeof(E);
-                if constexpr (sizeof(E) == 2) {
+                if constexpr (FROM == From::kTurned) {
                     typedef __attribute__((address_space(3))) i16x4 lds_v;
                     union { i16x4 h[2]; u32x4 v; } r;
                     const int o = (q * 8 + (m >> 2)) * line + (j * 16 + (m & 3) * 4) * 2;
@@ -105,14 +102,13 @@ __global__ void __launch_bounds__(kWaves * 64, 4) k_shrink(ShrinkArgs a) {
                 } else {
 #pragma unroll
                     for (int i = 0; i < V; ++i)
-                        u.e[i] = *reinterpret_cast<const E *>(own + min((q * V + i) * line + (j * 16 + m) * 4, kOwn - 4));
+                        u.e[i] = *reinterpret_cast<const E *>(own + min((q * V + i) * line + (j * 16 + m) * (int)sizeof(E),
+                                                                        kOwn - (int)sizeof(E)));
                 }
-            } else {
-                u.f = column(lw, j);
             }
             fw[j] = u.f;
         }
-        if constexpr (FROM == From::kTurned) wave_lds();       // before the next step overwrites it
+        if constexpr (FROM != From::kDirect) wave_lds();       // before the next step overwrites it
 #pragma unroll
         for (int i = 0; i < RB; ++i) {
             u.v = lx[i];
@@ -146,8 +142,7 @@ __global__ void __launch_bounds__(kWaves * 64, 4) k_shrink(ShrinkArgs a) {
     }
     if (wave != 0) return;
 
-    // lane: place m of block i; columns 16 j + 4 q + e, kAny: (4 q + e) V + j.  Zeros past the
-    // rank (not 0 x infinity).
+    // lane: place m of block i, columns 16 j + 4 q + e.  Zeros past the rank (not 0 x infinity).
     const float s = a.scale ? a.scale[rt.g] : 1.0f;
     const int blocks = (a.rank + kRankBlock - 1) / kRankBlock;
 #pragma unroll
@@ -155,33 +150,24 @@ __global__ void __launch_bounds__(kWaves * 64, 4) k_shrink(ShrinkArgs a) {
         if (!in_tile[i]) continue;
         char *at = static_cast<char *>(a.low) + static_cast<int64_t>(rt.p0 + i * 16 + m) * blocks * kLowBytes;
         auto put = [&](int c, f32x4 v) {
-            if (c0 + c >= blocks * kRankBlock) return;
+            if (c >= blocks * kRankBlock) return;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = c + e < cols ? v[e] * s : 0.0f;
-            store_low<E>(at + (c0 + c) / kRankBlock * kLowBytes, (c0 + c) % kRankBlock, v);
+            for (int e = 0; e < 4; ++e) v[e] = c + e < a.rank ? v[e] * s : 0.0f;
+            store_low<E>(at + c / kRankBlock * kLowBytes, c % kRankBlock, v);
         };
-        if constexpr (FROM == From::kAny) {
 #pragma unroll
-            for (int j = 0; j < NF; j += 4)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    put((4 * q + e) * V + j, f32x4{acc[i][j][e], acc[i][j + 1][e], acc[i][j + 2][e], acc[i][j + 3][e]});
-        } else {
-#pragma unroll
-            for (int j = 0; j < NF; ++j) put(j * 16 + 4 * q, acc[i][j]);
-            if constexpr (NF == 1) put(16 + 4 * q, f32x4{});       // the block's other half
-        }
+        for (int j = 0; j < NF; ++j) put(j * 16 + 4 * q, acc[i][j]);
+        if constexpr (NF == 1) put(16 + 4 * q, f32x4{});       // the block's other half
     }
 }
 
 template <class E, From FROM, int NF>
 hipError_t go(const ShrinkArgs &a, int cus, hipStream_t s) {
-    const int ct = FROM == From::kAny ? (a.rank + 16 * NF - 1) / (16 * NF) : 1;
     auto tiles = [&](int bm) { return static_cast<uint32_t>(a.g.n / bm + (a.g.n < a.g.G ? a.g.n : a.g.G)); };
     // two blocks of rows share the weights' loads where the device stays full
-    if constexpr (FROM != From::kAny && NF <= 4)
+    if constexpr (NF <= 4)
         if (a.g.n >= 32 * cus) return launch_kernel(k_shrink<E, FROM, NF, 2>, dim3(tiles(32)), dim3(kWaves * 64), 0, s, a);
-    return launch_kernel(k_shrink<E, FROM, NF, 1>, dim3(tiles(16) * ct), dim3(kWaves * 64), 0, s, a);
+    return launch_kernel(k_shrink<E, FROM, NF, 1>, dim3(tiles(16)), dim3(kWaves * 64), 0, s, a);
 }
 
 template <class E, From FROM>
@@ -194,10 +180,10 @@ hipError_t ranks(const ShrinkArgs &a, int cus, hipStream_t s) {
 
 template <class E>
 hipError_t pick(bool ks, const ShrinkArgs &a, int cus, hipStream_t s) {
-    constexpr int V = Elem<E>::kEpc;
     if (!ks) return ranks<E, From::kDirect>(a, cus, s);
-    if (a.rank % V == 0 && (reinterpret_cast<uintptr_t>(a.w) & 15) == 0) return ranks<E, From::kTurned>(a, cus, s);
-    return go<E, From::kAny, V>(a, cus, s);
+    if constexpr (sizeof(E) == 2)
+        if (a.rank % 4 == 0) return ranks<E, From::kTurned>(a, cus, s);
+    return ranks<E, From::kPicked>(a, cus, s);
 }
 
 }  // namespace

@@ -5,6 +5,20 @@
 
 namespace hwr {
 
+// Copies of matrices with rows padded by zeros to whole, aligned chunks of 16 bytes.
+constexpr int kMaxPads = 3;
+struct PadArgs {
+    struct Matrix {
+        const void *src;
+        void *dst;
+        int64_t rows, ld;         // elements
+        int width;
+    } m[kMaxPads];
+    int count;
+};
+int64_t padded_width(bool bf16, int width);   // elements
+hipError_t launch_pad(bool bf16, const PadArgs &a, hipStream_t s);
+
 // Low-rank intermediates (s x A, u) are kept by place, in blocks of kRankBlock
 // columns of 128 bytes: fp32 values, or bf16 pairs hi[kRankBlock], lo[kRankBlock]
 // with hi + lo the value to 16 significant bits.
@@ -25,6 +39,8 @@ struct RowsArgs {
     int64_t ldx;                  // elements
     const void *w;                // KS: [k][m], else [m][k] (transposed use)
     int64_t w_stride;             // elements between groups
+    int ldw, mw;                  // elements between rows of w; columns there are (KS: m, or more that are not used)
+    bool padded;                  // rows of x (and of w, not KS) go on with zeros up to a whole chunk
     void *y;
     int64_t ldy;
     const void *zeros;            // 256 zero bytes
@@ -51,7 +67,8 @@ struct ShrinkArgs {
 // Weight gradients: out[g][p][q] = sum over places of g of P[place][p] Q[place][q].
 struct ColsArgs {
     GroupsArg g;
-    int np, nq;                   // widths of P and Q as they stand in out
+    int np, nq;                   // widths of P and Q as they stand in out (rows may go on to a whole chunk)
+    bool padded;                  // they do
     const void *p, *q;            // rows through order, or low-rank intermediates by place
     int64_t ldp, ldq;             // elements
     void *out;                    // [G][np][nq]

@@ -141,6 +141,15 @@ SHAPES = [
     (2049, 1000, 24, 40, "skew", False, 0),
     (4100, 2, 1024, 512, "skew", False, 0),
     (3000, 3, 96, 96, "even", False, 5),
+    # large enough for copies with whole chunks, for parts of the contraction and of the places, for each tile
+    (4000, 3, 1001, 1003, "skew", False, 0),
+    (4000, 2, 1000, 1003, "skew", False, 1),
+    (4000, 2, 1001, 1000, "skew", True, 0),
+    (300, 1, 1600, 520, "even", False, 0),
+    (300, 2, 1601, 523, "skew", False, 0),
+    (4096, 1, 2048, 1024, "even", False, 0),
+    (9000, 2, 2048, 1032, "skew", False, 0),
+    (700, 9, 640, 40, "skew", False, 0),
 ]
 
 
@@ -186,6 +195,14 @@ ADAPTERS = [
     (1025, 3, 128, 390, 128, "even", True, 0, True),
     (3000, 6, 768, 768, 8, "skew", False, 0, True),
     (2600, 900, 32, 64, 16, "skew", False, 0, True),
+    # narrow ranks over many steps, odd ranks, copies with whole chunks, parts, each tile
+    (300, 3, 1100, 264, 4, "skew", False, 0, True),
+    (300, 2, 1101, 263, 7, "skew", False, 0, True),
+    (500, 3, 1029, 200, 50, "skew", False, 0, True),
+    (500, 3, 640, 1024, 100, "skew", False, 0, True),
+    (4000, 3, 1001, 1003, 16, "skew", False, 0, True),
+    (9000, 4, 1024, 2048, 32, "skew", False, 0, True),
+    (9000, 4, 768, 384, 6, "skew", True, 0, False),
 ]
 
 

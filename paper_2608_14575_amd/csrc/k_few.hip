@@ -243,7 +243,13 @@ hipError_t go(const FewArgs &a, hipStream_t s) {
 
 }  // namespace
 
-bool few_rows(int n, int G, bool adapter) { return adapter ? n <= kFewRows : n <= kFewRows || n <= 16 * G; }
+// Up to where 16-row tiles that read the weights once each beat larger tiles (which
+// take a launch or two more with an adapter).  us, few / larger, 2048 x 2048: adapter bf16
+// 128 rows 22.3 / 25.2, 192 rows 23.7 / 28.6, 256 rows 28.1 / 27.7; fp32 256 rows 37 / 44;
+// grouped (2 groups) bf16 96 rows 14.3 / 13.7, fp32 256 rows 38 / 44, 384 rows 48 / 44.
+bool few_rows(int n, int G, bool adapter, bool bf16) {
+    return n <= (bf16 ? (adapter ? 192 : 64) : 256) || (!adapter && n <= kFewTile * G);
+}
 
 int few_tiles(int n, int G, bool adapter) {
     return adapter ? (n + kFewTile - 1) / kFewTile : n / kFewTile + (n < G + 1 ? n : G + 1);

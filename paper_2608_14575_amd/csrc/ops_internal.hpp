@@ -79,7 +79,7 @@ struct ColsArgs {
 };
 
 // Few rows: y = x w_g, or with an adapter x w + scale[g] (x a_g) b_g, by streaming the weights.
-constexpr int kFewRows = 64, kFewTile = 16;
+constexpr int kFewTile = 16;
 struct FewArgs {
     GroupsArg g;
     int k, m, m_pad, rank;        // m_pad: m up to a multiple of 4
@@ -117,7 +117,7 @@ struct RowsPlan {
 RowsPlan rows_plan(bool bf16, RowsKind kind, bool ks, const RowsArgs &a, int cus);
 hipError_t launch_rows(bool bf16, RowsKind kind, bool ks, const RowsArgs &a, int cus, hipStream_t s);
 hipError_t launch_shrink(bool bf16, bool ks, const ShrinkArgs &a, int cus, hipStream_t s);
-bool few_rows(int n, int G, bool adapter);              // whether launch_few is meant for the batch
+bool few_rows(int n, int G, bool adapter, bool bf16);              // whether launch_few is meant for the batch
 int few_tiles(int n, int G, bool adapter);
 int few_parts(int n, int G, int k, int m, bool bf16, bool adapter, int cus);
 hipError_t launch_few(bool bf16, bool adapter, const FewArgs &a, hipStream_t s);

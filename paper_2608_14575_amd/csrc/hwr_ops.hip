@@ -150,14 +150,6 @@ GroupsArg groups_arg(const hwr_groups *g) { return {g->n, g->n_groups, g->offset
 int rank_blocks(int rank) { return (rank + kRankBlock - 1) / kRankBlock; }
 uint64_t low_bytes(int n, int rank) { return static_cast<uint64_t>(n) * rank_blocks(rank) * kLowBytes; }
 
-// low[place] = scale[g] x[row] w_g
-hwr_status shrink(hwr_ops *c, const hwr_groups *g, int32_t dtype, bool ks, const void *x, int64_t ldx, int k, const void *w,
-                  int rank, const float *scale, void *low) {
-    const ShrinkArgs r{groups_arg(g), k, rank, x, ldx, w, scale, low};
-    OPS_HIP(c, launch_shrink(dtype == HWR_BF16, ks, r, c->cus, c->stream));
-    return HWR_OK;
-}
-
 // ---------------------------------------------------------------- odd widths
 // Matrices of a call whose rows are not whole, aligned chunks, and their padded
 // copies in the work space.
@@ -427,7 +419,8 @@ hwr_status adapter_matmul(hwr_ops *c, const hwr_groups *g, const hwr_adapter_arg
     uint64_t used = low_bytes(g->n, a->rank);
     char *low = nullptr;
     if (hwr_status st = workspace(c, used, &low)) return st;
-    if (hwr_status st = shrink(c, g, a->dtype, true, a->x, ldx, a->k, a->a, a->rank, a->scale, low)) return st;
+    const ShrinkArgs to_low{groups_arg(g), a->k, a->rank, a->x, ldx, a->a, a->scale, low};
+    OPS_HIP(c, launch_shrink(bf16, true, to_low, c->cus, c->stream));
     const void *x = a->x, *w = a->w;
     int64_t ldxp = ldx, ldw = a->m;
     bool padded = false;
@@ -463,10 +456,13 @@ hwr_status adapter_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_adapte
     char *up = nullptr;
     if (hwr_status st = workspace(c, used, &up)) return st;
     char *low = up + each;
-    if (g->n > 0 && (a->dx || a->da))
-        if (hwr_status st = shrink(c, g, a->dtype, false, a->dy, lddy, a->m, a->b, a->rank, a->scale, up)) return st;
-    if (g->n > 0 && a->db)
-        if (hwr_status st = shrink(c, g, a->dtype, true, a->x, ldx, a->k, a->a, a->rank, a->scale, low)) return st;
+    const ShrinkArgs to_up{groups_arg(g), a->m, a->rank, a->dy, lddy, a->b, a->scale, up};
+    const ShrinkArgs to_low{groups_arg(g), a->k, a->rank, a->x, ldx, a->a, a->scale, low};
+    if (g->n > 0) {
+        if ((a->dx || a->da) && a->db) OPS_HIP(c, launch_shrink_pair(bf16, to_up, to_low, c->cus, c->stream));
+        else if (a->dx || a->da) OPS_HIP(c, launch_shrink(bf16, false, to_up, c->cus, c->stream));
+        else if (a->db) OPS_HIP(c, launch_shrink(bf16, true, to_low, c->cus, c->stream));
+    }
     const void *dy = a->dy, *x = a->x, *w = a->w;
     int64_t lddyp = lddy, ldxp = ldx, ldw = a->m;
     bool padded = false;
@@ -482,28 +478,38 @@ hwr_status adapter_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_adapte
         r.rank = a->rank;
         if (hwr_status st = rows(c, bf16, RowsKind::kAdapter, false, r, used)) return st;
     }
-    ColsArgs d{};
-    d.g = groups_arg(g);
-    d.padded = padded;
-    d.blocks = rank_blocks(a->rank);
-    if (a->da) {
-        d.np = a->k;
-        d.nq = a->rank;
-        d.p = x;
-        d.ldp = ldxp;
-        d.q = up;
-        d.out = a->da;
-        if (hwr_status st = weight_grad(c, bf16, ColsKind::kLowQ, d, used)) return st;
+    ColsArgs da{}, db{};
+    da.g = db.g = groups_arg(g);
+    da.padded = db.padded = padded;
+    da.blocks = db.blocks = rank_blocks(a->rank);
+    da.np = a->k;
+    da.nq = a->rank;
+    da.p = x;
+    da.ldp = ldxp;
+    da.q = up;
+    da.out = a->da;
+    db.np = a->rank;
+    db.nq = a->m;
+    db.p = low;
+    db.q = dy;
+    db.ldq = lddyp;
+    db.out = a->db;
+    if (a->da && a->db && cols_plan(bf16, ColsKind::kLowQ, da, c->cus).direct && cols_plan(bf16, ColsKind::kLowP, db, c->cus).direct) {
+        const uint64_t first = weight_grad_bytes(c, bf16, ColsKind::kLowQ, da);
+        char *ws = nullptr;
+        if (hwr_status st = workspace(c, used + first + weight_grad_bytes(c, bf16, ColsKind::kLowP, db), &ws)) return st;
+        da.parts = cols_plan(bf16, ColsKind::kLowQ, da, c->cus).parts;
+        db.parts = cols_plan(bf16, ColsKind::kLowP, db, c->cus).parts;
+        da.partial = reinterpret_cast<float *>(ws + used);
+        db.partial = reinterpret_cast<float *>(ws + used + first);
+        da.zeros = db.zeros = c->zeros;
+        OPS_HIP(c, launch_cols_low_pair(bf16, da, db, c->stream));
+        return HWR_OK;
     }
-    if (a->db) {
-        d.np = a->rank;
-        d.nq = a->m;
-        d.p = low;
-        d.q = dy;
-        d.ldq = lddyp;
-        d.out = a->db;
-        if (hwr_status st = weight_grad(c, bf16, ColsKind::kLowP, d, used)) return st;
-    }
+    if (a->da)
+        if (hwr_status st = weight_grad(c, bf16, ColsKind::kLowQ, da, used)) return st;
+    if (a->db)
+        if (hwr_status st = weight_grad(c, bf16, ColsKind::kLowP, db, used)) return st;
     return HWR_OK;
 }
 

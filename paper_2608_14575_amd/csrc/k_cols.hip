@@ -36,11 +36,11 @@ __device__ inline int largest_group(const GroupsArg &g, int turn) {
 __host__ __device__ inline int cols_shares(int64_t per) { return per < 32 ? 1 : per < 128 ? static_cast<int>(per / 16) : 8; }
 
 template <ColsKind KIND, int BP, int BQ, int kBk>
-__device__ inline bool my_tile(const ColsArgs &a, ColsTile &t) {
+__device__ inline bool my_tile(const ColsArgs &a, int block, ColsTile &t) {
     const int tp = KIND == ColsKind::kLowP ? a.blocks : (a.np + BP - 1) / BP;
     const int tq = KIND == ColsKind::kLowQ ? a.blocks : (a.nq + BQ - 1) / BQ;
     const int per = tp * tq * a.parts, shares = cols_shares(per), share = (per + shares - 1) / shares;
-    const int at = blockIdx.x >> 3, turn = at / share * 8 + (blockIdx.x & 7);
+    const int at = block >> 3, turn = at / share * 8 + (block & 7);
     const int in_group = turn % shares * share + at % share;
     if (turn >= a.g.G * shares || in_group >= per) return false;
     t.g = largest_group(a.g, turn / shares);
@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(WP *WQ * 64) k_cols(ColsArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wp = wave / WQ, wq = wave % WQ;
     ColsTile t;
-    if (!my_tile<KIND, BP, BQ, kBk>(a, t)) return;
+    if (!my_tile<KIND, BP, BQ, kBk>(a, blockIdx.x, t)) return;
 
     f32x4 acc[PF][QF] = {};
     constexpr int UP = PT::kChunks / NT, UQ = QT::kChunks / NT;
@@ -193,8 +193,11 @@ __global__ void __launch_bounds__(WP *WQ * 64) k_cols(ColsArgs a) {
 // Whole chunks of 16 bytes everywhere: operands go from memory straight into LDS
 // (run_stages); a stage's rows are looked up when the stage before it is loaded.  Places past the last are zeros on both sides; columns
 // past the last are loaded from a valid place and not stored.
+template <class E, ColsKind KIND, int BP, int BQ>
+constexpr int kColsBuf = ColsTiles<E, KIND, BP, BQ>::PT::kBytes + ColsTiles<E, KIND, BP, BQ>::QT::kBytes;
+
 template <class E, ColsKind KIND, int BP, int BQ, int WP, int WQ>
-__global__ void __launch_bounds__(WP *WQ * 64) k_cols_direct(ColsArgs a) {
+__device__ inline void cols_direct(const ColsArgs &a, int block, char *buf0, char *buf1, char *buf2, char *buf3) {
     using El = Elem<E>;
     using TT = ColsTiles<E, KIND, BP, BQ>;
     using PT = typename TT::PT;
@@ -203,16 +206,11 @@ __global__ void __launch_bounds__(WP *WQ * 64) k_cols_direct(ColsArgs a) {
     constexpr int NT = WP * WQ * 64, PF = BP / WP / 16, QF = BQ / WQ / 16, kBk = El::kBk, kEpc = El::kEpc;
     constexpr int UP = PT::kChunks / NT, UQ = QT::kChunks / NT;
     static_assert(PT::kChunks % NT == 0 && QT::kChunks % NT == 0);
-    // an array each, so that the compiler sees that reads of one do not depend on the
-    // loads in flight into the other
-    constexpr int kBuf = PT::kBytes + QT::kBytes;
-    __shared__ __attribute__((aligned(16))) char buf0[kBuf], buf1[kBuf];
     constexpr bool kDeep = BP == 64 && BQ == 64;     // run_stages_deep
-    __shared__ __attribute__((aligned(16))) char buf2[kDeep ? kBuf : 16], buf3[kDeep ? kBuf : 16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wp = wave / WQ, wq = wave % WQ;
     ColsTile t;
-    if (!my_tile<KIND, BP, BQ, kBk>(a, t)) return;
+    if (!my_tile<KIND, BP, BQ, kBk>(a, block, t)) return;
 
     // the thread's chunks: byte within the row.  Lines 16 apart have the same order of chunks.
     constexpr int kLinesP = NT / PT::kCpl, kLinesQ = NT / QT::kCpl;
@@ -287,10 +285,30 @@ __global__ void __launch_bounds__(WP *WQ * 64) k_cols_direct(ColsArgs a) {
     store_tile<E, KIND, BP, BQ, WP, WQ>(a, t, acc, lane, wp, wq);
 }
 
+template <class E, ColsKind KIND, int BP, int BQ, int WP, int WQ>
+__global__ void __launch_bounds__(WP *WQ * 64) k_cols_direct(ColsArgs a) {
+    // an array each, so that the compiler sees that reads of one do not depend on the
+    // loads in flight into the other
+    constexpr int kBuf = kColsBuf<E, KIND, BP, BQ>, kMore = BP == 64 && BQ == 64 ? kBuf : 16;
+    __shared__ __attribute__((aligned(16))) char buf0[kBuf], buf1[kBuf], buf2[kMore], buf3[kMore];
+    cols_direct<E, KIND, BP, BQ, WP, WQ>(a, blockIdx.x, buf0, buf1, buf2, buf3);
+}
+
+// Both low-rank gradients in one launch, eight workgroups (one on each L2) of each in turn.
+template <class E>
+__global__ void __launch_bounds__(256) k_cols_low_pair(ColsArgs a, ColsArgs b) {
+    constexpr int L = kLowBytes / sizeof(E), kBuf = kColsBuf<E, ColsKind::kLowQ, 128, L>;
+    static_assert(kBuf == kColsBuf<E, ColsKind::kLowP, L, 128>);
+    __shared__ __attribute__((aligned(16))) char buf0[kBuf], buf1[kBuf];
+    const int block = blockIdx.x >> 4 << 3 | (blockIdx.x & 7);
+    if (blockIdx.x & 8) cols_direct<E, ColsKind::kLowP, L, 128, 1, 4>(b, block, buf0, buf1, nullptr, nullptr);
+    else cols_direct<E, ColsKind::kLowQ, 128, L, 4, 1>(a, block, buf0, buf1, nullptr, nullptr);
+}
+
 // out = sum of the parts
 template <class E>
-__global__ void __launch_bounds__(256) k_cols_sum(ColsArgs a, int64_t count) {
-    const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
+__device__ inline void sum_parts(const ColsArgs &a, int64_t i) {
+    const int64_t count = static_cast<int64_t>(a.g.G) * a.np * a.nq;
     if (i >= count) return;
     if (i + 4 <= count) {
         f32x4 v = {};
@@ -306,6 +324,22 @@ __global__ void __launch_bounds__(256) k_cols_sum(ColsArgs a, int64_t count) {
     }
 }
 
+// (of one gradient, or of two: grid.y)
+template <class E>
+__global__ void __launch_bounds__(256) k_cols_sum(ColsArgs a, ColsArgs b) {
+    const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
+    const ColsArgs &c = blockIdx.y ? b : a;
+    if (c.parts > 1) sum_parts<E>(c, i);
+}
+
+template <class E>
+hipError_t sum(const ColsArgs &a, const ColsArgs *b, hipStream_t s) {
+    auto blocks = [](const ColsArgs &c) { return c.parts > 1 ? (static_cast<int64_t>(c.g.G) * c.np * c.nq + 1023) / 1024 : 0; };
+    const int64_t most = std::max(blocks(a), b ? blocks(*b) : 0);
+    if (most == 0) return hipSuccess;
+    return launch_kernel(k_cols_sum<E>, dim3(static_cast<uint32_t>(most), b ? 2 : 1), dim3(256), 0, s, a, b ? *b : a);
+}
+
 // Rows in whole, aligned chunks of 16 bytes.
 template <class E, ColsKind KIND>
 bool whole_chunks(const ColsArgs &a) {
@@ -316,20 +350,30 @@ bool whole_chunks(const ColsArgs &a) {
     return (KIND == ColsKind::kLowP || whole(a.p, a.ldp, a.np)) && (KIND == ColsKind::kLowQ || whole(a.q, a.ldq, a.nq));
 }
 
+// Workgroups: a multiple of 8.
+int64_t cols_blocks(const ColsArgs &a, int64_t tp, int64_t tq) {
+    const int64_t per = tp * tq * a.parts, shares = cols_shares(per), share = (per + shares - 1) / shares;
+    return (a.g.G * shares + 7) / 8 * 8 * share;
+}
+
 template <class E, ColsKind KIND, int BP, int BQ, int WP, int WQ, bool DIRECT>
 hipError_t go(const ColsArgs &a, hipStream_t s) {
-    const int64_t tp = KIND == ColsKind::kLowP ? a.blocks : (a.np + BP - 1) / BP;
-    const int64_t tq = KIND == ColsKind::kLowQ ? a.blocks : (a.nq + BQ - 1) / BQ;
-    const int64_t per = tp * tq * a.parts, shares = cols_shares(per), share = (per + shares - 1) / shares;
-    const int64_t blocks = (a.g.G * shares + 7) / 8 * 8 * share;
+    const int64_t blocks = cols_blocks(a, KIND == ColsKind::kLowP ? a.blocks : (a.np + BP - 1) / BP,
+                                       KIND == ColsKind::kLowQ ? a.blocks : (a.nq + BQ - 1) / BQ);
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
     const dim3 grid(static_cast<uint32_t>(blocks)), block(WP * WQ * 64);
     hipError_t e;
     if constexpr (DIRECT) e = launch_kernel(k_cols_direct<E, KIND, BP, BQ, WP, WQ>, grid, block, 0, s, a);
     else e = launch_kernel(k_cols<E, KIND, BP, BQ, WP, WQ>, grid, block, 0, s, a);
-    if (e != hipSuccess || a.parts == 1) return e;
-    const int64_t count = static_cast<int64_t>(a.g.G) * a.np * a.nq;
-    return launch_kernel(k_cols_sum<E>, dim3(static_cast<uint32_t>((count + 1023) / 1024)), dim3(256), 0, s, a, count);
+    return e != hipSuccess ? e : sum<E>(a, nullptr, s);
+}
+
+template <class E>
+hipError_t low_pair(const ColsArgs &a, const ColsArgs &b, hipStream_t s) {
+    const int64_t most = std::max(cols_blocks(a, (a.np + 127) / 128, a.blocks), cols_blocks(b, b.blocks, (b.nq + 127) / 128));
+    if (2 * most > INT32_MAX) return hipErrorInvalidValue;
+    const hipError_t e = launch_kernel(k_cols_low_pair<E>, dim3(static_cast<uint32_t>(2 * most)), dim3(256), 0, s, a, b);
+    return e != hipSuccess ? e : sum<E>(a, &b, s);
 }
 
 template <class E>
@@ -391,6 +435,10 @@ ColsPlan cols_plan(bool bf16, ColsKind kind, const ColsArgs &a, int cus) {
 hipError_t launch_cols(bool bf16, ColsKind kind, const ColsArgs &a, int cus, hipStream_t s) {
     const ColsPlan p = cols_plan(bf16, kind, a, cus);
     return bf16 ? pick<__bf16>(kind, p, a, s) : pick<float>(kind, p, a, s);
+}
+
+hipError_t launch_cols_low_pair(bool bf16, const ColsArgs &q, const ColsArgs &p, hipStream_t s) {
+    return bf16 ? low_pair<__bf16>(q, p, s) : low_pair<float>(q, p, s);
 }
 
 }  // namespace hwr

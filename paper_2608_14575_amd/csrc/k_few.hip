@@ -182,22 +182,26 @@ __global__ void __launch_bounds__(kJoinThreads) k_join(FewArgs a) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int ct = (a.m_pad / 4 + kJoinThreads - 1) / kJoinThreads;
     const int p = blockIdx.x / ct, c = (blockIdx.x % ct * kJoinThreads + tid) * 4;
+    // everything that the place alone says first: the row, its group and that group's
+    // weights are looked up while it is on its way
+    f32x4 v = {};
+    if (c < a.m)
+#pragma unroll 4
+        for (int s = 0; s < a.parts; ++s)
+            v += *reinterpret_cast<const f32x4 *>(a.partial + (static_cast<int64_t>(s) * a.g.n + p) * a.m_pad + c);
     const int row = row_at(a.g, p);
     int g = a.g.G;
     if (ADAPTER) {
+        float t = 0.0f;
         g = group_of(a.g, p, lane);
         if (g < a.g.G && tid < a.rank) {
-            float v = 0.0f;
-            for (int s = 0; s < a.low_parts; ++s) v += a.low[(static_cast<int64_t>(s) * a.g.n + p) * a.rank + tid];
-            low[tid] = a.scale ? a.scale[g] * v : v;
+#pragma unroll 4
+            for (int s = 0; s < a.low_parts; ++s) t += a.low[(static_cast<int64_t>(s) * a.g.n + p) * a.rank + tid];
+            low[tid] = a.scale ? a.scale[g] * t : t;
         }
         __syncthreads();
     }
     if (row < 0 || c >= a.m) return;
-    f32x4 v = {};
-#pragma unroll 4
-    for (int s = 0; s < a.parts; ++s)
-        v += *reinterpret_cast<const f32x4 *>(a.partial + (static_cast<int64_t>(s) * a.g.n + p) * a.m_pad + c);
     const bool whole = c + 4 <= a.m;
     if (ADAPTER && g < a.g.G) {
         const E *b = static_cast<const E *>(a.b) + static_cast<int64_t>(g) * a.rank * a.m + c;

@@ -22,19 +22,24 @@ typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), may_alias));
 // the transposing read (bf16, ranks that are multiples of 4), kPicked by single elements.
 enum class From { kDirect, kTurned, kPicked };
 
-// NF column fragments, RB row fragments.
 template <class E, From FROM, int NF, int RB>
-__global__ void __launch_bounds__(kWaves * 64, NF == 8 || (FROM == From::kPicked && NF * RB == 8) ? 2 : 4) k_shrink(ShrinkArgs a) {
-    using El = Elem<E>;
-    constexpr int V = El::kEpc, BM = 16 * RB, kStep = 4 * V, kCols = 16 * NF;
-    constexpr int kAcc = RB * NF, kDeep = NF <= 2 ? 4 : 2;
+struct Sizes {
+    static constexpr int kStep = 4 * Elem<E>::kEpc;
     // a step's weights for each wave, or half of the waves' sums
-    constexpr int kOwn = FROM != From::kDirect ? kStep * kCols * sizeof(E) : 0, kSums = kAcc * 64 * 16;
-    constexpr int kLds = kWaves * kOwn > kWaves / 2 * kSums ? kWaves * kOwn : kWaves / 2 * kSums;
-    __shared__ __attribute__((aligned(16))) char lds[kLds];
+    static constexpr int kOwn = FROM != From::kDirect ? kStep * 16 * NF * (int)sizeof(E) : 0, kSums = RB * NF * 64 * 16;
+    static constexpr int kLds = kWaves * kOwn > kWaves / 2 * kSums ? kWaves * kOwn : kWaves / 2 * kSums;
+    static constexpr int kMinWaves = NF == 8 || (FROM == From::kPicked && NF * RB == 8) ? 2 : 4;   // a SIMD
+};
+
+// NF column fragments, RB row fragments; tile t of the batch.
+template <class E, From FROM, int NF, int RB>
+__device__ inline void shrink_tile(const ShrinkArgs &a, int t, char *lds) {
+    using El = Elem<E>;
+    using Sz = Sizes<E, FROM, NF, RB>;
+    constexpr int V = El::kEpc, BM = 16 * RB, kStep = Sz::kStep, kOwn = Sz::kOwn;
+    constexpr int kAcc = RB * NF, kDeep = NF <= 2 ? 4 : 2;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int m = lane & 15, q = lane >> 4;
-    const int t = blockIdx.x;
     if (t >= count_tiles(a.g, BM, false, lane)) return;
     const RowTile rt = find_tile(a.g, t, BM, false, lane);
     const E *w = static_cast<const E *>(a.w) + static_cast<int64_t>(rt.g) * a.k * a.rank;
@@ -161,35 +166,62 @@ __global__ void __launch_bounds__(kWaves * 64, NF == 8 || (FROM == From::kPicked
     }
 }
 
+template <class E, From FROM, int NF, int RB>
+__global__ void __launch_bounds__(kWaves * 64, (Sizes<E, FROM, NF, RB>::kMinWaves)) k_shrink(ShrinkArgs a) {
+    __shared__ __attribute__((aligned(16))) char lds[Sizes<E, FROM, NF, RB>::kLds];
+    shrink_tile<E, FROM, NF, RB>(a, blockIdx.x, lds);
+}
+
+// Two in one launch: the first's tiles take the even workgroups.
+template <class E, From FROM, int NF, int RB>
+__global__ void __launch_bounds__(kWaves * 64, (Sizes<E, FROM, NF, RB>::kMinWaves)) k_shrink_pair(ShrinkArgs a, ShrinkArgs b) {
+    constexpr int kA = Sizes<E, From::kDirect, NF, RB>::kLds, kB = Sizes<E, FROM, NF, RB>::kLds;
+    __shared__ __attribute__((aligned(16))) char lds[kA > kB ? kA : kB];
+    if (blockIdx.x & 1) shrink_tile<E, FROM, NF, RB>(b, blockIdx.x >> 1, lds);
+    else shrink_tile<E, From::kDirect, NF, RB>(a, blockIdx.x >> 1, lds);
+}
+
+// One (pair null), or with it [rank][k] weights beside `pair`'s [k][rank].
+template <class E, From FROM, int NF, int RB>
+hipError_t go(const ShrinkArgs &a, const ShrinkArgs *pair, hipStream_t s) {
+    const uint32_t tiles = static_cast<uint32_t>(a.g.n / (16 * RB) + (a.g.n < a.g.G ? a.g.n : a.g.G));
+    if constexpr (FROM != From::kDirect)
+        if (pair) return launch_kernel(k_shrink_pair<E, FROM, NF, RB>, dim3(2 * tiles), dim3(kWaves * 64), 0, s, a, *pair);
+    return launch_kernel(k_shrink<E, FROM, NF, RB>, dim3(tiles), dim3(kWaves * 64), 0, s, a);
+}
+
 template <class E, From FROM, int NF>
-hipError_t go(const ShrinkArgs &a, int cus, hipStream_t s) {
-    auto tiles = [&](int bm) { return static_cast<uint32_t>(a.g.n / bm + (a.g.n < a.g.G ? a.g.n : a.g.G)); };
+hipError_t rows(const ShrinkArgs &a, const ShrinkArgs *pair, int cus, hipStream_t s) {
     // two blocks of rows share the weights' loads where the device stays full
     if constexpr (NF <= 4)
-        if (a.g.n >= 32 * cus) return launch_kernel(k_shrink<E, FROM, NF, 2>, dim3(tiles(32)), dim3(kWaves * 64), 0, s, a);
-    return launch_kernel(k_shrink<E, FROM, NF, 1>, dim3(tiles(16)), dim3(kWaves * 64), 0, s, a);
+        if (a.g.n >= 32 * cus) return go<E, FROM, NF, 2>(a, pair, s);
+    return go<E, FROM, NF, 1>(a, pair, s);
 }
 
 template <class E, From FROM>
-hipError_t ranks(const ShrinkArgs &a, int cus, hipStream_t s) {
-    if (a.rank <= 16) return go<E, FROM, 1>(a, cus, s);
-    if (a.rank <= 32) return go<E, FROM, 2>(a, cus, s);
-    if (a.rank <= 64) return go<E, FROM, 4>(a, cus, s);
-    return go<E, FROM, 8>(a, cus, s);
+hipError_t ranks(const ShrinkArgs &a, const ShrinkArgs *pair, int cus, hipStream_t s) {
+    if (a.rank <= 16) return rows<E, FROM, 1>(a, pair, cus, s);
+    if (a.rank <= 32) return rows<E, FROM, 2>(a, pair, cus, s);
+    if (a.rank <= 64) return rows<E, FROM, 4>(a, pair, cus, s);
+    return rows<E, FROM, 8>(a, pair, cus, s);
 }
 
 template <class E>
-hipError_t pick(bool ks, const ShrinkArgs &a, int cus, hipStream_t s) {
-    if (!ks) return ranks<E, From::kDirect>(a, cus, s);
+hipError_t pick(bool ks, const ShrinkArgs &a, const ShrinkArgs *pair, int cus, hipStream_t s) {
+    if (!ks && !pair) return ranks<E, From::kDirect>(a, nullptr, cus, s);
     if constexpr (sizeof(E) == 2)
-        if (a.rank % 4 == 0) return ranks<E, From::kTurned>(a, cus, s);
-    return ranks<E, From::kPicked>(a, cus, s);
+        if (a.rank % 4 == 0) return ranks<E, From::kTurned>(a, pair, cus, s);
+    return ranks<E, From::kPicked>(a, pair, cus, s);
 }
 
 }  // namespace
 
 hipError_t launch_shrink(bool bf16, bool ks, const ShrinkArgs &a, int cus, hipStream_t s) {
-    return bf16 ? pick<__bf16>(ks, a, cus, s) : pick<float>(ks, a, cus, s);
+    return bf16 ? pick<__bf16>(ks, a, nullptr, cus, s) : pick<float>(ks, a, nullptr, cus, s);
+}
+
+hipError_t launch_shrink_pair(bool bf16, const ShrinkArgs &direct, const ShrinkArgs &ks, int cus, hipStream_t s) {
+    return bf16 ? pick<__bf16>(false, direct, &ks, cus, s) : pick<float>(false, direct, &ks, cus, s);
 }
 
 }  // namespace hwr

@@ -117,6 +117,8 @@ struct RowsPlan {
 RowsPlan rows_plan(bool bf16, RowsKind kind, bool ks, const RowsArgs &a, int cus);
 hipError_t launch_rows(bool bf16, RowsKind kind, bool ks, const RowsArgs &a, int cus, hipStream_t s);
 hipError_t launch_shrink(bool bf16, bool ks, const ShrinkArgs &a, int cus, hipStream_t s);
+// Two of the same rows and rank in one launch: with [rank][k] and with [k][rank] weights.
+hipError_t launch_shrink_pair(bool bf16, const ShrinkArgs &direct, const ShrinkArgs &ks, int cus, hipStream_t s);
 bool few_rows(int n, int G, bool adapter, bool bf16);              // whether launch_few is meant for the batch
 int few_tiles(int n, int G, bool adapter);
 int few_parts(int n, int G, int k, int m, bool bf16, bool adapter, int cus);
@@ -131,5 +133,7 @@ struct ColsPlan {
 };
 ColsPlan cols_plan(bool bf16, ColsKind kind, const ColsArgs &a, int cus);
 hipError_t launch_cols(bool bf16, ColsKind kind, const ColsArgs &a, int cus, hipStream_t s);
+// kLowQ and kLowP of the same groups and rank in one launch; both plans direct
+hipError_t launch_cols_low_pair(bool bf16, const ColsArgs &q, const ColsArgs &p, hipStream_t s);
 
 }  // namespace hwr

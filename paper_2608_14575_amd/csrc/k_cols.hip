@@ -127,9 +127,9 @@ __device__ inline void multiply_tile(const char *lds, int at_q, int p0, int q0, 
     for (int sub = 0; sub < 2; ++sub) {
         typename Elem<E>::Frag fq[QF], fp[PF];
 #pragma unroll
-        for (int j = 0; j < QF; ++j) fq[j] = QT::frag(lds, at_q, q0 + j * 16, sub, lane);
+        for (int j = 0; j < QF; ++j) fq[j] = QT::frag(lds, at_q, q0 + j * 16, sub, QT::base(lane));
 #pragma unroll
-        for (int i = 0; i < PF; ++i) fp[i] = PT::frag(lds, 0, p0 + i * 16, sub, lane);
+        for (int i = 0; i < PF; ++i) fp[i] = PT::frag(lds, 0, p0 + i * 16, sub, PT::base(lane));
 #pragma unroll
         for (int i = 0; i < PF; ++i)
 #pragma unroll

@@ -86,12 +86,12 @@ __device__ inline void add_adapters(const RowsArgs &a, const RowTile &rt, int c0
             for (int sub = 0; sub < 2; ++sub) {
                 typename El::Frag fw[CF];
 #pragma unroll
-                for (int j = 0; j < CF; ++j) fw[j] = WT::frag(sw, 0, (wc * CF + j) * 16, sub, lane);
+                for (int j = 0; j < CF; ++j) fw[j] = WT::frag(sw, 0, (wc * CF + j) * 16, sub, WT::base(lane));
 #pragma unroll
                 for (int i = 0; i < RF; ++i) {
                     const int f0 = rt.p0 + (wr * RF + i) * 16;
                     if (f0 + 16 <= lo || f0 >= hi) continue;
-                    const typename El::Frag fx = XT::frag(sx, 0, (wr * RF + i) * 16, sub, lane);
+                    const typename El::Frag fx = XT::frag(sx, 0, (wr * RF + i) * 16, sub, XT::base(lane));
                     const int p = f0 + (lane & 15);
                     const bool in_group = p >= lo && p < hi;
 #pragma unroll
@@ -241,9 +241,9 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows(RowsArgs a) {
         for (int sub = 0; sub < 2; ++sub) {
             typename El::Frag fw[CF], fx[RF];
 #pragma unroll
-            for (int j = 0; j < CF; ++j) fw[j] = WT::frag(sw, 0, (wc * CF + j) * 16, sub, lane);
+            for (int j = 0; j < CF; ++j) fw[j] = WT::frag(sw, 0, (wc * CF + j) * 16, sub, WT::base(lane));
 #pragma unroll
-            for (int i = 0; i < RF; ++i) fx[i] = XT::frag(sx, 0, (wr * RF + i) * 16, sub, lane);
+            for (int i = 0; i < RF; ++i) fx[i] = XT::frag(sx, 0, (wr * RF + i) * 16, sub, XT::base(lane));
 #pragma unroll
             for (int i = 0; i < RF; ++i)
 #pragma unroll

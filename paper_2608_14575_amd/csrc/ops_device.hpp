@@ -71,31 +71,34 @@ struct Tile {
         else if constexpr (kCpl == 4) return ((line >> 3) & 1) << 1;
         else return 0;
     }
+    // Byte of the lane's share of the fragment at row (column) 0 of the tile's first
+    // half.  A lane's line keeps its chunk order from one fragment to the next, so that the
+    // others differ by constants, added or (within a line) xored.
+    static __device__ int base(int lane) {
+        const int m = lane & 15, q = lane >> 4;
+        if constexpr (!KS) return m * 128 + ((q ^ swz(m)) << 4);
+        else if constexpr (sizeof(E) == 4) return q * 4 * (kCpl * 16) + (((m >> 2) ^ swz(q * 4)) << 4) + (m & 3) * 4;
+        else return (q * 8 + (m >> 2)) * (kCpl * 16) + ((((m & 3) >> 1) ^ swz(q * 8 + (m >> 2))) << 4) + (m & 1) * 8;
+    }
     // Fragment of the 16 rows (columns) from c0 on, contraction half `sub` of the
     // stage; the tile lies at byte `at` of the LDS array.  (One offset, added once:
     // the compiler follows an array through few additions only, and reads that it
     // cannot place wait for every load in flight into LDS.)
-    static __device__ typename Elem<E>::Frag frag(const char *lds, int at, int c0, int sub, int lane) {
-        const int m = lane & 15, q = lane >> 4;
+    static __device__ typename Elem<E>::Frag frag(const char *lds, int at, int c0, int sub, int base) {
         if constexpr (!KS) {
-            const int line = c0 + m, o = at + line * 128 + (((sub * 4 + q) ^ swz(line)) << 4);
+            const int o = (base ^ (sub * 64)) + at + c0 * 128;
             return *reinterpret_cast<const typename Elem<E>::Frag *>(lds + o);
         } else if constexpr (sizeof(E) == 4) {
+            const int o = (base ^ (c0 * 4)) + at + sub * 16 * (kCpl * 16);
             f32x4 v;
-            const int c = c0 + m;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int line = sub * 16 + q * 4 + i;
-                const int o = at + line * (kCpl * 16) + (((c >> 2) ^ swz(line)) << 4) + (c & 3) * 4;
-                v[i] = *reinterpret_cast<const float *>(lds + o);
-            }
+            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const float *>(lds + o + i * (kCpl * 16));
             return v;
         } else {
             // the transposing read: 16 lanes fetch 4 lines x 16 columns, lane m gets
             // column m (line + 4 has the same chunk order)
             typedef __attribute__((address_space(3))) i16x4 lds_v;
-            const int c = c0 + (m & 3) * 4, line = sub * 32 + q * 8 + (m >> 2);
-            const int o = at + line * (kCpl * 16) + (((c >> 3) ^ swz(line)) << 4) + (c & 4) * 2;
+            const int o = (base ^ (c0 * 2)) + at + sub * 32 * (kCpl * 16);
             union { i16x4 h[2]; bf16x8 f; } u;
             u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v *)(lds + o));
             u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v *)(lds + o + 4 * kCpl * 16));
@@ -282,10 +285,11 @@ __device__ inline void run_stages(int stages, Issue issue, char *buf0, char *buf
     using El = Elem<E>;
     constexpr int kAhead = RF / 2, kBarrier = 2 * RF - kAhead;
     typename El::Frag x[RF], w[2][CF];
+    int xb = XT::base(lane), wb = WT::base(lane);
     auto read_x = [&](const char *b, int group) {        // groups 0 .. 2 RF - 1 of a stage
-        x[group % RF] = XT::frag(b, 0, x0 + group % RF * 16, group / RF, lane);
+        x[group % RF] = XT::frag(b, 0, x0 + group % RF * 16, group / RF, xb);
     };
-    auto read_w = [&](const char *b, int half, int j) { w[half][j] = WT::frag(b, XT::kBytes, w0 + j * 16, half, lane); };
+    auto read_w = [&](const char *b, int half, int j) { w[half][j] = WT::frag(b, XT::kBytes, w0 + j * 16, half, wb); };
     auto arrived = [&] {
         wait_lds();
         wait_vm<0>();
@@ -300,6 +304,8 @@ __device__ inline void run_stages(int stages, Issue issue, char *buf0, char *buf
     auto stage = [&](char *cur, char *next, int s) {
 #pragma unroll
         for (int group = 0; group < 2 * RF; ++group) {
+            // addresses are made where they are used (kept, they would fill the registers)
+            if (group % RF == 0) asm volatile("" : "+v"(xb), "+v"(wb));
             if (group == kBarrier) {
                 arrived();
                 if (s + 2 < stages) issue(cur, s + 2);
@@ -346,11 +352,12 @@ __device__ inline void run_stages_deep(int stages, Issue issue, char *buf0, char
                                        int lane, f32x4 (&acc)[RF][CF]) {
     using El = Elem<E>;
     typename El::Frag x[2][RF], w[2][CF];
+    const int xb = XT::base(lane), wb = WT::base(lane);
     auto read = [&](const char *b, int half) {
 #pragma unroll
-        for (int j = 0; j < CF; ++j) w[half][j] = WT::frag(b, XT::kBytes, w0 + j * 16, half, lane);
+        for (int j = 0; j < CF; ++j) w[half][j] = WT::frag(b, XT::kBytes, w0 + j * 16, half, wb);
 #pragma unroll
-        for (int i = 0; i < RF; ++i) x[half][i] = XT::frag(b, 0, x0 + i * 16, half, lane);
+        for (int i = 0; i < RF; ++i) x[half][i] = XT::frag(b, 0, x0 + i * 16, half, xb);
     };
     auto multiply = [&](int half) {
 #pragma unroll

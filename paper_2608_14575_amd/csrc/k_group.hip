@@ -1,23 +1,23 @@
 // Rows by group: a stable counting sort of the routed rows.
 //
-// A wave takes 512 rows in order, 64 at a time, and counts them by key in LDS.
-// A row's place is where its key begins, plus the rows of the key before the
-// wave, plus those before the row in the wave: lanes of one key find each other by
+// A wave takes 512 (several blocks: 256) rows in order, 64 at a time, and counts them by
+// key in LDS.  A row's place is where its key begins, plus the rows of the key before
+// the wave, plus those before the row in the wave: lanes of one key find each other by
 // a ballot for each bit of the key.  Up to 8,192 rows fit one workgroup and one
-// launch; more take three: counts by block, a scan over the blocks of every key, and the
-// places.  Latency bounds the small form, three launches and the scattered row
-// numbers the large one (8 MB for a million rows).
+// launch; more take two, counts by block and the places, or three with a scan over the
+// blocks of every key between them (two_launches).  Latency bounds the small form,
+// the launches and the scattered row numbers the large one (8 MB for a million rows).
 #include "ops_device.hpp"
 
 namespace hwr {
 namespace {
 
-constexpr int kChunks = 8, kWaveRows = 64 * kChunks;
-constexpr int kBlockWaves = 4, kBlockRows = kBlockWaves * kWaveRows;     // several blocks
-constexpr int kOneWaves = 16, kOneRows = kOneWaves * kWaveRows;          // one workgroup
+constexpr int kSmallWaves = 4, kWaves = 16;
+constexpr int kChunks = 8;                                               // one workgroup: 64 rows each
+constexpr int kSmallRows = kSmallWaves * 64 * kChunks, kOneRows = kWaves * 64 * kChunks;
+constexpr int kBlockChunks = 4, kBlockRows = kWaves * 64 * kBlockChunks; // several
 
-__device__ inline int group_key(const GroupRowsArgs &a, int row) {
-    int c = a.choice[row];
+__device__ inline int group_key(const GroupRowsArgs &a, int c) {
     if (a.table) c = static_cast<unsigned>(c) < static_cast<unsigned>(a.n_table) ? a.table[c] : -1;
     return static_cast<unsigned>(c) < static_cast<unsigned>(a.G) ? c : a.G;
 }
@@ -43,17 +43,54 @@ __device__ inline void scan_keys(int count, Value value, Use use) {
     }
 }
 
-enum class Step { kAll, kCount, kPlace };
+enum class Step { kAll, kCount, kPlace, kSumAndPlace };
 
-template <Step STEP, int WAVES>
+// total and before of every key, from the counts by block: all of its rows, and those in
+// the blocks before this one.  A wave takes four keys at a time.
+template <int WAVES>
+__device__ inline void sum_blocks(const GroupRowsArgs &a, int keys, int *total, int *before) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int i0 = wave; i0 < keys; i0 += 4 * WAVES) {
+        int t[4] = {}, b[4] = {};
+#pragma unroll 4
+        for (int at = lane; at < a.blocks; at += 64)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int key = i0 + j * WAVES;
+                const int v = key < keys ? a.hist[static_cast<int64_t>(key) * a.blocks + at] : 0;
+                t[j] += v;
+                b[j] += at < static_cast<int>(blockIdx.x) ? v : 0;
+            }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+#pragma unroll
+            for (int d = 32; d; d >>= 1) {
+                t[j] += __shfl_xor(t[j], d);
+                b[j] += __shfl_xor(b[j], d);
+            }
+            if (lane == 0 && i0 + j * WAVES < keys) {
+                total[i0 + j * WAVES] = t[j];
+                before[i0 + j * WAVES] = b[j];
+            }
+        }
+    }
+}
+
+template <Step STEP, int WAVES, int kChunks>
 __global__ void __launch_bounds__(WAVES * 64) k_group(GroupRowsArgs a) {
+    constexpr int kWaveRows = 64 * kChunks;
+    constexpr bool kSum = STEP == Step::kSumAndPlace;
     // counts by wave, then the place of the wave's next row of each key
     __shared__ int count[WAVES][kMaxPairs + 1];
+    __shared__ int total[kSum ? kMaxPairs + 1 : 1], in_blocks[kSum ? kMaxPairs + 1 : 1];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, keys = a.G + 1;
     const int64_t r0 = (static_cast<int64_t>(blockIdx.x) * WAVES + wave) * kWaveRows + lane;
     int key[kChunks];
 #pragma unroll
-    for (int j = 0; j < kChunks; ++j) key[j] = r0 + j * 64 < a.n ? group_key(a, static_cast<int>(r0 + j * 64)) : -1;
+    for (int j = 0; j < kChunks; ++j) key[j] = r0 + j * 64 < a.n ? a.choice[r0 + j * 64] : -1;
+    if constexpr (kSum) sum_blocks<WAVES>(a, keys, total, in_blocks);    // while the choices are on their way
+#pragma unroll
+    for (int j = 0; j < kChunks; ++j) key[j] = r0 + j * 64 < a.n ? group_key(a, key[j]) : -1;
     for (int i = lane; i < keys; i += 64) count[wave][i] = 0;
     __syncthreads();
 #pragma unroll
@@ -71,10 +108,11 @@ __global__ void __launch_bounds__(WAVES * 64) k_group(GroupRowsArgs a) {
         return;
     }
     scan_keys<WAVES>(
-        keys, [&](int i) { return STEP == Step::kAll ? in_block(i) : a.totals[i]; },
+        keys, [&](int i) { return STEP == Step::kAll ? in_block(i) : kSum ? total[i] : a.totals[i]; },
         [&](int i, int before) {
             if (blockIdx.x == 0 && i <= a.G) a.offsets[i] = before;
             if (STEP == Step::kPlace) before += a.hist[static_cast<int64_t>(i) * a.blocks + blockIdx.x];
+            if (kSum) before += in_blocks[i];
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) {
                 const int c = count[w][i];
@@ -123,14 +161,23 @@ __global__ void __launch_bounds__(256) k_group_scan(GroupRowsArgs a) {
 
 int group_rows_blocks(int n) { return n > kOneRows ? static_cast<int>((static_cast<int64_t>(n) + kBlockRows - 1) / kBlockRows) : 1; }
 
+// Whether every block of the places sums the counts of the blocks itself, rather than a
+// launch between: one round of 64 keys and 256 blocks.  (us, two / three launches: 100,000
+// rows 5 keys 9.8 / 12.3, 64 keys 10.8 / 12.0, 201 keys 17.6 / 13.0; 1,048,576 rows 33 keys
+// 12.4 / 13.6, 64 keys 13.5 / 14.5, 201 keys 21.4 / 16.5; 3,145,728 rows 33 keys 33.9 / 26.3.)
+static bool two_launches(const GroupRowsArgs &a) { return a.G < 64 && a.blocks <= 256; }
+
 hipError_t launch_group_rows(const GroupRowsArgs &a, hipStream_t s) {
-    if (a.n <= kBlockRows) return launch_kernel(k_group<Step::kAll, kBlockWaves>, dim3(1), dim3(kBlockWaves * 64), 0, s, a);
-    if (a.blocks == 1) return launch_kernel(k_group<Step::kAll, kOneWaves>, dim3(1), dim3(kOneWaves * 64), 0, s, a);
-    hipError_t e = launch_kernel(k_group<Step::kCount, kBlockWaves>, dim3(a.blocks), dim3(kBlockWaves * 64), 0, s, a);
+    if (a.n <= kSmallRows)
+        return launch_kernel(k_group<Step::kAll, kSmallWaves, kChunks>, dim3(1), dim3(kSmallWaves * 64), 0, s, a);
+    const dim3 grid(a.blocks), block(kWaves * 64);
+    if (a.blocks == 1) return launch_kernel(k_group<Step::kAll, kWaves, kChunks>, grid, block, 0, s, a);
+    hipError_t e = launch_kernel(k_group<Step::kCount, kWaves, kBlockChunks>, grid, block, 0, s, a);
     if (e != hipSuccess) return e;
+    if (two_launches(a)) return launch_kernel(k_group<Step::kSumAndPlace, kWaves, kBlockChunks>, grid, block, 0, s, a);
     e = launch_kernel(k_group_scan, dim3((a.G + 4) / 4), dim3(256), 0, s, a);
     if (e != hipSuccess) return e;
-    return launch_kernel(k_group<Step::kPlace, kBlockWaves>, dim3(a.blocks), dim3(kBlockWaves * 64), 0, s, a);
+    return launch_kernel(k_group<Step::kPlace, kWaves, kBlockChunks>, grid, block, 0, s, a);
 }
 
 }  // namespace hwr

@@ -13,13 +13,39 @@ heads of the chosen models, all on the device and one stream.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 
 from . import hwr
 from .hwr import HWR_BF16, HWR_ERR_INVALID_ARG, HWR_F32, HwrError
 
 
+_MAX_INT = 2 ** 31 - 1
+
+
 def _bad(name, msg):
     raise HwrError(HWR_ERR_INVALID_ARG, f"{name}: {msg}")
+
+
+class _Call:
+    """An entry point that takes hwr_groups and a structure of arguments: both are
+    packed into one block that stays (a structure made anew for every call took
+    about 1 us of a call's 10; a context is not used by two threads at once)."""
+    _CODES = {C.c_int32: "i", C.c_int64: "q", C.c_void_p: "P"}
+
+    def __init__(self, fn, args):
+        codes = ["".join(self._CODES[t] for _, t in s._fields_) for s in (hwr.hwr_groups, args)]
+        at = C.sizeof(hwr.hwr_groups)                  # a multiple of every alignment
+        self._block = C.create_string_buffer(at + C.sizeof(args))
+        self._pack = struct.Struct("@" + "".join(codes)).pack_into
+        self._fn = C.cast(fn, C.CFUNCTYPE(C.c_int, C.c_void_p, C.c_void_p, C.c_void_p))
+        self._at = C.addressof(self._block), C.addressof(self._block) + at
+
+    def __call__(self, ctx, n, G, offsets, order, args) -> int:
+        try:
+            self._pack(self._block, 0, n, G, offsets, order, *args)
+        except struct.error as e:
+            _bad("sizes", f"outside their types ({e})")
+        return self._fn(ctx, *self._at)
 
 
 class RoutedOps:
@@ -39,6 +65,10 @@ class RoutedOps:
         self.device, self.stream = int(device), int(stream)
         self.ctx = hwr.hwr_ops_init(self.device, self.stream)
         self._lib = hwr.load()
+        self._matmul = _Call(self._lib.hwr_grouped_matmul, hwr.hwr_matmul_args)
+        self._matmul_grad = _Call(self._lib.hwr_grouped_matmul_grad, hwr.hwr_matmul_grad_args)
+        self._adapter = _Call(self._lib.hwr_adapter_matmul, hwr.hwr_adapter_args)
+        self._adapter_grad = _Call(self._lib.hwr_adapter_matmul_grad, hwr.hwr_adapter_grad_args)
 
     def close(self) -> None:
         if getattr(self, "ctx", None):
@@ -56,25 +86,26 @@ class RoutedOps:
         hwr.hwr_ops_reserve(self.ctx, int(nbytes))
 
     # ------------------------------------------------------------ checks
-    def _dense(self, name, t, dtype, *shape) -> int:
-        if not t.is_cuda or t.get_device() != self.device:
+    # (the reason for a refusal is looked for once a tensor does not fit)
+    def _refuse(self, name, t, dtype, shape):
+        if t.get_device() != self.device:
             _bad(name, f"on {t.device}, expected cuda:{self.device}")
         if t.dtype is not dtype:
             _bad(name, f"dtype {t.dtype} (expected {dtype})")
         if t.shape != shape:
             _bad(name, f"shape {tuple(t.shape)}, expected {shape}")
-        if not t.is_contiguous():
-            _bad(name, "not contiguous")
+        _bad(name, "not contiguous")
+
+    def _dense(self, name, t, dtype, shape) -> int:
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != self.device or not t.is_contiguous():
+            self._refuse(name, t, dtype, shape)
         return t.data_ptr()
 
-    def _rows(self, name, t, dtype, n, width):
+    def _rows(self, name, t, dtype, shape):
         """Pointer and row stride of an [n][width] matrix."""
-        if not t.is_cuda or t.get_device() != self.device:
-            _bad(name, f"on {t.device}, expected cuda:{self.device}")
-        if t.dtype is not dtype:
-            _bad(name, f"dtype {t.dtype} (expected {dtype})")
-        if t.shape != (n, width):
-            _bad(name, f"shape {tuple(t.shape)}, expected {(n, width)}")
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != self.device:
+            self._refuse(name, t, dtype, shape)
+        n, width = shape
         if t.is_contiguous():
             return t.data_ptr(), width
         ld, unit = t.stride()
@@ -82,20 +113,18 @@ class RoutedOps:
             _bad(name, f"strides {t.stride()}: rows must be contiguous and must not overlap")
         return t.data_ptr(), max(ld, width)
 
-    def _groups(self, n, groups, offsets, order) -> hwr.hwr_groups:
-        return hwr.hwr_groups(n, groups, self._dense("offsets", offsets, self._i32, groups + 1),
-                              None if order is None else self._dense("order", order, self._i32, n))
+    def _x(self, x):
+        """Type and shape of the rows."""
+        dt, shape = x.dtype, x.shape
+        if dt not in self._kinds:
+            _bad("x", f"dtype {dt} (expected bfloat16 or float32)")
+        if len(shape) != 2:
+            _bad("x", f"{len(shape)} dimensions, expected 2")
+        return dt, shape
 
-    def _kind(self, t):
-        kind = self._kinds.get(t.dtype)
-        if kind is None:
-            _bad("x", f"dtype {t.dtype} (expected bfloat16 or float32)")
-        if t.dim() != 2:
-            _bad("x", f"{t.dim()} dimensions, expected 2")
-        return kind
-
-    def _call(self, fn, groups, args):
-        st = fn(self.ctx, C.byref(groups), C.byref(args))
+    def _run(self, call, n, G, offsets, order, *args):
+        st = call(self.ctx, n, G, self._dense("offsets", offsets, self._i32, (G + 1,)),
+                  0 if order is None else self._dense("order", order, self._i32, (n,)), args)
         if st:
             raise HwrError(st, hwr.hwr_ops_last_error(self.ctx))
 
@@ -104,71 +133,70 @@ class RoutedOps:
         """Rows by group: ``choice`` [n] int32, the group of each row or (with
         ``table`` [pairs] int32) the pair whose group the table holds; anything out
         of range is a row in no group.  Writes ``offsets`` [n_groups + 1] and ``order`` [n]."""
-        n = choice.shape[0]
-        i32 = self._i32
-        c = self._dense("choice", choice, i32, n)
-        t, nt = (None, 0) if table is None else (self._dense("table", table, i32, table.numel()), table.numel())
-        st = self._lib.hwr_group_rows(self.ctx, n, c, t, nt, n_groups,
-                                      self._dense("offsets", offsets, i32, n_groups + 1), self._dense("order", order, i32, n))
+        i32, n, nt = self._i32, choice.numel(), 0 if table is None else table.numel()
+        if max(n, nt, n_groups) > _MAX_INT or n_groups < 0:
+            _bad("choice, table, n_groups", f"{n}, {nt}, {n_groups}: outside 32 bits")
+        st = self._lib.hwr_group_rows(self.ctx, n, self._dense("choice", choice, i32, (n,)),
+                                      None if table is None else self._dense("table", table, i32, (nt,)), nt, n_groups,
+                                      self._dense("offsets", offsets, i32, (n_groups + 1,)),
+                                      self._dense("order", order, i32, (n,)))
         if st:
             raise HwrError(st, hwr.hwr_ops_last_error(self.ctx))
 
-    def matmul(self, x, w, offsets, order=None, *, y) -> None:
-        """y[r] = x[r] w[g(r)]; w [G][k][m].  A row in no group gets zeros."""
-        kind, dt = self._kind(x), x.dtype
-        n, k = x.shape
+    def _weights(self, w):
         if w.dim() != 3:
             _bad("w", f"{w.dim()} dimensions, expected 3")
-        G, _, m = w.shape
-        xp, ldx = self._rows("x", x, dt, n, k)
-        yp, ldy = self._rows("y", y, dt, n, m)
-        self._call(self._lib.hwr_grouped_matmul, self._groups(n, G, offsets, order),
-                   hwr.hwr_matmul_args(kind, k, m, xp, ldx, self._dense("w", w, dt, G, k, m), yp, ldy))
+        return w.shape
+
+    def matmul(self, x, w, offsets, order=None, *, y) -> None:
+        """y[r] = x[r] w[g(r)]; w [G][k][m].  A row in no group gets zeros."""
+        dt, (n, k) = self._x(x)
+        G, _, m = self._weights(w)
+        xp, ldx = self._rows("x", x, dt, (n, k))
+        yp, ldy = self._rows("y", y, dt, (n, m))
+        self._run(self._matmul, n, G, offsets, order,
+                  self._kinds[dt], k, m, xp, ldx, self._dense("w", w, dt, (G, k, m)), yp, ldy)
 
     def matmul_grad(self, dy, x, w, offsets, order=None, *, dx=None, dw=None) -> None:
         """Gradients of ``matmul``: dx [n][k] and dw [G][k][m], either may be left out."""
-        kind, dt = self._kind(x), x.dtype
-        n, k = x.shape
-        if w.dim() != 3:
-            _bad("w", f"{w.dim()} dimensions, expected 3")
-        G, _, m = w.shape
-        dyp, lddy = self._rows("dy", dy, dt, n, m)
-        xp, ldx = self._rows("x", x, dt, n, k)
-        dxp, lddx = (None, 0) if dx is None else self._rows("dx", dx, dt, n, k)
-        self._call(self._lib.hwr_grouped_matmul_grad, self._groups(n, G, offsets, order),
-                   hwr.hwr_matmul_grad_args(kind, k, m, dyp, lddy, xp, ldx, self._dense("w", w, dt, G, k, m), dxp, lddx,
-                                            None if dw is None else self._dense("dw", dw, dt, G, k, m)))
+        dt, (n, k) = self._x(x)
+        G, _, m = self._weights(w)
+        dyp, lddy = self._rows("dy", dy, dt, (n, m))
+        xp, ldx = self._rows("x", x, dt, (n, k))
+        dxp, lddx = (0, 0) if dx is None else self._rows("dx", dx, dt, (n, k))
+        self._run(self._matmul_grad, n, G, offsets, order,
+                  self._kinds[dt], k, m, dyp, lddy, xp, ldx, self._dense("w", w, dt, (G, k, m)), dxp, lddx,
+                  0 if dw is None else self._dense("dw", dw, dt, (G, k, m)))
 
-    def _adapter(self, x, w, a, b, scale):
-        kind, dt = self._kind(x), x.dtype
-        n, k = x.shape
+    def _adapters(self, dt, k, w, a, b, scale):
+        """Sizes m, G and rank, and the pointers."""
         if w.dim() != 2 or a.dim() != 3:
             _bad("w, a", f"{w.dim()} and {a.dim()} dimensions, expected 2 and 3")
         m, (G, _, R) = w.shape[1], a.shape
-        return (kind, dt, n, k, m, G, R, self._dense("w", w, dt, k, m), self._dense("a", a, dt, G, k, R),
-                self._dense("b", b, dt, G, R, m),
-                None if scale is None else self._dense("scale", scale, self._f32, G))
+        return (m, G, R, self._dense("w", w, dt, (k, m)), self._dense("a", a, dt, (G, k, R)),
+                self._dense("b", b, dt, (G, R, m)), 0 if scale is None else self._dense("scale", scale, self._f32, (G,)))
 
     def adapter(self, x, w, a, b, scale, offsets, order=None, *, y) -> None:
         """y[r] = x[r] w + scale[g] (x[r] a[g]) b[g]; w [k][m], a [G][k][rank],
         b [G][rank][m], scale [G] float32 or None (1).  A row in no group gets x[r] w."""
-        kind, dt, n, k, m, G, R, wp, ap, bp, sp = self._adapter(x, w, a, b, scale)
-        xp, ldx = self._rows("x", x, dt, n, k)
-        yp, ldy = self._rows("y", y, dt, n, m)
-        self._call(self._lib.hwr_adapter_matmul, self._groups(n, G, offsets, order),
-                   hwr.hwr_adapter_args(kind, k, m, R, xp, ldx, wp, ap, bp, sp, yp, ldy))
+        dt, (n, k) = self._x(x)
+        m, G, R, wp, ap, bp, sp = self._adapters(dt, k, w, a, b, scale)
+        xp, ldx = self._rows("x", x, dt, (n, k))
+        yp, ldy = self._rows("y", y, dt, (n, m))
+        self._run(self._adapter, n, G, offsets, order, self._kinds[dt], k, m, R, xp, ldx, wp, ap, bp, sp, yp, ldy)
 
     def adapter_grad(self, dy, x, w, a, b, scale, offsets, order=None, *, dx=None, da=None, db=None) -> None:
         """Gradients of ``adapter``: dx [n][k], da [G][k][rank] and db [G][rank][m],
         any may be left out; w is frozen."""
-        kind, dt, n, k, m, G, R, wp, ap, bp, sp = self._adapter(x, w, a, b, scale)
-        dyp, lddy = self._rows("dy", dy, dt, n, m)
-        xp, ldx = self._rows("x", x, dt, n, k)
-        dxp, lddx = (None, 0) if dx is None else self._rows("dx", dx, dt, n, k)
-        self._call(self._lib.hwr_adapter_matmul_grad, self._groups(n, G, offsets, order),
-                   hwr.hwr_adapter_grad_args(kind, k, m, R, dyp, lddy, xp, ldx, wp, ap, bp, sp, dxp, lddx,
-                                             None if da is None else self._dense("da", da, dt, G, k, R),
-                                             None if db is None else self._dense("db", db, dt, G, R, m)))
+        dt, (n, k) = self._x(x)
+        m, G, R, wp, ap, bp, sp = self._adapters(dt, k, w, a, b, scale)
+        dyp, lddy = self._rows("dy", dy, dt, (n, m))
+        xp, ldx = self._rows("x", x, dt, (n, k))
+        dxp, lddx = (0, 0) if dx is None else self._rows("dx", dx, dt, (n, k))
+        self._run(self._adapter_grad, n, G, offsets, order,
+                  self._kinds[dt], k, m, R, dyp, lddy, xp, ldx, wp, ap, bp, sp, dxp, lddx,
+                  0 if da is None else self._dense("da", da, dt, (G, k, R)),
+                  0 if db is None else self._dense("db", db, dt, (G, R, m)))
 
 
 def example(steps: int = 5, n: int = 4096, seed: int = 7) -> list:

@@ -48,3 +48,21 @@ def test_no_device_is_a_clean_error():
     with pytest.raises(hwr.HwrError) as e:
         routed.RoutedOps()
     assert e.value.status == hwr.HWR_ERR_HIP
+
+
+@pytest.mark.parametrize("name", STRUCTS[1:])
+def test_packed_arguments_are_the_structures(name):
+    """What a call packs reads back, through the structures, as what it was given; what
+    no field can hold is refused."""
+    cls = getattr(hwr, name)
+    call = routed._Call(hwr.load().hwr_grouped_matmul, cls)
+    values = [(i + 3) << (40 if t is not C.c_int32 else 8) for i, (_, t) in enumerate(cls._fields_)]
+    assert call(None, 5, 6, 7 << 40, 0, values) == hwr.HWR_ERR_INVALID_ARG     # (no context: nothing is read)
+    g = hwr.hwr_groups.from_buffer(call._block)
+    assert (g.n, g.n_groups, g.offsets, g.order) == (5, 6, 7 << 40, None)
+    a = cls.from_buffer(call._block, C.sizeof(hwr.hwr_groups))
+    assert [getattr(a, f) for f, _ in cls._fields_] == values
+    for n, bad in ((2 ** 31, values), (-2 ** 31 - 1, values), (5, [2 ** 31] + values[1:])):
+        with pytest.raises(hwr.HwrError) as e:
+            call(None, n, 6, 1, 0, bad)
+        assert e.value.status == hwr.HWR_ERR_INVALID_ARG

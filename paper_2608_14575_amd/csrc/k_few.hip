@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_join(FewArgs a) {
         f32x4 add = {};
         if (whole) {
             struct __attribute__((packed, aligned(sizeof(E)))) Four { E e[4]; };
-#pragma unroll 8
+#pragma unroll 16
             for (int r = 0; r < a.rank; ++r) {
                 const Four f = *reinterpret_cast<const Four *>(b + static_cast<int64_t>(r) * a.m);
 #pragma unroll

@@ -117,11 +117,14 @@ __device__ inline u32x4 load_chunk(const E *line, int e, int len) {
         const typename Elem<E>::Vec v = *reinterpret_cast<const typename Elem<E>::Vec *>(line + e);
         return u32x4{v[0], v[1], v[2], v[3]};
     }
+    // the end of a line: every element is loaded, of those past it the last (loads under a
+    // condition each wait for the one before)
     union { u32x4 v; E s[kEpc]; } u;
-    u.v = u32x4{0, 0, 0, 0};
+    E at[kEpc];
 #pragma unroll
-    for (int i = 0; i < kEpc; ++i)
-        if (e + i < len) u.s[i] = line[e + i];
+    for (int i = 0; i < kEpc; ++i) at[i] = line[min(e + i, len - 1)];
+#pragma unroll
+    for (int i = 0; i < kEpc; ++i) u.s[i] = e + i < len ? at[i] : static_cast<E>(0.0f);
     return u.v;
 }
 

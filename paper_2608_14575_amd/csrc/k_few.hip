@@ -204,9 +204,11 @@ __global__ void __launch_bounds__(kJoinThreads) k_join(FewArgs a) {
     if (row < 0 || c >= a.m) return;
     const bool whole = c + 4 <= a.m;
     if (ADAPTER && g < a.g.G) {
-        const E *b = static_cast<const E *>(a.b) + static_cast<int64_t>(g) * a.rank * a.m + c;
+        // (the row's last columns, where they are cut: the four that end with the row)
+        const int first = a.m < 4 ? c : min(c, a.m - 4);
+        const E *b = static_cast<const E *>(a.b) + static_cast<int64_t>(g) * a.rank * a.m + first;
         f32x4 add = {};
-        if (whole) {
+        if (a.m >= 4) {
             struct __attribute__((packed, aligned(sizeof(E)))) Four { E e[4]; };
 #pragma unroll 16
             for (int r = 0; r < a.rank; ++r) {
@@ -219,6 +221,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_join(FewArgs a) {
                 for (int e = 0; e < 4; ++e)
                     if (c + e < a.m) add[e] = fmaf(low[r], static_cast<float>(b[static_cast<int64_t>(r) * a.m + e]), add[e]);
         }
+        for (int skip = first; skip < c; ++skip) add = f32x4{add[1], add[2], add[3], 0.0f};
         v += add;
     }
     E *at = static_cast<E *>(a.y) + row * a.ldy + c;

@@ -172,9 +172,13 @@ class Pads {
     // past the first *used bytes of the work space (and counts them in), leaves their
     // addresses and row strides where the matrices' were, and sets *padded.  A copy is a
     // pass over the matrix (3.5 TB/s, 3 us to launch); without it operands pass through
-    // registers, which takes about twice the time of the products at their ordinary rate.
-    hwr_status copy(hwr_ops *c, double flops, uint64_t *used, bool *padded) {
-        *padded = all_ > 0 && all_ / 1.75e12 + 3e-6 < flops / (bf16_ ? 6e14 : 8e13);
+    // registers, which takes about twice the time of the products at their ordinary rate,
+    // and more where a weight gradient is among them.  (bf16, us with / without copies: adapter
+    // 15,945 x 1176 x 1046 121.9 / 134.9, 8,413 x 1385 x 320 53.8 / 47.4; grouped gradients 5,198 x 427 x
+    // 1058 in 20 groups 58.9 / 72.4, 116 x 1061 x 278 in 32 groups 44.8 / 31.8.)
+    hwr_status copy(hwr_ops *c, double flops, bool gradients, uint64_t *used, bool *padded) {
+        const double rate = (bf16_ ? 6e14 : 8e13) / (gradients ? 2 : 1);
+        *padded = all_ > 0 && all_ / 1.75e12 + 3e-6 < flops / rate;
         if (!*padded || args_.count == 0) return HWR_OK;
         char *at = nullptr;
         if (hwr_status st = workspace(c, *used + bytes(), &at)) return st;
@@ -339,7 +343,7 @@ hwr_status grouped_matmul(hwr_ops *c, const hwr_groups *g, const hwr_matmul_args
     Pads pads(bf16);
     pads.add(&x, &ldx, g->n, a->k);
     pads.add(&w, &ldw, static_cast<int64_t>(g->n_groups) * a->k, a->m);
-    if (hwr_status st = pads.copy(c, 2.0 * g->n * a->k * a->m, &used, &padded)) return st;
+    if (hwr_status st = pads.copy(c, 2.0 * g->n * a->k * a->m, false, &used, &padded)) return st;
     return rows(c, bf16, RowsKind::kGrouped, true,
                 rows_args(c, g, true, padded, x, ldx, a->k, w, ldw, a->k, false, a->m, a->y, dense(a->ldy, a->m)), used);
 }
@@ -364,7 +368,7 @@ hwr_status grouped_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_matmul
     pads.add(&dy, &lddy, g->n, a->m);
     pads.add(&w, &ldw, static_cast<int64_t>(g->n_groups) * a->k, a->m, a->dx != nullptr);
     pads.add(&x, &ldx, g->n, a->k, a->dw != nullptr);
-    if (hwr_status st = pads.copy(c, 4.0 * g->n * a->k * a->m, &used, &padded)) return st;
+    if (hwr_status st = pads.copy(c, 4.0 * g->n * a->k * a->m, true, &used, &padded)) return st;
     if (a->dx && g->n > 0) {
         const RowsArgs r =
             rows_args(c, g, false, padded, dy, lddy, a->m, w, ldw, a->k, false, a->k, a->dx, dense(a->lddx, a->k));
@@ -427,7 +431,7 @@ hwr_status adapter_matmul(hwr_ops *c, const hwr_groups *g, const hwr_adapter_arg
     Pads pads(bf16);
     pads.add(&x, &ldxp, g->n, a->k);
     pads.add(&w, &ldw, a->k, a->m);
-    if (hwr_status st = pads.copy(c, 2.0 * g->n * a->k * a->m, &used, &padded)) return st;
+    if (hwr_status st = pads.copy(c, 2.0 * g->n * a->k * a->m, false, &used, &padded)) return st;
     RowsArgs r = rows_args(c, g, true, padded, x, ldxp, a->k, w, ldw, a->k, true, a->m, a->y, dense(a->ldy, a->m));
     r.low = low;
     r.lw = a->b;
@@ -470,7 +474,7 @@ hwr_status adapter_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_adapte
     pads.add(&dy, &lddyp, g->n, a->m, a->dx || a->db);
     pads.add(&w, &ldw, a->k, a->m, a->dx != nullptr);
     pads.add(&x, &ldxp, g->n, a->k, a->da != nullptr);
-    if (hwr_status st = pads.copy(c, 2.0 * g->n * a->k * a->m, &used, &padded)) return st;
+    if (hwr_status st = pads.copy(c, 2.0 * g->n * a->k * a->m, true, &used, &padded)) return st;
     if (g->n > 0 && a->dx) {
         RowsArgs r = rows_args(c, g, false, padded, dy, lddyp, a->m, w, ldw, a->k, true, a->k, a->dx, dense(a->lddx, a->k));
         r.low = up;

@@ -74,7 +74,6 @@ __device__ inline void store_tile(const ColsArgs &a, const ColsTile &t, const f3
     const int64_t each = static_cast<int64_t>(a.np) * a.nq;
     E *out = static_cast<E *>(a.out) + t.g * each;
     float *part = a.partial + (static_cast<int64_t>(t.part) * a.g.G + t.g) * each;
-    const bool vec = (a.nq & 3) == 0 && (a.parts > 1 || (reinterpret_cast<uintptr_t>(a.out) & (4 * sizeof(E) - 1)) == 0);
 #pragma unroll
     for (int i = 0; i < PN; ++i) {
         const int pr = p_first + i * 16 + (lane & 15);
@@ -89,23 +88,9 @@ __device__ inline void store_tile(const ColsArgs &a, const ColsTile &t, const f3
                 for (int e = 0; e < 4; ++e) v[e] = __builtin_isfinite(v[e]) ? v[e] + lo[e] : v[e];
             }
             const int c = q_first + j * 16 + (lane >> 4) * 4;
-            const int64_t at = static_cast<int64_t>(pr) * a.nq + c;
-            if (a.parts > 1) {
-                if (vec && c < a.nq) *reinterpret_cast<f32x4 *>(part + at) = v;
-                else
-                    for (int e = 0; e < 4; ++e)
-                        if (c + e < a.nq) part[at + e] = v[e];
-                continue;
-            }
-            typename El::Out4 o;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = static_cast<E>(v[e]);
-            if (vec && c < a.nq) *reinterpret_cast<typename El::Out4 *>(out + at) = o;
-            else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (c + e < a.nq) out[at + e] = o[e];
-            }
+            const int64_t line = static_cast<int64_t>(pr) * a.nq;
+            if (a.parts > 1) store_four<float>(part + line, c, a.nq, v);
+            else store_four<E>(out + line, c, a.nq, v);
         }
     }
 }
@@ -314,7 +299,10 @@ __device__ inline void sum_parts(const ColsArgs &a, int64_t i) {
         f32x4 v = {};
 #pragma unroll 4
         for (int s = 0; s < a.parts; ++s) v += *reinterpret_cast<const f32x4_a4 *>(a.partial + s * count + i);
-        for (int e = 0; e < 4; ++e) static_cast<E *>(a.out)[i + e] = static_cast<E>(v[e]);
+        typename Elem<E>::Out4 o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = static_cast<E>(v[e]);
+        *reinterpret_cast<typename Elem<E>::Out4 *>(static_cast<E *>(a.out) + i) = o;
     } else {
         for (int64_t j = i; j < count; ++j) {
             float v = 0.0f;

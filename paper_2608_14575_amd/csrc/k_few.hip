@@ -202,7 +202,6 @@ __global__ void __launch_bounds__(kJoinThreads) k_join(FewArgs a) {
         __syncthreads();
     }
     if (row < 0 || c >= a.m) return;
-    const bool whole = c + 4 <= a.m;
     if (ADAPTER && g < a.g.G) {
         // (the row's last columns, where they are cut: the four that end with the row)
         const int first = a.m < 4 ? c : min(c, a.m - 4);
@@ -224,9 +223,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_join(FewArgs a) {
         for (int skip = first; skip < c; ++skip) add = f32x4{add[1], add[2], add[3], 0.0f};
         v += add;
     }
-    E *at = static_cast<E *>(a.y) + row * a.ldy + c;
-    for (int e = 0; e < 4; ++e)
-        if (whole || c + e < a.m) at[e] = static_cast<E>(v[e]);
+    store_four<E>(static_cast<E *>(a.y) + row * a.ldy, c, a.m, v);
 }
 
 template <class E, bool ADAPTER>

@@ -112,7 +112,6 @@ template <class E, int BM, int BN, int WR, int WC>
 __device__ inline void store_rows(const RowsArgs &a, const RowTile &rt, int c0, int part, const int *rows,
                                   const f32x4 (&acc)[BM / WR / 16][BN / WC / 16], int tid) {
     constexpr int RF = BM / WR / 16, CF = BN / WC / 16;
-    using El = Elem<E>;
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WC, wc = wave % WC;
     const int q = lane >> 4;
     if (a.parts > 1) {
@@ -130,7 +129,6 @@ __device__ inline void store_rows(const RowsArgs &a, const RowTile &rt, int c0, 
         return;
     }
     E *y = static_cast<E *>(a.y);
-    const bool vec = (a.m & 3) == 0 && (a.ldy & 3) == 0 && (reinterpret_cast<uintptr_t>(y) & (4 * sizeof(E) - 1)) == 0;
 #pragma unroll
     for (int i = 0; i < RF; ++i) {
         const int r = rows[(wr * RF + i) * 16 + (lane & 15)];
@@ -138,16 +136,7 @@ __device__ inline void store_rows(const RowsArgs &a, const RowTile &rt, int c0, 
         E *line = y + r * a.ldy;
 #pragma unroll
         for (int j = 0; j < CF; ++j) {
-            const int c = c0 + (wc * CF + j) * 16 + q * 4;
-            typename El::Out4 o;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = static_cast<E>(acc[i][j][e]);
-            if (vec && c < a.m) *reinterpret_cast<typename El::Out4 *>(line + c) = o;
-            else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (c + e < a.m) line[c + e] = o[e];
-            }
+            store_four<E>(line, c0 + (wc * CF + j) * 16 + q * 4, a.m, acc[i][j]);
         }
     }
 }

@@ -21,6 +21,7 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef __bf16 bf16x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
 
 template <class E>
 struct Elem;
@@ -29,7 +30,7 @@ template <>
 struct Elem<__bf16> {
     using Frag = bf16x8;
     using Vec = u32x4_a2;
-    using Out4 = bf16x4;
+    using Out4 = bf16x4_a2;
     static constexpr int kBk = 64;    // contraction elements of a stage
     static constexpr int kEpc = 8;    // elements of a 16-byte chunk
     static __device__ f32x4 mma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -39,7 +40,7 @@ template <>
 struct Elem<float> {
     using Frag = f32x4;
     using Vec = u32x4_a4;
-    using Out4 = f32x4;
+    using Out4 = f32x4_a4;
     static constexpr int kBk = 32;
     static constexpr int kEpc = 4;
     static __device__ f32x4 mma(Frag a, Frag b, f32x4 c) {
@@ -126,6 +127,21 @@ __device__ inline u32x4 load_chunk(const E *line, int e, int len) {
 #pragma unroll
     for (int i = 0; i < kEpc; ++i) u.s[i] = e + i < len ? at[i] : static_cast<E>(0.0f);
     return u.v;
+}
+
+// Four neighbouring elements from column c on, where the line of m columns has them.
+template <class E>
+__device__ inline void store_four(E *line, int c, int m, f32x4 v) {
+    typename Elem<E>::Out4 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = static_cast<E>(v[e]);
+    if (c + 4 <= m) {
+        *reinterpret_cast<typename Elem<E>::Out4 *>(line + c) = o;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c + e < m) line[c + e] = o[e];
+    }
 }
 
 // Operand fragment j of V 16-byte vectors: element j of each.

@@ -123,6 +123,21 @@ def test_group(ops, n, G, P):
     assert np.array_equal(offsets.cpu().numpy(), np.searchsorted(key[want], np.arange(G + 1)))
 
 
+@pytest.mark.parametrize("n", [8192, 8193, 12288, 1048576, 1048577])
+@pytest.mark.parametrize("G", [3, 63, 64])
+def test_group_many_rows(ops, n, G):
+    """Either side of where one workgroup, two launches and three take over."""
+    gen = torch.Generator("cuda").manual_seed(n + G)
+    choice = torch.randint(-1, G + 1, (n,), generator=gen, device="cuda", dtype=torch.int32)
+    order = torch.full((n,), -7, dtype=torch.int32, device="cuda")
+    offsets = torch.full((G + 1,), -7, dtype=torch.int32, device="cuda")
+    ops.group(choice, G, offsets=offsets, order=order)
+    key = np.where((choice.cpu().numpy() >= 0) & (choice.cpu().numpy() < G), choice.cpu().numpy(), G)
+    want = np.argsort(key, kind="stable")
+    assert np.array_equal(order.cpu().numpy(), want)
+    assert np.array_equal(offsets.cpu().numpy(), np.searchsorted(key[want], np.arange(G + 1)))
+
+
 # ---------------------------------------------------------------- grouped products
 SHAPES = [
     # n, G, k, m, groups, already ordered, stride padding
@@ -260,6 +275,58 @@ def test_adapter_and_gradients(ops, n, G, k, m, R, kind, ordered, pad, with_scal
         alone = torch.zeros_like(v)
         ops.adapter_grad(dy, x, w, a, b, scale, off, order, **{name: alone})
         assert torch.equal(alone, v), name
+
+
+# ---------------------------------------------------------------- alignment
+def offset_by_one(t):
+    """The same matrix, dense, one element past a 16-byte boundary; what stands around it."""
+    buf = torch.full((t.numel() + 2,), 5.0, dtype=t.dtype, device="cuda")
+    v = buf[1:-1].view(t.shape)
+    v.copy_(t)
+    return v, buf
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,G,k,m,R", [(5, 2, 40, 72, 8), (50, 3, 37, 131, 5), (300, 2, 264, 135, 12), (700, 3, 256, 128, 40),
+                                       (4000, 2, 1001, 1003, 16), (2600, 5, 3, 2, 1)])
+def test_pointers_aligned_to_their_elements_alone(ops, n, G, k, m, R, dtype):
+    """Every matrix starts one element past a boundary; outputs are whole and nothing
+    beside them is written."""
+    t, u, lo = TYPES[dtype]
+    gen = torch.Generator("cuda").manual_seed(n + m)
+    gid, off, order = grouped(sizes_of("skew", n, G, np.random.default_rng(n)), G)
+    x, dy = offset_by_one(rand(gen, n, k, dtype=t))[0], offset_by_one(rand(gen, n, m, dtype=t))[0]
+    w, ws = offset_by_one(rand(gen, G, k, m, dtype=t))[0], offset_by_one(rand(gen, k, m, dtype=t))[0]
+    a, b = offset_by_one(rand(gen, G, k, R, dtype=t))[0], offset_by_one(rand(gen, G, R, m, dtype=t))[0]
+    out, around = {}, {}
+    for name, like in (("y", dy), ("z", dy), ("dx", x), ("dz", x), ("dw", w), ("da", a), ("db", b)):
+        out[name], around[name] = offset_by_one(torch.full_like(like, 7.0))
+    ops.matmul(x, w, off, order, y=out["y"])
+    ops.matmul_grad(dy, x, w, off, order, dx=out["dx"], dw=out["dw"])
+    ops.adapter(x, ws, a, b, None, off, order, y=out["z"])
+    ops.adapter_grad(dy, x, ws, a, b, None, off, order, dx=out["dz"], da=out["da"], db=out["db"])
+    for name, buf in around.items():
+        assert buf[0] == 5.0 and buf[-1] == 5.0, name
+    T = lambda v: v.transpose(-1, -2).contiguous()  # noqa: E731
+    shared = np.zeros(n, np.int64)
+    ref, s = product(x, w, gid)
+    close(out["y"], ref, u * ref.abs() + (k + 16) * EPS * s)
+    ref, s = product(dy, T(w), gid)
+    close(out["dx"], ref, u * ref.abs() + (m + 16) * EPS * s)
+    ref, s, cnt = outer(x, dy, gid, G)
+    close(out["dw"], ref, u * ref.abs() + (cnt + 16) * EPS * s)
+    low, slow = product(x, a, gid)
+    up, sup = product(dy, T(b), gid)
+    for got, p, wide, mid, smid, thin, width in ((out["z"], x, ws[None], low, slow, b, k), (out["dz"], dy, T(ws)[None], up, sup, T(a), m)):
+        main, smain = product(p, wide, shared)
+        add, _ = product(mid, thin, gid)
+        exactly, _ = product(mid.abs(), thin.abs(), gid)
+        sadd, _ = product(smid, thin.abs(), gid)
+        close(got, main + add, u * (main + add).abs() + (width + R + 32) * EPS * (smain + sadd) + 2 * lo * exactly)
+    ref, _, cnt = outer(x, up, gid, G)
+    close(out["da"], ref, u * ref.abs() + (m + cnt + 32) * EPS * outer(x.abs(), sup, gid, G)[0] + 2 * lo * outer(x.abs(), up.abs(), gid, G)[0])
+    ref, _, _ = outer(low, dy, gid, G)
+    close(out["db"], ref, u * ref.abs() + (k + cnt + 32) * EPS * outer(slow, dy.abs(), gid, G)[0] + 2 * lo * outer(low.abs(), dy.abs(), gid, G)[0])
 
 
 # ---------------------------------------------------------------- gradients against differences

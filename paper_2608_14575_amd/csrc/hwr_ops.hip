@@ -322,7 +322,7 @@ hwr_status grouped_matmul(hwr_ops *c, const hwr_groups *g, const hwr_matmul_args
     if (!a->x || !a->w || !a->y) return invalid(c, "x, w and y are required");
     if (misaligned(a->dtype, {a->x, a->w, a->y})) return invalid(c, "a pointer is not aligned to its elements");
     if (hwr_status st = use_device(c)) return st;
-    if (few_rows(g->n, g->n_groups, false, a->dtype == HWR_BF16)) {
+    if (few_rows(g->n, g->n_groups, a->k, a->m, false, a->dtype == HWR_BF16)) {
         FewArgs f{};
         f.g = groups_arg(g);
         f.k = a->k;
@@ -403,7 +403,7 @@ hwr_status adapter_matmul(hwr_ops *c, const hwr_groups *g, const hwr_adapter_arg
         return invalid(c, "a pointer is not aligned to its elements");
     if (hwr_status st = use_device(c)) return st;
     const int64_t ldx = dense(a->ldx, a->k);
-    if (few_rows(g->n, g->n_groups, true, a->dtype == HWR_BF16)) {
+    if (few_rows(g->n, g->n_groups, a->k, a->m, true, a->dtype == HWR_BF16)) {
         FewArgs f{};
         f.g = groups_arg(g);
         f.k = a->k;

@@ -248,11 +248,14 @@ hipError_t go(const FewArgs &a, hipStream_t s) {
 }  // namespace
 
 // Up to where 16-row tiles that read the weights once each beat larger tiles (which
-// take a launch or two more with an adapter).  us, few / larger, 2048 x 2048: adapter bf16
-// 128 rows 22.3 / 25.2, 192 rows 23.7 / 28.6, 256 rows 28.1 / 27.7; fp32 256 rows 37 / 44;
-// grouped (2 groups) bf16 96 rows 14.3 / 13.7, fp32 256 rows 38 / 44, 384 rows 48 / 44.
-bool few_rows(int n, int G, bool adapter, bool bf16) {
-    return n <= (bf16 ? (adapter ? 192 : 64) : 256) || (!adapter && n <= kFewTile * G);
+// take a launch or two more with an adapter).  us, few / larger: adapter bf16 1024 x 1024
+// 192 rows 17.0 / 18.2; 2048 x 2048 130 rows 19.4 / 23.0, 192 rows 20.8 / 22.8, 256 rows 28.1 / 27.7;
+// 2752 x 3712 80 rows 24.9 / 27.2, 130 rows 45.4 / 30.5; 4096 x 4096 96 rows 27.8 / 34.6, 130 rows
+// 41.8 / 36.8; fp32 2048 x 2048 256 rows 37 / 44; grouped (2 groups) bf16 4096 x 4096 49 rows
+// 19.1 / 20.1, 64 rows 26.7 / 20.4, fp32 2048 x 2048 256 rows 38 / 44, 384 rows 48 / 44.
+bool few_rows(int n, int G, int k, int m, bool adapter, bool bf16) {
+    const int most = !bf16 ? 256 : !adapter ? 48 : static_cast<int64_t>(k) * m <= 1 << 22 ? 192 : 96;
+    return n <= most || (!adapter && n <= kFewTile * G);
 }
 
 int few_tiles(int n, int G, bool adapter) {

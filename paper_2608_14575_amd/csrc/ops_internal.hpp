@@ -119,7 +119,7 @@ hipError_t launch_rows(bool bf16, RowsKind kind, bool ks, const RowsArgs &a, int
 hipError_t launch_shrink(bool bf16, bool ks, const ShrinkArgs &a, int cus, hipStream_t s);
 // Two of the same rows and rank in one launch: with [rank][k] and with [k][rank] weights.
 hipError_t launch_shrink_pair(bool bf16, const ShrinkArgs &direct, const ShrinkArgs &ks, int cus, hipStream_t s);
-bool few_rows(int n, int G, bool adapter, bool bf16);              // whether launch_few is meant for the batch
+bool few_rows(int n, int G, int k, int m, bool adapter, bool bf16);  // whether launch_few is meant for the batch
 int few_tiles(int n, int G, bool adapter);
 int few_parts(int n, int G, int k, int m, bool bf16, bool adapter, int cus);
 hipError_t launch_few(bool bf16, bool adapter, const FewArgs &a, hipStream_t s);

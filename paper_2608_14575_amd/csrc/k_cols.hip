@@ -385,7 +385,10 @@ hipError_t pick(ColsKind kind, const ColsPlan &p, const ColsArgs &a, hipStream_t
 
 // The largest tile with which workgroups fill the device, sharing tiles' places if need be:
 // each part has at least 8 stages of an average group (4 with the smallest tile; its
-// partial sums are written and read once, 1.6 ps an element).
+// partial sums are written and read once, 1.6 ps an element).  fp32: not 128 for one to three tiles
+// a compute unit, whose rounds come out uneven (both gradients, us, 64 / 128: 3,408 x 832 x 320 in 22 groups
+// 68 / 80, 2,400 x 1024 x 1536 in 4 175 / 190, 1,455 x 284 x 1160 in 9 43 / 56; one group of 4,096 x 1024 x
+// 1024 185 / 162 in parts).
 ColsPlan cols_plan(bool bf16, ColsKind kind, const ColsArgs &a, int cus) {
     ColsPlan p{false, 64, 1};
     if (bf16)
@@ -407,6 +410,7 @@ ColsPlan cols_plan(bool bf16, ColsKind kind, const ColsArgs &a, int cus) {
     if (kind == ColsKind::kDense) {
         for (int t = p.direct && bf16 ? 256 : 128; t >= 64; t /= 2) {
             const int64_t n = parts(tiles(t), cus);
+            if (!bf16 && t > 64 && tiles(t) >= cus && tiles(t) < 3 * cus) continue;
             if (t > 64 && (a.np < t || a.nq < t || n > std::max<int64_t>(1, stages / 8))) continue;
             p.tile = t;
             p.parts = static_cast<int>(std::min<int64_t>(n, std::max<int64_t>(1, stages / 4)));

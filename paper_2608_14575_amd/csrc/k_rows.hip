@@ -383,7 +383,9 @@ bool whole_chunks(bool bf16, bool ks, const RowsArgs &a) {
 // The largest tile that gives most compute units a workgroup: 256 half of them with an
 // adapter, three of four without (us, 256 / 128: adapter 2,100 x 2048 x 4096 72 / 98, 3,300 x 1024 x 4096
 // 50 / 80, 4,208 x 2200 x 3226 89 / 153; grouped, 4 groups, 2048 x 4096 1,600 rows 56 / 41, 2,100 rows 58 / 61,
-// 3,000 rows 61 / 74); where even small tiles leave units idle, parts of the contraction of at least
+// 3,000 rows 61 / 74); fp32 128 from three a compute unit, for below that rounds and the ends of groups
+// cost more (64 / 128: 4,096 x 1536 x 1536 in one group 165 / 202, 4,096 x 1024 x 1024 in 32 115 / 137,
+// with adapters 4,096 x 1024 x 1536 in 8 136 / 155; 16,384 x 1024 x 1536 in one 444 / 406); where even small tiles leave units idle, parts of the contraction of at least
 // four stages.
 RowsPlan rows_plan(bool bf16, RowsKind kind, bool ks, const RowsArgs &a, int cus) {
     auto tiles = [&](int64_t bm, int64_t bn) {
@@ -393,7 +395,7 @@ RowsPlan rows_plan(bool bf16, RowsKind kind, bool ks, const RowsArgs &a, int cus
     const int stages = (a.k + (bf16 ? 63 : 31)) / (bf16 ? 64 : 32);
     const int enough = kind == RowsKind::kAdapter ? cus / 2 : cus * 3 / 4;
     if (p.direct && bf16 && a.mw >= 256 && tiles(256, 256) >= enough) p.bm = p.bn = 256;
-    else if ((!p.direct || a.mw >= 128) && tiles(128, 128) >= cus) p.bm = p.bn = 128;
+    else if ((!p.direct || a.mw >= 128) && tiles(128, 128) >= (bf16 || !p.direct ? 1 : 3) * cus) p.bm = p.bn = 128;
     else if (p.direct && !bf16 && tiles(64, 64) < 2 * cus) p.bm = 32;
     while (p.bm < 256 && tiles(p.bm, p.bn) * p.parts < cus && stages >= 8 * p.parts) p.parts *= 2;
     return p;

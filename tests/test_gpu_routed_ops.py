@@ -165,6 +165,9 @@ SHAPES = [
     (4096, 1, 2048, 1024, "even", False, 0),
     (9000, 2, 2048, 1032, "skew", False, 0),
     (700, 9, 640, 40, "skew", False, 0),
+    # tiles of 256 on part of the device; fp32 tiles of 64 where 128 would come out uneven
+    (2900, 2, 520, 4104, "skew", False, 0),
+    (3408, 22, 832, 320, "skew", False, 0),
 ]
 
 
@@ -218,6 +221,12 @@ ADAPTERS = [
     (4000, 3, 1001, 1003, 16, "skew", False, 0, True),
     (9000, 4, 1024, 2048, 32, "skew", False, 0, True),
     (9000, 4, 768, 384, 6, "skew", True, 0, False),
+    # tiles of 256 on half the device; either side of where few rows end for small and large weights
+    (2300, 3, 520, 4104, 16, "skew", False, 0, True),
+    (96, 4, 2104, 2056, 8, "skew", False, 0, True),
+    (97, 4, 2104, 2056, 8, "skew", False, 0, True),
+    (192, 4, 512, 520, 8, "skew", False, 0, True),
+    (193, 4, 512, 520, 8, "skew", False, 0, True),
 ]
 
 

@@ -126,7 +126,7 @@ struct Shape {
 // Null when sound, else what is wrong.
 const char *check_groups(const hwr_groups *g) {
     if (!g) return "groups is NULL";
-    if (g->n < 0) return "n < 0";
+    if (g->n < 0 || g->n > HWR_OPS_MAX_ROWS) return "rows outside 0..2147483136";
     if (g->n_groups < 1 || g->n_groups > kMaxPairs) return "n_groups outside 1..1024";
     if (!g->offsets) return "offsets is NULL";
     return nullptr;

@@ -1,0 +1,179 @@
+// Host-only driver of the operators on a routed batch (tests/test_ops_host_cpu.py
+// builds and runs it).  The HIP runtime functions that they call are defined here, in
+// the executable, and so take the place of the runtime's: memory is an address without
+// anything behind it, kernels are recorded by name and grid and not run.
+//
+//   ops_path <scenario>        prints "ok", or the failed checks (exit 1)
+#include <hip/hip_runtime_api.h>
+
+#include <cstdint>
+#include <cstdio>
+#include <cstring>
+#include <map>
+#include <string>
+#include <vector>
+
+#include "hwr_ops.h"
+
+namespace {
+
+struct Launch {
+    std::string kernel;
+    dim3 grid, block;
+};
+std::vector<Launch> g_log;
+std::map<const void *, std::string> &kernels() {      // registered before main
+    static std::map<const void *, std::string> m;
+    return m;
+}
+std::map<uintptr_t, size_t> g_mem;
+uintptr_t g_next = uintptr_t(1) << 40;
+dim3 g_grid, g_block;
+size_t g_shm;
+hipStream_t g_stream;
+
+hipError_t launch(const void *f, dim3 grid, dim3 block) {
+    g_log.push_back({kernels()[f], grid, block});
+    return hipSuccess;
+}
+
+}  // namespace
+
+extern "C" {
+void **__hipRegisterFatBinary(const void *) {
+    static void *h;
+    return &h;
+}
+void __hipUnregisterFatBinary(void **) {}
+void __hipRegisterFunction(void **, const void *host, char *, const char *name, unsigned, void *, void *, void *, void *, int *) {
+    kernels()[host] = name;
+}
+void __hipRegisterVar(void **, void *, char *, char *, int, size_t, int, int) {}
+hipError_t __hipPushCallConfiguration(dim3 g, dim3 b, size_t shm, hipStream_t s) {
+    g_grid = g, g_block = b, g_shm = shm, g_stream = s;
+    return hipSuccess;
+}
+hipError_t __hipPopCallConfiguration(dim3 *g, dim3 *b, size_t *shm, hipStream_t *s) {
+    *g = g_grid, *b = g_block, *shm = g_shm, *s = g_stream;
+    return hipSuccess;
+}
+hipError_t hipLaunchKernel(const void *f, dim3 grid, dim3 block, void **, size_t, hipStream_t) { return launch(f, grid, block); }
+hipError_t hipExtLaunchKernel(const void *f, dim3 grid, dim3 block, void **, size_t, hipStream_t, hipEvent_t, hipEvent_t, int) {
+    return launch(f, grid, block);
+}
+hipError_t hipMalloc(void **p, size_t n) {
+    g_mem[g_next] = n;
+    *p = reinterpret_cast<void *>(g_next);
+    g_next += (n + 4095) / 4096 * 4096 + 4096;
+    return hipSuccess;
+}
+hipError_t hipFree(void *p) {
+    g_mem.erase(reinterpret_cast<uintptr_t>(p));
+    return hipSuccess;
+}
+hipError_t hipMemset(void *, int, size_t) { return hipSuccess; }
+hipError_t hipDeviceSynchronize() { return hipSuccess; }
+hipError_t hipGetDeviceCount(int *n) { return *n = 1, hipSuccess; }
+hipError_t hipGetDevice(int *d) { return *d = 0, hipSuccess; }
+hipError_t hipSetDevice(int) { return hipSuccess; }
+hipError_t hipGetDevicePropertiesR0600(hipDeviceProp_tR0600 *p, int) {
+    *p = {};
+    std::strcpy(p->gcnArchName, "gfx950");
+    p->multiProcessorCount = 256;
+    return hipSuccess;
+}
+const char *hipGetErrorName(hipError_t) { return "error"; }
+const char *hipGetErrorString(hipError_t) { return "injected"; }
+hipError_t hipGetLastError() { return hipSuccess; }
+hipError_t hipStreamSynchronize(hipStream_t) { return hipSuccess; }
+hipError_t hipStreamIsCapturing(hipStream_t, hipStreamCaptureStatus *c) { return *c = hipStreamCaptureStatusNone, hipSuccess; }
+}
+
+namespace {
+
+int g_bad = 0;
+void check(bool ok, const std::string &what) {
+    if (!ok) {
+        std::printf("FAIL %s\n", what.c_str());
+        ++g_bad;
+    }
+}
+
+// Addresses that stand for matrices far apart
+template <class T>
+T *at(int i) {
+    return reinterpret_cast<T *>((uintptr_t(2) << 44) + (uintptr_t(i) << 40));
+}
+
+// A context, and the five operators on matrices of given sizes.
+struct Rig {
+    hwr_ops *ops = nullptr;
+    int dtype = HWR_BF16, n = 0, G = 1, k = 8, m = 8, rank = 4;
+
+    Rig() { check(hwr_ops_init(0, reinterpret_cast<void *>(0x1000), &ops) == HWR_OK, "init"); }
+    ~Rig() { hwr_ops_free(ops); }
+    hwr_groups groups() const { return {n, G, at<int32_t>(0), at<int32_t>(1)}; }
+    hwr_status group() { return hwr_group_rows(ops, n, at<int32_t>(2), nullptr, 0, G, at<int32_t>(0), at<int32_t>(1)); }
+    hwr_status matmul() {
+        const hwr_groups g = groups();
+        const hwr_matmul_args a{dtype, k, m, at<char>(3), 0, at<char>(4), at<char>(5), 0};
+        return hwr_grouped_matmul(ops, &g, &a);
+    }
+    hwr_status matmul_grad(bool dx = true, bool dw = true) {
+        const hwr_groups g = groups();
+        const hwr_matmul_grad_args a{dtype, k, m, at<char>(5), 0, at<char>(3), 0, at<char>(4), dx ? at<char>(6) : nullptr, 0,
+                                     dw ? at<char>(7) : nullptr};
+        return hwr_grouped_matmul_grad(ops, &g, &a);
+    }
+    hwr_status adapter() {
+        const hwr_groups g = groups();
+        const hwr_adapter_args a{dtype, k, m, rank, at<char>(3), 0, at<char>(4), at<char>(8), at<char>(9), nullptr, at<char>(5), 0};
+        return hwr_adapter_matmul(ops, &g, &a);
+    }
+    hwr_status adapter_grad(bool dx = true, bool da = true, bool db = true) {
+        const hwr_groups g = groups();
+        const hwr_adapter_grad_args a{dtype, k, m, rank, at<char>(5), 0, at<char>(3), 0, at<char>(4), at<char>(8), at<char>(9), nullptr,
+                                      dx ? at<char>(6) : nullptr, 0, da ? at<char>(10) : nullptr, db ? at<char>(11) : nullptr};
+        return hwr_adapter_matmul_grad(ops, &g, &a);
+    }
+};
+
+// Places are counted in 32 bits, up to a few tiles past the last: a batch with fewer
+// than 512 rows to 2^31 is refused, and nothing is launched.
+void row_limit() {
+    Rig r;
+    r.k = r.m = 1, r.rank = 1;
+    for (int n : {HWR_OPS_MAX_ROWS + 1, INT32_MAX}) {
+        r.n = n;
+        g_log.clear();
+        check(r.matmul() == HWR_ERR_INVALID_ARG, "matmul of " + std::to_string(n) + " rows");
+        check(r.matmul_grad() == HWR_ERR_INVALID_ARG, "matmul_grad of " + std::to_string(n) + " rows");
+        check(r.adapter() == HWR_ERR_INVALID_ARG, "adapter of " + std::to_string(n) + " rows");
+        check(r.adapter_grad() == HWR_ERR_INVALID_ARG, "adapter_grad of " + std::to_string(n) + " rows");
+        check(g_log.empty(), "nothing launched");
+        check(std::strstr(hwr_ops_last_error(r.ops), "rows") != nullptr, "the message says why");
+    }
+    r.n = HWR_OPS_MAX_ROWS;
+    check(r.matmul() == HWR_OK && r.matmul_grad() == HWR_OK, "the largest batch");
+    r.n = INT32_MAX;
+    check(r.group() == HWR_OK, "rows by group take any number");
+}
+
+struct Scenario {
+    const char *name;
+    void (*run)();
+};
+const Scenario kScenarios[] = {{"row_limit", row_limit}};
+
+}  // namespace
+
+int main(int argc, char **argv) {
+    if (argc != 2) return 2;
+    for (const Scenario &s : kScenarios)
+        if (std::strcmp(argv[1], s.name) == 0) {
+            s.run();
+            std::printf(g_bad ? "%d failed\n" : "ok\n", g_bad);
+            return g_bad ? 1 : 0;
+        }
+    return 2;
+}

@@ -30,9 +30,9 @@
  * [k][m] (adapter), A [G][k][rank], B [G][rank][m]; gradients have the layout of
  * what they belong to.  Rows of x, y, dy and dx may be strided: ldx etc. are the
  * distances of rows in elements, 0 for dense.  Every pointer is device memory
- * and no output overlaps an input.  Any number of rows up to HWR_OPS_MAX_ROWS, any
- * width up to 65536 and any element alignment is accepted; products run fastest
- * where widths, row strides and pointers are multiples of 16 bytes.
+ * and no output overlaps an input.  Any number of rows up to 2^31 - 512 (hwr_group_rows:
+ * 2^31 - 1), any width up to 65536 and any element alignment is accepted; products run
+ * fastest where widths, row strides and pointers are multiples of 16 bytes.
  *
  * Precision.  HWR_BF16 (raw bit patterns) or HWR_F32, one type for every matrix
  * of a call; scale is fp32.  Products accumulate in fp32 and each output is
@@ -75,12 +75,8 @@ const char *hwr_ops_last_error(const hwr_ops *ops);
 /* Work space for later calls: at least `bytes`. */
 hwr_status hwr_ops_reserve(hwr_ops *ops, uint64_t bytes);
 
-/* Rows of a product: places are counted in 32 bits, up to a few tiles past the last.
- * (hwr_group_rows takes any number.) */
-#define HWR_OPS_MAX_ROWS (2147483647 - 511)
-
 typedef struct {
-    int32_t n;                    /* rows, 0..HWR_OPS_MAX_ROWS                  */
+    int32_t n;                    /* rows, 0..2147483136 (2^31 - 512)            */
     int32_t n_groups;             /* G, 1..1024 (as many as pairs)              */
     const int32_t *offsets;       /* [G + 1]                                    */
     const int32_t *order;         /* [n] row at each place, or NULL             */

@@ -29,6 +29,7 @@ thread_local std::string g_ops_error;
 
 constexpr int kMaxWidth = 65536;
 constexpr int kMaxRank = 128;
+constexpr int kMaxRows = INT32_MAX - 511;    // places are counted in 32 bits, up to a few tiles past the last
 constexpr uint64_t kZeroBytes = 256;
 
 hwr_status fail(hwr_ops *c, hwr_status s, const std::string &msg) {
@@ -126,7 +127,7 @@ struct Shape {
 // Null when sound, else what is wrong.
 const char *check_groups(const hwr_groups *g) {
     if (!g) return "groups is NULL";
-    if (g->n < 0 || g->n > HWR_OPS_MAX_ROWS) return "rows outside 0..2147483136";
+    if (g->n < 0 || g->n > kMaxRows) return "rows outside 0..2147483136";
     if (g->n_groups < 1 || g->n_groups > kMaxPairs) return "n_groups outside 1..1024";
     if (!g->offsets) return "offsets is NULL";
     return nullptr;

@@ -138,12 +138,14 @@ struct Rig {
     }
 };
 
+constexpr int kMaxRows = INT32_MAX - 511;
+
 // Places are counted in 32 bits, up to a few tiles past the last: a batch with fewer
 // than 512 rows to 2^31 is refused, and nothing is launched.
 void row_limit() {
     Rig r;
     r.k = r.m = 1, r.rank = 1;
-    for (int n : {HWR_OPS_MAX_ROWS + 1, INT32_MAX}) {
+    for (int n : {kMaxRows + 1, INT32_MAX}) {
         r.n = n;
         g_log.clear();
         check(r.matmul() == HWR_ERR_INVALID_ARG, "matmul of " + std::to_string(n) + " rows");
@@ -153,7 +155,7 @@ void row_limit() {
         check(g_log.empty(), "nothing launched");
         check(std::strstr(hwr_ops_last_error(r.ops), "rows") != nullptr, "the message says why");
     }
-    r.n = HWR_OPS_MAX_ROWS;
+    r.n = kMaxRows;
     check(r.matmul() == HWR_OK && r.matmul_grad() == HWR_OK, "the largest batch");
     r.n = INT32_MAX;
     check(r.group() == HWR_OK, "rows by group take any number");

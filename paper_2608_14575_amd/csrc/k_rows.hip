@@ -141,23 +141,13 @@ __device__ inline void store_rows(const RowsArgs &a, const RowTile &rt, int c0, 
     }
 }
 
-// The workgroup's tile of places, first column and part.  Tiles go in panels of 8 row
-// tiles, column by column, so that the workgroups that run together on one L2
-// share rows and weights.  False past the last tile.
+// The workgroup's tile of places, first column and part.  False past the last tile.
 template <RowsKind KIND, int BM, int BN>
 __device__ inline bool my_tile(const RowsArgs &a, int lane, RowTile &rt, int &c0, int &part) {
     const bool tail = KIND == RowsKind::kGrouped;
     const int tiles = KIND == RowsKind::kAdapter ? (a.g.n + BM - 1) / BM : count_tiles(a.g, BM, tail, lane);
-    const int ct = (a.m + BN - 1) / BN;
-    int item = xcd_item(blockIdx.x, tiles * ct * a.parts);
-    if (item < 0) return false;
-    part = item / (tiles * ct);
-    item -= part * (tiles * ct);
-    const int panel = item / (8 * ct) * 8, in = item - panel * ct, rp = min(8, tiles - panel);
-    const int t = panel + in % rp;
-    // the last tile of columns ends with the row: it shares columns with the one before
-    // (both give them the same bits), and no chunk is cut
-    c0 = a.mw < BN ? 0 : min(in / rp * BN, a.mw - BN);
+    int t;
+    if (!row_item(blockIdx.x, tiles, a.m, a.mw, BN, a.parts, t, c0, part)) return false;
     if (KIND == RowsKind::kAdapter) rt = {0, t * BM, min(t * BM + BM, a.g.n)};
     else rt = find_tile(a.g, t, BM, tail, lane);
     return true;

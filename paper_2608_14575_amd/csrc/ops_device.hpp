@@ -1,6 +1,6 @@
 // Device code shared by the operators on a routed batch: element types and
-// their matrix instruction, staged tiles and their LDS layout, and the walk
-// over ragged groups.
+// their matrix instruction, staged tiles and their LDS layout.  (The walk
+// over ragged groups: ops_groups.hpp.)
 //
 // All products run on 16x16 MFMA with the weights (or the right-hand factor) as
 // the A operand and the rows as the B operand, so that a lane ends up with four
@@ -172,91 +172,6 @@ __device__ inline void store_low(char *block, int c, f32x4 v) {
         *reinterpret_cast<bf16x4 *>(block + c * 2) = hi;
         *reinterpret_cast<bf16x4 *>(block + kLowBytes / 2 + c * 2) = lo;
     }
-}
-
-// ---------------------------------------------------------------- groups
-// offsets as places: clamped to [0, n], so that whatever the array holds stays in bounds
-__device__ inline int place_of(const GroupsArg &g, int i) {
-    const int v = g.offsets[i];
-    return v < 0 ? 0 : v > g.n ? g.n : v;
-}
-
-// Row at place p, or -1.
-__device__ inline int row_at(const GroupsArg &g, int p) {
-    const int r = g.order ? g.order[p] : p;
-    return static_cast<unsigned>(r) < static_cast<unsigned>(g.n) ? r : -1;
-}
-
-// Rows of a tile: places [p0, p1) of group g (g == G: the rows in no group).
-struct RowTile {
-    int g, p0, p1;
-};
-
-// Every group is cut into tiles of bm places.  The tiles of lane i's groups in
-// a block of 64 groups; group G are the rows in no group.
-__device__ inline int lane_tiles(const GroupsArg &g, int i, int bm, bool tail, int &p0, int &p1) {
-    p0 = p1 = 0;
-    if (i < g.G) {
-        p0 = place_of(g, i);
-        p1 = place_of(g, i + 1);
-    } else if (i == g.G && tail) {
-        p0 = place_of(g, i);
-        p1 = g.n;
-    }
-    return p1 > p0 ? (p1 - p0 + bm - 1) / bm : 0;
-}
-
-__device__ inline int wave_scan(int v, int lane) {   // inclusive
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(v, d);
-        if (lane >= d) v += o;
-    }
-    return v;
-}
-
-// Tiles of all groups; one wave.
-__device__ inline int count_tiles(const GroupsArg &g, int bm, bool tail, int lane) {
-    int sum = 0, p0, p1;
-    for (int b = 0; b <= g.G; b += 64) sum += lane_tiles(g, b + lane, bm, tail, p0, p1);
-#pragma unroll
-    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-    return __builtin_amdgcn_readfirstlane(sum);
-}
-
-// Tile t of all groups (t < count_tiles); one wave.
-__device__ inline RowTile find_tile(const GroupsArg &g, int t, int bm, bool tail, int lane) {
-    for (int b = 0; b <= g.G; b += 64) {
-        int p0, p1;
-        const int mine = lane_tiles(g, b + lane, bm, tail, p0, p1);
-        const int upto = wave_scan(mine, lane);
-        const uint64_t hit = __ballot(upto > t);
-        if (hit) {
-            const int l = __builtin_ctzll(hit);
-            const int first = __builtin_amdgcn_readlane(upto - mine, l);
-            const int a = __builtin_amdgcn_readlane(p0, l) + (t - first) * bm, e = __builtin_amdgcn_readlane(p1, l);
-            return {b + l, a, a + bm < e ? a + bm : e};
-        }
-        t -= __builtin_amdgcn_readlane(upto, 63);
-    }
-    return {g.G, 0, 0};
-}
-
-// First group that ends past place p (G if none); one wave.
-__device__ inline int group_of(const GroupsArg &g, int p, int lane) {
-    for (int b = 0; b < g.G; b += 64) {
-        const uint64_t hit = __ballot(b + lane < g.G && place_of(g, b + lane + 1) > p);
-        if (hit) return b + __builtin_ctzll(hit);
-    }
-    return g.G;
-}
-
-// Workgroup id -> work item, so that the items of one of the 8 L2s (ids are
-// dealt out in turn) are neighbours.  Returns -1 past the last item.
-__device__ inline int xcd_item(int id, int items) {
-    const int share = (items + 7) >> 3;
-    const int at = id >> 3, i = (id & 7) * share + at;
-    return at < share && i < items ? i : -1;
 }
 
 // 16 bytes of every lane from memory into LDS, lane after lane from the wave's

@@ -2,6 +2,7 @@
 #pragma once
 
 #include "hwr_internal.hpp"
+#include "ops_groups.hpp"
 
 namespace hwr {
 
@@ -24,11 +25,6 @@ hipError_t launch_pad(bool bf16, const PadArgs &a, hipStream_t s);
 // with hi + lo the value to 16 significant bits.
 constexpr int kRankBlock = 32;
 constexpr int kLowBytes = 128;
-
-struct GroupsArg {
-    int n, G;
-    const int32_t *offsets, *order;   // order may be null
-};
 
 // Products by row: out[r][c] = sum_e x[r][e] w_g(e, c), and for the adapter
 // plus sum_e low[place][e] lw_g(e, c).

@@ -1,6 +1,7 @@
 """The host side of the operators on a routed batch on a stand-in HIP runtime (no
 device): tests/hip_stub/ops_path.cpp defines the HIP functions that they call, runs
-a scenario through the C ABI and checks what was asked of the runtime."""
+a scenario through the C ABI and checks what was asked of the runtime.
+tests/hip_stub/group_walk.cpp runs the kernels' walk over ragged groups lane by lane."""
 import os
 import shutil
 import subprocess
@@ -13,6 +14,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 PKG = os.path.dirname(hwr.LIB_PATH)
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
+
+
+CSRC = os.path.join(PKG, "csrc")
 
 
 @pytest.fixture(scope="module")
@@ -33,4 +37,20 @@ def driver(tmp_path_factory):
 @pytest.mark.parametrize("scenario", ["row_limit"])
 def test_operators_host_side(driver, scenario):
     r = subprocess.run([driver, scenario], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout + r.stderr
+
+
+@pytest.fixture(scope="module")
+def walk(tmp_path_factory):
+    if shutil.which("g++") is None:
+        pytest.skip("g++ not available")
+    exe = str(tmp_path_factory.mktemp("hip_stub") / "group_walk")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-fwrapv", "-Wall", "-Wno-unknown-pragmas", "-I", CSRC,
+                    os.path.join(HERE, "hip_stub", "group_walk.cpp"), "-o", exe], check=True)
+    return exe
+
+
+@pytest.mark.parametrize("scenario", ["tiles_cover_the_places", "anything_in_offsets"])
+def test_walk_over_groups(walk, scenario):
+    r = subprocess.run([walk, scenario], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout + r.stderr

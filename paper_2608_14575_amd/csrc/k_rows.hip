@@ -142,12 +142,12 @@ __device__ inline void store_rows(const RowsArgs &a, const RowTile &rt, int c0, 
 }
 
 // The workgroup's tile of places, first column and part.  False past the last tile.
-template <RowsKind KIND, int BM, int BN>
+template <RowsKind KIND, int BM, int BN, int NT>
 __device__ inline bool my_tile(const RowsArgs &a, int lane, RowTile &rt, int &c0, int &part) {
     const bool tail = KIND == RowsKind::kGrouped;
     const int tiles = KIND == RowsKind::kAdapter ? (a.g.n + BM - 1) / BM : count_tiles(a.g, BM, tail, lane);
     int t;
-    if (!row_item(blockIdx.x, tiles, a.m, a.mw, BN, a.parts, t, c0, part)) return false;
+    if (!row_item(block_id<NT>(), tiles, a.m, a.mw, BN, a.parts, t, c0, part)) return false;
     if (KIND == RowsKind::kAdapter) rt = {0, t * BM, min(t * BM + BM, a.g.n)};
     else rt = find_tile(a.g, t, BM, tail, lane);
     return true;
@@ -172,7 +172,7 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows(RowsArgs a) {
     const int wr = wave / WC, wc = wave % WC;
     RowTile rt;
     int c0, part;
-    if (!my_tile<KIND, BM, BN>(a, lane, rt, c0, part)) return;
+    if (!my_tile<KIND, BM, BN, NT>(a, lane, rt, c0, part)) return;
 
     for (int i = tid; i < BM; i += NT) rows[i] = rt.p0 + i < rt.p1 ? row_at(a.g, rt.p0 + i) : -1;
     __syncthreads();
@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows_direct(RowsArgs a) {
     const int wr = wave / WC, wc = wave % WC;
     RowTile rt;
     int c0, part;
-    if (!my_tile<KIND, BM, BN>(a, lane, rt, c0, part)) return;
+    if (!my_tile<KIND, BM, BN, NT>(a, lane, rt, c0, part)) return;
     for (int i = tid; i < BM; i += NT) rows[i] = rt.p0 + i < rt.p1 ? row_at(a.g, rt.p0 + i) : -1;
     __syncthreads();
 
@@ -332,8 +332,8 @@ hipError_t go(const RowsArgs &a, hipStream_t s) {
     const int64_t tiles = KIND == RowsKind::kAdapter ? (n + BM - 1) / BM : n / BM + (n < a.g.G + 1 ? n : a.g.G + 1);
     const int64_t items = tiles * ((a.m + BN - 1) / BN) * a.parts;
     const int64_t blocks = (items + 7) / 8 * 8;
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
-    const dim3 grid(static_cast<uint32_t>(blocks)), block(WR * WC * 64);
+    if (blocks > INT32_MAX - grid_row(WR * WC * 64)) return hipErrorInvalidValue;
+    const dim3 grid = wide_grid(blocks, WR * WC * 64), block(WR * WC * 64);
     if constexpr (DIRECT) return launch_kernel(k_rows_direct<E, KIND, KS, BM, BN, WR, WC>, grid, block, 0, s, a);
     else return launch_kernel(k_rows<E, KIND, KS, BM, BN, WR, WC>, grid, block, 0, s, a);
 }

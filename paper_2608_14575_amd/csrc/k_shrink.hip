@@ -169,7 +169,7 @@ __device__ inline void shrink_tile(const ShrinkArgs &a, int t, char *lds) {
 template <class E, From FROM, int NF, int RB>
 __global__ void __launch_bounds__(kWaves * 64, (Sizes<E, FROM, NF, RB>::kMinWaves)) k_shrink(ShrinkArgs a) {
     __shared__ __attribute__((aligned(16))) char lds[Sizes<E, FROM, NF, RB>::kLds];
-    shrink_tile<E, FROM, NF, RB>(a, blockIdx.x, lds);
+    shrink_tile<E, FROM, NF, RB>(a, block_id<kWaves * 64>(), lds);
 }
 
 // Two in one launch: the first's tiles take the even workgroups.
@@ -177,17 +177,19 @@ template <class E, From FROM, int NF, int RB>
 __global__ void __launch_bounds__(kWaves * 64, (Sizes<E, FROM, NF, RB>::kMinWaves)) k_shrink_pair(ShrinkArgs a, ShrinkArgs b) {
     constexpr int kA = Sizes<E, From::kDirect, NF, RB>::kLds, kB = Sizes<E, FROM, NF, RB>::kLds;
     __shared__ __attribute__((aligned(16))) char lds[kA > kB ? kA : kB];
-    if (blockIdx.x & 1) shrink_tile<E, FROM, NF, RB>(b, blockIdx.x >> 1, lds);
-    else shrink_tile<E, From::kDirect, NF, RB>(a, blockIdx.x >> 1, lds);
+    const int id = block_id<kWaves * 64>();
+    if (id & 1) shrink_tile<E, FROM, NF, RB>(b, id >> 1, lds);
+    else shrink_tile<E, From::kDirect, NF, RB>(a, id >> 1, lds);
 }
 
 // One (pair null), or with it [rank][k] weights beside `pair`'s [k][rank].
 template <class E, From FROM, int NF, int RB>
 hipError_t go(const ShrinkArgs &a, const ShrinkArgs *pair, hipStream_t s) {
-    const uint32_t tiles = static_cast<uint32_t>(a.g.n / (16 * RB) + (a.g.n < a.g.G ? a.g.n : a.g.G));
+    const int64_t tiles = a.g.n / (16 * RB) + (a.g.n < a.g.G ? a.g.n : a.g.G);
+    constexpr int NT = kWaves * 64;
     if constexpr (FROM != From::kDirect)
-        if (pair) return launch_kernel(k_shrink_pair<E, FROM, NF, RB>, dim3(2 * tiles), dim3(kWaves * 64), 0, s, a, *pair);
-    return launch_kernel(k_shrink<E, FROM, NF, RB>, dim3(tiles), dim3(kWaves * 64), 0, s, a);
+        if (pair) return launch_kernel(k_shrink_pair<E, FROM, NF, RB>, wide_grid(2 * tiles, NT), dim3(NT), 0, s, a, *pair);
+    return launch_kernel(k_shrink<E, FROM, NF, RB>, wide_grid(tiles, NT), dim3(NT), 0, s, a);
 }
 
 template <class E, From FROM, int NF>

@@ -174,6 +174,13 @@ __device__ inline void store_low(char *block, int c, f32x4 v) {
     }
 }
 
+// Number of the workgroup in a wide_grid.  (Rows of a constant length: to read the grid's
+// took 0.2 us at the start of a kernel.)
+template <int THREADS>
+__device__ inline int block_id() {
+    return static_cast<int>(blockIdx.y * static_cast<uint32_t>(grid_row(THREADS)) + blockIdx.x);
+}
+
 // 16 bytes of every lane from memory into LDS, lane after lane from the wave's
 // uniform address on.
 __device__ inline void load_lds(const char *src, char *dst) {

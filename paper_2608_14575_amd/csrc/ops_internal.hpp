@@ -6,6 +6,15 @@
 
 namespace hwr {
 
+// A grid of many workgroups: the runtime takes fewer than 2^32 threads in a dimension, so
+// past this many they go in several rows (block_id numbers them; up to a row too many).
+constexpr int64_t grid_row(int threads) { return ((int64_t{1} << 32) - 1) / threads / 16 * 16; }
+inline dim3 wide_grid(int64_t blocks, int threads) {
+    const int64_t most = grid_row(threads);
+    if (blocks <= most) return dim3(static_cast<uint32_t>(blocks));
+    return dim3(static_cast<uint32_t>(most), static_cast<uint32_t>((blocks + most - 1) / most));
+}
+
 // Copies of matrices with rows padded by zeros to whole, aligned chunks of 16 bytes.
 constexpr int kMaxPads = 3;
 struct PadArgs {

@@ -161,11 +161,31 @@ void row_limit() {
     check(r.group() == HWR_OK, "rows by group take any number");
 }
 
+// The runtime takes no grid of 2^32 threads or more in a dimension (hip_runtime_api.h says so
+// of hipModuleLaunchKernel): the largest batches that memory can hold stay below.
+void largest_grids() {
+    struct Batch {
+        int n, k, m, rank, G;
+    };
+    Rig r;
+    for (const Batch &b : {Batch{1 << 27, 8, 8, 128, 4}, Batch{(1 << 28) + 5, 8, 8, 16, 1}, Batch{kMaxRows, 1, 1, 1, 1},
+                           Batch{kMaxRows, 1, 1, 33, 1024}, Batch{(1 << 29) + 3, 8, 72, 8, 2}, Batch{1 << 30, 8, 64, 8, 1024}})
+        for (int dtype : {HWR_BF16, HWR_F32}) {
+            r.n = b.n, r.k = b.k, r.m = b.m, r.rank = b.rank, r.G = b.G, r.dtype = dtype;
+            g_log.clear();
+            check(r.group() == HWR_OK && r.matmul() == HWR_OK && r.matmul_grad() == HWR_OK && r.adapter() == HWR_OK &&
+                      r.adapter_grad() == HWR_OK && r.adapter_grad(true, false, false) == HWR_OK, "queued");
+            for (const Launch &l : g_log)
+                check(static_cast<uint64_t>(l.grid.x) * l.block.x < uint64_t(1) << 32 && l.grid.y <= 65535 && l.grid.z == 1,
+                      std::to_string(b.n) + " rows: " + std::to_string(l.grid.x) + " x " + std::to_string(l.block.x) + " of " + l.kernel);
+        }
+}
+
 struct Scenario {
     const char *name;
     void (*run)();
 };
-const Scenario kScenarios[] = {{"row_limit", row_limit}};
+const Scenario kScenarios[] = {{"row_limit", row_limit}, {"largest_grids", largest_grids}};
 
 }  // namespace
 

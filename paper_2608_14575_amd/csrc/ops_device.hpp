@@ -156,18 +156,21 @@ __device__ inline f32x4 column(const u32x4 (&in)[4], int j) {
     return f32x4{__uint_as_float(in[0][j]), __uint_as_float(in[1][j]), __uint_as_float(in[2][j]), __uint_as_float(in[3][j])};
 }
 
-// Four values of a low-rank intermediate, at column c of its 128-byte block.
+// Four values of a low-rank intermediate, at column c of its 128-byte block.  (A finite value
+// whose high part would round to an infinity has the largest bf16 there: the low part holds
+// the rest.)
 template <class E>
 __device__ inline void store_low(char *block, int c, f32x4 v) {
     if constexpr (sizeof(E) == 4) {
         *reinterpret_cast<f32x4 *>(block + c * 4) = v;
     } else {
+        constexpr float kTop = 0x1.FEp127f;
         bf16x4 hi, lo;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            hi[e] = static_cast<__bf16>(v[e]);
-            const float h = static_cast<float>(hi[e]);
-            lo[e] = static_cast<__bf16>(__builtin_isfinite(h) ? v[e] - h : 0.0f);
+            const float inner = __builtin_isfinite(v[e]) ? fminf(fmaxf(v[e], -kTop), kTop) : v[e];
+            hi[e] = static_cast<__bf16>(inner);
+            lo[e] = static_cast<__bf16>(__builtin_isfinite(v[e]) ? v[e] - static_cast<float>(hi[e]) : 0.0f);
         }
         *reinterpret_cast<bf16x4 *>(block + c * 2) = hi;
         *reinterpret_cast<bf16x4 *>(block + kLowBytes / 2 + c * 2) = lo;

@@ -1,5 +1,5 @@
 """More of the operators on a routed batch (include/hwr_ops.h): batches of up to 2^31
-rows.
+rows, and intermediates near the largest values.
 
 Tolerances: inputs whose products and sums are whole numbers below 2^24 give exact
 sums in fp32, in any order, so that a bf16 result is off by its rounding alone (2^-8
@@ -93,3 +93,45 @@ def test_adapters_of_2_27_rows(ops):
         assert both > 2 ** 18
         for got, want in ((da[g], float(b[g]) * both), (db[g], float(a[g]) * both)):
             assert abs(float(got) - want) <= 2.0 ** -8 * want
+
+
+# ---------------------------------------------------------------- the largest values
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("n", [8, 300])
+def test_intermediates_past_the_largest_bf16(ops, n, sign):
+    """A low-rank intermediate that fp32 holds and bf16 rounds to an infinity: what is
+    made of it is finite, of few rows and of many.  In bf16 calls the intermediate is a sum of
+    two bf16 values, exact here (2^-8: the rounding of the result)."""
+    t, k, m, R, top = torch.bfloat16, 16, 24, 4, (2 - 2 ** -7) * 2.0 ** 127
+    v = sign * (top + 1.75 * 2.0 ** 119)
+    assert torch.tensor(v).isfinite() and torch.tensor(v).to(t).isinf()
+    zeros = lambda *s: torch.zeros(s, dtype=t, device="cuda")  # noqa: E731
+    off = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    big = torch.tensor([top, 1.75 * 2.0 ** 119], dtype=t, device="cuda") * sign
+
+    def near(got, want):
+        assert (got.double() - want).abs().max() <= 2.0 ** -8 * abs(want), (got, want)
+
+    # s x A of row 1, column 2 is v
+    x, w, a, b = zeros(n, k), zeros(k, m), zeros(1, k, R), zeros(1, R, m)
+    x[1, :2] = 1
+    a[0, :2, 2] = big
+    b[0, 2] = 2.0 ** -10
+    y = torch.full((n, m), 7.0, dtype=t, device="cuda")
+    ops.adapter(x, w, a, b, None, off, y=y)
+    near(y[1], v * 2.0 ** -10)
+    assert not y[0].any() and not y[2:].any()
+    dy, db = zeros(n, m), torch.empty_like(b)
+    dy[1] = 2.0 ** -9
+    ops.adapter_grad(dy, x, w, a, b, None, off, db=db)
+    near(db[0, 2], v * 2.0 ** -9)
+    # u of row 1, column 2 is v
+    x, dy, a, b = zeros(n, k), zeros(n, m), zeros(1, k, R), zeros(1, R, m)
+    dy[1, :2] = 1
+    b[0, 2, :2] = big
+    a[0, :, 2] = 2.0 ** -10
+    x[1] = 2.0 ** -9
+    dx, da = torch.empty_like(x), torch.empty_like(a)
+    ops.adapter_grad(dy, x, w, a, b, None, off, dx=dx, da=da)
+    near(dx[1], v * 2.0 ** -10)
+    near(da[0, :, 2], v * 2.0 ** -9)

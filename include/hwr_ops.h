@@ -45,9 +45,10 @@
  * Every call is queued on the context's stream and returns without waiting.
  * Inputs written and outputs read on another stream have to be ordered against
  * it by the caller.  Work space belongs to the context: a call that needs more
- * than it has allocates (and keeps what it had until hwr_ops_free, so that
- * captured graphs stay valid); under stream capture it is HWR_ERR_STATE instead:
- * make the call once outside, or hwr_ops_reserve, before capturing.  A context is not
+ * than it has allocates, before it queues anything (and keeps what it had until
+ * hwr_ops_free, so that captured graphs stay valid); under stream capture it is
+ * HWR_ERR_STATE instead, with nothing recorded: make the call once outside, or reserve
+ * what the message names (hwr_ops_reserve), before capturing.  A context is not
  * thread-safe.  Sizes and pointers are checked; the contents of offsets, order,
  * choice and table are not: values out of range give unspecified results, and
  * all memory accesses stay in bounds.

@@ -2,6 +2,7 @@
 // space and launches.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstring>
 #include <string>
 #include <vector>
@@ -169,28 +170,32 @@ class Pads {
         slots_[args_.count] = {src, ld};
         args_.m[args_.count++] = m;
     }
-    // Where copies are worth their time for products of so many operations: makes them
-    // past the first *used bytes of the work space (and counts them in), leaves their
-    // addresses and row strides where the matrices' were, and sets *padded.  A copy is a
+    // Whether copies are worth their time for products of so many operations.  If so they lie
+    // past the first *used bytes of the work space (and are counted in), and the matrices' row
+    // strides become theirs, their addresses distances from the work space's start.  A copy is a
     // pass over the matrix (3.5 TB/s, 3 us to launch); without it operands pass through
     // registers, which takes about twice the time of the products at their ordinary rate,
     // and more where a weight gradient is among them.  (bf16, us with / without copies: adapter
     // 15,945 x 1176 x 1046 121.9 / 134.9, 8,413 x 1385 x 320 53.8 / 47.4; grouped gradients 5,198 x 427 x
     // 1058 in 20 groups 58.9 / 72.4, 116 x 1061 x 278 in 32 groups 44.8 / 31.8.)
-    hwr_status copy(hwr_ops *c, double flops, bool gradients, uint64_t *used, bool *padded) {
+    bool plan(double flops, bool gradients, uint64_t *used) {
         const double rate = (bf16_ ? 6e14 : 8e13) / (gradients ? 2 : 1);
-        *padded = all_ > 0 && all_ / 1.75e12 + 3e-6 < flops / rate;
-        if (!*padded || args_.count == 0) return HWR_OK;
-        char *at = nullptr;
-        if (hwr_status st = workspace(c, *used + bytes(), &at)) return st;
-        at += *used;
-        *used += bytes();
-        for (int i = 0; i < args_.count; ++i) {
-            args_.m[i].dst = at;
-            *slots_[i].src = at;
-            *slots_[i].ld = padded_width(bf16_, args_.m[i].width);
-            at += size(args_.m[i]);
+        if (all_ == 0 || all_ / 1.75e12 + 3e-6 >= flops / rate) {
+            args_.count = 0;
+            return false;
         }
+        for (int i = 0; i < args_.count; ++i) {
+            at_[i] = *used;
+            *used += size(args_.m[i]);
+            *slots_[i].src = reinterpret_cast<const void *>(at_[i]);
+            *slots_[i].ld = padded_width(bf16_, args_.m[i].width);
+        }
+        return true;
+    }
+    // Makes the copies that were planned; the matrices' addresses become theirs.
+    hwr_status copy(hwr_ops *c, char *ws) {
+        if (args_.count == 0) return HWR_OK;
+        for (int i = 0; i < args_.count; ++i) *slots_[i].src = args_.m[i].dst = ws + at_[i];
         OPS_HIP(c, launch_pad(bf16_, args_, c->stream));
         return HWR_OK;
     }
@@ -200,11 +205,6 @@ class Pads {
         const void **src;
         int64_t *ld;
     };
-    uint64_t bytes() const {
-        uint64_t b = 0;
-        for (int i = 0; i < args_.count; ++i) b += size(args_.m[i]);
-        return b;
-    }
     uint64_t size(const PadArgs::Matrix &m) const {
         return (static_cast<uint64_t>(m.rows) * padded_width(bf16_, m.width) * (bf16_ ? 2 : 4) + 255) / 256 * 256;
     }
@@ -212,6 +212,7 @@ class Pads {
     uint64_t all_ = 0;
     PadArgs args_;
     Slot slots_[kMaxPads];
+    uint64_t at_[kMaxPads];
 };
 
 // A product by row: w has `lines` rows of `ldw` elements a group, or one group for all rows (shared).
@@ -238,13 +239,10 @@ uint64_t rows_bytes(hwr_ops *c, bool bf16, RowsKind kind, bool ks, const RowsArg
     const int parts = rows_plan(bf16, kind, ks, r, c->cus).parts;
     return parts > 1 ? static_cast<uint64_t>(parts) * r.g.n * r.m_pad * sizeof(float) : 0;
 }
-// With its partial sums past the first `used` bytes of the work space.  (A block that has
-// to be larger leaves the one before as it is, so what lies there stays.)
-hwr_status rows(hwr_ops *c, bool bf16, RowsKind kind, bool ks, RowsArgs r, uint64_t used) {
-    char *ws = nullptr;
-    if (hwr_status st = workspace(c, used + rows_bytes(c, bf16, kind, ks, r), &ws)) return st;
+// With its partial sums (rows_bytes) at `partial`.
+hwr_status rows(hwr_ops *c, bool bf16, RowsKind kind, bool ks, RowsArgs r, char *partial) {
     r.parts = rows_plan(bf16, kind, ks, r, c->cus).parts;
-    r.partial = reinterpret_cast<float *>(ws + used);
+    r.partial = reinterpret_cast<float *>(partial);
     OPS_HIP(c, launch_rows(bf16, kind, ks, r, c->cus, c->stream));
     if (r.parts == 1) return HWR_OK;
     FewArgs f{};
@@ -259,16 +257,14 @@ hwr_status rows(hwr_ops *c, bool bf16, RowsKind kind, bool ks, RowsArgs r, uint6
     return HWR_OK;
 }
 
-// out[g] = P^T Q, with the partial sums past the first `used` bytes of the work space.
+// out[g] = P^T Q, with its partial sums (weight_grad_bytes) at `partial`.
 uint64_t weight_grad_bytes(hwr_ops *c, bool bf16, ColsKind kind, const ColsArgs &w) {
     const int parts = cols_plan(bf16, kind, w, c->cus).parts;
     return parts > 1 ? static_cast<uint64_t>(parts) * w.g.G * w.np * w.nq * sizeof(float) : 0;
 }
-hwr_status weight_grad(hwr_ops *c, bool bf16, ColsKind kind, ColsArgs w, uint64_t used) {
-    char *ws = nullptr;
-    if (hwr_status st = workspace(c, used + weight_grad_bytes(c, bf16, kind, w), &ws)) return st;
+hwr_status weight_grad(hwr_ops *c, bool bf16, ColsKind kind, ColsArgs w, char *partial) {
     w.parts = cols_plan(bf16, kind, w, c->cus).parts;
-    w.partial = reinterpret_cast<float *>(ws + used);
+    w.partial = reinterpret_cast<float *>(partial);
     w.zeros = c->zeros;
     OPS_HIP(c, launch_cols(bf16, kind, w, c->cus, c->stream));
     return HWR_OK;
@@ -340,13 +336,17 @@ hwr_status grouped_matmul(hwr_ops *c, const hwr_groups *g, const hwr_matmul_args
     const void *x = a->x, *w = a->w;
     int64_t ldx = dense(a->ldx, a->k), ldw = a->m;
     uint64_t used = 0;
-    bool padded = false;
     Pads pads(bf16);
     pads.add(&x, &ldx, g->n, a->k);
     pads.add(&w, &ldw, static_cast<int64_t>(g->n_groups) * a->k, a->m);
-    if (hwr_status st = pads.copy(c, 2.0 * g->n * a->k * a->m, false, &used, &padded)) return st;
-    return rows(c, bf16, RowsKind::kGrouped, true,
-                rows_args(c, g, true, padded, x, ldx, a->k, w, ldw, a->k, false, a->m, a->y, dense(a->ldy, a->m)), used);
+    const bool padded = pads.plan(2.0 * g->n * a->k * a->m, false, &used);
+    RowsArgs r = rows_args(c, g, true, padded, x, ldx, a->k, w, ldw, a->k, false, a->m, a->y, dense(a->ldy, a->m));
+    char *ws = nullptr;
+    if (hwr_status st = workspace(c, used + rows_bytes(c, bf16, RowsKind::kGrouped, true, r), &ws)) return st;
+    if (hwr_status st = pads.copy(c, ws)) return st;
+    r.x = x;
+    r.w = w;
+    return rows(c, bf16, RowsKind::kGrouped, true, r, ws + used);
 }
 
 hwr_status grouped_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_matmul_grad_args *a) {
@@ -364,30 +364,35 @@ hwr_status grouped_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_matmul
     const void *dy = a->dy, *x = a->x, *w = a->w;
     int64_t lddy = dense(a->lddy, a->m), ldx = dense(a->ldx, a->k), ldw = a->m;
     uint64_t used = 0;
-    bool padded = false;
     Pads pads(bf16);
     pads.add(&dy, &lddy, g->n, a->m);
     pads.add(&w, &ldw, static_cast<int64_t>(g->n_groups) * a->k, a->m, a->dx != nullptr);
     pads.add(&x, &ldx, g->n, a->k, a->dw != nullptr);
-    if (hwr_status st = pads.copy(c, 4.0 * g->n * a->k * a->m, true, &used, &padded)) return st;
-    if (a->dx && g->n > 0) {
-        const RowsArgs r =
-            rows_args(c, g, false, padded, dy, lddy, a->m, w, ldw, a->k, false, a->k, a->dx, dense(a->lddx, a->k));
-        if (hwr_status st = rows(c, bf16, RowsKind::kGrouped, false, r, used)) return st;
-    }
-    if (a->dw) {
-        ColsArgs d{};
-        d.g = groups_arg(g);
-        d.np = a->k;
-        d.nq = a->m;
-        d.padded = padded;
-        d.p = x;
-        d.q = dy;
-        d.ldp = ldx;
-        d.ldq = lddy;
-        d.out = a->dw;
-        if (hwr_status st = weight_grad(c, bf16, ColsKind::kDense, d, used)) return st;
-    }
+    const bool padded = pads.plan(4.0 * g->n * a->k * a->m, true, &used), dx = a->dx && g->n > 0;
+    RowsArgs r = rows_args(c, g, false, padded, dy, lddy, a->m, w, ldw, a->k, false, a->k, a->dx, dense(a->lddx, a->k));
+    ColsArgs d{};
+    d.g = groups_arg(g);
+    d.np = a->k;
+    d.nq = a->m;
+    d.padded = padded;
+    d.p = x;
+    d.q = dy;
+    d.ldp = ldx;
+    d.ldq = lddy;
+    d.out = a->dw;
+    // (one after the other: they share the place of their partial sums)
+    const uint64_t sums = std::max(dx ? rows_bytes(c, bf16, RowsKind::kGrouped, false, r) : 0,
+                                   a->dw ? weight_grad_bytes(c, bf16, ColsKind::kDense, d) : 0);
+    char *ws = nullptr;
+    if (hwr_status st = workspace(c, used + sums, &ws)) return st;
+    if (hwr_status st = pads.copy(c, ws)) return st;
+    r.x = d.q = dy;
+    r.w = w;
+    d.p = x;
+    if (dx)
+        if (hwr_status st = rows(c, bf16, RowsKind::kGrouped, false, r, ws + used)) return st;
+    if (a->dw)
+        if (hwr_status st = weight_grad(c, bf16, ColsKind::kDense, d, ws + used)) return st;
     return HWR_OK;
 }
 
@@ -422,22 +427,24 @@ hwr_status adapter_matmul(hwr_ops *c, const hwr_groups *g, const hwr_adapter_arg
     }
     const bool bf16 = a->dtype == HWR_BF16;
     uint64_t used = low_bytes(g->n, a->rank);
-    char *low = nullptr;
-    if (hwr_status st = workspace(c, used, &low)) return st;
-    const ShrinkArgs to_low{groups_arg(g), a->k, a->rank, a->x, ldx, a->a, a->scale, low};
-    OPS_HIP(c, launch_shrink(bf16, true, to_low, c->cus, c->stream));
     const void *x = a->x, *w = a->w;
     int64_t ldxp = ldx, ldw = a->m;
-    bool padded = false;
     Pads pads(bf16);
     pads.add(&x, &ldxp, g->n, a->k);
     pads.add(&w, &ldw, a->k, a->m);
-    if (hwr_status st = pads.copy(c, 2.0 * g->n * a->k * a->m, false, &used, &padded)) return st;
+    const bool padded = pads.plan(2.0 * g->n * a->k * a->m, false, &used);
     RowsArgs r = rows_args(c, g, true, padded, x, ldxp, a->k, w, ldw, a->k, true, a->m, a->y, dense(a->ldy, a->m));
-    r.low = low;
     r.lw = a->b;
     r.rank = a->rank;
-    return rows(c, bf16, RowsKind::kAdapter, true, r, used);
+    char *ws = nullptr;
+    if (hwr_status st = workspace(c, used + rows_bytes(c, bf16, RowsKind::kAdapter, true, r), &ws)) return st;
+    const ShrinkArgs to_low{groups_arg(g), a->k, a->rank, a->x, ldx, a->a, a->scale, ws};
+    OPS_HIP(c, launch_shrink(bf16, true, to_low, c->cus, c->stream));
+    if (hwr_status st = pads.copy(c, ws)) return st;
+    r.x = x;
+    r.w = w;
+    r.low = ws;
+    return rows(c, bf16, RowsKind::kAdapter, true, r, ws + used);
 }
 
 hwr_status adapter_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_adapter_grad_args *a) {
@@ -458,31 +465,16 @@ hwr_status adapter_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_adapte
     const int64_t lddy = dense(a->lddy, a->m), ldx = dense(a->ldx, a->k);
     const uint64_t each = low_bytes(g->n, a->rank);
     uint64_t used = 2 * each;
-    char *up = nullptr;
-    if (hwr_status st = workspace(c, used, &up)) return st;
-    char *low = up + each;
-    const ShrinkArgs to_up{groups_arg(g), a->m, a->rank, a->dy, lddy, a->b, a->scale, up};
-    const ShrinkArgs to_low{groups_arg(g), a->k, a->rank, a->x, ldx, a->a, a->scale, low};
-    if (g->n > 0) {
-        if ((a->dx || a->da) && a->db) OPS_HIP(c, launch_shrink_pair(bf16, to_up, to_low, c->cus, c->stream));
-        else if (a->dx || a->da) OPS_HIP(c, launch_shrink(bf16, false, to_up, c->cus, c->stream));
-        else if (a->db) OPS_HIP(c, launch_shrink(bf16, true, to_low, c->cus, c->stream));
-    }
     const void *dy = a->dy, *x = a->x, *w = a->w;
     int64_t lddyp = lddy, ldxp = ldx, ldw = a->m;
-    bool padded = false;
     Pads pads(bf16);
     pads.add(&dy, &lddyp, g->n, a->m, a->dx || a->db);
     pads.add(&w, &ldw, a->k, a->m, a->dx != nullptr);
     pads.add(&x, &ldxp, g->n, a->k, a->da != nullptr);
-    if (hwr_status st = pads.copy(c, 2.0 * g->n * a->k * a->m, true, &used, &padded)) return st;
-    if (g->n > 0 && a->dx) {
-        RowsArgs r = rows_args(c, g, false, padded, dy, lddyp, a->m, w, ldw, a->k, true, a->k, a->dx, dense(a->lddx, a->k));
-        r.low = up;
-        r.lw = a->a;
-        r.rank = a->rank;
-        if (hwr_status st = rows(c, bf16, RowsKind::kAdapter, false, r, used)) return st;
-    }
+    const bool padded = pads.plan(2.0 * g->n * a->k * a->m, true, &used), dx = a->dx && g->n > 0;
+    RowsArgs r = rows_args(c, g, false, padded, dy, lddyp, a->m, w, ldw, a->k, true, a->k, a->dx, dense(a->lddx, a->k));
+    r.lw = a->a;
+    r.rank = a->rank;
     ColsArgs da{}, db{};
     da.g = db.g = groups_arg(g);
     da.padded = db.padded = padded;
@@ -491,30 +483,51 @@ hwr_status adapter_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_adapte
     da.nq = a->rank;
     da.p = x;
     da.ldp = ldxp;
-    da.q = up;
     da.out = a->da;
     db.np = a->rank;
     db.nq = a->m;
-    db.p = low;
     db.q = dy;
     db.ldq = lddyp;
     db.out = a->db;
-    if (a->da && a->db && cols_plan(bf16, ColsKind::kLowQ, da, c->cus).direct && cols_plan(bf16, ColsKind::kLowP, db, c->cus).direct) {
-        const uint64_t first = weight_grad_bytes(c, bf16, ColsKind::kLowQ, da);
-        char *ws = nullptr;
-        if (hwr_status st = workspace(c, used + first + weight_grad_bytes(c, bf16, ColsKind::kLowP, db), &ws)) return st;
+    // dx, then dA and dB together where both are direct, else one after the other: what
+    // runs after another shares the place of its partial sums
+    const bool pair = a->da && a->db && cols_plan(bf16, ColsKind::kLowQ, da, c->cus).direct &&
+                      cols_plan(bf16, ColsKind::kLowP, db, c->cus).direct;
+    const uint64_t da_sums = a->da ? weight_grad_bytes(c, bf16, ColsKind::kLowQ, da) : 0,
+                   db_sums = a->db ? weight_grad_bytes(c, bf16, ColsKind::kLowP, db) : 0;
+    const uint64_t sums = std::max(dx ? rows_bytes(c, bf16, RowsKind::kAdapter, false, r) : 0,
+                                   pair ? da_sums + db_sums : std::max(da_sums, db_sums));
+    char *ws = nullptr;
+    if (hwr_status st = workspace(c, used + sums, &ws)) return st;
+    char *up = ws, *low = ws + each, *partial = ws + used;
+    const ShrinkArgs to_up{groups_arg(g), a->m, a->rank, a->dy, lddy, a->b, a->scale, up};
+    const ShrinkArgs to_low{groups_arg(g), a->k, a->rank, a->x, ldx, a->a, a->scale, low};
+    if (g->n > 0) {
+        if ((a->dx || a->da) && a->db) OPS_HIP(c, launch_shrink_pair(bf16, to_up, to_low, c->cus, c->stream));
+        else if (a->dx || a->da) OPS_HIP(c, launch_shrink(bf16, false, to_up, c->cus, c->stream));
+        else if (a->db) OPS_HIP(c, launch_shrink(bf16, true, to_low, c->cus, c->stream));
+    }
+    if (hwr_status st = pads.copy(c, ws)) return st;
+    r.x = db.q = dy;
+    r.w = w;
+    r.low = da.q = up;
+    da.p = x;
+    db.p = low;
+    if (dx)
+        if (hwr_status st = rows(c, bf16, RowsKind::kAdapter, false, r, partial)) return st;
+    if (pair) {
         da.parts = cols_plan(bf16, ColsKind::kLowQ, da, c->cus).parts;
         db.parts = cols_plan(bf16, ColsKind::kLowP, db, c->cus).parts;
-        da.partial = reinterpret_cast<float *>(ws + used);
-        db.partial = reinterpret_cast<float *>(ws + used + first);
+        da.partial = reinterpret_cast<float *>(partial);
+        db.partial = reinterpret_cast<float *>(partial + da_sums);
         da.zeros = db.zeros = c->zeros;
         OPS_HIP(c, launch_cols_low_pair(bf16, da, db, c->stream));
         return HWR_OK;
     }
     if (a->da)
-        if (hwr_status st = weight_grad(c, bf16, ColsKind::kLowQ, da, used)) return st;
+        if (hwr_status st = weight_grad(c, bf16, ColsKind::kLowQ, da, partial)) return st;
     if (a->db)
-        if (hwr_status st = weight_grad(c, bf16, ColsKind::kLowP, db, used)) return st;
+        if (hwr_status st = weight_grad(c, bf16, ColsKind::kLowP, db, partial)) return st;
     return HWR_OK;
 }
 

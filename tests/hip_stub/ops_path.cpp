@@ -8,6 +8,7 @@
 
 #include <cstdint>
 #include <cstdio>
+#include <cstdlib>
 #include <cstring>
 #include <map>
 #include <string>
@@ -28,6 +29,9 @@ std::map<const void *, std::string> &kernels() {      // registered before main
 }
 std::map<uintptr_t, size_t> g_mem;
 uintptr_t g_next = uintptr_t(1) << 40;
+int g_mallocs = 0;
+size_t g_fail = SIZE_MAX;         // allocations of this many bytes or more fail
+bool g_capturing = false;
 dim3 g_grid, g_block;
 size_t g_shm;
 hipStream_t g_stream;
@@ -62,6 +66,8 @@ hipError_t hipExtLaunchKernel(const void *f, dim3 grid, dim3 block, void **, siz
     return launch(f, grid, block);
 }
 hipError_t hipMalloc(void **p, size_t n) {
+    ++g_mallocs;
+    if (n >= g_fail) return hipErrorOutOfMemory;
     g_mem[g_next] = n;
     *p = reinterpret_cast<void *>(g_next);
     g_next += (n + 4095) / 4096 * 4096 + 4096;
@@ -86,7 +92,10 @@ const char *hipGetErrorName(hipError_t) { return "error"; }
 const char *hipGetErrorString(hipError_t) { return "injected"; }
 hipError_t hipGetLastError() { return hipSuccess; }
 hipError_t hipStreamSynchronize(hipStream_t) { return hipSuccess; }
-hipError_t hipStreamIsCapturing(hipStream_t, hipStreamCaptureStatus *c) { return *c = hipStreamCaptureStatusNone, hipSuccess; }
+hipError_t hipStreamIsCapturing(hipStream_t, hipStreamCaptureStatus *c) {
+    *c = g_capturing ? hipStreamCaptureStatusActive : hipStreamCaptureStatusNone;
+    return hipSuccess;
+}
 }
 
 namespace {
@@ -181,11 +190,68 @@ void largest_grids() {
         }
 }
 
+// A call has all of its work space before it queues anything: where it cannot, nothing is
+// queued, and reserving what the refusal asks for is enough.
+void work_space() {
+    struct Batch {
+        int n, k, m, rank, G;
+    };
+    struct Call {
+        const char *name;
+        hwr_status (*make)(Rig &);
+    };
+    const Call calls[] = {{"group", [](Rig &r) { return r.group(); }},
+                          {"matmul", [](Rig &r) { return r.matmul(); }},
+                          {"matmul_grad", [](Rig &r) { return r.matmul_grad(); }},
+                          {"matmul_grad dw", [](Rig &r) { return r.matmul_grad(false, true); }},
+                          {"adapter", [](Rig &r) { return r.adapter(); }},
+                          {"adapter_grad", [](Rig &r) { return r.adapter_grad(); }},
+                          {"adapter_grad dx", [](Rig &r) { return r.adapter_grad(true, false, false); }},
+                          {"adapter_grad db", [](Rig &r) { return r.adapter_grad(false, false, true); }}};
+    int needed = 0;
+    for (const Batch &b : {Batch{16000, 1001, 1003, 16, 3}, Batch{400, 4104, 4096, 16, 2}, Batch{300, 1601, 523, 100, 1},
+                           Batch{40, 4096, 4096, 16, 32}, Batch{9000, 1024, 2048, 32, 4}, Batch{100000, 40, 24, 4, 1000}})
+        for (int dtype : {HWR_BF16, HWR_F32})
+            for (const Call &c : calls) {
+                const std::string what = std::string(c.name) + " of " + std::to_string(b.n) + (dtype == HWR_BF16 ? " bf16" : " fp32");
+                Rig r;
+                r.n = b.n, r.k = b.k, r.m = b.m, r.rank = b.rank, r.G = b.G, r.dtype = dtype;
+                g_log.clear();
+                g_capturing = true;
+                const hwr_status first = c.make(r);
+                if (first == HWR_OK) {
+                    g_capturing = false;
+                    continue;                                  // takes none
+                }
+                ++needed;
+                check(first == HWR_ERR_STATE && g_log.empty(), what + ": " + std::to_string(g_log.size()) + " launches recorded, then refused");
+                const char *ask = std::strstr(hwr_ops_last_error(r.ops), "hwr_ops_reserve ");
+                const unsigned long long bytes = ask ? std::strtoull(ask + 16, nullptr, 10) : 0;
+                g_capturing = false;
+                check(bytes > 0 && hwr_ops_reserve(r.ops, bytes) == HWR_OK, what + ": reserve");
+                g_capturing = true;
+                check(c.make(r) == HWR_OK, what + ": what was asked for is enough");
+                g_capturing = false;
+                // a context of its own: one allocation; and none to be had
+                Rig s;
+                s.n = b.n, s.k = b.k, s.m = b.m, s.rank = b.rank, s.G = b.G, s.dtype = dtype;
+                g_log.clear();
+                g_fail = 1;
+                check(c.make(s) == HWR_ERR_OOM && g_log.empty(), what + ": no memory, nothing queued");
+                g_fail = SIZE_MAX;
+                g_mallocs = 0;
+                check(c.make(s) == HWR_OK && g_mallocs == 1, what + ": " + std::to_string(g_mallocs) + " allocations");
+                g_mallocs = 0;
+                check(c.make(s) == HWR_OK && g_mallocs == 0, what + ": once");
+            }
+    check(needed > 50, std::to_string(needed) + " calls took work space");
+}
+
 struct Scenario {
     const char *name;
     void (*run)();
 };
-const Scenario kScenarios[] = {{"row_limit", row_limit}, {"largest_grids", largest_grids}};
+const Scenario kScenarios[] = {{"row_limit", row_limit}, {"largest_grids", largest_grids}, {"work_space", work_space}};
 
 }  // namespace
 

@@ -42,7 +42,8 @@
  * the same bits.  An infinity or a NaN stays in the rows (and groups) that it
  * belongs to.
  *
- * Every call is queued on the context's stream and returns without waiting.
+ * Every call is queued on the context's stream and returns without waiting; the
+ * calling thread's current device is left as it was.
  * Inputs written and outputs read on another stream have to be ordered against
  * it by the caller.  Work space belongs to the context: a call that needs more
  * than it has allocates, before it queues anything (and keeps what it had until

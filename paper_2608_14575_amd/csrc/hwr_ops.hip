@@ -56,12 +56,31 @@ void release(hwr_ops *c) {
     delete c;
 }
 
-hwr_status use_device(hwr_ops *c) {
-    int dev = -1;
-    OPS_HIP(c, hipGetDevice(&dev));
-    if (dev != c->dev) OPS_HIP(c, hipSetDevice(c->dev));
-    return HWR_OK;
-}
+// Makes a device current for a scope; the caller's is current again after it.
+class OnDevice {
+  public:
+    explicit OnDevice(int dev) {
+        error = hipGetDevice(&before_);
+        if (error == hipSuccess && before_ != dev) {
+            error = hipSetDevice(dev);
+            changed_ = error == hipSuccess;
+        }
+    }
+    ~OnDevice() {
+        if (changed_) (void)hipSetDevice(before_);
+    }
+    OnDevice(const OnDevice &) = delete;
+    OnDevice &operator=(const OnDevice &) = delete;
+    hipError_t error;
+
+  private:
+    int before_ = 0;
+    bool changed_ = false;
+};
+
+#define OPS_ON_DEVICE(ctx, dev)    \
+    const OnDevice on_device(dev); \
+    if (on_device.error != hipSuccess) return hip_fail((ctx), on_device.error, "hipSetDevice")
 
 // At least `bytes` of work space at *out.
 hwr_status workspace(hwr_ops *c, uint64_t bytes, char **out) {
@@ -104,7 +123,7 @@ hwr_status init_impl(int32_t device, void *stream, hwr_ops **out) {
         return fail(nullptr, HWR_ERR_HIP, "hipGetDeviceProperties failed");
     if (std::strncmp(prop.gcnArchName, "gfx950", 6) != 0)
         return fail(nullptr, HWR_ERR_UNSUPPORTED, std::string("library is built for gfx950, device is ") + prop.gcnArchName);
-    OPS_HIP(nullptr, hipSetDevice(device));
+    OPS_ON_DEVICE(nullptr, device);
     hwr_ops *c = new hwr_ops();
     c->dev = device;
     c->cus = prop.multiProcessorCount;
@@ -296,7 +315,7 @@ hwr_status group_rows(hwr_ops *c, int32_t n, const int32_t *choice, const int32_
     if (!offsets || (n > 0 && (!choice || !order))) return invalid(c, "choice, offsets and order are required");
     if (table ? n_table < 1 : n_table != 0) return invalid(c, "n_table must be > 0 with a table and 0 without");
     if (misaligned(HWR_F32, {choice, table, offsets, order})) return invalid(c, "a pointer is not aligned to its elements");
-    if (hwr_status st = use_device(c)) return st;
+    OPS_ON_DEVICE(c, c->dev);
     GroupRowsArgs a{n, n_table, n_groups, choice, table, offsets, order, group_rows_blocks(n), nullptr, nullptr};
     if (a.blocks > 1) {
         const uint64_t counts = static_cast<uint64_t>(n_groups + 1) * a.blocks;
@@ -318,7 +337,7 @@ hwr_status grouped_matmul(hwr_ops *c, const hwr_groups *g, const hwr_matmul_args
     if (g->n == 0) return HWR_OK;
     if (!a->x || !a->w || !a->y) return invalid(c, "x, w and y are required");
     if (misaligned(a->dtype, {a->x, a->w, a->y})) return invalid(c, "a pointer is not aligned to its elements");
-    if (hwr_status st = use_device(c)) return st;
+    OPS_ON_DEVICE(c, c->dev);
     if (few_rows(g->n, g->n_groups, a->k, a->m, false, a->dtype == HWR_BF16)) {
         FewArgs f{};
         f.g = groups_arg(g);
@@ -359,7 +378,7 @@ hwr_status grouped_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_matmul
     if (g->n > 0 && (!a->dy || (a->dx && !a->w) || (a->dw && !a->x)))
         return invalid(c, "dy is required, w for dx, and x for dw");
     if (misaligned(a->dtype, {a->dy, a->x, a->w, a->dx, a->dw})) return invalid(c, "a pointer is not aligned to its elements");
-    if (hwr_status st = use_device(c)) return st;
+    OPS_ON_DEVICE(c, c->dev);
     const bool bf16 = a->dtype == HWR_BF16;
     const void *dy = a->dy, *x = a->x, *w = a->w;
     int64_t lddy = dense(a->lddy, a->m), ldx = dense(a->ldx, a->k), ldw = a->m;
@@ -407,7 +426,7 @@ hwr_status adapter_matmul(hwr_ops *c, const hwr_groups *g, const hwr_adapter_arg
     if (!a->x || !a->w || !a->a || !a->b || !a->y) return invalid(c, "x, w, a, b and y are required");
     if (misaligned(a->dtype, {a->x, a->w, a->a, a->b, a->y}) || misaligned(HWR_F32, {a->scale}))
         return invalid(c, "a pointer is not aligned to its elements");
-    if (hwr_status st = use_device(c)) return st;
+    OPS_ON_DEVICE(c, c->dev);
     const int64_t ldx = dense(a->ldx, a->k);
     if (few_rows(g->n, g->n_groups, a->k, a->m, true, a->dtype == HWR_BF16)) {
         FewArgs f{};
@@ -460,7 +479,7 @@ hwr_status adapter_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_adapte
         return invalid(c, "dy is required; w, a and b for dx; x and b for da; x and a for db");
     if (misaligned(a->dtype, {a->dy, a->x, a->w, a->a, a->b, a->dx, a->da, a->db}) || misaligned(HWR_F32, {a->scale}))
         return invalid(c, "a pointer is not aligned to its elements");
-    if (hwr_status st = use_device(c)) return st;
+    OPS_ON_DEVICE(c, c->dev);
     const bool bf16 = a->dtype == HWR_BF16;
     const int64_t lddy = dense(a->lddy, a->m), ldx = dense(a->ldx, a->k);
     const uint64_t each = low_bytes(g->n, a->rank);
@@ -543,7 +562,7 @@ void hwr_ops_free(hwr_ops *ops) {
     if (!ops) return;
     c_boundary(
         [&] {
-            (void)hipSetDevice(ops->dev);
+            const OnDevice on_device(ops->dev);
             (void)hipStreamSynchronize(ops->stream);
             release(ops);
             return HWR_OK;
@@ -558,7 +577,7 @@ hwr_status hwr_ops_reserve(hwr_ops *ops, uint64_t bytes) {
         [&]() -> hwr_status {
             if (!ops) return invalid(nullptr, "ops is NULL");
             if (bytes > uint64_t(1) << 40) return invalid(ops, "bytes above 1 TiB");
-            if (hwr_status st = use_device(ops)) return st;
+            OPS_ON_DEVICE(ops, ops->dev);
             char *p;
             return workspace(ops, bytes, &p);
         },

@@ -21,6 +21,7 @@ namespace {
 struct Launch {
     std::string kernel;
     dim3 grid, block;
+    int device;
 };
 std::vector<Launch> g_log;
 std::map<const void *, std::string> &kernels() {      // registered before main
@@ -32,12 +33,15 @@ uintptr_t g_next = uintptr_t(1) << 40;
 int g_mallocs = 0;
 size_t g_fail = SIZE_MAX;         // allocations of this many bytes or more fail
 bool g_capturing = false;
+int g_device = 0, g_wrong_device = 0;     // current; calls made on another than the context's
+int g_context_device = 0;
 dim3 g_grid, g_block;
 size_t g_shm;
 hipStream_t g_stream;
 
 hipError_t launch(const void *f, dim3 grid, dim3 block) {
-    g_log.push_back({kernels()[f], grid, block});
+    g_log.push_back({kernels()[f], grid, block, g_device});
+    g_wrong_device += g_device != g_context_device;
     return hipSuccess;
 }
 
@@ -67,6 +71,7 @@ hipError_t hipExtLaunchKernel(const void *f, dim3 grid, dim3 block, void **, siz
 }
 hipError_t hipMalloc(void **p, size_t n) {
     ++g_mallocs;
+    g_wrong_device += g_device != g_context_device;
     if (n >= g_fail) return hipErrorOutOfMemory;
     g_mem[g_next] = n;
     *p = reinterpret_cast<void *>(g_next);
@@ -75,13 +80,14 @@ hipError_t hipMalloc(void **p, size_t n) {
 }
 hipError_t hipFree(void *p) {
     g_mem.erase(reinterpret_cast<uintptr_t>(p));
+    g_wrong_device += g_device != g_context_device;
     return hipSuccess;
 }
 hipError_t hipMemset(void *, int, size_t) { return hipSuccess; }
 hipError_t hipDeviceSynchronize() { return hipSuccess; }
-hipError_t hipGetDeviceCount(int *n) { return *n = 1, hipSuccess; }
-hipError_t hipGetDevice(int *d) { return *d = 0, hipSuccess; }
-hipError_t hipSetDevice(int) { return hipSuccess; }
+hipError_t hipGetDeviceCount(int *n) { return *n = 2, hipSuccess; }
+hipError_t hipGetDevice(int *d) { return *d = g_device, hipSuccess; }
+hipError_t hipSetDevice(int d) { return g_device = d, hipSuccess; }
 hipError_t hipGetDevicePropertiesR0600(hipDeviceProp_tR0600 *p, int) {
     *p = {};
     std::strcpy(p->gcnArchName, "gfx950");
@@ -119,7 +125,7 @@ struct Rig {
     hwr_ops *ops = nullptr;
     int dtype = HWR_BF16, n = 0, G = 1, k = 8, m = 8, rank = 4;
 
-    Rig() { check(hwr_ops_init(0, reinterpret_cast<void *>(0x1000), &ops) == HWR_OK, "init"); }
+    explicit Rig(int device = 0) { check(hwr_ops_init(device, reinterpret_cast<void *>(0x1000), &ops) == HWR_OK, "init"); }
     ~Rig() { hwr_ops_free(ops); }
     hwr_groups groups() const { return {n, G, at<int32_t>(0), at<int32_t>(1)}; }
     hwr_status group() { return hwr_group_rows(ops, n, at<int32_t>(2), nullptr, 0, G, at<int32_t>(0), at<int32_t>(1)); }
@@ -247,11 +253,42 @@ void work_space() {
     check(needed > 50, std::to_string(needed) + " calls took work space");
 }
 
+// Whatever device is current when a call is made, the call works on its context's and
+// leaves the current one as it was, also where it is refused or fails.
+void current_device() {
+    for (int device : {0, 1})
+        for (int current : {0, 1}) {
+            const std::string what = "context on " + std::to_string(device) + ", current " + std::to_string(current);
+            g_context_device = device, g_device = current, g_wrong_device = 0;
+            {
+                Rig r(device);
+                check(g_device == current, what + ": init");
+                r.n = 300, r.k = 264, r.m = 392, r.rank = 16, r.G = 3;
+                check(r.group() == HWR_OK && r.matmul() == HWR_OK && r.matmul_grad() == HWR_OK && r.adapter() == HWR_OK &&
+                          r.adapter_grad() == HWR_OK, what + ": queued");
+                check(g_device == current, what + ": calls");
+                check(hwr_ops_reserve(r.ops, 1 << 24) == HWR_OK && g_device == current, what + ": reserve");
+                g_fail = 1;
+                r.n = 200000;
+                check(r.adapter() == HWR_ERR_OOM && g_device == current, what + ": no memory");
+                g_fail = SIZE_MAX;
+                r.k = 0;
+                check(r.matmul() == HWR_ERR_INVALID_ARG && g_device == current, what + ": refused");
+            }
+            check(g_device == current, what + ": free");
+            check(g_wrong_device == 0, what + ": " + std::to_string(g_wrong_device) + " on the wrong device");
+        }
+    hwr_ops *none = nullptr;
+    g_device = 1, g_fail = 1;
+    check(hwr_ops_init(0, nullptr, &none) == HWR_ERR_OOM && g_device == 1, "init without memory");
+    g_device = 0, g_fail = SIZE_MAX;
+}
+
 struct Scenario {
     const char *name;
     void (*run)();
 };
-const Scenario kScenarios[] = {{"row_limit", row_limit}, {"largest_grids", largest_grids}, {"work_space", work_space}};
+const Scenario kScenarios[] = {{"row_limit", row_limit}, {"largest_grids", largest_grids}, {"work_space", work_space}, {"current_device", current_device}};
 
 }  // namespace
 

@@ -39,7 +39,9 @@ hwr_status fail(hwr_ops *c, hwr_status s, const std::string &msg) {
 }
 hwr_status invalid(hwr_ops *c, const char *msg) { return fail(c, HWR_ERR_INVALID_ARG, msg); }
 
+// (The runtime keeps the error until it is asked for: the next launch would report it again.)
 hwr_status hip_fail(hwr_ops *c, hipError_t e, const char *what) {
+    (void)hipGetLastError();
     std::string m = std::string(what) + ": " + hipGetErrorName(e) + " (" + hipGetErrorString(e) + ")";
     return fail(c, e == hipErrorOutOfMemory ? HWR_ERR_OOM : HWR_ERR_HIP, m);
 }
@@ -100,10 +102,7 @@ hwr_status workspace(hwr_ops *c, uint64_t bytes, char **out) {
             size = bytes;
             e = hipMalloc(&p, size);
         }
-        if (e != hipSuccess) {
-            (void)hipGetLastError();
-            return hip_fail(c, e, "work space");
-        }
+        if (e != hipSuccess) return hip_fail(c, e, "work space");
         c->blocks.push_back(p);
         c->size = size;
     }
@@ -116,11 +115,14 @@ hwr_status init_impl(int32_t device, void *stream, hwr_ops **out) {
     *out = nullptr;
     int ndev = 0;
     hipError_t e = hipGetDeviceCount(&ndev);
-    if (e != hipSuccess || ndev < 1) return fail(nullptr, HWR_ERR_HIP, "no HIP device available");
+    if (e != hipSuccess || ndev < 1) {
+        (void)hipGetLastError();
+        return fail(nullptr, HWR_ERR_HIP, "no HIP device available");
+    }
     if (device < 0 || device >= ndev) return invalid(nullptr, "device ordinal out of range");
     hipDeviceProp_t prop;
-    if (hipGetDeviceProperties(&prop, device) != hipSuccess)
-        return fail(nullptr, HWR_ERR_HIP, "hipGetDeviceProperties failed");
+    e = hipGetDeviceProperties(&prop, device);
+    if (e != hipSuccess) return hip_fail(nullptr, e, "hipGetDeviceProperties");
     if (std::strncmp(prop.gcnArchName, "gfx950", 6) != 0)
         return fail(nullptr, HWR_ERR_UNSUPPORTED, std::string("library is built for gfx950, device is ") + prop.gcnArchName);
     OPS_ON_DEVICE(nullptr, device);
@@ -140,10 +142,6 @@ hwr_status init_impl(int32_t device, void *stream, hwr_ops **out) {
 }
 
 // ---------------------------------------------------------------- checks
-struct Shape {
-    int32_t dtype, k, m;
-};
-
 // Null when sound, else what is wrong.
 const char *check_groups(const hwr_groups *g) {
     if (!g) return "groups is NULL";

@@ -33,6 +33,7 @@ uintptr_t g_next = uintptr_t(1) << 40;
 int g_mallocs = 0;
 size_t g_fail = SIZE_MAX;         // allocations of this many bytes or more fail
 bool g_capturing = false;
+hipError_t g_error = hipSuccess;  // the last error: stays until it is asked for
 int g_device = 0, g_wrong_device = 0;     // current; calls made on another than the context's
 int g_context_device = 0;
 dim3 g_grid, g_block;
@@ -72,7 +73,7 @@ hipError_t hipExtLaunchKernel(const void *f, dim3 grid, dim3 block, void **, siz
 hipError_t hipMalloc(void **p, size_t n) {
     ++g_mallocs;
     g_wrong_device += g_device != g_context_device;
-    if (n >= g_fail) return hipErrorOutOfMemory;
+    if (n >= g_fail) return g_error = hipErrorOutOfMemory;
     g_mem[g_next] = n;
     *p = reinterpret_cast<void *>(g_next);
     g_next += (n + 4095) / 4096 * 4096 + 4096;
@@ -96,7 +97,11 @@ hipError_t hipGetDevicePropertiesR0600(hipDeviceProp_tR0600 *p, int) {
 }
 const char *hipGetErrorName(hipError_t) { return "error"; }
 const char *hipGetErrorString(hipError_t) { return "injected"; }
-hipError_t hipGetLastError() { return hipSuccess; }
+hipError_t hipGetLastError() {
+    const hipError_t e = g_error;
+    g_error = hipSuccess;
+    return e;
+}
 hipError_t hipStreamSynchronize(hipStream_t) { return hipSuccess; }
 hipError_t hipStreamIsCapturing(hipStream_t, hipStreamCaptureStatus *c) {
     *c = g_capturing ? hipStreamCaptureStatusActive : hipStreamCaptureStatusNone;
@@ -284,11 +289,35 @@ void current_device() {
     g_device = 0, g_fail = SIZE_MAX;
 }
 
+// An error that was reported once is not reported again by the next launch.
+void errors_are_reported_once() {
+    Rig r;
+    r.n = 300, r.k = 264, r.m = 392, r.rank = 16, r.G = 3;
+    hwr_ops *none = nullptr;
+    g_fail = 1;
+    check(hwr_ops_init(0, nullptr, &none) == HWR_ERR_OOM && !none, "init without memory");
+    g_fail = SIZE_MAX;
+    check(r.matmul() == HWR_OK, "a launch after it");
+    g_fail = 1;
+    r.n = 200000;
+    check(r.adapter() == HWR_ERR_OOM, "no memory");
+    g_fail = SIZE_MAX;
+    r.n = 300;
+    check(r.matmul() == HWR_OK, "a launch after it");
+    // the rounded size is not to be had, the size itself is
+    Rig s;
+    s.n = 200000, s.k = s.m = 40;
+    g_fail = size_t(1) << 25;      // 200,000 rows of 128 bytes: 24.4 MB
+    check(s.adapter() == HWR_OK, "no room to round up");
+    g_fail = SIZE_MAX;
+}
+
 struct Scenario {
     const char *name;
     void (*run)();
 };
-const Scenario kScenarios[] = {{"row_limit", row_limit}, {"largest_grids", largest_grids}, {"work_space", work_space}, {"current_device", current_device}};
+const Scenario kScenarios[] = {{"row_limit", row_limit}, {"largest_grids", largest_grids}, {"work_space", work_space}, {"current_device", current_device},
+                               {"errors_are_reported_once", errors_are_reported_once}};
 
 }  // namespace
 

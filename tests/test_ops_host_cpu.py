@@ -34,7 +34,8 @@ def driver(tmp_path_factory):
     return exe
 
 
-@pytest.mark.parametrize("scenario", ["row_limit", "largest_grids", "work_space", "current_device"])
+@pytest.mark.parametrize("scenario", ["row_limit", "largest_grids", "work_space", "current_device",
+                                      "errors_are_reported_once"])
 def test_operators_host_side(driver, scenario):
     r = subprocess.run([driver, scenario], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout + r.stderr

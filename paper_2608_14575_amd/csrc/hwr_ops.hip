@@ -142,12 +142,18 @@ hwr_status init_impl(int32_t device, void *stream, hwr_ops **out) {
 }
 
 // ---------------------------------------------------------------- checks
+bool misaligned(int32_t dtype, std::initializer_list<const void *> ptrs) {
+    for (const void *p : ptrs)
+        if (reinterpret_cast<uintptr_t>(p) & (dtype == HWR_BF16 ? 1 : 3)) return true;
+    return false;
+}
 // Null when sound, else what is wrong.
 const char *check_groups(const hwr_groups *g) {
     if (!g) return "groups is NULL";
     if (g->n < 0 || g->n > kMaxRows) return "rows outside 0..2147483136";
     if (g->n_groups < 1 || g->n_groups > kMaxPairs) return "n_groups outside 1..1024";
     if (!g->offsets) return "offsets is NULL";
+    if (misaligned(HWR_F32, {g->offsets, g->order})) return "offsets or order is not aligned to its elements";
     return nullptr;
 }
 const char *check_shape(int32_t dtype, int32_t k, int32_t m) {
@@ -158,12 +164,6 @@ const char *check_shape(int32_t dtype, int32_t k, int32_t m) {
 const char *check_rank(int32_t rank) { return rank < 1 || rank > kMaxRank ? "rank outside 1..128" : nullptr; }
 bool bad_ld(int64_t ld, int32_t width) { return ld != 0 && ld < width; }
 int64_t dense(int64_t ld, int32_t width) { return ld ? ld : width; }
-bool misaligned(int32_t dtype, std::initializer_list<const void *> ptrs) {
-    for (const void *p : ptrs)
-        if (reinterpret_cast<uintptr_t>(p) & (dtype == HWR_BF16 ? 1 : 3)) return true;
-    return false;
-}
-
 GroupsArg groups_arg(const hwr_groups *g) { return {g->n, g->n_groups, g->offsets, g->order}; }
 
 int rank_blocks(int rank) { return (rank + kRankBlock - 1) / kRankBlock; }

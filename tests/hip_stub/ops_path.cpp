@@ -312,12 +312,37 @@ void errors_are_reported_once() {
     g_fail = SIZE_MAX;
 }
 
+// Every pointer has to be aligned to its elements.
+void alignment() {
+    Rig r;
+    r.n = 300, r.k = 264, r.m = 392, r.rank = 16, r.G = 3;
+    g_log.clear();
+    for (int which = 0; which < 2; ++which)
+        for (int by = 1; by < 4; ++by) {
+            hwr_groups g = r.groups();
+            const int32_t *&p = which ? g.order : g.offsets;
+            p = reinterpret_cast<const int32_t *>(reinterpret_cast<uintptr_t>(p) + by);
+            const hwr_matmul_args m{HWR_BF16, 264, 392, at<char>(3), 0, at<char>(4), at<char>(5), 0};
+            const hwr_matmul_grad_args mg{HWR_BF16, 264, 392, at<char>(5), 0, at<char>(3), 0, at<char>(4), at<char>(6), 0, at<char>(7)};
+            const hwr_adapter_args a{HWR_BF16, 264, 392, 16, at<char>(3), 0, at<char>(4), at<char>(8), at<char>(9), nullptr, at<char>(5), 0};
+            const hwr_adapter_grad_args ag{HWR_BF16, 264, 392, 16, at<char>(5), 0, at<char>(3), 0, at<char>(4), at<char>(8), at<char>(9),
+                                           nullptr, at<char>(6), 0, at<char>(10), at<char>(11)};
+            const std::string what = std::string(which ? "order" : "offsets") + " off by " + std::to_string(by);
+            check(hwr_grouped_matmul(r.ops, &g, &m) == HWR_ERR_INVALID_ARG, what + ": matmul");
+            check(hwr_grouped_matmul_grad(r.ops, &g, &mg) == HWR_ERR_INVALID_ARG, what + ": matmul_grad");
+            check(hwr_adapter_matmul(r.ops, &g, &a) == HWR_ERR_INVALID_ARG, what + ": adapter");
+            check(hwr_adapter_matmul_grad(r.ops, &g, &ag) == HWR_ERR_INVALID_ARG, what + ": adapter_grad");
+            check(std::strstr(hwr_ops_last_error(r.ops), "aligned") != nullptr, what + ": the message says why");
+        }
+    check(g_log.empty(), "nothing launched");
+}
+
 struct Scenario {
     const char *name;
     void (*run)();
 };
 const Scenario kScenarios[] = {{"row_limit", row_limit}, {"largest_grids", largest_grids}, {"work_space", work_space}, {"current_device", current_device},
-                               {"errors_are_reported_once", errors_are_reported_once}};
+                               {"errors_are_reported_once", errors_are_reported_once}, {"alignment", alignment}};
 
 }  // namespace
 

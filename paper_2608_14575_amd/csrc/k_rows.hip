@@ -1,5 +1,7 @@
 // Products by row: every row of a routed batch with the weights of its group
 // (kGrouped), or with shared weights plus its group's low-rank adapter (kAdapter).
+#include <algorithm>
+
 #include "ops_device.hpp"
 
 namespace hwr {
@@ -378,8 +380,8 @@ bool whole_chunks(bool bf16, bool ks, const RowsArgs &a) {
 // with adapters 4,096 x 1024 x 1536 in 8 136 / 155; 16,384 x 1024 x 1536 in one 444 / 406); where even small tiles leave units idle, parts of the contraction of at least
 // four stages.
 RowsPlan rows_plan(bool bf16, RowsKind kind, bool ks, const RowsArgs &a, int cus) {
-    auto tiles = [&](int64_t bm, int64_t bn) {
-        return (a.g.n / bm + (kind == RowsKind::kAdapter ? 1 : a.g.G)) * ((a.m + bn - 1) / bn);
+    auto tiles = [&](int64_t bm, int64_t bn) {          // (at most n groups hold a row)
+        return (a.g.n / bm + (kind == RowsKind::kAdapter ? 1 : std::min(a.g.n, a.g.G))) * ((a.m + bn - 1) / bn);
     };
     RowsPlan p{whole_chunks(bf16, ks, a) && a.mw >= 64, 64, 64, 1};
     const int stages = (a.k + (bf16 ? 63 : 31)) / (bf16 ? 64 : 32);

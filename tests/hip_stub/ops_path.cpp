@@ -337,12 +337,30 @@ void alignment() {
     check(g_log.empty(), "nothing launched");
 }
 
+// The input gradient of few rows of many groups: n rows make n tiles at most, however many
+// groups there are, so small tiles and parts of the contraction occupy the device.
+void few_rows_of_many_groups() {
+    struct Batch {
+        int n, G, k;
+    };
+    for (const Batch &b : {Batch{1, 32, 4096}, Batch{4, 1024, 2048}, Batch{7, 9, 2048}}) {
+        Rig r;
+        r.n = b.n, r.G = b.G, r.k = r.m = b.k;
+        g_log.clear();
+        check(r.matmul_grad(true, false) == HWR_OK && g_log.size() == 2, "dx: parts and their sum");
+        const uint64_t tiles = uint64_t(b.n) * ((b.k + 63) / 64);
+        check(g_log[0].kernel.find("Li64ELi64E") != std::string::npos, "tiles of 64: " + g_log[0].kernel);
+        check(g_log[0].grid.x >= 256 || g_log[0].grid.x >= 4 * tiles, std::to_string(g_log[0].grid.x) + " workgroups");
+    }
+}
+
 struct Scenario {
     const char *name;
     void (*run)();
 };
 const Scenario kScenarios[] = {{"row_limit", row_limit}, {"largest_grids", largest_grids}, {"work_space", work_space}, {"current_device", current_device},
-                               {"errors_are_reported_once", errors_are_reported_once}, {"alignment", alignment}};
+                               {"errors_are_reported_once", errors_are_reported_once}, {"alignment", alignment},
+                               {"few_rows_of_many_groups", few_rows_of_many_groups}};
 
 }  // namespace
 

@@ -1,12 +1,15 @@
 """More of the operators on a routed batch (include/hwr_ops.h): batches of up to 2^31
-rows, and intermediates near the largest values.
+rows, intermediates near the largest values, few rows of many groups.
 
 Tolerances: inputs whose products and sums are whole numbers below 2^24 give exact
 sums in fp32, in any order, so that a bf16 result is off by its rounding alone (2^-8
-of its value)."""
+of its value).  Otherwise: a sum of K products in fp32 is off by at most (K + 16) 2^-24 times the
+sum of the terms' magnitudes, and its rounding by 2^-8 (bf16) or 2^-24 (fp32) of the value."""
+import numpy as np
 import pytest
 
 from paper_2608_14575_amd import hwr, routed
+from test_gpu_routed_ops import EPS, TYPES, close, grouped, outer, product, rand, sizes_of
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -135,3 +138,23 @@ def test_intermediates_past_the_largest_bf16(ops, n, sign):
     ops.adapter_grad(dy, x, w, a, b, None, off, dx=dx, da=da)
     near(dx[1], v * 2.0 ** -10)
     near(da[0, :, 2], v * 2.0 ** -9)
+
+
+# ---------------------------------------------------------------- few rows of many groups
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,G,k,m,kind", [(1, 32, 2048, 1032, "one"), (4, 300, 1024, 1024, "even"), (7, 9, 1032, 2056, "skew"),
+                                          (20, 70, 1027, 1029, "skew"), (5, 40, 1024, 1536, "one")])
+def test_gradients_of_fewer_rows_than_groups(ops, n, G, k, m, kind, dtype):
+    t, u, _ = TYPES[dtype]
+    gen = torch.Generator("cuda").manual_seed(n + k)
+    gid, off, order = grouped(sizes_of(kind, n, G, np.random.default_rng(n)), G)
+    x, dy, w = rand(gen, n, k, dtype=t), rand(gen, n, m, dtype=t), rand(gen, G, k, m, dtype=t)
+    dx, dw = torch.full_like(x, 7.0), torch.full_like(w, 7.0)
+    ops.matmul_grad(dy, x, w, off, order, dx=dx, dw=dw)
+    ref, s = product(dy, w.transpose(1, 2).contiguous(), gid)
+    close(dx, ref, u * ref.abs() + (m + 16) * EPS * s)
+    ref, s, cnt = outer(x, dy, gid, G)
+    close(dw, ref, u * ref.abs() + (cnt + 16) * EPS * s)
+    again = torch.full_like(x, 7.0)
+    ops.matmul_grad(dy, x, w, off, order, dx=again)
+    assert torch.equal(again, dx)

@@ -35,7 +35,7 @@ def driver(tmp_path_factory):
 
 
 @pytest.mark.parametrize("scenario", ["row_limit", "largest_grids", "work_space", "current_device",
-                                      "errors_are_reported_once", "alignment"])
+                                      "errors_are_reported_once", "alignment", "few_rows_of_many_groups"])
 def test_operators_host_side(driver, scenario):
     r = subprocess.run([driver, scenario], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout + r.stderr

@@ -136,6 +136,8 @@ class RoutedOps:
         i32, n, nt = self._i32, choice.numel(), 0 if table is None else table.numel()
         if max(n, nt, n_groups) > _MAX_INT or n_groups < 0:
             _bad("choice, table, n_groups", f"{n}, {nt}, {n_groups}: outside 32 bits")
+        if table is not None and nt == 0:              # (without an address it would be no table)
+            _bad("table", "empty")
         st = self._lib.hwr_group_rows(self.ctx, n, self._dense("choice", choice, i32, (n,)),
                                       None if table is None else self._dense("table", table, i32, (nt,)), nt, n_groups,
                                       self._dense("offsets", offsets, i32, (n_groups + 1,)),

@@ -66,3 +66,21 @@ def test_packed_arguments_are_the_structures(name):
         with pytest.raises(hwr.HwrError) as e:
             call(None, n, 6, 1, 0, bad)
         assert e.value.status == hwr.HWR_ERR_INVALID_ARG
+
+
+def test_an_empty_table_is_refused():
+    """An empty tensor has no address, which the library reads as no table."""
+    import torch
+
+    class Library:
+        def hwr_group_rows(self, *args):
+            raise AssertionError(f"reached the library: {args}")
+
+    ops = object.__new__(routed.RoutedOps)
+    ops.ctx, ops._lib, ops.device, ops._i32 = None, Library(), -1, torch.int32
+    i = lambda n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    with pytest.raises(hwr.HwrError) as e:
+        ops.group(i(4), 2, table=i(0), offsets=i(3), order=i(4))
+    assert e.value.status == hwr.HWR_ERR_INVALID_ARG and "table" in str(e.value)
+    with pytest.raises(AssertionError, match="reached"):
+        ops.group(i(4), 2, table=i(1), offsets=i(3), order=i(4))

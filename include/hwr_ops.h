@@ -49,7 +49,10 @@
  * than it has allocates, before it queues anything (and keeps what it had until
  * hwr_ops_free, so that captured graphs stay valid); under stream capture it is
  * HWR_ERR_STATE instead, with nothing recorded: make the call once outside, or reserve
- * what the message names (hwr_ops_reserve), before capturing.  A context is not
+ * what the message names (hwr_ops_reserve), before capturing.  All calls of a context, and
+ * all replays of graphs captured from it, use the same work space: a replay has to be
+ * ordered against the context's other calls and against its other graphs' replays (an event
+ * does), or each graph captured from a context of its own.  A context is not
  * thread-safe.  Sizes and pointers are checked; the contents of offsets, order,
  * choice and table are not: values out of range give unspecified results, and
  * all memory accesses stay in bounds.

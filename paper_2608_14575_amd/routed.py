@@ -82,7 +82,9 @@ class RoutedOps:
             pass
 
     def reserve(self, nbytes: int) -> None:
-        """Work space for later calls (needed before calls under graph capture)."""
+        """Work space for later calls (needed before calls under graph capture).  A context's
+        calls and the replays of all graphs captured from it share that space: order replays
+        on other streams against them, or capture each graph from a context of its own."""
         hwr.hwr_ops_reserve(self.ctx, int(nbytes))
 
     # ------------------------------------------------------------ checks

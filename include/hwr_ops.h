@@ -36,26 +36,32 @@
  *
  * Precision.  HWR_BF16 (raw bit patterns) or HWR_F32, one type for every matrix
  * of a call; scale is fp32.  Products accumulate in fp32 and each output is
- * rounded once (nearest, ties to even).  The low-rank intermediates s (x A) and u are kept in
- * fp32 (HWR_F32) or as the sum of two bf16 values (HWR_BF16: 16 significant bits),
- * not rounded to bf16.  Sums have a fixed order: the same call on the same device gives
- * the same bits.  An infinity or a NaN stays in the rows (and groups) that it
- * belongs to.
+ * rounded once (nearest, ties to even).  The low-rank intermediates s (x A) and u are not
+ * rounded to bf16: HWR_F32 calls hold them in fp32; HWR_BF16 calls as the sum of two bf16
+ * values (16 significant bits, so that the second product runs on bf16 operands),
+ * except hwr_adapter_matmul of few rows (at most 192, fewer with large weights), which
+ * holds them in fp32.  So the number of rows in a batch can change a row's last bits.
+ * Sums have a fixed order: the same call on the same device gives the same bits.  An
+ * infinity or a NaN stays in the rows (and groups) that it belongs to.
+ *
+ * Gradients are calls of their own; nothing is recorded for automatic differentiation.
  *
  * Every call is queued on the context's stream and returns without waiting; the
- * calling thread's current device is left as it was.
- * Inputs written and outputs read on another stream have to be ordered against
- * it by the caller.  Work space belongs to the context: a call that needs more
- * than it has allocates, before it queues anything (and keeps what it had until
- * hwr_ops_free, so that captured graphs stay valid); under stream capture it is
- * HWR_ERR_STATE instead, with nothing recorded: make the call once outside, or reserve
- * what the message names (hwr_ops_reserve), before capturing.  All calls of a context, and
- * all replays of graphs captured from it, use the same work space: a replay has to be
- * ordered against the context's other calls and against its other graphs' replays (an event
- * does), or each graph captured from a context of its own.  A context is not
- * thread-safe.  Sizes and pointers are checked; the contents of offsets, order,
- * choice and table are not: values out of range give unspecified results, and
- * all memory accesses stay in bounds.
+ * calling thread's current device is left as it was.  Inputs written and outputs read
+ * on another stream have to be ordered against it by the caller.
+ *
+ * Work space belongs to the context: a call that needs more than it has allocates,
+ * before it queues anything (and keeps what it had until hwr_ops_free, so that captured
+ * graphs stay valid); under stream capture it is HWR_ERR_STATE instead, with nothing
+ * recorded: make the call once outside, or reserve what the message names
+ * (hwr_ops_reserve), before capturing.  All calls of a context, and all replays of graphs
+ * captured from it, use the same work space: a replay has to be ordered against the
+ * context's other calls and against its other graphs' replays (an event does), or each
+ * graph captured from a context of its own.
+ *
+ * A context is not thread-safe.  Sizes and pointers are checked; the contents of offsets,
+ * order, choice and table are not: values out of range give unspecified results, and all
+ * memory accesses stay in bounds.
  */
 #ifndef HWR_OPS_H
 #define HWR_OPS_H

@@ -4,14 +4,16 @@
 // A lane (m = l % 16, q = l / 16) loads 16 bytes of V columns from each of V
 // weight rows, V = 8 (bf16) or 4 (fp32): rows q V .. q V + V - 1 of a step of 4 V,
 // columns m V .. m V + V - 1.  Its V x V block transposed is the lane's share of V
-// A-operand fragments: fragment j holds the columns m V + j.  No LDS, no
-// barrier: each wave keeps two steps of loads in flight.  The waves of a
-// workgroup take every kWaves-th step and add up through LDS; workgroups that share
-// a tile write fp32 partial sums that k_join adds, in order.
+// A-operand fragments: fragment j holds the columns m V + j.  The steps need no LDS and
+// no barrier: a wave has the next step's loads in flight while it multiplies one.
+// The waves of a workgroup take every kWaves-th step and add up through LDS at the end;
+// workgroups that share a tile write fp32 partial sums that k_join adds, in order.
 //
 // A tile is 16 rows: tiles of the same weights run side by side on one L2 (48
 // rows, 4096 x 4096 bf16: 14.8 us; with tiles of 32 rows 17.0, of 64 rows 20.7, for
-// want of registers to load ahead).
+// want of registers to load ahead: the loads of cut columns and of a last cut step stand
+// in the same loop, which takes all 128 registers in bf16 and spills 14 to 16 of them, read
+// back on those paths alone).
 #include "ops_device.hpp"
 
 namespace hwr {
@@ -251,8 +253,14 @@ hipError_t go(const FewArgs &a, hipStream_t s) {
 // take a launch or two more with an adapter).  us, few / larger: adapter bf16 1024 x 1024
 // 192 rows 17.0 / 18.2; 2048 x 2048 130 rows 19.4 / 23.0, 192 rows 20.8 / 22.8, 256 rows 28.1 / 27.7;
 // 2752 x 3712 80 rows 24.9 / 27.2, 130 rows 45.4 / 30.5; 4096 x 4096 96 rows 27.8 / 34.6, 130 rows
-// 41.8 / 36.8; fp32 2048 x 2048 256 rows 37 / 44; grouped (2 groups) bf16 4096 x 4096 49 rows
-// 19.1 / 20.1, 64 rows 26.7 / 20.4, fp32 2048 x 2048 256 rows 38 / 44, 384 rows 48 / 44.
+// 41.8 / 36.8; fp32 2048 x 2048 256 rows 37 / 44; grouped (2 groups) bf16 4096 x 4096 33 rows 18.7 / 19.5,
+// 48 rows 18.6 / 19.5, 64 rows 19.0 to 26.7 / 19.9, 1024 x 2048 48 rows 9.7 to 10.3 / 8.6, 64 rows 10.2 / 8.6 (beside
+// 8 to 10 of the call's host time): three tiles; fp32 2048 x 2048 256 rows 38 / 44, 384 rows 48 / 44.
+// And where groups have at most 16 rows on average, for a larger tile's other rows are then
+// empty: 32 groups evenly, bf16 1024 x 2048 128 rows 25.4 / 30.8, 512 rows 26.3 / 30.8, 2048 x 2048 47.5 / 55.2,
+// fp32 1024 x 1024 512 rows 26.2 / 41.3; 1,024 groups 512 x 512 16,384 rows bf16 200 / 216, fp32 326 / 610; 8 groups bf16
+// 1024 x 2048 96 rows 13.0 / 9.5, 128 rows 9.3 / 9.5.  The rule does not see how rows lie: all in one
+// group of 32, 512 rows 12.8 / 30.7; of 1,024, 16,384 rows 112 / 47, fp32 203 / 105.
 bool few_rows(int n, int G, int k, int m, bool adapter, bool bf16) {
     const int most = !bf16 ? 256 : !adapter ? 48 : static_cast<int64_t>(k) * m <= 1 << 22 ? 192 : 96;
     return n <= most || (!adapter && n <= kFewTile * G);

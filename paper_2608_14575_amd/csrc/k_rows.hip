@@ -373,12 +373,14 @@ bool whole_chunks(bool bf16, bool ks, const RowsArgs &a) {
 }  // namespace
 
 // The largest tile that gives most compute units a workgroup: 256 half of them with an
-// adapter, three of four without (us, 256 / 128: adapter 2,100 x 2048 x 4096 72 / 98, 3,300 x 1024 x 4096
-// 50 / 80, 4,208 x 2200 x 3226 89 / 153; grouped, 4 groups, 2048 x 4096 1,600 rows 56 / 41, 2,100 rows 58 / 61,
-// 3,000 rows 61 / 74); fp32 128 from three a compute unit, for below that rounds and the ends of groups
-// cost more (64 / 128: 4,096 x 1536 x 1536 in one group 165 / 202, 4,096 x 1024 x 1024 in 32 115 / 137,
-// with adapters 4,096 x 1024 x 1536 in 8 136 / 155; 16,384 x 1024 x 1536 in one 444 / 406); where even small tiles leave units idle, parts of the contraction of at least
-// four stages.
+// adapter (whose tiles of 128 take 260 to 271 registers in bf16 and so run one workgroup on a
+// compute unit; without an adapter 174 and two), three of four without.  us, 256 / 128:
+// adapter 2,100 x 2048 x 4096 72 / 98, 3,300 x 1024 x 4096 50 / 80, 4,208 x 2200 x 3226 89 / 153; grouped,
+// 4 groups, 2048 x 4096 1,600 rows 56 / 41, 2,100 rows 58 / 61, 3,000 rows 61 / 74.  fp32 128 from three
+// a compute unit, for below that rounds and the ends of groups cost more (64 / 128: 4,096 x
+// 1536 x 1536 in one group 165 / 202, 4,096 x 1024 x 1024 in 32 115 / 137, with adapters 4,096 x 1024 x
+// 1536 in 8 136 / 155; 16,384 x 1024 x 1536 in one 444 / 406).  Where even small tiles leave units
+// idle, parts of the contraction of at least four stages.
 RowsPlan rows_plan(bool bf16, RowsKind kind, bool ks, const RowsArgs &a, int cus) {
     auto tiles = [&](int64_t bm, int64_t bn) {          // (at most n groups hold a row)
         return (a.g.n / bm + (kind == RowsKind::kAdapter ? 1 : std::min(a.g.n, a.g.G))) * ((a.m + bn - 1) / bn);

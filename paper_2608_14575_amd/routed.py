@@ -56,7 +56,11 @@ class RoutedOps:
     Matrices are bfloat16 or float32, one type in a call.  Rows of x, y, dy and
     dx may be strided (unit stride within a row); weights and their gradients are
     dense.  ``offsets`` and ``order`` are what ``group`` writes; ``order`` None means
-    that row i is at place i."""
+    that row i is at place i.
+
+    Gradients are calls of their own: nothing is recorded for torch's autograd, also where
+    an input requires a gradient, and outputs are written without a new version of the tensor.
+    A ``torch.autograd.Function`` around a product and its gradient records them."""
 
     def __init__(self, device: int = 0, stream: int = 0):
         import torch

@@ -378,3 +378,36 @@ def test_replays_in_order_with_other_calls(ops):
     torch.cuda.synchronize()
     del graphs
     o.close()
+
+
+# ---------------------------------------------------------------- autograd
+def test_in_an_autograd_function(ops):
+    """The calls themselves record nothing; a Function around a product and its gradient does."""
+    gen = torch.Generator("cuda").manual_seed(31)
+    n, G, k, m, t = 500, 3, 72, 40, torch.float32
+    gid, off, order = grouped(sizes_of("skew", n, G, np.random.default_rng(5)), G)
+    x, w, c = rand(gen, n, k, dtype=t).requires_grad_(), rand(gen, G, k, m, dtype=t).requires_grad_(), rand(gen, n, m, dtype=t)
+    y = torch.empty_like(c)
+    ops.matmul(x, w, off, order, y=y)
+    assert not y.requires_grad
+
+    class Grouped(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, w):
+            ctx.save_for_backward(x, w)
+            y = torch.empty_like(c)
+            ops.matmul(x, w, off, order, y=y)
+            return y
+
+        @staticmethod
+        def backward(ctx, dy):
+            x, w = ctx.saved_tensors
+            dx, dw = torch.empty_like(x), torch.empty_like(w)
+            ops.matmul_grad(dy.contiguous(), x, w, off, order, dx=dx, dw=dw)
+            return dx, dw
+
+    (Grouped.apply(x, w) * c).sum().backward()
+    ref, s = product(c, w.detach().transpose(1, 2).contiguous(), gid)
+    close(x.grad, ref, EPS * ref.abs() + (m + 16) * EPS * s)
+    ref, s, cnt = outer(x.detach(), c, gid, G)
+    close(w.grad, ref, EPS * ref.abs() + (cnt + 16) * EPS * s)

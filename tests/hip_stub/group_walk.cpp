@@ -175,11 +175,25 @@ void anything_in_offsets() {
             }
 }
 
+// An order that holds anything gives a row of the batch or none.
+void anything_in_order() {
+    std::mt19937 rng(3);
+    for (int n : {1, 7, 1000, INT32_MAX - 511}) {
+        std::vector<int32_t> order = {0, -1, n - 1, n, INT32_MIN, INT32_MAX};
+        for (int i = 0; i < 100; ++i) order.push_back(static_cast<int32_t>(rng()));
+        const hwr::GroupsArg g{n, 1, nullptr, order.data()}, plain{n, 1, nullptr, nullptr};
+        for (size_t p = 0; p < order.size(); ++p)
+            check(hwr::row_at(g, static_cast<int>(p)) == (order[p] >= 0 && order[p] < n ? order[p] : -1), "order " + std::to_string(order[p]));
+        check(hwr::row_at(plain, n - 1) == n - 1, "without an order");
+    }
+}
+
 struct Scenario {
     const char *name;
     void (*run)();
 };
-const Scenario kScenarios[] = {{"tiles_cover_the_places", tiles_cover_the_places}, {"anything_in_offsets", anything_in_offsets}};
+const Scenario kScenarios[] = {{"tiles_cover_the_places", tiles_cover_the_places}, {"anything_in_offsets", anything_in_offsets},
+                               {"anything_in_order", anything_in_order}};
 
 }  // namespace
 

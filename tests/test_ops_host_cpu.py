@@ -51,7 +51,7 @@ def walk(tmp_path_factory):
     return exe
 
 
-@pytest.mark.parametrize("scenario", ["tiles_cover_the_places", "anything_in_offsets"])
+@pytest.mark.parametrize("scenario", ["tiles_cover_the_places", "anything_in_offsets", "anything_in_order"])
 def test_walk_over_groups(walk, scenario):
     r = subprocess.run([walk, scenario], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout + r.stderr

@@ -18,6 +18,9 @@
  *                            dA[g] = sum over rows r of g of x[r]^T u[r],
  *                            dB[g] = sum of s[g] (x[r] A[g])^T dy[r]
  *                            (the shared W is frozen)
+ *   hwr_log_probs            of rows of logits: the log probability of a given token,
+ *                            the entropy, the most likely tokens
+ *   hwr_log_probs_grad       the gradient of the logits
  *
  * Groups.  `order` lists the rows of group 0, then of group 1, ..., and last
  * the rows in no group; group g has the places offsets[g] .. offsets[g+1]-1,
@@ -148,6 +151,48 @@ typedef struct {
     void *db;                     /* [G][rank][m] or NULL                       */
 } hwr_adapter_grad_args;
 hwr_status hwr_adapter_matmul_grad(hwr_ops *ops, const hwr_groups *g, const hwr_adapter_grad_args *a);
+
+/* Of every row r of logits x, with z = scale x:
+ *   lse[r]     = ln sum over tokens c of exp(z[c])
+ *   logp[r]    = z[token[r]] - lse[r]; 0 where token[r] is outside [0, m): no token
+ *   entropy[r] = - sum over c of p[c] ln p[c], p[c] = exp(z[c] - lse[r])
+ *   top_token[r], top_logp[r]: the `top` most likely tokens, the most likely first, of
+ *                equal logits the lower token, and their log probabilities.
+ * Outputs may be NULL.  A token at -inf is not allowed: p is 0, and it comes last among the most
+ * likely.  Logits below -3.3e38 (the lowest finite values of either type) count as -inf;
+ * a row of nothing else has lse -inf, logp -inf (0 without a token), entropy 0 and top_logp -inf.  A NaN or +inf in a
+ * row makes its lse, logp, entropy and top_logp NaN (which tokens are listed is then unspecified).
+ * Sums are fp32; how many rows a call has can change a row's last bits. */
+typedef struct {
+    int32_t dtype;                /* hwr_dtype of x                             */
+    int32_t n, m;                 /* rows, 0 or more; tokens, 1..16777216       */
+    int32_t top;                  /* 0..32, at most m                           */
+    float scale;                  /* 2^-64..2^64 (1 / temperature)              */
+    const void *x; int64_t ldx;   /* [n][m]                                     */
+    const int32_t *token;         /* [n]; needed for logp                       */
+    float *logp, *lse, *entropy;  /* [n]                                        */
+    float *top_logp;              /* [n][top]                                   */
+    int32_t *top_token;           /* [n][top]                                   */
+} hwr_log_probs_args;
+hwr_status hwr_log_probs(hwr_ops *ops, const hwr_log_probs_args *a);
+
+/* The gradient of the logits from those of logp and entropy, with ln p[c] = scale x[c] - lse[r]:
+ *   dx[r][c] = scale (dlogp[r] (1[c = token[r]] - p[c]) - dentropy[r] p[c] (ln p[c] + entropy[r]))
+ * A row without a token has no first term; without both terms, or with lse -inf, it gets zeros.
+ * dx may be x itself, with the same row stride.  lse holds ln p to 2^-24 of its magnitude. */
+typedef struct {
+    int32_t dtype;
+    int32_t n, m;
+    float scale;
+    const void *x; int64_t ldx;   /* [n][m]                                     */
+    const int32_t *token;         /* [n]; needed with dlogp                     */
+    const float *lse;             /* [n]                                        */
+    const float *dlogp;           /* [n] or NULL: zeros                         */
+    const float *entropy;         /* [n]; with dentropy, and only then          */
+    const float *dentropy;        /* [n] or NULL: zeros                         */
+    void *dx; int64_t lddx;       /* [n][m]                                     */
+} hwr_log_probs_grad_args;
+hwr_status hwr_log_probs_grad(hwr_ops *ops, const hwr_log_probs_grad_args *a);
 
 #ifdef __cplusplus
 }

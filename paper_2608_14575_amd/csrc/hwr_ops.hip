@@ -3,89 +3,18 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <cstring>
-#include <string>
-#include <vector>
 
-#include "c_boundary.hpp"
-#include "hwr_ops.h"
+#include "ops_context.hpp"
 #include "ops_internal.hpp"
 
 using namespace hwr;
 
-struct hwr_ops {
-    int dev = 0, cus = 0;
-    hipStream_t stream = nullptr;
-    void *zeros = nullptr;
-    // Work space: the last block is in use.  Blocks grow by powers of two and stay
-    // until hwr_ops_free: captured graphs hold their addresses.
-    std::vector<void *> blocks;
-    uint64_t size = 0;
-    std::string err;
-};
-
-namespace {
-
-thread_local std::string g_ops_error;
-
-constexpr int kMaxWidth = 65536;
-constexpr int kMaxRank = 128;
-constexpr int kMaxRows = INT32_MAX - 511;    // places are counted in 32 bits, up to a few tiles past the last
-constexpr uint64_t kZeroBytes = 256;
-
-hwr_status fail(hwr_ops *c, hwr_status s, const std::string &msg) {
-    (c ? c->err : g_ops_error) = msg;
-    return s;
-}
-hwr_status invalid(hwr_ops *c, const char *msg) { return fail(c, HWR_ERR_INVALID_ARG, msg); }
-
-// (The runtime keeps the error until it is asked for: the next launch would report it again.)
-hwr_status hip_fail(hwr_ops *c, hipError_t e, const char *what) {
-    (void)hipGetLastError();
-    std::string m = std::string(what) + ": " + hipGetErrorName(e) + " (" + hipGetErrorString(e) + ")";
-    return fail(c, e == hipErrorOutOfMemory ? HWR_ERR_OOM : HWR_ERR_HIP, m);
+std::string &hwr::ops_error() {
+    static thread_local std::string last;
+    return last;
 }
 
-#define OPS_HIP(ctx, call)                                           \
-    do {                                                             \
-        hipError_t e_ = (call);                                      \
-        if (e_ != hipSuccess) return hip_fail((ctx), e_, #call);     \
-    } while (0)
-
-void release(hwr_ops *c) {
-    for (void *p : c->blocks) (void)hipFree(p);
-    if (c->zeros) (void)hipFree(c->zeros);
-    delete c;
-}
-
-// Makes a device current for a scope; the caller's is current again after it.
-class OnDevice {
-  public:
-    explicit OnDevice(int dev) {
-        error = hipGetDevice(&before_);
-        if (error == hipSuccess && before_ != dev) {
-            error = hipSetDevice(dev);
-            changed_ = error == hipSuccess;
-        }
-    }
-    ~OnDevice() {
-        if (changed_) (void)hipSetDevice(before_);
-    }
-    OnDevice(const OnDevice &) = delete;
-    OnDevice &operator=(const OnDevice &) = delete;
-    hipError_t error;
-
-  private:
-    int before_ = 0;
-    bool changed_ = false;
-};
-
-#define OPS_ON_DEVICE(ctx, dev)    \
-    const OnDevice on_device(dev); \
-    if (on_device.error != hipSuccess) return hip_fail((ctx), on_device.error, "hipSetDevice")
-
-// At least `bytes` of work space at *out.
-hwr_status workspace(hwr_ops *c, uint64_t bytes, char **out) {
+hwr_status hwr::workspace(hwr_ops *c, uint64_t bytes, char **out) {
     if (bytes > c->size) {
         hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
         if (c->stream) OPS_HIP(c, hipStreamIsCapturing(c->stream, &cap));
@@ -108,6 +37,19 @@ hwr_status workspace(hwr_ops *c, uint64_t bytes, char **out) {
     }
     *out = c->blocks.empty() ? nullptr : static_cast<char *>(c->blocks.back());
     return HWR_OK;
+}
+
+namespace {
+
+constexpr int kMaxWidth = 65536;
+constexpr int kMaxRank = 128;
+constexpr int kMaxRows = INT32_MAX - 511;    // places are counted in 32 bits, up to a few tiles past the last
+constexpr uint64_t kZeroBytes = 256;
+
+void release(hwr_ops *c) {
+    for (void *p : c->blocks) (void)hipFree(p);
+    if (c->zeros) (void)hipFree(c->zeros);
+    delete c;
 }
 
 hwr_status init_impl(int32_t device, void *stream, hwr_ops **out) {
@@ -142,11 +84,6 @@ hwr_status init_impl(int32_t device, void *stream, hwr_ops **out) {
 }
 
 // ---------------------------------------------------------------- checks
-bool misaligned(int32_t dtype, std::initializer_list<const void *> ptrs) {
-    for (const void *p : ptrs)
-        if (reinterpret_cast<uintptr_t>(p) & (dtype == HWR_BF16 ? 1 : 3)) return true;
-    return false;
-}
 // Null when sound, else what is wrong.
 const char *check_groups(const hwr_groups *g) {
     if (!g) return "groups is NULL";
@@ -162,8 +99,6 @@ const char *check_shape(int32_t dtype, int32_t k, int32_t m) {
     return nullptr;
 }
 const char *check_rank(int32_t rank) { return rank < 1 || rank > kMaxRank ? "rank outside 1..128" : nullptr; }
-bool bad_ld(int64_t ld, int32_t width) { return ld != 0 && ld < width; }
-int64_t dense(int64_t ld, int32_t width) { return ld ? ld : width; }
 GroupsArg groups_arg(const hwr_groups *g) { return {g->n, g->n_groups, g->offsets, g->order}; }
 
 int rank_blocks(int rank) { return (rank + kRankBlock - 1) / kRankBlock; }
@@ -568,7 +503,7 @@ void hwr_ops_free(hwr_ops *ops) {
         [](const char *) {});
 }
 
-const char *hwr_ops_last_error(const hwr_ops *ops) { return ops ? ops->err.c_str() : g_ops_error.c_str(); }
+const char *hwr_ops_last_error(const hwr_ops *ops) { return ops ? ops->err.c_str() : ops_error().c_str(); }
 
 hwr_status hwr_ops_reserve(hwr_ops *ops, uint64_t bytes) {
     return c_boundary(

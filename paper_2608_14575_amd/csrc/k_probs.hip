@@ -1,0 +1,427 @@
+// Log probabilities from rows of logits: of a given token, with the entropy of the
+// distribution and its most likely tokens, and the gradient of the logits.
+//
+// With z = scale x, M = max z, S = sum exp(z - M) and T = sum exp(z - M) (z - M):
+//   lse = M + ln S,  log p[t] = z[t] - M - ln S,  H = ln S - T / S.
+// One pass: a thread keeps M, S and T of the elements that it has seen and rescales S and T
+// when M grows.  Exponents are taken of scale (x - M), which cannot overflow, so that masks of the
+// type's lowest value are as good as infinities.  A row of nothing but masks (below kMasked) is
+// empty: lse -inf.  (Its lse could not tell ln S from 0, and a gradient from it would be m times too large.)
+#include <algorithm>
+
+#include "ops_device.hpp"
+
+namespace hwr {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.693147180559945309417f;
+// the lowest finite values of bf16 and fp32 are below (-3.30e38)
+constexpr float kMasked = -0x1.Fp127f;
+// exp2 of less is 0 in fp32; products of it with a difference of logits stay finite
+constexpr float kFar = -200.0f;
+
+template <class E>
+constexpr int kEpc = Elem<E>::kEpc;
+
+template <class E>
+__device__ inline void unpack(u32x4 v, float (&f)[kEpc<E>]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(E) == 2) {
+            f[2 * i] = __uint_as_float(v[i] << 16);
+            f[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u);
+        } else {
+            f[i] = __uint_as_float(v[i]);
+        }
+    }
+}
+
+// Elements [0, n) of a row from p on: single ones up to an address of whole chunks, chunks,
+// and single ones after them.
+template <class E>
+struct Span {
+    const E *p;
+    int n, head, chunks;
+    __device__ Span(const E *at, int len) : p(at), n(len) {
+        head = min(len, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(at) & 15)) & 15) / static_cast<int>(sizeof(E)));
+        chunks = (len - head) / kEpc<E>;
+    }
+    // the i-th single element, or -1 (there are fewer than 2 kEpc)
+    __device__ int single(int i) const {
+        const int e = i < head ? i : i + chunks * kEpc<E>;
+        return e < n && i < 2 * kEpc<E> ? e : -1;
+    }
+    __device__ int first(int chunk) const { return head + chunk * kEpc<E>; }
+    __device__ u32x4 load(int chunk) const { return *reinterpret_cast<const u32x4 *>(p + first(chunk)); }
+};
+
+// M, S and T of some elements; M at least kMasked, so that S = 0 tells that there is no
+// element, or that all are masks.
+struct Sums {
+    float m = kMasked, s = 0.0f, t = 0.0f;
+    // elements of which m is at least the maximum, after rescale
+    __device__ void add(float x, float c2) {
+        const float d = (x - m) * c2, e = __builtin_amdgcn_exp2f(d);
+        s += e;
+        t = fmaf(e, fmaxf(d, kFar), t);
+    }
+    // sums relative to a maximum that is no smaller
+    __device__ void rescale(float to, float c2) {
+        const float d = fmaxf((m - to) * c2, kFar), f = __builtin_amdgcn_exp2f(d);
+        t = f * fmaf(s, d, t);
+        s *= f;
+        m = to;
+    }
+    __device__ void join(float m2, float s2, float t2, float c2) {
+        Sums o;
+        o.m = m2, o.s = s2, o.t = t2;
+        const float to = fmaxf(m, m2);
+        rescale(to, c2);
+        o.rescale(to, c2);
+        s += o.s;
+        t += o.t;
+    }
+};
+
+// Order of the most likely tokens: larger logits first, of equal ones the lower token.  Both
+// zeros are equal.  (A NaN has a place in the order too, so that there are always enough.)
+__device__ inline uint32_t order_key(float x) {
+    if (x != x) return 0xFFFFFFFFu;
+    const uint32_t b = __float_as_uint(x + 0.0f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ inline float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
+__device__ inline uint64_t rank_key(uint32_t key, int token) { return static_cast<uint64_t>(key) << 32 | ~static_cast<uint32_t>(token); }
+
+// Candidates of a team, and what its threads exchange.
+constexpr int kCandidates = 512;
+struct TeamSpace {
+    float m[16], s[16], t[16];
+    float most[256];
+    uint64_t best[16];
+    uint64_t candidate[kCandidates];
+    uint32_t floor;
+    int count;
+};
+
+template <int T>
+__device__ inline void team_sync() {
+    if constexpr (T == 64) wave_lds();
+    else __syncthreads();
+}
+
+// out(rank, key, token) of the `top` first of the row, ranks in any order; T threads, whose largest
+// elements are `most`.
+//
+// The top-th largest of the threads' maxima bounds the top-th largest element from below, and is
+// reached by at least `top` elements: those at or above it are the candidates (a few more than
+// `top` unless values are equal), and only threads whose maximum reaches it look for them.
+// Each candidate's rank is the number of candidates before it.  Where there are more
+// than kCandidates (long runs of equal logits), they are found one by one instead.
+template <class E, int T, class Out>
+__device__ inline void select_top(const Span<E> &row, int offset, int top, float most, TeamSpace &ts, int tid, Out out) {
+    constexpr int kTeams = T > 256 ? 256 : T, kShare = T / kTeams;    // of threads that share a maximum
+    float shared = most;
+#pragma unroll
+    for (int d = 1; d < kShare; d <<= 1) shared = fmaxf(shared, __shfl_xor(shared, d));
+    const int team = tid / kShare;
+    if (tid % kShare == 0) ts.most[team] = shared;
+    if (tid == 0) ts.count = 0, ts.floor = 0;
+    team_sync<T>();
+    if (tid % kShare == 0) {
+        int before = 0;
+        for (int i = 0; i < kTeams; i += 4) {
+            const f32x4 o = *reinterpret_cast<const f32x4 *>(&ts.most[i]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) before += o[j] > shared || (o[j] == shared && i + j < team);
+        }
+        // (kMasked: threads without elements, or with masks alone: all elements are candidates)
+        if (before == top - 1 && shared > kMasked) ts.floor = order_key(shared);
+    }
+    team_sync<T>();
+    const uint32_t floor = ts.floor;
+    auto each = [&](auto visit) {
+        const int e = row.single(tid);
+        if (e >= 0) visit(order_key(static_cast<float>(row.p[e])), offset + e);
+        for (int c = tid; c < row.chunks; c += T) {
+            float f[kEpc<E>];
+            unpack<E>(row.load(c), f);
+#pragma unroll
+            for (int i = 0; i < kEpc<E>; ++i) visit(order_key(f[i]), offset + row.first(c) + i);
+        }
+    };
+    if (floor == 0 || order_key(most) >= floor)
+        each([&](uint32_t key, int token) {
+            if (key < floor) return;
+            const int at = atomicAdd(&ts.count, 1);
+            if (at < kCandidates) ts.candidate[at] = rank_key(key, token);
+        });
+    team_sync<T>();
+    const int count = ts.count;
+    if (count <= kCandidates) {
+        for (int i = tid; i < count; i += T) {
+            const uint64_t mine = ts.candidate[i];
+            int before = 0;
+            for (int j = 0; j < count; ++j) before += ts.candidate[j] > mine;
+            if (before < top) out(before, static_cast<uint32_t>(mine >> 32), static_cast<int>(~static_cast<uint32_t>(mine)));
+        }
+        return;
+    }
+    uint64_t last = ~uint64_t{0};
+    for (int r = 0; r < top; ++r) {
+        uint64_t best = 0;
+        each([&](uint32_t key, int token) {
+            const uint64_t k = rank_key(key, token);
+            if (k < last && k > best) best = k;
+        });
+#pragma unroll
+        for (int d = 32; d; d >>= 1) best = max(best, static_cast<uint64_t>(__shfl_xor(static_cast<unsigned long long>(best), d)));
+        if constexpr (T > 64) {
+            if ((tid & 63) == 0) ts.best[tid >> 6] = best;
+            __syncthreads();
+            for (int w = 0; w < T / 64; ++w) best = max(best, ts.best[w]);
+            __syncthreads();
+        }
+        if (tid == 0) out(r, static_cast<uint32_t>(best >> 32), static_cast<int>(~static_cast<uint32_t>(best)));
+        last = best;
+    }
+}
+
+// Log probability of a logit.
+__device__ inline float log_prob(const ProbsArgs &a, const Sums &v, float log_s, float x) {
+    return v.s == 0.0f || x < kMasked ? v.s == v.s ? -INFINITY : NAN : (x - v.m) * a.scale - log_s;
+}
+
+// The results of a row but the most likely tokens, from its sums.
+template <class E>
+__device__ inline void store_sums(const ProbsArgs &a, int64_t r, const Sums &v, float log_s) {
+    const bool empty = v.s == 0.0f;
+    if (a.lse) a.lse[r] = empty ? -INFINITY : fmaf(v.m, a.scale, log_s);
+    if (a.entropy) a.entropy[r] = empty ? 0.0f : fmaxf(log_s - kLn2 * (v.t / v.s), v.s == v.s ? 0.0f : NAN);
+    if (a.logp) {
+        const int t = a.token[r];
+        float lp = 0.0f;
+        if (static_cast<unsigned>(t) < static_cast<unsigned>(a.m)) {
+            const float x = static_cast<float>(static_cast<const E *>(a.x)[r * a.ldx + t]);
+            lp = log_prob(a, v, log_s, x);
+        }
+        a.logp[r] = lp;
+    }
+}
+
+// Partial results of a row: [n][parts] sums, then [n][parts][top] keys.
+__device__ inline f32x4 *part_sums(const ProbsArgs &a, int64_t r, int part) {
+    return static_cast<f32x4 *>(a.partial) + r * a.parts + part;
+}
+__device__ inline uint64_t *part_top(const ProbsArgs &a, int64_t r, int part) {
+    return reinterpret_cast<uint64_t *>(static_cast<f32x4 *>(a.partial) + a.n * a.parts) + (r * a.parts + part) * a.top;
+}
+
+// T threads to a row, or to a part of it; 256 / T rows to a workgroup where T is less.
+template <class E, int T>
+__global__ void __launch_bounds__(T < 256 ? 256 : T) k_probs(ProbsArgs a) {
+    constexpr int NT = T < 256 ? 256 : T, kRows = NT / T, U = 4;
+    static_assert(T == 64 || kRows == 1);
+    __shared__ TeamSpace space[kRows];
+    const int tid = threadIdx.x % T, lane = tid & 63;
+    TeamSpace &ts = space[threadIdx.x / T];
+    const int64_t item = static_cast<int64_t>(block_id<NT>()) * kRows + threadIdx.x / T;
+    const int64_t r = kRows > 1 ? item : item / a.parts;
+    const int part = kRows > 1 ? 0 : static_cast<int>(item % a.parts);
+    if (r >= a.n) return;
+    const int first = static_cast<int>(static_cast<int64_t>(a.m) * part / a.parts);
+    const int last = static_cast<int>(static_cast<int64_t>(a.m) * (part + 1) / a.parts);
+    const Span<E> row(static_cast<const E *>(a.x) + r * a.ldx + first, last - first);
+    const float c2 = a.scale * kLog2e;
+
+    Sums v;
+    if (const int e = row.single(tid); e >= 0) {
+        const float x = static_cast<float>(row.p[e]);
+        v.m = fmaxf(v.m, x);
+        v.add(x, c2);
+    }
+    for (int c = tid; c < row.chunks; c += U * T) {
+        u32x4 in[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t none = sizeof(E) == 2 ? 0xFF80FF80u : 0xFF800000u;      // -inf
+            in[u] = u32x4{none, none, none, none};
+            if (c + u * T < row.chunks) in[u] = row.load(c + u * T);
+        }
+        float f[U][kEpc<E>], most = v.m;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            unpack<E>(in[u], f[u]);
+#pragma unroll
+            for (int i = 0; i < kEpc<E>; ++i) most = fmaxf(most, f[u][i]);
+        }
+        v.rescale(most, c2);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < kEpc<E>; ++i) v.add(f[u][i], c2);
+    }
+
+    const float mine = v.m;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) v.join(__shfl_xor(v.m, d), __shfl_xor(v.s, d), __shfl_xor(v.t, d), c2);
+    if constexpr (T > 64) {
+        if (lane == 0) ts.m[tid >> 6] = v.m, ts.s[tid >> 6] = v.s, ts.t[tid >> 6] = v.t;
+        __syncthreads();
+        v = Sums{};
+        for (int w = 0; w < T / 64; ++w) v.join(ts.m[w], ts.s[w], ts.t[w], c2);
+    }
+    const float log_s = logf(v.s);
+    if (a.parts > 1) {
+        if (tid == 0) *part_sums(a, r, part) = f32x4{v.m, v.s, v.t, 0.0f};
+        if (a.top) {
+            uint64_t *out = part_top(a, r, part);    // (a part has more elements than kMaxTop)
+            select_top<E, T>(row, first, a.top, mine, ts, tid,
+                             [&](int rank, uint32_t key, int token) { out[rank] = rank_key(key, token); });
+        }
+        return;
+    }
+    if (tid == 0) store_sums<E>(a, r, v, log_s);
+    if (a.top)
+        select_top<E, T>(row, 0, a.top, mine, ts, tid, [&](int rank, uint32_t key, int token) {
+            if (a.top_logp) a.top_logp[r * a.top + rank] = log_prob(a, v, log_s, key_value(key));
+            if (a.top_token) a.top_token[r * a.top + rank] = token;
+        });
+}
+
+// A row's results from those of its parts.
+constexpr int kMaxParts = 16;
+constexpr int kPartElements = 4096;
+static_assert(kPartElements >= kMaxTop);
+constexpr int kJoinThreads = 256;
+template <class E>
+__global__ void __launch_bounds__(kJoinThreads) k_probs_join(ProbsArgs a) {
+    __shared__ uint64_t key[kMaxParts * kMaxTop];
+    const int64_t r = block_id<kJoinThreads>();
+    const int tid = threadIdx.x;
+    if (r >= a.n) return;
+    const float c2 = a.scale * kLog2e;
+    Sums v;
+    for (int p = 0; p < a.parts; ++p) {
+        const f32x4 o = *part_sums(a, r, p);
+        v.join(o[0], o[1], o[2], c2);
+    }
+    const float log_s = logf(v.s);
+    if (tid == 0) store_sums<E>(a, r, v, log_s);
+    if (!a.top) return;
+    const int count = a.parts * a.top;
+    const uint64_t *top = part_top(a, r, 0);
+    for (int i = tid; i < count; i += kJoinThreads) key[i] = top[i];
+    __syncthreads();
+    for (int i = tid; i < count; i += kJoinThreads) {
+        const uint64_t mine = key[i];
+        int before = 0;
+        for (int j = 0; j < count; ++j) before += key[j] > mine;
+        if (before >= a.top) continue;
+        if (a.top_logp) a.top_logp[r * a.top + before] = log_prob(a, v, log_s, key_value(static_cast<uint32_t>(mine >> 32)));
+        if (a.top_token) a.top_token[r * a.top + before] = static_cast<int>(~static_cast<uint32_t>(mine));
+    }
+}
+
+// dx = scale (dlogp (1[c = t] - p) - dentropy p (ln p + H)), ln p = scale x - lse.  A row without
+// a token has no first term; one that has neither term, or is empty, gets zeros unread.
+template <class E, int T>
+__global__ void __launch_bounds__(256) k_probs_grad(ProbsGradArgs a, int slabs) {
+    constexpr int kRows = 256 / T, U = 4, kSlab = T * U * kEpc<E>;
+    const int tid = threadIdx.x % T;
+    const int64_t item = static_cast<int64_t>(block_id<256>()) * kRows + threadIdx.x / T;
+    const int64_t r = item / slabs;
+    if (r >= a.n) return;
+    const int slab = static_cast<int>(item - r * slabs);
+    const E *x = static_cast<const E *>(a.x) + r * a.ldx;
+    E *dx = static_cast<E *>(a.dx) + r * a.lddx;
+    // chunks are whole in dx
+    const Span<E> row(dx, a.m);
+    const int t = a.token ? a.token[r] : -1;
+    const bool held = static_cast<unsigned>(t) < static_cast<unsigned>(a.m);
+    const float lse = a.lse[r], dl = a.dlogp && held ? a.dlogp[r] : 0.0f;
+    const float dh = a.dentropy ? a.dentropy[r] : 0.0f, h = a.dentropy ? a.entropy[r] : 0.0f;
+    const bool zero = lse == -INFINITY || (dl == 0.0f && dh == 0.0f);
+    const float nl = -dl * a.scale, nh = -dh * a.scale;
+    auto value = [&](float xv, int c) {
+        const float v = fmaf(xv, a.scale, -lse), p = __builtin_amdgcn_exp2f(v * kLog2e);
+        const float g = p * fmaf(nh, fmaxf(v, kFar) + h, nl);
+        return c == t ? g - nl : g;
+    };
+    if (slab == 0) {
+        const int e = row.single(tid);
+        if (e >= 0) dx[e] = static_cast<E>(zero ? 0.0f : value(static_cast<float>(x[e]), e));
+    }
+    const int c0 = slab * U * T + tid;
+    u32x4 in[U];
+    if (!zero) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (c0 + u * T < row.chunks) {
+                const typename Elem<E>::Vec l = *reinterpret_cast<const typename Elem<E>::Vec *>(x + row.first(c0 + u * T));
+                in[u] = u32x4{l[0], l[1], l[2], l[3]};
+            }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (c0 + u * T >= row.chunks) continue;
+        union { u32x4 v; E e[kEpc<E>]; } o;
+        o.v = u32x4{0, 0, 0, 0};
+        const int c = row.first(c0 + u * T);
+        if (!zero) {
+            float f[kEpc<E>];
+            unpack<E>(in[u], f);
+#pragma unroll
+            for (int i = 0; i < kEpc<E>; ++i) o.e[i] = static_cast<E>(value(f[i], c + i));
+        }
+        *reinterpret_cast<u32x4 *>(dx + c) = o.v;
+    }
+}
+
+template <class E, int T>
+hipError_t go(const ProbsArgs &a, hipStream_t s) {
+    constexpr int NT = T < 256 ? 256 : T, kRows = NT / T;
+    const int64_t blocks = kRows > 1 ? (a.n + kRows - 1) / kRows : a.n * a.parts;
+    if (blocks > INT32_MAX - grid_row(NT)) return hipErrorInvalidValue;
+    hipError_t e = launch_kernel(k_probs<E, T>, wide_grid(blocks, NT), dim3(NT), 0, s, a);
+    if (e != hipSuccess || a.parts == 1) return e;
+    return launch_kernel(k_probs_join<E>, wide_grid(a.n, kJoinThreads), dim3(kJoinThreads), 0, s, a);
+}
+template <class E>
+hipError_t pick(const ProbsArgs &a, hipStream_t s) {
+    if (a.m <= 2048) return go<E, 64>(a, s);
+    return go<E, 256>(a, s);
+}
+
+template <class E, int T>
+hipError_t go_grad(const ProbsGradArgs &a, hipStream_t s) {
+    constexpr int kRows = 256 / T, kSlab = T * 4 * kEpc<E>;
+    const int slabs = (a.m + kSlab - 1) / kSlab;
+    const int64_t blocks = (a.n * slabs + kRows - 1) / kRows;
+    if (blocks > INT32_MAX - grid_row(256)) return hipErrorInvalidValue;
+    return launch_kernel(k_probs_grad<E, T>, wide_grid(blocks, 256), dim3(256), 0, s, a, slabs);
+}
+template <class E>
+hipError_t pick_grad(const ProbsGradArgs &a, hipStream_t s) {
+    if (a.m <= 2048) return go_grad<E, 64>(a, s);
+    return go_grad<E, 256>(a, s);
+}
+
+}  // namespace
+
+// Rows are shared where there are fewer than compute units, in parts of at least kPartElements.
+int probs_parts(bool bf16, int64_t n, int m, int cus) {
+    if (m <= 2048) return 1;
+    const int64_t want = (cus + n - 1) / n;
+    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({want, m / kPartElements, kMaxParts})));
+}
+uint64_t probs_bytes(const ProbsArgs &a) {
+    return a.parts > 1 ? static_cast<uint64_t>(a.n) * a.parts * (sizeof(f32x4) + a.top * sizeof(uint64_t)) : 0;
+}
+hipError_t launch_probs(bool bf16, const ProbsArgs &a, hipStream_t s) { return bf16 ? pick<__bf16>(a, s) : pick<float>(a, s); }
+hipError_t launch_probs_grad(bool bf16, const ProbsGradArgs &a, hipStream_t s) {
+    return bf16 ? pick_grad<__bf16>(a, s) : pick_grad<float>(a, s);
+}
+
+}  // namespace hwr

@@ -109,6 +109,32 @@ struct GroupRowsArgs {
     int32_t *hist, *totals;       // [G + 1][blocks], [G + 1] work space
 };
 
+// Log probabilities, entropies and the most likely tokens of rows of logits, and the logits' gradient.
+constexpr int kMaxTop = 32;
+struct ProbsArgs {
+    int64_t n;
+    int m, top;
+    float scale;
+    const void *x;
+    int64_t ldx;                  // elements
+    const int32_t *token;
+    float *logp, *lse, *entropy, *top_logp;
+    int32_t *top_token;
+    int parts;                    // workgroups that share a row (probs_parts)
+    void *partial;                // with parts > 1: probs_bytes
+};
+struct ProbsGradArgs {
+    int64_t n;
+    int m;
+    float scale;
+    const void *x;
+    int64_t ldx;
+    const int32_t *token;
+    const float *lse, *dlogp, *entropy, *dentropy;
+    void *dx;
+    int64_t lddx;
+};
+
 enum class RowsKind { kGrouped, kAdapter };
 
 hipError_t launch_group_rows(const GroupRowsArgs &a, hipStream_t s);
@@ -140,5 +166,9 @@ ColsPlan cols_plan(bool bf16, ColsKind kind, const ColsArgs &a, int cus);
 hipError_t launch_cols(bool bf16, ColsKind kind, const ColsArgs &a, int cus, hipStream_t s);
 // kLowQ and kLowP of the same groups and rank in one launch; both plans direct
 hipError_t launch_cols_low_pair(bool bf16, const ColsArgs &q, const ColsArgs &p, hipStream_t s);
+int probs_parts(bool bf16, int64_t n, int m, int cus);
+uint64_t probs_bytes(const ProbsArgs &a);     // of partial
+hipError_t launch_probs(bool bf16, const ProbsArgs &a, hipStream_t s);
+hipError_t launch_probs_grad(bool bf16, const ProbsGradArgs &a, hipStream_t s);
 
 }  // namespace hwr

@@ -35,7 +35,8 @@ EXPORTS = ["hwr_init", "hwr_update_hw_state", "hwr_route_batch", "hwr_route_batc
            "hwr_probe_mfma_bf16", "hwr_probe_hbm_read", "hwr_probe_hbm_write", "hwr_probe_launch_floor",
            "hwr_probe_feature_log",
            "hwr_ops_init", "hwr_ops_free", "hwr_ops_last_error", "hwr_ops_reserve", "hwr_group_rows",
-           "hwr_grouped_matmul", "hwr_grouped_matmul_grad", "hwr_adapter_matmul", "hwr_adapter_matmul_grad"]
+           "hwr_grouped_matmul", "hwr_grouped_matmul_grad", "hwr_adapter_matmul", "hwr_adapter_matmul_grad",
+           "hwr_log_probs", "hwr_log_probs_grad"]
 
 _STATUS = {0: "HWR_OK", -1: "HWR_ERR_INVALID_ARG", -2: "HWR_ERR_OOM", -3: "HWR_ERR_HIP",
            -4: "HWR_ERR_STATE", -5: "HWR_ERR_UNSUPPORTED"}
@@ -146,6 +147,18 @@ class hwr_adapter_grad_args(C.Structure):
                 ("dx", _vp), ("lddx", C.c_int64), ("da", _vp), ("db", _vp)]
 
 
+class hwr_log_probs_args(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n", C.c_int32), ("m", C.c_int32), ("top", C.c_int32), ("scale", C.c_float),
+                ("x", _vp), ("ldx", C.c_int64), ("token", _vp), ("logp", _vp), ("lse", _vp), ("entropy", _vp),
+                ("top_logp", _vp), ("top_token", _vp)]
+
+
+class hwr_log_probs_grad_args(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n", C.c_int32), ("m", C.c_int32), ("scale", C.c_float), ("x", _vp),
+                ("ldx", C.c_int64), ("token", _vp), ("lse", _vp), ("dlogp", _vp), ("entropy", _vp), ("dentropy", _vp),
+                ("dx", _vp), ("lddx", C.c_int64)]
+
+
 hwr_sim_router_fn = C.CFUNCTYPE(C.c_int32, C.c_void_p, C.POINTER(hwr_hw_state), C.c_int32, C.c_int32,
                                 C.c_int32, _i32p, _f32p, _f32p)
 STATE_DTYPE = np.dtype([("running_q", "<i4"), ("waiting_q", "<i4"), ("kv_util", "<f4"),
@@ -220,6 +233,9 @@ def load(path: Optional[str] = None) -> C.CDLL:
                      ("hwr_adapter_matmul", hwr_adapter_args), ("hwr_adapter_matmul_grad", hwr_adapter_grad_args)):
         getattr(L, fn).restype = C.c_int
         getattr(L, fn).argtypes = [_vp, C.POINTER(hwr_groups), C.POINTER(args)]
+    for fn, args in (("hwr_log_probs", hwr_log_probs_args), ("hwr_log_probs_grad", hwr_log_probs_grad_args)):
+        getattr(L, fn).restype = C.c_int
+        getattr(L, fn).argtypes = [_vp, C.POINTER(args)]
     if path is None:
         _lib = L
     return L
@@ -355,6 +371,14 @@ def hwr_adapter_matmul(ops, groups: hwr_groups, args: hwr_adapter_args) -> None:
 
 def hwr_adapter_matmul_grad(ops, groups: hwr_groups, args: hwr_adapter_grad_args) -> None:
     _check_ops(load().hwr_adapter_matmul_grad(ops, C.byref(groups), C.byref(args)), ops)
+
+
+def hwr_log_probs(ops, args: hwr_log_probs_args) -> None:
+    _check_ops(load().hwr_log_probs(ops, C.byref(args)), ops)
+
+
+def hwr_log_probs_grad(ops, args: hwr_log_probs_grad_args) -> None:
+    _check_ops(load().hwr_log_probs_grad(ops, C.byref(args)), ops)
 
 
 # ---------------------------------------------------------------- convenience

@@ -30,7 +30,7 @@ class _Call:
     """An entry point that takes hwr_groups and a structure of arguments: both are
     packed into one block that stays (a structure made anew for every call took
     about 1 us of a call's 10; a context is not used by two threads at once)."""
-    _CODES = {C.c_int32: "i", C.c_int64: "q", C.c_void_p: "P"}
+    _CODES = {C.c_int32: "i", C.c_int64: "q", C.c_void_p: "P", C.c_float: "f", C.c_double: "d", C.c_uint64: "Q"}
 
     def __init__(self, fn, args):
         codes = ["".join(self._CODES[t] for _, t in s._fields_) for s in (hwr.hwr_groups, args)]
@@ -46,6 +46,23 @@ class _Call:
         except struct.error as e:
             _bad("sizes", f"outside their types ({e})")
         return self._fn(ctx, *self._at)
+
+
+class _Args(_Call):
+    """The same for an entry point without groups."""
+
+    def __init__(self, fn, args):
+        self._block = C.create_string_buffer(C.sizeof(args))
+        self._pack = struct.Struct("@" + "".join(self._CODES[t] for _, t in args._fields_)).pack_into
+        self._fn = C.cast(fn, C.CFUNCTYPE(C.c_int, C.c_void_p, C.c_void_p))
+        self._at = C.addressof(self._block)
+
+    def __call__(self, ctx, *args) -> int:
+        try:
+            self._pack(self._block, 0, *args)
+        except (struct.error, OverflowError) as e:
+            _bad("sizes", f"outside their types ({e})")
+        return self._fn(ctx, self._at)
 
 
 class RoutedOps:
@@ -73,6 +90,8 @@ class RoutedOps:
         self._matmul_grad = _Call(self._lib.hwr_grouped_matmul_grad, hwr.hwr_matmul_grad_args)
         self._adapter = _Call(self._lib.hwr_adapter_matmul, hwr.hwr_adapter_args)
         self._adapter_grad = _Call(self._lib.hwr_adapter_matmul_grad, hwr.hwr_adapter_grad_args)
+        self._log_probs = _Args(self._lib.hwr_log_probs, hwr.hwr_log_probs_args)
+        self._log_probs_grad = _Args(self._lib.hwr_log_probs_grad, hwr.hwr_log_probs_grad_args)
 
     def close(self) -> None:
         if getattr(self, "ctx", None):
@@ -205,6 +224,46 @@ class RoutedOps:
                   self._kinds[dt], k, m, R, dyp, lddy, xp, ldx, wp, ap, bp, sp, dxp, lddx,
                   0 if da is None else self._dense("da", da, dt, (G, k, R)),
                   0 if db is None else self._dense("db", db, dt, (G, R, m)))
+
+    # ------------------------------------------------------------ from logits
+    def _optional(self, name, t, dtype, shape) -> int:
+        return 0 if t is None else self._dense(name, t, dtype, shape)
+
+    def log_probs(self, x, token=None, *, scale=1.0, logp=None, lse=None, entropy=None, top_logp=None, top_token=None) -> None:
+        """Of rows of logits x [n][m], scaled: ``lse`` [n], the log probability ``logp`` [n] of
+        ``token`` [n] int32 (0 where it is outside [0, m)), ``entropy`` [n], and the most likely
+        tokens, ``top_token`` [n][top] int32 and ``top_logp`` [n][top], top at most 32.  Outputs are
+        float32, any may be left out.  Tokens at -inf are not allowed ones."""
+        dt, (n, m) = self._x(x)
+        f32, i32 = self._f32, self._i32
+        xp, ldx = self._rows("x", x, dt, (n, m))
+        some = top_token if top_token is not None else top_logp
+        if some is not None and some.dim() != 2:
+            _bad("top_token, top_logp", f"{some.dim()} dimensions, expected 2")
+        top = 0 if some is None else some.shape[1]
+        if some is not None and top == 0:
+            _bad("top_token, top_logp", "no columns")
+        st = self._log_probs(self.ctx, self._kinds[dt], n, m, top, scale, xp, ldx, self._optional("token", token, i32, (n,)),
+                             self._optional("logp", logp, f32, (n,)), self._optional("lse", lse, f32, (n,)),
+                             self._optional("entropy", entropy, f32, (n,)),
+                             self._optional("top_logp", top_logp, f32, (n, top)),
+                             self._optional("top_token", top_token, i32, (n, top)))
+        if st:
+            raise HwrError(st, hwr.hwr_ops_last_error(self.ctx))
+
+    def log_probs_grad(self, x, token, lse, dlogp, *, entropy=None, dentropy=None, scale=1.0, dlogits) -> None:
+        """Gradient of the logits x [n][m] from those of ``log_probs``' logp (``dlogp`` [n]; None,
+        with token: none) and entropy (``dentropy`` [n], with ``entropy``).  ``dlogits`` may be x."""
+        dt, (n, m) = self._x(x)
+        f32 = self._f32
+        xp, ldx = self._rows("x", x, dt, (n, m))
+        dxp, lddx = self._rows("dlogits", dlogits, dt, (n, m))
+        st = self._log_probs_grad(self.ctx, self._kinds[dt], n, m, scale, xp, ldx,
+                                  self._optional("token", token, self._i32, (n,)), self._dense("lse", lse, f32, (n,)),
+                                  self._optional("dlogp", dlogp, f32, (n,)), self._optional("entropy", entropy, f32, (n,)),
+                                  self._optional("dentropy", dentropy, f32, (n,)), dxp, lddx)
+        if st:
+            raise HwrError(st, hwr.hwr_ops_last_error(self.ctx))
 
 
 def example(steps: int = 5, n: int = 4096, seed: int = 7) -> list:

@@ -1,0 +1,431 @@
+"""Log probabilities, entropies and most likely tokens of rows of logits, and the logits'
+gradient (include/hwr_ops.h), against 64 bits: widths from one token to long rows, odd and
+strided ones, shared and whole rows; masks of infinities and of the type's lowest value that
+leave a few tokens, one or none; equal logits; NaNs; refusals; other streams and graphs.
+
+Tolerances, with u = 2^-24, R the range of a row's scaled logits that are not masked, E the mean
+distance of them from the largest (of the distribution).  An exponent (x - M) scale log2 e is off by
+4 u of itself, an exponential by 2 u of itself besides; a thread adds at most m / 64 of a short
+row's or m / 256 of a long row's terms, and its sums are rescaled and joined a few times, each by 3 u and
+4 u of the distance:
+  S, relative:  a = u (8 R + min(m, 2048) / 64 + m / 256 + 64)
+  lse, log p:   a + 4 u (|value| + ln S + 1)
+  entropy:      a + E (2 a + 8 u) + 4 u (ln S + 1)
+  gradient:     scale u (p (3 |v| + 8) (|dlogp| + |dentropy| (|v| + |H|)) + 2 |dlogp| at the token)
+                and half a step of its type, v = ln p."""
+import math
+
+import numpy as np
+import pytest
+
+from paper_2608_14575_amd import hwr, routed
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+TYPES = {"bf16": (torch.bfloat16, 2.0 ** -8), "f32": (torch.float32, 2.0 ** -24)}
+U = 2.0 ** -24
+MASKED = -3.3e38
+
+
+@pytest.fixture(scope="module")
+def ops():
+    assert torch.cuda.is_available(), "GPU tests need a device"
+    o = routed.RoutedOps(stream=torch.cuda.current_stream().cuda_stream)
+    yield o
+    o.close()
+
+
+def logits(n, m, dtype, mask, seed, pad=0):
+    g = torch.Generator("cuda").manual_seed(seed)
+    x = torch.randn((n, m), generator=g, device="cuda") * 2.5
+    rnd = torch.rand((n, m), generator=g, device="cuda")
+    if mask == "some":
+        x[rnd < 0.1] = -math.inf
+    elif mask == "most":                  # a handful of tokens left, in some rows none
+        x[rnd > 3.0 / m] = -math.inf
+    elif mask == "lowest":
+        x[rnd < 0.5] = torch.finfo(dtype).min
+        x[::3] = torch.finfo(dtype).min
+    elif mask == "one":
+        keep = torch.randint(0, m, (n,), generator=g, device="cuda")
+        x.masked_fill_(torch.arange(m, device="cuda")[None] != keep[:, None], -math.inf)
+    elif mask == "equal":                 # long runs of equal logits, in some rows all
+        x = torch.round(x / 4)
+        x[::2] = 1.5
+    elif mask == "zeros":                 # of both signs
+        x = torch.where(rnd < 0.5, 0.0, -0.0)
+    buf = torch.full((n, m + pad), float("nan"), dtype=dtype, device="cuda")
+    buf[:, :m] = x.to(dtype)
+    token = torch.randint(0, m, (n,), generator=g, device="cuda", dtype=torch.int32)
+    token[1::7] = -100
+    token[3::11] = m
+    return buf[:, :m], token
+
+
+def expected(x, token, scale):
+    """In 64 bits: lse, logp, entropy, and what the tolerances need."""
+    z = torch.where(x.double() < MASKED, -math.inf, x.double() * scale)
+    m = z.shape[1]
+    most = z.amax(1)
+    empty = most == -math.inf
+    d = z - torch.where(empty, 0.0, most)[:, None]
+    e = d.exp()
+    s = e.sum(1)
+    ln_s = torch.where(empty, 0.0, s.log())
+    lse = torch.where(empty, -math.inf, most + ln_s)
+    mean = torch.where(empty, 0.0, -torch.where(e > 0, e * d, 0.0).sum(1) / torch.where(empty, 1.0, s))
+    held = (token >= 0) & (token < m)
+    zt = z.gather(1, token.long().clamp(0, m - 1)[:, None])[:, 0]
+    logp = torch.where(held, torch.where(empty, -math.inf, zt - lse), 0.0)
+    span = torch.where(empty, 0.0, torch.where(z > -math.inf, -d, 0.0).amax(1))
+    a = U * (8 * span + min(m, 2048) / 64 + m / 256 + 64)
+    return {"z": z, "lse": lse, "logp": logp, "entropy": ln_s + mean, "ln_s": ln_s, "mean": mean, "a": a, "empty": empty}
+
+
+def close(name, got, ref, tol):
+    got, ref, tol = got.double(), ref.double(), tol.double().expand_as(ref)
+    same = (got == ref) | (got.isnan() & ref.isnan())
+    bad = ~same & ~((got - ref).abs() <= tol)
+    assert not bad.any(), (f"{name}: {int(bad.sum())} of {bad.numel()} off, worst "
+                           f"{((got - ref).abs() / tol)[bad].max():.3g} of the tolerance, first {got[bad][0]} for {ref[bad][0]}")
+
+
+def outputs(n, top):
+    f = lambda *s: torch.full(s, 7.0, device="cuda")  # noqa: E731
+    o = {"logp": f(n), "lse": f(n), "entropy": f(n)}
+    if top:
+        o.update(top_logp=f(n, top), top_token=torch.full((n, top), -7, dtype=torch.int32, device="cuda"))
+    return o
+
+
+def check(x, token, scale, top, o):
+    w = expected(x, token, scale)
+    near = lambda v: w["a"] + 4 * U * (torch.nan_to_num(v, posinf=0.0, neginf=0.0).abs() + w["ln_s"] + 1)  # noqa: E731
+    close("lse", o["lse"], w["lse"], near(w["lse"]))
+    close("logp", o["logp"], w["logp"], near(w["logp"]))
+    close("entropy", o["entropy"], w["entropy"], w["a"] + w["mean"] * (2 * w["a"] + 8 * U) + 4 * U * (w["ln_s"] + 1))
+    if top:
+        at = torch.sort(x.float(), dim=1, descending=True, stable=True)[1][:, :top]
+        assert torch.equal(o["top_token"].long(), at)
+        want = torch.where(w["empty"][:, None], -math.inf, w["z"].gather(1, at) - w["lse"][:, None])
+        finite = torch.nan_to_num(want, neginf=0.0).abs()
+        close("top_logp", o["top_logp"], want, w["a"][:, None] + 4 * U * (finite + w["ln_s"][:, None] + 1))
+    return w
+
+
+def differ(x, token, w, scale, dlogp, ent, dent):
+    """The gradient in 64 bits and its tolerance, from the lse and entropy that the call is given."""
+    lse = w["lse"].float().double()
+    v = w["z"] - torch.where(w["empty"], 0.0, lse)[:, None]
+    p = torch.where(w["empty"][:, None], 0.0, v.exp())
+    v = torch.where(p > 0, v, 0.0)
+    m = x.shape[1]
+    held = ((token >= 0) & (token < m) & ~w["empty"])
+    dl = torch.where(held, dlogp.double(), 0.0) if dlogp is not None else torch.zeros_like(lse)
+    dh = torch.where(w["empty"], 0.0, dent.double()) if dent is not None else torch.zeros_like(lse)
+    h = ent.double() if ent is not None else torch.zeros_like(lse)
+    hit = torch.zeros_like(v).scatter_(1, token.long().clamp(0, m - 1)[:, None], 1.0) * held[:, None]
+    d = scale * (dl[:, None] * (hit - p) - dh[:, None] * p * (v + h[:, None]))
+    dl, dh, h = dl.abs()[:, None], dh.abs()[:, None], h.abs()[:, None]
+    tol = scale * U * (p * (3 * v.abs() + 8) * (dl + dh * (v.abs() + h)) + 2 * dl * hit)
+    return d, tol + TYPES["bf16" if x.dtype == torch.bfloat16 else "f32"][1] * d.abs() + 1e-37
+
+
+# rows, tokens, top, scale, mask, padding of the rows
+SHAPES = [
+    (1, 1, 1, 1.0, "none", 0), (3, 2, 2, 2.0, "none", 3), (1, 96, 5, 1.0, "none", 0), (70, 97, 32, 0.7, "some", 1),
+    (5, 255, 20, 1.0, "most", 0), (33, 2048, 20, 1.25, "none", 0), (33, 2049, 20, 1.25, "none", 0), (9, 2047, 32, 1.0, "equal", 5),
+    (1, 32000, 5, 1.0, "none", 0), (48, 32003, 20, 0.5, "some", 0), (7, 50000, 20, 1.0, "most", 8), (6, 9001, 32, 1.0, "lowest", 0),
+    (260, 10007, 7, 0.8, "some", 0), (257, 4096, 0, 1.0, "lowest", 4), (11, 4099, 1, 1.0, "one", 0), (9, 128, 3, 3.0, "one", 0),
+    (2, 160001, 32, 1.0, "none", 0), (2, 131072, 32, 1.0, "equal", 0), (300, 3000, 13, 1.0, "equal", 2), (40, 5000, 9, 1.0, "zeros", 0),
+    (301, 700, 9, 1.0, "zeros", 0), (5, 33, 32, 1.0, "most", 0), (300, 8193, 20, 1.0, "most", 0),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,m,top,scale,mask,pad", SHAPES)
+def test_log_probs_and_gradient(ops, n, m, top, scale, mask, pad, dtype):
+    x, token = logits(n, m, TYPES[dtype][0], mask, n * 7 + m, pad)
+    o = outputs(n, top)
+    ops.log_probs(x, token, scale=scale, **o)
+    again = outputs(n, top)
+    ops.log_probs(x, token, scale=scale, **again)
+    assert all(torch.equal(o[k], again[k]) for k in o)
+    w = check(x, token, scale, top, o)
+    g = torch.Generator("cuda").manual_seed(m)
+    dlogp, dent = (torch.randn(n, generator=g, device="cuda") for _ in range(2))
+    ent = w["entropy"].float()
+    for with_p, with_h in ((True, True), (True, False), (False, True)):
+        args = (dlogp if with_p else None, ent if with_h else None, dent if with_h else None)
+        buf = torch.full((n, m + pad), 7.0, dtype=x.dtype, device="cuda")
+        ops.log_probs_grad(x, token if with_p else None, w["lse"].float(), args[0], entropy=args[1], dentropy=args[2], scale=scale,
+                           dlogits=buf[:, :m])
+        d, tol = differ(x, token, w, scale, *args)
+        close(f"dlogits {with_p} {with_h}", buf[:, :m], d, tol)
+        assert (buf[:, m:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_outputs_one_by_one(ops, dtype):
+    """Every output alone, and logp without the others, are what they are together."""
+    n, m, top = 37, 3001, 6
+    x, token = logits(n, m, TYPES[dtype][0], "some", 5)
+    o = outputs(n, top)
+    ops.log_probs(x, token, **o)
+    for k in o:
+        alone = torch.empty_like(o[k])
+        ops.log_probs(x, token if k == "logp" else None, **{k: alone})
+        assert torch.equal(alone, o[k]), k
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,m", [(3, 1000), (3, 20001), (300, 5000)])
+def test_pointers_aligned_to_their_elements_alone(ops, n, m, dtype):
+    t = TYPES[dtype][0]
+    x, token = logits(n, m, t, "some", 3)
+    for off in range(1, 16 // x.element_size()):
+        flat = torch.full((n * m + 32,), float("nan"), dtype=t, device="cuda")
+        y = flat[off:off + n * m].view(n, m)
+        y.copy_(x)
+        o = outputs(n, 4)
+        ops.log_probs(y, token, **o)
+        w = check(x, token, 1.0, 4, o)
+        dflat = torch.full((n * m + 32,), 7.0, dtype=t, device="cuda")
+        d = dflat[off + 1:off + 1 + n * m].view(n, m)
+        dlogp = torch.linspace(-1, 1, n, device="cuda")
+        ops.log_probs_grad(y, token, w["lse"].float(), dlogp, dlogits=d)
+        close("dlogits", d, *differ(x, token, w, 1.0, dlogp, None, None))
+        assert (dflat[:off + 1] == 7.0).all() and (dflat[off + 1 + n * m:] == 7.0).all()
+
+
+def test_values_stay_in_their_rows(ops):
+    """NaNs and infinities above make their row's results NaN, and no other's; its tokens are listed once each."""
+    n, m, top = 12, 5003, 8
+    for dtype in (torch.bfloat16, torch.float32):
+        x, token = logits(n, m, dtype, "some", 9)
+        token[:] = 17
+        x[2, 4000] = float("nan")
+        x[5, 17] = math.inf
+        x[7] = float("nan")
+        o = outputs(n, top)
+        ops.log_probs(x, token, **o)
+        sick = torch.tensor([i in (2, 5, 7) for i in range(n)], device="cuda")
+        for k in ("lse", "logp", "entropy"):
+            assert o[k][sick].isnan().all() and not o[k][~sick].isnan().any(), k
+        assert o["top_logp"][sick].isnan().all()
+        clean = x[~sick]
+        check(clean, token[~sick], 1.0, top, {k: v[~sick] for k, v in o.items()})
+        t = o["top_token"].long()
+        assert ((t >= 0) & (t < m)).all() and all(len(set(r.tolist())) == top for r in t)
+        d = torch.empty_like(x)
+        ops.log_probs_grad(x, token, o["lse"], torch.ones(n, device="cuda"), dlogits=d)
+        assert d[sick].isnan().all() and not d[~sick].isnan().any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gradient_in_place(ops, dtype):
+    n, m = 19, 4001
+    x, token = logits(n, m, TYPES[dtype][0], "some", 21, 7)
+    w = expected(x, token, 1.0)
+    dlogp = torch.linspace(-1, 1, n, device="cuda")
+    apart = torch.empty(n, m, dtype=x.dtype, device="cuda")
+    ops.log_probs_grad(x, token, w["lse"].float(), dlogp, dlogits=apart)
+    ops.log_probs_grad(x, token, w["lse"].float(), dlogp, dlogits=x)
+    assert torch.equal(x, apart)
+
+
+def test_gradient_is_the_difference(ops):
+    """sum of a logp + b H through the operators, differences in 64 bits of the formula."""
+    n, m, scale = 4, 37, 0.8
+    x, token = logits(n, m, torch.float32, "none", 2)
+    token[:] = torch.tensor([0, 36, -1, 5])
+    a, b = torch.linspace(-1, 1, n, device="cuda"), torch.linspace(0.5, -0.5, n, device="cuda")
+    o = outputs(n, 0)
+    ops.log_probs(x, token, scale=scale, **o)
+    d = torch.empty_like(x)
+    ops.log_probs_grad(x, token, o["lse"], a, entropy=o["entropy"], dentropy=b, scale=scale, dlogits=d)
+
+    def value(x):
+        w = expected(x, token, scale)
+        return (a.double() * w["logp"] + b.double() * w["entropy"]).sum()
+
+    h, x64 = 1e-4, x.double()
+    for r in range(n):
+        for c in range(m):
+            step = torch.zeros_like(x64)
+            step[r, c] = h
+            slope = (value(x64 + step) - value(x64 - step)) / (2 * h)
+            assert abs(float(slope - d[r, c])) < 1e-5      # h^2 / 6 of a third derivative below 6, and fp32 results' 1e-6
+
+
+def test_agrees_with_autograd(ops):
+    """In an autograd function: cross entropy of rows with and without a token."""
+    class LogProbs(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, token):
+            logp, lse = (torch.empty(x.shape[0], device="cuda") for _ in range(2))
+            ops.log_probs(x, token, logp=logp, lse=lse)
+            ctx.save_for_backward(x, token, lse)
+            return logp
+
+        @staticmethod
+        def backward(ctx, dlogp):
+            x, token, lse = ctx.saved_tensors
+            dx = torch.empty_like(x)
+            ops.log_probs_grad(x, token, lse, dlogp.contiguous(), dlogits=dx)
+            return dx, None
+
+    x, token = logits(50, 501, torch.float32, "none", 4)
+    x = x.contiguous().requires_grad_()
+    (-LogProbs.apply(x, token).sum()).backward()
+    y = x.detach().double().requires_grad_()
+    held = (token >= 0) & (token < 501)
+    torch.nn.functional.cross_entropy(y[held], token[held].long(), reduction="sum").backward()
+    # p within (3 |v| + 8) u and the lse's own a: v below 25 here
+    assert (x.grad.double() - y.grad).abs().max() < (3 * 25 + 8 + 8 * 25 + 128) * U
+
+
+def test_empty_batch(ops):
+    x = torch.empty(0, 100, device="cuda")
+    i, f = torch.empty(0, dtype=torch.int32, device="cuda"), torch.empty(0, device="cuda")
+    ops.log_probs(x, i, logp=f, lse=f, top_token=torch.empty(0, 3, dtype=torch.int32, device="cuda"))
+    ops.log_probs_grad(x, i, f, f, dlogits=torch.empty_like(x))
+
+
+def test_rows_past_32_bit_offsets(ops):
+    n, m = 70001, 33000                      # 2.3e9 logits
+    x = torch.zeros(n, m, dtype=torch.bfloat16, device="cuda")
+    rows = [0, 65075, 65076, 70000]          # either side of 2^31 elements, and the last
+    ref, token = logits(4, m, torch.bfloat16, "some", 6)
+    x[rows] = ref
+    tokens = torch.zeros(n, dtype=torch.int32, device="cuda")
+    tokens[rows] = token
+    o = outputs(n, 5)
+    ops.log_probs(x, tokens, **o)
+    w = check(ref, token, 1.0, 5, {k: v[rows] for k, v in o.items()})
+    assert abs(float(o["lse"][40000]) - math.log(m)) < 1e-4 and o["top_token"][40000].tolist() == [0, 1, 2, 3, 4]
+    lse = o["lse"].clone()
+    lse[rows] = w["lse"].float()
+    dlogp = torch.ones(n, device="cuda")
+    ops.log_probs_grad(x, tokens, lse, dlogp, dlogits=x)
+    close("dlogits", x[rows], *differ(ref, token, w, 1.0, dlogp[rows], None, None))
+
+
+def test_other_stream_and_graph(ops):
+    s = torch.cuda.Stream()
+    mine = routed.RoutedOps(stream=s.cuda_stream)
+    n, m, top = 20, 40000, 5
+    x, token = logits(n, m, torch.bfloat16, "some", 1)
+    dlogp = torch.linspace(-1, 1, n, device="cuda")
+    o, d = outputs(n, top), torch.empty(n, m, dtype=torch.bfloat16, device="cuda")
+    s.wait_stream(torch.cuda.current_stream())
+
+    def step():
+        mine.log_probs(x, token, **o)
+        mine.log_probs_grad(x, token, o["lse"], dlogp, dlogits=d)
+
+    with torch.cuda.stream(s):
+        step()
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        step()
+    for seed in range(3):
+        new, _ = logits(n, m, torch.bfloat16, "some", 100 + seed)
+        x.copy_(new)
+        for v in o.values():
+            v.fill_(3)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        check(x, token, 1.0, top, o)
+        eager, ed = outputs(n, top), torch.empty_like(d)
+        ops.log_probs(x, token, **eager)
+        ops.log_probs_grad(x, token, eager["lse"], dlogp, dlogits=ed)
+        assert all(torch.equal(o[k], eager[k]) for k in o) and torch.equal(d, ed)
+    mine.close()
+
+
+def test_capture_needs_reserved_space():
+    s = torch.cuda.Stream()
+    fresh = routed.RoutedOps(stream=s.cuda_stream)
+    x, token = logits(2, 40000, torch.bfloat16, "none", 1)
+    o = outputs(2, 5)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        with pytest.raises(hwr.HwrError) as e:
+            fresh.log_probs(x, token, **o)
+        assert e.value.status == hwr.HWR_ERR_STATE
+        x.add_(0)
+    fresh.reserve(1 << 16)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        fresh.log_probs(x, token, **o)
+    graph.replay()
+    torch.cuda.synchronize()
+    check(x, token, 1.0, 5, o)
+    fresh.close()
+
+
+def test_refusals(ops):
+    n, m = 4, 50
+    x, token = logits(n, m, torch.float32, "none", 1)
+    x = x.contiguous()
+    f = lambda *s: torch.empty(s, device="cuda")  # noqa: E731
+    i = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")  # noqa: E731
+
+    def refused(what, call, *args, **kw):
+        with pytest.raises(hwr.HwrError) as e:
+            call(*args, **kw)
+        assert e.value.status == hwr.HWR_ERR_INVALID_ARG and what in str(e.value), str(e.value)
+
+    refused("no output", ops.log_probs, x, token)
+    refused("token for logp", ops.log_probs, x, logp=f(n))
+    refused("x: dtype", ops.log_probs, x.half(), token, lse=f(n))
+    refused("x: 1 dim", ops.log_probs, x[0], token, lse=f(n))
+    refused("token: dtype", ops.log_probs, x, token.long(), logp=f(n))
+    refused("lse: shape", ops.log_probs, x, lse=f(n + 1))
+    refused("lse: on cpu", ops.log_probs, x, lse=torch.empty(n))
+    refused("top outside", ops.log_probs, x, top_token=i(n, 33))
+    refused("top outside", ops.log_probs, x[:, :3].contiguous(), top_token=i(n, 4))
+    refused("no columns", ops.log_probs, x, top_token=i(n, 0))
+    refused("top_logp: shape", ops.log_probs, x, top_token=i(n, 3), top_logp=f(n, 4))
+    refused("strides", ops.log_probs, x.t().contiguous().t(), lse=f(n))
+    for scale in (0.0, -1.0, math.inf, math.nan, 1e-30, 1e300):
+        refused("scale outside", ops.log_probs, x, lse=f(n), scale=scale)
+        refused("scale outside", ops.log_probs_grad, x, token, f(n), f(n), dlogits=f(n, m), scale=scale)
+    refused("m outside", ops.log_probs, f(n, 0), lse=f(n))
+    refused("dlogp or dentropy", ops.log_probs_grad, x, token, f(n), None, dlogits=f(n, m))
+    refused("go together", ops.log_probs_grad, x, token, f(n), f(n), entropy=f(n), dlogits=f(n, m))
+    refused("go together", ops.log_probs_grad, x, token, f(n), f(n), dentropy=f(n), dlogits=f(n, m))
+    refused("token is required", ops.log_probs_grad, x, None, f(n), f(n), dlogits=f(n, m))
+    refused("dlogits: dtype", ops.log_probs_grad, x, token, f(n), f(n), dlogits=f(n, m).bfloat16())
+    wide = f(n, m + 6)
+    refused("row stride", ops.log_probs_grad, wide[:, :m], token, f(n), f(n), dlogits=wide.view(-1)[:n * m].view(n, m))
+
+
+@pytest.mark.parametrize("n,m", [(1, 16777216), (1, 16777213)])
+def test_longest_rows(ops, n, m):
+    x = torch.zeros(n, m, dtype=torch.bfloat16, device="cuda")
+    x[0, m - 1] = 10.0
+    o = outputs(n, 3)
+    ops.log_probs(x, torch.tensor([m - 1], dtype=torch.int32, device="cuda"), **o)
+    assert o["top_token"][0].tolist() == [m - 1, 0, 1]
+    assert abs(float(o["lse"]) - math.log(m - 1 + math.exp(10))) < U * (m / 256 + 500)
+    with pytest.raises(hwr.HwrError):
+        big = torch.empty(1, 16777217, dtype=torch.bfloat16, device="cuda")
+        ops.log_probs(big, lse=torch.empty(1, device="cuda"))
+
+
+def test_many_rows(ops):
+    """More rows than a row of the grid has workgroups."""
+    n, m = 16777216 + 77, 3
+    x = torch.zeros(n, m, dtype=torch.bfloat16, device="cuda")
+    x[-1] = torch.tensor([1.0, 3.0, 2.0])
+    lse = torch.empty(n, device="cuda")
+    tok = torch.empty(n, 2, dtype=torch.int32, device="cuda")
+    ops.log_probs(x, lse=lse, top_token=tok)
+    assert (lse[:-1] - math.log(3)).abs().max() < 1e-6 and tok[-1].tolist() == [1, 2] and (tok[:-1] == torch.tensor([0, 1], device="cuda", dtype=torch.int32)).all()
+    assert np.isclose(float(lse[-1]), math.log(math.e + math.e ** 2 + math.e ** 3), rtol=1e-6)

@@ -21,6 +21,7 @@
  *   hwr_log_probs            of rows of logits: the log probability of a given token,
  *                            the entropy, the most likely tokens
  *   hwr_log_probs_grad       the gradient of the logits
+ *   hwr_adamw_step           one step of AdamW over many tensors
  *
  * Groups.  `order` lists the rows of group 0, then of group 1, ..., and last
  * the rows in no group; group g has the places offsets[g] .. offsets[g+1]-1,
@@ -193,6 +194,57 @@ typedef struct {
     void *dx; int64_t lddx;       /* [n][m]                                     */
 } hwr_log_probs_grad_args;
 hwr_status hwr_log_probs_grad(hwr_ops *ops, const hwr_log_probs_grad_args *a);
+
+/* AdamW.  A step number t over all values of some tensors at once, in fp32:
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * Weights p and gradients g are of one type.  Weights in HWR_BF16 have an fp32 master, which
+ * is what is stepped (p is its rounding), or none: p is then rounded up or down at random.
+ * States have 32 bits, m and v in fp32; or 8: e4m3 (1 sign, 4 exponent, 3 mantissa bits, no
+ * infinities) with an fp32 scale for every 256 values of a tensor from its first on, rounded up or
+ * down at random, and sqrt(v) in place of v.  Each is the stored value times its scale.  Zeros
+ * (with any finite scales) are a beginning for all.  A block of which every value is below 2^-100
+ * becomes zeros.
+ * The random numbers are a function of seed, t and the value's number (tensors are numbered
+ * one after the other, each from a multiple of 256 on): the same call gives the same bits.
+ * A NaN or infinity in g stays in its value, with states of 8 bits in its block of 256.
+ *
+ * hwr_adamw_init keeps what it needs of the tensors' addresses and sizes (not their contents) in
+ * device memory; their memory has to stay until hwr_adamw_free.  Nothing that is written may overlap
+ * anything else.  It copies from the host and waits: not under capture.  hwr_adamw_free waits for the
+ * device; the context may be freed before. */
+typedef struct hwr_adamw hwr_adamw;   /* opaque, owned by the library */
+
+typedef struct {
+    int64_t count;                /* values, 0..2^40                            */
+    void *p;                      /* [count]                                    */
+    const void *g;                /* [count]                                    */
+    float *master;                /* [count]; all tensors of a step or none     */
+    void *m, *v;                  /* [count]                                    */
+    float *m_scale, *v_scale;     /* [(count + 255) / 256]; 8 bits              */
+} hwr_adamw_tensor;
+
+typedef struct {
+    int32_t dtype;                /* hwr_dtype of p and g                       */
+    int32_t bits;                 /* of m and v: 8 or 32                        */
+    int32_t n_tensors;            /* 0..1048576                                 */
+    const hwr_adamw_tensor *tensors;   /* host memory, not kept                 */
+} hwr_adamw_config;
+hwr_status hwr_adamw_init(hwr_ops *ops, const hwr_adamw_config *config, hwr_adamw **out);
+void hwr_adamw_free(hwr_adamw *adamw);
+
+typedef struct {
+    double lr, beta1, beta2;      /* lr 0 or more; betas in [0, 1)              */
+    double eps, weight_decay;     /* eps in [0, 1); weight_decay 0 or more      */
+    uint64_t seed;
+    int64_t step;                 /* t, 1 or more                               */
+    int64_t *steps;               /* or, in device memory, the steps before this one: counted up
+                                     by the call, which may then be captured (without, a captured
+                                     call is HWR_ERR_STATE); step is not read   */
+    const float *lr_device;       /* with steps: in place of lr, or NULL        */
+} hwr_adamw_args;
+/* On the stream of ops, a context of the device that the adamw was made on. */
+hwr_status hwr_adamw_step(hwr_ops *ops, hwr_adamw *adamw, const hwr_adamw_args *a);
 
 #ifdef __cplusplus
 }

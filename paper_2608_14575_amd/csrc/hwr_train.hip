@@ -1,11 +1,24 @@
-// Host side of what follows the products in a training step (hwr_ops.h): log probabilities and
-// the logits' gradient.
+// Host side of what follows the products in a training step (hwr_ops.h): log probabilities,
+// the logits' gradient, and the step of the weights.
 #include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <memory>
 
 #include "ops_context.hpp"
 #include "ops_internal.hpp"
 
 using namespace hwr;
+
+struct hwr_adamw {
+    int dev = 0;
+    bool bf16 = false, master = false, states8 = false;
+    int64_t n_chunks = 0;
+    uint64_t chunks_at = 0;       // byte of memory
+    char *memory = nullptr;       // coefficients, tensors, chunks
+    AdamwCoef *coef() const { return reinterpret_cast<AdamwCoef *>(memory); }
+};
 
 namespace {
 
@@ -88,9 +101,155 @@ hwr_status log_probs_grad(hwr_ops *c, const hwr_log_probs_grad_args *a) {
     return HWR_OK;
 }
 
+// ---------------------------------------------------------------- AdamW
+constexpr uint64_t kCoefBytes = 256;
+constexpr int kMaxTensors = 1 << 20;
+constexpr int64_t kMaxValues = int64_t{1} << 40;
+
+// Bytes that a step reads or writes: [at, end).
+struct Range {
+    uintptr_t at, end;
+    bool written;
+};
+
+hwr_status adamw_init(hwr_ops *c, const hwr_adamw_config *f, hwr_adamw **out) {
+    if (!c) return invalid(nullptr, "ops is NULL");
+    if (!out) return invalid(c, "out is NULL");
+    *out = nullptr;
+    if (!f) return invalid(c, "config is NULL");
+    if (f->dtype != HWR_F32 && f->dtype != HWR_BF16) return invalid(c, "unknown dtype");
+    if (f->bits != 8 && f->bits != 32) return invalid(c, "bits other than 8 and 32");
+    if (f->n_tensors < 0 || f->n_tensors > kMaxTensors) return invalid(c, "n_tensors outside 0..1048576");
+    if (f->n_tensors > 0 && !f->tensors) return invalid(c, "tensors is NULL");
+    const bool bf16 = f->dtype == HWR_BF16, states8 = f->bits == 8;
+    const int64_t size = bf16 ? 2 : 4;
+    std::vector<AdamwTensor> tensors;
+    std::vector<AdamwChunk> chunks;
+    std::vector<Range> ranges;
+    bool master = false, first = true;
+    int64_t place = 0;
+    for (int i = 0; i < f->n_tensors; ++i) {
+        const hwr_adamw_tensor &t = f->tensors[i];
+        const std::string which = "tensor " + std::to_string(i) + ": ";
+        auto refuse = [&](const char *m) { return fail(c, HWR_ERR_INVALID_ARG, which + m); };
+        if (t.count < 0 || t.count > kMaxValues) return refuse("count outside 0..2^40");
+        if (t.count == 0) continue;
+        if (!t.p || !t.g || !t.m || !t.v) return refuse("p, g, m and v are required");
+        if (states8 != (t.m_scale != nullptr) || states8 != (t.v_scale != nullptr))
+            return refuse("m_scale and v_scale are required with states of 8 bits, and only then");
+        if (t.master && !bf16) return refuse("a master is for bf16 weights");
+        if (!first && master != (t.master != nullptr)) return refuse("a master for some tensors and not for others");
+        first = false;
+        master = t.master != nullptr;
+        if (misaligned(f->dtype, {t.p, t.g}) || misaligned(HWR_F32, {t.master, t.m_scale, t.v_scale}) ||
+            (!states8 && misaligned(HWR_F32, {t.m, t.v})))
+            return refuse("a pointer is not aligned to its elements");
+        const int64_t blocks = (t.count + kAdamwBlock - 1) / kAdamwBlock, state = states8 ? 1 : 4;
+        auto range = [&](const void *p, int64_t bytes, bool written) {
+            const auto at = reinterpret_cast<uintptr_t>(p);
+            if (p) ranges.push_back({at, at + bytes, written});
+        };
+        range(t.p, t.count * size, true);
+        range(t.g, t.count * size, false);
+        range(t.master, t.count * 4, true);
+        range(t.m, t.count * state, true);
+        range(t.v, t.count * state, true);
+        range(t.m_scale, blocks * 4, true);
+        range(t.v_scale, blocks * 4, true);
+        const int64_t n = (t.count + kAdamwChunk - 1) / kAdamwChunk;
+        if (static_cast<int64_t>(chunks.size()) + n > INT32_MAX / 2) return refuse("more than 2^41 values in all");
+        for (int64_t j = 0; j < n; ++j) chunks.push_back({static_cast<int>(tensors.size()), static_cast<int>(j)});
+        tensors.push_back({t.p, t.g, t.master, t.m, t.v, t.m_scale, t.v_scale, t.count, place});
+        place += blocks * kAdamwBlock;
+    }
+    // nothing that is written may be a part of anything else
+    std::sort(ranges.begin(), ranges.end(), [](const Range &a, const Range &b) { return a.at < b.at; });
+    uintptr_t end = 0, written_end = 0;           // of the ranges so far
+    for (const Range &r : ranges) {
+        if (r.at < (r.written ? end : written_end)) return invalid(c, "tensors overlap (gradients alone may)");
+        end = std::max(end, r.end);
+        if (r.written) written_end = std::max(written_end, r.end);
+    }
+    OPS_ON_DEVICE(c, c->dev);
+    auto a = std::make_unique<hwr_adamw>();
+    a->dev = c->dev;
+    a->bf16 = bf16;
+    a->master = master;
+    a->states8 = states8;
+    a->n_chunks = static_cast<int64_t>(chunks.size());
+    const uint64_t tb = tensors.size() * sizeof(AdamwTensor), cb = chunks.size() * sizeof(AdamwChunk);
+    OPS_HIP(c, hipMalloc(reinterpret_cast<void **>(&a->memory), kCoefBytes + tb + cb));
+    hipError_t e = hipSuccess;
+    if (tb) e = hipMemcpy(a->memory + kCoefBytes, tensors.data(), tb, hipMemcpyHostToDevice);
+    if (e == hipSuccess && cb) e = hipMemcpy(a->memory + kCoefBytes + tb, chunks.data(), cb, hipMemcpyHostToDevice);
+    if (e != hipSuccess) {
+        (void)hipFree(a->memory);
+        return hip_fail(c, e, "hipMemcpy");
+    }
+    a->chunks_at = kCoefBytes + tb;
+    *out = a.release();
+    return HWR_OK;
+}
+
+hwr_status adamw_step(hwr_ops *c, const hwr_adamw *w, const hwr_adamw_args *a) {
+    if (!c) return invalid(nullptr, "ops is NULL");
+    if (!w) return invalid(c, "adamw is NULL");
+    if (!a) return invalid(c, "arguments are NULL");
+    if (w->dev != c->dev) return invalid(c, "adamw belongs to another device");
+    if (!(a->beta1 >= 0 && a->beta1 < 1 && a->beta2 >= 0 && a->beta2 < 1)) return invalid(c, "a beta outside [0, 1)");
+    if (!(a->eps >= 0 && a->eps < 1)) return invalid(c, "eps outside [0, 1)");
+    if (!std::isfinite(a->weight_decay) || a->weight_decay < 0) return invalid(c, "weight_decay is negative or not finite");
+    if (!a->lr_device && (!std::isfinite(a->lr) || a->lr < 0)) return invalid(c, "lr is negative or not finite");
+    if (!a->steps && a->step < 1) return invalid(c, "step < 1");
+    if (a->lr_device && !a->steps) return invalid(c, "lr_device is for steps that are counted on the device");
+    if (misaligned(HWR_F32, {a->lr_device}) || reinterpret_cast<uintptr_t>(a->steps) % 8)
+        return invalid(c, "a pointer is not aligned to its elements");
+    OPS_ON_DEVICE(c, c->dev);
+    if (!a->steps) {
+        hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+        if (c->stream) OPS_HIP(c, hipStreamIsCapturing(c->stream, &cap));
+        if (cap != hipStreamCaptureStatusNone)
+            return fail(c, HWR_ERR_STATE, "a graph would repeat the same step: have the steps counted on the device");
+    }
+    AdamwArgs k{};
+    k.tensors = reinterpret_cast<const AdamwTensor *>(w->memory + kCoefBytes);
+    k.chunks = reinterpret_cast<const AdamwChunk *>(w->memory + w->chunks_at);
+    k.n_chunks = static_cast<int>(w->n_chunks);
+    if (a->steps) {
+        const AdamwRates r{a->lr, a->beta1, a->beta2, a->eps, a->weight_decay, a->seed, a->steps, a->lr_device};
+        OPS_HIP(c, launch_adamw_coef(r, w->coef(), c->stream));
+        k.coef_device = w->coef();
+    } else {
+        k.coef = adamw_coef(a->lr, a->beta1, a->beta2, a->eps, a->weight_decay, a->seed, a->step);
+    }
+    if (w->n_chunks == 0) return HWR_OK;
+    OPS_HIP(c, launch_adamw(w->bf16, w->master, w->states8, k, c->stream));
+    return HWR_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+hwr_status hwr_adamw_init(hwr_ops *ops, const hwr_adamw_config *config, hwr_adamw **out) {
+    return c_boundary([&] { return adamw_init(ops, config, out); }, [&](const char *m) { fail(ops, HWR_ERR_OOM, m); });
+}
+
+hwr_status hwr_adamw_step(hwr_ops *ops, hwr_adamw *adamw, const hwr_adamw_args *a) {
+    return c_boundary([&] { return adamw_step(ops, adamw, a); }, [&](const char *m) { fail(ops, HWR_ERR_OOM, m); });
+}
+
+void hwr_adamw_free(hwr_adamw *adamw) {
+    if (!adamw) return;
+    c_boundary(
+        [&] {
+            const OnDevice on_device(adamw->dev);
+            (void)hipFree(adamw->memory);        // (waits for the device)
+            delete adamw;
+            return HWR_OK;
+        },
+        [](const char *) {});
+}
 
 hwr_status hwr_log_probs(hwr_ops *ops, const hwr_log_probs_args *a) {
     return c_boundary([&] { return log_probs(ops, a); }, [&](const char *m) { fail(ops, HWR_ERR_OOM, m); });

@@ -135,6 +135,41 @@ struct ProbsGradArgs {
     int64_t lddx;
 };
 
+// One step of AdamW over many tensors.  Values go in blocks of kAdamwBlock, which share a
+// scale where states have 8 bits; every tensor begins a block.
+constexpr int kAdamwBlock = 256;
+constexpr int kAdamwChunk = 2048;                // values of a workgroup
+struct AdamwTensor {
+    void *p;
+    const void *g;
+    float *master;
+    void *m, *v;
+    float *m_scale, *v_scale;
+    int64_t count, place;         // values, and the number of the first among the step's
+};
+struct AdamwChunk {
+    int tensor, at;               // chunk of the tensor
+};
+struct AdamwCoef {
+    float decay, beta1, beta1_rest, beta2, beta2_rest, root_rate, rate, eps;
+    uint32_t key;                 // of the noise
+};
+// What coefficients are made from on the device.
+struct AdamwRates {
+    double lr, beta1, beta2, eps, weight_decay;
+    uint64_t seed;
+    int64_t *steps;               // counted up
+    const float *lr_device;       // or null: lr
+};
+struct AdamwArgs {
+    const AdamwTensor *tensors;
+    const AdamwChunk *chunks;
+    int n_chunks;
+    AdamwCoef coef;
+    const AdamwCoef *coef_device; // in place of coef, or null
+};
+AdamwCoef adamw_coef(double lr, double beta1, double beta2, double eps, double weight_decay, uint64_t seed, int64_t step);
+
 enum class RowsKind { kGrouped, kAdapter };
 
 hipError_t launch_group_rows(const GroupRowsArgs &a, hipStream_t s);
@@ -170,5 +205,7 @@ int probs_parts(bool bf16, int64_t n, int m, int cus);
 uint64_t probs_bytes(const ProbsArgs &a);     // of partial
 hipError_t launch_probs(bool bf16, const ProbsArgs &a, hipStream_t s);
 hipError_t launch_probs_grad(bool bf16, const ProbsGradArgs &a, hipStream_t s);
+hipError_t launch_adamw_coef(const AdamwRates &a, AdamwCoef *out, hipStream_t s);
+hipError_t launch_adamw(bool bf16, bool master, bool states8, const AdamwArgs &a, hipStream_t s);
 
 }  // namespace hwr

@@ -36,7 +36,8 @@ EXPORTS = ["hwr_init", "hwr_update_hw_state", "hwr_route_batch", "hwr_route_batc
            "hwr_probe_feature_log",
            "hwr_ops_init", "hwr_ops_free", "hwr_ops_last_error", "hwr_ops_reserve", "hwr_group_rows",
            "hwr_grouped_matmul", "hwr_grouped_matmul_grad", "hwr_adapter_matmul", "hwr_adapter_matmul_grad",
-           "hwr_log_probs", "hwr_log_probs_grad"]
+           "hwr_log_probs", "hwr_log_probs_grad",
+           "hwr_adamw_init", "hwr_adamw_step", "hwr_adamw_free"]
 
 _STATUS = {0: "HWR_OK", -1: "HWR_ERR_INVALID_ARG", -2: "HWR_ERR_OOM", -3: "HWR_ERR_HIP",
            -4: "HWR_ERR_STATE", -5: "HWR_ERR_UNSUPPORTED"}
@@ -159,6 +160,21 @@ class hwr_log_probs_grad_args(C.Structure):
                 ("dx", _vp), ("lddx", C.c_int64)]
 
 
+class hwr_adamw_tensor(C.Structure):
+    _fields_ = [("count", C.c_int64), ("p", _vp), ("g", _vp), ("master", _vp), ("m", _vp), ("v", _vp),
+                ("m_scale", _vp), ("v_scale", _vp)]
+
+
+class hwr_adamw_config(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("bits", C.c_int32), ("n_tensors", C.c_int32),
+                ("tensors", C.POINTER(hwr_adamw_tensor))]
+
+
+class hwr_adamw_args(C.Structure):
+    _fields_ = [(k, C.c_double) for k in ("lr", "beta1", "beta2", "eps", "weight_decay")] + [
+        ("seed", C.c_uint64), ("step", C.c_int64), ("steps", _vp), ("lr_device", _vp)]
+
+
 hwr_sim_router_fn = C.CFUNCTYPE(C.c_int32, C.c_void_p, C.POINTER(hwr_hw_state), C.c_int32, C.c_int32,
                                 C.c_int32, _i32p, _f32p, _f32p)
 STATE_DTYPE = np.dtype([("running_q", "<i4"), ("waiting_q", "<i4"), ("kv_util", "<f4"),
@@ -236,6 +252,12 @@ def load(path: Optional[str] = None) -> C.CDLL:
     for fn, args in (("hwr_log_probs", hwr_log_probs_args), ("hwr_log_probs_grad", hwr_log_probs_grad_args)):
         getattr(L, fn).restype = C.c_int
         getattr(L, fn).argtypes = [_vp, C.POINTER(args)]
+    L.hwr_adamw_init.restype = C.c_int
+    L.hwr_adamw_init.argtypes = [_vp, C.POINTER(hwr_adamw_config), C.POINTER(_vp)]
+    L.hwr_adamw_step.restype = C.c_int
+    L.hwr_adamw_step.argtypes = [_vp, _vp, C.POINTER(hwr_adamw_args)]
+    L.hwr_adamw_free.restype = None
+    L.hwr_adamw_free.argtypes = [_vp]
     if path is None:
         _lib = L
     return L
@@ -379,6 +401,20 @@ def hwr_log_probs(ops, args: hwr_log_probs_args) -> None:
 
 def hwr_log_probs_grad(ops, args: hwr_log_probs_grad_args) -> None:
     _check_ops(load().hwr_log_probs_grad(ops, C.byref(args)), ops)
+
+
+def hwr_adamw_init(ops, config: hwr_adamw_config):
+    adamw = _vp()
+    _check_ops(load().hwr_adamw_init(ops, C.byref(config), C.byref(adamw)), ops)
+    return adamw
+
+
+def hwr_adamw_step(ops, adamw, args: hwr_adamw_args) -> None:
+    _check_ops(load().hwr_adamw_step(ops, adamw, C.byref(args)), ops)
+
+
+def hwr_adamw_free(adamw) -> None:
+    load().hwr_adamw_free(adamw)
 
 
 # ---------------------------------------------------------------- convenience

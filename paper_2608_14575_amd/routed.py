@@ -266,6 +266,120 @@ class RoutedOps:
             raise HwrError(st, hwr.hwr_ops_last_error(self.ctx))
 
 
+class AdamW:
+    """AdamW over many tensors at once, in one launch a step, on the stream of a ``RoutedOps``.
+
+    ``params`` and ``grads`` are lists of dense tensors, of one type (bfloat16 or float32), pair by pair of
+    one size; the same tensors are read and written at every step.  bfloat16 weights are stepped through
+    float32 masters (``master=True``) or alone, rounded up or down at random.  States have 32
+    bits or 8 (``bits``): float8_e4m3fn with a float32 scale for every 256 values, the root of the second
+    moment in place of it, rounded at random, from ``seed``, the step and the value's place.
+
+    ``state`` is a dict of lists, as the attribute of the same name: "m" and "v", with 8 bits "m_scale" and
+    "v_scale", with masters "master"; left out, it is made here (zeros, and copies of the weights).
+
+    ``steps``, the number of steps done, is counted up by ``step``: an int, or a device tensor of one int64, which
+    a captured ``step`` needs.  ``lr`` may be a device tensor of one float32 then.  Both,
+    ``betas``, ``eps`` and ``weight_decay`` may be changed between steps (a captured step keeps what
+    it was captured with, but for the contents of the tensors)."""
+
+    def __init__(self, ops, params, grads, *, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, bits=32, master=False,
+                 state=None, steps=0, seed=0):
+        import torch
+        self._handle = None
+        params, grads = list(params), list(grads)
+        if len(params) != len(grads):
+            _bad("grads", f"{len(grads)} tensors for {len(params)} weights")
+        dt = params[0].dtype if params else torch.float32
+        if dt not in ops._kinds:
+            _bad("params", f"dtype {dt} (expected bfloat16 or float32)")
+        if state is None:
+            if bits not in (8, 32):
+                _bad("bits", f"{bits} (expected 8 or 32)")
+            if master and dt is torch.float32:
+                _bad("master", "for bfloat16 weights")
+            state = self._make_state(torch, params, bits, master)
+        state = {k: list(v) for k, v in state.items()}
+        bits = 8 if "m_scale" in state else 32
+        kind = torch.float8_e4m3fn if bits == 8 else torch.float32
+        kinds = {"m": kind, "v": kind}
+        if bits == 8:
+            kinds.update(m_scale=torch.float32, v_scale=torch.float32)
+        if "master" in state:
+            kinds["master"] = torch.float32
+        if set(state) != set(kinds):
+            _bad("state", f"{sorted(state)}, expected {sorted(kinds)}")
+        for k, v in state.items():
+            if len(v) != len(params):
+                _bad(k, f"{len(v)} tensors for {len(params)} weights")
+        table = (hwr.hwr_adamw_tensor * len(params))()
+        for i, (t, p, g) in enumerate(zip(table, params, grads)):
+            n = t.count = p.numel()
+            t.p, t.g = self._address(ops, f"params[{i}]", p, dt, n), self._address(ops, f"grads[{i}]", g, dt, n)
+            for k, d in kinds.items():
+                setattr(t, k, self._address(ops, f"{k}[{i}]", state[k][i], d, (n + 255) // 256 if k.endswith("scale") else n))
+        config = hwr.hwr_adamw_config(ops._kinds[dt], bits, len(params), table)
+        self._handle = hwr.hwr_adamw_init(ops.ctx, config)
+        self.ops, self.params, self.grads, self.state = ops, params, grads, state
+        self.lr, self.betas, self.eps, self.weight_decay, self.steps, self.seed = lr, betas, eps, weight_decay, steps, seed
+        self._i64 = torch.int64
+        self._args = _Args(ops._lib.hwr_adamw_step, hwr.hwr_adamw_args)
+        self._fn = C.cast(ops._lib.hwr_adamw_step, C.CFUNCTYPE(C.c_int, C.c_void_p, C.c_void_p, C.c_void_p))
+        self._args._fn = lambda ctx, at: self._fn(ctx, self._handle, at)
+
+    @staticmethod
+    def _address(ops, name, t, dtype, n):
+        if t.get_device() != ops.device:
+            _bad(name, f"on {t.device}, expected cuda:{ops.device}")
+        if t.dtype is not dtype or t.numel() != n:
+            _bad(name, f"{t.numel()} of {t.dtype}, expected {n} of {dtype}")
+        if not t.is_contiguous():
+            _bad(name, "not contiguous")
+        return t.data_ptr()
+
+    @staticmethod
+    def _make_state(torch, params, bits, master):
+        def zeros(p, n, dtype):
+            return torch.zeros(n, dtype=dtype, device=p.device)
+
+        kind = torch.float8_e4m3fn if bits == 8 else torch.float32
+        state = {k: [zeros(p, p.shape, kind) for p in params] for k in ("m", "v")}
+        if bits == 8:
+            state.update({k: [zeros(p, (p.numel() + 255) // 256, torch.float32) for p in params] for k in ("m_scale", "v_scale")})
+        if master:
+            state["master"] = [p.detach().float() for p in params]
+        return state
+
+    def close(self) -> None:
+        if getattr(self, "_handle", None):
+            hwr.hwr_adamw_free(self._handle)
+            self._handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def step(self) -> None:
+        """One step of all tensors, queued on the stream of the ``RoutedOps``."""
+        if not self._handle:
+            _bad("AdamW", "closed")
+        ops, steps, lr, (b1, b2) = self.ops, self.steps, self.lr, self.betas
+        number, counter, rate = 0, 0, 0
+        if isinstance(steps, int):
+            number = steps + 1
+        else:
+            counter = ops._dense("steps", steps.view(1) if steps.dim() == 0 else steps, self._i64, (1,))
+        if not isinstance(lr, (int, float)):
+            rate, lr = ops._dense("lr", lr.view(1) if lr.dim() == 0 else lr, ops._f32, (1,)), 0.0
+        st = self._args(ops.ctx, lr, b1, b2, self.eps, self.weight_decay, self.seed & 0xFFFFFFFFFFFFFFFF, number, counter, rate)
+        if st:
+            raise HwrError(st, hwr.hwr_ops_last_error(ops.ctx))
+        if not counter:
+            self.steps = number
+
+
 def example(steps: int = 5, n: int = 4096, seed: int = 7) -> list:
     """Routes n queries, groups them by the chosen pair's model, and trains, on
     the grouped rows, one low-rank adapter per model beside a shared projection

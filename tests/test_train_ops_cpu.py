@@ -10,7 +10,7 @@ import pytest
 from paper_2608_14575_amd import hwr, routed
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-STRUCTS = ["hwr_log_probs_args", "hwr_log_probs_grad_args"]
+STRUCTS = ["hwr_log_probs_args", "hwr_log_probs_grad_args", "hwr_adamw_tensor", "hwr_adamw_config", "hwr_adamw_args"]
 
 
 def test_layout_matches_header(tmp_path):
@@ -33,16 +33,24 @@ def test_null_contexts():
     for fn, args in (("hwr_log_probs", "hwr_log_probs_args"), ("hwr_log_probs_grad", "hwr_log_probs_grad_args")):
         assert getattr(lib, fn)(None, C.byref(getattr(hwr, args)())) == hwr.HWR_ERR_INVALID_ARG
         assert "ops is NULL" in hwr.hwr_ops_last_error(None)
+    out = C.c_void_p(7)
+    for call in (lambda: lib.hwr_adamw_init(None, C.byref(hwr.hwr_adamw_config()), C.byref(out)),
+                 lambda: lib.hwr_adamw_step(None, None, C.byref(hwr.hwr_adamw_args()))):
+        assert call() == hwr.HWR_ERR_INVALID_ARG
+        assert "ops is NULL" in hwr.hwr_ops_last_error(None)
+    hwr.hwr_adamw_free(None)
 
 
 def test_packed_arguments_are_the_structures():
-    for name in ("hwr_log_probs_args", "hwr_log_probs_grad_args"):
+    for name in ("hwr_log_probs_args", "hwr_log_probs_grad_args", "hwr_adamw_args"):
         cls = getattr(hwr, name)
-        call = routed._Args(hwr.load().hwr_log_probs, cls)
-        values = [0.5 if t is C.c_float else (i + 3) << (8 if t is C.c_int32 else 40) for i, (_, t) in enumerate(cls._fields_)]
+        call = routed._Args(hwr.load().hwr_log_probs, cls)        # (any function: without a context it reads nothing)
+        values = [0.5 if t in (C.c_float, C.c_double) else (i + 3) << (8 if t is C.c_int32 else 40) for i, (_, t) in enumerate(cls._fields_)]
         assert call(None, *values) == hwr.HWR_ERR_INVALID_ARG          # (no context: nothing is read)
         a = cls.from_buffer(call._block)
         assert [getattr(a, f) for f, _ in cls._fields_] == values
+        if cls._fields_[0][1] is not C.c_int32:
+            continue
         with pytest.raises(hwr.HwrError) as e:
             call(None, 2 ** 31, *values[1:])
         assert e.value.status == hwr.HWR_ERR_INVALID_ARG

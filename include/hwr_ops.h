@@ -10,6 +10,9 @@
  *   hwr_grouped_matmul       y[r] = x[r] W[g(r)]
  *   hwr_grouped_matmul_grad  dx[r] = dy[r] W[g(r)]^T,
  *                            dW[g] = sum over rows r of g of x[r]^T dy[r]
+ *   hwr_grouped_linear       y[r] = act(x[r] W[g(r)] + bias[g(r)]) + residual[r]
+ *   hwr_grouped_linear_grad  with dz[r] = dy[r] act'(z[r]): dx and dW as above from dz,
+ *                            dbias[g] = sum over rows r of g of dz[r]
  *   hwr_adapter_matmul       y[r] = x[r] W + s[g(r)] (x[r] A[g(r)]) B[g(r)],
  *                            one projection shared by all rows and the
  *                            low-rank adapter of the row's group
@@ -123,6 +126,45 @@ typedef struct {
     void *dw;                     /* [G][k][m] or NULL                          */
 } hwr_matmul_grad_args;
 hwr_status hwr_grouped_matmul_grad(hwr_ops *ops, const hwr_groups *g, const hwr_matmul_grad_args *a);
+
+/* A layer: z[r] = x[r] W[g] + bias[g], y[r] = act(z[r]) + residual[r].  A row in no group has
+ * y the residual (zeros without one) and z zeros.  z, which the gradient reads, is written where
+ * it is not NULL; y is made of the sums before z is rounded.  y and z may not be x, the residual or each other. */
+typedef enum {
+    HWR_ACT_NONE = 0,             /* z                                          */
+    HWR_ACT_RELU = 1,             /* max(z, 0)                                  */
+    HWR_ACT_SILU = 2,             /* z / (1 + exp(-z))                          */
+    HWR_ACT_GELU = 3              /* z times the normal distribution at z       */
+} hwr_act;
+
+typedef struct {
+    int32_t dtype;
+    int32_t k, m;
+    int32_t act;                  /* hwr_act                                    */
+    const void *x; int64_t ldx;   /* [n][k]                                     */
+    const void *w;                /* [G][k][m]                                  */
+    const void *bias;             /* [G][m] or NULL                             */
+    const void *residual; int64_t ldr;   /* [n][m] or NULL                      */
+    void *y; int64_t ldy;         /* [n][m]                                     */
+    void *z; int64_t ldz;         /* [n][m] or NULL                             */
+} hwr_linear_args;
+hwr_status hwr_grouped_linear(hwr_ops *ops, const hwr_groups *g, const hwr_linear_args *a);
+
+/* With dz[r] = dy[r] act'(z[r]) (rounded once to the type of the matrices for dx and dw, not for
+ * dbias).  The gradient of the residual is dy itself.  dx may not be dy, z or x. */
+typedef struct {
+    int32_t dtype;
+    int32_t k, m;
+    int32_t act;
+    const void *dy; int64_t lddy; /* [n][m]                                     */
+    const void *z; int64_t ldz;   /* [n][m]; needed but for HWR_ACT_NONE        */
+    const void *x; int64_t ldx;   /* [n][k]; needed for dw                      */
+    const void *w;                /* [G][k][m]; needed for dx                   */
+    void *dx; int64_t lddx;       /* [n][k] or NULL                             */
+    void *dw;                     /* [G][k][m] or NULL                          */
+    void *dbias;                  /* [G][m] or NULL                             */
+} hwr_linear_grad_args;
+hwr_status hwr_grouped_linear_grad(hwr_ops *ops, const hwr_groups *g, const hwr_linear_grad_args *a);
 
 typedef struct {
     int32_t dtype;

@@ -205,7 +205,8 @@ hwr_status rows(hwr_ops *c, bool bf16, RowsKind kind, bool ks, RowsArgs r, char 
     f.ldy = r.ldy;
     f.parts = r.parts;
     f.partial = r.partial;
-    OPS_HIP(c, launch_join(bf16, f, c->stream));
+    f.end = r.end;
+    OPS_HIP(c, launch_join(bf16, kind, f, c->stream));
     return HWR_OK;
 }
 
@@ -225,7 +226,8 @@ hwr_status weight_grad(hwr_ops *c, bool bf16, ColsKind kind, ColsArgs w, char *p
 constexpr int kLowParts = 4;      // parts of the shrink's contraction, few rows
 
 // Few rows: the weights are streamed (launch_few), with its partial sums in the work space.
-hwr_status few(hwr_ops *c, FewArgs f, bool bf16, bool adapter) {
+hwr_status few(hwr_ops *c, FewArgs f, bool bf16, RowsKind kind) {
+    const bool adapter = kind == RowsKind::kAdapter;
     f.m_pad = (f.m + 3) / 4 * 4;
     f.parts = few_parts(f.g.n, f.g.G, f.k, f.m, bf16, adapter, c->cus);
     f.low_parts = kLowParts;
@@ -235,7 +237,7 @@ hwr_status few(hwr_ops *c, FewArgs f, bool bf16, bool adapter) {
     if (hwr_status st = workspace(c, (sums + lows) * sizeof(float), &ws)) return st;
     f.partial = reinterpret_cast<float *>(ws);
     f.low = f.partial + sums;
-    OPS_HIP(c, launch_few(bf16, adapter, f, c->stream));
+    OPS_HIP(c, launch_few(bf16, kind, f, c->stream));
     return HWR_OK;
 }
 
@@ -261,17 +263,11 @@ hwr_status group_rows(hwr_ops *c, int32_t n, const int32_t *choice, const int32_
     return HWR_OK;
 }
 
-hwr_status grouped_matmul(hwr_ops *c, const hwr_groups *g, const hwr_matmul_args *a) {
-    if (!c) return invalid(nullptr, "ops is NULL");
-    if (const char *m = check_groups(g)) return invalid(c, m);
-    if (!a) return invalid(c, "arguments are NULL");
-    if (const char *m = check_shape(a->dtype, a->k, a->m)) return invalid(c, m);
-    if (bad_ld(a->ldx, a->k) || bad_ld(a->ldy, a->m)) return invalid(c, "a row stride is smaller than the row");
-    if (g->n == 0) return HWR_OK;
-    if (!a->x || !a->w || !a->y) return invalid(c, "x, w and y are required");
-    if (misaligned(a->dtype, {a->x, a->w, a->y})) return invalid(c, "a pointer is not aligned to its elements");
+// y = x W[g], and for kLinear what `end` says; arguments are sound.
+hwr_status product(hwr_ops *c, const hwr_groups *g, const hwr_matmul_args *a, RowsKind kind, const Epilogue &end) {
     OPS_ON_DEVICE(c, c->dev);
-    if (few_rows(g->n, g->n_groups, a->k, a->m, false, a->dtype == HWR_BF16)) {
+    const bool bf16 = a->dtype == HWR_BF16;
+    if (few_rows(g->n, g->n_groups, a->k, a->m, false, bf16)) {
         FewArgs f{};
         f.g = groups_arg(g);
         f.k = a->k;
@@ -282,9 +278,9 @@ hwr_status grouped_matmul(hwr_ops *c, const hwr_groups *g, const hwr_matmul_args
         f.w_stride = static_cast<int64_t>(a->k) * a->m;
         f.y = a->y;
         f.ldy = dense(a->ldy, a->m);
-        return few(c, f, a->dtype == HWR_BF16, false);
+        f.end = end;
+        return few(c, f, bf16, kind);
     }
-    const bool bf16 = a->dtype == HWR_BF16;
     const void *x = a->x, *w = a->w;
     int64_t ldx = dense(a->ldx, a->k), ldw = a->m;
     uint64_t used = 0;
@@ -293,34 +289,79 @@ hwr_status grouped_matmul(hwr_ops *c, const hwr_groups *g, const hwr_matmul_args
     pads.add(&w, &ldw, static_cast<int64_t>(g->n_groups) * a->k, a->m);
     const bool padded = pads.plan(2.0 * g->n * a->k * a->m, false, &used);
     RowsArgs r = rows_args(c, g, true, padded, x, ldx, a->k, w, ldw, a->k, false, a->m, a->y, dense(a->ldy, a->m));
+    r.end = end;
     char *ws = nullptr;
-    if (hwr_status st = workspace(c, used + rows_bytes(c, bf16, RowsKind::kGrouped, true, r), &ws)) return st;
+    if (hwr_status st = workspace(c, used + rows_bytes(c, bf16, kind, true, r), &ws)) return st;
     if (hwr_status st = pads.copy(c, ws)) return st;
     r.x = x;
     r.w = w;
-    return rows(c, bf16, RowsKind::kGrouped, true, r, ws + used);
+    return rows(c, bf16, kind, true, r, ws + used);
 }
 
-hwr_status grouped_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_matmul_grad_args *a) {
+hwr_status grouped_matmul(hwr_ops *c, const hwr_groups *g, const hwr_matmul_args *a) {
     if (!c) return invalid(nullptr, "ops is NULL");
     if (const char *m = check_groups(g)) return invalid(c, m);
     if (!a) return invalid(c, "arguments are NULL");
     if (const char *m = check_shape(a->dtype, a->k, a->m)) return invalid(c, m);
-    if (bad_ld(a->lddy, a->m) || bad_ld(a->ldx, a->k) || bad_ld(a->lddx, a->k))
+    if (bad_ld(a->ldx, a->k) || bad_ld(a->ldy, a->m)) return invalid(c, "a row stride is smaller than the row");
+    if (g->n == 0) return HWR_OK;
+    if (!a->x || !a->w || !a->y) return invalid(c, "x, w and y are required");
+    if (misaligned(a->dtype, {a->x, a->w, a->y})) return invalid(c, "a pointer is not aligned to its elements");
+    return product(c, g, a, RowsKind::kGrouped, Epilogue{});
+}
+
+const char *check_act(int32_t act) { return act < HWR_ACT_NONE || act > HWR_ACT_GELU ? "unknown activation" : nullptr; }
+
+hwr_status grouped_linear(hwr_ops *c, const hwr_groups *g, const hwr_linear_args *a) {
+    if (!c) return invalid(nullptr, "ops is NULL");
+    if (const char *m = check_groups(g)) return invalid(c, m);
+    if (!a) return invalid(c, "arguments are NULL");
+    if (const char *m = check_shape(a->dtype, a->k, a->m)) return invalid(c, m);
+    if (const char *m = check_act(a->act)) return invalid(c, m);
+    if (bad_ld(a->ldx, a->k) || bad_ld(a->ldr, a->m) || bad_ld(a->ldy, a->m) || bad_ld(a->ldz, a->m))
         return invalid(c, "a row stride is smaller than the row");
-    if (g->n > 0 && (!a->dy || (a->dx && !a->w) || (a->dw && !a->x)))
-        return invalid(c, "dy is required, w for dx, and x for dw");
-    if (misaligned(a->dtype, {a->dy, a->x, a->w, a->dx, a->dw})) return invalid(c, "a pointer is not aligned to its elements");
+    if (g->n == 0) return HWR_OK;
+    if (!a->x || !a->w || !a->y) return invalid(c, "x, w and y are required");
+    if (misaligned(a->dtype, {a->x, a->w, a->bias, a->residual, a->y, a->z}))
+        return invalid(c, "a pointer is not aligned to its elements");
+    // (tiles of columns overlap at a row's end: a residual that is written over would be added twice)
+    if (a->y == a->residual || a->y == a->z || (a->z && a->z == a->residual) || a->y == a->x || a->z == a->x)
+        return invalid(c, "y and z may not be each other, x or the residual");
+    const hwr_matmul_args p{a->dtype, a->k, a->m, a->x, a->ldx, a->w, a->y, a->ldy};
+    return product(c, g, &p, RowsKind::kLinear,
+                   Epilogue{a->act, a->bias, a->residual, dense(a->ldr, a->m), a->z, dense(a->ldz, a->m)});
+}
+
+// dx = dz W[g]^T, dW[g] = sum x^T dz and dbias[g] = sum dz with dz = dy act'(z); arguments are sound.
+hwr_status product_grad(hwr_ops *c, const hwr_groups *g, const hwr_matmul_grad_args *a, int act, const void *z, int64_t ldz,
+                        void *dbias) {
     OPS_ON_DEVICE(c, c->dev);
     const bool bf16 = a->dtype == HWR_BF16;
     const void *dy = a->dy, *x = a->x, *w = a->w;
     int64_t lddy = dense(a->lddy, a->m), ldx = dense(a->ldx, a->k), ldw = a->m;
     uint64_t used = 0;
     Pads pads(bf16);
-    pads.add(&dy, &lddy, g->n, a->m);
+    const bool sloped = act != HWR_ACT_NONE && (a->dx || a->dw);
+    if (act == HWR_ACT_NONE) pads.add(&dy, &lddy, g->n, a->m);
     pads.add(&w, &ldw, static_cast<int64_t>(g->n_groups) * a->k, a->m, a->dx != nullptr);
     pads.add(&x, &ldx, g->n, a->k, a->dw != nullptr);
     const bool padded = pads.plan(4.0 * g->n * a->k * a->m, true, &used), dx = a->dx && g->n > 0;
+    // dz in place of dy (an address in the work space, as the copies' are)
+    SlopeArgs s{};
+    s.g = groups_arg(g);
+    s.m = a->m;
+    s.m_pad = (a->m + 7) / 8 * 8;
+    s.dy = a->dy;
+    s.lddy = dense(a->lddy, a->m);
+    s.z = z;
+    s.ldz = ldz;
+    s.dbias = dbias;
+    const uint64_t dz_at = used;
+    if (sloped) {
+        lddy = s.lddz = padded_width(bf16, a->m);
+        dy = reinterpret_cast<const void *>(dz_at);
+        used += (static_cast<uint64_t>(g->n) * lddy * (bf16 ? 2 : 4) + 255) / 256 * 256;
+    }
     RowsArgs r = rows_args(c, g, false, padded, dy, lddy, a->m, w, ldw, a->k, false, a->k, a->dx, dense(a->lddx, a->k));
     ColsArgs d{};
     d.g = groups_arg(g);
@@ -333,11 +374,15 @@ hwr_status grouped_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_matmul
     d.ldq = lddy;
     d.out = a->dw;
     // (one after the other: they share the place of their partial sums)
-    const uint64_t sums = std::max(dx ? rows_bytes(c, bf16, RowsKind::kGrouped, false, r) : 0,
-                                   a->dw ? weight_grad_bytes(c, bf16, ColsKind::kDense, d) : 0);
+    const uint64_t sums = std::max({dx ? rows_bytes(c, bf16, RowsKind::kGrouped, false, r) : 0,
+                                    a->dw ? weight_grad_bytes(c, bf16, ColsKind::kDense, d) : 0,
+                                    dbias ? uint64_t{sizeof(float)} * slope_tiles(g->n, g->n_groups) * s.m_pad : 0});
     char *ws = nullptr;
     if (hwr_status st = workspace(c, used + sums, &ws)) return st;
     if (hwr_status st = pads.copy(c, ws)) return st;
+    if (sloped) dy = s.dz = ws + dz_at;
+    if (dbias) s.partial = reinterpret_cast<float *>(ws + used);
+    if (sloped || dbias) OPS_HIP(c, launch_slope(bf16, act, s, c->stream));
     r.x = d.q = dy;
     r.w = w;
     d.p = x;
@@ -346,6 +391,36 @@ hwr_status grouped_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_matmul
     if (a->dw)
         if (hwr_status st = weight_grad(c, bf16, ColsKind::kDense, d, ws + used)) return st;
     return HWR_OK;
+}
+
+hwr_status grouped_matmul_grad(hwr_ops *c, const hwr_groups *g, const hwr_matmul_grad_args *a) {
+    if (!c) return invalid(nullptr, "ops is NULL");
+    if (const char *m = check_groups(g)) return invalid(c, m);
+    if (!a) return invalid(c, "arguments are NULL");
+    if (const char *m = check_shape(a->dtype, a->k, a->m)) return invalid(c, m);
+    if (bad_ld(a->lddy, a->m) || bad_ld(a->ldx, a->k) || bad_ld(a->lddx, a->k))
+        return invalid(c, "a row stride is smaller than the row");
+    if (g->n > 0 && (!a->dy || (a->dx && !a->w) || (a->dw && !a->x)))
+        return invalid(c, "dy is required, w for dx, and x for dw");
+    if (misaligned(a->dtype, {a->dy, a->x, a->w, a->dx, a->dw})) return invalid(c, "a pointer is not aligned to its elements");
+    return product_grad(c, g, a, HWR_ACT_NONE, nullptr, 0, nullptr);
+}
+
+hwr_status grouped_linear_grad(hwr_ops *c, const hwr_groups *g, const hwr_linear_grad_args *a) {
+    if (!c) return invalid(nullptr, "ops is NULL");
+    if (const char *m = check_groups(g)) return invalid(c, m);
+    if (!a) return invalid(c, "arguments are NULL");
+    if (const char *m = check_shape(a->dtype, a->k, a->m)) return invalid(c, m);
+    if (const char *m = check_act(a->act)) return invalid(c, m);
+    if (bad_ld(a->lddy, a->m) || bad_ld(a->ldz, a->m) || bad_ld(a->ldx, a->k) || bad_ld(a->lddx, a->k))
+        return invalid(c, "a row stride is smaller than the row");
+    if (g->n > 0 && (!a->dy || (a->act != HWR_ACT_NONE && !a->z) || (a->dx && !a->w) || (a->dw && !a->x)))
+        return invalid(c, "dy is required, z with an activation, w for dx, and x for dw");
+    if (misaligned(a->dtype, {a->dy, a->z, a->x, a->w, a->dx, a->dw, a->dbias}))
+        return invalid(c, "a pointer is not aligned to its elements");
+    if (a->dx && (a->dx == a->dy || a->dx == a->z || a->dx == a->x)) return invalid(c, "dx may not be dy, z or x");
+    const hwr_matmul_grad_args p{a->dtype, a->k, a->m, a->dy, a->lddy, a->x, a->ldx, a->w, a->dx, a->lddx, a->dw};
+    return product_grad(c, g, &p, a->act, a->z, dense(a->ldz, a->m), a->dbias);
 }
 
 hwr_status adapter_matmul(hwr_ops *c, const hwr_groups *g, const hwr_adapter_args *a) {
@@ -375,7 +450,7 @@ hwr_status adapter_matmul(hwr_ops *c, const hwr_groups *g, const hwr_adapter_arg
         f.a = a->a;
         f.b = a->b;
         f.scale = a->scale;
-        return few(c, f, a->dtype == HWR_BF16, true);
+        return few(c, f, a->dtype == HWR_BF16, RowsKind::kAdapter);
     }
     const bool bf16 = a->dtype == HWR_BF16;
     uint64_t used = low_bytes(g->n, a->rank);
@@ -529,6 +604,14 @@ hwr_status hwr_grouped_matmul(hwr_ops *ops, const hwr_groups *g, const hwr_matmu
 
 hwr_status hwr_grouped_matmul_grad(hwr_ops *ops, const hwr_groups *g, const hwr_matmul_grad_args *a) {
     return c_boundary([&] { return grouped_matmul_grad(ops, g, a); }, [&](const char *m) { fail(ops, HWR_ERR_OOM, m); });
+}
+
+hwr_status hwr_grouped_linear(hwr_ops *ops, const hwr_groups *g, const hwr_linear_args *a) {
+    return c_boundary([&] { return grouped_linear(ops, g, a); }, [&](const char *m) { fail(ops, HWR_ERR_OOM, m); });
+}
+
+hwr_status hwr_grouped_linear_grad(hwr_ops *ops, const hwr_groups *g, const hwr_linear_grad_args *a) {
+    return c_boundary([&] { return grouped_linear_grad(ops, g, a); }, [&](const char *m) { fail(ops, HWR_ERR_OOM, m); });
 }
 
 hwr_status hwr_adapter_matmul(hwr_ops *ops, const hwr_groups *g, const hwr_adapter_args *a) {

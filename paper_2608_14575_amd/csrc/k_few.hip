@@ -14,7 +14,7 @@
 // want of registers to load ahead: the loads of cut columns and of a last cut step stand
 // in the same loop, which takes all 128 registers in bf16 and spills 14 to 16 of them, read
 // back on those paths alone).
-#include "ops_device.hpp"
+#include "ops_act.hpp"
 
 namespace hwr {
 namespace {
@@ -60,8 +60,9 @@ __device__ void few_shrink(const FewArgs &a, int item, float *lds) {
     }
 }
 
-template <class E, bool ADAPTER>
+template <class E, RowsKind KIND>
 __global__ void __launch_bounds__(kWaves * 64, 4) k_few(FewArgs a) {   // two workgroups on a compute unit
+    constexpr bool ADAPTER = KIND == RowsKind::kAdapter;
     using El = Elem<E>;
     constexpr int V = El::kEpc, BM = kFewTile, BN = 16 * V, kStep = 4 * V;
     __shared__ f32x4 part[kWaves / 2 * V * 64];
@@ -157,6 +158,17 @@ __global__ void __launch_bounds__(kWaves * 64, 4) k_few(FewArgs a) {   // two wo
                 if (c < a.m_pad)
                     *reinterpret_cast<f32x4_a4 *>(out + c) = f32x4{acc[j][e], acc[j + 1][e], acc[j + 2][e], acc[j + 3][e]};
             }
+    } else if (KIND == RowsKind::kLinear && row >= 0) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const Finish<E, V> finish(a.end, c0 + (4 * q + e) * V, a.m, a.g.G, rt.g);
+            Some<E, V> res;
+            finish.load(row, res);
+            float v[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] = acc[j][e];
+            finish.store(row, res, v, static_cast<E *>(a.y), a.ldy);
+        }
     } else if (row >= 0) {
         E *y = static_cast<E *>(a.y) + row * a.ldy;
 #pragma unroll
@@ -178,8 +190,9 @@ __global__ void __launch_bounds__(kWaves * 64, 4) k_few(FewArgs a) {   // two wo
 
 // y[row] = sum of the parts, plus scale[g] low[place] b_g: a thread per four columns of a place
 constexpr int kJoinThreads = 128;
-template <class E, bool ADAPTER>
+template <class E, RowsKind KIND>
 __global__ void __launch_bounds__(kJoinThreads) k_join(FewArgs a) {
+    constexpr bool ADAPTER = KIND == RowsKind::kAdapter;
     __shared__ float low[128];
     const int tid = threadIdx.x, lane = tid & 63;
     const int ct = (a.m_pad / 4 + kJoinThreads - 1) / kJoinThreads;
@@ -193,6 +206,16 @@ __global__ void __launch_bounds__(kJoinThreads) k_join(FewArgs a) {
             v += *reinterpret_cast<const f32x4 *>(a.partial + (static_cast<int64_t>(s) * a.g.n + p) * a.m_pad + c);
     const int row = row_at(a.g, p);
     int g = a.g.G;
+    if constexpr (KIND == RowsKind::kLinear) {
+        g = group_of(a.g, p, lane);
+        if (row < 0) return;
+        const float sum[4] = {v[0], v[1], v[2], v[3]};
+        const Finish<E, 4> finish(a.end, c, a.m, a.g.G, g);
+        Some<E, 4> res;
+        finish.load(row, res);
+        finish.store(row, res, sum, static_cast<E *>(a.y), a.ldy);
+        return;
+    }
     if (ADAPTER) {
         float t = 0.0f;
         g = group_of(a.g, p, lane);
@@ -228,23 +251,24 @@ __global__ void __launch_bounds__(kJoinThreads) k_join(FewArgs a) {
     store_four<E>(static_cast<E *>(a.y) + row * a.ldy, c, a.m, v);
 }
 
-template <class E, bool ADAPTER>
+template <class E, RowsKind KIND>
 hipError_t join(const FewArgs &a, hipStream_t s) {
     const int64_t blocks = static_cast<int64_t>((a.m_pad / 4 + kJoinThreads - 1) / kJoinThreads) * a.g.n;
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
-    return launch_kernel(k_join<E, ADAPTER>, dim3(static_cast<uint32_t>(blocks)), dim3(kJoinThreads), 0, s, a);
+    return launch_kernel(k_join<E, KIND>, dim3(static_cast<uint32_t>(blocks)), dim3(kJoinThreads), 0, s, a);
 }
 
-template <class E, bool ADAPTER>
+template <class E, RowsKind KIND>
 hipError_t go(const FewArgs &a, hipStream_t s) {
+    constexpr bool ADAPTER = KIND == RowsKind::kAdapter;
     const int ct = (a.m + 16 * Elem<E>::kEpc - 1) / (16 * Elem<E>::kEpc);
     const int64_t items = static_cast<int64_t>(few_tiles(a.g.n, a.g.G, ADAPTER)) * ct * a.parts +
                           (ADAPTER ? static_cast<int64_t>(a.g.n) * a.low_parts : 0);
     if (items > INT32_MAX) return hipErrorInvalidValue;
     const dim3 grid(static_cast<uint32_t>(items)), block(kWaves * 64);
-    const hipError_t e = launch_kernel(k_few<E, ADAPTER>, grid, block, 0, s, a);
+    const hipError_t e = launch_kernel(k_few<E, KIND>, grid, block, 0, s, a);
     if (e != hipSuccess || (!ADAPTER && a.parts == 1)) return e;
-    return join<E, ADAPTER>(a, s);
+    return join<E, KIND>(a, s);
 }
 
 }  // namespace
@@ -282,13 +306,18 @@ int few_parts(int n, int G, int k, int m, bool bf16, bool adapter, int cus) {
     return parts;
 }
 
-hipError_t launch_few(bool bf16, bool adapter, const FewArgs &a, hipStream_t s) {
-    if (bf16) return adapter ? go<__bf16, true>(a, s) : go<__bf16, false>(a, s);
-    return adapter ? go<float, true>(a, s) : go<float, false>(a, s);
+template <class E>
+static hipError_t pick(RowsKind kind, const FewArgs &a, hipStream_t s) {
+    if (kind == RowsKind::kAdapter) return go<E, RowsKind::kAdapter>(a, s);
+    return kind == RowsKind::kLinear ? go<E, RowsKind::kLinear>(a, s) : go<E, RowsKind::kGrouped>(a, s);
+}
+hipError_t launch_few(bool bf16, RowsKind kind, const FewArgs &a, hipStream_t s) {
+    return bf16 ? pick<__bf16>(kind, a, s) : pick<float>(kind, a, s);
 }
 
-hipError_t launch_join(bool bf16, const FewArgs &a, hipStream_t s) {
-    return bf16 ? join<__bf16, false>(a, s) : join<float, false>(a, s);
+hipError_t launch_join(bool bf16, RowsKind kind, const FewArgs &a, hipStream_t s) {
+    if (kind == RowsKind::kLinear) return bf16 ? join<__bf16, RowsKind::kLinear>(a, s) : join<float, RowsKind::kLinear>(a, s);
+    return bf16 ? join<__bf16, RowsKind::kGrouped>(a, s) : join<float, RowsKind::kGrouped>(a, s);
 }
 
 }  // namespace hwr

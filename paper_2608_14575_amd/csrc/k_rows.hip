@@ -1,8 +1,9 @@
 // Products by row: every row of a routed batch with the weights of its group
-// (kGrouped), or with shared weights plus its group's low-rank adapter (kAdapter).
+// (kGrouped; kLinear: and what follows in a layer), or with shared weights plus its group's
+// low-rank adapter (kAdapter).
 #include <algorithm>
 
-#include "ops_device.hpp"
+#include "ops_act.hpp"
 
 namespace hwr {
 namespace {
@@ -110,7 +111,7 @@ __device__ inline void add_adapters(const RowsArgs &a, const RowTile &rt, int c0
 }
 
 // A lane holds, for row l % 16 of fragment i, four columns of fragment j.
-template <class E, int BM, int BN, int WR, int WC>
+template <class E, RowsKind KIND, int BM, int BN, int WR, int WC>
 __device__ inline void store_rows(const RowsArgs &a, const RowTile &rt, int c0, int part, const int *rows,
                                   const f32x4 (&acc)[BM / WR / 16][BN / WC / 16], int tid) {
     constexpr int RF = BM / WR / 16, CF = BN / WC / 16;
@@ -131,6 +132,25 @@ __device__ inline void store_rows(const RowsArgs &a, const RowTile &rt, int c0, 
         return;
     }
     E *y = static_cast<E *>(a.y);
+    if constexpr (KIND == RowsKind::kLinear) {
+#pragma unroll
+        for (int j = 0; j < CF; ++j) {
+            const Finish<E, 4> finish(a.end, c0 + (wc * CF + j) * 16 + q * 4, a.m, a.g.G, rt.g);
+            int r[RF];
+            Some<E, 4> res[RF];
+#pragma unroll
+            for (int i = 0; i < RF; ++i) {
+                r[i] = rows[(wr * RF + i) * 16 + (lane & 15)];
+                finish.load(max(r[i], 0), res[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < RF; ++i) {
+                const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+                if (r[i] >= 0) finish.store(r[i], res[i], v, y, a.ldy);
+            }
+        }
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < RF; ++i) {
         const int r = rows[(wr * RF + i) * 16 + (lane & 15)];
@@ -146,7 +166,7 @@ __device__ inline void store_rows(const RowsArgs &a, const RowTile &rt, int c0, 
 // The workgroup's tile of places, first column and part.  False past the last tile.
 template <RowsKind KIND, int BM, int BN, int NT>
 __device__ inline bool my_tile(const RowsArgs &a, int lane, RowTile &rt, int &c0, int &part) {
-    const bool tail = KIND == RowsKind::kGrouped;
+    const bool tail = KIND != RowsKind::kAdapter;
     const int tiles = KIND == RowsKind::kAdapter ? (a.g.n + BM - 1) / BM : count_tiles(a.g, BM, tail, lane);
     int t;
     if (!row_item(block_id<NT>(), tiles, a.m, a.mw, BN, a.parts, t, c0, part)) return false;
@@ -181,7 +201,7 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows(RowsArgs a) {
 
     const E *x = static_cast<const E *>(a.x);
     const E *w = static_cast<const E *>(a.w) + (KIND == RowsKind::kAdapter ? 0 : rt.g) * a.w_stride;
-    const int k = KIND == RowsKind::kGrouped && rt.g == a.g.G ? 0 : a.k;
+    const int k = KIND != RowsKind::kAdapter && rt.g == a.g.G ? 0 : a.k;
     int first, last;
     my_stages((k + kBk - 1) / kBk, part, a.parts, first, last);
 
@@ -235,7 +255,7 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows(RowsArgs a) {
 
     if constexpr (KIND == RowsKind::kAdapter)
         if (part == 0) add_adapters<E, KS, BM, BN, WR, WC>(a, rt, c0, sx, sw, acc, tid);
-    store_rows<E, BM, BN, WR, WC>(a, rt, c0, part, rows, acc, tid);
+    store_rows<E, KIND, BM, BN, WR, WC>(a, rt, c0, part, rows, acc, tid);
 }
 
 // Whole chunks of 16 bytes everywhere (rows padded to them with zeros) and at least BN columns: operands go from
@@ -269,7 +289,7 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows_direct(RowsArgs a) {
     for (int i = tid; i < BM; i += NT) rows[i] = rt.p0 + i < rt.p1 ? row_at(a.g, rt.p0 + i) : -1;
     __syncthreads();
 
-    const int k = KIND == RowsKind::kGrouped && rt.g == a.g.G ? 0 : a.k;
+    const int k = KIND != RowsKind::kAdapter && rt.g == a.g.G ? 0 : a.k;
     int first, last;
     my_stages((k + kBk - 1) / kBk, part, a.parts, first, last);
     const int xline = tid / XT::kCpl, xe = ((tid % XT::kCpl) ^ XT::swz(xline)) * kEpc;   // first element of the thread's chunks
@@ -324,7 +344,7 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows_direct(RowsArgs a) {
 
     if constexpr (KIND == RowsKind::kAdapter)
         if (part == 0) add_adapters<E, KS, BM, BN, WR, WC>(a, rt, c0, buf0, buf0 + XT::kBytes, acc, tid);
-    store_rows<E, BM, BN, WR, WC>(a, rt, c0, part, rows, acc, tid);
+    store_rows<E, KIND, BM, BN, WR, WC>(a, rt, c0, part, rows, acc, tid);
 }
 
 template <class E, RowsKind KIND, bool KS, int BM, int BN, int WR, int WC, bool DIRECT>
@@ -357,6 +377,7 @@ hipError_t pick(const RowsPlan &p, const RowsArgs &a, hipStream_t s) {
 
 template <class E>
 hipError_t pick_kind(RowsKind kind, bool ks, const RowsPlan &p, const RowsArgs &a, hipStream_t s) {
+    if (kind == RowsKind::kLinear) return pick<E, RowsKind::kLinear, true>(p, a, s);
     if (kind == RowsKind::kGrouped)
         return ks ? pick<E, RowsKind::kGrouped, true>(p, a, s) : pick<E, RowsKind::kGrouped, false>(p, a, s);
     return ks ? pick<E, RowsKind::kAdapter, true>(p, a, s) : pick<E, RowsKind::kAdapter, false>(p, a, s);

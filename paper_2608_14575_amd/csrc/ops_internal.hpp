@@ -2,6 +2,7 @@
 #pragma once
 
 #include "hwr_internal.hpp"
+#include "hwr_ops.h"
 #include "ops_groups.hpp"
 
 namespace hwr {
@@ -35,6 +36,16 @@ hipError_t launch_pad(bool bf16, const PadArgs &a, hipStream_t s);
 constexpr int kRankBlock = 32;
 constexpr int kLowBytes = 128;
 
+// What follows a product in a layer (kLinear): z = sums + bias[g], y = act(z) + residual.
+struct Epilogue {
+    int act;                      // hwr_act
+    const void *bias;             // [G][m] or null
+    const void *residual;         // [n][m] or null
+    int64_t ldr;                  // elements
+    void *z;                      // [n][m] or null
+    int64_t ldz;
+};
+
 // Products by row: out[r][c] = sum_e x[r][e] w_g(e, c), and for the adapter
 // plus sum_e low[place][e] lw_g(e, c).
 struct RowsArgs {
@@ -56,6 +67,7 @@ struct RowsArgs {
     const void *low;              // [n][blocks] low-rank intermediates
     const void *lw;               // [G][rank][m] (KS) or [G][m][rank]
     int rank;
+    Epilogue end;                 // layers
 };
 
 // low[place] = scale[g] x[row] w_g
@@ -99,6 +111,19 @@ struct FewArgs {
     int parts, low_parts;         // parts of the contraction
     float *partial;               // [parts][n][m_pad], with parts > 1 or an adapter
     float *low;                   // [low_parts][n][rank]
+    Epilogue end;                 // layers
+};
+
+// dz[row] = dy[row] act'(z[row]) for the rows of groups, and its sums by group.
+struct SlopeArgs {
+    GroupsArg g;
+    int m, m_pad;                 // m_pad: m up to a multiple of 8
+    const void *dy, *z;
+    int64_t lddy, ldz;            // elements
+    void *dz;                     // rows of whole, aligned chunks of 16 bytes, or null
+    int64_t lddz;
+    float *partial;               // [slope_tiles][m_pad], with dbias
+    void *dbias;                  // [G][m] or null
 };
 
 struct GroupRowsArgs {
@@ -170,7 +195,7 @@ struct AdamwArgs {
 };
 AdamwCoef adamw_coef(double lr, double beta1, double beta2, double eps, double weight_decay, uint64_t seed, int64_t step);
 
-enum class RowsKind { kGrouped, kAdapter };
+enum class RowsKind { kGrouped, kAdapter, kLinear };
 
 hipError_t launch_group_rows(const GroupRowsArgs &a, hipStream_t s);
 int group_rows_blocks(int n);
@@ -188,9 +213,11 @@ hipError_t launch_shrink_pair(bool bf16, const ShrinkArgs &direct, const ShrinkA
 bool few_rows(int n, int G, int k, int m, bool adapter, bool bf16);  // whether launch_few is meant for the batch
 int few_tiles(int n, int G, bool adapter);
 int few_parts(int n, int G, int k, int m, bool bf16, bool adapter, int cus);
-hipError_t launch_few(bool bf16, bool adapter, const FewArgs &a, hipStream_t s);
-// y[row] = sum of the partial sums of its place
-hipError_t launch_join(bool bf16, const FewArgs &a, hipStream_t s);
+hipError_t launch_few(bool bf16, RowsKind kind, const FewArgs &a, hipStream_t s);
+// y[row] = sum of the partial sums of its place (kGrouped, kLinear)
+hipError_t launch_join(bool bf16, RowsKind kind, const FewArgs &a, hipStream_t s);
+int slope_tiles(int n, int G);
+hipError_t launch_slope(bool bf16, int act, const SlopeArgs &a, hipStream_t s);
 enum class ColsKind { kDense, kLowP, kLowQ };
 // Tile, and parts of the places, for a weight gradient.
 struct ColsPlan {

@@ -25,6 +25,7 @@ HWR_FLAG_RESIDENT = 2
 HWR_SCORE_NORMALIZED, HWR_SCORE_PAPER = 0, 1
 HWR_BOUND_GIVEN, HWR_BOUND_PAPER = 0, 1
 HWR_MAX_WEIGHTS = 8
+HWR_ACT_NONE, HWR_ACT_RELU, HWR_ACT_SILU, HWR_ACT_GELU = range(4)
 HWR_K_STATE, HWR_K_QUALITY, HWR_K_GATHER, HWR_K_MLP, HWR_K_EPILOGUE, HWR_K_FUSED, HWR_K_MERGE, HWR_K_SINGLE = range(8)
 HWR_K_COUNT = 8
 KERNEL_NAMES = ["state", "quality", "gather", "mlp", "epilogue", "fused", "merge", "single"]
@@ -36,7 +37,7 @@ EXPORTS = ["hwr_init", "hwr_update_hw_state", "hwr_route_batch", "hwr_route_batc
            "hwr_probe_feature_log",
            "hwr_ops_init", "hwr_ops_free", "hwr_ops_last_error", "hwr_ops_reserve", "hwr_group_rows",
            "hwr_grouped_matmul", "hwr_grouped_matmul_grad", "hwr_adapter_matmul", "hwr_adapter_matmul_grad",
-           "hwr_log_probs", "hwr_log_probs_grad",
+           "hwr_grouped_linear", "hwr_grouped_linear_grad", "hwr_log_probs", "hwr_log_probs_grad",
            "hwr_adamw_init", "hwr_adamw_step", "hwr_adamw_free"]
 
 _STATUS = {0: "HWR_OK", -1: "HWR_ERR_INVALID_ARG", -2: "HWR_ERR_OOM", -3: "HWR_ERR_HIP",
@@ -135,6 +136,18 @@ class hwr_matmul_args(C.Structure):
 class hwr_matmul_grad_args(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("k", C.c_int32), ("m", C.c_int32), ("dy", _vp), ("lddy", C.c_int64),
                 ("x", _vp), ("ldx", C.c_int64), ("w", _vp), ("dx", _vp), ("lddx", C.c_int64), ("dw", _vp)]
+
+
+class hwr_linear_args(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("k", C.c_int32), ("m", C.c_int32), ("act", C.c_int32), ("x", _vp), ("ldx", C.c_int64),
+                ("w", _vp), ("bias", _vp), ("residual", _vp), ("ldr", C.c_int64), ("y", _vp), ("ldy", C.c_int64),
+                ("z", _vp), ("ldz", C.c_int64)]
+
+
+class hwr_linear_grad_args(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("k", C.c_int32), ("m", C.c_int32), ("act", C.c_int32), ("dy", _vp),
+                ("lddy", C.c_int64), ("z", _vp), ("ldz", C.c_int64), ("x", _vp), ("ldx", C.c_int64), ("w", _vp), ("dx", _vp),
+                ("lddx", C.c_int64), ("dw", _vp), ("dbias", _vp)]
 
 
 class hwr_adapter_args(C.Structure):
@@ -246,6 +259,7 @@ def load(path: Optional[str] = None) -> C.CDLL:
     L.hwr_group_rows.restype = C.c_int
     L.hwr_group_rows.argtypes = [_vp, C.c_int32, _vp, _vp, C.c_int32, C.c_int32, _vp, _vp]
     for fn, args in (("hwr_grouped_matmul", hwr_matmul_args), ("hwr_grouped_matmul_grad", hwr_matmul_grad_args),
+                     ("hwr_grouped_linear", hwr_linear_args), ("hwr_grouped_linear_grad", hwr_linear_grad_args),
                      ("hwr_adapter_matmul", hwr_adapter_args), ("hwr_adapter_matmul_grad", hwr_adapter_grad_args)):
         getattr(L, fn).restype = C.c_int
         getattr(L, fn).argtypes = [_vp, C.POINTER(hwr_groups), C.POINTER(args)]
@@ -385,6 +399,14 @@ def hwr_grouped_matmul(ops, groups: hwr_groups, args: hwr_matmul_args) -> None:
 
 def hwr_grouped_matmul_grad(ops, groups: hwr_groups, args: hwr_matmul_grad_args) -> None:
     _check_ops(load().hwr_grouped_matmul_grad(ops, C.byref(groups), C.byref(args)), ops)
+
+
+def hwr_grouped_linear(ops, groups: hwr_groups, args: hwr_linear_args) -> None:
+    _check_ops(load().hwr_grouped_linear(ops, C.byref(groups), C.byref(args)), ops)
+
+
+def hwr_grouped_linear_grad(ops, groups: hwr_groups, args: hwr_linear_grad_args) -> None:
+    _check_ops(load().hwr_grouped_linear_grad(ops, C.byref(groups), C.byref(args)), ops)
 
 
 def hwr_adapter_matmul(ops, groups: hwr_groups, args: hwr_adapter_args) -> None:

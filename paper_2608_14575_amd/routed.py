@@ -20,6 +20,7 @@ from .hwr import HWR_BF16, HWR_ERR_INVALID_ARG, HWR_F32, HwrError
 
 
 _MAX_INT = 2 ** 31 - 1
+_ACTS = {"none": hwr.HWR_ACT_NONE, "relu": hwr.HWR_ACT_RELU, "silu": hwr.HWR_ACT_SILU, "gelu": hwr.HWR_ACT_GELU}
 
 
 def _bad(name, msg):
@@ -88,6 +89,8 @@ class RoutedOps:
         self._lib = hwr.load()
         self._matmul = _Call(self._lib.hwr_grouped_matmul, hwr.hwr_matmul_args)
         self._matmul_grad = _Call(self._lib.hwr_grouped_matmul_grad, hwr.hwr_matmul_grad_args)
+        self._linear = _Call(self._lib.hwr_grouped_linear, hwr.hwr_linear_args)
+        self._linear_grad = _Call(self._lib.hwr_grouped_linear_grad, hwr.hwr_linear_grad_args)
         self._adapter = _Call(self._lib.hwr_adapter_matmul, hwr.hwr_adapter_args)
         self._adapter_grad = _Call(self._lib.hwr_adapter_matmul_grad, hwr.hwr_adapter_grad_args)
         self._log_probs = _Args(self._lib.hwr_log_probs, hwr.hwr_log_probs_args)
@@ -194,6 +197,39 @@ class RoutedOps:
         self._run(self._matmul_grad, n, G, offsets, order,
                   self._kinds[dt], k, m, dyp, lddy, xp, ldx, self._dense("w", w, dt, (G, k, m)), dxp, lddx,
                   0 if dw is None else self._dense("dw", dw, dt, (G, k, m)))
+
+    def _act(self, act) -> int:
+        if act not in _ACTS:
+            _bad("act", f"{act!r}, expected one of {sorted(_ACTS)}")
+        return _ACTS[act]
+
+    def linear(self, x, w, offsets, order=None, *, bias=None, act="none", residual=None, y, z=None) -> None:
+        """A layer: z[r] = x[r] w[g(r)] + bias[g(r)], y[r] = act(z[r]) + residual[r]; w [G][k][m],
+        bias [G][m], act "none", "relu", "silu" or "gelu" (of the normal distribution).  ``z``, which
+        ``linear_grad`` reads, is written where it is given.  A row in no group gets the residual, or zeros."""
+        dt, (n, k) = self._x(x)
+        G, _, m = self._weights(w)
+        xp, ldx = self._rows("x", x, dt, (n, k))
+        rp, ldr = (0, 0) if residual is None else self._rows("residual", residual, dt, (n, m))
+        yp, ldy = self._rows("y", y, dt, (n, m))
+        zp, ldz = (0, 0) if z is None else self._rows("z", z, dt, (n, m))
+        self._run(self._linear, n, G, offsets, order,
+                  self._kinds[dt], k, m, self._act(act), xp, ldx, self._dense("w", w, dt, (G, k, m)),
+                  0 if bias is None else self._dense("bias", bias, dt, (G, m)), rp, ldr, yp, ldy, zp, ldz)
+
+    def linear_grad(self, dy, x, w, offsets, order=None, *, act="none", z=None, dx=None, dw=None, dbias=None) -> None:
+        """Gradients of ``linear``: dx [n][k], dw [G][k][m] and dbias [G][m], any may be left out (the
+        residual's is dy); ``z`` is needed with an activation."""
+        dt, (n, k) = self._x(x)
+        G, _, m = self._weights(w)
+        dyp, lddy = self._rows("dy", dy, dt, (n, m))
+        zp, ldz = (0, 0) if z is None else self._rows("z", z, dt, (n, m))
+        xp, ldx = self._rows("x", x, dt, (n, k))
+        dxp, lddx = (0, 0) if dx is None else self._rows("dx", dx, dt, (n, k))
+        self._run(self._linear_grad, n, G, offsets, order,
+                  self._kinds[dt], k, m, self._act(act), dyp, lddy, zp, ldz, xp, ldx, self._dense("w", w, dt, (G, k, m)),
+                  dxp, lddx, 0 if dw is None else self._dense("dw", dw, dt, (G, k, m)),
+                  0 if dbias is None else self._dense("dbias", dbias, dt, (G, m)))
 
     def _adapters(self, dt, k, w, a, b, scale):
         """Sizes m, G and rank, and the pointers."""

@@ -1,0 +1,464 @@
+"""Layers of a routed batch (include/hwr_ops.h): product, bias, activation and residual, and
+their gradients, against 64 bits: every activation at ragged, odd, empty, strided and single-row
+sizes, with and without each operand; rows in no group; values that stay in their rows; aliases
+and refusals; graphs; and a whole training step of layer, loss and weights.
+
+Tolerances, u = 2^-24, h half a step of the type.  The sums z: (K + 18) u S, S the magnitudes' sum
+with the bias's.  An activation carries that on by its slope, at most 1.13, and is off by itself:
+  silu: (8 + 2 |z|) u |y| (an exponent of |z| log2 e rounded, an exponential, a reciprocal)
+  gelu: (8 + 2 z^2) u |y|, and in bf16 calls 3.6e-5 of |z| times the distribution's tail (its fit)
+its slope by ds: silu u (8 + 4 |z|), gelu u (8 + (8 + 2 z^2)(|z| density + tail)) and in bf16 3.6e-5 of the tail.
+The gradients of x and W are compared with products of dz rounded as the call rounds it; a dz that ds can carry
+over the middle of a step may be a whole step off."""
+import numpy as np
+import pytest
+
+from paper_2608_14575_amd import hwr, routed
+from test_gpu_routed_ops import EPS, SHAPES, TYPES, close, grouped, offset_by_one, outer, product, rand, sizes_of, strided
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+ACTS = ["none", "relu", "silu", "gelu"]
+
+
+@pytest.fixture(scope="module")
+def ops():
+    assert torch.cuda.is_available(), "GPU tests need a device"
+    o = routed.RoutedOps(stream=torch.cuda.current_stream().cuda_stream)
+    yield o
+    o.close()
+
+
+def normal(z):
+    tail = 0.5 * torch.erfc(z.abs() * 0.5 ** 0.5)
+    return torch.where(z > 0, 1 - tail, tail), tail, torch.exp(-0.5 * z * z) * 0.3989422804014327
+
+
+def activation(act, z, bf16):
+    """Value, what it is off by, slope, what that is off by."""
+    if act == "none":
+        return z, 0 * z, torch.ones_like(z), 0 * z
+    if act == "relu":
+        return z.clamp(min=0), 0 * z, (z > 0).double(), 0 * z
+    if act == "silu":
+        s = torch.sigmoid(z)
+        return z * s, (8 + 2 * z.abs()) * EPS * (z * s).abs(), s * (1 + z * (1 - s)), EPS * (8 + 4 * z.abs())
+    upto, tail, density = normal(z)
+    fit = 3.6e-5 * tail if bf16 else 0 * z
+    return (z * upto, (8 + 2 * z * z) * EPS * (z * upto).abs() + z.abs() * fit, upto + z * density,
+            EPS * (8 + (8 + 2 * z * z) * (z.abs() * density + tail)) + fit)
+
+
+def nearest(d, t):
+    return d.to(t).double()
+
+
+def rounded(d, slack, t):
+    """d as t, and how far off a value may be that is `slack` off before its rounding."""
+    lo, hi = nearest(d - slack, t), nearest(d + slack, t)
+    at = nearest(d, t)
+    return at, torch.maximum((hi - at).abs(), (at - lo).abs())
+
+
+def check_layer(out, x, w, gid, bias, act, residual, dtype):
+    t, h, _ = TYPES[dtype]
+    inside = torch.from_numpy(gid >= 0).cuda()[:, None]
+    z, s = product(x, w, gid)
+    if bias is not None:
+        at = torch.from_numpy(np.maximum(gid, 0)).cuda()
+        z, s = z + torch.where(inside, bias.double()[at], 0.0), s + torch.where(inside, bias.double()[at].abs(), 0.0)
+    tz = (x.shape[1] + 18) * EPS * s
+    y, ty, _, _ = activation(act, z, dtype == "bf16")
+    y, ty = torch.where(inside, y, 0.0), torch.where(inside, ty + 1.13 * tz, 0.0)
+    if residual is not None:
+        y, ty = y + residual.double(), ty + EPS * (y.abs() + residual.double().abs())
+    close(out["y"], y, h * y.abs() + (1 + h) * ty + 1e-38)
+    if "z" in out:
+        close(out["z"], z, h * z.abs() + (1 + h) * tz)
+    outside = ~inside[:, 0]
+    assert torch.equal(out["y"][outside], residual[outside] if residual is not None else torch.zeros_like(out["y"][outside]))
+    assert "z" not in out or (out["z"][outside] == 0).all()
+
+
+def check_gradients(out, dy, z, x, w, gid, act, dtype):
+    t, h, _ = TYPES[dtype]
+    G, k, m = w.shape
+    _, _, slope, ds = activation(act, z.double(), dtype == "bf16")
+    d64 = dy.double() * slope
+    slack = dy.double().abs() * ds + 2 * EPS * d64.abs()
+    if act == "none":
+        slack = 0 * slack
+    dz, off = rounded(d64, slack, t)
+    T = lambda v: v.transpose(1, 2).contiguous()  # noqa: E731
+    if "dx" in out:
+        ref, s = product(dz, T(w), gid)
+        close(out["dx"], ref, h * ref.abs() + (m + 16) * EPS * s + (1 + h) * product(off, T(w).abs(), gid)[0])
+    if "dw" in out:
+        ref, s, cnt = outer(x, dz, gid, G)
+        close(out["dw"], ref, h * ref.abs() + (cnt + 16) * EPS * s + (1 + h) * outer(x.abs(), off, gid, G)[0])
+    if "dbias" in out:
+        one = torch.ones(len(gid), 1, dtype=torch.float64, device="cuda")
+        ref, s, cnt = outer(one, d64, gid, G)
+        close(out["dbias"][:, None], ref, h * ref.abs() + (1 + h) * ((cnt + 16) * EPS * s + outer(one, slack, gid, G)[0]))
+
+
+CASES = [s + (ACTS[i % 4], bool(i & 1), bool(i & 2), bool(i % 3)) for i, s in enumerate(SHAPES)] + [
+    (40, 16, 256, 200, "skew", False, 0, "silu", True, True, True),
+    (1, 3, 520, 1032, "one", False, 3, "gelu", True, True, True),
+    (200, 30, 512, 512, "skew", False, 0, "gelu", True, False, True),
+    (700, 9, 640, 40, "skew", False, 5, "silu", True, True, True),
+    (9000, 2, 1024, 1032, "skew", False, 0, "gelu", True, True, True),
+    (9000, 3, 264, 1032, "skew", False, 0, "relu", False, True, True),
+    (4000, 3, 1001, 1003, "skew", False, 0, "silu", True, True, True),
+    (4000, 3, 640, 641, "skew", False, 1, "gelu", True, True, False),
+    (300, 3, 128, 128, "none", False, 0, "gelu", True, True, True),
+    (5000, 4, 64, 2, "skew", False, 0, "gelu", True, True, True),
+    (70, 2, 2048, 3, "skew", False, 0, "silu", True, True, True),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,G,k,m,kind,ordered,pad,act,biased,added,kept", CASES)
+def test_layer_and_gradients(ops, n, G, k, m, kind, ordered, pad, act, biased, added, kept, dtype):
+    t, _, _ = TYPES[dtype]
+    gen = torch.Generator("cuda").manual_seed(n + k)
+    gid, off, order = grouped(sizes_of(kind, n, G, np.random.default_rng(n)), G, ordered)
+    x, dy = strided(rand(gen, n, k, dtype=t), pad), strided(rand(gen, n, m, dtype=t), pad)
+    w = rand(gen, G, k, m, dtype=t, std=1.5 * k ** -0.5)
+    bias = rand(gen, G, m, dtype=t) if biased else None
+    res = strided(rand(gen, n, m, dtype=t), pad) if added else None
+    fresh = lambda: strided(torch.full((n, m), 7.0, dtype=t, device="cuda"), pad)  # noqa: E731
+    out = {"y": fresh(), "z": fresh()} if kept else {"y": fresh()}
+    ops.linear(x, w, off, order, bias=bias, act=act, residual=res, **out)
+    check_layer(out, x, w, gid, bias, act, res, dtype)
+    again = {q: torch.zeros_like(v) for q, v in out.items()}
+    ops.linear(x, w, off, order, bias=bias, act=act, residual=res, **again)
+    assert all(torch.equal(out[q], again[q]) for q in out)
+
+    z = strided(rand(gen, n, m, dtype=t, std=1.5), pad)
+    grads = {"dx": strided(torch.full((n, k), 7.0, dtype=t, device="cuda"), pad),
+             "dw": torch.full((G, k, m), 7.0, dtype=t, device="cuda"), "dbias": torch.full((G, m), 7.0, dtype=t, device="cuda")}
+    ops.linear_grad(dy, x, w, off, order, act=act, z=None if act == "none" else z, **grads)
+    check_gradients(grads, dy, z, x, w, gid, act, dtype)
+    for q in grads:                               # each alone: the same bits
+        alone = torch.zeros_like(grads[q])
+        ops.linear_grad(dy, x, w, off, order, act=act, z=z, **{q: alone})
+        assert torch.equal(alone, grads[q]), q
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_bare_layer_is_the_product(ops, dtype):
+    t = TYPES[dtype][0]
+    gen = torch.Generator("cuda").manual_seed(1)
+    for n, G, k, m in ((30, 4, 512, 392), (3000, 4, 264, 392), (4000, 3, 1001, 1003)):
+        gid, off, order = grouped(sizes_of("skew", n, G, np.random.default_rng(n)), G)
+        x, dy, w = rand(gen, n, k, dtype=t), rand(gen, n, m, dtype=t), rand(gen, G, k, m, dtype=t)
+        a, b, z = (torch.empty(n, m, dtype=t, device="cuda") for _ in range(3))
+        ops.matmul(x, w, off, order, y=a)
+        ops.linear(x, w, off, order, y=b, z=z)
+        assert torch.equal(a, b) and torch.equal(a, z)
+        ga, gb = [(torch.empty_like(x), torch.empty_like(w)) for _ in range(2)]
+        ops.matmul_grad(dy, x, w, off, order, dx=ga[0], dw=ga[1])
+        ops.linear_grad(dy, x, w, off, order, dx=gb[0], dw=gb[1])
+        assert torch.equal(ga[0], gb[0]) and torch.equal(ga[1], gb[1])
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_activations_over_their_range(ops, act, dtype):
+    """From sums of every size: one input of 1, the weights its sums.  Far from 0 they end as they should, without NaNs."""
+    t, h, _ = TYPES[dtype]
+    v = torch.cat([torch.linspace(-30, 30, 4001), torch.tensor([1e-30, -1e-30, 0.0, -0.0, 100, -100, 200, -200, 1e4, -1e4, 1e30, -1e30,
+                                                               3e38, -3e38])]).to(t).cuda()
+    m = len(v)
+    x, w = torch.ones(1, 1, dtype=t, device="cuda"), v.view(1, 1, m).contiguous()
+    off = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    y = torch.empty(1, m, dtype=t, device="cuda")
+    ops.linear(x, w, off, act=act, y=y)
+    ref, ty, slope, ds = activation(act, v.double(), dtype == "bf16")
+    close(y[0], ref, (h + 4 * EPS) * ref.abs() + ty + 1e-37)
+    dy, dbias = torch.ones(1, m, dtype=t, device="cuda"), torch.empty(1, m, dtype=t, device="cuda")
+    ops.linear_grad(dy, x, w, off, act=act, z=v.view(1, m), dbias=dbias)
+    near = v.abs() < 50                           # (past that ds' bound grows with z; the slope is 0 or 1 to the last bit)
+    close(dbias[0], slope, (h + 4 * EPS) * slope.abs() + torch.where(near, ds, 8 * EPS) + 1e-37)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,G,k,m", [(5, 2, 40, 72), (50, 3, 37, 131), (700, 3, 256, 128), (4000, 2, 1001, 1003), (2600, 5, 3, 2)])
+def test_pointers_aligned_to_their_elements_alone(ops, n, G, k, m, dtype):
+    t, _, _ = TYPES[dtype]
+    gen = torch.Generator("cuda").manual_seed(n + m)
+    gid, off, order = grouped(sizes_of("skew", n, G, np.random.default_rng(n)), G)
+    o = lambda *s: offset_by_one(rand(gen, *s, dtype=t))[0]  # noqa: E731
+    x, dy, z, res, w, bias = o(n, k), o(n, m), o(n, m), o(n, m), o(G, k, m), o(G, m)
+    out, around = {}, {}
+    for name, like in (("y", dy), ("z", dy), ("dx", x), ("dw", w), ("dbias", bias)):
+        out[name], around[name] = offset_by_one(torch.full_like(like, 7.0))
+    ops.linear(x, w, off, order, bias=bias, act="silu", residual=res, y=out["y"], z=out["z"])
+    ops.linear_grad(dy, x, w, off, order, act="gelu", z=z, dx=out["dx"], dw=out["dw"], dbias=out["dbias"])
+    for name, buf in around.items():
+        assert buf[0] == 5.0 and buf[-1] == 5.0, name
+    check_layer({"y": out["y"], "z": out["z"]}, x, w, gid, bias, "silu", res, dtype)
+    check_gradients({q: out[q] for q in ("dx", "dw", "dbias")}, dy, z, x, w, gid, "gelu", dtype)
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("what", ["x", "w", "bias", "residual"])
+def test_gradient_is_the_difference(ops, what, act):
+    """sum(y dy) through the operators, in fp32, against central differences of the formula in 64 bits."""
+    t = torch.float32
+    gen = torch.Generator("cuda").manual_seed(7)
+    n, G, k, m = 9, 2, 6, 5
+    gid, off, order = grouped(sizes_of("skew", n, G, np.random.default_rng(5)), G)
+    v = {"x": rand(gen, n, k, dtype=t), "w": rand(gen, G, k, m, dtype=t), "bias": rand(gen, G, m, dtype=t),
+         "residual": rand(gen, n, m, dtype=t)}
+    dy = rand(gen, n, m, dtype=t)
+    y, z = torch.empty(n, m, device="cuda"), torch.empty(n, m, device="cuda")
+    ops.linear(v["x"], v["w"], off, order, bias=v["bias"], act=act, residual=v["residual"], y=y, z=z)
+    g = {"x": torch.empty(n, k, device="cuda"), "w": torch.empty(G, k, m, device="cuda"), "bias": torch.empty(G, m, device="cuda"),
+         "residual": dy}
+    ops.linear_grad(dy, v["x"], v["w"], off, order, act=act, z=z, dx=g["x"], dw=g["w"], dbias=g["bias"])
+    inside = torch.from_numpy(gid >= 0).cuda()[:, None]
+    at = torch.from_numpy(np.maximum(gid, 0)).cuda()
+
+    def value(v):
+        s = torch.where(inside, (v["x"][:, None] @ v["w"][at])[:, 0] + v["bias"][at], 0.0)
+        if act == "relu":      # the side of every sum that the call saw: a difference does not straddle the corner
+            return ((torch.where(z > 0, s, 0.0) + v["residual"]) * dy.double()).sum()
+        return ((torch.where(inside, activation(act, s, False)[0], 0.0) + v["residual"]) * dy.double()).sum()
+
+    base = {q: u.double() for q, u in v.items()}
+    flat, step = base[what].reshape(-1), 1e-5
+    for i in range(flat.numel()):
+        side = []
+        for sign in (1, -1):
+            u = flat.clone()
+            u[i] += sign * step
+            side.append(value({**base, what: u.view_as(base[what])}))
+        # fp32 results of sums below 200 in magnitude, and the difference's own 1e-9
+        assert abs(float((side[0] - side[1]) / (2 * step) - g[what].reshape(-1)[i])) < 1e-4
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,k,m", [(40, 264, 130), (900, 264, 136), (3000, 512, 264)])
+def test_values_stay_in_their_rows_and_groups(ops, dtype, n, k, m):
+    """A row of NaNs in each operand, a group of infinite weights and biases: others do not see them,
+    and rows in no group are not touched by anything but their residual."""
+    t, _, _ = TYPES[dtype]
+    G = 4
+    gen = torch.Generator("cuda").manual_seed(n)
+    gid, off, order = grouped(sizes_of("skew", n, G, np.random.default_rng(n)), G)
+    x, res, dy, z = rand(gen, n, k, dtype=t), rand(gen, n, m, dtype=t), rand(gen, n, m, dtype=t), rand(gen, n, m, dtype=t)
+    w, bias = rand(gen, G, k, m, dtype=t), rand(gen, G, m, dtype=t)
+    free = np.nonzero(gid < 0)[0]
+    sick = np.nonzero(gid == 0)[0][0]
+    x2, z2, dy2, w2, b2 = (v.clone() for v in (x, z, dy, w, bias))
+    for v in (x2, z2, dy2):
+        v[sick] = float("nan")
+        v[torch.from_numpy(free).cuda()] = float("inf")
+    w2[3], b2[3] = float("inf"), float("nan")
+    outs = []
+    for a, b, c, d, e in ((x, z, dy, w, bias), (x2, z2, dy2, w2, b2)):
+        o = {"y": torch.empty_like(res), "z": torch.empty_like(res)}
+        g = {"dx": torch.empty_like(x), "dw": torch.empty_like(w), "dbias": torch.empty_like(bias)}
+        ops.linear(a, d, off, order, bias=e, act="gelu", residual=res, **o)
+        ops.linear_grad(c, a, d, off, order, act="silu", z=b, **g)
+        outs.append((o, g))
+    rows = torch.from_numpy(np.array([i for i in range(n) if i != sick and gid[i] != 3])).cuda()
+    (o, g), (o2, g2) = outs
+    assert torch.equal(o["y"][rows], o2["y"][rows]) and torch.equal(o["z"][rows], o2["z"][rows])
+    assert torch.equal(g["dx"][rows], g2["dx"][rows])
+    assert o2["y"][sick].isnan().all() and g2["dx"][sick].isnan().all()
+    for q in ("dw", "dbias"):
+        assert torch.equal(g[q][1:], g2[q][1:]) and g2[q][0].isnan().all()
+
+
+def test_empty_batch(ops):
+    e = lambda *s: torch.full(s, 7.0, device="cuda")  # noqa: E731
+    off, order = torch.zeros(3, dtype=torch.int32, device="cuda"), torch.zeros(0, dtype=torch.int32, device="cuda")
+    w, dw, db = e(2, 8, 16), e(2, 8, 16), e(2, 16)
+    ops.linear(e(0, 8), w, off, order, bias=e(2, 16), act="silu", residual=e(0, 16), y=e(0, 16), z=e(0, 16))
+    ops.linear_grad(e(0, 16), e(0, 8), w, off, order, act="silu", z=e(0, 16), dx=e(0, 8), dw=dw, dbias=db)
+    assert (dw == 0).all() and (db == 0).all()
+
+
+def test_rows_past_32_bit_offsets(ops):
+    """Rows whose byte and element offsets pass 2^31 and 2^32."""
+    n, k, m, G = 2200000, 8, 1000, 2
+    gen = torch.Generator("cuda").manual_seed(2)
+    x, w, bias = rand(gen, n, k, dtype=torch.bfloat16), rand(gen, G, k, m, dtype=torch.bfloat16), rand(gen, G, m, dtype=torch.bfloat16)
+    gid = np.arange(n) % 3 - 1
+    gid, off, order = grouped(gid, G)
+    res = torch.empty(n, m, dtype=torch.bfloat16, device="cuda").fill_(0.5)
+    y, z = torch.empty_like(res), torch.empty_like(res)
+    ops.linear(x, w, off, order, bias=bias, act="gelu", residual=res, y=y, z=z)
+    rows = np.r_[0:3, n // 2:n // 2 + 3, 2147483:2147486, n - 3:n]
+    check_layer({"y": y[rows], "z": z[rows]}, x[rows], w, gid[rows], bias, "gelu", res[rows], "bf16")
+    dx = torch.empty_like(x)
+    ops.linear_grad(y, x, w, off, order, act="silu", z=z, dx=dx)
+    check_gradients({"dx": dx[rows]}, y[rows], z[rows], x[rows], w, gid[rows], "silu", "bf16")
+
+
+def problem(gen, n, G, k, m, t):
+    gid, off, order = grouped(sizes_of("skew", n, G, np.random.default_rng(n)), G)
+    v = {"x": rand(gen, n, k, dtype=t), "dy": rand(gen, n, m, dtype=t), "w": rand(gen, G, k, m, dtype=t, std=k ** -0.5),
+         "bias": rand(gen, G, m, dtype=t), "res": rand(gen, n, m, dtype=t), "off": off, "order": order}
+    out = {q: torch.empty_like(v[s]) for q, s in (("y", "dy"), ("z", "dy"), ("dx", "x"), ("dw", "w"), ("dbias", "bias"))}
+    return v, out
+
+
+def layer(q, v, out, act="gelu"):
+    q.linear(v["x"], v["w"], v["off"], v["order"], bias=v["bias"], act=act, residual=v["res"], y=out["y"], z=out["z"])
+    q.linear_grad(v["dy"], v["x"], v["w"], v["off"], v["order"], act=act, z=out["z"], dx=out["dx"], dw=out["dw"], dbias=out["dbias"])
+
+
+@pytest.mark.parametrize("n,G,k,m", [(40, 16, 256, 200), (900, 3, 257, 131), (3000, 4, 512, 520)])
+def test_graph_and_other_stream(ops, n, G, k, m):
+    s = torch.cuda.Stream()
+    mine = routed.RoutedOps(stream=s.cuda_stream)
+    gen = torch.Generator("cuda").manual_seed(4)
+    v, out = problem(gen, n, G, k, m, torch.bfloat16)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        if n > 40:
+            with pytest.raises(hwr.HwrError) as e:     # work space; nothing is recorded
+                mine.linear_grad(v["dy"], v["x"], v["w"], v["off"], v["order"], act="gelu", z=v["res"], dw=out["dw"])
+            assert e.value.status == hwr.HWR_ERR_STATE
+        v["x"].add_(0)
+    layer(mine, v, out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        layer(mine, v, out)
+    for _ in range(3):
+        v["x"].copy_(rand(gen, n, k, dtype=torch.bfloat16))
+        want = {q: torch.full_like(u, 3.0) for q, u in out.items()}
+        layer(ops, v, want)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(out[q], want[q]) for q in out)
+    mine.close()
+
+
+def test_a_training_step(ops):
+    """Two layers, the log probabilities of given tokens, their gradients and the weights' step, as they are used
+    together: in fp32 against the same in 64 bits through torch's autograd, and in a captured graph."""
+    n, G, k, m, V = 500, 3, 72, 96, 301
+    gen = torch.Generator("cuda").manual_seed(6)
+    f32 = torch.float32
+    gid, off, order = grouped(sizes_of("skew", n, G, np.random.default_rng(3)), G)
+    x = rand(gen, n, k, dtype=f32)
+    p = {"w1": rand(gen, G, k, m, dtype=f32, std=k ** -0.5), "b1": rand(gen, G, m, dtype=f32, std=0.1),
+         "w2": rand(gen, G, m, V, dtype=f32, std=m ** -0.5), "b2": rand(gen, G, V, dtype=f32, std=0.1)}
+    token = torch.randint(0, V, (n,), generator=gen, device="cuda", dtype=torch.int32)
+    token[torch.from_numpy(gid < 0).cuda()] = -1
+    grads = {q: torch.empty_like(v) for q, v in p.items()}
+    e = lambda *s: torch.empty(s, device="cuda")  # noqa: E731
+    h, z, logits, dlogits, dh = e(n, m), e(n, m), e(n, V), e(n, V), e(n, m)
+    logp, lse, ent = e(n), e(n), e(n)
+    dlogp, dent = torch.full((n,), -1.0 / n, device="cuda"), torch.full((n,), 0.01 / n, device="cuda")
+    s = torch.cuda.Stream()
+    mine = routed.RoutedOps(stream=s.cuda_stream)
+    steps = torch.zeros(1, dtype=torch.int64, device="cuda")
+    first = {q: v.clone() for q, v in p.items()}
+
+    def step(q, opt):
+        q.linear(x, p["w1"], off, order, bias=p["b1"], act="silu", y=h, z=z)
+        q.linear(h, p["w2"], off, order, bias=p["b2"], y=logits)
+        q.log_probs(logits, token, logp=logp, lse=lse, entropy=ent)
+        q.log_probs_grad(logits, token, lse, dlogp, entropy=ent, dentropy=dent, dlogits=dlogits)
+        q.linear_grad(dlogits, h, p["w2"], off, order, dx=dh, dw=grads["w2"], dbias=grads["b2"])
+        q.linear_grad(dh, x, p["w1"], off, order, act="silu", z=z, dw=grads["w1"], dbias=grads["b1"])
+        opt.step()
+
+    hyper = {"lr": 1e-2, "betas": (0.9, 0.99), "weight_decay": 0.05}
+    opt = routed.AdamW(ops, list(p.values()), list(grads.values()), **hyper)
+    step(ops, opt)
+    # the same in 64 bits
+    ref = {q: v.double().requires_grad_() for q, v in first.items()}
+    at, inside = torch.from_numpy(np.maximum(gid, 0)).cuda(), torch.from_numpy(gid >= 0).cuda()
+    rows = inside.nonzero()[:, 0]
+    zz = (x.double()[rows][:, None] @ ref["w1"][at[rows]])[:, 0] + ref["b1"][at[rows]]
+    out = ((zz * torch.sigmoid(zz))[:, None] @ ref["w2"][at[rows]])[:, 0] + ref["b2"][at[rows]]
+    lp = torch.log_softmax(out, 1)
+    picked = lp.gather(1, token[rows].long()[:, None])[:, 0]
+    loss = (picked * (-1.0 / n)).sum() + (-(lp.exp() * lp).sum(1) * (0.01 / n)).sum()
+    loss.backward()
+    # values of order 10 through products of 300 terms: each within 400 u of its magnitudes, below 1e-4 of the largest gradient
+    for q in p:
+        assert (grads[q].double() - ref[q].grad).abs().max() < 1e-4 * ref[q].grad.abs().max(), q
+        g = grads[q].double()
+        want = first[q].double() * (1 - 1e-2 * 0.05) - 1e-2 * g / (g.abs() + 1e-8)
+        # (g / |g|: near eps of 1e-8, sqrt(v) is off by 8 u and m by 4 u of it)
+        assert (p[q].double() - want).abs().max() < 1e-2 * 32 * EPS + 4 * EPS * 10
+    assert (logp[~inside] == 0).all()
+    # captured: three replays are three more eager steps
+    eager = {q: v.clone() for q, v in p.items()}
+    for q in p:
+        p[q].copy_(first[q])
+    mine.reserve(1 << 26)
+    cap = routed.AdamW(mine, list(p.values()), list(grads.values()), steps=steps, **hyper)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        step(mine, cap)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(p[q], eager[q]) for q in p)
+    for _ in range(2):
+        graph.replay()
+        torch.cuda.synchronize()
+    third = {q: v.clone() for q, v in p.items()}
+    for q in p:
+        p[q].copy_(first[q])
+    opt2 = routed.AdamW(ops, list(p.values()), list(grads.values()), **hyper)
+    for _ in range(3):
+        step(ops, opt2)
+    assert int(steps) == 3 == opt2.steps and all(torch.equal(p[q], third[q]) for q in p)
+    mine.close()
+
+
+def test_refusals(ops):
+    e = lambda *s, dtype=torch.bfloat16: torch.zeros(s, dtype=dtype, device="cuda")  # noqa: E731
+    off, order = torch.zeros(3, dtype=torch.int32, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    x, y, w, b = e(4, 8), e(4, 16), e(2, 8, 16), e(2, 16)
+
+    def refused(what, f):
+        with pytest.raises(hwr.HwrError) as err:
+            f()
+        assert err.value.status == hwr.HWR_ERR_INVALID_ARG and what in str(err.value), str(err.value)
+
+    refused("act", lambda: ops.linear(x, w, off, order, act="tanh", y=y))
+    refused("act", lambda: ops.linear_grad(y, x, w, off, order, act=None, dx=e(4, 8)))
+    refused("bias", lambda: ops.linear(x, w, off, order, bias=e(16), y=y))
+    refused("bias", lambda: ops.linear(x, w, off, order, bias=b.float(), y=y))
+    refused("residual", lambda: ops.linear(x, w, off, order, residual=e(3, 16), y=y))
+    refused("residual: strides", lambda: ops.linear(x, w, off, order, residual=e(1, 16).expand(4, 16), y=y))
+    refused("z", lambda: ops.linear(x, w, off, order, y=y, z=e(4, 15)))
+    refused("may not be", lambda: ops.linear(x, w, off, order, residual=y, y=y))
+    refused("may not be", lambda: ops.linear(x, w, off, order, y=y, z=y))
+    z = e(4, 16)
+    refused("may not be", lambda: ops.linear(x, w, off, order, residual=z, y=y, z=z))
+    refused("may not be", lambda: ops.linear(e(4, 16), e(2, 16, 16), off, order, residual=z, y=z))
+    refused("z with an activation", lambda: ops.linear_grad(y, x, w, off, order, act="relu", dx=e(4, 8)))
+    refused("dbias", lambda: ops.linear_grad(y, x, w, off, order, dbias=e(16)))
+    refused("dx may not", lambda: ops.linear_grad(y, x, w, off, order, dx=x))
+    refused("dw", lambda: ops.linear_grad(y, x, w, off, order, dw=e(2, 16, 8)))
+    import ctypes as C
+    lib = hwr.load()
+    g = hwr.hwr_groups(4, 2, off.data_ptr(), order.data_ptr())
+    good = dict(dtype=hwr.HWR_BF16, k=8, m=16, act=0, x=x.data_ptr(), w=w.data_ptr(), y=y.data_ptr())
+    for change in (dict(dtype=2), dict(k=0), dict(m=65537), dict(act=4), dict(act=-1), dict(x=None), dict(w=None), dict(y=None),
+                   dict(ldx=7), dict(ldy=-1), dict(ldr=15), dict(ldz=15), dict(bias=b.data_ptr() + 1)):
+        a = hwr.hwr_linear_args(**{**good, **change})
+        assert lib.hwr_grouped_linear(ops.ctx, C.byref(g), C.byref(a)) == hwr.HWR_ERR_INVALID_ARG, change
+    good = dict(dtype=hwr.HWR_BF16, k=8, m=16, act=1, dy=y.data_ptr(), z=z.data_ptr(), x=x.data_ptr(), w=w.data_ptr(), dx=e(4, 8).data_ptr())
+    for change in (dict(dtype=2), dict(act=9), dict(z=None), dict(dy=None), dict(w=None), dict(lddy=15), dict(ldz=3), dict(lddx=7),
+                   dict(dw=w.data_ptr(), x=None), dict(dbias=b.data_ptr() + 1)):
+        a = hwr.hwr_linear_grad_args(**{**good, **change})
+        assert lib.hwr_grouped_linear_grad(ops.ctx, C.byref(g), C.byref(a)) == hwr.HWR_ERR_INVALID_ARG, change
+    assert lib.hwr_grouped_linear(ops.ctx, C.byref(g), None) == hwr.HWR_ERR_INVALID_ARG
+    assert lib.hwr_grouped_linear_grad(ops.ctx, None, C.byref(hwr.hwr_linear_grad_args(**good))) == hwr.HWR_ERR_INVALID_ARG

@@ -10,7 +10,8 @@ import pytest
 from paper_2608_14575_amd import hwr, routed
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-STRUCTS = ["hwr_log_probs_args", "hwr_log_probs_grad_args", "hwr_adamw_tensor", "hwr_adamw_config", "hwr_adamw_args"]
+STRUCTS = ["hwr_linear_args", "hwr_linear_grad_args", "hwr_log_probs_args", "hwr_log_probs_grad_args",
+           "hwr_adamw_tensor", "hwr_adamw_config", "hwr_adamw_args"]
 
 
 def test_layout_matches_header(tmp_path):

@@ -90,6 +90,14 @@ typedef enum {
 } hwr_status;
 
 typedef enum { HWR_F32 = 0, HWR_BF16 = 1 } hwr_dtype;
+
+/* What follows the sums z of a layer (hwr_ops.h) */
+typedef enum {
+    HWR_ACT_NONE = 0,             /* z                                          */
+    HWR_ACT_RELU = 1,             /* max(z, 0)                                  */
+    HWR_ACT_SILU = 2,             /* z / (1 + exp(-z))                          */
+    HWR_ACT_GELU = 3              /* z times the normal distribution at z       */
+} hwr_act;
 typedef enum { HWR_MEM_DEVICE = 0, HWR_MEM_HOST = 1 } hwr_mem;
 
 /* How a batch is computed.  FUSED: a predictor table, then the decisions from

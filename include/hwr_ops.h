@@ -130,17 +130,10 @@ hwr_status hwr_grouped_matmul_grad(hwr_ops *ops, const hwr_groups *g, const hwr_
 /* A layer: z[r] = x[r] W[g] + bias[g], y[r] = act(z[r]) + residual[r].  A row in no group has
  * y the residual (zeros without one) and z zeros.  z, which the gradient reads, is written where
  * it is not NULL; y is made of the sums before z is rounded.  y and z may not be x, the residual or each other. */
-typedef enum {
-    HWR_ACT_NONE = 0,             /* z                                          */
-    HWR_ACT_RELU = 1,             /* max(z, 0)                                  */
-    HWR_ACT_SILU = 2,             /* z / (1 + exp(-z))                          */
-    HWR_ACT_GELU = 3              /* z times the normal distribution at z       */
-} hwr_act;
-
 typedef struct {
     int32_t dtype;
     int32_t k, m;
-    int32_t act;                  /* hwr_act                                    */
+    int32_t act;                  /* hwr_act (hwr.h)                            */
     const void *x; int64_t ldx;   /* [n][k]                                     */
     const void *w;                /* [G][k][m]                                  */
     const void *bias;             /* [G][m] or NULL                             */

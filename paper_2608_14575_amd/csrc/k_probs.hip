@@ -73,16 +73,18 @@ struct Sums {
         s *= f;
         m = to;
     }
-    __device__ void join(float m2, float s2, float t2, float c2) {
-        Sums o;
-        o.m = m2, o.s = s2, o.t = t2;
-        const float to = fmaxf(m, m2);
-        rescale(to, c2);
-        o.rescale(to, c2);
-        s += o.s;
-        t += o.t;
-    }
+    __device__ void join_lanes(float c2);
 };
+
+// (of all lanes of a wave, in every lane: the largest maximum first, then one rescale and sums)
+__device__ inline void Sums::join_lanes(float c2) {
+    float to = m;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) to = fmaxf(to, __shfl_xor(to, d));
+    rescale(to, c2);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) s += __shfl_xor(s, d), t += __shfl_xor(t, d);
+}
 
 // Order of the most likely tokens: larger logits first, of equal ones the lower token.  Both
 // zeros are equal.  (A NaN has a place in the order too, so that there are always enough.)
@@ -96,12 +98,12 @@ __device__ inline uint64_t rank_key(uint32_t key, int token) { return static_cas
 
 // Candidates of a team, and what its threads exchange.
 constexpr int kCandidates = 512;
+constexpr int kShares = 64;       // maxima that the candidates' bound is found from
 struct TeamSpace {
     float m[16], s[16], t[16];
-    float most[256];
+    float most[kShares];
     uint64_t best[16];
     uint64_t candidate[kCandidates];
-    uint32_t floor;
     int count;
 };
 
@@ -111,59 +113,90 @@ __device__ inline void team_sync() {
     else __syncthreads();
 }
 
+// How many of keys[0, count) are larger.
+__device__ inline int larger(const uint64_t *keys, int count, uint64_t than) {
+    int n = 0, j = 0;
+    for (; j + 8 <= count; j += 8)
+#pragma unroll
+        for (int u = 0; u < 8; ++u) n += keys[j + u] > than;
+    for (; j < count; ++j) n += keys[j] > than;
+    return n;
+}
+
+// Chunks of a row that a thread loads at a time.
+constexpr int kLoad = 4;
+
 // out(rank, key, token) of the `top` first of the row, ranks in any order; T threads, whose largest
-// elements are `most`.
+// elements are `most`, and whose chunks, where the row has kLoad a thread at most, are `in` (KEPT; else they
+// are loaded again: to keep them takes registers that many workgroups want).
 //
-// The top-th largest of the threads' maxima bounds the top-th largest element from below, and is
-// reached by at least `top` elements: those at or above it are the candidates (a few more than
-// `top` unless values are equal), and only threads whose maximum reaches it look for them.
-// Each candidate's rank is the number of candidates before it.  Where there are more
+// The threads' maxima are joined to kShares.  The top-th largest of those bounds the top-th largest element
+// from below, and is reached by at least `top` elements: those at or above it are the candidates (a
+// few more than `top` unless values are equal: 24 for the 20th of 64, 44 for the 32nd), and only threads whose maximum reaches
+// it look for them.  Each candidate's rank is the number of candidates before it.  Where there are more
 // than kCandidates (long runs of equal logits), they are found one by one instead.
-template <class E, int T, class Out>
-__device__ inline void select_top(const Span<E> &row, int offset, int top, float most, TeamSpace &ts, int tid, Out out) {
-    constexpr int kTeams = T > 256 ? 256 : T, kShare = T / kTeams;    // of threads that share a maximum
+template <class E, int T, bool KEPT, class Out>
+__device__ inline void select_top(const Span<E> &row, const u32x4 (&in)[kLoad], int offset, int top, float most, TeamSpace &ts,
+                                  int tid, Out out) {
+    constexpr int kShare = T / kShares;    // threads that share a maximum
     float shared = most;
 #pragma unroll
     for (int d = 1; d < kShare; d <<= 1) shared = fmaxf(shared, __shfl_xor(shared, d));
-    const int team = tid / kShare;
-    if (tid % kShare == 0) ts.most[team] = shared;
-    if (tid == 0) ts.count = 0, ts.floor = 0;
+    if (tid % kShare == 0) ts.most[tid / kShare] = shared;
+    if (tid == 0) ts.count = 0;
     team_sync<T>();
-    if (tid % kShare == 0) {
-        int before = 0;
-        for (int i = 0; i < kTeams; i += 4) {
-            const f32x4 o = *reinterpret_cast<const f32x4 *>(&ts.most[i]);
+    // (each wave for itself, bit by bit from the top: the largest key that `top` shares reach.  The low half of a bf16
+    // value's key tells nothing: without it the bound is at most the value.)
+    const uint32_t key = order_key(ts.most[tid & 63]);
+    uint32_t floor = 0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) before += o[j] > shared || (o[j] == shared && i + j < team);
-        }
-        // (kMasked: threads without elements, or with masks alone: all elements are candidates)
-        if (before == top - 1 && shared > kMasked) ts.floor = order_key(shared);
+    for (int bit = 31; bit >= (sizeof(E) == 2 ? 16 : 0); --bit) {
+        const uint32_t at = floor | 1u << bit;
+        if (__popcll(__ballot(key >= at)) >= top) floor = at;
     }
-    team_sync<T>();
-    const uint32_t floor = ts.floor;
-    auto each = [&](auto visit) {
-        const int e = row.single(tid);
-        if (e >= 0) visit(order_key(static_cast<float>(row.p[e])), offset + e);
-        for (int c = tid; c < row.chunks; c += T) {
-            float f[kEpc<E>];
-            unpack<E>(row.load(c), f);
+    // (kMasked: threads without elements, or with masks alone: all elements are candidates)
+    if (floor <= order_key(kMasked)) floor = 0;
+    const float bound = floor ? key_value(floor) : -INFINITY;
+    // chunks of the row: the thread's
+    auto chunks = [&](bool kept, auto visit) {
+        if (KEPT && kept && row.chunks <= kLoad * T) {
 #pragma unroll
-            for (int i = 0; i < kEpc<E>; ++i) visit(order_key(f[i]), offset + row.first(c) + i);
+            for (int u = 0; u < kLoad; ++u)
+                if (tid + u * T < row.chunks) visit(in[u], tid + u * T);
+        } else {
+#pragma unroll 1
+            for (int c = tid; c < row.chunks; c += T) visit(row.load(c), c);
         }
     };
-    if (floor == 0 || order_key(most) >= floor)
-        each([&](uint32_t key, int token) {
-            if (key < floor) return;
+    auto elements = [&](u32x4 v, int c, auto visit) {
+        float f[kEpc<E>];
+        unpack<E>(v, f);
+#pragma unroll
+        for (int i = 0; i < kEpc<E>; ++i) visit(f[i], offset + row.first(c) + i);
+    };
+    if (floor == 0 || most >= bound) {
+        auto add = [&](float x, int token) {
+            if (floor && !(x >= bound)) return;
             const int at = atomicAdd(&ts.count, 1);
-            if (at < kCandidates) ts.candidate[at] = rank_key(key, token);
+            if (at < kCandidates) ts.candidate[at] = rank_key(order_key(x), token);
+        };
+        const int e = row.single(tid);
+        if (e >= 0) add(static_cast<float>(row.p[e]), offset + e);
+        chunks(true, [&](u32x4 v, int c) {
+            // (a wave goes through the elements of a chunk where one of its lanes has a candidate in it)
+            float f[kEpc<E>], largest = -INFINITY;
+            unpack<E>(v, f);
+#pragma unroll
+            for (int i = 0; i < kEpc<E>; ++i) largest = fmaxf(largest, f[i]);
+            if (floor == 0 || largest >= bound) elements(v, c, add);
         });
+    }
     team_sync<T>();
     const int count = ts.count;
     if (count <= kCandidates) {
         for (int i = tid; i < count; i += T) {
             const uint64_t mine = ts.candidate[i];
-            int before = 0;
-            for (int j = 0; j < count; ++j) before += ts.candidate[j] > mine;
+            const int before = larger(ts.candidate, count, mine);
             if (before < top) out(before, static_cast<uint32_t>(mine >> 32), static_cast<int>(~static_cast<uint32_t>(mine)));
         }
         return;
@@ -171,10 +204,13 @@ __device__ inline void select_top(const Span<E> &row, int offset, int top, float
     uint64_t last = ~uint64_t{0};
     for (int r = 0; r < top; ++r) {
         uint64_t best = 0;
-        each([&](uint32_t key, int token) {
-            const uint64_t k = rank_key(key, token);
+        auto next = [&](float x, int token) {
+            const uint64_t k = rank_key(order_key(x), token);
             if (k < last && k > best) best = k;
-        });
+        };
+        const int e = row.single(tid);
+        if (e >= 0) next(static_cast<float>(row.p[e]), offset + e);
+        chunks(false, [&](u32x4 v, int c) { elements(v, c, next); });
 #pragma unroll
         for (int d = 32; d; d >>= 1) best = max(best, static_cast<uint64_t>(__shfl_xor(static_cast<unsigned long long>(best), d)));
         if constexpr (T > 64) {
@@ -219,11 +255,12 @@ __device__ inline uint64_t *part_top(const ProbsArgs &a, int64_t r, int part) {
 }
 
 // T threads to a row, or to a part of it; 256 / T rows to a workgroup where T is less.
-template <class E, int T>
-__global__ void __launch_bounds__(T < 256 ? 256 : T) k_probs(ProbsArgs a) {
-    constexpr int NT = T < 256 ? 256 : T, kRows = NT / T, U = 4;
+template <class E, int T, bool TOP>
+__global__ void __launch_bounds__(T < 256 ? 256 : T, T == 64 ? 8 : 1) k_probs(ProbsArgs a) {
+    constexpr int NT = T < 256 ? 256 : T, kRows = NT / T, U = kLoad;
     static_assert(T == 64 || kRows == 1);
     __shared__ TeamSpace space[kRows];
+    constexpr bool kKept = T == 1024;
     const int tid = threadIdx.x % T, lane = tid & 63;
     TeamSpace &ts = space[threadIdx.x / T];
     const int64_t item = static_cast<int64_t>(block_id<NT>()) * kRows + threadIdx.x / T;
@@ -241,8 +278,8 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T) k_probs(ProbsArgs a) {
         v.m = fmaxf(v.m, x);
         v.add(x, c2);
     }
+    u32x4 in[U];
     for (int c = tid; c < row.chunks; c += U * T) {
-        u32x4 in[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const uint32_t none = sizeof(E) == 2 ? 0xFF80FF80u : 0xFF800000u;      // -inf
@@ -264,27 +301,27 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T) k_probs(ProbsArgs a) {
     }
 
     const float mine = v.m;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v.join(__shfl_xor(v.m, d), __shfl_xor(v.s, d), __shfl_xor(v.t, d), c2);
+    v.join_lanes(c2);
     if constexpr (T > 64) {
         if (lane == 0) ts.m[tid >> 6] = v.m, ts.s[tid >> 6] = v.s, ts.t[tid >> 6] = v.t;
         __syncthreads();
         v = Sums{};
-        for (int w = 0; w < T / 64; ++w) v.join(ts.m[w], ts.s[w], ts.t[w], c2);
+        if (lane < T / 64) v.m = ts.m[lane], v.s = ts.s[lane], v.t = ts.t[lane];
+        v.join_lanes(c2);
     }
     const float log_s = logf(v.s);
     if (a.parts > 1) {
         if (tid == 0) *part_sums(a, r, part) = f32x4{v.m, v.s, v.t, 0.0f};
-        if (a.top) {
+        if constexpr (TOP) {
             uint64_t *out = part_top(a, r, part);    // (a part has more elements than kMaxTop)
-            select_top<E, T>(row, first, a.top, mine, ts, tid,
+            select_top<E, T, kKept>(row, in, first, a.top, mine, ts, tid,
                              [&](int rank, uint32_t key, int token) { out[rank] = rank_key(key, token); });
         }
         return;
     }
     if (tid == 0) store_sums<E>(a, r, v, log_s);
-    if (a.top)
-        select_top<E, T>(row, 0, a.top, mine, ts, tid, [&](int rank, uint32_t key, int token) {
+    if constexpr (TOP)
+        select_top<E, T, kKept>(row, in, 0, a.top, mine, ts, tid, [&](int rank, uint32_t key, int token) {
             if (a.top_logp) a.top_logp[r * a.top + rank] = log_prob(a, v, log_s, key_value(key));
             if (a.top_token) a.top_token[r * a.top + rank] = token;
         });
@@ -292,7 +329,7 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T) k_probs(ProbsArgs a) {
 
 // A row's results from those of its parts.
 constexpr int kMaxParts = 16;
-constexpr int kPartElements = 4096;
+constexpr int kPartElements = 16384;
 static_assert(kPartElements >= kMaxTop);
 constexpr int kJoinThreads = 256;
 template <class E>
@@ -303,10 +340,11 @@ __global__ void __launch_bounds__(kJoinThreads) k_probs_join(ProbsArgs a) {
     if (r >= a.n) return;
     const float c2 = a.scale * kLog2e;
     Sums v;
-    for (int p = 0; p < a.parts; ++p) {
-        const f32x4 o = *part_sums(a, r, p);
-        v.join(o[0], o[1], o[2], c2);
+    if ((tid & 63) < a.parts) {
+        const f32x4 o = *part_sums(a, r, tid & 63);
+        v.m = o[0], v.s = o[1], v.t = o[2];
     }
+    v.join_lanes(c2);
     const float log_s = logf(v.s);
     if (tid == 0) store_sums<E>(a, r, v, log_s);
     if (!a.top) return;
@@ -316,8 +354,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_probs_join(ProbsArgs a) {
     __syncthreads();
     for (int i = tid; i < count; i += kJoinThreads) {
         const uint64_t mine = key[i];
-        int before = 0;
-        for (int j = 0; j < count; ++j) before += key[j] > mine;
+        const int before = larger(key, count, mine);
         if (before >= a.top) continue;
         if (a.top_logp) a.top_logp[r * a.top + before] = log_prob(a, v, log_s, key_value(static_cast<uint32_t>(mine >> 32)));
         if (a.top_token) a.top_token[r * a.top + before] = static_cast<int>(~static_cast<uint32_t>(mine));
@@ -384,13 +421,18 @@ hipError_t go(const ProbsArgs &a, hipStream_t s) {
     constexpr int NT = T < 256 ? 256 : T, kRows = NT / T;
     const int64_t blocks = kRows > 1 ? (a.n + kRows - 1) / kRows : a.n * a.parts;
     if (blocks > INT32_MAX - grid_row(NT)) return hipErrorInvalidValue;
-    hipError_t e = launch_kernel(k_probs<E, T>, wide_grid(blocks, NT), dim3(NT), 0, s, a);
+    hipError_t e = a.top ? launch_kernel(k_probs<E, T, true>, wide_grid(blocks, NT), dim3(NT), 0, s, a)
+                         : launch_kernel(k_probs<E, T, false>, wide_grid(blocks, NT), dim3(NT), 0, s, a);
     if (e != hipSuccess || a.parts == 1) return e;
     return launch_kernel(k_probs_join<E>, wide_grid(a.n, kJoinThreads), dim3(kJoinThreads), 0, s, a);
 }
+// Rows up to kWaveElements have a wave each; longer ones 256 threads, or 1024 where workgroups are
+// few and long.
+constexpr int kWaveElements = 2048, kFewTeams = 512, kTeamElements = 8192;
 template <class E>
 hipError_t pick(const ProbsArgs &a, hipStream_t s) {
-    if (a.m <= 2048) return go<E, 64>(a, s);
+    if (a.m <= kWaveElements) return go<E, 64>(a, s);
+    if (a.n * a.parts <= kFewTeams && a.m / a.parts >= kTeamElements) return go<E, 1024>(a, s);
     return go<E, 256>(a, s);
 }
 
@@ -404,7 +446,7 @@ hipError_t go_grad(const ProbsGradArgs &a, hipStream_t s) {
 }
 template <class E>
 hipError_t pick_grad(const ProbsGradArgs &a, hipStream_t s) {
-    if (a.m <= 2048) return go_grad<E, 64>(a, s);
+    if (a.m <= kWaveElements) return go_grad<E, 64>(a, s);
     return go_grad<E, 256>(a, s);
 }
 
@@ -412,8 +454,8 @@ hipError_t pick_grad(const ProbsGradArgs &a, hipStream_t s) {
 
 // Rows are shared where there are fewer than compute units, in parts of at least kPartElements.
 int probs_parts(bool bf16, int64_t n, int m, int cus) {
-    if (m <= 2048) return 1;
-    const int64_t want = (cus + n - 1) / n;
+    if (m <= kWaveElements) return 1;
+    const int64_t want = cus / n;
     return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({want, m / kPartElements, kMaxParts})));
 }
 uint64_t probs_bytes(const ProbsArgs &a) {

@@ -163,6 +163,60 @@ __device__ inline void store_rows(const RowsArgs &a, const RowTile &rt, int c0, 
     }
 }
 
+// A layer's tile: what follows the product goes over whole rows.  A lane's sums are four columns of 16 rows'
+// distance; two row fragments of every wave at a time pass through LDS (fp32, in turn through the two stage
+// buffers, which the products are done with), and come back as 16-byte chunks of a row, neighbouring
+// lanes neighbouring chunks: the residual is read, y and z are written 128 bytes and more at a time.  (Straight
+// from the sums, 8 bytes of 16 rows at a time, 12,288 rows 2048 x 4096 in 8 groups with gelu, residual and z took 409 us.)
+// Chunk c of row i is stored at c ^ (i % 16): writes of 16 rows, and reads, spread over the banks.
+template <class E, int BM, int BN, int WR, int WC>
+__device__ inline void store_layer(const RowsArgs &a, const RowTile &rt, int c0, const int *rows, char *buf0, char *buf1,
+                                   const f32x4 (&acc)[BM / WR / 16][BN / WC / 16], int tid) {
+    constexpr int NT = WR * WC * 64, RF = BM / WR / 16, CF = BN / WC / 16, V = 16 / sizeof(E);
+    constexpr int kTurnRows = 32 * WR, kLine = BN * 4, kCpr = BN / V, U = kTurnRows * kCpr / NT;
+    static_assert(RF % 2 == 0 && NT % kCpr == 0 && kTurnRows * kLine <= (BM + BN) * kStageBytes);
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WC, wc = wave % WC;
+    const int col = tid % kCpr;
+    const Finish<E, V> finish(a.end, c0 + col * V, a.m, a.g.G, rt.g);
+    Some<E, V> res[2][U];
+    int row[2][U];
+    auto fetch = [&](int turn) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = u * (NT / kCpr) + tid / kCpr;        // row of the turn
+            row[turn & 1][u] = rows[i / 32 * (RF * 16) + turn * 32 + i % 32];
+            finish.load(max(row[turn & 1][u], 0), res[turn & 1][u]);
+        }
+    };
+    fetch(0);
+#pragma unroll
+    for (int turn = 0; turn < RF / 2; ++turn) {
+        char *buf = turn & 1 ? buf1 : buf0;
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int j = 0; j < CF; ++j) {
+                const int i = wr * 32 + f * 16 + (lane & 15), c = (wc * CF + j) * 4 + (lane >> 4);
+                *reinterpret_cast<f32x4 *>(buf + i * kLine + ((c ^ (i & 15)) << 4)) = acc[turn * 2 + f][j];
+            }
+        if (turn + 1 < RF / 2) fetch(turn + 1);
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = u * (NT / kCpr) + tid / kCpr;
+            float v[V];
+#pragma unroll
+            for (int h = 0; h < V / 4; ++h) {
+                const f32x4 s = *reinterpret_cast<const f32x4 *>(buf + i * kLine + (((col * (V / 4) + h) ^ (i & 15)) << 4));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[h * 4 + e] = s[e];
+            }
+            const int r = row[turn & 1][u];
+            if (r >= 0) finish.store(r, res[turn & 1][u], v, static_cast<E *>(a.y), a.ldy);
+        }
+    }
+}
+
 // The workgroup's tile of places, first column and part.  False past the last tile.
 template <RowsKind KIND, int BM, int BN, int NT>
 __device__ inline bool my_tile(const RowsArgs &a, int lane, RowTile &rt, int &c0, int &part) {
@@ -344,6 +398,9 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows_direct(RowsArgs a) {
 
     if constexpr (KIND == RowsKind::kAdapter)
         if (part == 0) add_adapters<E, KS, BM, BN, WR, WC>(a, rt, c0, buf0, buf0 + XT::kBytes, acc, tid);
+    if constexpr (KIND == RowsKind::kLinear) {
+        if (a.parts == 1) return store_layer<E, BM, BN, WR, WC>(a, rt, c0, rows, buf0, buf1, acc, tid);
+    }
     store_rows<E, KIND, BM, BN, WR, WC>(a, rt, c0, part, rows, acc, tid);
 }
 

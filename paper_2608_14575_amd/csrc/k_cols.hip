@@ -267,6 +267,19 @@ __device__ inline void cols_direct(const ColsArgs &a, int block, char *buf0, cha
         if constexpr (kDeep) run_stages_deep<E, PT, QT, PF, QF, UP + UQ>(stages, issue, buf0, buf1, buf2, buf3, p_at, q_at, lane, acc);
         else run_stages<E, PT, QT, PF, QF>(stages, issue, buf0, buf1, p_at, q_at, lane, acc);
     }
+    if constexpr (KIND == ColsKind::kDense) {
+        if (a.parts == 1) {                // whole rows of the output
+            using L = ThroughLds<E, BP, BQ, WP, WQ>;
+            const int q = t.iq * BQ + L::column(tid);
+            E *out = static_cast<E *>(a.out) + static_cast<int64_t>(t.g) * a.np * a.nq;
+            __syncthreads();               // (the last products have read the buffers)
+            L::run(buf0, buf1, acc, tid, [](int, int, int) {}, [&](int, int, int row, const float (&v)[L::V]) __attribute__((always_inline)) {
+                const int p = t.ip * BP + row;
+                if (p < a.np && q < a.nq) Some<E, L::V>(v).store(out + static_cast<int64_t>(p) * a.nq, q, a.nq);
+            });
+            return;
+        }
+    }
     store_tile<E, KIND, BP, BQ, WP, WQ>(a, t, acc, lane, wp, wq);
 }
 

@@ -111,26 +111,31 @@ __device__ inline void add_adapters(const RowsArgs &a, const RowTile &rt, int c0
 }
 
 // A lane holds, for row l % 16 of fragment i, four columns of fragment j.
+template <class E, int BM, int BN, int WR, int WC>
+__device__ inline void store_parts(const RowsArgs &a, const RowTile &rt, int c0, int part,
+                                   const f32x4 (&acc)[BM / WR / 16][BN / WC / 16], int tid) {
+    constexpr int RF = BM / WR / 16, CF = BN / WC / 16;
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WC, wc = wave % WC;
+    const int q = lane >> 4;
+    float *out = a.partial + static_cast<int64_t>(part) * a.g.n * a.m_pad;
+#pragma unroll
+    for (int i = 0; i < RF; ++i) {
+        const int p = rt.p0 + (wr * RF + i) * 16 + (lane & 15);
+        if (p >= rt.p1) continue;
+#pragma unroll
+        for (int j = 0; j < CF; ++j) {
+            const int c = c0 + (wc * CF + j) * 16 + q * 4;
+            if (c < a.m_pad) *reinterpret_cast<f32x4_a4 *>(out + static_cast<int64_t>(p) * a.m_pad + c) = acc[i][j];
+        }
+    }
+}
 template <class E, RowsKind KIND, int BM, int BN, int WR, int WC>
 __device__ inline void store_rows(const RowsArgs &a, const RowTile &rt, int c0, int part, const int *rows,
                                   const f32x4 (&acc)[BM / WR / 16][BN / WC / 16], int tid) {
     constexpr int RF = BM / WR / 16, CF = BN / WC / 16;
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WC, wc = wave % WC;
     const int q = lane >> 4;
-    if (a.parts > 1) {
-        float *out = a.partial + static_cast<int64_t>(part) * a.g.n * a.m_pad;
-#pragma unroll
-        for (int i = 0; i < RF; ++i) {
-            const int p = rt.p0 + (wr * RF + i) * 16 + (lane & 15);
-            if (p >= rt.p1) continue;
-#pragma unroll
-            for (int j = 0; j < CF; ++j) {
-                const int c = c0 + (wc * CF + j) * 16 + q * 4;
-                if (c < a.m_pad) *reinterpret_cast<f32x4_a4 *>(out + static_cast<int64_t>(p) * a.m_pad + c) = acc[i][j];
-            }
-        }
-        return;
-    }
+    if (a.parts > 1) return store_parts<E, BM, BN, WR, WC>(a, rt, c0, part, acc, tid);
     E *y = static_cast<E *>(a.y);
     if constexpr (KIND == RowsKind::kLinear) {
 #pragma unroll
@@ -163,58 +168,28 @@ __device__ inline void store_rows(const RowsArgs &a, const RowTile &rt, int c0, 
     }
 }
 
-// A layer's tile: what follows the product goes over whole rows.  A lane's sums are four columns of 16 rows'
-// distance; two row fragments of every wave at a time pass through LDS (fp32, in turn through the two stage
-// buffers, which the products are done with), and come back as 16-byte chunks of a row, neighbouring
-// lanes neighbouring chunks: the residual is read, y and z are written 128 bytes and more at a time.  (Straight
-// from the sums, 8 bytes of 16 rows at a time, 12,288 rows 2048 x 4096 in 8 groups with gelu, residual and z took 409 us.)
-// Chunk c of row i is stored at c ^ (i % 16): writes of 16 rows, and reads, spread over the banks.
-template <class E, int BM, int BN, int WR, int WC>
-__device__ inline void store_layer(const RowsArgs &a, const RowTile &rt, int c0, const int *rows, char *buf0, char *buf1,
-                                   const f32x4 (&acc)[BM / WR / 16][BN / WC / 16], int tid) {
-    constexpr int NT = WR * WC * 64, RF = BM / WR / 16, CF = BN / WC / 16, V = 16 / sizeof(E);
-    constexpr int kTurnRows = 32 * WR, kLine = BN * 4, kCpr = BN / V, U = kTurnRows * kCpr / NT;
-    static_assert(RF % 2 == 0 && NT % kCpr == 0 && kTurnRows * kLine <= (BM + BN) * kStageBytes);
-    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WC, wc = wave % WC;
-    const int col = tid % kCpr;
-    const Finish<E, V> finish(a.end, c0 + col * V, a.m, a.g.G, rt.g);
-    Some<E, V> res[2][U];
-    int row[2][U];
-    auto fetch = [&](int turn) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int i = u * (NT / kCpr) + tid / kCpr;        // row of the turn
-            row[turn & 1][u] = rows[i / 32 * (RF * 16) + turn * 32 + i % 32];
-            finish.load(max(row[turn & 1][u], 0), res[turn & 1][u]);
-        }
+// A tile's rows, whole: y and z written, and the residual read, in chunks (through_lds).
+template <class E, RowsKind KIND, int BM, int BN, int WR, int WC>
+__device__ inline void store_whole_rows(const RowsArgs &a, const RowTile &rt, int c0, const int *rows, char *buf0, char *buf1,
+                                        const f32x4 (&acc)[BM / WR / 16][BN / WC / 16], int tid) {
+    using T = ThroughLds<E, BM, BN, WR, WC>;
+    constexpr int V = T::V;
+    constexpr bool kLayer = KIND == RowsKind::kLinear;
+    const int c = c0 + T::column(tid);
+    const Finish<E, V> finish(a.end, c, a.m, a.g.G, rt.g);     // (layers)
+    Some<E, V> res[2][T::U];
+    int row[2][T::U];
+    auto fetch = [&](int turn, int u, int i) __attribute__((always_inline)) {
+        row[turn & 1][u] = rows[i];
+        if constexpr (kLayer) finish.load(max(row[turn & 1][u], 0), res[turn & 1][u]);
     };
-    fetch(0);
-#pragma unroll
-    for (int turn = 0; turn < RF / 2; ++turn) {
-        char *buf = turn & 1 ? buf1 : buf0;
-#pragma unroll
-        for (int f = 0; f < 2; ++f)
-#pragma unroll
-            for (int j = 0; j < CF; ++j) {
-                const int i = wr * 32 + f * 16 + (lane & 15), c = (wc * CF + j) * 4 + (lane >> 4);
-                *reinterpret_cast<f32x4 *>(buf + i * kLine + ((c ^ (i & 15)) << 4)) = acc[turn * 2 + f][j];
-            }
-        if (turn + 1 < RF / 2) fetch(turn + 1);
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int i = u * (NT / kCpr) + tid / kCpr;
-            float v[V];
-#pragma unroll
-            for (int h = 0; h < V / 4; ++h) {
-                const f32x4 s = *reinterpret_cast<const f32x4 *>(buf + i * kLine + (((col * (V / 4) + h) ^ (i & 15)) << 4));
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[h * 4 + e] = s[e];
-            }
-            const int r = row[turn & 1][u];
-            if (r >= 0) finish.store(r, res[turn & 1][u], v, static_cast<E *>(a.y), a.ldy);
-        }
-    }
+    auto put = [&](int turn, int u, int, const float (&v)[V]) __attribute__((always_inline)) {
+        const int r = row[turn & 1][u];
+        if (r < 0 || c >= a.m) return;
+        if constexpr (kLayer) finish.store(r, res[turn & 1][u], v, static_cast<E *>(a.y), a.ldy);
+        else Some<E, V>(v).store(static_cast<E *>(a.y) + r * a.ldy, c, a.m);
+    };
+    T::run(buf0, buf1, acc, tid, fetch, put);
 }
 
 // The workgroup's tile of places, first column and part.  False past the last tile.
@@ -398,10 +373,8 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows_direct(RowsArgs a) {
 
     if constexpr (KIND == RowsKind::kAdapter)
         if (part == 0) add_adapters<E, KS, BM, BN, WR, WC>(a, rt, c0, buf0, buf0 + XT::kBytes, acc, tid);
-    if constexpr (KIND == RowsKind::kLinear) {
-        if (a.parts == 1) return store_layer<E, BM, BN, WR, WC>(a, rt, c0, rows, buf0, buf1, acc, tid);
-    }
-    store_rows<E, KIND, BM, BN, WR, WC>(a, rt, c0, part, rows, acc, tid);
+    if (a.parts == 1) store_whole_rows<E, KIND, BM, BN, WR, WC>(a, rt, c0, rows, buf0, buf1, acc, tid);
+    else store_parts<E, BM, BN, WR, WC>(a, rt, c0, part, acc, tid);
 }
 
 template <class E, RowsKind KIND, bool KS, int BM, int BN, int WR, int WC, bool DIRECT>

@@ -74,29 +74,6 @@ __device__ __host__ __forceinline__ auto with_act(int act, Run &&run) {
     return run(std::integral_constant<int, HWR_ACT_NONE>{});
 }
 
-// V neighbouring elements of a line of m, from column c < m on.
-template <class E, int V>
-struct __attribute__((packed, aligned(sizeof(E)))) Some {
-    E e[V];
-    __device__ __forceinline__ void load(const E *line, int c, int m) {
-        if (c + V <= m) {
-            *this = *reinterpret_cast<const Some *>(line + c);
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i) e[i] = line[min(c + i, m - 1)];
-        }
-    }
-    __device__ __forceinline__ void store(E *line, int c, int m) const {
-        if (c + V <= m) {
-            *reinterpret_cast<Some *>(line + c) = *this;
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (c + i < m) line[c + i] = e[i];
-        }
-    }
-};
-
 // What follows a product for V neighbouring columns c (below m) of rows of one group (g == G: of none, which
 // have zeros for z and no activation).
 template <class E, int V>

@@ -144,6 +144,34 @@ __device__ inline void store_four(E *line, int c, int m, f32x4 v) {
     }
 }
 
+// V neighbouring elements of a line of m, from column c < m on.
+template <class E, int V>
+struct __attribute__((packed, aligned(sizeof(E)))) Some {
+    E e[V];
+    Some() = default;
+    __device__ __forceinline__ explicit Some(const float (&v)[V]) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) e[i] = static_cast<E>(v[i]);
+    }
+    __device__ __forceinline__ void load(const E *line, int c, int m) {
+        if (c + V <= m) {
+            *this = *reinterpret_cast<const Some *>(line + c);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) e[i] = line[min(c + i, m - 1)];
+        }
+    }
+    __device__ __forceinline__ void store(E *line, int c, int m) const {
+        if (c + V <= m) {
+            *reinterpret_cast<Some *>(line + c) = *this;
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (c + i < m) line[c + i] = e[i];
+        }
+    }
+};
+
 // Operand fragment j of V 16-byte vectors: element j of each.
 __device__ inline bf16x8 column(const u32x4 (&in)[8], int j) {
     union { u32x4 v; bf16x8 f; } o;
@@ -347,5 +375,63 @@ __device__ inline void run_stages_deep(int stages, Issue issue, char *buf0, char
         if (++s >= stages) break;
     }
 }
+
+// ---------------------------------------------------------------- whole rows
+// A tile's sums by rows.  A lane's are four columns of one row of 16: stored from there, a wave writes 8 bytes
+// (bf16) of 16 rows at a time.  Here two row fragments of every wave pass through LDS (fp32, in turn
+// through two buffers of a stage, which the products are done with) and come back as 16-byte chunks of a
+// row, neighbouring lanes neighbouring chunks, so that memory is written, and read, 128 bytes and more at a time.
+// us, through LDS / from the sums: layers of 12,288 rows 2048 x 4096 in 8 groups with gelu, residual and z 314 / 409;
+// products of 12,000 rows 2048 x 2048 106 / 113, with adapters 130 / 140, of 16,384 rows 2048 x 4096 in 16 groups 349 / 364.
+// Chunk c of row i is stored at c ^ (i % 16): writes of 16 rows, and reads, spread over the banks.
+template <class E, int BM, int BN, int WR, int WC>
+struct ThroughLds {
+    static constexpr int NT = WR * WC * 64, RF = BM / WR / 16, CF = BN / WC / 16;
+    static constexpr int V = 16 / sizeof(E);                   // columns of a chunk
+    static constexpr int kCpr = BN / V;                        // chunks of a row
+    static constexpr int U = 32 * WR * kCpr / NT;              // chunks of a thread in a turn
+    static constexpr int kLine = BN * 4;
+    static_assert(RF % 2 == 0 && NT % kCpr == 0 && 32 * WR * kLine <= (BM + BN) * kStageBytes);
+    // first column of the thread's chunks
+    static __device__ int column(int tid) { return tid % kCpr * V; }
+    // prepare(turn, u, row) for the thread's chunks of a turn before its barrier, put(turn, u, row, values) after it;
+    // rows count from the tile's first
+    template <class Prepare, class Put>
+    static __device__ __forceinline__ void run(char *buf0, char *buf1, const f32x4 (&acc)[RF][CF], int tid, Prepare prepare, Put put) {
+        const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WC, wc = wave % WC;
+        const int col = tid % kCpr;
+        auto row_of = [&](int turn, int i) { return i / 32 * (RF * 16) + turn * 32 + i % 32; };
+        auto mine = [&](int u) { return u * (NT / kCpr) + tid / kCpr; };
+#pragma unroll
+        for (int u = 0; u < U; ++u) prepare(0, u, row_of(0, mine(u)));
+#pragma unroll
+        for (int turn = 0; turn < RF / 2; ++turn) {
+            char *buf = turn & 1 ? buf1 : buf0;
+#pragma unroll
+            for (int f = 0; f < 2; ++f)
+#pragma unroll
+                for (int j = 0; j < CF; ++j) {
+                    const int i = wr * 32 + f * 16 + (lane & 15), chunk = (wc * CF + j) * 4 + (lane >> 4);
+                    *reinterpret_cast<f32x4 *>(buf + i * kLine + ((chunk ^ (i & 15)) << 4)) = acc[turn * 2 + f][j];
+                }
+            if (turn + 1 < RF / 2)
+#pragma unroll
+                for (int u = 0; u < U; ++u) prepare(turn + 1, u, row_of(turn + 1, mine(u)));
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = mine(u);
+                float v[V];
+#pragma unroll
+                for (int h = 0; h < V / 4; ++h) {
+                    const f32x4 s = *reinterpret_cast<const f32x4 *>(buf + i * kLine + (((col * (V / 4) + h) ^ (i & 15)) << 4));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[h * 4 + e] = s[e];
+                }
+                put(turn, u, row_of(turn, i), v);
+            }
+        }
+    }
+};
 
 }  // namespace hwr

@@ -19,7 +19,7 @@ BUILD = os.path.join(PKG, "_build")
 SOURCES = ["hwr_api.hip", "k_common.hip", "k_bf16.hip", "k_table.hip", "k_route.hip", "k_f32.hip",
            "k_single.hip", "k_probe.hip", "hwr_sim.cpp",
            "hwr_ops.hip", "k_group.hip", "k_rows.hip", "k_few.hip", "k_shrink.hip", "k_cols.hip", "k_pad.hip",
-           "hwr_train.hip", "k_probs.hip", "k_adamw.hip", "k_slope.hip"]
+           "hwr_train.hip", "k_probs.hip", "k_adamw.hip", "k_slope.hip", "k_grad.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -191,11 +191,7 @@ uint64_t rows_bytes(hwr_ops *c, bool bf16, RowsKind kind, bool ks, const RowsArg
     const int parts = rows_plan(bf16, kind, ks, r, c->cus).parts;
     return parts > 1 ? static_cast<uint64_t>(parts) * r.g.n * r.m_pad * sizeof(float) : 0;
 }
-// With its partial sums (rows_bytes) at `partial`.
-hwr_status rows(hwr_ops *c, bool bf16, RowsKind kind, bool ks, RowsArgs r, char *partial) {
-    r.parts = rows_plan(bf16, kind, ks, r, c->cus).parts;
-    r.partial = reinterpret_cast<float *>(partial);
-    OPS_HIP(c, launch_rows(bf16, kind, ks, r, c->cus, c->stream));
+hwr_status join_rows(hwr_ops *c, bool bf16, RowsKind kind, const RowsArgs &r) {
     if (r.parts == 1) return HWR_OK;
     FewArgs f{};
     f.g = r.g;
@@ -208,6 +204,13 @@ hwr_status rows(hwr_ops *c, bool bf16, RowsKind kind, bool ks, RowsArgs r, char 
     f.end = r.end;
     OPS_HIP(c, launch_join(bf16, kind, f, c->stream));
     return HWR_OK;
+}
+// With its partial sums (rows_bytes) at `partial`.
+hwr_status rows(hwr_ops *c, bool bf16, RowsKind kind, bool ks, RowsArgs r, char *partial) {
+    r.parts = rows_plan(bf16, kind, ks, r, c->cus).parts;
+    r.partial = reinterpret_cast<float *>(partial);
+    OPS_HIP(c, launch_rows(bf16, kind, ks, r, c->cus, c->stream));
+    return join_rows(c, bf16, kind, r);
 }
 
 // out[g] = P^T Q, with its partial sums (weight_grad_bytes) at `partial`.
@@ -373,10 +376,14 @@ hwr_status product_grad(hwr_ops *c, const hwr_groups *g, const hwr_matmul_grad_a
     d.ldp = ldx;
     d.ldq = lddy;
     d.out = a->dw;
-    // (one after the other: they share the place of their partial sums)
-    const uint64_t sums = std::max({dx ? rows_bytes(c, bf16, RowsKind::kGrouped, false, r) : 0,
-                                    a->dw ? weight_grad_bytes(c, bf16, ColsKind::kDense, d) : 0,
-                                    dbias ? uint64_t{sizeof(float)} * slope_tiles(g->n, g->n_groups) * s.m_pad : 0});
+    // in one launch, or one after the other: then they share the place of their partial sums
+    const RowsPlan rp = rows_plan(bf16, RowsKind::kGrouped, false, r, c->cus);
+    const ColsPlan cp = cols_plan(bf16, ColsKind::kDense, d, c->cus);
+    const bool pair = dx && a->dw && grad_pair(rp, cp);
+    const uint64_t row_sums = dx ? rows_bytes(c, bf16, RowsKind::kGrouped, false, r) : 0,
+                   weight_sums = a->dw ? weight_grad_bytes(c, bf16, ColsKind::kDense, d) : 0;
+    const uint64_t sums = std::max(pair ? row_sums + weight_sums : std::max(row_sums, weight_sums),
+                                   dbias ? uint64_t{sizeof(float)} * slope_tiles(g->n, g->n_groups) * s.m_pad : 0);
     char *ws = nullptr;
     if (hwr_status st = workspace(c, used + sums, &ws)) return st;
     if (hwr_status st = pads.copy(c, ws)) return st;
@@ -386,6 +393,17 @@ hwr_status product_grad(hwr_ops *c, const hwr_groups *g, const hwr_matmul_grad_a
     r.x = d.q = dy;
     r.w = w;
     d.p = x;
+    if (pair) {
+        r.parts = rp.parts;
+        r.partial = reinterpret_cast<float *>(ws + used);
+        d.parts = cp.parts;
+        d.partial = reinterpret_cast<float *>(ws + used + row_sums);
+        d.zeros = c->zeros;
+        OPS_HIP(c, launch_grad(bf16, rp, r, d, c->stream));
+        if (hwr_status st = join_rows(c, bf16, RowsKind::kGrouped, r)) return st;
+        OPS_HIP(c, launch_cols_sum(bf16, d, c->stream));
+        return HWR_OK;
+    }
     if (dx)
         if (hwr_status st = rows(c, bf16, RowsKind::kGrouped, false, r, ws + used)) return st;
     if (a->dw)

@@ -228,6 +228,10 @@ ColsPlan cols_plan(bool bf16, ColsKind kind, const ColsArgs &a, int cus);
 hipError_t launch_cols(bool bf16, ColsKind kind, const ColsArgs &a, int cus, hipStream_t s);
 // kLowQ and kLowP of the same groups and rank in one launch; both plans direct
 hipError_t launch_cols_low_pair(bool bf16, const ColsArgs &q, const ColsArgs &p, hipStream_t s);
+hipError_t launch_cols_sum(bool bf16, const ColsArgs &a, hipStream_t s);   // of parts, where there are
+// dx (kGrouped, not ks) and dW (kDense) in one launch, before the sums of their parts
+bool grad_pair(const RowsPlan &p, const ColsPlan &q);
+hipError_t launch_grad(bool bf16, const RowsPlan &p, const RowsArgs &a, const ColsArgs &b, hipStream_t s);
 int probs_parts(bool bf16, int64_t n, int m, int cus);
 uint64_t probs_bytes(const ProbsArgs &a);     // of partial
 hipError_t launch_probs(bool bf16, const ProbsArgs &a, hipStream_t s);

@@ -146,10 +146,14 @@ class Pads {
     }
     // Makes the copies that were planned; the matrices' addresses become theirs.
     hwr_status copy(hwr_ops *c, char *ws) {
-        if (args_.count == 0) return HWR_OK;
-        for (int i = 0; i < args_.count; ++i) *slots_[i].src = args_.m[i].dst = ws + at_[i];
-        OPS_HIP(c, launch_pad(bf16_, args_, c->stream));
+        const PadArgs &a = place(ws);
+        if (a.count) OPS_HIP(c, launch_pad(bf16_, a, c->stream));
         return HWR_OK;
+    }
+    // The same for a launch that makes the copies besides.
+    const PadArgs &place(char *ws) {
+        for (int i = 0; i < args_.count; ++i) *slots_[i].src = args_.m[i].dst = ws + at_[i];
+        return args_;
     }
 
   private:
@@ -359,6 +363,7 @@ hwr_status product_grad(hwr_ops *c, const hwr_groups *g, const hwr_matmul_grad_a
     s.z = z;
     s.ldz = ldz;
     s.dbias = dbias;
+    s.places = slope_places(bf16, g->n, g->n_groups, a->m, c->cus);
     const uint64_t dz_at = used;
     if (sloped) {
         lddy = s.lddz = padded_width(bf16, a->m);
@@ -382,14 +387,16 @@ hwr_status product_grad(hwr_ops *c, const hwr_groups *g, const hwr_matmul_grad_a
     const bool pair = dx && a->dw && grad_pair(rp, cp);
     const uint64_t row_sums = dx ? rows_bytes(c, bf16, RowsKind::kGrouped, false, r) : 0,
                    weight_sums = a->dw ? weight_grad_bytes(c, bf16, ColsKind::kDense, d) : 0;
-    const uint64_t sums = std::max(pair ? row_sums + weight_sums : std::max(row_sums, weight_sums),
-                                   dbias ? uint64_t{sizeof(float)} * slope_tiles(g->n, g->n_groups) * s.m_pad : 0);
+    const uint64_t bias_sums = dbias ? uint64_t{sizeof(float)} * slope_tiles(g->n, g->n_groups, s.places) * s.m_pad : 0;
+    const uint64_t bias_at = pair ? (row_sums + weight_sums + 255) / 256 * 256 : 0;
+    const uint64_t sums = std::max({row_sums, weight_sums, pair ? row_sums + weight_sums : 0, bias_at + bias_sums});
     char *ws = nullptr;
     if (hwr_status st = workspace(c, used + sums, &ws)) return st;
-    if (hwr_status st = pads.copy(c, ws)) return st;
     if (sloped) dy = s.dz = ws + dz_at;
-    if (dbias) s.partial = reinterpret_cast<float *>(ws + used);
-    if (sloped || dbias) OPS_HIP(c, launch_slope(bf16, act, s, c->stream));
+    if (dbias) s.partial = reinterpret_cast<float *>(ws + used + bias_at);
+    if (sloped || dbias) OPS_HIP(c, launch_slope(bf16, act, s, pads.place(ws), c->stream));
+    else if (hwr_status st = pads.copy(c, ws)) return st;
+    if (dbias && !pair) OPS_HIP(c, launch_bias(bf16, s, c->stream));
     r.x = d.q = dy;
     r.w = w;
     d.p = x;
@@ -399,7 +406,7 @@ hwr_status product_grad(hwr_ops *c, const hwr_groups *g, const hwr_matmul_grad_a
         d.parts = cp.parts;
         d.partial = reinterpret_cast<float *>(ws + used + row_sums);
         d.zeros = c->zeros;
-        OPS_HIP(c, launch_grad(bf16, rp, r, d, c->stream));
+        OPS_HIP(c, launch_grad(bf16, rp, r, d, s, c->stream));
         if (hwr_status st = join_rows(c, bf16, RowsKind::kGrouped, r)) return st;
         OPS_HIP(c, launch_cols_sum(bf16, d, c->stream));
         return HWR_OK;

@@ -122,6 +122,7 @@ struct SlopeArgs {
     int64_t lddy, ldz;            // elements
     void *dz;                     // rows of whole, aligned chunks of 16 bytes, or null
     int64_t lddz;
+    int places;                   // of a workgroup (slope_places)
     float *partial;               // [slope_tiles][m_pad], with dbias
     void *dbias;                  // [G][m] or null
 };
@@ -216,8 +217,11 @@ int few_parts(int n, int G, int k, int m, bool bf16, bool adapter, int cus);
 hipError_t launch_few(bool bf16, RowsKind kind, const FewArgs &a, hipStream_t s);
 // y[row] = sum of the partial sums of its place (kGrouped, kLinear)
 hipError_t launch_join(bool bf16, RowsKind kind, const FewArgs &a, hipStream_t s);
-int slope_tiles(int n, int G);
-hipError_t launch_slope(bool bf16, int act, const SlopeArgs &a, hipStream_t s);
+int slope_tiles(int n, int G, int places);
+int slope_places(bool bf16, int n, int G, int m, int cus);
+// (and copies besides)
+hipError_t launch_slope(bool bf16, int act, const SlopeArgs &a, const PadArgs &pads, hipStream_t s);
+hipError_t launch_bias(bool bf16, const SlopeArgs &a, hipStream_t s);   // dbias of its partial sums
 enum class ColsKind { kDense, kLowP, kLowQ };
 // Tile, and parts of the places, for a weight gradient.
 struct ColsPlan {
@@ -231,7 +235,8 @@ hipError_t launch_cols_low_pair(bool bf16, const ColsArgs &q, const ColsArgs &p,
 hipError_t launch_cols_sum(bool bf16, const ColsArgs &a, hipStream_t s);   // of parts, where there are
 // dx (kGrouped, not ks) and dW (kDense) in one launch, before the sums of their parts
 bool grad_pair(const RowsPlan &p, const ColsPlan &q);
-hipError_t launch_grad(bool bf16, const RowsPlan &p, const RowsArgs &a, const ColsArgs &b, hipStream_t s);
+// and launch_bias, where bias.dbias is not null
+hipError_t launch_grad(bool bf16, const RowsPlan &p, const RowsArgs &a, const ColsArgs &b, const SlopeArgs &bias, hipStream_t s);
 int probs_parts(bool bf16, int64_t n, int m, int cus);
 uint64_t probs_bytes(const ProbsArgs &a);     // of partial
 hipError_t launch_probs(bool bf16, const ProbsArgs &a, hipStream_t s);

@@ -14,6 +14,7 @@
 // Bound by memory: 28 bytes a value with fp32 states, 10 to 18 with 8 bits.  A workgroup takes 8
 // blocks of a tensor, a thread 8 values, a half-wave a block.
 #include <cmath>
+#include <utility>
 
 #include "ops_device.hpp"
 
@@ -88,12 +89,12 @@ __device__ inline void from_e4m3(u32x2_a1 v, float scale, float (&f)[kPer]) {
     }
 }
 
-// 0 <= x <= 448 to e4m3, up or down by 16 bits of noise.  Below 2^-6, where steps no longer shrink with
-// the value, 2^-6 is added first: the code is then that of the sum, less that of 2^-6.
-__device__ inline uint32_t to_e4m3(float x, uint32_t noise) {
-    const bool small = x < 0x1p-6f;
-    const uint32_t bits = __float_as_uint(small ? x + 0x1p-6f : x) + (noise << 4);
-    return min((bits >> 20) - (small ? 968u : 960u), 126u);
+// Byte SEL of `into` becomes x (at most 448 in magnitude) in e4m3, up or down by the 16 bits of noise at the top of
+// `noise`: the instruction adds the noise's upper 20 bits to the bits of x below those that stay (below 2^-6, where
+// steps no longer shrink with the value, to the bits below that step), and cuts them.
+template <int SEL>
+__device__ inline uint32_t to_e4m3(float x, uint32_t noise, uint32_t into) {
+    return static_cast<uint32_t>(__builtin_amdgcn_cvt_sr_fp8_f32(x, static_cast<int>(noise), static_cast<int>(into), SEL));
 }
 // fp32 to the bits of a bf16, as fp32.  (One that would round past the largest stays below.)
 __device__ inline float to_bf16(float x, uint32_t noise) {
@@ -110,8 +111,14 @@ __device__ inline float block_scale(const float (&f)[kPer], float &factor) {
 #pragma unroll
     for (int d = 1; d < kBlockLanes; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
     const bool none = most < 0x1p-100f;
-    factor = none ? 0.0f : 448.0f / most;
+    // (a few last bits less: no product rounds past 448, and none has to be cut there)
+    factor = none ? 0.0f : 448.0f / most * (1.0f - 0x1p-22f);
     return none ? 0.0f : most * (1.0f / 448.0f);
+}
+
+template <class F, int... I>
+__device__ inline void each_of(F f, std::integer_sequence<int, I...>) {
+    (f(std::integral_constant<int, I>{}), ...);
 }
 
 template <class E, bool MASTER, bool STATES8>
@@ -147,8 +154,13 @@ __global__ void __launch_bounds__(kThreads) k_adamw(AdamwArgs a) {
     for (int i = 0; i < kPer; ++i) {
         m[i] = m[i] * c.beta1 + g[i] * c.beta1_rest;
         v[i] = v[i] * c.beta2 + g[i] * g[i] * c.beta2_rest;
-        root[i] = sqrtf(v[i]);
-        p[i] = p[i] * c.decay - m[i] / (root[i] * c.root_rate + c.eps) * c.rate;
+        if constexpr (STATES8) {               // (the hardware's root and reciprocal, 1 ulp each)
+            root[i] = __builtin_amdgcn_sqrtf(v[i]);
+            p[i] = p[i] * c.decay - m[i] * __builtin_amdgcn_rcpf(fmaf(root[i], c.root_rate, c.eps)) * c.rate;
+        } else {
+            root[i] = sqrtf(v[i]);
+            p[i] = p[i] * c.decay - m[i] / (root[i] * c.root_rate + c.eps) * c.rate;
+        }
     }
     uint32_t noise[kPer], more[kPer];
     if constexpr (STATES8 || (!MASTER && sizeof(E) == 2)) {
@@ -172,17 +184,14 @@ __global__ void __launch_bounds__(kThreads) k_adamw(AdamwArgs a) {
         float mf, vf;
         const float ms = block_scale(m, mf), vs = block_scale(root, vf);
         uint32_t mb[2] = {0, 0}, vb[2] = {0, 0};
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const float my = fminf(fabsf(m[i]) * mf, 448.0f), vy = fminf(root[i] * vf, 448.0f);
-            uint32_t mc = to_e4m3(my, noise[i] & 0xFFFFu) | (m[i] < 0.0f ? 0x80u : 0u);
-            uint32_t vc = to_e4m3(vy, noise[i] >> 16);
-            if (vy > 0.0f) vc = max(vc, 1u);
-            if (m[i] != m[i]) mc = 0x7Fu;        // NaN
-            if (root[i] != root[i]) vc = 0x7Fu;
-            mb[i / 4] |= mc << (i % 4 * 8);
-            vb[i / 4] |= vc << (i % 4 * 8);
-        }
+        auto encode = [&](auto at) {
+            constexpr int i = decltype(at)::value;
+            mb[i / 4] = to_e4m3<i % 4>(m[i] * mf, noise[i] << 16, mb[i / 4]);
+            // (a root is never rounded down to 0; NaNs stay)
+            const float y = root[i] * vf;
+            vb[i / 4] = to_e4m3<i % 4>(y > 0.0f && y < 0x1p-9f ? 0x1p-9f : y, noise[i] & 0xFFFF0000u, vb[i / 4]);
+        };
+        each_of(encode, std::make_integer_sequence<int, kPer>{});
         store8_bytes(static_cast<uint8_t *>(t.m) + at, e, len, mb);
         store8_bytes(static_cast<uint8_t *>(t.v) + at, e, len, vb);
         if (has_block && threadIdx.x % kBlockLanes == 0) {

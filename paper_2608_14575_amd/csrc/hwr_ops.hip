@@ -188,6 +188,7 @@ RowsArgs rows_args(hwr_ops *c, const hwr_groups *g, bool ks, bool padded, const 
     r.y = y;
     r.ldy = ldy;
     r.zeros = c->zeros;
+    r.units = c->cus;
     r.m_pad = (m + 3) / 4 * 4;
     return r;
 }

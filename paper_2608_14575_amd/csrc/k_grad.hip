@@ -17,9 +17,16 @@ __global__ void __launch_bounds__(WR *WC * 64) k_grad(RowsArgs a, ColsArgs b, Sl
     __shared__ __attribute__((aligned(16))) char buf0[kBuf], buf1[kBuf], buf2[kMore], buf3[kMore];
     __shared__ int rows[BM];
     const int id = block_id<WR * WC * 64>();
-    if (id < first) rows_direct<E, RowsKind::kGrouped, false, BM, BN, WR, WC>(a, id, buf0, buf1, buf2, buf3, rows);
-    else if (id < second) cols_direct<E, ColsKind::kDense, BP, BP, WP, WQ>(b, id - first, buf0, buf1, buf2, buf3);
-    else if (c.dbias && id - second < bias_blocks(c)) sum_bias<E, WR * WC * 64>(c, id - second, reinterpret_cast<f32x4 *>(buf0));
+    if (id < first) {
+        RowTile rt;
+        int c0, part;
+        if (row_tile<RowsKind::kGrouped, BM, BN>(a, id, threadIdx.x & 63, rt, c0, part))
+            rows_direct<E, RowsKind::kGrouped, false, BM, BN, WR, WC>(a, rt, c0, part, buf0, buf1, buf2, buf3, rows);
+    } else if (id < second) {
+        cols_direct<E, ColsKind::kDense, BP, BP, WP, WQ>(b, id - first, buf0, buf1, buf2, buf3);
+    } else if (c.dbias && id - second < bias_blocks(c)) {
+        sum_bias<E, WR * WC * 64>(c, id - second, reinterpret_cast<f32x4 *>(buf0));
+    }
 }
 
 template <class E, int BM, int BN, int WR, int WC, int BP, int WP, int WQ>

@@ -85,6 +85,10 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows(RowsArgs a) {
     store_rows<E, KIND, BM, BN, WR, WC>(a, rt, c0, part, rows, acc, tid);
 }
 
+// Tiles of 256 of groups run one to a compute unit, without parts: the last round is cut.
+template <RowsKind KIND, int BM>
+constexpr bool kCut = BM == 256 && KIND != RowsKind::kAdapter;
+
 template <class E, RowsKind KIND, bool KS, int BM, int BN, int WR, int WC>
 __global__ void __launch_bounds__(WR *WC * 64) k_rows_direct(RowsArgs a) {
     // an array each, so that the compiler sees that reads of one do not depend on the
@@ -92,12 +96,24 @@ __global__ void __launch_bounds__(WR *WC * 64) k_rows_direct(RowsArgs a) {
     constexpr int kBuf = kRowsBuf<BM, BN>, kMore = kRowsDeep<BN> ? kBuf : 16;
     __shared__ __attribute__((aligned(16))) char buf0[kBuf], buf1[kBuf], buf2[kMore], buf3[kMore];
     __shared__ int rows[BM];
-    rows_direct<E, KIND, KS, BM, BN, WR, WC>(a, block_id<WR * WC * 64>(), buf0, buf1, buf2, buf3, rows);
+    const int id = block_id<WR * WC * 64>(), lane = threadIdx.x & 63;
+    RowTile rt;
+    int c0, part = 0;
+    if constexpr (kCut<KIND, BM>) {
+        int quarter;
+        if (!cut_tile(a, id, lane, rt, c0, quarter)) return;
+        if (quarter < 0) rows_direct<E, KIND, KS, BM, BN, WR, WC>(a, rt, c0, 0, buf0, buf1, buf2, buf3, rows);
+        else rows_direct<E, KIND, KS, BM / 2, BN / 2, WR, WC>(a, rt, c0, 0, buf0, buf1, buf2, buf3, rows);
+    } else {
+        if (!row_tile<KIND, BM, BN>(a, id, lane, rt, c0, part)) return;
+        rows_direct<E, KIND, KS, BM, BN, WR, WC>(a, rt, c0, part, buf0, buf1, buf2, buf3, rows);
+    }
 }
 
 template <class E, RowsKind KIND, bool KS, int BM, int BN, int WR, int WC, bool DIRECT>
 hipError_t go(const RowsArgs &a, hipStream_t s) {
-    const int64_t blocks = rows_blocks<KIND, BM, BN>(a);
+    int64_t blocks = rows_blocks<KIND, BM, BN>(a);
+    if constexpr (DIRECT && kCut<KIND, BM>) blocks = cut_blocks<KIND>(a);
     if (blocks > INT32_MAX - grid_row(WR * WC * 64)) return hipErrorInvalidValue;
     const dim3 grid = wide_grid(blocks, WR * WC * 64), block(WR * WC * 64);
     if constexpr (DIRECT) return launch_kernel(k_rows_direct<E, KIND, KS, BM, BN, WR, WC>, grid, block, 0, s, a);

@@ -102,20 +102,54 @@ __device__ inline int xcd_item(int id, int items) {
     return at < share && i < items ? i : -1;
 }
 
-// Work item of a product by row: tile t of places, first column c0, part.  Tiles go in
-// panels of 8 row tiles, column by column, so that the workgroups that run together on
-// one L2 share rows and weights.  False past the last.
-__device__ inline bool row_item(int id, int tiles, int m, int mw, int bn, int parts, int &t, int &c0, int &part) {
-    const int ct = (m + bn - 1) / bn;
-    int item = xcd_item(id, tiles * ct * parts);
-    if (item < 0) return false;
-    part = item / (tiles * ct);
-    item -= part * (tiles * ct);
+// Tile of places t and first column c0 of an item.  Tiles go in panels of 8 row tiles, column by
+// column, so that the workgroups that run together on one L2 share rows and weights.
+__device__ inline void panel_item(int item, int tiles, int ct, int mw, int bn, int &t, int &c0) {
     const int panel = item / (8 * ct) * 8, in = item - panel * ct, rp = min(8, tiles - panel);
     t = panel + in % rp;
     // the last tile of columns ends with the row: it shares columns with the one before
     // (both give them the same bits), and no chunk is cut
     c0 = mw < bn ? 0 : min(in / rp * bn, mw - bn);
+}
+
+// Work item of a product by row: tile t of places, first column c0, part.  False past the last.
+__device__ inline bool row_item(int id, int tiles, int m, int mw, int bn, int parts, int &t, int &c0, int &part) {
+    const int ct = (m + bn - 1) / bn;
+    int item = xcd_item(id, tiles * ct * parts);
+    if (item < 0) return false;
+    part = item / (tiles * ct);
+    panel_item(item - part * (tiles * ct), tiles, ct, mw, bn, t, c0);
+    return true;
+}
+
+// The same where one workgroup runs on each of `units` compute units, and the last round of whole tiles would leave
+// three of four idle or more: its tiles are cut into quarters, which make one round (0: the first rows and columns, 1: the
+// first rows, the other columns, ...; -1: a whole tile).  us, cut / whole: 8,192 rows 2048 x 2048 in 8 groups 87 / 108, layers of
+// 12,288 rows 2048 x 4096 in 8 281 / 313; in two rounds of quarters, 16,384 rows 2048 x 4096 in 16 357 / 341.  Last, of rows in no group, come `tail` tiles, which have no products and would unbalance
+// the rounds: tiles [tiles, tiles + tail).  At most items + 3 units / 4 + 24 workgroups for as many items.
+__device__ inline bool cut_item(int id, int tiles, int tail, int m, int mw, int bn, int units, int &t, int &c0, int &quarter) {
+    const int ct = (m + bn - 1) / bn, all = tiles * ct, rest = all % units;
+    const int cut = rest * 4 <= units ? rest : 0, whole = all - cut;
+    quarter = -1;
+    const int whole8 = (whole + 7) / 8 * 8, cut8 = (4 * cut + 7) / 8 * 8;
+    int item;
+    if (id < whole8) {
+        item = xcd_item(id, whole);
+    } else if (id - whole8 < cut8) {
+        item = xcd_item(id - whole8, 4 * cut);
+        if (item >= 0) {
+            quarter = item & 3;
+            item = whole + (item >> 2);
+        }
+    } else {
+        item = xcd_item(id - whole8 - cut8, tail * ct);
+        if (item < 0) return false;
+        panel_item(item, tail, ct, mw, bn, t, c0);
+        t += tiles;
+        return true;
+    }
+    if (item < 0) return false;
+    panel_item(item, tiles, ct, mw, bn, t, c0);
     return true;
 }
 

@@ -61,6 +61,7 @@ struct RowsArgs {
     int64_t ldy;
     const void *zeros;            // 256 zero bytes
     int parts;                    // workgroups that share a tile's contraction (rows_plan)
+    int units;                    // compute units
     int m_pad;                    // m up to a multiple of 4
     float *partial;               // [parts][n][m_pad], with parts > 1
     // adapter

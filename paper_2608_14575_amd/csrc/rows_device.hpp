@@ -204,6 +204,21 @@ __device__ inline bool row_tile(const RowsArgs &a, int id, int lane, RowTile &rt
     return true;
 }
 
+// The same for whole tiles of 256 and quarters of them (cut_item).
+__device__ inline bool cut_tile(const RowsArgs &a, int id, int lane, RowTile &rt, int &c0, int &quarter) {
+    constexpr int BM = 256, BN = 256;
+    const int tiles = count_tiles(a.g, BM, false, lane);
+    const int tail = (a.g.n - place_of(a.g, a.g.G) + BM - 1) / BM;
+    int t;
+    if (!cut_item(id, tiles, tail, a.m, a.mw, BN, a.units, t, c0, quarter)) return false;
+    rt = find_tile(a.g, t, BM, true, lane);
+    if (quarter < 0) return true;
+    c0 += (quarter & 1) * (BN / 2);
+    rt.p0 += (quarter >> 1) * (BM / 2);
+    rt.p1 = min(rt.p1, rt.p0 + BM / 2);
+    return rt.p0 < rt.p1 && c0 < a.m;
+}
+
 // Stages of a part of the contraction.
 __device__ inline void my_stages(int stages, int part, int parts, int &first, int &last) {
     first = static_cast<int>(static_cast<int64_t>(stages) * part / parts);
@@ -213,14 +228,15 @@ __device__ inline void my_stages(int stages, int part, int parts, int &first, in
 // Whole chunks of 16 bytes everywhere (rows padded to them with zeros) and at least BN columns: operands go from
 // memory straight into LDS (run_stages).  A place without a row computes one that it
 // does not store; contraction elements past the last are zeros on both sides.
-// Workgroup `id` of them, its buffers of LDS (rows_buf bytes each; the last two where kRowsDeep) and places for BM row numbers.
+// Places rt and columns from c0 on, a part of the contraction; kRowsBuf bytes of LDS each (the last two where kRowsDeep) and
+// room for BM row numbers.
 template <int BM, int BN>
 constexpr int kRowsBuf = (BM + BN) * kStageBytes;
 template <int BN>
 constexpr bool kRowsDeep = BN == 64;       // run_stages_deep
 
 template <class E, RowsKind KIND, bool KS, int BM, int BN, int WR, int WC>
-__device__ __forceinline__ void rows_direct(const RowsArgs &a, int id, char *buf0, char *buf1, char *buf2, char *buf3, int *rows) {
+__device__ __forceinline__ void rows_direct(const RowsArgs &a, const RowTile &rt, int c0, int part, char *buf0, char *buf1, char *buf2, char *buf3, int *rows) {
     using El = Elem<E>;
     constexpr int NT = WR * WC * 64, RF = BM / WR / 16, CF = BN / WC / 16, kBk = El::kBk, kEpc = El::kEpc;
     using XT = Tile<E, false, BM>;
@@ -236,9 +252,6 @@ __device__ __forceinline__ void rows_direct(const RowsArgs &a, int id, char *buf
     constexpr bool kDeep = kRowsDeep<BN>;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wr = wave / WC, wc = wave % WC;
-    RowTile rt;
-    int c0, part;
-    if (!row_tile<KIND, BM, BN>(a, id, lane, rt, c0, part)) return;
     for (int i = tid; i < BM; i += NT) rows[i] = rt.p0 + i < rt.p1 ? row_at(a.g, rt.p0 + i) : -1;
     __syncthreads();
 
@@ -309,6 +322,9 @@ int64_t rows_blocks(const RowsArgs &a) {
     const int64_t tiles = KIND == RowsKind::kAdapter ? (n + BM - 1) / BM : n / BM + (n < a.g.G + 1 ? n : a.g.G + 1);
     return (tiles * ((a.m + BN - 1) / BN) * a.parts + 7) / 8 * 8;
 }
+// Of tiles of 256, cut (cut_item).
+template <RowsKind KIND>
+int64_t cut_blocks(const RowsArgs &a) { return rows_blocks<KIND, 256, 256>(a) + (3 * a.units / 4 + 24 + 7) / 8 * 8; }
 
 }  // namespace
 }  // namespace hwr

@@ -72,8 +72,10 @@ hwr_status init_impl(int32_t device, void *stream, hwr_ops **out) {
     c->dev = device;
     c->cus = prop.multiProcessorCount;
     c->stream = static_cast<hipStream_t>(stream);
-    e = hipMalloc(&c->zeros, kZeroBytes);
-    if (e == hipSuccess) e = hipMemset(c->zeros, 0, kZeroBytes);
+    const uint64_t bytes = kZeroBytes + kMaxShared * sizeof(int);
+    e = hipMalloc(&c->zeros, bytes);
+    if (e == hipSuccess) e = hipMemset(c->zeros, 0, bytes);
+    c->arrived = reinterpret_cast<int *>(static_cast<char *>(c->zeros) + kZeroBytes);
     if (e == hipSuccess) e = hipDeviceSynchronize();
     if (e != hipSuccess) {
         release(c);

@@ -65,6 +65,7 @@ hwr_status log_probs(hwr_ops *c, const hwr_log_probs_args *a) {
     char *ws = nullptr;
     if (hwr_status st = workspace(c, probs_bytes(p), &ws)) return st;
     p.partial = ws;
+    p.arrived = c->arrived;
     OPS_HIP(c, launch_probs(bf16, p, c->stream));
     return HWR_OK;
 }

@@ -246,12 +246,64 @@ __device__ inline void store_sums(const ProbsArgs &a, int64_t r, const Sums &v, 
     }
 }
 
-// Partial results of a row: [n][parts] sums, then [n][parts][top] keys.
-__device__ inline f32x4 *part_sums(const ProbsArgs &a, int64_t r, int part) {
-    return static_cast<f32x4 *>(a.partial) + r * a.parts + part;
-}
+// Partial results of a row: [n][parts] sums, then [n][parts][top] keys.  They are written and read past the caches that
+// compute units do not share.
+__device__ inline float *part_sums(const ProbsArgs &a, int64_t r, int part) { return static_cast<float *>(a.partial) + (r * a.parts + part) * 4; }
 __device__ inline uint64_t *part_top(const ProbsArgs &a, int64_t r, int part) {
-    return reinterpret_cast<uint64_t *>(static_cast<f32x4 *>(a.partial) + a.n * a.parts) + (r * a.parts + part) * a.top;
+    return reinterpret_cast<uint64_t *>(part_sums(a, a.n, 0)) + (r * a.parts + part) * a.top;
+}
+template <class V>
+__device__ inline void put_shared(V *at, V v) { __hip_atomic_store(at, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <class V>
+__device__ inline V get_shared(V *at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+constexpr int kMaxParts = 16;
+constexpr int kPartElements = 16384;
+static_assert(kPartElements >= kMaxTop && kMaxParts * kMaxTop <= kCandidates && kMaxParts <= 64);
+
+// Whether this workgroup is the last of the row's parts; what the others have put is then there to be got.  No one waits for
+// another: whoever comes last goes on, and leaves the count at zero.  What is shared goes through put_shared and get_shared
+// alone, past the L2s (an XCD's each), so that it is enough that a part's stores are done (vmcnt, every wave before the barrier)
+// before it is counted.  (Fences of the whole device, which write back an L2 in every wave: 48 x 128,000 with
+// twenty tokens 58 us; a second launch instead 14.6.)
+__device__ inline bool last_part(const ProbsArgs &a, int64_t r, TeamSpace &ts, int tid) {
+    wait_vm<0>();
+    __syncthreads();
+    if (tid == 0) {
+        ts.count = __hip_atomic_fetch_add(a.arrived + r, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (ts.count == a.parts - 1) put_shared(a.arrived + r, 0);
+    }
+    __syncthreads();
+    return ts.count == a.parts - 1;
+}
+
+// A row's results from those of its parts.
+template <class E, int T, bool TOP>
+__device__ inline void join_parts(const ProbsArgs &a, int64_t r, TeamSpace &ts, int tid, float c2) {
+    Sums v;
+    const int lane = tid & 63;
+    if (lane < a.parts) {
+        float *o = part_sums(a, r, lane);
+        v.m = get_shared(o), v.s = get_shared(o + 1), v.t = get_shared(o + 2);
+    }
+    const int count = a.parts * a.top;
+    if constexpr (TOP) {
+        uint64_t *top = part_top(a, r, 0);
+        for (int i = tid; i < count; i += T) ts.candidate[i] = get_shared(top + i);
+    }
+    v.join_lanes(c2);
+    const float log_s = logf(v.s);
+    if (tid == 0) store_sums<E>(a, r, v, log_s);
+    if constexpr (TOP) {
+        __syncthreads();
+        for (int i = tid; i < count; i += T) {
+            const uint64_t mine = ts.candidate[i];
+            const int before = larger(ts.candidate, count, mine);
+            if (before >= a.top) continue;
+            if (a.top_logp) a.top_logp[r * a.top + before] = log_prob(a, v, log_s, key_value(static_cast<uint32_t>(mine >> 32)));
+            if (a.top_token) a.top_token[r * a.top + before] = static_cast<int>(~static_cast<uint32_t>(mine));
+        }
+    }
 }
 
 // T threads to a row, or to a part of it; 256 / T rows to a workgroup where T is less.
@@ -309,56 +361,26 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T, T == 64 ? 8 : 1) k_probs(Pr
         if (lane < T / 64) v.m = ts.m[lane], v.s = ts.s[lane], v.t = ts.t[lane];
         v.join_lanes(c2);
     }
-    const float log_s = logf(v.s);
-    if (a.parts > 1) {
-        if (tid == 0) *part_sums(a, r, part) = f32x4{v.m, v.s, v.t, 0.0f};
+    if (T == 1024 && a.parts > 1) {
+        if (tid == 0) {
+            float *o = part_sums(a, r, part);
+            put_shared(o, v.m), put_shared(o + 1, v.s), put_shared(o + 2, v.t);
+        }
         if constexpr (TOP) {
             uint64_t *out = part_top(a, r, part);    // (a part has more elements than kMaxTop)
             select_top<E, T, kKept>(row, in, first, a.top, mine, ts, tid,
-                             [&](int rank, uint32_t key, int token) { out[rank] = rank_key(key, token); });
+                                    [&](int rank, uint32_t key, int token) { put_shared(out + rank, rank_key(key, token)); });
         }
+        if (last_part(a, r, ts, tid)) join_parts<E, T, TOP>(a, r, ts, tid, c2);
         return;
     }
+    const float log_s = logf(v.s);
     if (tid == 0) store_sums<E>(a, r, v, log_s);
     if constexpr (TOP)
         select_top<E, T, kKept>(row, in, 0, a.top, mine, ts, tid, [&](int rank, uint32_t key, int token) {
             if (a.top_logp) a.top_logp[r * a.top + rank] = log_prob(a, v, log_s, key_value(key));
             if (a.top_token) a.top_token[r * a.top + rank] = token;
         });
-}
-
-// A row's results from those of its parts.
-constexpr int kMaxParts = 16;
-constexpr int kPartElements = 16384;
-static_assert(kPartElements >= kMaxTop);
-constexpr int kJoinThreads = 256;
-template <class E>
-__global__ void __launch_bounds__(kJoinThreads) k_probs_join(ProbsArgs a) {
-    __shared__ uint64_t key[kMaxParts * kMaxTop];
-    const int64_t r = block_id<kJoinThreads>();
-    const int tid = threadIdx.x;
-    if (r >= a.n) return;
-    const float c2 = a.scale * kLog2e;
-    Sums v;
-    if ((tid & 63) < a.parts) {
-        const f32x4 o = *part_sums(a, r, tid & 63);
-        v.m = o[0], v.s = o[1], v.t = o[2];
-    }
-    v.join_lanes(c2);
-    const float log_s = logf(v.s);
-    if (tid == 0) store_sums<E>(a, r, v, log_s);
-    if (!a.top) return;
-    const int count = a.parts * a.top;
-    const uint64_t *top = part_top(a, r, 0);
-    for (int i = tid; i < count; i += kJoinThreads) key[i] = top[i];
-    __syncthreads();
-    for (int i = tid; i < count; i += kJoinThreads) {
-        const uint64_t mine = key[i];
-        const int before = larger(key, count, mine);
-        if (before >= a.top) continue;
-        if (a.top_logp) a.top_logp[r * a.top + before] = log_prob(a, v, log_s, key_value(static_cast<uint32_t>(mine >> 32)));
-        if (a.top_token) a.top_token[r * a.top + before] = static_cast<int>(~static_cast<uint32_t>(mine));
-    }
 }
 
 // dx = scale (dlogp (1[c = t] - p) - dentropy p (ln p + H)), ln p = scale x - lse.  A row without
@@ -421,10 +443,8 @@ hipError_t go(const ProbsArgs &a, hipStream_t s) {
     constexpr int NT = T < 256 ? 256 : T, kRows = NT / T;
     const int64_t blocks = kRows > 1 ? (a.n + kRows - 1) / kRows : a.n * a.parts;
     if (blocks > INT32_MAX - grid_row(NT)) return hipErrorInvalidValue;
-    hipError_t e = a.top ? launch_kernel(k_probs<E, T, true>, wide_grid(blocks, NT), dim3(NT), 0, s, a)
-                         : launch_kernel(k_probs<E, T, false>, wide_grid(blocks, NT), dim3(NT), 0, s, a);
-    if (e != hipSuccess || a.parts == 1) return e;
-    return launch_kernel(k_probs_join<E>, wide_grid(a.n, kJoinThreads), dim3(kJoinThreads), 0, s, a);
+    return a.top ? launch_kernel(k_probs<E, T, true>, wide_grid(blocks, NT), dim3(NT), 0, s, a)
+                 : launch_kernel(k_probs<E, T, false>, wide_grid(blocks, NT), dim3(NT), 0, s, a);
 }
 // Rows up to kWaveElements have a wave each; longer ones 256 threads, or 1024 where workgroups are
 // few and long.
@@ -432,6 +452,7 @@ constexpr int kWaveElements = 2048, kFewTeams = 512, kTeamElements = 8192;
 template <class E>
 hipError_t pick(const ProbsArgs &a, hipStream_t s) {
     if (a.m <= kWaveElements) return go<E, 64>(a, s);
+    if (a.parts > 1) return go<E, 1024>(a, s);
     if (a.n * a.parts <= kFewTeams && a.m / a.parts >= kTeamElements) return go<E, 1024>(a, s);
     return go<E, 256>(a, s);
 }
@@ -459,7 +480,7 @@ int probs_parts(bool bf16, int64_t n, int m, int cus) {
     return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({want, m / kPartElements, kMaxParts})));
 }
 uint64_t probs_bytes(const ProbsArgs &a) {
-    return a.parts > 1 ? static_cast<uint64_t>(a.n) * a.parts * (sizeof(f32x4) + a.top * sizeof(uint64_t)) : 0;
+    return a.parts > 1 ? static_cast<uint64_t>(a.n) * a.parts * (4 * sizeof(float) + a.top * sizeof(uint64_t)) : 0;
 }
 hipError_t launch_probs(bool bf16, const ProbsArgs &a, hipStream_t s) { return bf16 ? pick<__bf16>(a, s) : pick<float>(a, s); }
 hipError_t launch_probs_grad(bool bf16, const ProbsGradArgs &a, hipStream_t s) {

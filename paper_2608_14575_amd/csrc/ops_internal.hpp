@@ -138,6 +138,7 @@ struct GroupRowsArgs {
 
 // Log probabilities, entropies and the most likely tokens of rows of logits, and the logits' gradient.
 constexpr int kMaxTop = 32;
+constexpr int kMaxShared = 1024;  // rows that are shared, at most half as many as compute units
 struct ProbsArgs {
     int64_t n;
     int m, top;
@@ -149,6 +150,7 @@ struct ProbsArgs {
     int32_t *top_token;
     int parts;                    // workgroups that share a row (probs_parts)
     void *partial;                // with parts > 1: probs_bytes
+    int *arrived;                 // [kMaxShared] zeros, and zeros again
 };
 struct ProbsGradArgs {
     int64_t n;

@@ -108,7 +108,7 @@ struct ColsTiles {
 template <class E, ColsKind KIND, int BP, int BQ>
 constexpr int kColsBuf = ColsTiles<E, KIND, BP, BQ>::PT::kBytes + ColsTiles<E, KIND, BP, BQ>::QT::kBytes;
 
-template <class E, ColsKind KIND, int BP, int BQ, int WP, int WQ>
+template <class E, ColsKind KIND, int BP, int BQ, int WP, int WQ, bool DEEP = BP == 64 && BQ == 64>
 __device__ inline void cols_direct(const ColsArgs &a, int block, char *buf0, char *buf1, char *buf2, char *buf3) {
     using El = Elem<E>;
     using TT = ColsTiles<E, KIND, BP, BQ>;
@@ -118,7 +118,6 @@ __device__ inline void cols_direct(const ColsArgs &a, int block, char *buf0, cha
     constexpr int NT = WP * WQ * 64, PF = BP / WP / 16, QF = BQ / WQ / 16, kBk = El::kBk, kEpc = El::kEpc;
     constexpr int UP = PT::kChunks / NT, UQ = QT::kChunks / NT;
     static_assert(PT::kChunks % NT == 0 && QT::kChunks % NT == 0);
-    constexpr bool kDeep = BP == 64 && BQ == 64;     // run_stages_deep
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wp = wave / WQ, wq = wave % WQ;
     ColsTile t;
@@ -142,7 +141,7 @@ __device__ inline void cols_direct(const ColsArgs &a, int block, char *buf0, cha
     // a check here would wait for the loads in flight).  Tiles of one width share them.
     // Looked up one stage before they are loaded, or four (run_stages_deep), in turn.
     constexpr bool kShared = KIND == ColsKind::kDense && BP == BQ;
-    constexpr int kSlots = kDeep ? 4 : 1, kLead = kDeep ? 4 : 1;
+    constexpr int kSlots = DEEP ? 4 : 1, kLead = DEEP ? 4 : 1;
     int pr[kSlots][UP], qr[kSlots][kShared ? 1 : UQ];
     auto look_up = [&](int stage, int slot) {
         const int p = t.p0 + stage * kBk;
@@ -162,7 +161,7 @@ __device__ inline void cols_direct(const ColsArgs &a, int block, char *buf0, cha
     const char *ps = static_cast<const char *>(a.p), *qs = static_cast<const char *>(a.q);
     auto in_range = [&](int row) { return min(static_cast<unsigned>(row), static_cast<unsigned>(a.g.n - 1)); };
     auto issue = [&](char *b, int stage, auto... in_turn) {
-        constexpr int slot = kDeep ? (decltype(in_turn)::value + ... + 0) : 0;
+        constexpr int slot = DEEP ? (decltype(in_turn)::value + ... + 0) : 0;
         const int p = t.p0 + stage * kBk;
         auto p_row = [&](int i) -> int64_t { return TT::kLowP ? p + i * kLinesP + tid / PT::kCpl : in_range(pr[slot][i]); };
         auto q_row = [&](int i) -> int64_t {
@@ -191,7 +190,7 @@ __device__ inline void cols_direct(const ColsArgs &a, int block, char *buf0, cha
         const int stages = (t.p1 - t.p0 + kBk - 1) / kBk, p_at = wp * PF * 16, q_at = wq * QF * 16;
 #pragma unroll
         for (int i = 0; i < kLead; ++i) look_up(i, i);
-        if constexpr (kDeep) run_stages_deep<E, PT, QT, PF, QF, UP + UQ>(stages, issue, buf0, buf1, buf2, buf3, p_at, q_at, lane, acc);
+        if constexpr (DEEP) run_stages_deep<E, PT, QT, PF, QF, UP + UQ>(stages, issue, buf0, buf1, buf2, buf3, p_at, q_at, lane, acc);
         else run_stages<E, PT, QT, PF, QF>(stages, issue, buf0, buf1, p_at, q_at, lane, acc);
     }
     if constexpr (KIND == ColsKind::kDense) {

@@ -8,22 +8,23 @@ namespace hwr {
 namespace {
 
 // Workgroups [0, first) make tiles of dx, those to `second` tiles of dW, the largest groups' first: tiles of dx take the longest
-// but for those, and short ones fill the end.  The others add up the bias gradient's partial sums.
+// but for those, and short ones fill the end.  The others add up the bias gradient's partial sums.  Two stage buffers, tiles of 64
+// too: there are many workgroups, and more of them on a compute unit hide more than more stages of each (us, two / four: fp32
+// 2,051 rows 771 x 390 53 / 61, 4,096 x 1024 x 1024 173 / 188; bf16 2,000 x 512 x 512 9.2 / 13.7, 700 x 256 x 512 9.5 / 8.8).
 template <class E, int BM, int BN, int WR, int WC, int BP, int WP, int WQ>
 __global__ void __launch_bounds__(WR *WC * 64) k_grad(RowsArgs a, ColsArgs b, SlopeArgs c, int first, int second) {
     static_assert(WR * WC == WP * WQ);
     constexpr int kCols = kColsBuf<E, ColsKind::kDense, BP, BP>, kBuf = std::max(kRowsBuf<BM, BN>, kCols);
-    constexpr int kMore = std::max(kRowsDeep<BN> ? kRowsBuf<BM, BN> : 16, BP == 64 ? kCols : 16);
-    __shared__ __attribute__((aligned(16))) char buf0[kBuf], buf1[kBuf], buf2[kMore], buf3[kMore];
+    __shared__ __attribute__((aligned(16))) char buf0[kBuf], buf1[kBuf];
     __shared__ int rows[BM];
     const int id = block_id<WR * WC * 64>();
     if (id < first) {
         RowTile rt;
         int c0, part;
         if (row_tile<RowsKind::kGrouped, BM, BN>(a, id, threadIdx.x & 63, rt, c0, part))
-            rows_direct<E, RowsKind::kGrouped, false, BM, BN, WR, WC>(a, rt, c0, part, buf0, buf1, buf2, buf3, rows);
+            rows_direct<E, RowsKind::kGrouped, false, BM, BN, WR, WC, false>(a, rt, c0, part, buf0, buf1, nullptr, nullptr, rows);
     } else if (id < second) {
-        cols_direct<E, ColsKind::kDense, BP, BP, WP, WQ>(b, id - first, buf0, buf1, buf2, buf3);
+        cols_direct<E, ColsKind::kDense, BP, BP, WP, WQ, false>(b, id - first, buf0, buf1, nullptr, nullptr);
     } else if (c.dbias && id - second < bias_blocks(c)) {
         sum_bias<E, WR * WC * 64>(c, id - second, reinterpret_cast<f32x4 *>(buf0));
     }

@@ -235,7 +235,7 @@ constexpr int kRowsBuf = (BM + BN) * kStageBytes;
 template <int BN>
 constexpr bool kRowsDeep = BN == 64;       // run_stages_deep
 
-template <class E, RowsKind KIND, bool KS, int BM, int BN, int WR, int WC>
+template <class E, RowsKind KIND, bool KS, int BM, int BN, int WR, int WC, bool DEEP = kRowsDeep<BN>>
 __device__ __forceinline__ void rows_direct(const RowsArgs &a, const RowTile &rt, int c0, int part, char *buf0, char *buf1, char *buf2, char *buf3, int *rows) {
     using El = Elem<E>;
     constexpr int NT = WR * WC * 64, RF = BM / WR / 16, CF = BN / WC / 16, kBk = El::kBk, kEpc = El::kEpc;
@@ -249,7 +249,6 @@ __device__ __forceinline__ void rows_direct(const RowsArgs &a, const RowTile &rt
     static_assert(kLinesX % 16 == 0);
     constexpr bool kOneOrder = kLinesW % 16 == 0;
     static_assert(kRowsBuf<BM, BN> == XT::kBytes + WT::kBytes);
-    constexpr bool kDeep = kRowsDeep<BN>;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wr = wave / WC, wc = wave % WC;
     for (int i = tid; i < BM; i += NT) rows[i] = rt.p0 + i < rt.p1 ? row_at(a.g, rt.p0 + i) : -1;
@@ -301,7 +300,7 @@ __device__ __forceinline__ void rows_direct(const RowsArgs &a, const RowTile &rt
     };
     f32x4 acc[RF][CF] = {};
     const int stages = last - first, x0 = wr * RF * 16, w0 = wc * CF * 16;
-    if constexpr (kDeep) {
+    if constexpr (DEEP) {
         if (stages > 0) run_stages_deep<E, XT, WT, RF, CF, UX + UW>(stages, issue, buf0, buf1, buf2, buf3, x0, w0, lane, acc);
     } else {
         if (stages > 0) run_stages<E, XT, WT, RF, CF>(stages, issue, buf0, buf1, x0, w0, lane, acc);

@@ -416,10 +416,9 @@ class AdamW:
             self.steps = number
 
 
-def example(steps: int = 5, n: int = 4096, seed: int = 7) -> list:
-    """Routes n queries, groups them by the chosen pair's model, and trains, on
-    the grouped rows, one low-rank adapter per model beside a shared projection
-    and one output head per model towards random targets; returns the losses."""
+def _routed(n, seed):
+    """Routes n queries and groups them by the chosen pair's model: the operators, the number of models, the
+    queries' embeddings as rows, their groups, and what to close at the end."""
     import numpy as np
     import torch
     from . import synth
@@ -442,16 +441,26 @@ def example(steps: int = 5, n: int = 4096, seed: int = 7) -> list:
     offsets = torch.empty(G + 1, dtype=torch.int32, device=dev)
     order = torch.empty(n, dtype=torch.int32, device=dev)
     ops.group(choice, G, table=torch.from_numpy(pb.dep_model).to(dev, torch.int32), offsets=offsets, order=order)
+    return ops, G, emb.view(torch.bfloat16).mul(sp.embed_dim ** 0.5), offsets, order, router
+
+
+def example(steps: int = 5, n: int = 4096, seed: int = 7) -> list:
+    """Routes n queries, groups them by the chosen pair's model, and trains, on
+    the grouped rows, one low-rank adapter per model beside a shared projection
+    and one output head per model towards random targets; returns the losses."""
+    import torch
+
+    ops, G, x, offsets, order, router = _routed(n, seed)
+    dev = x.device
 
     # h = x W + s (x A_g) B_g, out = h H_g; loss = |out - target|^2 / 2 per row
     g = torch.Generator(dev).manual_seed(seed)
     bf = torch.bfloat16
-    k, m, R, o = sp.embed_dim, 1024, 16, 128
+    k, m, R, o = x.shape[1], 1024, 16, 128
 
     def weights(*shape, std):
         return (torch.randn(shape, generator=g, device=dev) * std).to(bf)
 
-    x = emb.view(bf).mul(k ** 0.5)
     w = weights(k, m, std=k ** -0.5)
     p = {"a": weights(G, k, R, std=k ** -0.5), "b": torch.zeros(G, R, m, dtype=bf, device=dev),
          "head": weights(G, m, o, std=m ** -0.5)}
@@ -479,6 +488,72 @@ def example(steps: int = 5, n: int = 4096, seed: int = 7) -> list:
     return losses
 
 
+def train_tokens(steps: int = 5, n: int = 4096, tokens: int = 4096, seed: int = 7):
+    """Routes n queries and trains the models that they went to, on one token each: an adapter beside a shared projection,
+    a layer with bias and SiLU, and a head with the log probabilities of given tokens; bf16 weights alone, AdamW
+    with states in 8 bits.  The step is captured into a graph and replayed.  Returns the loss before every step, the
+    weights and their last gradients."""
+    import torch
+
+    ops, G, x, offsets, order, router = _routed(n, seed)
+    ops.close()
+    dev, bf, stream = x.device, torch.bfloat16, torch.cuda.Stream()
+    ops = RoutedOps(stream=stream.cuda_stream)
+    stream.wait_stream(torch.cuda.current_stream())
+    g = torch.Generator(dev).manual_seed(seed)
+    k, m, h, R = x.shape[1], 1024, 512, 16
+
+    def weights(*shape, std):
+        return (torch.randn(shape, generator=g, device=dev) * std).to(bf)
+
+    w, scale = weights(k, m, std=k ** -0.5), torch.full((G,), 2.0, device=dev)
+    p = {"a": weights(G, k, R, std=k ** -0.5), "b": weights(G, R, m, std=1e-2), "layer": weights(G, m, h, std=m ** -0.5),
+         "layer_bias": weights(G, h, std=0.1), "head": weights(G, h, tokens, std=h ** -0.5), "head_bias": weights(G, tokens, std=0.1)}
+    grad = {name: torch.empty_like(v) for name, v in p.items()}
+    token = torch.randint(0, tokens, (n,), generator=g, device=dev, dtype=torch.int32)
+
+    def rows(width, dtype=bf):
+        return torch.empty((n, width), dtype=dtype, device=dev)
+
+    y, z, hidden, logits = rows(m), rows(h), rows(h), rows(tokens)
+    dy, dhidden = rows(m), rows(h)
+    logp, lse = torch.empty(n, device=dev), torch.empty(n, device=dev)
+    dlogp = torch.full((n,), -1.0 / n, device=dev)               # loss: minus the mean log probability
+    opt = AdamW(ops, list(p.values()), list(grad.values()), lr=1e-2, weight_decay=0.0, bits=8, seed=seed,
+                steps=torch.zeros(1, dtype=torch.int64, device=dev))
+
+    def step():
+        ops.adapter(x, w, p["a"], p["b"], scale, offsets, order, y=y)
+        ops.linear(y, p["layer"], offsets, order, bias=p["layer_bias"], act="silu", y=hidden, z=z)
+        ops.linear(hidden, p["head"], offsets, order, bias=p["head_bias"], y=logits)
+        ops.log_probs(logits, token, logp=logp, lse=lse)
+        ops.log_probs_grad(logits, token, lse, dlogp, dlogits=logits)
+        ops.linear_grad(logits, hidden, p["head"], offsets, order, dx=dhidden, dw=grad["head"], dbias=grad["head_bias"])
+        ops.linear_grad(dhidden, y, p["layer"], offsets, order, act="silu", z=z, dx=dy, dw=grad["layer"], dbias=grad["layer_bias"])
+        ops.adapter_grad(dy, x, w, p["a"], p["b"], scale, offsets, order, da=grad["a"], db=grad["b"])
+        opt.step()
+
+    losses, graph = [], None
+    for _ in range(steps):
+        if graph:
+            graph.replay()
+        else:
+            step()                                               # (the first makes the work space)
+        torch.cuda.synchronize()
+        losses.append(-float(logp.mean()))
+        if graph is None:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream):
+                step()
+    del graph
+    opt.close()
+    ops.close()
+    router.close()
+    return losses, p, grad
+
+
 if __name__ == "__main__":
     for i, loss in enumerate(example()):
         print(f"step {i}: loss {loss:.4f}", flush=True)
+    for i, loss in enumerate(train_tokens()[0]):
+        print(f"tokens, step {i}: loss {loss:.4f}", flush=True)

@@ -421,6 +421,19 @@ def test_a_training_step(ops):
     mine.close()
 
 
+def test_example_of_tokens():
+    """Runs, eager and replayed; gradients and weights are finite, and the weights move."""
+    losses, p, grad = routed.train_tokens(steps=3, n=1500, tokens=1001)
+    assert len(losses) == 3 and np.isfinite(losses).all()
+    again, q, _ = routed.train_tokens(steps=3, n=1500, tokens=1001)
+    assert again == losses and all(torch.equal(p[k], q[k]) for k in p)
+    first, before, g1 = routed.train_tokens(steps=1, n=1500, tokens=1001)
+    assert first[0] == losses[0]
+    for k in p:
+        assert grad[k].isfinite().all() and p[k].isfinite().all() and not torch.equal(p[k], before[k]), k
+        assert float(g1[k].abs().max()) > 0, k
+
+
 def test_refusals(ops):
     e = lambda *s, dtype=torch.bfloat16: torch.zeros(s, dtype=dtype, device="cuda")  # noqa: E731
     off, order = torch.zeros(3, dtype=torch.int32, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")

@@ -242,11 +242,12 @@ hwr_status hwr_log_probs_grad(hwr_ops *ops, const hwr_log_probs_grad_args *a);
  * becomes zeros.
  * The random numbers are a function of seed, t and the value's number (tensors are numbered
  * one after the other, each from a multiple of 256 on): the same call gives the same bits.
- * A NaN or infinity in g stays in its value, with states of 8 bits in its block of 256.
+ * A NaN or infinity in g stays in its value, with states of 8 bits in its block of 256.  (With eps 0 a value whose
+ * moments are 0 becomes NaN: 0 / 0.)
  *
  * hwr_adamw_init keeps what it needs of the tensors' addresses and sizes (not their contents) in
  * device memory; their memory has to stay until hwr_adamw_free.  Nothing that is written may overlap
- * anything else.  It copies from the host and waits: not under capture.  hwr_adamw_free waits for the
+ * anything else.  Steps of one hwr_adamw have to be ordered among each other.  Init copies from the host and waits: not under capture.  hwr_adamw_free waits for the
  * device; the context may be freed before. */
 typedef struct hwr_adamw hwr_adamw;   /* opaque, owned by the library */
 

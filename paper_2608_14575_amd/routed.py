@@ -317,7 +317,10 @@ class AdamW:
     ``steps``, the number of steps done, is counted up by ``step``: an int, or a device tensor of one int64, which
     a captured ``step`` needs.  ``lr`` may be a device tensor of one float32 then.  Both,
     ``betas``, ``eps`` and ``weight_decay`` may be changed between steps (a captured step keeps what
-    it was captured with, but for the contents of the tensors)."""
+    it was captured with, but for the contents of the tensors).
+
+    As with the operators, torch does not see the writes (no new version of a tensor).  Steps of one object are
+    ordered among each other by the caller, on whatever streams they run."""
 
     def __init__(self, ops, params, grads, *, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, bits=32, master=False,
                  state=None, steps=0, seed=0):
@@ -403,11 +406,11 @@ class AdamW:
             _bad("AdamW", "closed")
         ops, steps, lr, (b1, b2) = self.ops, self.steps, self.lr, self.betas
         number, counter, rate = 0, 0, 0
-        if isinstance(steps, int):
-            number = steps + 1
+        if not hasattr(steps, "data_ptr"):
+            number = int(steps) + 1
         else:
             counter = ops._dense("steps", steps.view(1) if steps.dim() == 0 else steps, self._i64, (1,))
-        if not isinstance(lr, (int, float)):
+        if hasattr(lr, "data_ptr"):
             rate, lr = ops._dense("lr", lr.view(1) if lr.dim() == 0 else lr, ops._f32, (1,)), 0.0
         st = self._args(ops.ctx, lr, b1, b2, self.eps, self.weight_decay, self.seed & 0xFFFFFFFFFFFFFFFF, number, counter, rate)
         if st:

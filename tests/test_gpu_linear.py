@@ -115,6 +115,11 @@ CASES = [s + (ACTS[i % 4], bool(i & 1), bool(i & 2), bool(i % 3)) for i, s in en
     (300, 3, 128, 128, "none", False, 0, "gelu", True, True, True),
     (5000, 4, 64, 2, "skew", False, 0, "gelu", True, True, True),
     (70, 2, 2048, 3, "skew", False, 0, "silu", True, True, True),
+    # bf16 tiles of 256 whose last round is cut into quarters (34 to 35 row tiles), and one of quarters alone
+    (10240, 2, 264, 2056, "skew", False, 8, "gelu", True, True, True),
+    (10240, 2, 520, 2041, "skew", False, 0, "silu", True, True, True),
+    (8250, 1, 136, 2048, "even", True, 0, "none", False, False, True),
+    (12288, 1, 128, 1032, "one", False, 0, "relu", True, False, False),
 ]
 
 
@@ -151,7 +156,7 @@ def test_layer_and_gradients(ops, n, G, k, m, kind, ordered, pad, act, biased, a
 def test_a_bare_layer_is_the_product(ops, dtype):
     t = TYPES[dtype][0]
     gen = torch.Generator("cuda").manual_seed(1)
-    for n, G, k, m in ((30, 4, 512, 392), (3000, 4, 264, 392), (4000, 3, 1001, 1003)):
+    for n, G, k, m in ((30, 4, 512, 392), (3000, 4, 264, 392), (4000, 3, 1001, 1003), (10240, 2, 264, 2056)):
         gid, off, order = grouped(sizes_of("skew", n, G, np.random.default_rng(n)), G)
         x, dy, w = rand(gen, n, k, dtype=t), rand(gen, n, m, dtype=t), rand(gen, G, k, m, dtype=t)
         a, b, z = (torch.empty(n, m, dtype=t, device="cuda") for _ in range(3))

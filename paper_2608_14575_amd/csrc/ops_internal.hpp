@@ -175,9 +175,7 @@ struct AdamwTensor {
     void *m, *v;
     float *m_scale, *v_scale;
     int64_t count, place;         // values, and the number of the first among the step's
-};
-struct AdamwChunk {
-    int tensor, at;               // chunk of the tensor
+    int64_t first;                // number of its first chunk
 };
 struct AdamwCoef {
     float decay, beta1, beta1_rest, beta2, beta2_rest, root_rate, rate, eps;
@@ -192,7 +190,7 @@ struct AdamwRates {
 };
 struct AdamwArgs {
     const AdamwTensor *tensors;
-    const AdamwChunk *chunks;
+    const int *chunks;            // [n_chunks] the tensor of each chunk
     int n_chunks;
     AdamwCoef coef;
     const AdamwCoef *coef_device; // in place of coef, or null

@@ -351,12 +351,16 @@ class AdamW:
         for k, v in state.items():
             if len(v) != len(params):
                 _bad(k, f"{len(v)} tensors for {len(params)} weights")
+        values, address = [], self._address
+        lists = [(k, state[k], kinds[k], k.endswith("scale")) if k in kinds else None
+                 for k in ("master", "m", "v", "m_scale", "v_scale")]
+        for i, (p, g) in enumerate(zip(params, grads)):
+            n = p.numel()
+            values += (n, address(ops, "params", i, p, dt, n), address(ops, "grads", i, g, dt, n))
+            for q in lists:
+                values.append(0 if q is None else address(ops, q[0], i, q[1][i], q[2], (n + 255) // 256 if q[3] else n))
         table = (hwr.hwr_adamw_tensor * len(params))()
-        for i, (t, p, g) in enumerate(zip(table, params, grads)):
-            n = t.count = p.numel()
-            t.p, t.g = self._address(ops, f"params[{i}]", p, dt, n), self._address(ops, f"grads[{i}]", g, dt, n)
-            for k, d in kinds.items():
-                setattr(t, k, self._address(ops, f"{k}[{i}]", state[k][i], d, (n + 255) // 256 if k.endswith("scale") else n))
+        struct.pack_into(f"@{len(values)}Q", table, 0, *values)        # (the structure: eight numbers of 64 bits)
         config = hwr.hwr_adamw_config(ops._kinds[dt], bits, len(params), table)
         self._handle = hwr.hwr_adamw_init(ops.ctx, config)
         self.ops, self.params, self.grads, self.state = ops, params, grads, state
@@ -367,13 +371,13 @@ class AdamW:
         self._args._fn = lambda ctx, at: self._fn(ctx, self._handle, at)
 
     @staticmethod
-    def _address(ops, name, t, dtype, n):
+    def _address(ops, name, i, t, dtype, n):
         if t.get_device() != ops.device:
-            _bad(name, f"on {t.device}, expected cuda:{ops.device}")
+            _bad(f"{name}[{i}]", f"on {t.device}, expected cuda:{ops.device}")
         if t.dtype is not dtype or t.numel() != n:
-            _bad(name, f"{t.numel()} of {t.dtype}, expected {n} of {dtype}")
+            _bad(f"{name}[{i}]", f"{t.numel()} of {t.dtype}, expected {n} of {dtype}")
         if not t.is_contiguous():
-            _bad(name, "not contiguous")
+            _bad(f"{name}[{i}]", "not contiguous")
         return t.data_ptr()
 
     @staticmethod

@@ -72,10 +72,10 @@ hwr_status init_impl(int32_t device, void *stream, hwr_ops **out) {
     c->dev = device;
     c->cus = prop.multiProcessorCount;
     c->stream = static_cast<hipStream_t>(stream);
-    const uint64_t bytes = kZeroBytes + kMaxShared * sizeof(int);
+    const uint64_t bytes = kZeroBytes + kMaxShared * sizeof(unsigned);
     e = hipMalloc(&c->zeros, bytes);
     if (e == hipSuccess) e = hipMemset(c->zeros, 0, bytes);
-    c->arrived = reinterpret_cast<int *>(static_cast<char *>(c->zeros) + kZeroBytes);
+    c->arrived = reinterpret_cast<unsigned *>(static_cast<char *>(c->zeros) + kZeroBytes);
     if (e == hipSuccess) e = hipDeviceSynchronize();
     if (e != hipSuccess) {
         release(c);
@@ -239,6 +239,7 @@ constexpr int kLowParts = 4;      // parts of the shrink's contraction, few rows
 hwr_status few(hwr_ops *c, FewArgs f, bool bf16, RowsKind kind) {
     const bool adapter = kind == RowsKind::kAdapter;
     f.m_pad = (f.m + 3) / 4 * 4;
+    f.units = c->cus;
     f.parts = few_parts(f.g.n, f.g.G, f.k, f.m, bf16, adapter, c->cus);
     f.low_parts = kLowParts;
     const uint64_t sums = adapter || f.parts > 1 ? static_cast<uint64_t>(f.parts) * f.g.n * f.m_pad : 0;

@@ -267,17 +267,15 @@ constexpr int kPartElements = 16384;
 static_assert(kPartElements >= kMaxTop && kMaxParts * kMaxTop <= kCandidates && kMaxParts <= 64);
 
 // Whether this workgroup is the last of the row's parts; what the others have put is then there to be got.  No one waits for
-// another: whoever comes last goes on, and leaves the count at zero.  What is shared goes through put_shared and get_shared
+// another: whoever comes last goes on, and the count is zero again.  What is shared goes through put_shared and get_shared
 // alone, past the L2s (an XCD's each), so that it is enough that a part's stores are done (vmcnt, every wave before the barrier)
 // before it is counted.  (Fences of the whole device, which write back an L2 in every wave: 48 x 128,000 with
 // twenty tokens 58 us; a second launch instead 14.6.)
 __device__ inline bool last_part(const ProbsArgs &a, int64_t r, TeamSpace &ts, int tid) {
     wait_vm<0>();
     __syncthreads();
-    if (tid == 0) {
-        ts.count = __hip_atomic_fetch_add(a.arrived + r, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (ts.count == a.parts - 1) put_shared(a.arrived + r, 0);
-    }
+    // (counts up to the last part, and from there to zero again)
+    if (tid == 0) ts.count = static_cast<int>(atomicInc(a.arrived + r, static_cast<unsigned>(a.parts - 1)));
     __syncthreads();
     return ts.count == a.parts - 1;
 }

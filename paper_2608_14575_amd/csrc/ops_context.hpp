@@ -16,7 +16,7 @@ struct hwr_ops {
     int dev = 0, cus = 0;
     hipStream_t stream = nullptr;
     void *zeros = nullptr;
-    int *arrived = nullptr;       // zeros between calls (launch_probs)
+    unsigned *arrived = nullptr;       // zeros between calls (launch_probs)
     // Work space: the last block is in use.  Blocks grow by powers of two and stay
     // until hwr_ops_free: captured graphs hold their addresses.
     std::vector<void *> blocks;

@@ -109,6 +109,7 @@ struct FewArgs {
     int64_t ldy;
     const void *a, *b;            // adapters
     const float *scale;
+    int units;                    // compute units
     int parts, low_parts;         // parts of the contraction
     float *partial;               // [parts][n][m_pad], with parts > 1 or an adapter
     float *low;                   // [low_parts][n][rank]
@@ -150,7 +151,7 @@ struct ProbsArgs {
     int32_t *top_token;
     int parts;                    // workgroups that share a row (probs_parts)
     void *partial;                // with parts > 1: probs_bytes
-    int *arrived;                 // [kMaxShared] zeros, and zeros again
+    unsigned *arrived;            // [kMaxShared] zeros, and zeros again
 };
 struct ProbsGradArgs {
     int64_t n;

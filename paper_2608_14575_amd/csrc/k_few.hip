@@ -149,6 +149,15 @@ __global__ void __launch_bounds__(kWaves * 64, DEEP ? 2 : 4) k_few(FewArgs a) { 
         }
     }
 
+    // what follows the sums in a layer is on its way while they are added up (G = 0: nothing is loaded)
+    const bool ends = KIND == RowsKind::kLinear && a.parts == 1 && wave == 0;
+    auto columns_of = [&](int e) { return Finish<E, V>(a.end, c0 + (4 * q + e) * V, a.m, ends ? a.g.G : 0, rt.g); };
+    const Finish<E, V> finish[4] = {columns_of(0), columns_of(1), columns_of(2), columns_of(3)};
+    Some<E, V> res[4];
+    if (ends)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) finish[e].load(max(row, 0), res[e]);
+
     // sum over the waves, halving; wave 0 ends with the total
 #pragma unroll
     for (int half = kWaves / 2; half; half /= 2) {
@@ -177,13 +186,10 @@ __global__ void __launch_bounds__(kWaves * 64, DEEP ? 2 : 4) k_few(FewArgs a) { 
     } else if (KIND == RowsKind::kLinear && row >= 0) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const Finish<E, V> finish(a.end, c0 + (4 * q + e) * V, a.m, a.g.G, rt.g);
-            Some<E, V> res;
-            finish.load(row, res);
             float v[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) v[j] = acc[j][e];
-            finish.store(row, res, v, static_cast<E *>(a.y), a.ldy);
+            finish[e].store(row, res[e], v, static_cast<E *>(a.y), a.ldy);
         }
     } else if (row >= 0) {
         E *y = static_cast<E *>(a.y) + row * a.ldy;

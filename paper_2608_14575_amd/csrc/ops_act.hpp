@@ -78,17 +78,14 @@ __device__ __host__ __forceinline__ auto with_act(int act, Run &&run) {
 // have zeros for z and no activation).
 template <class E, int V>
 struct Finish {
-    float bias[V];
+    Some<E, V> b;                 // the bias as it stands in memory: converted where it is used, so that no one waits for it here
     const Epilogue &a;
     int c, m, act;
-    bool in_group;
+    bool in_group, biased;
     __device__ __forceinline__ Finish(const Epilogue &end, int c_, int m_, int G, int g) : a(end), c(c_), m(m_), in_group(g < G) {
         act = in_group ? a.act : static_cast<int>(HWR_ACT_NONE);
-        Some<E, V> b;
-        const bool have = in_group && a.bias && c < m;
-        if (have) b.load(static_cast<const E *>(a.bias) + static_cast<int64_t>(g) * m, c, m);
-#pragma unroll
-        for (int i = 0; i < V; ++i) bias[i] = have ? static_cast<float>(b.e[i]) : 0.0f;
+        biased = in_group && a.bias;
+        if (biased && c < m) b.load(static_cast<const E *>(a.bias) + static_cast<int64_t>(g) * m, c, m);
     }
     // the residual of row r
     __device__ __forceinline__ void load(int64_t r, Some<E, V> &res) const {
@@ -99,7 +96,7 @@ struct Finish {
         if (c >= m) return;
         float z[V], o[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) z[i] = in_group ? v[i] + bias[i] : 0.0f;
+        for (int i = 0; i < V; ++i) z[i] = !in_group ? 0.0f : biased ? v[i] + static_cast<float>(b.e[i]) : v[i];
         with_act(act, [&](auto A) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < V; ++i) o[i] = activate<E, A.value>(z[i]);

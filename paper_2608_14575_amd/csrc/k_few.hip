@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(kWaves * 64, DEEP ? 2 : 4) k_few(FewArgs a) { 
     // what follows the sums in a layer is on its way while they are added up (G = 0: nothing is loaded)
     const bool ends = KIND == RowsKind::kLinear && a.parts == 1 && wave == 0;
     auto columns_of = [&](int e) { return Finish<E, V>(a.end, c0 + (4 * q + e) * V, a.m, ends ? a.g.G : 0, rt.g); };
-    const Finish<E, V> finish[4] = {columns_of(0), columns_of(1), columns_of(2), columns_of(3)};
+    Finish<E, V> finish[4] = {columns_of(0), columns_of(1), columns_of(2), columns_of(3)};
     Some<E, V> res[4];
     if (ends)
 #pragma unroll
@@ -189,6 +189,7 @@ __global__ void __launch_bounds__(kWaves * 64, DEEP ? 2 : 4) k_few(FewArgs a) { 
             float v[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) v[j] = acc[j][e];
+            finish[e].settle();
             finish[e].store(row, res[e], v, static_cast<E *>(a.y), a.ldy);
         }
     } else if (row >= 0) {
@@ -232,9 +233,10 @@ __global__ void __launch_bounds__(kJoinThreads) k_join(FewArgs a) {
         g = group_of(a.g, p, lane);
         if (row < 0) return;
         const float sum[4] = {v[0], v[1], v[2], v[3]};
-        const Finish<E, 4> finish(a.end, c, a.m, a.g.G, g);
+        Finish<E, 4> finish(a.end, c, a.m, a.g.G, g);
         Some<E, 4> res;
         finish.load(row, res);
+        finish.settle();
         finish.store(row, res, sum, static_cast<E *>(a.y), a.ldy);
         return;
     }

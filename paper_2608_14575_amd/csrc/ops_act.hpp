@@ -74,18 +74,21 @@ __device__ __host__ __forceinline__ auto with_act(int act, Run &&run) {
     return run(std::integral_constant<int, HWR_ACT_NONE>{});
 }
 
-// What follows a product for V neighbouring columns c (below m) of rows of one group (g == G: of none, which
-// have zeros for z and no activation).
+// What follows a product for V neighbouring columns c (below m) of rows of one group (g == G: of none: their
+// sums are zeros, and stay so without a bias, whatever the activation).
 template <class E, int V>
 struct Finish {
-    Some<E, V> b;                 // the bias as it stands in memory: converted where it is used, so that no one waits for it here
+    Some<E, V> b;                 // the bias as it stands in memory, until settle(): no one waits for it here
+    float bias[V];
     const Epilogue &a;
-    int c, m, act;
-    bool in_group, biased;
-    __device__ __forceinline__ Finish(const Epilogue &end, int c_, int m_, int G, int g) : a(end), c(c_), m(m_), in_group(g < G) {
-        act = in_group ? a.act : static_cast<int>(HWR_ACT_NONE);
-        biased = in_group && a.bias;
-        if (biased && c < m) b.load(static_cast<const E *>(a.bias) + static_cast<int64_t>(g) * m, c, m);
+    int c, m;
+    bool biased;
+    __device__ __forceinline__ Finish(const Epilogue &end, int c_, int m_, int G, int g) : a(end), c(c_), m(m_), biased(g < G && end.bias && c_ < m_) {
+        if (biased) b.load(static_cast<const E *>(a.bias) + static_cast<int64_t>(g) * m, c, m);
+    }
+    __device__ __forceinline__ void settle() {
+#pragma unroll
+        for (int i = 0; i < V; ++i) bias[i] = biased ? static_cast<float>(b.e[i]) : 0.0f;
     }
     // the residual of row r
     __device__ __forceinline__ void load(int64_t r, Some<E, V> &res) const {
@@ -96,19 +99,17 @@ struct Finish {
         if (c >= m) return;
         float z[V], o[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) z[i] = !in_group ? 0.0f : biased ? v[i] + static_cast<float>(b.e[i]) : v[i];
-        with_act(act, [&](auto A) __attribute__((always_inline)) {
+        for (int i = 0; i < V; ++i) z[i] = v[i] + bias[i];
+        if (a.z) Some<E, V>(z).store(static_cast<E *>(a.z) + r * a.ldz, c, m);
+        with_act(a.act, [&](auto A) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < V; ++i) o[i] = activate<E, A.value>(z[i]);
         });
-        Some<E, V> out;
+        if (a.residual) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) out.e[i] = static_cast<E>(a.residual ? o[i] + static_cast<float>(res.e[i]) : o[i]);
-        out.store(y + r * ldy, c, m);
-        if (!a.z) return;
-#pragma unroll
-        for (int i = 0; i < V; ++i) out.e[i] = static_cast<E>(z[i]);
-        out.store(static_cast<E *>(a.z) + r * a.ldz, c, m);
+            for (int i = 0; i < V; ++i) o[i] += static_cast<float>(res.e[i]);
+        }
+        Some<E, V>(o).store(y + r * ldy, c, m);
     }
 };
 

@@ -390,22 +390,26 @@ struct ThroughLds {
     static constexpr int V = 16 / sizeof(E);                   // columns of a chunk
     static constexpr int kCpr = BN / V;                        // chunks of a row
     static constexpr int U = 32 * WR * kCpr / NT;              // chunks of a thread in a turn
-    static constexpr int kLine = BN * 4;
+    static constexpr int kLine = BN * 4, kTurns = RF / 2;
     static_assert(RF % 2 == 0 && NT % kCpr == 0 && 32 * WR * kLine <= (BM + BN) * kStageBytes);
     // first column of the thread's chunks
     static __device__ int column(int tid) { return tid % kCpr * V; }
-    // prepare(turn, u, row) for the thread's chunks of a turn before its barrier, put(turn, u, row, values) after it;
-    // rows count from the tile's first
+    // prepare(turn, u, row) for the thread's chunks of a turn, two turns before (what three turns read is in flight
+    // at once), put(turn, u, row, values) in its turn; rows count from the tile's first
     template <class Prepare, class Put>
     static __device__ __forceinline__ void run(char *buf0, char *buf1, const f32x4 (&acc)[RF][CF], int tid, Prepare prepare, Put put) {
         const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WC, wc = wave % WC;
         const int col = tid % kCpr;
         auto row_of = [&](int turn, int i) { return i / 32 * (RF * 16) + turn * 32 + i % 32; };
         auto mine = [&](int u) { return u * (NT / kCpr) + tid / kCpr; };
+        auto prepare_turn = [&](int turn) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) prepare(0, u, row_of(0, mine(u)));
+            for (int u = 0; u < U; ++u) prepare(turn, u, row_of(turn, mine(u)));
+        };
+        prepare_turn(0);
+        if (kTurns > 1) prepare_turn(1);
 #pragma unroll
-        for (int turn = 0; turn < RF / 2; ++turn) {
+        for (int turn = 0; turn < kTurns; ++turn) {
             char *buf = turn & 1 ? buf1 : buf0;
 #pragma unroll
             for (int f = 0; f < 2; ++f)
@@ -414,9 +418,7 @@ struct ThroughLds {
                     const int i = wr * 32 + f * 16 + (lane & 15), chunk = (wc * CF + j) * 4 + (lane >> 4);
                     *reinterpret_cast<f32x4 *>(buf + i * kLine + ((chunk ^ (i & 15)) << 4)) = acc[turn * 2 + f][j];
                 }
-            if (turn + 1 < RF / 2)
-#pragma unroll
-                for (int u = 0; u < U; ++u) prepare(turn + 1, u, row_of(turn + 1, mine(u)));
+            if (turn + 2 < kTurns) prepare_turn(turn + 2);
             __syncthreads();
 #pragma unroll
             for (int u = 0; u < U; ++u) {

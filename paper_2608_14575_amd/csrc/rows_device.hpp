@@ -140,7 +140,7 @@ __device__ inline void store_rows(const RowsArgs &a, const RowTile &rt, int c0, 
     if constexpr (KIND == RowsKind::kLinear) {
 #pragma unroll
         for (int j = 0; j < CF; ++j) {
-            const Finish<E, 4> finish(a.end, c0 + (wc * CF + j) * 16 + q * 4, a.m, a.g.G, rt.g);
+            Finish<E, 4> finish(a.end, c0 + (wc * CF + j) * 16 + q * 4, a.m, a.g.G, rt.g);
             int r[RF];
             Some<E, 4> res[RF];
 #pragma unroll
@@ -148,6 +148,7 @@ __device__ inline void store_rows(const RowsArgs &a, const RowTile &rt, int c0, 
                 r[i] = rows[(wr * RF + i) * 16 + (lane & 15)];
                 finish.load(max(r[i], 0), res[i]);
             }
+            finish.settle();
 #pragma unroll
             for (int i = 0; i < RF; ++i) {
                 const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
@@ -176,17 +177,18 @@ __device__ inline void store_whole_rows(const RowsArgs &a, const RowTile &rt, in
     constexpr int V = T::V;
     constexpr bool kLayer = KIND == RowsKind::kLinear;
     const int c = c0 + T::column(tid);
-    const Finish<E, V> finish(a.end, c, a.m, a.g.G, rt.g);     // (layers)
-    Some<E, V> res[2][T::U];
-    int row[2][T::U];
+    Finish<E, V> finish(a.end, c, a.m, a.g.G, rt.g);           // (layers)
+    Some<E, V> res[3][T::U];
+    int row[3][T::U];
     auto fetch = [&](int turn, int u, int i) __attribute__((always_inline)) {
-        row[turn & 1][u] = rows[i];
-        if constexpr (kLayer) finish.load(max(row[turn & 1][u], 0), res[turn & 1][u]);
+        row[turn % 3][u] = rows[i];
+        if constexpr (kLayer) finish.load(max(row[turn % 3][u], 0), res[turn % 3][u]);
     };
     auto put = [&](int turn, int u, int, const float (&v)[V]) __attribute__((always_inline)) {
-        const int r = row[turn & 1][u];
+        if (kLayer && turn == 0 && u == 0) finish.settle();
+        const int r = row[turn % 3][u];
         if (r < 0 || c >= a.m) return;
-        if constexpr (kLayer) finish.store(r, res[turn & 1][u], v, static_cast<E *>(a.y), a.ldy);
+        if constexpr (kLayer) finish.store(r, res[turn % 3][u], v, static_cast<E *>(a.y), a.ldy);
         else Some<E, V>(v).store(static_cast<E *>(a.y) + r * a.ldy, c, a.m);
     };
     T::run(buf0, buf1, acc, tid, fetch, put);

@@ -153,21 +153,31 @@ struct __attribute__((packed, aligned(sizeof(E)))) Some {
 #pragma unroll
         for (int i = 0; i < V; ++i) e[i] = static_cast<E>(v[i]);
     }
+    // (Cut ones go element by element through the first place, in loops that stay loops: unrolled, they are most of a kernel's
+    // code, between what runs.)
     __device__ __forceinline__ void load(const E *line, int c, int m) {
         if (c + V <= m) {
             *this = *reinterpret_cast<const Some *>(line + c);
         } else {
+#pragma unroll 1
+            for (int i = V - 1; i >= 0; --i) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) e[i] = line[min(c + i, m - 1)];
+                for (int j = V - 1; j > 0; --j) e[j] = e[j - 1];
+                e[0] = line[min(c + i, m - 1)];
+            }
         }
     }
     __device__ __forceinline__ void store(E *line, int c, int m) const {
         if (c + V <= m) {
             *reinterpret_cast<Some *>(line + c) = *this;
         } else {
+            Some s = *this;
+#pragma unroll 1
+            for (; c < m; ++c) {
+                line[c] = s.e[0];
 #pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (c + i < m) line[c + i] = e[i];
+                for (int j = 1; j < V; ++j) s.e[j - 1] = s.e[j];
+            }
         }
     }
 };

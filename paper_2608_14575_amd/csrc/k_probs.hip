@@ -78,17 +78,19 @@ struct Sums {
         s *= f;
         m = to;
     }
+    template <int LANES = 64>
     __device__ void join_lanes(float c2);
 };
 
-// (of all lanes of a wave, in every lane: the largest maximum first, then one rescale and sums)
+// (of all lanes of a wave, or of LANES neighbours, in every lane: the largest maximum first, then one rescale and sums)
+template <int LANES>
 __device__ inline void Sums::join_lanes(float c2) {
     float to = m;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) to = fmaxf(to, __shfl_xor(to, d));
+    for (int d = 1; d < LANES; d <<= 1) to = fmaxf(to, __shfl_xor(to, d));
     rescale(to, c2);
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) s += __shfl_xor(s, d), t += __shfl_xor(t, d);
+    for (int d = 1; d < LANES; d <<= 1) s += __shfl_xor(s, d), t += __shfl_xor(t, d);
 }
 
 // Order of the most likely tokens: larger logits first, of equal ones the lower token.  Both
@@ -131,7 +133,13 @@ __device__ inline int larger(const uint64_t *keys, int count, uint64_t than) {
 // Chunks of a row that a thread loads at a time.
 constexpr int kLoad = 4;
 
-// out(rank, key, token) of the `top` first of the row, ranks in any order; T threads, whose largest
+// Rows up to kShortElements, which 16 threads load at a time, have those, up to kWaveElements a wave; longer ones
+// 256 threads, or 1024 where workgroups are few and long.  us, 16 threads / a wave: bf16 16,384 x 128 5.7 / 12.7, 16,384 x 512 5.8 / 12.8,
+// 1,000 x 300 5.7 / 5.1 (the call's host time); the gradient 5.6 / 7.0, 7.9 / 8.5, 5.5 / 5.1.
+template <class E>
+constexpr int kShortElements = 16 * kLoad * kEpc<E>;
+constexpr int kWaveElements = 2048, kFewTeams = 512, kTeamElements = 8192;
+// out(rank, key, token) of the `top` first of the row, ranks in any order; T threads, `threads` of which have chunks, whose largest
 // elements are `most`, and whose chunks, where the row has kLoad a thread at most, are `in` (KEPT; else they
 // are loaded again: to keep them takes registers that many workgroups want).
 //
@@ -141,8 +149,8 @@ constexpr int kLoad = 4;
 // it look for them.  Each candidate's rank is the number of candidates before it.  Where there are more
 // than kCandidates (long runs of equal logits), they are found one by one instead.
 template <class E, int T, bool KEPT, class Out>
-__device__ inline void select_top(const Span<E> &row, const u32x4 (&in)[kLoad], int offset, int top, float most, TeamSpace &ts,
-                                  int tid, Out out) {
+__device__ inline void select_top(const Span<E> &row, const u32x4 (&in)[kLoad], int threads, int offset, int top, float most,
+                                  TeamSpace &ts, int tid, Out out) {
     constexpr int kShare = T / kShares;    // threads that share a maximum
     float shared = most;
 #pragma unroll
@@ -170,7 +178,7 @@ __device__ inline void select_top(const Span<E> &row, const u32x4 (&in)[kLoad], 
                 if (tid + u * T < row.chunks) visit(in[u], tid + u * T);
         } else {
 #pragma unroll 1
-            for (int c = tid; c < row.chunks; c += T) visit(row.load(c), c);
+            for (int c = tid < threads ? tid : row.chunks; c < row.chunks; c += threads) visit(row.load(c), c);
         }
     };
     auto elements = [&](u32x4 v, int c, auto visit) {
@@ -309,15 +317,15 @@ __device__ inline void join_parts(const ProbsArgs &a, int64_t r, TeamSpace &ts, 
     }
 }
 
-// T threads to a row, or to a part of it; 256 / T rows to a workgroup where T is less.
+// T threads to a row, or to a part of it; 256 / T rows to a workgroup where T is less (less than a wave without tokens alone).
 template <class E, int T, bool TOP>
 __global__ void __launch_bounds__(T < 256 ? 256 : T, T == 64 ? 8 : 1) k_probs(ProbsArgs a) {
     constexpr int NT = T < 256 ? 256 : T, kRows = NT / T, U = kLoad;
-    static_assert(T == 64 || kRows == 1);
-    __shared__ TeamSpace space[kRows];
+    static_assert(T == 64 || kRows == 1 || !TOP);
+    __shared__ TeamSpace space[T >= 64 ? kRows : 1];
     constexpr bool kKept = T == 1024;
     const int tid = threadIdx.x % T, lane = tid & 63;
-    TeamSpace &ts = space[threadIdx.x / T];
+    TeamSpace &ts = space[T >= 64 ? threadIdx.x / T : 0];
     const int64_t item = static_cast<int64_t>(block_id<NT>()) * kRows + threadIdx.x / T;
     const int64_t r = kRows > 1 ? item : item / a.parts;
     const int part = kRows > 1 ? 0 : static_cast<int>(item % a.parts);
@@ -334,12 +342,14 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T, T == 64 ? 8 : 1) k_probs(Pr
         v.add(x, c2);
     }
     u32x4 in[U];
-    for (int c = tid; c < row.chunks; c += U * T) {
+    // (a wave on a short row: 16 threads as without tokens, so that its sums have the same bits)
+    const int threads = T == 64 && a.m <= kShortElements<E> ? 16 : T;
+    for (int c = tid < threads ? tid : row.chunks; c < row.chunks; c += U * threads) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const uint32_t none = sizeof(E) == 2 ? 0xFF80FF80u : 0xFF800000u;      // -inf
             in[u] = u32x4{none, none, none, none};
-            if (c + u * T < row.chunks) in[u] = row.load(c + u * T);
+            if (c + u * threads < row.chunks) in[u] = row.load(c + u * threads);
         }
         float f[U][kEpc<E>], most = v.m;
 #pragma unroll
@@ -356,7 +366,7 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T, T == 64 ? 8 : 1) k_probs(Pr
     }
 
     const float mine = v.m;
-    v.join_lanes(c2);
+    v.join_lanes<(T < 64 ? T : 64)>(c2);
     if constexpr (T > 64) {
         if (lane == 0) ts.m[tid >> 6] = v.m, ts.s[tid >> 6] = v.s, ts.t[tid >> 6] = v.t;
         __syncthreads();
@@ -371,7 +381,7 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T, T == 64 ? 8 : 1) k_probs(Pr
         }
         if constexpr (TOP) {
             uint64_t *out = part_top(a, r, part);    // (a part has more elements than kMaxTop)
-            select_top<E, T, kKept>(row, in, first, a.top, mine, ts, tid,
+            select_top<E, T, kKept>(row, in, threads, first, a.top, mine, ts, tid,
                                     [&](int rank, uint32_t key, int token) { put_shared(out + rank, rank_key(key, token)); });
         }
         if (last_part(a, r, ts, tid)) join_parts<E, T, TOP>(a, r, ts, tid, c2);
@@ -380,7 +390,7 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T, T == 64 ? 8 : 1) k_probs(Pr
     const float log_s = logf(v.s);
     if (tid == 0) store_sums<E>(a, r, v, log_s);
     if constexpr (TOP)
-        select_top<E, T, kKept>(row, in, 0, a.top, mine, ts, tid, [&](int rank, uint32_t key, int token) {
+        select_top<E, T, kKept>(row, in, threads, 0, a.top, mine, ts, tid, [&](int rank, uint32_t key, int token) {
             if (a.top_logp) a.top_logp[r * a.top + rank] = log_prob(a, v, log_s, key_value(key));
             if (a.top_token) a.top_token[r * a.top + rank] = token;
         });
@@ -446,14 +456,13 @@ hipError_t go(const ProbsArgs &a, hipStream_t s) {
     constexpr int NT = T < 256 ? 256 : T, kRows = NT / T;
     const int64_t blocks = kRows > 1 ? (a.n + kRows - 1) / kRows : a.n * a.parts;
     if (blocks > INT32_MAX - grid_row(NT)) return hipErrorInvalidValue;
-    return a.top ? launch_kernel(k_probs<E, T, true>, wide_grid(blocks, NT), dim3(NT), 0, s, a)
-                 : launch_kernel(k_probs<E, T, false>, wide_grid(blocks, NT), dim3(NT), 0, s, a);
+    if constexpr (T >= 64)
+        if (a.top) return launch_kernel(k_probs<E, T, true>, wide_grid(blocks, NT), dim3(NT), 0, s, a);
+    return launch_kernel(k_probs<E, T, false>, wide_grid(blocks, NT), dim3(NT), 0, s, a);
 }
-// Rows up to kWaveElements have a wave each; longer ones 256 threads, or 1024 where workgroups are
-// few and long.
-constexpr int kWaveElements = 2048, kFewTeams = 512, kTeamElements = 8192;
 template <class E>
 hipError_t pick(const ProbsArgs &a, hipStream_t s) {
+    if (!a.top && a.m <= kShortElements<E>) return go<E, 16>(a, s);
     if (a.m <= kWaveElements) return go<E, 64>(a, s);
     if (a.parts > 1) return go<E, 1024>(a, s);
     if (a.n * a.parts <= kFewTeams && a.m / a.parts >= kTeamElements) return go<E, 1024>(a, s);
@@ -470,6 +479,7 @@ hipError_t go_grad(const ProbsGradArgs &a, hipStream_t s) {
 }
 template <class E>
 hipError_t pick_grad(const ProbsGradArgs &a, hipStream_t s) {
+    if (a.m <= kShortElements<E>) return go_grad<E, 16>(a, s);
     if (a.m <= kWaveElements) return go_grad<E, 64>(a, s);
     return go_grad<E, 256>(a, s);
 }

@@ -11,8 +11,9 @@ row's or m / 256 of a long row's terms, and its sums are rescaled and joined a f
   S, relative:  a = u (8 R + min(m, 2048) / 64 + m / 256 + 64)
   lse, log p:   a + 4 u (|value| + ln S + 1)
   entropy:      a + E (2 a + 8 u) + 4 u (ln S + 1)
-  gradient:     scale u (p (3 |v| + 8) (|dlogp| + |dentropy| (|v| + |H|)) + 2 |dlogp| at the token)
-                and half a step of its type, v = ln p."""
+  gradient:     scale u (p (3 |v| + |z| + 8) (|dlogp| + |dentropy| (|v| + |H|)) + p |dentropy| |z| + 2 |dlogp| at the token)
+                and half a step of its type, v = ln p.  (|z|: the call takes the scale as fp32, which is u of it off, and so
+                z = scale x by u |z|; v = z - lse and, of it, p by as much absolutely, however small v is.)"""
 import math
 
 import numpy as np
@@ -128,7 +129,8 @@ def differ(x, token, w, scale, dlogp, ent, dent):
     hit = torch.zeros_like(v).scatter_(1, token.long().clamp(0, m - 1)[:, None], 1.0) * held[:, None]
     d = scale * (dl[:, None] * (hit - p) - dh[:, None] * p * (v + h[:, None]))
     dl, dh, h = dl.abs()[:, None], dh.abs()[:, None], h.abs()[:, None]
-    tol = scale * U * (p * (3 * v.abs() + 8) * (dl + dh * (v.abs() + h)) + 2 * dl * hit)
+    z = torch.where(p > 0, w["z"], 0.0).abs()
+    tol = scale * U * (p * (3 * v.abs() + z + 8) * (dl + dh * (v.abs() + h)) + p * dh * z + 2 * dl * hit)
     return d, tol + TYPES["bf16" if x.dtype == torch.bfloat16 else "f32"][1] * d.abs() + 1e-37
 
 
@@ -140,6 +142,9 @@ SHAPES = [
     (260, 10007, 7, 0.8, "some", 0), (257, 4096, 0, 1.0, "lowest", 4), (11, 4099, 1, 1.0, "one", 0), (9, 128, 3, 3.0, "one", 0),
     (2, 160001, 32, 1.0, "none", 0), (2, 131072, 32, 1.0, "equal", 0), (300, 3000, 13, 1.0, "equal", 2), (40, 5000, 9, 1.0, "zeros", 0),
     (301, 700, 9, 1.0, "zeros", 0), (5, 33, 32, 1.0, "most", 0), (300, 8193, 20, 1.0, "most", 0),
+    # either side of where 16 threads, and a wave, make a row
+    (333, 256, 0, 1.0, "some", 0), (333, 257, 20, 1.0, "none", 1), (333, 512, 32, 1.0, "equal", 0), (333, 513, 17, 1.0, "some", 0),
+    (1001, 128, 0, 0.9, "lowest", 3), (77, 511, 20, 1.0, "most", 0), (65, 519, 0, 1.0, "none", 0), (18, 31, 31, 1.0, "some", 0),
 ]
 
 
@@ -167,9 +172,9 @@ def test_log_probs_and_gradient(ops, n, m, top, scale, mask, pad, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_outputs_one_by_one(ops, dtype):
+@pytest.mark.parametrize("n,m,top", [(37, 3001, 6), (37, 250, 20), (500, 511, 32), (9, 17, 1), (3, 700, 5), (70, 40001, 20)])
+def test_outputs_one_by_one(ops, n, m, top, dtype):
     """Every output alone, and logp without the others, are what they are together."""
-    n, m, top = 37, 3001, 6
     x, token = logits(n, m, TYPES[dtype][0], "some", 5)
     o = outputs(n, top)
     ops.log_probs(x, token, **o)
@@ -345,6 +350,32 @@ def test_other_stream_and_graph(ops):
         ops.log_probs_grad(x, token, eager["lse"], dlogp, dlogits=ed)
         assert all(torch.equal(o[k], eager[k]) for k in o) and torch.equal(d, ed)
     mine.close()
+
+
+def test_contexts_side_by_side(ops):
+    """Two contexts on two streams at once, and calls of one that share their rows by other numbers of parts, in turn:
+    each call's results are its own, time after time."""
+    calls = []
+    for n, m, top in ((48, 128000, 20), (2, 160001, 32), (100, 40000, 0), (1, 70001, 5), (17, 131072, 3)):
+        x, token = logits(n, m, torch.bfloat16, "some", n)
+        want = outputs(n, top)
+        ops.log_probs(x, token, **want)
+        calls.append((x, token, top, want))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    mine = [routed.RoutedOps(stream=s.cuda_stream) for s in streams]
+    got = []
+    for i in range(6):
+        for j, o in enumerate(mine):
+            for x, token, top, want in calls[::1 if (i + j) % 2 else -1]:
+                out = outputs(x.shape[0], top)
+                streams[j].wait_stream(torch.cuda.current_stream())
+                o.log_probs(x, token, **out)
+                got.append((out, want))
+    torch.cuda.synchronize()
+    assert all(torch.equal(out[k], want[k]) for out, want in got for k in out)
+    for o in mine:
+        o.close()
 
 
 def test_capture_needs_reserved_space():

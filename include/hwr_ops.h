@@ -37,7 +37,7 @@
  * [k][m] (adapter), A [G][k][rank], B [G][rank][m]; gradients have the layout of
  * what they belong to.  Rows of x, y, dy and dx may be strided: ldx etc. are the
  * distances of rows in elements, 0 for dense.  Every pointer is device memory
- * and no output overlaps an input.  Any number of rows up to 2^31 - 512 (hwr_group_rows:
+ * and no output overlaps an input (but dx of hwr_log_probs_grad).  Any number of rows up to 2^31 - 512 (hwr_group_rows:
  * 2^31 - 1), any width up to 65536 and any element alignment is accepted; products run
  * fastest where widths, row strides and pointers are multiples of 16 bytes.
  *

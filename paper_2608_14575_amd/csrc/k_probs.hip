@@ -136,9 +136,15 @@ constexpr int kLoad = 4;
 // Rows up to kShortElements, which 16 threads load at a time, have those, up to kWaveElements a wave; longer ones
 // 256 threads, or 1024 where workgroups are few and long.  us, 16 threads / a wave: bf16 16,384 x 128 5.7 / 12.7, 16,384 x 512 5.8 / 12.8,
 // 1,000 x 300 5.7 / 5.1 (the call's host time); the gradient 5.6 / 7.0, 7.9 / 8.5, 5.5 / 5.1.
+// A wave / 256 threads, with 20 tokens: bf16 16,384 x 1,000 29.5 / 67.6, 4,000 x 2,000 11.2 / 19.9.  Many rows fill the card with a wave
+// each, without joins between waves: kManyRows of up to kManyElements have one too (with tokens, whose search is the longer part of a
+// wave's time, kManyTops): 16,384 x 4,000 25.5 / 47.9 and 45.0 / 70.4 with 20 tokens, 2,000 x 4,000 5.7 / 8.8 and 12.2 / 13.3; but 300 x 6,000
+// 5.4 / 5.1 and 13.3 / 8.4, 2,000 x 6,000 with tokens 17.1 / 14.2; fp32 8,192 x 8,000 40.3 / 39.7 and 76.0 / 64.8.
+// 1024 threads / 256, with 20 tokens: bf16 2 x 32,000 9.4 / 12.5, 100 x 32,000 10.0 / 14.1, but 512 x 16,384 16.5 / 11.8, 1,000 x 9,000
+// 28.7 / 11.8.
 template <class E>
 constexpr int kShortElements = 16 * kLoad * kEpc<E>;
-constexpr int kWaveElements = 2048, kFewTeams = 512, kTeamElements = 8192;
+constexpr int kWaveElements = 2048, kManyElements = 6144, kManyRows = 1024, kManyTops = 4096, kFewTeams = 256, kTeamElements = 8192;
 // out(rank, key, token) of the `top` first of the row, ranks in any order; T threads, `threads` of which have chunks, whose largest
 // elements are `most`, and whose chunks, where the row has kLoad a thread at most, are `in` (KEPT; else they
 // are loaded again: to keep them takes registers that many workgroups want).
@@ -463,7 +469,7 @@ hipError_t go(const ProbsArgs &a, hipStream_t s) {
 template <class E>
 hipError_t pick(const ProbsArgs &a, hipStream_t s) {
     if (!a.top && a.m <= kShortElements<E>) return go<E, 16>(a, s);
-    if (a.m <= kWaveElements) return go<E, 64>(a, s);
+    if (a.m <= (a.n >= (a.top ? kManyTops : kManyRows) ? kManyElements : kWaveElements)) return go<E, 64>(a, s);
     if (a.parts > 1) return go<E, 1024>(a, s);
     if (a.n * a.parts <= kFewTeams && a.m / a.parts >= kTeamElements) return go<E, 1024>(a, s);
     return go<E, 256>(a, s);
@@ -486,7 +492,9 @@ hipError_t pick_grad(const ProbsGradArgs &a, hipStream_t s) {
 
 }  // namespace
 
-// Rows are shared where there are fewer than compute units, in parts of at least kPartElements.
+// Rows are shared where there are fewer than compute units, in parts of at least kPartElements
+// (bf16 with 20 tokens, us, at 8,192 / 16,384 / 65,536: 2 x 32,000 11.6 / 9.4 / -, 100 x 32,000 11.9 / 10.0 / -, 1 x 128,000
+// 15.5 / 13.3 / 19.6, 48 x 128,000 - / 13.3 / 21.5).
 int probs_parts(bool bf16, int64_t n, int m, int cus) {
     if (m <= kWaveElements) return 1;
     const int64_t want = cus / n;

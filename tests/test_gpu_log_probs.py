@@ -145,6 +145,9 @@ SHAPES = [
     # either side of where 16 threads, and a wave, make a row
     (333, 256, 0, 1.0, "some", 0), (333, 257, 20, 1.0, "none", 1), (333, 512, 32, 1.0, "equal", 0), (333, 513, 17, 1.0, "some", 0),
     (1001, 128, 0, 0.9, "lowest", 3), (77, 511, 20, 1.0, "most", 0), (65, 519, 0, 1.0, "none", 0), (18, 31, 31, 1.0, "some", 0),
+    # many rows: either side of where a wave makes a long one, and few and more workgroups of long rows
+    (1023, 4001, 0, 1.0, "some", 0), (1024, 6144, 0, 1.0, "none", 1), (1030, 6145, 0, 0.8, "lowest", 0), (4095, 2500, 20, 1.0, "some", 0),
+    (4097, 2503, 20, 1.0, "most", 5), (4096, 2049, 32, 1.0, "equal", 0), (256, 8197, 20, 1.0, "some", 0), (257, 16400, 5, 1.0, "none", 3),
 ]
 
 

@@ -506,7 +506,6 @@ def train_tokens(steps: int = 5, n: int = 4096, tokens: int = 4096, seed: int = 
     ops.close()
     dev, bf, stream = x.device, torch.bfloat16, torch.cuda.Stream()
     ops = RoutedOps(stream=stream.cuda_stream)
-    stream.wait_stream(torch.cuda.current_stream())
     g = torch.Generator(dev).manual_seed(seed)
     k, m, h, R = x.shape[1], 1024, 512, 16
 
@@ -528,6 +527,7 @@ def train_tokens(steps: int = 5, n: int = 4096, tokens: int = 4096, seed: int = 
     dlogp = torch.full((n,), -1.0 / n, device=dev)               # loss: minus the mean log probability
     opt = AdamW(ops, list(p.values()), list(grad.values()), lr=1e-2, weight_decay=0.0, bits=8, seed=seed,
                 steps=torch.zeros(1, dtype=torch.int64, device=dev))
+    stream.wait_stream(torch.cuda.current_stream())              # (all of these were filled there)
 
     def step():
         ops.adapter(x, w, p["a"], p["b"], scale, offsets, order, y=y)

@@ -367,8 +367,8 @@ class AdamW:
         self.lr, self.betas, self.eps, self.weight_decay, self.steps, self.seed = lr, betas, eps, weight_decay, steps, seed
         self._i64 = torch.int64
         self._args = _Args(ops._lib.hwr_adamw_step, hwr.hwr_adamw_args)
-        self._fn = C.cast(ops._lib.hwr_adamw_step, C.CFUNCTYPE(C.c_int, C.c_void_p, C.c_void_p, C.c_void_p))
-        self._args._fn = lambda ctx, at: self._fn(ctx, self._handle, at)
+        fn, handle = C.cast(ops._lib.hwr_adamw_step, C.CFUNCTYPE(C.c_int, C.c_void_p, C.c_void_p, C.c_void_p)), self._handle
+        self._args._fn = lambda ctx, at: fn(ctx, handle, at)       # (not of self, which would stay until its cycle is collected)
 
     @staticmethod
     def _address(ops, name, i, t, dtype, n):

@@ -1,10 +1,14 @@
 """The objects of paper_2608_14575_amd/routed.py without a device: what is ordered against
 what, on stand-ins for streams and contexts that write down the calls."""
 import contextlib
+import ctypes as C
+import gc
+import types
+import weakref
 
 import pytest
 
-from paper_2608_14575_amd import routed
+from paper_2608_14575_amd import hwr, routed
 
 torch = pytest.importorskip("torch")
 
@@ -71,3 +75,40 @@ def test_training_example_waits_for_its_tensors(monkeypatch, log, caller):
     last = max(i for i, e in enumerate(log) if e == ("fill",))
     first = min(i for i, e in enumerate(log) if e[0] == "op")
     assert ("op", "adapter") == log[first] and ("wait", 8, 7) in log[last:first], log
+
+
+class Plan:
+    """A context without a device for AdamW objects: hwr_adamw_init and _free note what they are called for, hwr_adamw_step
+    what it is called with."""
+    device, stream, ctx = -1, 0, 3
+
+    def __init__(self, monkeypatch, log):
+        @C.CFUNCTYPE(C.c_int, C.c_void_p, C.c_void_p, C.c_void_p)
+        def step(ctx, handle, args):
+            log.append(("step", ctx, handle, hwr.hwr_adamw_args.from_address(args).step))
+            return 0
+
+        def init(ctx, config):
+            log.append(("init", ctx, config.n_tensors))
+            return C.c_void_p(5)
+
+        monkeypatch.setattr(hwr, "hwr_adamw_init", init)
+        monkeypatch.setattr(hwr, "hwr_adamw_free", lambda handle: log.append(("free", handle.value)))
+        self._kinds = {torch.bfloat16: hwr.HWR_BF16, torch.float32: hwr.HWR_F32}
+        self._f32 = torch.float32
+        self._lib = types.SimpleNamespace(hwr_adamw_step=step)
+
+
+def test_dropped_adamw_is_freed_at_once(monkeypatch, log, caller):
+    """Without the cycle collector, which would free device memory at any later moment, also while a stream is captured."""
+    caller.cuda_stream = 0
+    opt = routed.AdamW(Plan(monkeypatch, log), [torch.ones(4)], [torch.ones(4)], lr=1e-3, steps=8)
+    opt.step()
+    assert log[-1] == ("step", 3, 5, 9) and opt.steps == 9
+    state, whole = weakref.ref(opt.state["m"][0]), weakref.ref(opt)
+    gc.disable()
+    try:
+        del opt
+        assert whole() is None and state() is None and log[-1] == ("free", 5)
+    finally:
+        gc.enable()

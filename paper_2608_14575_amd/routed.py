@@ -312,7 +312,8 @@ class AdamW:
     moment in place of it, rounded at random, from ``seed``, the step and the value's place.
 
     ``state`` is a dict of lists, as the attribute of the same name: "m" and "v", with 8 bits "m_scale" and
-    "v_scale", with masters "master"; left out, it is made here (zeros, and copies of the weights).
+    "v_scale", with masters "master"; left out, it is made here (zeros, and copies of the weights as they are on torch's
+    current stream) and there before any step.
 
     ``steps``, the number of steps done, is counted up by ``step``: an int, or a device tensor of one int64, which
     a captured ``step`` needs.  ``lr`` may be a device tensor of one float32 then.  Both,
@@ -338,6 +339,9 @@ class AdamW:
             if master and dt is torch.float32:
                 _bad("master", "for bfloat16 weights")
             state = self._make_state(torch, params, bits, master)
+            made = torch.cuda.current_stream(ops.device)
+            if made.cuda_stream != ops.stream:         # (steps run on the other)
+                made.synchronize()
         state = {k: list(v) for k, v in state.items()}
         bits = 8 if "m_scale" in state else 32
         kind = torch.float8_e4m3fn if bits == 8 else torch.float32

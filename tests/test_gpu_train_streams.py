@@ -34,3 +34,22 @@ def test_training_example_on_a_stream(monkeypatch):
         assert got == want
         for name in p:
             assert torch.equal(p[name], q[name]) and torch.equal(grad[name], d[name]), name
+
+
+def test_made_state_on_another_stream(monkeypatch):
+    """States that are made on a stream which the context does not run on are there before the first step."""
+    def run(ops):
+        g = torch.Generator("cuda").manual_seed(2)
+        p, d = ([torch.randn(n, generator=g, device="cuda") for n in (5000, 3, 256)] for _ in range(2))
+        torch.cuda.synchronize()
+        opt = routed.AdamW(ops, p, d, lr=1e-2)
+        opt.step()
+        torch.cuda.synchronize()
+        return p + opt.state["m"] + opt.state["v"]
+
+    want = run(routed.RoutedOps(stream=torch.cuda.current_stream().cuda_stream))
+    own = torch.cuda.Stream()
+    monkeypatch.setattr(torch, "zeros", late(torch.zeros))
+    with torch.cuda.stream(torch.cuda.Stream()):
+        got = run(routed.RoutedOps(stream=own.cuda_stream))
+    assert all(torch.equal(a, b) for a, b in zip(want, got))

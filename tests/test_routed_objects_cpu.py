@@ -112,3 +112,22 @@ def test_dropped_adamw_is_freed_at_once(monkeypatch, log, caller):
         assert whole() is None and state() is None and log[-1] == ("free", 5)
     finally:
         gc.enable()
+
+
+@pytest.mark.parametrize("bits,master", [(32, False), (8, False), (8, True)])
+def test_made_state_is_there_before_the_first_step(monkeypatch, log, caller, bits, master):
+    """States are made on torch's current stream, steps run on the context's: where they are two, the object waits for the first.
+    A program's own state is the program's to order."""
+    monkeypatch.setattr(torch, "zeros", noting(log, torch.zeros))
+    p = [torch.ones(4, dtype=torch.bfloat16)]
+    opt = routed.AdamW(Plan(monkeypatch, log), p, [torch.ones_like(p[0])], lr=1e-3, bits=bits, master=master)
+    last = max(i for i, e in enumerate(log) if e == ("fill",))
+    assert ("synchronize", 7) in log[last:], log
+    state = opt.state
+    del log[:]
+    routed.AdamW(Plan(monkeypatch, log), p, [torch.ones_like(p[0])], lr=1e-3, state=state)
+    assert ("synchronize", 7) not in log
+    caller.cuda_stream = 0                                      # the context's own
+    del log[:]
+    routed.AdamW(Plan(monkeypatch, log), p, [torch.ones_like(p[0])], lr=1e-3, bits=bits, master=master)
+    assert ("fill",) in log and not any(e[0] == "synchronize" for e in log)

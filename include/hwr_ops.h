@@ -247,8 +247,9 @@ hwr_status hwr_log_probs_grad(hwr_ops *ops, const hwr_log_probs_grad_args *a);
  *
  * hwr_adamw_init keeps what it needs of the tensors' addresses and sizes (not their contents) in
  * device memory; their memory has to stay until hwr_adamw_free.  Nothing that is written may overlap
- * anything else.  Steps of one hwr_adamw have to be ordered among each other.  Init copies from the host and waits: not under capture.  hwr_adamw_free waits for the
- * device; the context may be freed before. */
+ * anything else.  Steps of one hwr_adamw have to be ordered among each other.  Init copies from the host and waits: HWR_ERR_STATE
+ * while the stream of ops is captured, with nothing recorded (while another of the thread's is, it is not to be called).  hwr_adamw_free
+ * waits for the device, and is not to be called while a stream is captured; the context may be freed before. */
 typedef struct hwr_adamw hwr_adamw;   /* opaque, owned by the library */
 
 typedef struct {

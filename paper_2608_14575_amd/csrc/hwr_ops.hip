@@ -16,9 +16,9 @@ std::string &hwr::ops_error() {
 
 hwr_status hwr::workspace(hwr_ops *c, uint64_t bytes, char **out) {
     if (bytes > c->size) {
-        hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
-        if (c->stream) OPS_HIP(c, hipStreamIsCapturing(c->stream, &cap));
-        if (cap != hipStreamCaptureStatusNone)
+        bool captured = false;
+        OPS_HIP(c, is_captured(c, &captured));
+        if (captured)
             return fail(c, HWR_ERR_STATE, "this call needs more work space than the context has, and its stream is being "
                         "captured: hwr_ops_reserve " + std::to_string(bytes) + " bytes before");
         uint64_t size = c->size ? c->size : uint64_t(1) << 20;

@@ -171,6 +171,9 @@ hwr_status adamw_init(hwr_ops *c, const hwr_adamw_config *f, hwr_adamw **out) {
         if (r.written) written_end = std::max(written_end, r.end);
     }
     OPS_ON_DEVICE(c, c->dev);
+    bool captured = false;
+    OPS_HIP(c, is_captured(c, &captured));
+    if (captured) return fail(c, HWR_ERR_STATE, "the stream is being captured: make it before");
     auto a = std::make_unique<hwr_adamw>();
     a->dev = c->dev;
     a->bf16 = bf16;
@@ -210,9 +213,9 @@ hwr_status adamw_step(hwr_ops *c, const hwr_adamw *w, const hwr_adamw_args *a) {
         return invalid(c, "a pointer is not aligned to its elements");
     OPS_ON_DEVICE(c, c->dev);
     if (!a->steps) {
-        hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
-        if (c->stream) OPS_HIP(c, hipStreamIsCapturing(c->stream, &cap));
-        if (cap != hipStreamCaptureStatusNone)
+        bool captured = false;
+        OPS_HIP(c, is_captured(c, &captured));
+        if (captured)
             return fail(c, HWR_ERR_STATE, "a graph would repeat the same step: have the steps counted on the device");
     }
     AdamwArgs k{};

@@ -74,6 +74,14 @@ class OnDevice {
     const OnDevice on_device(dev); \
     if (on_device.error != hipSuccess) return hip_fail((ctx), on_device.error, "hipSetDevice")
 
+// Whether the context's stream is being captured.
+inline hipError_t is_captured(const hwr_ops *c, bool *out) {
+    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+    const hipError_t e = c->stream ? hipStreamIsCapturing(c->stream, &cap) : hipSuccess;
+    *out = cap != hipStreamCaptureStatusNone;
+    return e;
+}
+
 // At least `bytes` of work space at *out.
 hwr_status workspace(hwr_ops *c, uint64_t bytes, char **out);
 

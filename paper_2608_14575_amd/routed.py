@@ -327,6 +327,8 @@ class AdamW:
                  state=None, steps=0, seed=0):
         import torch
         self._handle = None
+        if torch.cuda.is_current_stream_capturing():
+            raise HwrError(hwr.HWR_ERR_STATE, "AdamW: torch's current stream is being captured: make it before")
         params, grads = list(params), list(grads)
         if len(params) != len(grads):
             _bad("grads", f"{len(grads)} tensors for {len(params)} weights")

@@ -34,6 +34,7 @@ def caller(monkeypatch, log):
     """The stream that is torch's current one."""
     s = Stream(7, log)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: s)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     return s
 
 
@@ -131,3 +132,12 @@ def test_made_state_is_there_before_the_first_step(monkeypatch, log, caller, bit
     del log[:]
     routed.AdamW(Plan(monkeypatch, log), p, [torch.ones_like(p[0])], lr=1e-3, bits=bits, master=master)
     assert ("fill",) in log and not any(e[0] == "synchronize" for e in log)
+
+
+def test_adamw_is_not_made_under_capture(monkeypatch, log, caller):
+    """Nothing is filled, allocated or asked of the library."""
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    monkeypatch.setattr(torch, "zeros", noting(log, torch.zeros))
+    with pytest.raises(hwr.HwrError) as e:
+        routed.AdamW(Plan(monkeypatch, log), [torch.ones(4)], [torch.ones(4)], lr=1e-3)
+    assert e.value.status == hwr.HWR_ERR_STATE and log == []

@@ -26,7 +26,7 @@ __global__ void __launch_bounds__(WR *WC * 64) k_grad(RowsArgs a, ColsArgs b, Sl
     } else if (id < second) {
         cols_direct<E, ColsKind::kDense, BP, BP, WP, WQ, false>(b, id - first, buf0, buf1, nullptr, nullptr);
     } else if (c.dbias && id - second < bias_blocks(c)) {
-        sum_bias<E, WR * WC * 64>(c, id - second, reinterpret_cast<f32x4 *>(buf0));
+        sum_bias<E>(c, id - second, reinterpret_cast<f32x4 *>(buf0));
     }
 }
 

@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(kThreads) k_slope(SlopeArgs a, int tiles, PadA
 template <class E>
 __global__ void __launch_bounds__(kThreads) k_bias(SlopeArgs a) {
     __shared__ f32x4 part[kThreads];
-    sum_bias<E, kThreads>(a, blockIdx.x, part);
+    sum_bias<E>(a, blockIdx.x, part);
 }
 
 template <class E>

@@ -20,10 +20,11 @@ __device__ inline void pad_rows(const PadArgs::Matrix &m, int block) {
     }
 }
 
-// dbias[g][c]: the sums of the group's tiles.  Workgroup `id` of bias_blocks, NT threads and as many f32x4 of LDS.
-template <class E, int NT>
+// dbias[g][c]: the sums of the group's tiles.  Workgroup `id` of bias_blocks, 256 f32x4 of LDS.  The first four waves
+// add them up in workgroups of any size: the order of additions, and so the bits, are the same.
+template <class E>
 __device__ inline void sum_bias(const SlopeArgs &a, int id, f32x4 *part) {
-    constexpr int kWaves = NT / 64;
+    constexpr int kWaves = 4;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int slabs = (a.m + 255) / 256, g = id / slabs, c = (id % slabs * 64 + lane) * 4;
     // (tiles are capped as count_tiles caps them: offsets may hold anything)
@@ -37,12 +38,12 @@ __device__ inline void sum_bias(const SlopeArgs &a, int id, f32x4 *part) {
     }
     const int last = min(first + lane_tiles(a.g, g, a.places, false, p0, p1), all);
     f32x4 sum = {};
-    if (c < a.m) {
+    if (wave < kWaves && c < a.m) {
 #pragma unroll 8
         for (int t = first + wave; t < last; t += kWaves)
             sum += *reinterpret_cast<const f32x4 *>(a.partial + static_cast<int64_t>(t) * a.m_pad + c);
     }
-    part[wave * 64 + lane] = sum;
+    if (wave < kWaves) part[wave * 64 + lane] = sum;
     __syncthreads();
     if (wave != 0 || c >= a.m) return;
     for (int w = 1; w < kWaves; ++w) sum += part[w * 64 + lane];

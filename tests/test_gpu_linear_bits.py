@@ -1,0 +1,51 @@
+"""The bits of a layer's gradients do not depend on which others are asked for, nor on how much work
+space there is: sums that cancel, so that another order of additions shows in bf16 too."""
+import pytest
+
+from paper_2608_14575_amd import routed
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def ops():
+    assert torch.cuda.is_available(), "GPU tests need a device"
+    o = routed.RoutedOps(stream=torch.cuda.current_stream().cuda_stream)
+    yield o
+    o.close()
+
+
+def cancelling(g, n, width, dtype):
+    """Magnitudes over 2^20, each with its negative somewhere among the rows, and ones of size 1."""
+    big = torch.randn((n // 2, width), generator=g, device="cuda") * 2.0 ** (20 * torch.rand((n // 2, width), generator=g, device="cuda"))
+    x = torch.cat([big, -big, torch.randn((n - n // 2 * 2, width), generator=g, device="cuda")])
+    x[:16] += 1
+    return x[torch.randperm(n, generator=g, device="cuda")].to(TYPES[dtype])
+
+
+def problem(n, G, k, m, dtype):
+    g = torch.Generator("cuda").manual_seed(n)
+    edges = torch.tensor([i * n // G for i in range(G + 1)], dtype=torch.int32, device="cuda")
+    dy = cancelling(g, n, m, dtype)
+    x = torch.randn((n, k), generator=g, device="cuda").to(TYPES[dtype])
+    w = (torch.randn((G, k, m), generator=g, device="cuda") * 0.1).to(TYPES[dtype])
+    z = torch.randn((n, m), generator=g, device="cuda").to(TYPES[dtype])
+    return dy, x, w, edges, z
+
+
+# bf16 tiles of 256, 128 and 64, fp32 of 128, 64 and 32
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["none", "silu"])
+@pytest.mark.parametrize("n,G,k,m", [(9001, 2, 2048, 2048), (9001, 2, 1024, 2048), (4001, 2, 512, 1024), (701, 3, 256, 512), (1203, 1, 512, 512)])
+def test_each_gradient_alone(ops, n, G, k, m, act, dtype):
+    dy, x, w, edges, z = problem(n, G, k, m, dtype)
+    out = {"dx": torch.empty_like(x), "dw": torch.empty_like(w), "dbias": torch.empty((G, m), dtype=x.dtype, device="cuda")}
+    ops.linear_grad(dy, x, w, edges, act=act, z=z, **out)
+    for some in (("dx",), ("dw",), ("dbias",), ("dx", "dbias"), ("dw", "dbias"), ("dx", "dw")):
+        got = {q: torch.empty_like(out[q]) for q in some}
+        ops.linear_grad(dy, x, w, edges, act=act, z=z, **got)
+        for q in some:
+            assert torch.equal(got[q], out[q]), f"{q} of {some}: {int((got[q] != out[q]).sum())} of {got[q].numel()} differ"

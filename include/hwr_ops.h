@@ -61,7 +61,8 @@
  * before it queues anything (and keeps what it had until hwr_ops_free, so that captured
  * graphs stay valid); under stream capture it is HWR_ERR_STATE instead, with nothing
  * recorded: make the call once outside, or reserve what the message names
- * (hwr_ops_reserve), before capturing.  All calls of a context, and all replays of graphs
+ * (hwr_ops_reserve), before capturing.  (Both gradients of a grouped product or layer run in one launch, or, in
+ * less space and more time, where there is not enough for that, in two, with the same bits.)  All calls of a context, and all replays of graphs
  * captured from it, use the same work space: a replay has to be ordered against the
  * context's other calls and against its other graphs' replays (an event does), or each
  * graph captured from a context of its own.

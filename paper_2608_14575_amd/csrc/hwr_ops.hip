@@ -385,17 +385,26 @@ hwr_status product_grad(hwr_ops *c, const hwr_groups *g, const hwr_matmul_grad_a
     d.ldp = ldx;
     d.ldq = lddy;
     d.out = a->dw;
-    // in one launch, or one after the other: then they share the place of their partial sums
+    // in one launch, or, in less work space, one after the other: then they share the place of their partial sums
     const RowsPlan rp = rows_plan(bf16, RowsKind::kGrouped, false, r, c->cus);
     const ColsPlan cp = cols_plan(bf16, ColsKind::kDense, d, c->cus);
-    const bool pair = dx && a->dw && grad_pair(rp, cp);
+    bool pair = dx && a->dw && grad_pair(rp, cp);
     const uint64_t row_sums = dx ? rows_bytes(c, bf16, RowsKind::kGrouped, false, r) : 0,
                    weight_sums = a->dw ? weight_grad_bytes(c, bf16, ColsKind::kDense, d) : 0;
     const uint64_t bias_sums = dbias ? uint64_t{sizeof(float)} * slope_tiles(g->n, g->n_groups, s.places) * s.m_pad : 0;
-    const uint64_t bias_at = pair ? (row_sums + weight_sums + 255) / 256 * 256 : 0;
-    const uint64_t sums = std::max({row_sums, weight_sums, pair ? row_sums + weight_sums : 0, bias_at + bias_sums});
+    const uint64_t joint_sums = row_sums + weight_sums, joint_bias_at = (joint_sums + 255) / 256 * 256;
     char *ws = nullptr;
-    if (hwr_status st = workspace(c, used + sums, &ws)) return st;
+    if (pair) {
+        // (the same bits either way.  A refusal asks for what one launch needs.)
+        if (hwr_status st = workspace(c, used + std::max(joint_sums, joint_bias_at + bias_sums), &ws)) {
+            const std::string why = c->err;
+            pair = false;
+            if (workspace(c, used + std::max({row_sums, weight_sums, bias_sums}), &ws)) return fail(c, st, why);
+        }
+    } else if (hwr_status st = workspace(c, used + std::max({row_sums, weight_sums, bias_sums}), &ws)) {
+        return st;
+    }
+    const uint64_t bias_at = pair ? joint_bias_at : 0;
     if (sloped) dy = s.dz = ws + dz_at;
     if (dbias) s.partial = reinterpret_cast<float *>(ws + used + bias_at);
     if (sloped || dbias) OPS_HIP(c, launch_slope(bf16, act, s, pads.place(ws), c->stream));

@@ -6,6 +6,8 @@
 #include "ops_path.cpp"
 #undef main
 
+#include <algorithm>
+
 int g_copies = 0;
 extern "C" hipError_t hipMemcpy(void *, const void *, size_t, hipMemcpyKind) {
     ++g_copies;
@@ -32,7 +34,50 @@ void adamw_init() {
     }
 }
 
-const Scenario kCapture[] = {{"adamw_init", adamw_init}};
+// Both gradients of a product run in the space that they need one after the other, in which they
+// cannot share a launch: a graph that was captured with so much can be captured again.
+void gradients_one_after_the_other() {
+    auto asked = [](Rig &r, bool dx, bool dw) -> uint64_t {
+        g_capturing = true;
+        const hwr_status st = r.matmul_grad(dx, dw);
+        g_capturing = false;
+        const char *ask = std::strstr(hwr_ops_last_error(r.ops), "hwr_ops_reserve ");
+        return st == HWR_ERR_STATE && ask ? std::strtoull(ask + 16, nullptr, 10) : 0;
+    };
+    auto launched = [](const char *kernel) {
+        for (const Launch &l : g_log)
+            if (l.kernel.find(kernel) != std::string::npos) return true;
+        return false;
+    };
+    int found = 0;
+    for (int n = 100; n < 3000; n += n / 8)
+        for (int dtype : {HWR_BF16, HWR_F32}) {
+            const std::string what = std::to_string(n) + (dtype == HWR_BF16 ? " rows, bf16" : " rows, fp32");
+            auto set = [&](Rig &r) { r.n = n, r.k = r.m = 512, r.dtype = dtype; };
+            Rig r, more;
+            set(r), set(more);
+            const uint64_t both = asked(r, true, true), least = std::max(asked(r, true, false), asked(r, false, true));
+            if (!least) continue;
+            check(hwr_ops_reserve(r.ops, least) == HWR_OK && hwr_ops_reserve(more.ops, both) == HWR_OK, what + ": reserve");
+            g_log.clear();
+            g_capturing = true;
+            check(r.matmul_grad() == HWR_OK, what + ": " + std::to_string(least) + " bytes, " + hwr_ops_last_error(r.ops));
+            found += !launched("k_grad");
+            g_log.clear();
+            check(more.matmul_grad() == HWR_OK && launched("k_grad"), what + ": one launch in what is asked for");
+            g_capturing = false;
+            // and where memory is short
+            Rig s;
+            set(s);
+            g_fail = least + 1;
+            g_log.clear();
+            check(s.matmul_grad() == HWR_OK && launched("k_grad") == (both <= least), what + ": short of memory");
+            g_fail = SIZE_MAX;
+        }
+    check(found > 2, std::to_string(found) + " in two launches");
+}
+
+const Scenario kCapture[] = {{"adamw_init", adamw_init}, {"gradients_one_after_the_other", gradients_one_after_the_other}};
 
 }  // namespace
 

@@ -25,7 +25,7 @@ def driver(tmp_path_factory):
     return exe
 
 
-@pytest.mark.parametrize("scenario", ["adamw_init"])
+@pytest.mark.parametrize("scenario", ["adamw_init", "gradients_one_after_the_other"])
 def test_captured_calls(driver, scenario):
     r = subprocess.run([driver, scenario], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout + r.stderr

@@ -49,3 +49,41 @@ def test_each_gradient_alone(ops, n, G, k, m, act, dtype):
         ops.linear_grad(dy, x, w, edges, act=act, z=z, **got)
         for q in some:
             assert torch.equal(got[q], out[q]), f"{q} of {some}: {int((got[q] != out[q]).sum())} of {got[q].numel()} differ"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,k,m", [(805, 512, 512), (1630, 512, 512), (567, 512, 768)])
+def test_captured_with_the_space_of_one_at_a_time(ops, n, k, m, dtype):
+    """Space for the gradients one after the other is enough under capture, and gives the same bits."""
+    dy, x, w, edges, z = problem(n, 1, k, m, dtype)
+    want = {"dx": torch.empty_like(x), "dw": torch.empty_like(w), "dbias": torch.empty((1, m), dtype=x.dtype, device="cuda")}
+    product = {"dx": torch.empty_like(x), "dw": torch.empty_like(w)}
+    ops.linear_grad(dy, x, w, edges, act="silu", z=z, **want)
+    ops.matmul_grad(dy, x, w, edges, **product)
+    s = torch.cuda.Stream()
+    for layer in (False, True):
+        mine = routed.RoutedOps(stream=s.cuda_stream)
+        got = {q: torch.empty_like(want[q]) for q in (want if layer else product)}
+
+        def run(some):
+            if layer:
+                mine.linear_grad(dy, x, w, edges, act="silu", z=z, **some)
+            else:
+                mine.matmul_grad(dy, x, w, edges, **some)
+
+        torch.cuda.synchronize()
+        for q in got:
+            run({q: got[q]})
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            run(got)
+        for _ in range(3):
+            for q in got:
+                got[q].fill_(7)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(got[q], (want if layer else product)[q]) for q in got)
+        del graph
+        mine.close()

@@ -62,12 +62,14 @@ __device__ void few_shrink(const FewArgs &a, int item, float *lds) {
     }
 }
 
-// DEEP: workgroups have a compute unit each, and so twice the registers: three steps (fp32: two) are in flight, not one.  us from
-// memory, three / one: bf16 one row 4096 x 4096 10.0 / 13.2, 40 rows of 16 groups 1024 x 2048 18.7 / 21.0, 32 of 8 4096 x 1024 19.6 / 23.5;
-// fp32, two / one, 40 of 16 512 x 1024 10.0 / 10.6 (three 11.5).  The sums' order, and so their bits, are the same.
+// DEEP (bf16): workgroups have a compute unit each, and so twice the registers: three steps are in flight, not one.  us from
+// memory, three / one: one row 4096 x 4096 12.4 / 12.8, 40 rows of 16 groups 1024 x 2048 14.9 / 15.8, 32 of 8 4096 x 1024 17.6 / 18.9.
+// (Two in fp32: one row 4096 x 4096 19.3 / 18.4, 32 of 8 4096 x 1024 31.3 / 30.7.)  The sums' order, and so their bits, are the same.
+// The form with one step has its loop written out over plain arrays: with the other's, whose loads are told the step's array, the
+// compiler made a loop that took 3 to 5% more (adapters, bf16 one row 4096 x 4096 13.1 / 13.7, fp32 96 rows 2048 x 2048 21.0 / 22.0).
 template <class E, RowsKind KIND, bool DEEP>
 __global__ void __launch_bounds__(kWaves * 64, DEEP ? 2 : 4) k_few(FewArgs a) {   // else two workgroups on a compute unit
-    constexpr int kAhead = !DEEP ? 1 : sizeof(E) == 2 ? 3 : 2;
+    constexpr int kAhead = 3;
     constexpr bool ADAPTER = KIND == RowsKind::kAdapter;
     using El = Elem<E>;
     constexpr int V = El::kEpc, BM = kFewTile, BN = 16 * V, kStep = 4 * V;
@@ -98,54 +100,96 @@ __global__ void __launch_bounds__(kWaves * 64, DEEP ? 2 : 4) k_few(FewArgs a) { 
     // the wave's steps: first, first + stride, ... < steps
     const int steps = (k + kStep - 1) / kStep, stride = a.parts * kWaves;
     f32x4 acc[V] = {};
-    u32x4 nw[kAhead][V], nx[kAhead];
     // whole steps of whole columns: one lane offset, the rest of the address is uniform
     const uint32_t lane_at = static_cast<uint32_t>((q * V * a.m + c0 + m * V) * sizeof(E));
     const bool columns = c0 + BN <= a.m;
-    auto load_weights = [&](int step, u32x4 (&nw)[V]) __attribute__((always_inline)) {
-        if (columns && (step + 1) * kStep <= k) {
-            const char *base = reinterpret_cast<const char *>(w + static_cast<int64_t>(step) * kStep * a.m);
+    const int place = rt.p0 + m;
+    int row;
+    if constexpr (!DEEP) {
+        u32x4 nw[V], nx;
+        auto load_weights = [&](int step) {
+            if (columns && (step + 1) * kStep <= k) {
+                const char *base = reinterpret_cast<const char *>(w + static_cast<int64_t>(step) * kStep * a.m);
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    nw[i] = *reinterpret_cast<const typename El::Vec *>(base + static_cast<int64_t>(i) * a.m * sizeof(E) + lane_at);
+                return;
+            }
+            const int e = step * kStep + q * V;
 #pragma unroll
             for (int i = 0; i < V; ++i)
-                nw[i] = *reinterpret_cast<const typename El::Vec *>(base + static_cast<int64_t>(i) * a.m * sizeof(E) + lane_at);
-            return;
-        }
-        const int e = step * kStep + q * V;
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            nw[i] = load_chunk<E>(e + i < k ? w + static_cast<int64_t>(e + i) * a.m : nullptr, c0 + m * V, a.m);
-    };
-    int step = s * kWaves + wave;
-    // (on their way while the rows are looked up)
-#pragma unroll
-    for (int d = 0; d < kAhead; ++d)
-        if (step + d * stride < steps) load_weights(step + d * stride, nw[d]);
-    const int place = rt.p0 + m, row = place < rt.p1 ? row_at(a.g, place) : -1;
-    // (a place without a row computes one that it does not store)
-    const E *x = static_cast<const E *>(a.x) + (row < 0 ? 0 : row) * a.ldx + q * V;
-    auto load_row = [&](int step, u32x4 &nx) __attribute__((always_inline)) {
-        if ((step + 1) * kStep <= k) nx = *reinterpret_cast<const typename El::Vec *>(x + step * kStep);
-        else nx = load_chunk<E>(x, step * kStep, k - q * V);
-    };
-#pragma unroll
-    for (int d = 0; d < kAhead; ++d)
-        if (step + d * stride < steps) load_row(step + d * stride, nx[d]);
-    for (; step < steps; step += kAhead * stride) {
-#pragma unroll
-        for (int d = 0; d < kAhead; ++d) {
-            if (step + d * stride >= steps) break;
+                nw[i] = load_chunk<E>(e + i < k ? w + static_cast<int64_t>(e + i) * a.m : nullptr, c0 + m * V, a.m);
+        };
+        int step = s * kWaves + wave;
+        if (step < steps) load_weights(step);        // on their way while the rows are looked up
+        row = place < rt.p1 ? row_at(a.g, place) : -1;
+        // (a place without a row computes one that it does not store)
+        const E *x = static_cast<const E *>(a.x) + (row < 0 ? 0 : row) * a.ldx + q * V;
+        auto load_row = [&](int step) {
+            if ((step + 1) * kStep <= k) nx = *reinterpret_cast<const typename El::Vec *>(x + step * kStep);
+            else nx = load_chunk<E>(x, step * kStep, k - q * V);
+        };
+        if (step < steps) load_row(step);
+        for (; step < steps; step += stride) {
             typename El::Frag fw[V];
             union { u32x4 v; typename El::Frag f; } fx;
-            fx.v = nx[d];
+            fx.v = nx;
 #pragma unroll
-            for (int j = 0; j < V; ++j) fw[j] = column(nw[d], j);
-            const int next = step + (d + kAhead) * stride;
-            if (next < steps) {
-                load_weights(next, nw[d]);
-                load_row(next, nx[d]);
+            for (int j = 0; j < V; ++j) fw[j] = column(nw, j);
+            if (step + stride < steps) {
+                load_weights(step + stride);
+                load_row(step + stride);
             }
 #pragma unroll
             for (int j = 0; j < V; ++j) acc[j] = El::mma(fw[j], fx.f, acc[j]);
+        }
+    } else {
+        u32x4 nw[kAhead][V], nx[kAhead];
+        auto load_weights = [&](int step, u32x4 (&nw)[V]) __attribute__((always_inline)) {
+            if (columns && (step + 1) * kStep <= k) {
+                const char *base = reinterpret_cast<const char *>(w + static_cast<int64_t>(step) * kStep * a.m);
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    nw[i] = *reinterpret_cast<const typename El::Vec *>(base + static_cast<int64_t>(i) * a.m * sizeof(E) + lane_at);
+                return;
+            }
+            const int e = step * kStep + q * V;
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                nw[i] = load_chunk<E>(e + i < k ? w + static_cast<int64_t>(e + i) * a.m : nullptr, c0 + m * V, a.m);
+        };
+        int step = s * kWaves + wave;
+        // (on their way while the rows are looked up)
+#pragma unroll
+        for (int d = 0; d < kAhead; ++d)
+            if (step + d * stride < steps) load_weights(step + d * stride, nw[d]);
+        row = place < rt.p1 ? row_at(a.g, place) : -1;
+        // (a place without a row computes one that it does not store)
+        const E *x = static_cast<const E *>(a.x) + (row < 0 ? 0 : row) * a.ldx + q * V;
+        auto load_row = [&](int step, u32x4 &nx) __attribute__((always_inline)) {
+            if ((step + 1) * kStep <= k) nx = *reinterpret_cast<const typename El::Vec *>(x + step * kStep);
+            else nx = load_chunk<E>(x, step * kStep, k - q * V);
+        };
+#pragma unroll
+        for (int d = 0; d < kAhead; ++d)
+            if (step + d * stride < steps) load_row(step + d * stride, nx[d]);
+        for (; step < steps; step += kAhead * stride) {
+#pragma unroll
+            for (int d = 0; d < kAhead; ++d) {
+                if (step + d * stride >= steps) break;
+                typename El::Frag fw[V];
+                union { u32x4 v; typename El::Frag f; } fx;
+                fx.v = nx[d];
+#pragma unroll
+                for (int j = 0; j < V; ++j) fw[j] = column(nw[d], j);
+                const int next = step + (d + kAhead) * stride;
+                if (next < steps) {
+                    load_weights(next, nw[d]);
+                    load_row(next, nx[d]);
+                }
+#pragma unroll
+                for (int j = 0; j < V; ++j) acc[j] = El::mma(fw[j], fx.f, acc[j]);
+            }
         }
     }
 
@@ -293,8 +337,8 @@ hipError_t go(const FewArgs &a, hipStream_t s) {
     // tiles that are likely (few rows to a group make one): one workgroup on a compute unit, if there are no more
     const int64_t likely = a.g.n <= 4 * a.g.G ? static_cast<int64_t>(std::min(a.g.n, a.g.G)) * ct * a.parts : items;
     hipError_t e;
-    if constexpr (ADAPTER) e = launch_kernel(k_few<E, KIND, false>, grid, block, 0, s, a);
-    else if (likely <= a.units) e = launch_kernel(k_few<E, KIND, true>, grid, block, 0, s, a);
+    constexpr bool kDeep = !ADAPTER && sizeof(E) == 2;
+    if (kDeep && likely <= a.units) e = launch_kernel(k_few<E, KIND, kDeep>, grid, block, 0, s, a);
     else e = launch_kernel(k_few<E, KIND, false>, grid, block, 0, s, a);
     if (e != hipSuccess || (!ADAPTER && a.parts == 1)) return e;
     return join<E, KIND>(a, s);

@@ -273,7 +273,7 @@ void hwr_adamw_free(hwr_adamw *adamw);
 
 typedef struct {
     double lr, beta1, beta2;      /* lr 0 or more; betas in [0, 1)              */
-    double eps, weight_decay;     /* eps in [0, 1); weight_decay 0 or more      */
+    double eps, weight_decay;     /* eps in [0, 1) (2^-126 for less, but for 0); weight_decay 0 or more */
     uint64_t seed;
     int64_t step;                 /* t, 1 or more                               */
     int64_t *steps;               /* or, in device memory, the steps before this one: counted up

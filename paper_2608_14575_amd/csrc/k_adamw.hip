@@ -223,7 +223,8 @@ __host__ __device__ inline AdamwCoef coefficients(double lr, double beta1, doubl
     c.beta2_rest = static_cast<float>(1.0 - beta2);
     c.rate = static_cast<float>(lr / (1.0 - pow(beta1, static_cast<double>(step))));
     c.root_rate = static_cast<float>(1.0 / sqrt(1.0 - pow(beta2, static_cast<double>(step))));
-    c.eps = static_cast<float>(eps);
+    // (the hardware's reciprocal takes smaller ones for 0, and the conversion may: 0 / 0 is for an eps of 0 alone)
+    c.eps = eps > 0.0 ? fmaxf(static_cast<float>(eps), 0x1p-126f) : 0.0f;
     c.key = static_cast<uint32_t>((seed * 0x9E3779B97F4A7C15u + static_cast<uint64_t>(step)) * 0xBB67AE8584CAA73Bu >> 32);
     return c;
 }

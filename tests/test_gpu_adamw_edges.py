@@ -1,0 +1,35 @@
+"""AdamW at the ends of its arguments' ranges."""
+import pytest
+
+from paper_2608_14575_amd import routed
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def ops():
+    assert torch.cuda.is_available(), "GPU tests need a device"
+    o = routed.RoutedOps(stream=torch.cuda.current_stream().cuda_stream)
+    yield o
+    o.close()
+
+
+@pytest.mark.parametrize("eps", [1e-300, 1e-46, 1e-44, 1e-40, 1e-38, 2e-38, 1e-30])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_values_without_moments_stay_with_the_smallest_eps(ops, bits, eps):
+    """Only an eps of 0 makes 0 / 0 of a value that has had no gradient, and no eps above it changes a step by moments of size 1
+    (lr 2^-10 of 1, whatever rounding: p is off by 4 u of itself and 16 u of the update)."""
+    n = 768
+    p, g = torch.ones(n, device="cuda"), torch.zeros(n, device="cuda")
+    g[:256] = 1.0
+    g[300] = 1.0
+    opt = routed.AdamW(ops, [p], [g], lr=2.0 ** -10, eps=eps, weight_decay=0.0, bits=bits)
+    for _ in range(2):
+        opt.step()
+    assert p.isfinite().all() and (p[512:] == 1).all() and (p[256:300] == 1).all()
+    opt.close()
+    p.fill_(1)
+    opt = routed.AdamW(ops, [p], [g], lr=2.0 ** -10, eps=eps, weight_decay=0.0, bits=bits)
+    opt.step()
+    assert (p[g == 1].double() - (1 - 2.0 ** -10)).abs().max() < (4 + 16 * 2.0 ** -10) * 2.0 ** -24

@@ -9,9 +9,11 @@
 // smaller than half a step of e4m3 (2^-4 of the value), and of bf16 weights that have no
 // master smaller than 2^-9: rounded to nearest they would stand still, so they are rounded up or
 // down with the probability of the remainder.  The noise is a hash of the seed, the step
-// and the value's place.
+// and the value's place.  The root is without a bias then, its square is not: it grows by the variance of the
+// rounding, in a step at most the root's way (half of 1 - b2 of |g^2 / v - 1|) times the codes' distance (an eighth of the root), over the
+// 1 / (1 - b2) steps that v remembers by some 5% of v, with a standard deviation of 0.34.
 //
-// Bound by memory: 28 bytes a value with fp32 states, 10 to 18 with 8 bits.  A workgroup takes 8
+// Bound by memory: 28 bytes a value with fp32 states (bf16 without masters 22), 16 with 8 bits (bf16 without masters 10).  A workgroup takes 8
 // blocks of a tensor, a thread 8 values (16 bytes of bf16 at a time), a half-wave a block, so that a scale takes five
 // exchanges.  67.6 M values in 16 tensors: bf16 with masters and fp32 states 357 us (5.3 TB/s), bf16 alone with states of 8 bits
 // 137 us (5.0 TB/s; 180 when the roundings were made of integer steps, at 105 instructions a value); 466,000 fp32 values in 48

@@ -309,7 +309,8 @@ class AdamW:
     one size; the same tensors are read and written at every step.  bfloat16 weights are stepped through
     float32 masters (``master=True``) or alone, rounded up or down at random.  States have 32
     bits or 8 (``bits``): float8_e4m3fn with a float32 scale for every 256 values, the root of the second
-    moment in place of it, rounded at random, from ``seed``, the step and the value's place.
+    moment in place of it, rounded at random, from ``seed``, the step and the value's place (the second moment's
+    noise: a third of it, 5% above on the mean; include/hwr_ops.h has the figures).
 
     ``state`` is a dict of lists, as the attribute of the same name: "m" and "v", with 8 bits "m_scale" and
     "v_scale", with masters "master"; left out, it is made here (zeros, and copies of the weights as they are on torch's

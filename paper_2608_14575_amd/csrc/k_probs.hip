@@ -94,10 +94,10 @@ __device__ inline void Sums::join_lanes(float c2) {
 }
 
 // Order of the most likely tokens: larger logits first, of equal ones the lower token.  Both
-// zeros are equal.  (A NaN has a place in the order too, so that there are always enough.)
+// zeros are equal, and all masks.  (A NaN has a place in the order too, so that there are always enough.)
 __device__ inline uint32_t order_key(float x) {
     if (x != x) return 0xFFFFFFFFu;
-    const uint32_t b = __float_as_uint(x + 0.0f);
+    const uint32_t b = __float_as_uint(x < kMasked ? -INFINITY : x + 0.0f);
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ inline float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }

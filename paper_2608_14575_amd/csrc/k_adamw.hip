@@ -101,10 +101,11 @@ template <int SEL>
 __device__ inline uint32_t to_e4m3(float x, uint32_t noise, uint32_t into) {
     return static_cast<uint32_t>(__builtin_amdgcn_cvt_sr_fp8_f32(x, static_cast<int>(noise), static_cast<int>(into), SEL));
 }
-// fp32 to the bits of a bf16, as fp32.  (One that would round past the largest stays below.)
+// fp32 to the bits of a bf16, as fp32.  (One that would round past the largest stays below; the sum of a NaN's bits and
+// the noise may pass all ones, and be a zero's.)
 __device__ inline float to_bf16(float x, uint32_t noise) {
     const uint32_t bits = __float_as_uint(x), up = bits + noise;
-    return __uint_as_float(((up & 0x7F800000u) == 0x7F800000u ? bits : up) & 0xFFFF0000u);
+    return __uint_as_float((x != x || (up & 0x7F800000u) == 0x7F800000u ? bits : up) & 0xFFFF0000u);
 }
 
 // sqrt(v), one step of the residual's correction after the hardware's reciprocal root: rounded right but for

@@ -33,3 +33,25 @@ def test_values_without_moments_stay_with_the_smallest_eps(ops, bits, eps):
     opt = routed.AdamW(ops, [p], [g], lr=2.0 ** -10, eps=eps, weight_decay=0.0, bits=bits)
     opt.step()
     assert (p[g == 1].double() - (1 - 2.0 ** -10)).abs().max() < (4 + 16 * 2.0 ** -10) * 2.0 ** -24
+
+
+@pytest.mark.parametrize("payload", [0x7FFFFFFF, -1, 0x7FC00001, 0x7F800001, -0x7FFFFF, 0x7F800000])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_any_nan_stays_when_weights_are_rounded_at_random(ops, bits, payload):
+    """bf16 weights alone: a NaN of whatever bits in a moment (in 8 bits, in its scale) makes its weights NaN, and no zero of them."""
+    n = 512
+    p, g = torch.ones(n, dtype=torch.bfloat16, device="cuda"), torch.ones(n, dtype=torch.bfloat16, device="cuda")
+    for seed in range(8):
+        p.fill_(1)
+        opt = routed.AdamW(ops, [p], [g], lr=1e-3, bits=bits, seed=seed)
+        opt.step()
+        state = opt.state["m_scale" if bits == 8 else "m"][0]
+        state.view(torch.int32)[0] = payload
+        opt.step()
+        sick = torch.arange(n, device="cuda") < (256 if bits == 8 else 1)
+        if payload == 0x7F800000:
+            assert not p[sick].isfinite().any()
+        else:
+            assert p[sick].isnan().all()
+        assert p[~sick].isfinite().all()
+        opt.close()

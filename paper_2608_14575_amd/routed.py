@@ -306,7 +306,8 @@ class AdamW:
     """AdamW over many tensors at once, in one launch a step, on the stream of a ``RoutedOps``.
 
     ``params`` and ``grads`` are lists of dense tensors, of one type (bfloat16 or float32), pair by pair of
-    one size; the same tensors are read and written at every step.  bfloat16 weights are stepped through
+    one size; the same tensors are read and written at every step, in the memory that they have here (one that is given
+    other memory later, as by ``p.data = ...``, needs a new object).  bfloat16 weights are stepped through
     float32 masters (``master=True``) or alone, rounded up or down at random.  States have 32
     bits or 8 (``bits``): float8_e4m3fn with a float32 scale for every 256 values, the root of the second
     moment in place of it, rounded at random, from ``seed``, the step and the value's place (the second moment's
@@ -371,6 +372,8 @@ class AdamW:
         config = hwr.hwr_adamw_config(ops._kinds[dt], bits, len(params), table)
         self._handle = hwr.hwr_adamw_init(ops.ctx, config)
         self.ops, self.params, self.grads, self.state = ops, params, grads, state
+        # (steps go by addresses: the memory stays, also where a tensor is given other)
+        self._memory = [t.untyped_storage() for q in (params, grads, *state.values()) for t in q]
         self.lr, self.betas, self.eps, self.weight_decay, self.steps, self.seed = lr, betas, eps, weight_decay, steps, seed
         self._i64 = torch.int64
         self._args = _Args(ops._lib.hwr_adamw_step, hwr.hwr_adamw_args)
@@ -402,8 +405,8 @@ class AdamW:
 
     def close(self) -> None:
         if getattr(self, "_handle", None):
-            hwr.hwr_adamw_free(self._handle)
-            self._handle = None
+            hwr.hwr_adamw_free(self._handle)           # (waits for the device)
+            self._handle, self._memory = None, []
 
     def __del__(self):
         try:

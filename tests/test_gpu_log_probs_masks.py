@@ -35,3 +35,22 @@ def test_masks_of_both_kinds_are_equal(n, m, top, dtype):
     assert (logp[masked] == -math.inf).all() and logp[~masked].isfinite().all()
     assert ((lse == -math.inf) == (z == -math.inf).all(1)).all()
     ops.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kept", [5, 20, 21, 70, 600])
+@pytest.mark.parametrize("n,m", [(48, 32003), (3, 128000), (300, 5000), (4100, 2600)])
+def test_allowed_tokens_side_by_side(n, m, kept, dtype):
+    """A run of allowed tokens, as few and a few more than are asked for: few threads hold them all."""
+    top, t = 20, TYPES[dtype]
+    ops = routed.RoutedOps(stream=torch.cuda.current_stream().cuda_stream)
+    g = torch.Generator("cuda").manual_seed(kept)
+    first = torch.randint(0, m - kept + 1, (n, 1), generator=g, device="cuda")
+    at = torch.arange(m, device="cuda")[None]
+    x = torch.randn((n, m), generator=g, device="cuda").masked_fill_((at < first) | (at >= first + kept), -math.inf).to(t)
+    token, logp = torch.empty((n, top), dtype=torch.int32, device="cuda"), torch.empty((n, top), device="cuda")
+    ops.log_probs(x, top_token=token, top_logp=logp)
+    z, want = torch.sort(x.float(), dim=1, descending=True, stable=True)
+    assert torch.equal(token.long(), want[:, :top])
+    assert torch.equal(logp == -math.inf, z[:, :top] == -math.inf)
+    ops.close()

@@ -6,6 +6,7 @@ import gc
 import types
 import weakref
 
+import numpy as np
 import pytest
 
 from paper_2608_14575_amd import hwr, routed
@@ -141,3 +142,20 @@ def test_adamw_is_not_made_under_capture(monkeypatch, log, caller):
     with pytest.raises(hwr.HwrError) as e:
         routed.AdamW(Plan(monkeypatch, log), [torch.ones(4)], [torch.ones(4)], lr=1e-3)
     assert e.value.status == hwr.HWR_ERR_STATE and log == []
+
+
+def test_memory_stays_while_steps_write_it(monkeypatch, log, caller):
+    """A tensor that is given other memory leaves the object its own: steps write what is there, until the object is dropped."""
+    caller.cuda_stream = 0
+    values = [np.ones(4, np.float32) for _ in range(5)]
+    p, g, m, v = (torch.from_numpy(x) for x in values[:4])
+    opt = routed.AdamW(Plan(monkeypatch, log), [p], [g], lr=1e-3, state={"m": [m], "v": [v]})
+    gone = [weakref.ref(x) for x in values[:4]]
+    for t in (p, g, m, v):
+        t.data = torch.from_numpy(values[4])
+    del values[:4], t
+    gc.collect()
+    assert all(r() is not None for r in gone)
+    del opt
+    gc.collect()
+    assert all(r() is None for r in gone)

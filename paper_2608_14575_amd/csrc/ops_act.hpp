@@ -6,7 +6,7 @@
 //   Phi(-a) = exp(-a^2 / 2) R(t), t = 1 / (1 + 0.38 a), a >= 0,
 // with R of five powers of t, fitted here to erfc over 0 <= a <= 14 by least squares reweighted towards
 // the smallest largest relative error (3.6e-5, 2^-14.8; past 14 Phi(-a) is below the smallest
-// fp32 value), and the hardware's exp2 and reciprocal (1 ulp).
+// normal fp32 value), and the hardware's exp2 and reciprocal (1 ulp).
 #pragma once
 
 #include "ops_device.hpp"

@@ -243,7 +243,7 @@ hwr_status hwr_log_probs_grad(hwr_ops *ops, const hwr_log_probs_grad_args *a);
  * 0).  Each is the stored value times its scale.  Zeros (with any finite scales) are a beginning for all.
  * A block of which every value is below 2^-100 becomes zeros.  The roots are rounded without a bias, so
  * their squares have one, and noise: with normal gradients and beta2 0.999 (0.98) v settles 5% (4%) too
- * large on the mean, with a standard deviation of 0.34 (0.30) of itself; 98% of the values' updates are
+ * large on the mean, with a standard deviation of 0.35 (0.30) of itself; 98% of the values' updates are
  * within 0.70 to 1.42 (0.73 to 1.36) of what they should be, their mean 1.4% (1.2%) above.
  * The random numbers are a function of seed, t and the value's number (tensors are numbered
  * one after the other, each from a multiple of 256 on): the same call gives the same bits.

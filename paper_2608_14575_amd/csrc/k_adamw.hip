@@ -11,7 +11,7 @@
 // down with the probability of the remainder.  The noise is a hash of the seed, the step
 // and the value's place.  The root is without a bias then, its square is not: it grows by the variance of the
 // rounding, in a step at most the root's way (half of 1 - b2 of |g^2 / v - 1|) times the codes' distance (an eighth of the root), over the
-// 1 / (1 - b2) steps that v remembers by some 5% of v, with a standard deviation of 0.34.
+// 1 / (1 - b2) steps that v remembers by some 5% of v, with a standard deviation of 0.35.
 //
 // Bound by memory: 28 bytes a value with fp32 states (bf16 without masters 22), 16 with 8 bits (bf16 without masters 10).  A workgroup takes 8
 // blocks of a tensor, a thread 8 values (16 bytes of bf16 at a time), a half-wave a block, so that a scale takes five

@@ -323,7 +323,8 @@ class AdamW:
     it was captured with, but for the contents of the tensors).
 
     As with the operators, torch does not see the writes (no new version of a tensor).  Steps of one object are
-    ordered among each other by the caller, on whatever streams they run."""
+    ordered among each other by the caller, on whatever streams they run.  An object is made, closed and dropped (which
+    waits for the device) while no stream is captured."""
 
     def __init__(self, ops, params, grads, *, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, bits=32, master=False,
                  state=None, steps=0, seed=0):
